@@ -262,8 +262,101 @@ LMHEAD_API int flowrl_tb_loss(const float* logp, const float* logp_ref, const fl
                    void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * Preference loss over the responses of each prompt: paired log-ratios, as in direct preference optimisation and its relatives.
+ *     s_r = sum_{t < len_r} (logp[r,t] - logp_ref[r,t])     (logp_ref NULL: logp alone; mean = 1: divided by len_r; 0 if len_r = 0)
+ * Pairs (a, b) of responses of one prompt with reward[a] > reward[b]: all of them, or with LMHEAD_PAIRS_EXTREMES only the
+ * best and the worst response (of equal rewards the lowest index; a prompt whose rewards are all equal has no pair).  A NaN reward
+ * is in no pair.  For each pair
+ *     u = s_a - s_b,    h = beta u - margin - margin_scale (reward[a] - reward[b])
+ *     LMHEAD_PREF_LOGISTIC  l = -(1 - smoothing) log sigma(h) - smoothing log sigma(-h),   dl/du = beta (smoothing - sigma(-h))
+ *     LMHEAD_PREF_HINGE     l = max(0, 1 - h),                                             dl/du = -beta [h < 1]
+ *     LMHEAD_PREF_SQUARED   l = (h / beta - 1 / (2 beta))^2,                               dl/du = 2 (h / beta - 1 / (2 beta))
+ *     l += nll_coef * (-(1/len_a) sum_t logp[a,t])         (the likelihood of what was preferred)
+ *     loss = sum over pairs of w l,   w = 1 / (P M_p) (weights = 0: mean over prompts of the mean over the prompt's M_p pairs; a prompt
+ *     without pairs contributes 0) or 1 / M (weights = 1: mean over all M pairs)
+ *     g_logp[r,t] = dloss/dlogp[r,t], the sum over all pairs that r is in; 0 on padding.  The reference is a constant.
+ * Sums over a response, the pairs and their sums are evaluated in fp64: u is a small difference of long sums.
+ *   logp, logp_ref float[N]; reward float[R]; len int32[R] (clamped into [0, T]);
+ *   loss float[1] (out; 0 without pairs); g_logp float[N] or NULL (out); ratio float[R] or NULL: s_r (out);
+ *   stats (optional, float[4]): share of the pairs with u > 0, pair-mean beta s_a, pair-mean beta s_b, M.
+ * Limits: those of lmhead_loss_workspace_bytes (P * G <= 65535).  LMHEAD_E_SHAPE for beta <= 0, smoothing outside [0, 1] or with another
+ * loss than the logistic one, a negative nll_coef, a number that is not finite, an unknown selector.
+ */
+enum { LMHEAD_PREF_LOGISTIC = 0, LMHEAD_PREF_HINGE = 1, LMHEAD_PREF_SQUARED = 2 };
+enum { LMHEAD_PAIRS_ALL = 0, LMHEAD_PAIRS_EXTREMES = 1 };
+typedef struct lmhead_preference {
+  int32_t loss;       /* LMHEAD_PREF_*                          */
+  int32_t pairs;      /* LMHEAD_PAIRS_*                         */
+  int32_t mean;       /* 1: s_r is the mean over the tokens      */
+  int32_t weights;    /* 0: per prompt, 1: per pair              */
+  float beta, margin, margin_scale, smoothing, nll_coef;
+  int32_t reserved;   /* must be 0                              */
+} lmhead_preference;
+LMHEAD_API size_t preference_workspace_bytes(int32_t P, int32_t G, int32_t T);
+LMHEAD_API int preference_loss(const lmhead_preference* params, const float* logp, const float* logp_ref, const float* reward,
+                               const int32_t* len, int32_t P, int32_t G, int32_t T, float* loss, float* g_logp, float* ratio,
+                               float* stats, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Rows of a weight matrix by token id, and the gradient of that matrix: the other end of a model whose head is the matrix W above
+ * (tied weights), or an embedding of its own.  R responses of T slots, N = R*T; slot i = r*T + t is valid iff t < len[r].
+ *   embed_fwd:  X[i,:] = scale W[tok[i],:], rounded once to the rows' type; 0 on padded slots
+ *   embed_bwd:  dW[v,:] = scale sum_{valid i, tok[i] = v} gX[i,:]    (fp32; rows of ids that do not occur = 0)
+ * With LMHEAD_FLAG_ACCUM_DW embed_bwd adds to the contents of dW instead, e.g. to what lmhead_logprob_bwd left there; rows of ids
+ * that do not occur are then not touched.  The rows of one id are summed in the order of their slots, in pieces that are joined in a
+ * fixed order: bit-reproducible, whatever ids repeat.
+ *   W    [V x d], row stride ldW, storage type dtype    (in)        tok int32[N]  (in)     len int32[R], or NULL: every slot valid  (in)
+ *   X    [N x d], row stride ldX, storage type rows      (out; what lies between its rows is left as it was)
+ *   gX   [N x d], row stride ldX, storage type rows      (in)
+ *   dW   float [V x d], dense row stride d              (out)
+ * A length outside [0, T] is clamped; an id outside [0, V) on a valid slot gives a row of 0 and adds to no gradient; either sets the
+ * error word of ws (lmhead_check -> LMHEAD_E_RANGE; cleared when a call starts).
+ */
+typedef struct lmhead_embed_desc {
+  int32_t R, T;       /* N = R*T <= 2^31 - 2^20 slots                                           */
+  int32_t d, V;       /* row length (a multiple of 8, at most 65536) and rows of the matrix       */
+  int32_t dtype;      /* LMHEAD_F32 or LMHEAD_BF16: storage type of W                            */
+  int32_t rows;       /* LMHEAD_F32 or LMHEAD_BF16: storage type of X, gX                        */
+  uint32_t flags;     /* LMHEAD_FLAG_ACCUM_DW or 0 (embed_fwd ignores it)                        */
+  int32_t reserved;   /* must be 0                                                               */
+  int64_t ldW, ldX;   /* row strides in elements (>= d, a multiple of 16 bytes)                  */
+} lmhead_embed_desc;
+LMHEAD_API int embed_validate_desc(const lmhead_embed_desc* desc);
+LMHEAD_API size_t embed_workspace_bytes(const lmhead_embed_desc* desc);   /* either call; 0 if the descriptor is invalid */
+LMHEAD_API int embed_fwd(const lmhead_embed_desc* desc, const void* W, const int32_t* tok, const int32_t* len, float scale,
+                         void* X, void* ws, size_t ws_bytes, void* stream);
+LMHEAD_API int embed_bwd(const lmhead_embed_desc* desc, const void* gX, const int32_t* tok, const int32_t* len, float scale,
+                         float* dW, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * The norm over all gradients of a step, and their clipping.
+ *     norm = sqrt(sum over all tensors and elements of g^2)       (squares and sums in fp64: no overflow, no lost small ones)
+ *     c    = min(1, max_norm / (norm + eps)),    out = c g        (in fp32, rounded once to the type of out)
+ * norm[0] = norm; grad_clip also writes norm[1] = c.  As the formulas say, a norm of +inf gives c = 0 and a norm of NaN gives NaN
+ * everywhere: look at norm[0] before the optimiser takes such a step.
+ *   g    host array of `count` tensors (1 .. 65536): device pointer, elements (0 allowed), LMHEAD_F32 or LMHEAD_BF16.  Pointers need
+ *        only their type's alignment; tensors that are not 16-byte aligned are read and written more slowly.
+ *   out  host array of `count` tensors with the same element counts, of either type, or NULL: g is scaled in place (and left
+ *        untouched in memory where c is 1).  An output may be its own input (same pointer, same type); any other overlap
+ *        of an output with an input or an output is refused (LMHEAD_E_SHAPE).
+ *   ws   grad_workspace_bytes() bytes, 256-byte aligned
+ * The arrays are read during the call and not kept; the call may be captured into a graph, which then holds the pointers.
+ * LMHEAD_E_SHAPE also for max_norm < 0 or NaN, for eps < 0 or not finite, for more than 2^37 elements in a tensor.
+ */
+typedef struct lmhead_tensor {
+  void* data;         /* device memory                    */
+  int64_t n;          /* elements                         */
+  int32_t dtype;      /* LMHEAD_F32 or LMHEAD_BF16        */
+  int32_t reserved;   /* must be 0                        */
+} lmhead_tensor;
+LMHEAD_API size_t grad_workspace_bytes(void);
+LMHEAD_API int grad_norm(const lmhead_tensor* g, int32_t count, float* norm, void* ws, size_t ws_bytes, void* stream);
+LMHEAD_API int grad_clip(const lmhead_tensor* g, const lmhead_tensor* out, int32_t count, float max_norm, float eps, float* norm,
+                         void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Synchronises `stream` and returns LMHEAD_OK, LMHEAD_E_RANGE if the last
- * lmhead_logprob_fwd/bwd call that used `ws` saw an out-of-range length or token
+ * lmhead_logprob_fwd/bwd or embed_fwd/bwd call that used `ws` saw an out-of-range length or token
  * id, or LMHEAD_E_HIP if the stream reports an error.  `ws` must be a workspace
  * that has been passed to one of those calls.
  */

@@ -30,7 +30,26 @@ from .binding import (
     lmhead_probe_mfma,
     workspace_region,
     WS_NV, WS_ROW_SLOT, WS_TOK_C, WS_GATHERED_ID,
+    FLAG_ACCUM_DW,
     EXPORTED_SYMBOLS,
+)
+
+from .train import (
+    PreferenceParams,
+    make_preference,
+    preference_workspace_bytes,
+    preference_loss,
+    EmbedDesc,
+    make_embed_desc,
+    embed_validate_desc,
+    embed_workspace_bytes,
+    embed_fwd,
+    embed_bwd,
+    GradList,
+    make_grad_list,
+    grad_workspace_bytes,
+    grad_norm,
+    grad_clip,
 )
 
 from .dynakv import (
@@ -58,5 +77,8 @@ __all__ = [
     "workspace_bytes", "loss_workspace_bytes", "validate_desc",
     "lmhead_logprob_fwd", "lmhead_logprob_fwd_multi", "multi_workspace_bytes", "lmhead_logprob_bwd", "group_advantage", "grpo_loss", "grpo_loss_noalloc",
     "flowrl_tb_loss", "ce_loss", "lmhead_check", "lmhead_timing_enable", "lmhead_timing_read", "EXPORTED_SYMBOLS",
-    "lmhead_probe_mfma", "workspace_region", "WS_NV", "WS_ROW_SLOT", "WS_TOK_C", "WS_GATHERED_ID",
+    "lmhead_probe_mfma", "workspace_region", "WS_NV", "WS_ROW_SLOT", "WS_TOK_C", "WS_GATHERED_ID", "FLAG_ACCUM_DW",
+    "PreferenceParams", "make_preference", "preference_workspace_bytes", "preference_loss",
+    "EmbedDesc", "make_embed_desc", "embed_validate_desc", "embed_workspace_bytes", "embed_fwd", "embed_bwd",
+    "GradList", "make_grad_list", "grad_workspace_bytes", "grad_norm", "grad_clip",
 ]

@@ -19,6 +19,8 @@ EXPORTED_SYMBOLS = [
     "group_advantage",
     "lmhead_loss_workspace_bytes", "grpo_loss", "grpo_loss_noalloc", "flowrl_tb_loss", "ce_loss", "lmhead_check",
     "lmhead_timing_enable", "lmhead_timing_read", "lmhead_workspace_region", "lmhead_probe_mfma",
+    "preference_workspace_bytes", "preference_loss", "embed_validate_desc", "embed_workspace_bytes", "embed_fwd", "embed_bwd",
+    "grad_workspace_bytes", "grad_norm", "grad_clip",
 ]
 
 ERRORS = {

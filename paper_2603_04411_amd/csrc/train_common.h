@@ -1,0 +1,95 @@
+// Internal declarations of the operators around the head in a training step: preference loss, embedding lookup and its gradient,
+// gradient norm and clipping.
+#pragma once
+
+#include "common.h"
+
+namespace lmhead {
+
+// ---- preference loss (lmhead_pref.hip) --------------------------------------------------
+
+struct PrefLayout {
+  int64_t R, nb;         // responses, blocks of kLossSlotsPerBlock slots in one
+  size_t done, sums, rank, part, total;
+};
+static inline PrefLayout pref_layout(int64_t P, int64_t G, int64_t T) {
+  PrefLayout L{};
+  L.R = P * G;
+  L.nb = (T + kLossSlotsPerBlock - 1) / kLossSlotsPerBlock;
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t o = off;
+    off += round_up(bytes, 256);
+    return o;
+  };
+  L.done = take(256);
+  L.sums = take((size_t)(L.R * L.nb) * 2 * sizeof(double));   // [response][block]{log-ratio, log-prob}
+  L.rank = take((size_t)L.R * 2 * sizeof(int32_t));           // [response]{pairs in which it is preferred, best | worst << 1}
+  L.part = take((size_t)L.R * 4 * sizeof(double));            // [response]{loss, u > 0, beta s_a, beta s_b} of those pairs
+  L.total = off;
+  return L;
+}
+hipError_t launch_preference(const lmhead_preference& q, const float* lp, const float* lr, const float* reward, const int32_t* len,
+                             int P, int G, int T, float* loss, float* g, float* ratio, float* stats, char* ws, hipStream_t s);
+
+// ---- embedding (lmhead_embed.hip) -------------------------------------------------------
+
+constexpr int kSortTile = 4096;      // slots per workgroup of a sorting pass
+constexpr int kSortBits = 9;         // digits have at most so many bits
+constexpr int kEmbedChunk = 64;      // sorted slots per unit of the gradient
+
+struct EmbedHeader {
+  int32_t err;      // sticky error bits (kErrLen, kErrTok), where lmhead_check reads them
+  int32_t nv;       // unused; lmhead_check copies it along
+  int32_t nlong;    // ids whose rows span three chunks or more
+  int32_t pad[61];
+};
+static_assert(sizeof(EmbedHeader) == 256, "header is one 256-byte line");
+
+struct EmbedLayout {
+  int64_t N;
+  int bits, passes, digit;   // bits of a key (ids and V, the key of a slot that does not count), sorting passes, bits of a pass
+  int64_t tiles, chunks;
+  size_t hdr, key[2], slot[2], hist, list, part, total;
+};
+static inline EmbedLayout embed_layout(const lmhead_embed_desc* d) {
+  EmbedLayout L{};
+  L.N = (int64_t)d->R * d->T;
+  L.bits = 1;
+  while (((int64_t)d->V >> L.bits) != 0) ++L.bits;
+  L.passes = (L.bits + kSortBits - 1) / kSortBits;
+  L.digit = (L.bits + L.passes - 1) / L.passes;
+  L.tiles = (L.N + kSortTile - 1) / kSortTile;
+  L.chunks = (L.N + kEmbedChunk - 1) / kEmbedChunk;
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t o = off;
+    off += round_up(bytes, 256);
+    return o;
+  };
+  L.hdr = take(sizeof(EmbedHeader));
+  for (int i = 0; i < 2; ++i) L.key[i] = take((size_t)L.N * 4);
+  for (int i = 0; i < 2; ++i) L.slot[i] = take((size_t)L.N * 4);
+  L.hist = take(((size_t)L.tiles << L.digit) * 4 + ((size_t)4 << L.digit));   // [digit][tile], then the totals
+  L.list = take((size_t)L.chunks * 4);
+  L.part = take((size_t)L.chunks * 2 * d->d * 4);              // [chunk]{of an id that began earlier, of one that goes on}[d]
+  L.total = off;
+  return L;
+}
+hipError_t launch_embed_fwd(const lmhead_embed_desc& d, const void* W, const int32_t* tok, const int32_t* len, float scale, void* X,
+                            EmbedHeader* hdr, hipStream_t s);
+hipError_t launch_embed_bwd(const lmhead_embed_desc& d, const void* gX, const int32_t* tok, const int32_t* len, float scale, float* dW,
+                            char* ws, hipStream_t s);
+
+// ---- gradient norm and clipping (lmhead_grad.hip) -----------------------------------------
+
+constexpr int kGradParts = 2048;     // workgroups, each with a partial sum, that one call's norm is shared by (at least one a launch)
+constexpr int kGradTensors = 96;     // tensors whose table one launch carries in its arguments
+constexpr int kGradCount = 65536;    // tensors of one call
+constexpr int64_t kGradMost = 1ll << 37;   // elements of a tensor; kGradTensors times its chunks fit 31 bits
+constexpr int kGradLaunches = (kGradCount + kGradTensors - 1) / kGradTensors;
+static inline size_t grad_ws_bytes() { return (size_t)(kGradParts + kGradLaunches) * sizeof(double) + 256; }
+hipError_t launch_grads(const lmhead_tensor* g, const lmhead_tensor* out, int count, bool clip, float max_norm, float eps, float* norm,
+                        char* ws, hipStream_t s);
+
+}  // namespace lmhead

@@ -1,0 +1,204 @@
+"""embed_fwd and embed_bwd against their oracle: types, strides, lengths, ids that are rare, frequent, repeated around the edges of the
+pieces they are summed in, out of range; what is added to, what is left alone."""
+import numpy as np
+import pytest
+
+from oracle import train_oracle as O
+from tests.harness import np64, to_device
+
+pytestmark = pytest.mark.gpu
+
+EPS = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
+
+
+def types(name):
+    import torch
+    return torch.bfloat16 if name == "bf16" else torch.float32
+
+
+def strided(n, d, ld, dtype, seed):
+    """[n x d] with row stride ld, NaN between the rows; and the whole buffer."""
+    import torch
+    buf = torch.full((n * ld,), float("nan"), dtype=types(dtype), device="cuda")
+    x = buf.as_strided((n, d), (ld, 1))
+    x.copy_(torch.randn(n, d, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda"))
+    return x, buf
+
+
+def ids(V, N, seed, hot=True):
+    r = np.random.default_rng(seed)
+    return (np.minimum(r.zipf(1.2, N), V) - 1 if hot else r.integers(0, V, N)).astype(np.int32)
+
+
+def forward(R, T, d, V, dtype, rows, tok, lens, scale, ldW=None, ldX=None, code=0):
+    import torch
+    import paper_2603_04411_amd as L
+    desc = L.make_embed_desc(R, T, d, V, dtype, rows=rows, ldW=ldW, ldX=ldX)
+    W, _ = strided(V, d, ldW or d, dtype, V + d)
+    X, buf = strided(R * T, d, ldX or d, rows, 5)
+    X.fill_(3.0)
+    ws = torch.full((L.embed_workspace_bytes(desc),), 0xFF, dtype=torch.uint8, device="cuda")
+    L.embed_fwd(desc, W, to_device(tok), None if lens is None else to_device(np.asarray(lens, dtype=np.int32)), scale, X, ws)
+    assert L.lmhead_check(ws) == code
+    want = O.embed_fwd(np64(W), tok, lens, R, T, float(np.float32(scale)))
+    # the product in fp32, then the rows' type
+    got = np64(X)
+    assert np.all(np.abs(got - want) <= (EPS["f32"] + (EPS["bf16"] if rows == "bf16" else 0)) * 1.01 * np.abs(want))
+    if ldX and ldX > d:
+        gap = buf.view(R * T, ldX)[:, d:]
+        assert bool(torch.isnan(gap).all()), "what lies between the rows was written"
+
+
+@pytest.mark.parametrize("dtype,rows", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("R,T,d", [(1, 1, 8), (3, 5, 64), (2, 33, 1000), (1, 7, 520), (5, 1, 4096), (2, 3, 5128)])
+def test_forward(dtype, rows, R, T, d):
+    V = 97
+    tok, lens = ids(V, R * T, R + d), np.random.default_rng(d).integers(0, T + 1, R)
+    forward(R, T, d, V, dtype, rows, tok, lens, 1.0)
+    forward(R, T, d, V, dtype, rows, tok, None, 45.25, ldW=d + 8, ldX=d + 16)
+
+
+def test_forward_of_many_rows():
+    forward(7, 9001, 64, 5000, "bf16", "bf16", ids(5000, 63007, 1), [9001, 0, 1, 9000, 17, 4096, 8192], 8.0)
+    forward(1, 70000, 8, 3, "f32", "bf16", ids(3, 70000, 2, hot=False), None, 0.5)
+
+
+def test_forward_reports_what_is_out_of_range():
+    tok = np.array([0, 5, -1, 4, 99, 3], dtype=np.int32)
+    forward(2, 3, 16, 5, "bf16", "bf16", tok, [3, 3], 1.0, code=-6)
+    forward(2, 3, 16, 5, "bf16", "bf16", np.array([0, 4, -1, 4, 99, 3], dtype=np.int32), [2, 1], 1.0)      # only on padding: no fault
+    forward(2, 3, 16, 5, "f32", "f32", np.array([0, 1, 2, 4, 4, 3], dtype=np.int32), [4, -1], 1.0, code=-6)
+    forward(2, 3, 16, 5, "f32", "f32", np.array([0, 1, 2, 4, 4, 3], dtype=np.int32), [3, 0], 1.0)
+
+
+def test_rows_of_infinities_come_through():
+    import torch
+    import paper_2603_04411_amd as L
+    W = torch.full((3, 8), float("inf"), device="cuda")
+    W[1] = float("nan")
+    W[2] = -0.0
+    desc = L.make_embed_desc(1, 4, 8, 3, "f32")
+    X, ws = torch.ones(4, 8, device="cuda"), torch.empty(L.embed_workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+    L.embed_fwd(desc, W, torch.tensor([0, 1, 2, 1], dtype=torch.int32, device="cuda"), torch.tensor([3], dtype=torch.int32, device="cuda"), 2.0, X, ws)
+    assert bool((X[0] == float("inf")).all()) and bool(X[1].isnan().all()) and bool((X[2] == 0).all()) and bool((X[3] == 0).all())
+
+
+def backward(R, T, d, V, rows, tok, lens, scale=1.5, ldX=None, add=False, code=0, g=None, ws=None):
+    import torch
+    import paper_2603_04411_amd as L
+    desc = L.make_embed_desc(R, T, d, V, "bf16", rows=rows, ldX=ldX, flags=L.FLAG_ACCUM_DW if add else 0)
+    if g is None:
+        g, _ = strided(R * T, d, ldX or d, rows, N_SEED + R + T)
+    dW = torch.randn(V, d, generator=torch.Generator(device="cuda").manual_seed(3), device="cuda")
+    base = dW.clone()
+    if ws is None:
+        ws = torch.full((L.embed_workspace_bytes(desc),), 0xFF, dtype=torch.uint8, device="cuda")
+    dt, dl = to_device(tok), None if lens is None else to_device(np.asarray(lens, dtype=np.int32))
+    L.embed_bwd(desc, g, dt, dl, scale, dW, ws)
+    assert L.lmhead_check(ws) == code
+    ok = O.valid_slots(tok, lens, R, T, V)
+    want, size = O.embed_bwd(np64(g), tok, lens, R, T, V, float(np.float32(scale)), np64(base) if add else None)
+    count = np.bincount(np.asarray(tok)[ok], minlength=V)[:, None]
+    # `count` - 1 additions, the scale, the addition to what was there: each off by half a step of at most the sum of magnitudes
+    err = np.abs(np64(dW) - want)
+    assert np.all(err <= 1.01 * (count + 1) * 2.0 ** -24 * size + 1e-40), float((err / np.maximum(size, 1e-30)).max())
+    absent = torch.from_numpy(count[:, 0] == 0).cuda()
+    assert torch.equal(dW[absent], base[absent] if add else torch.zeros_like(base[absent]))
+    again = base.clone()
+    L.embed_bwd(desc, g, dt, dl, scale, again, ws)
+    assert torch.equal(again, dW), "not the same bits twice"
+    return dW
+
+
+N_SEED = 100
+
+
+@pytest.mark.parametrize("rows", ["bf16", "f32"])
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("R,T,d,V", [(1, 1, 8, 1), (1, 1, 64, 300), (3, 5, 64, 7), (2, 33, 1000, 50), (4, 16, 520, 1), (1, 64, 256, 64),
+                                     (1, 65, 512, 2), (2, 200, 136, 511), (2, 200, 136, 512), (2, 200, 136, 513), (3, 700, 72, 40)])
+def test_backward(rows, add, R, T, d, V):
+    backward(R, T, d, V, rows, ids(V, R * T, T), np.random.default_rng(V).integers(0, T + 1, R), add=add, ldX=d + 8 if add else None)
+    backward(R, T, d, V, rows, ids(V, R * T, T + 1, hot=False), None, add=not add)
+
+
+@pytest.mark.parametrize("piece", [1, 7, 8, 9, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 191, 192, 193, 255, 256, 257, 1000])
+def test_ids_that_end_around_the_edges_of_the_pieces(piece):
+    # id 0 moves the others off the edges, each id then has `piece` slots, the last one takes the rest
+    for lead in (0, 1, 31, 63):
+        tok = np.concatenate([np.zeros(lead, dtype=np.int32), 1 + np.arange(1800 - lead, dtype=np.int32) // piece])
+        V = int(tok.max()) + 2
+        perm = np.random.default_rng(piece).permutation(tok.size)
+        backward(1, tok.size, 16, V, "f32" if lead else "bf16", tok[perm].astype(np.int32), None, add=lead == 1)
+
+
+# more than one sorting tile, ids of one, two and three digits, one id everywhere
+@pytest.mark.parametrize("R,T,V,hot", [(1, 4096, 400, True), (1, 4097, 400, True), (3, 4000, 200000, False), (2, 9000, 300000, True),
+                                       (1, 12000, 1, False), (5, 3001, 2, False)])
+def test_backward_of_many_rows(R, T, V, hot):
+    lens = np.random.default_rng(R).integers(T // 2, T + 1, R)
+    backward(R, T, 8, V, "bf16", ids(V, R * T, 9, hot), lens, add=True)
+    backward(R, T, 24, V, "f32", ids(V, R * T, 9, hot), None)
+
+
+def test_backward_of_nothing():
+    for add in (False, True):
+        backward(3, 50, 64, 20, "bf16", ids(20, 150, 1), [0, 0, 0], add=add)
+        backward(1, 6000, 64, 20, "bf16", ids(20, 6000, 1), [0], add=add)
+
+
+def test_backward_reports_what_is_out_of_range():
+    tok = np.array([0, 5, -1, 4, 99, 3, -(1 << 31), (1 << 31) - 1], dtype=np.int32)
+    for add in (False, True):
+        backward(2, 4, 16, 5, "bf16", tok, [4, 4], add=add, code=-6)
+        backward(2, 4, 16, 5, "bf16", tok, [1, 1], add=add, code=-6)      # the second response's only id is 99
+        backward(2, 4, 16, 5, "bf16", tok, [1, 0], add=add)
+        backward(2, 4, 16, 5, "bf16", np.abs(tok) % 5, [5, -3], add=add, code=-6)
+
+
+def test_padded_gradients_do_not_matter():
+    import torch
+    R, T, d, V = 3, 40, 64, 9
+    lens = [40, 0, 11]
+    g = torch.randn(R * T, d, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    pad = torch.tensor([i % T >= lens[i // T] for i in range(R * T)], device="cuda")
+    clean = backward(R, T, d, V, "f32", ids(V, R * T, 4), lens, g=g.masked_fill(pad[:, None], 0.0))
+    g[pad] = float("nan")
+    import paper_2603_04411_amd as L
+    desc = L.make_embed_desc(R, T, d, V, "f32")
+    dW, ws = torch.empty(V, d, device="cuda"), torch.empty(L.embed_workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+    L.embed_bwd(desc, g, to_device(ids(V, R * T, 4)), torch.tensor(lens, dtype=torch.int32, device="cuda"), 1.5, dW, ws)
+    assert torch.equal(dW, clean)
+
+
+def test_a_workspace_of_a_larger_batch_serves():
+    import torch
+    import paper_2603_04411_amd as L
+    big = L.make_embed_desc(9, 5000, 64, 700, "bf16")
+    ws = torch.full((L.embed_workspace_bytes(big),), 0xFF, dtype=torch.uint8, device="cuda")
+    for R, T, d, V in ((9, 5000, 64, 700), (1, 3, 64, 700), (2, 4100, 64, 700), (1, 300, 8, 5)):
+        backward(R, T, d, V, "bf16", ids(V, R * T, T), None, add=T % 2 == 1, ws=ws)
+
+
+def test_offsets_beyond_32_bits():
+    import torch
+    import paper_2603_04411_amd as L
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("needs 60 GB")
+    # the last rows of a matrix and of a batch that are larger than 4 GiB (8.6 and 17.2 GB)
+    V, d, N = 1 << 18, 8192, (1 << 18) + 3
+    W = torch.zeros(V, d, device="cuda")
+    W[-1] = torch.arange(d, device="cuda")
+    desc = L.make_embed_desc(1, N, d, V, "f32", rows="f32")
+    tok = torch.zeros(N, dtype=torch.int32, device="cuda")
+    tok[-2:] = V - 1
+    X = torch.full((N, d), 5.0, device="cuda")
+    ws = torch.empty(L.embed_workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+    L.embed_fwd(desc, W, tok, None, 2.0, X, ws)
+    assert L.lmhead_check(ws) == 0
+    assert torch.equal(X[-1], 2 * W[-1]) and torch.equal(X[-2], 2 * W[-1]) and not bool(X[:-2].any())
+    X[:-2] = 0
+    X[1] = 1.0
+    L.embed_bwd(desc, X, tok, None, 1.0, W, ws)
+    assert L.lmhead_check(ws) == 0
+    assert torch.equal(W[-1], 2 * X[-1]) and bool((W[0] == 1).all()) and not bool(W[1:-1].any())

@@ -1,0 +1,152 @@
+"""preference_loss against its oracle: every loss, pairing and weighting, lengths from none to several blocks, groups of one to
+hundreds, rewards that tie or are no numbers, values in masked places that must not matter."""
+import numpy as np
+import pytest
+
+from oracle import train_oracle as O
+from tests.harness import np64, to_device
+
+pytestmark = pytest.mark.gpu
+
+EPS = 2.0 ** -24
+
+
+def run(q, logp, ref, reward, lens, P, G, T, outs=True, ws=None):
+    import torch
+    import paper_2603_04411_amd as L
+    R, N = P * G, P * G * T
+    loss, g = torch.full((1,), 7.0, device="cuda"), torch.full((N,), 7.0, device="cuda")
+    ratio, stats = torch.full((R,), 7.0, device="cuda"), torch.full((4,), 7.0, device="cuda")
+    if ws is None:
+        ws = torch.full((L.preference_workspace_bytes(P, G, T),), 0xFF, dtype=torch.uint8, device="cuda")
+    L.preference_loss(q, logp, ref, reward, lens, P, G, T, loss, g if outs else None, ratio if outs else None, stats if outs else None, ws)
+    torch.cuda.synchronize()
+    return loss, g, ratio, stats
+
+
+def inputs(P, G, T, seed, lens=None, reward=None):
+    r = np.random.default_rng(seed)
+    R = P * G
+    lens = r.integers(0, T + 1, R) if lens is None else np.asarray(lens)
+    reward = r.integers(0, 5, R) / 4 if reward is None else reward
+    logp = (-12 * r.random(R * T) ** 3).astype(np.float32)
+    ref = (logp + 0.2 * r.standard_normal(R * T)).astype(np.float32)
+    # what padding holds must not matter
+    pad = (np.arange(T)[None, :] >= np.clip(lens, 0, T)[:, None]).reshape(-1)
+    logp[pad] = np.resize(np.array([np.nan, np.inf, -np.inf, 1e38], dtype=np.float32), int(pad.sum()))
+    ref[pad] = np.nan
+    return logp, ref, np.asarray(reward, dtype=np.float32), lens.astype(np.int32)
+
+
+def check(P, G, T, seed, lens=None, reward=None, use_ref=True, **kw):
+    import paper_2603_04411_amd as L
+    logp, ref, rw, lens = inputs(P, G, T, seed, lens, reward)
+    ref = ref if use_ref else None
+    q = L.make_preference(loss=kw.get("loss", "logistic"), pairs="extremes" if kw.get("extremes") else "all", mean=kw.get("mean", False),
+                          weights="pair" if kw.get("per_pair") else "prompt",
+                          **{k: kw[k] for k in ("beta", "margin", "margin_scale", "smoothing", "nll_coef") if k in kw})
+    got = run(q, to_device(logp), None if ref is None else to_device(ref), to_device(rw), to_device(lens), P, G, T)
+    # the parameters are given in fp32
+    okw = {k: float(np.float32(v)) if k in ("beta", "margin", "margin_scale", "smoothing", "nll_coef") else v for k, v in kw.items()}
+    okw.setdefault("beta", float(np.float32(0.1)))
+    want = O.preference_loss(logp, ref, rw, lens, P, G, T, **okw)
+    # fp64 throughout and one rounding to fp32: half a step, and what fp64 sums of values up to 12 T leave after cancellation
+    tiny = 1e-13 * max(1.0, 12.0 * T * okw["beta"]) * (1 if kw.get("loss") != "squared" else 12.0 * T)
+    for name, a, b in zip(("loss", "g_logp", "ratio", "stats"), got, want):
+        a, b = np64(a).reshape(-1), np.asarray(b, dtype=np.float64).reshape(-1)
+        assert np.all(np.abs(a - b) <= 1.01 * EPS * np.abs(b) + tiny + 1e-12 * (name == "ratio")), (name, float(np.abs(a - b).max()))
+    return got, q
+
+
+@pytest.mark.parametrize("loss", ["logistic", "hinge", "squared"])
+@pytest.mark.parametrize("extremes", [False, True])
+@pytest.mark.parametrize("mean,per_pair", [(False, False), (True, False), (False, True), (True, True)])
+def test_every_form(loss, extremes, mean, per_pair):
+    for seed, use_ref in ((1, True), (2, False)):
+        check(5, 4, 37, seed, use_ref=use_ref, loss=loss, extremes=extremes, mean=mean, per_pair=per_pair, beta=2.0 if mean else 0.3,
+              margin=0.25, margin_scale=0.5 * seed, smoothing=0.1 if loss == "logistic" else 0.0, nll_coef=0.3)
+
+
+@pytest.mark.parametrize("P,G,T", [(1, 1, 1), (1, 2, 1), (2, 2, 2), (1, 2, 2047), (1, 2, 2048), (1, 2, 2049), (3, 3, 4097), (300, 2, 5),
+                                   (1, 63, 3), (1, 64, 3), (1, 65, 3), (2, 255, 2), (1, 257, 2), (2, 300, 1), (1, 700, 2), (17, 16, 130)])
+def test_sizes(P, G, T):
+    check(P, G, T, 11, mean=G > 2, per_pair=T % 2 == 0, nll_coef=0.1)
+    check(P, G, T, 12, extremes=True, loss="squared", margin=0.1, use_ref=False)
+
+
+def test_lengths_of_none_one_and_out_of_range():
+    check(2, 3, 9, 3, lens=[0, 0, 0, 0, 1, 9], nll_coef=0.5)
+    check(2, 3, 9, 3, lens=[0, 0, 0, 0, 1, 9], mean=True)
+    check(2, 3, 9, 4, lens=[-5, 10, 1 << 30, -(1 << 31), 3, 9])          # clamped
+
+
+def test_rewards_that_tie_and_are_no_numbers():
+    nan, inf = float("nan"), float("inf")
+    for extremes in (False, True):
+        for per_pair in (False, True):
+            kw = dict(extremes=extremes, per_pair=per_pair)
+            got, _ = check(2, 3, 5, 5, reward=[1, 1, 1, 2, 2, 2], **kw)          # no pair at all
+            assert float(got[0]) == 0.0 and not got[1].any() and not got[3].any()
+            check(2, 3, 5, 6, reward=[1, 1, 1, 2, 1, 2], **kw)
+            check(2, 3, 5, 7, reward=[nan, 1, 0, nan, nan, nan], **kw)
+            check(2, 4, 5, 8, reward=[nan, 1, nan, 1, 0, inf, -inf, inf], **kw)
+
+
+def test_a_token_of_probability_zero():
+    import paper_2603_04411_amd as L
+    P, G, T = 1, 2, 3
+    logp = np.array([-1, -np.inf, -1, -1, -2, -3], dtype=np.float32)
+    q = L.make_preference(beta=0.5)
+    d = [to_device(a) for a in (logp, np.array([1, 0], dtype=np.float32), np.array([3, 3], dtype=np.int32))]
+    loss, g, ratio, stats = run(q, d[0], None, d[1], d[2], P, G, T)
+    assert float(loss) == np.inf and ratio.tolist() == [-np.inf, -6.0] and g.tolist() == [-0.5] * 3 + [0.5] * 3
+    # a NaN that counts is seen in the loss
+    for kind in ("logistic", "hinge", "squared"):
+        logp[1] = np.nan
+        loss, *_ = run(L.make_preference(loss=kind), to_device(logp), None, d[1], d[2], P, G, T)
+        assert np.isnan(float(loss))
+
+
+def test_far_apart_responses_neither_overflow_nor_vanish():
+    import paper_2603_04411_amd as L
+    lens, rw = to_device(np.array([8, 8], dtype=np.int32)), to_device(np.array([1, 0], dtype=np.float32))
+    for sign in (1.0, -1.0):
+        logp = np.concatenate([np.full(8, -100.0 if sign < 0 else -1e-3), np.full(8, -1e-3 if sign < 0 else -100.0)]).astype(np.float32)
+        want = O.preference_loss(logp, None, [1, 0], [8, 8], 1, 2, 8, beta=1.0)
+        loss, g, _, _ = run(L.make_preference(beta=1.0), to_device(logp), None, rw, lens, 1, 2, 8)
+        assert abs(float(loss) - want[0]) <= 1.01 * EPS * abs(want[0]) + 1e-45      # e^-800 is 0 in fp32
+        assert np.all(np.abs(np64(g) - want[1]) <= 1.01 * EPS * np.abs(want[1]) + 1e-45)
+
+
+def test_the_same_bits_each_time_and_with_fewer_outputs():
+    import torch
+    import paper_2603_04411_amd as L
+    P, G, T = 7, 5, 2100
+    a = [to_device(x) for x in inputs(P, G, T, 9)]
+    q = L.make_preference(weights="pair", nll_coef=0.2)
+    first = run(q, a[0], a[1], a[2], a[3], P, G, T)
+    for _ in range(3):
+        assert all(torch.equal(x, y) for x, y in zip(run(q, a[0], a[1], a[2], a[3], P, G, T), first))
+    loss, g, ratio, stats = run(q, a[0], a[1], a[2], a[3], P, G, T, outs=False)
+    assert torch.equal(loss, first[0]) and bool((g == 7).all()) and bool((ratio == 7).all()) and bool((stats == 7).all())
+
+
+def test_the_gradient_is_the_difference_quotient_of_the_loss():
+    import paper_2603_04411_amd as L
+    P, G, T = 2, 3, 4
+    logp, ref, rw, lens = inputs(P, G, T, 21, lens=[4, 2, 3, 1, 4, 4], reward=[0, 1, 2, 1, 0, 3])
+    q = L.make_preference(beta=0.5, smoothing=0.1, nll_coef=0.25)
+    d = [to_device(x) for x in (logp, ref, rw, lens)]
+    g = np64(run(q, d[0], d[1], d[2], d[3], P, G, T)[1])
+    for i in range(P * G * T):
+        if i % T >= lens[i // T]:
+            assert g[i] == 0
+            continue
+        step, at = 2.0 ** -5, []
+        for sign in (1, -1):
+            lp = logp.copy()
+            lp[i] += np.float32(sign * step)
+            at.append((float(run(q, to_device(lp), d[1], d[2], d[3], P, G, T)[0]), float(lp[i])))
+        slope = (at[0][0] - at[1][0]) / (at[0][1] - at[1][1])
+        # losses below 4 are known to 2^-23 and divided by 2^-4; the third derivative of the logistic loss is at most beta^3 / 8, times step^2 / 6
+        assert abs(slope - g[i]) <= 2 * 2.0 ** -23 * 4 / (2 * step) + 0.5 ** 3 / 8 * step ** 2 / 6 + 1e-7

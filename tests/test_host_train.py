@@ -1,0 +1,181 @@
+"""Host side of preference loss, embedding and gradient clipping: argument validation returns the documented codes before anything is
+launched, workspaces grow as documented, the binding refuses tensors that are not what the call needs."""
+import ctypes as C
+import os
+
+import pytest
+
+import paper_2603_04411_amd as L
+from paper_2603_04411_amd import train as B
+
+P_ = 0x10000   # never dereferenced: every call below has to fail in host-side validation
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(L.library_path()):
+        from paper_2603_04411_amd.build import build_library
+        build_library()
+    return B._lib()
+
+
+def test_structures_match_the_c_layout():
+    assert C.sizeof(B.PreferenceParams) == 40 and C.sizeof(B._Tensor) == 24
+    assert C.sizeof(B.EmbedDesc) == 8 * 4 + 2 * 8 and B.EmbedDesc.ldW.offset == 32
+
+
+def test_preference_refusals(lib):
+    need = L.preference_workspace_bytes(2, 4, 32)
+    assert need > 0 and L.preference_workspace_bytes(0, 4, 32) == 0 and L.preference_workspace_bytes(65536, 1, 1) == 0
+
+    def call(q=None, ws=P_, nbytes=need, P=2, null=None, **kw):
+        q = L.make_preference(**kw) if q is None else q
+        p = [P_, P_, P_, P_]
+        if null is not None:
+            p[null] = None
+        return lib.preference_loss(C.byref(q), p[0], None, p[1], p[2], P, 4, 32, p[3], None, None, None, ws, nbytes, None)
+    assert lib.preference_loss(None, P_, None, P_, P_, 2, 4, 32, P_, None, None, None, P_, need, None) == -1
+    for i in range(4):
+        assert call(null=i) == -1
+    assert call(ws=None) == -1 and call(ws=P_ + 8) == -4 and call(nbytes=need - 1) == -5 and call(P=-1) == -2 and call(P=1 << 20) == -2
+    nan, inf = float("nan"), float("inf")
+    for kw in (dict(loss=3), dict(loss=-1), dict(pairs=2), dict(weights=2), dict(mean=2), dict(beta=0.0), dict(beta=-1.0), dict(beta=nan),
+               dict(beta=inf), dict(margin=inf), dict(margin_scale=nan), dict(smoothing=-0.1), dict(smoothing=1.1), dict(smoothing=nan),
+               dict(smoothing=0.1, loss="hinge"), dict(smoothing=0.1, loss="squared"), dict(nll_coef=-1.0), dict(nll_coef=inf)):
+        assert call(**kw) == -2, kw
+    q = L.make_preference()
+    q.reserved = 1
+    assert call(q=q) == -2
+
+
+def test_embed_refusals(lib):
+    kw0 = dict(R=3, T=7, d=64, V=100, dtype="bf16")
+    ok = L.make_embed_desc(**kw0)
+    need = L.embed_workspace_bytes(ok)
+    assert L.embed_validate_desc(ok) == 0 and need > 0 and lib.embed_validate_desc(None) == -1
+    for change, code in [(dict(R=0), -2), (dict(T=0), -2), (dict(d=0), -2), (dict(d=60), -2), (dict(V=0), -2), (dict(d=65544), -2),
+                         (dict(dtype=2), -3), (dict(rows=3), -3), (dict(flags=1), -3), (dict(flags=8), -3), (dict(ldW=56), -2),
+                         (dict(ldX=63), -2), (dict(ldW=68), -4), (dict(ldX=66), -4), (dict(rows="f32", ldX=66), -4),
+                         (dict(R=1 << 16, T=1 << 15), -2), (dict(V=(1 << 31) - 1), -2), (dict(ldW=1 << 41), -2)]:
+        d = L.make_embed_desc(**{**kw0, **change})
+        assert L.embed_validate_desc(d) == code, change
+        assert L.embed_workspace_bytes(d) == 0
+        assert lib.embed_fwd(C.byref(d), P_, P_, P_, 1.0, P_, P_, 1 << 40, None) == code
+        assert lib.embed_bwd(C.byref(d), P_, P_, P_, 1.0, P_, P_, 1 << 40, None) == code
+    d = L.make_embed_desc(**kw0)
+    d.reserved = 5
+    assert L.embed_validate_desc(d) == -2
+    assert L.embed_validate_desc(L.make_embed_desc(**{**kw0, "rows": "f32", "ldX": 68})) == 0
+    assert L.embed_validate_desc(L.make_embed_desc(1, (1 << 31) - (1 << 20), 8, 100, "f32")) == 0
+    for call in (lib.embed_fwd, lib.embed_bwd):
+        d = C.byref(ok)
+        assert call(d, None, P_, P_, 1.0, P_, P_, need, None) == -1
+        assert call(d, P_, None, P_, 1.0, P_, P_, need, None) == -1
+        assert call(d, P_, P_, P_, 1.0, None, P_, need, None) == -1
+        assert call(d, P_, P_, P_, 1.0, P_, None, need, None) == -1
+        assert call(d, P_ + 8, P_, P_, 1.0, P_, P_, need, None) == -4
+        assert call(d, P_, P_, P_, 1.0, P_ + 4, P_, need, None) == -4
+        assert call(d, P_, P_, P_, 1.0, P_, P_ + 16, need, None) == -4
+        assert call(d, P_, P_, P_, 1.0, P_, P_, need - 1, None) == -5
+
+
+def test_embed_workspaces_of_large_batches_serve_smaller_ones():
+    for d, V in ((8, 1), (64, 511), (64, 512), (1024, 32000), (4096, 151936)):
+        sizes = [L.embed_workspace_bytes(L.make_embed_desc(1, n, d, V, "bf16")) for n in (1, 2, 63, 64, 65, 1000, 4096, 4097, 30000, 500000)]
+        assert sizes == sorted(sizes) and sizes[0] > 0
+
+
+def _tensors(*spans):
+    """(address, elements, dtype) each."""
+    a = (B._Tensor * len(spans))()
+    for i, s in enumerate(spans):
+        a[i] = B._Tensor(s[0], s[1], s[2] if len(s) > 2 else 0, 0)
+    return a
+
+
+def test_gradient_refusals(lib):
+    need = L.grad_workspace_bytes()
+    two = _tensors((P_, 100), (P_ + 4096, 100))
+    norm, clip = lib.grad_norm, lib.grad_clip
+    assert norm(None, 2, P_, P_, need, None) == -1 and norm(two, 2, None, P_, need, None) == -1 and norm(two, 2, P_, None, need, None) == -1
+    assert norm(two, 0, P_, P_, need, None) == -2 and norm(two, 65537, P_, P_, need, None) == -2
+    assert norm(two, 2, P_, P_ + 8, need, None) == -4 and norm(two, 2, P_, P_, need - 1, None) == -5
+    for t, code in [((P_, -1), -2), ((P_, (1 << 37) + 1), -2), ((P_, 4, 5), -3), ((None, 4), -1), ((P_ + 2, 4), -4), ((P_ + 1, 4, 1), -4)]:
+        assert norm(_tensors((P_, 1), t), 2, P_, P_, need, None) == code, t
+        assert clip(_tensors((P_, 1), t), None, 2, 1.0, 0.0, P_, P_, need, None) == code, t
+    bad = _tensors((P_, 4))
+    bad[0].reserved = 1
+    assert norm(bad, 1, P_, P_, need, None) == -2
+    for mx, eps in ((-1.0, 0.0), (float("nan"), 0.0), (1.0, -1.0), (1.0, float("inf")), (1.0, float("nan"))):
+        assert clip(two, None, 2, mx, eps, P_, P_, need, None) == -2
+
+
+def test_outputs_of_clipping_have_to_lie_apart(lib):
+    need = L.grad_workspace_bytes()
+
+    def code(g, out):
+        # a workspace that is too small is found before the overlap: pass it as large enough, and never reach a launch
+        return lib.grad_clip(g, out, len(g), 1.0, 0.0, P_, P_, need, None)
+    assert code(_tensors((P_, 100), (P_ + 396, 100)), None) == -2                                   # in place, twice the same element
+    assert code(_tensors((P_, 100), (P_, 100)), None) == -2
+    far = 1 << 24
+    g = _tensors((P_, 100), (P_ + 400, 100))
+    assert code(g, _tensors((far, 100), (far + 396, 100))) == -2                                    # output on output
+    assert code(g, _tensors((far, 100), (P_ + 396, 100))) == -2                                     # output on another's input
+    assert code(g, _tensors((P_ + 4, 99), (far, 100))) == -2                                        # other counts
+    assert code(g, _tensors((P_ + 4, 100), (far, 100))) == -2                                       # its own input, shifted
+    assert code(g, _tensors((P_, 100, 1), (far, 100))) == -2                                        # its own input, another type
+    assert code(g, _tensors((P_ + 400, 100), (P_, 100))) == -2                                      # exchanged
+    many = _tensors(*[(far + 64 * i, 16) for i in range(1000)], (far + 64 * 500 + 60, 1))
+    assert code(many, None) == -2
+    inside = _tensors((far, 1000), (P_, 4))
+    assert code(inside, _tensors((1 << 26, 1000), (far + 2000, 4))) == -2                           # an output inside a long input
+
+
+def test_binding_refuses_what_the_call_cannot_take():
+    import torch
+    cpu = torch.zeros(64)
+    q = L.make_preference()
+    with pytest.raises(ValueError):
+        L.make_grad_list([cpu])
+    with pytest.raises((ValueError, RuntimeError, AssertionError)):
+        L.preference_loss(q, cpu, None, cpu, cpu, 1, 2, 4, cpu, None, None, None, cpu)
+    with pytest.raises(ValueError):
+        B._arg(cpu, "x", torch.float32, 4, 0)
+    # what a device tensor is asked, on stand-ins
+    class Fake:
+        is_cuda, dtype = True, torch.float32
+
+        def __init__(self, shape, strides, device=0):
+            self.shape, self.strides, self.device_ = shape, strides, device
+
+        def get_device(self): return self.device_
+        def dim(self): return len(self.shape)
+        def numel(self):
+            n = 1
+            for s in self.shape:
+                n *= s
+            return n
+        def stride(self, i): return self.strides[i]
+        def is_contiguous(self):
+            want = 1
+            for s, st in zip(reversed(self.shape), reversed(self.strides)):
+                if s != 1 and st != want:
+                    return False
+                want *= s
+            return True
+        def data_ptr(self): return 4096
+    f32 = torch.float32
+    assert B._arg(Fake((8,), (1,)), "x", f32, 8, 0) == 4096
+    for t, n in ((Fake((8,), (1,), 1), 8), (Fake((8,), (1,)), 9), (Fake((8,), (2,)), 8)):
+        with pytest.raises(ValueError):
+            B._arg(t, "x", f32, n, 0)
+    with pytest.raises(ValueError):
+        B._arg(Fake((8,), (1,)), "x", torch.bfloat16, 8, 0)
+    assert B._rows(Fake((4, 8), (16, 1)), "x", f32, 4, 8, 16, 0) == 4096
+    assert B._rows(Fake((4, 8), (8, 1)), "x", f32, 4, 8, 8, 0) == 4096
+    assert B._rows(Fake((32,), (1,)), "x", f32, 4, 8, 8, 0) == 4096
+    for t, rows, ld, dev in ((Fake((4, 8), (16, 1)), 5, 16, 0), (Fake((4, 8), (16, 1)), 4, 24, 0), (Fake((4, 8), (1, 4)), 4, 8, 0),
+                             (Fake((4, 8), (16, 1)), 4, 8, 0), (Fake((4, 8), (8, 1)), 4, 16, 0), (Fake((4, 8), (16, 1)), 4, 16, 1)):
+        with pytest.raises(ValueError):
+            B._rows(t, "x", f32, rows, 8, ld, dev)
