@@ -54,14 +54,14 @@ struct Batch {
 };
 
 // Id of a slot, V where it does not count; error bits of what it met.
-__device__ inline uint32_t id_of(const Batch& b, int64_t i, int& err) {
-  const int r = (int)((uint32_t)i / (uint32_t)b.T), t = (int)((uint32_t)i % (uint32_t)b.T);
+__device__ inline uint32_t id_of(const Batch& b, uint32_t i, int& err) {
+  const uint32_t r = i / (uint32_t)b.T;
   int n = b.T;
   if (b.len) {
     n = b.len[r];
     if (n < 0 || n > b.T) err |= kErrLen;
   }
-  if (t >= n) return b.V;
+  if ((int)(i - r * (uint32_t)b.T) >= n) return b.V;
   const int v = b.tok[i];
   if (v < 0 || v >= b.V) {
     err |= kErrTok;
@@ -70,178 +70,73 @@ __device__ inline uint32_t id_of(const Batch& b, int64_t i, int& err) {
   return v;
 }
 
-__global__ void embed_clear_kernel(EmbedHeader* hdr) {
-  hdr->err = 0;
-  hdr->nlong = 0;
+__device__ inline int wave_or(int x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x |= __shfl_xor(x, o);
+  return x;
 }
 
-// A wavefront per row.
+// Error bits of all slots, by one workgroup of 256 threads, into the header.
+__device__ inline void report_all(const Batch& b, EmbedHeader* hdr) {
+  __shared__ int bits[4];
+  int err = 0;
+  for (uint32_t i = threadIdx.x; i < (uint32_t)b.R * (uint32_t)b.T; i += 256) id_of(b, i, err);
+  err = wave_or(err);
+  if ((threadIdx.x & 63) == 0) bits[threadIdx.x >> 6] = err;
+  __syncthreads();
+  if (threadIdx.x == 0) hdr->err = bits[0] | bits[1] | bits[2] | bits[3];
+}
+
+__global__ void embed_clear_kernel(EmbedHeader* hdr) { hdr->err = 0; }
+
+// 2^lanes neighbouring lanes per row.  Of a batch of few slots the last workgroup reports for all (`reports`); otherwise the header
+// has been cleared, and whoever meets an error adds it.
 template <typename TW, typename TX>
 __global__ __launch_bounds__(256) void embed_fwd_kernel(Batch b, const TW* __restrict__ W, int64_t ldW, int d, float scale,
-                                                        TX* __restrict__ X, int64_t ldX, EmbedHeader* hdr) {
-  const int lane = threadIdx.x & 63;
-  const int64_t N = (int64_t)b.R * b.T;
-  for (int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); i < N; i += (int64_t)gridDim.x * 4) {
+                                                        TX* __restrict__ X, int64_t ldX, EmbedHeader* hdr, int lanes, bool reports) {
+  constexpr int U = 4;
+  if (reports && blockIdx.x == gridDim.x - 1) return report_all(b, hdr);
+  const uint32_t N = (uint32_t)b.R * (uint32_t)b.T, step = (gridDim.x - reports) * (256u >> lanes);
+  const int in_row = threadIdx.x & ((1 << lanes) - 1), width = 8 << lanes;
+  for (uint64_t i = blockIdx.x * (256u >> lanes) + (threadIdx.x >> lanes); i < N; i += step) {
     int err = 0;
-    const uint32_t v = id_of(b, i, err);
-    if (err && lane == 0) atomicOr(&hdr->err, err);
-    for (int c = lane * 8; c < d; c += 512) {
-      float x[8] = {};
-      if (v < (uint32_t)b.V) {
-        Row8<TW> w;
-        w.load(W + v * ldW + c);
-        w.get(x);
+    const uint32_t v = id_of(b, (uint32_t)i, err);
+    if (!reports && err && in_row == 0) atomicOr(&hdr->err, err);
+    const bool valid = v < (uint32_t)b.V;
+    const TW* w = W + (int64_t)(valid ? v : 0) * ldW;
+    TX* x = X + (int64_t)i * ldX;
+    for (int c0 = in_row * 8; c0 < d; c0 += width * U) {
+      Row8<TW> in[U];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] *= scale;
-      }
-      Row8<TX>::store(X + i * ldX + c, x);
+      for (int u = 0; u < U; ++u)
+        if (valid && c0 + u * width < d) in[u].load(w + c0 + u * width);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (c0 + u * width < d) {
+          float y[8] = {};
+          if (valid) {
+            in[u].get(y);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) y[k] *= scale;
+          }
+          Row8<TX>::store(x + c0 + u * width, y);
+        }
     }
   }
 }
 
-// ---- the sort --------------------------------------------------------------------------
+// ---- the gradient's rows -----------------------------------------------------------------
 
-struct SortArgs {
-  Batch b;                 // first pass: keys come from here
-  bool first;
-  const uint32_t* key;
-  const uint32_t* slot;
-  uint32_t* key_out;
-  uint32_t* slot_out;
-  uint32_t* hist;          // [digit value][tile]: counts, then where the tile's slots of that value begin among all of that value
-  uint32_t* totals;        // [digit value]
-  int64_t N;
-  int tiles, shift, digit;
-  EmbedHeader* hdr;
-};
-
-__device__ inline uint32_t sort_key(const SortArgs& a, int64_t i, int& err) {
-  return a.first ? id_of(a.b, i, err) : a.key[i];
-}
-
-__global__ __launch_bounds__(256) void sort_count_kernel(SortArgs a) {
-  __shared__ uint32_t h[1 << kSortBits];
-  const int D = 1 << a.digit;
-  for (int i = threadIdx.x; i < D; i += 256) h[i] = 0;
-  __syncthreads();
-  const int64_t base = (int64_t)blockIdx.x * kSortTile;
-  int err = 0;
-  for (int j = threadIdx.x; j < kSortTile; j += 256)
-    if (base + j < a.N) atomicAdd(&h[sort_key(a, base + j, err) >> a.shift & (D - 1)], 1u);
-  if (a.first && err) atomicOr(&a.hdr->err, err);
-  __syncthreads();
-  for (int i = threadIdx.x; i < D; i += 256) a.hist[(int64_t)i * a.tiles + blockIdx.x] = h[i];
-}
-
-// A wavefront per digit value: exclusive sums over the tiles, and the total.
-__global__ __launch_bounds__(64) void sort_scan_kernel(SortArgs a) {
-  const int lane = threadIdx.x;
-  uint32_t* h = a.hist + (int64_t)blockIdx.x * a.tiles;
-  uint32_t sum = 0;
-  for (int t0 = 0; t0 < a.tiles; t0 += 64) {
-    const uint32_t x = t0 + lane < a.tiles ? h[t0 + lane] : 0;
-    uint32_t s = x;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint32_t y = __shfl_up(s, o);
-      if (lane >= o) s += y;
-    }
-    if (t0 + lane < a.tiles) h[t0 + lane] = sum + s - x;
-    sum += __shfl(s, 63);
-  }
-  if (lane == 0) a.totals[blockIdx.x] = sum;
-}
-
-// Slots to their places: stable, since wavefront w owns the w-th quarter of the tile and goes through it in order.
-__global__ __launch_bounds__(256) void sort_place_kernel(SortArgs a) {
-  __shared__ uint32_t at[4][1 << kSortBits];
-  __shared__ uint32_t wsum[4];
-  const int D = 1 << a.digit, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int64_t base = (int64_t)blockIdx.x * kSortTile + w * (kSortTile / 4);
-  for (int i = threadIdx.x; i < 4 * (1 << kSortBits); i += 256) (&at[0][0])[i] = 0;
-  __syncthreads();
-  int err = 0;
-  uint32_t key[kSortTile / 256];
-#pragma unroll
-  for (int j = 0; j < kSortTile / 256; ++j) {
-    const int64_t i = base + j * 64 + lane;
-    key[j] = i < a.N ? sort_key(a, i, err) : 0;
-    if (i < a.N) atomicAdd(&at[w][key[j] >> a.shift & (D - 1)], 1u);
-  }
-  // first place of each digit value: two neighbouring values per thread
-  uint32_t tot[2], s = 0;
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int v = threadIdx.x * 2 + k;
-    tot[k] = v < D ? a.totals[v] : 0;
-    s += tot[k];
-  }
-  const uint32_t own = s;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint32_t y = __shfl_up(s, o);
-    if (lane >= o) s += y;
-  }
-  if (lane == 63) wsum[w] = s;
-  __syncthreads();
-  uint32_t begin = s - own;
-  for (int k = 0; k < w; ++k) begin += wsum[k];
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int v = threadIdx.x * 2 + k;
-    if (v < D) {
-      uint32_t p = begin + a.hist[(int64_t)v * a.tiles + blockIdx.x];
-      for (int q = 0; q < 4; ++q) {
-        const uint32_t c = at[q][v];
-        at[q][v] = p;
-        p += c;
-      }
-    }
-    begin += tot[k];
-  }
-  __syncthreads();
-#pragma unroll
-  for (int j = 0; j < kSortTile / 256; ++j) {
-    const int64_t i = base + j * 64 + lane;
-    const bool have = i < a.N;
-    const uint32_t v = key[j] >> a.shift & (D - 1);
-    uint64_t same = __ballot(have);
-    for (int bit = 0; bit < a.digit; ++bit) {
-      const uint64_t m = __ballot(v >> bit & 1);
-      same &= v >> bit & 1 ? m : ~m;
-    }
-    if (!have) same = 0;
-    const int lead = have ? __ffsll((unsigned long long)same) - 1 : lane;
-    uint32_t p = 0;
-    if (have && lane == lead) p = atomicAdd(&at[w][v], (uint32_t)__popcll(same));
-    p = __shfl(p, lead) + __popcll(same & ((1ull << lane) - 1));
-    if (have) {
-      a.key_out[p] = key[j];
-      a.slot_out[p] = a.first ? (uint32_t)i : a.slot[i];
-    }
-  }
-}
-
-// ---- the sums --------------------------------------------------------------------------
-
-struct SumArgs {
-  const uint32_t* key;     // sorted; V at the end where slots do not count
-  const uint32_t* slot;
-  int64_t N, chunks;
-  int V, d;
-  int64_t ldX;
-  float scale;
+struct Rows {
+  const void* g;
+  int64_t ld;
   float* dW;
+  int d;
+  float scale;
   bool add;
-  float* part;
-  int32_t* list;
-  EmbedHeader* hdr;
 };
 
-__device__ inline uint32_t key_at(const SumArgs& a, int64_t p) { return p >= 0 && p < a.N ? a.key[p] : 0xffffffffu; }
-
-template <typename T>
-__device__ inline void put_row(const SumArgs& a, uint32_t v, int c, const float (&s)[8]) {
+__device__ inline void put_row(const Rows& a, uint32_t v, int c, const float (&s)[8]) {
   float* p = a.dW + (int64_t)v * a.d + c;
   float x[8];
 #pragma unroll
@@ -257,20 +152,319 @@ __device__ inline void put_row(const SumArgs& a, uint32_t v, int c, const float 
   Row8<float>::store(p, x);
 }
 
+template <typename T>
+__device__ inline void add_to(float (&s)[8], const Row8<T>& x) {
+  float y[8];
+  x.get(y);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) s[k] += y[k];
+}
+
+__device__ inline void clear(float (&s)[8]) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k) s[k] = 0.f;
+}
+
+// ---- few slots: one launch, no sort -------------------------------------------------------
+
+// The first `owners` workgroups take four slots and 512 columns each, a wavefront per slot.  The first slot of an id lists the
+// id's slots (every workgroup holds all ids in LDS: at most kFewSlots) and sums their rows; an id of more than kShared rows is shared by
+// the four wavefronts, whose sums are joined in order.  The other workgroups write zeros to the rows of their `rows_each` ids
+// that do not occur.  All slots pass through every workgroup, so the first one can report errors without a cleared header.
+constexpr int kShared = 32;
+template <typename T>
+__global__ __launch_bounds__(256) void embed_few_kernel(Batch b, Rows a, EmbedHeader* hdr, int owners, int cols, int rows_each) {
+  constexpr int U = 8;
+  __shared__ uint32_t id[kFewSlots];
+  __shared__ uint16_t list[4][kFewSlots];
+  __shared__ int count[4];
+  __shared__ uint32_t whose[4];
+  __shared__ float sums[4][512];
+  __shared__ int bits[4];
+  const int N = b.R * b.T, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const uint32_t V = (uint32_t)b.V;
+  int err = 0;
+  for (int i = threadIdx.x; i < N; i += 256) id[i] = id_of(b, i, err);
+  if (blockIdx.x == 0) {
+    err = wave_or(err);
+    if (lane == 0) bits[w] = err;
+  }
+  if ((int)blockIdx.x >= owners) {
+    // at most 64 ids: bit k of `present`, gathered by the four wavefronts
+    __shared__ uint64_t present;
+    if (threadIdx.x == 0) present = 0;
+    __syncthreads();
+    const uint32_t v0 = (blockIdx.x - owners) * (uint32_t)rows_each;
+    for (int i = threadIdx.x; i < N; i += 256)
+      if (id[i] - v0 < (uint32_t)rows_each) atomicOr(reinterpret_cast<unsigned long long*>(&present), 1ull << (id[i] - v0));
+    __syncthreads();
+    const uint64_t have = present;
+    for (int k = 0; k < rows_each && v0 + k < V; ++k) {
+      if (have >> k & 1) continue;
+      float* p = a.dW + (int64_t)(v0 + k) * a.d;
+      for (int c = threadIdx.x * 4; c < a.d; c += 1024) *reinterpret_cast<f32x4*>(p + c) = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    return;
+  }
+  __syncthreads();
+  if (blockIdx.x == 0 && threadIdx.x == 0) hdr->err = bits[0] | bits[1] | bits[2] | bits[3];
+  const int slot = (int)blockIdx.x / cols * 4 + w;
+  const uint32_t mine = slot < N ? id[slot] : V;
+  int n = 0;
+  if (mine < V) {
+    for (int i0 = 0; i0 < N; i0 += 64) {
+      const bool hit = i0 + lane < N && id[i0 + lane] == mine;
+      const uint64_t m = __ballot(hit);
+      if (i0 <= slot && (m & (slot - i0 >= 64 ? ~0ull : (1ull << (slot - i0)) - 1))) {
+        n = 0;      // an earlier slot has this id
+        break;
+      }
+      if (hit) list[w][n + __popcll(m & ((1ull << lane) - 1))] = (uint16_t)(i0 + lane);
+      n += __popcll(m);
+    }
+  }
+  if (lane == 0) {
+    count[w] = n;
+    whose[w] = mine;
+  }
+  const int c = (int)blockIdx.x % cols * 512 + lane * 8;
+  const bool in = c < a.d;
+  const T* g = static_cast<const T*>(a.g) + (in ? c : a.d - 8);
+  auto sum = [&](const uint16_t* l, int from, int to, float (&s)[8]) {
+    for (int i = from; i < to; i += U) {
+      Row8<T> x[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (i + u < to) x[u].load(g + (int64_t)__builtin_amdgcn_readfirstlane(l[i + u]) * a.ld);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (i + u < to) add_to(s, x[u]);
+    }
+  };
+  __syncthreads();
+  if (n > 0 && n <= kShared) {
+    float s[8] = {};
+    sum(list[w], 0, n, s);
+    if (in) put_row(a, mine, c, s);
+  }
+  for (int q = 0; q < 4; ++q) {
+    const int m = count[q];
+    if (m <= kShared) continue;
+    float s[8] = {};
+    sum(list[q], m * w / 4, m * (w + 1) / 4, s);
+    Row8<float>::store(&sums[w][lane * 8], s);
+    __syncthreads();
+    if (w == q) {
+      clear(s);
+      for (int k = 0; k < 4; ++k) {
+        Row8<float> x;
+        x.load(&sums[k][lane * 8]);
+        add_to(s, x);
+      }
+      if (in) put_row(a, whose[q], c, s);
+    }
+    __syncthreads();
+  }
+}
+
+// ---- the sort --------------------------------------------------------------------------
+
+// Zeros for [lo, hi) of dW, by workgroups that ride along in the launches of the sort.
+struct Fill {
+  float* p;
+  int64_t lo, hi;
+};
+constexpr int kFillEach = 16384;   // floats per workgroup
+__device__ inline void fill(const Fill& f, int64_t block) {
+  const int64_t lo = f.lo + block * kFillEach, hi = lo + kFillEach < f.hi ? lo + kFillEach : f.hi;
+  for (int64_t i = lo + threadIdx.x * 4; i < hi; i += 1024) *reinterpret_cast<f32x4*>(f.p + i) = f32x4{0.f, 0.f, 0.f, 0.f};
+}
+
+struct SortArgs {
+  Batch b;                 // first pass: keys come from here
+  bool first;
+  bool scanned;            // hist is [digit value][tile] and goes through sort_scan_kernel, or [tile][digit value]
+  const uint32_t* key;
+  const uint32_t* slot;
+  uint32_t* key_out;
+  uint32_t* slot_out;
+  uint32_t* hist;          // counts; scanned: then where the tile's slots of that value begin among all of that value
+  uint32_t* totals;        // scanned: [digit value]
+  uint32_t N;
+  int tiles, shift, digit;
+  EmbedHeader* hdr;
+  Fill f;
+};
+
+__device__ inline uint32_t sort_key(const SortArgs& a, uint32_t i, int& err) {
+  return a.first ? id_of(a.b, i, err) : a.key[i];
+}
+
+__global__ __launch_bounds__(256) void sort_count_kernel(SortArgs a) {
+  __shared__ uint32_t h[1 << kSortBits];
+  if ((int)blockIdx.x >= a.tiles) return fill(a.f, blockIdx.x - a.tiles);
+  const int D = 1 << a.digit;
+  for (int i = threadIdx.x; i < D; i += 256) h[i] = 0;
+  if (a.first && blockIdx.x == 0 && threadIdx.x == 0) {
+    a.hdr->err = 0;
+    a.hdr->nlong = 0;
+  }
+  __syncthreads();
+  int err = 0;      // reported by sort_place_kernel, after the header has been cleared
+#pragma unroll
+  for (int j = 0; j < kSortTile / 256; ++j) {
+    const uint32_t i = blockIdx.x * (uint32_t)kSortTile + j * 256 + threadIdx.x;
+    if (i < a.N) atomicAdd(&h[sort_key(a, i, err) >> a.shift & (D - 1)], 1u);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < D; i += 256) a.hist[a.scanned ? (int64_t)i * a.tiles + blockIdx.x : (int64_t)blockIdx.x * D + i] = h[i];
+}
+
+// A wavefront per digit value: exclusive sums over the tiles, and the total.
+__global__ __launch_bounds__(256) void sort_scan_kernel(SortArgs a) {
+  const int D = 1 << a.digit, groups = (D + 3) / 4;
+  if ((int)blockIdx.x >= groups) return fill(a.f, blockIdx.x - groups);
+  const int lane = threadIdx.x & 63, v = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (v >= D) return;
+  uint32_t* h = a.hist + (int64_t)v * a.tiles;
+  uint32_t sum = 0;
+  for (int t0 = 0; t0 < a.tiles; t0 += 64) {
+    const uint32_t x = t0 + lane < a.tiles ? h[t0 + lane] : 0;
+    uint32_t s = x;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint32_t y = __shfl_up(s, o);
+      if (lane >= o) s += y;
+    }
+    if (t0 + lane < a.tiles) h[t0 + lane] = sum + s - x;
+    sum += __shfl(s, 63);
+  }
+  if (lane == 0) a.totals[v] = sum;
+}
+
+// Slots to their places: stable, since wavefront w owns the w-th quarter of the tile and goes through it in order.
+__global__ __launch_bounds__(256) void sort_place_kernel(SortArgs a) {
+  constexpr int K = kSortTile / 256;
+  __shared__ uint32_t at[4][1 << kSortBits];
+  __shared__ uint32_t wsum[4];
+  if ((int)blockIdx.x >= a.tiles) return fill(a.f, blockIdx.x - a.tiles);
+  const int D = 1 << a.digit, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const uint32_t base = blockIdx.x * (uint32_t)kSortTile + w * (kSortTile / 4) + lane;
+  for (int i = threadIdx.x; i < 4 * (1 << kSortBits); i += 256) (&at[0][0])[i] = 0;
+  int err = 0;
+  uint32_t key[K], slot[K];
+#pragma unroll
+  for (int j = 0; j < K; ++j) {
+    const uint32_t i = base + j * 64;
+    key[j] = i < a.N ? sort_key(a, i, err) : 0;
+    slot[j] = a.first ? i : i < a.N ? a.slot[i] : 0;
+  }
+  // two neighbouring digit values per thread: how many slots have them, in all tiles and in those before this one
+  uint32_t tot[2] = {0, 0}, before[2] = {0, 0};
+  const int v0 = threadIdx.x * 2;
+  if (v0 < D) {
+    if (a.scanned) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        tot[k] = a.totals[v0 + k];
+        before[k] = a.hist[(int64_t)(v0 + k) * a.tiles + blockIdx.x];
+      }
+    } else {
+#pragma unroll 8
+      for (int q = 0; q < a.tiles; ++q) {
+        const uint2 x = *reinterpret_cast<const uint2*>(a.hist + (int64_t)q * D + v0);
+        tot[0] += x.x;
+        tot[1] += x.y;
+        if (q < (int)blockIdx.x) {
+          before[0] += x.x;
+          before[1] += x.y;
+        }
+      }
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < K; ++j)
+    if (base + j * 64 < a.N) atomicAdd(&at[w][key[j] >> a.shift & (D - 1)], 1u);
+  uint32_t s = tot[0] + tot[1];
+  const uint32_t own = s;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t y = __shfl_up(s, o);
+    if (lane >= o) s += y;
+  }
+  if (lane == 63) wsum[w] = s;
+  __syncthreads();
+  uint32_t begin = s - own;
+  for (int k = 0; k < w; ++k) begin += wsum[k];
+  if (v0 < D) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      uint32_t p = begin + before[k];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint32_t c = at[q][v0 + k];
+        at[q][v0 + k] = p;
+        p += c;
+      }
+      begin += tot[k];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < K; ++j) {
+    const bool have = base + j * 64 < a.N;
+    const uint32_t v = key[j] >> a.shift & (D - 1);
+    uint64_t same = __ballot(have);
+#pragma unroll
+    for (int bit = 0; bit < kSortBits; ++bit) {
+      const uint64_t m = __ballot(v >> bit & 1);
+      same &= v >> bit & 1 ? m : ~m;
+    }
+    if (!have) same = 0;
+    const int lead = have ? __ffsll((unsigned long long)same) - 1 : lane;
+    uint32_t p = 0;
+    if (have && lane == lead) p = atomicAdd(&at[w][v], (uint32_t)__popcll(same));
+    p = __shfl(p, lead) + __popcll(same & ((1ull << lane) - 1));
+    if (have) {
+      a.key_out[p] = key[j];
+      a.slot_out[p] = slot[j];
+    }
+  }
+  if (a.first && err) atomicOr(&a.hdr->err, err);
+}
+
+// ---- the sums --------------------------------------------------------------------------
+
+struct SumArgs {
+  Rows r;
+  const uint32_t* key;     // sorted; V at the end where slots do not count
+  const uint32_t* slot;
+  int64_t N, chunks;
+  int C;                   // sorted slots of a chunk, at most 64
+  int V;
+  float* part;
+  int32_t* list;
+  EmbedHeader* hdr;
+};
+
+__device__ inline uint32_t key_at(const SumArgs& a, int64_t p) { return p >= 0 && p < a.N ? a.key[p] : 0xffffffffu; }
+
 // A wavefront per chunk of sorted slots and 512 columns.  An id belongs to the chunk in which its first slot lies, which reads on
 // into the next chunk where the id ends there.  An id that ends later still is long: every chunk that it touches
 // leaves a partial sum, and embed_join_kernel adds them up.
 template <typename T>
-__global__ __launch_bounds__(64) void embed_sum_kernel(SumArgs a, const T* __restrict__ gX) {
-  constexpr int C = kEmbedChunk, U = 8;
-  const int lane = threadIdx.x;
+__global__ __launch_bounds__(256) void embed_sum_kernel(SumArgs a) {
+  constexpr int U = 8;
+  const int lane = threadIdx.x & 63, C = a.C, d = a.r.d;
   const int64_t chunk = blockIdx.x, p0 = chunk * C;
-  const int c = blockIdx.y * 512 + lane * 8;
-  const bool in = c < a.d;
-  const int c_load = in ? c : a.d - 8;             // lanes past the row read its end along
+  const int c = (blockIdx.y * (blockDim.x >> 6) + (threadIdx.x >> 6)) * 512 + lane * 8;
+  const bool in = c < d;
+  const T* gX = static_cast<const T*>(a.r.g) + (in ? c : d - 8);     // lanes past the row read its end along
   const uint32_t V = (uint32_t)a.V;
-  const uint32_t k0 = p0 + lane < a.N ? a.key[p0 + lane] : V;
-  const uint32_t s0 = p0 + lane < a.N ? a.slot[p0 + lane] : 0;
+  const bool mine = lane < C && p0 + lane < a.N;
+  const uint32_t k0 = mine ? a.key[p0 + lane] : V;
+  const uint32_t s0 = mine ? a.slot[p0 + lane] : 0;
   const int n = __popcll(__ballot(k0 < V));        // slots that count come first
   if (n == 0) return;
   auto rows = [&](uint32_t slots, int from, int to, uint32_t keys, uint32_t& cur, float (&s)[8], bool flush) {
@@ -278,26 +472,22 @@ __global__ __launch_bounds__(64) void embed_sum_kernel(SumArgs a, const T* __res
       Row8<T> x[U];
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (i + u < to) x[u].load(gX + (int64_t)(uint32_t)__builtin_amdgcn_readlane(slots, i + u) * a.ldX + c_load);
+        if (i + u < to) x[u].load(gX + (int64_t)(uint32_t)__builtin_amdgcn_readlane(slots, i + u) * a.r.ld);
 #pragma unroll
       for (int u = 0; u < U; ++u)
         if (i + u < to) {
           const uint32_t v = __builtin_amdgcn_readlane(keys, i + u);
           if (flush && v != cur) {
-            if (cur != V && in) put_row<T>(a, cur, c, s);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) s[k] = 0.f;
+            if (cur != V && in) put_row(a.r, cur, c, s);
+            clear(s);
             cur = v;
           }
-          float y[8];
-          x[u].get(y);
-#pragma unroll
-          for (int k = 0; k < 8; ++k) s[k] += y[k];
+          add_to(s, x[u]);
         }
     }
   };
   auto partial = [&](int which, const float (&s)[8]) {
-    if (in) Row8<float>::store(a.part + (chunk * 2 + which) * a.d + c, s);
+    if (in) Row8<float>::store(a.part + (chunk * 2 + which) * d + c, s);
   };
   // an id that began in an earlier chunk
   const uint32_t before = key_at(a, p0 - 1);
@@ -322,73 +512,75 @@ __global__ __launch_bounds__(64) void embed_sum_kernel(SumArgs a, const T* __res
   uint32_t cur = V;
   rows(s0, lead, end, k0, cur, s, true);
   if (goes_on && !is_long) {
-    const uint32_t k1 = key_at(a, p0 + C + lane);
-    const uint32_t s1 = p0 + C + lane < a.N ? a.slot[p0 + C + lane] : 0;
+    const uint32_t k1 = lane < C ? key_at(a, p0 + C + lane) : V;
+    const uint32_t s1 = lane < C && p0 + C + lane < a.N ? a.slot[p0 + C + lane] : 0;
     rows(s1, 0, __popcll(__ballot(k1 == tail)), k1, cur, s, false);
   }
-  if (cur != V && in) put_row<T>(a, cur, c, s);
+  if (cur != V && in) put_row(a.r, cur, c, s);
   if (is_long) {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) s[k] = 0.f;
+    clear(s);
     rows(s0, end, n, k0, cur, s, false);
     partial(1, s);
-    if (blockIdx.y == 0 && lane == 0) a.list[atomicAdd(&a.hdr->nlong, 1)] = (int32_t)chunk;
+    if (c == 0) a.list[atomicAdd(&a.hdr->nlong, 1)] = (int32_t)chunk;
   }
 }
 
-// The long ids: partial sums in the order of their chunks.
-__global__ __launch_bounds__(64) void embed_join_kernel(SumArgs a) {
-  constexpr int C = kEmbedChunk;
-  const int lane = threadIdx.x, c = blockIdx.y * 512 + lane * 8;
+// The long ids: a workgroup per id and 512 columns.  Wavefront w takes the w-th sixteenth of the id's partial sums in order, and
+// the sixteen sums are added in order.
+__global__ __launch_bounds__(1024) void embed_join_kernel(SumArgs a) {
+  constexpr int U = 8;
+  __shared__ float sums[16][512];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, c = blockIdx.y * 512 + lane * 8, d = a.r.d;
+  const bool in = c < d;
+  const float* part = a.part + (in ? c : d - 8);
   const int nlong = a.hdr->nlong;
   for (int i = blockIdx.x; i < nlong; i += gridDim.x) {
-    const int64_t chunk = a.list[i];
-    const uint32_t v = a.key[chunk * C + C - 1];
-    if (c >= a.d) continue;
-    float s[8];
-    Row8<float> x;
-    x.load(a.part + (chunk * 2 + 1) * a.d + c);
-    x.get(s);
-    for (int64_t q = chunk + 1; q < a.chunks && a.key[q * C] == v; ++q) {
-      x.load(a.part + q * 2 * a.d + c);
-      float y[8];
-      x.get(y);
+    const int64_t first = a.list[i];
+    const uint32_t v = a.key[first * a.C + a.C - 1];
+    int64_t end = first + 3;         // one past its last chunk: it reaches the third
+    for (;;) {
+      const int64_t q = end + lane;
+      const uint64_t m = __ballot(q < a.chunks && a.key[q * a.C] == v);
+      end += __popcll(m);
+      if (m != ~0ull) break;
+    }
+    const int64_t n = end - first, lo = first + n * w / 16, hi = first + n * (w + 1) / 16;
+    float s[8] = {};
+    for (int64_t q = lo; q < hi; q += U) {
+      Row8<float> x[U];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) s[k] += y[k];
+      for (int u = 0; u < U; ++u)
+        if (q + u < hi) x[u].load(part + ((q + u) * 2 + (q + u == first)) * d);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (q + u < hi) add_to(s, x[u]);
     }
-    put_row<float>(a, v, c, s);
-  }
-}
-
-// Zeros to the rows of ids that do not occur: a wavefront looks for 64 ids at a time, then fills.
-__global__ __launch_bounds__(256) void embed_zero_kernel(SumArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t v0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * 64, v = v0 + lane;
-  if (v0 >= a.V) return;
-  bool absent = false;
-  if (v < a.V) {
-    int64_t lo = 0, hi = a.N;     // first position whose key is v or more
-    while (lo < hi) {
-      const int64_t m = (lo + hi) >> 1;
-      if (a.key[m] < (uint32_t)v) lo = m + 1;
-      else hi = m;
+    Row8<float>::store(&sums[w][lane * 8], s);
+    __syncthreads();
+    if (w == 0) {
+      clear(s);
+      for (int k = 0; k < 16; ++k) {
+        Row8<float> x;
+        x.load(&sums[k][lane * 8]);
+        add_to(s, x);
+      }
+      if (in) put_row(a.r, v, c, s);
     }
-    absent = key_at(a, lo) != (uint32_t)v;
-  }
-  uint64_t todo = __ballot(absent);
-  while (todo) {
-    const int k = __ffsll((unsigned long long)todo) - 1;
-    todo &= todo - 1;
-    float* p = a.dW + (v0 + k) * a.d;
-    for (int c = lane * 4; c < a.d; c += 256) *reinterpret_cast<f32x4*>(p + c) = f32x4{0.f, 0.f, 0.f, 0.f};
+    __syncthreads();
   }
 }
 
 template <typename TW, typename TX>
 void run_fwd(const lmhead_embed_desc& d, const Batch& b, const void* W, float scale, void* X, EmbedHeader* hdr, hipStream_t s) {
-  const int64_t N = (int64_t)d.R * d.T, wgs = (N + 3) / 4;
-  hipLaunchKernelGGL((embed_fwd_kernel<TW, TX>), dim3((unsigned)(wgs < 65536 ? wgs : 65536)), dim3(256), 0, s, b,
-                     static_cast<const TW*>(W), d.ldW, d.d, scale, static_cast<TX*>(X), d.ldX, hdr);
+  const int64_t N = (int64_t)d.R * d.T;
+  int lanes = 0;
+  while (lanes < 6 && (8 << lanes) < d.d) ++lanes;
+  const bool reports = N <= kReportSlots;
+  int64_t wgs = (N + (256 >> lanes) - 1) / (256 >> lanes);
+  if (wgs > 65536) wgs = 65536;
+  if (!reports) hipLaunchKernelGGL(embed_clear_kernel, dim3(1), dim3(1), 0, s, hdr);
+  hipLaunchKernelGGL((embed_fwd_kernel<TW, TX>), dim3((unsigned)wgs + reports), dim3(256), 0, s, b, static_cast<const TW*>(W), d.ldW, d.d,
+                     scale, static_cast<TX*>(X), d.ldX, hdr, lanes, reports);
 }
 
 }  // namespace
@@ -396,7 +588,6 @@ void run_fwd(const lmhead_embed_desc& d, const Batch& b, const void* W, float sc
 hipError_t launch_embed_fwd(const lmhead_embed_desc& d, const void* W, const int32_t* tok, const int32_t* len, float scale, void* X,
                             EmbedHeader* hdr, hipStream_t s) {
   const Batch b{tok, len, d.R, d.T, d.V};
-  hipLaunchKernelGGL(embed_clear_kernel, dim3(1), dim3(1), 0, s, hdr);
   if (d.dtype == LMHEAD_BF16 && d.rows == LMHEAD_BF16) run_fwd<__bf16, __bf16>(d, b, W, scale, X, hdr, s);
   else if (d.dtype == LMHEAD_BF16) run_fwd<__bf16, float>(d, b, W, scale, X, hdr, s);
   else if (d.rows == LMHEAD_BF16) run_fwd<float, __bf16>(d, b, W, scale, X, hdr, s);
@@ -408,16 +599,40 @@ hipError_t launch_embed_bwd(const lmhead_embed_desc& d, const void* gX, const in
                             char* ws, hipStream_t s) {
   const EmbedLayout L = embed_layout(&d);
   EmbedHeader* hdr = reinterpret_cast<EmbedHeader*>(ws + L.hdr);
+  const Batch b{tok, len, d.R, d.T, d.V};
+  const bool add = (d.flags & LMHEAD_FLAG_ACCUM_DW) != 0, bf16 = d.rows == LMHEAD_BF16;
+  const Rows r{gX, d.ldX, dW, d.d, scale, add};
+  if (L.N <= kFewSlots) {
+    const int cols = (d.d + 511) / 512, owners = (int)((L.N + 3) / 4) * cols;
+    int rows_each = 16384 / d.d;
+    rows_each = rows_each < 1 ? 1 : rows_each > 64 ? 64 : rows_each;
+    const int64_t fills = add ? 0 : ((int64_t)d.V + rows_each - 1) / rows_each;
+    auto go = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)(owners + fills)), dim3(256), 0, s, b, r, hdr, owners, cols, rows_each);
+    };
+    if (bf16) go(embed_few_kernel<__bf16>);
+    else go(embed_few_kernel<float>);
+    return hipGetLastError();
+  }
   auto u32 = [&](size_t off) { return reinterpret_cast<uint32_t*>(ws + off); };
-  hipLaunchKernelGGL(embed_clear_kernel, dim3(1), dim3(1), 0, s, hdr);
   SortArgs so{};
-  so.b = Batch{tok, len, d.R, d.T, d.V};
-  so.N = L.N;
+  so.b = b;
+  so.N = (uint32_t)L.N;
   so.tiles = (int)L.tiles;
+  so.scanned = L.tiles > kScanTiles;
   so.digit = L.digit;
   so.hist = u32(L.hist);
   so.totals = so.hist + ((int64_t)L.tiles << L.digit);
   so.hdr = hdr;
+  const int launches = L.passes * (so.scanned ? 3 : 2);
+  int launch = 0;
+  const int64_t cells = add ? 0 : (int64_t)d.V * d.d;
+  // one launch of the sort, with its share of the zeros
+  auto go = [&](auto kernel, int64_t wgs) {
+    so.f = Fill{dW, cells / 8 * launch / launches * 8, cells / 8 * (launch + 1) / launches * 8};
+    ++launch;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(wgs + (so.f.hi - so.f.lo + kFillEach - 1) / kFillEach)), dim3(256), 0, s, so);
+  };
   for (int p = 0; p < L.passes; ++p) {
     so.first = p == 0;
     so.key = u32(L.key[(p + 1) & 1]);
@@ -425,31 +640,28 @@ hipError_t launch_embed_bwd(const lmhead_embed_desc& d, const void* gX, const in
     so.key_out = u32(L.key[p & 1]);
     so.slot_out = u32(L.slot[p & 1]);
     so.shift = p * L.digit;
-    hipLaunchKernelGGL(sort_count_kernel, dim3((unsigned)L.tiles), dim3(256), 0, s, so);
-    hipLaunchKernelGGL(sort_scan_kernel, dim3(1u << L.digit), dim3(64), 0, s, so);
-    hipLaunchKernelGGL(sort_place_kernel, dim3((unsigned)L.tiles), dim3(256), 0, s, so);
+    go(sort_count_kernel, L.tiles);
+    if (so.scanned) go(sort_scan_kernel, ((1 << L.digit) + 3) / 4);
+    go(sort_place_kernel, L.tiles);
   }
   SumArgs a{};
+  a.r = r;
   a.key = so.key_out;
   a.slot = so.slot_out;
   a.N = L.N;
+  a.C = L.C;
   a.chunks = L.chunks;
   a.V = d.V;
-  a.d = d.d;
-  a.ldX = d.ldX;
-  a.scale = scale;
-  a.dW = dW;
-  a.add = (d.flags & LMHEAD_FLAG_ACCUM_DW) != 0;
   a.part = reinterpret_cast<float*>(ws + L.part);
   a.list = reinterpret_cast<int32_t*>(ws + L.list);
   a.hdr = hdr;
-  const unsigned cols = (unsigned)((d.d + 511) / 512);
-  if (!a.add) hipLaunchKernelGGL(embed_zero_kernel, dim3((unsigned)(((int64_t)d.V + 255) / 256)), dim3(256), 0, s, a);
-  if (d.rows == LMHEAD_BF16)
-    hipLaunchKernelGGL(embed_sum_kernel<__bf16>, dim3((unsigned)L.chunks, cols), dim3(64), 0, s, a, static_cast<const __bf16*>(gX));
-  else
-    hipLaunchKernelGGL(embed_sum_kernel<float>, dim3((unsigned)L.chunks, cols), dim3(64), 0, s, a, static_cast<const float*>(gX));
-  hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)(L.chunks < 256 ? L.chunks : 256), cols), dim3(64), 0, s, a);
+  const unsigned cols = (unsigned)((d.d + 511) / 512), waves = cols < 4 ? cols : 4;
+  const dim3 grid((unsigned)L.chunks, (cols + waves - 1) / waves);
+  if (bf16) hipLaunchKernelGGL(embed_sum_kernel<__bf16>, grid, dim3(64 * waves), 0, s, a);
+  else hipLaunchKernelGGL(embed_sum_kernel<float>, grid, dim3(64 * waves), 0, s, a);
+  // an id is long from two chunks' slots on
+  const int64_t most = L.N / (2 * L.C) + 1;
+  hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)(most < 64 ? most : 64), cols), dim3(1024), 0, s, a);
   return hipGetLastError();
 }
 

@@ -34,9 +34,11 @@ hipError_t launch_preference(const lmhead_preference& q, const float* lp, const 
 
 // ---- embedding (lmhead_embed.hip) -------------------------------------------------------
 
-constexpr int kSortTile = 4096;      // slots per workgroup of a sorting pass
+constexpr int kSortTile = 1024;      // slots per workgroup of a sorting pass
 constexpr int kSortBits = 9;         // digits have at most so many bits
-constexpr int kEmbedChunk = 64;      // sorted slots per unit of the gradient
+constexpr int kScanTiles = 64;       // up to so many tiles each adds up the counts of all of them itself
+constexpr int kFewSlots = 2048;      // up to so many slots the gradient is one launch without a sort
+constexpr int kReportSlots = 4096;   // up to so many slots one workgroup of the lookup reports the errors of all
 
 struct EmbedHeader {
   int32_t err;      // sticky error bits (kErrLen, kErrTok), where lmhead_check reads them
@@ -50,6 +52,7 @@ struct EmbedLayout {
   int64_t N;
   int bits, passes, digit;   // bits of a key (ids and V, the key of a slot that does not count), sorting passes, bits of a pass
   int64_t tiles, chunks;
+  int C;                     // sorted slots per chunk of the sums
   size_t hdr, key[2], slot[2], hist, list, part, total;
 };
 static inline EmbedLayout embed_layout(const lmhead_embed_desc* d) {
@@ -60,7 +63,15 @@ static inline EmbedLayout embed_layout(const lmhead_embed_desc* d) {
   L.passes = (L.bits + kSortBits - 1) / kSortBits;
   L.digit = (L.bits + L.passes - 1) / L.passes;
   L.tiles = (L.N + kSortTile - 1) / kSortTile;
-  L.chunks = (L.N + kEmbedChunk - 1) / kEmbedChunk;
+  // long chunks leave fewer partial sums; short ones keep 8192 wavefronts busy (eight per SIMD) where slots are few
+  const int64_t cols = (d->d + 511) / 512;
+  L.C = 64;
+  while (L.C > 8 && L.N * cols < (int64_t)L.C * 8192) L.C /= 2;
+  L.chunks = (L.N + L.C - 1) / L.C;
+  // room for the chunks of any smaller batch: short ones are at most 16384 / cols
+  int64_t room = (L.N + 7) / 8;
+  if (room > 16384 / cols + 1) room = 16384 / cols + 1;
+  if (room < L.chunks) room = L.chunks;
   size_t off = 0;
   auto take = [&](size_t bytes) {
     const size_t o = off;
@@ -71,8 +82,8 @@ static inline EmbedLayout embed_layout(const lmhead_embed_desc* d) {
   for (int i = 0; i < 2; ++i) L.key[i] = take((size_t)L.N * 4);
   for (int i = 0; i < 2; ++i) L.slot[i] = take((size_t)L.N * 4);
   L.hist = take(((size_t)L.tiles << L.digit) * 4 + ((size_t)4 << L.digit));   // [digit][tile], then the totals
-  L.list = take((size_t)L.chunks * 4);
-  L.part = take((size_t)L.chunks * 2 * d->d * 4);              // [chunk]{of an id that began earlier, of one that goes on}[d]
+  L.list = take((size_t)room * 4);
+  L.part = take((size_t)room * 2 * d->d * 4);              // [chunk]{of an id that began earlier, of one that goes on}[d]
   L.total = off;
   return L;
 }

@@ -113,6 +113,21 @@ def backward(R, T, d, V, rows, tok, lens, scale=1.5, ldX=None, add=False, code=0
 N_SEED = 100
 
 
+def backward_checked_by_torch(N, d, V, tok):
+    """A batch for which the oracle's loop would take long: fp64 on the GPU by scattered additions of whole numbers, which are exact."""
+    import torch
+    import paper_2603_04411_amd as L
+    g = torch.randint(-8, 9, (N, d), generator=torch.Generator(device="cuda").manual_seed(N), device="cuda").float()
+    desc = L.make_embed_desc(1, N, d, V, "f32")
+    dW, ws = torch.full((V, d), 7.0, device="cuda"), torch.full((L.embed_workspace_bytes(desc),), 0xFF, dtype=torch.uint8, device="cuda")
+    dt = to_device(tok)
+    L.embed_bwd(desc, g, dt, None, 1.0, dW, ws)
+    assert L.lmhead_check(ws) == 0
+    # sums stay below 2^24: exact in fp32 in any order
+    want = torch.zeros(V, d, dtype=torch.float64, device="cuda").index_add_(0, dt.long(), g.double())
+    assert torch.equal(dW.double(), want)
+
+
 @pytest.mark.parametrize("rows", ["bf16", "f32"])
 @pytest.mark.parametrize("add", [False, True])
 @pytest.mark.parametrize("R,T,d,V", [(1, 1, 8, 1), (1, 1, 64, 300), (3, 5, 64, 7), (2, 33, 1000, 50), (4, 16, 520, 1), (1, 64, 256, 64),
@@ -130,6 +145,26 @@ def test_ids_that_end_around_the_edges_of_the_pieces(piece):
         V = int(tok.max()) + 2
         perm = np.random.default_rng(piece).permutation(tok.size)
         backward(1, tok.size, 16, V, "f32" if lead else "bf16", tok[perm].astype(np.int32), None, add=lead == 1)
+
+
+# rows of 16, 2104, 4104 and 5128 elements: pieces of 8, 16 and 32 slots; and, of many short rows, 64
+EDGES = [1, 7, 8, 9, 15, 16, 17, 23, 24, 25, 31, 32, 33, 47, 48, 49, 63, 64, 65, 95, 96, 97, 127, 128, 129, 191, 192, 193, 1000]
+
+
+@pytest.mark.parametrize("d,N,piece", [(16, 5003, p) for p in EDGES] + [
+    (d, N, p) for d, N in ((2104, 5003), (4104, 7001), (5128, 13001)) for p in (1, 8, 9, 16, 17, 24, 25, 32, 33, 49, 65, 97, 1000)])
+def test_sorted_ids_that_end_around_the_edges_of_the_pieces(d, N, piece):
+    lead = piece % 5
+    tok = np.concatenate([np.zeros(lead, dtype=np.int32), 1 + np.arange(N - lead, dtype=np.int32) // piece])
+    perm = np.random.default_rng(piece).permutation(tok.size)
+    backward(1, N, d, int(tok.max()) + 2, "f32" if piece % 2 else "bf16", tok[perm].astype(np.int32), None, add=piece % 3 == 0)
+
+
+@pytest.mark.parametrize("piece", [1, 63, 64, 65, 127, 128, 129, 191, 192, 193, 70000])
+def test_pieces_of_64(piece):
+    N = 530003
+    tok = (np.random.default_rng(piece).permutation(N) // piece).astype(np.int32)
+    backward_checked_by_torch(N, 8, int(tok.max()) + 1, tok)
 
 
 # more than one sorting tile, ids of one, two and three digits, one id everywhere
