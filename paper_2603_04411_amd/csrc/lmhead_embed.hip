@@ -22,6 +22,10 @@ struct Row8<float> {
     a = *reinterpret_cast<const f32x4*>(p);
     b = *reinterpret_cast<const f32x4*>(p + 4);
   }
+  __device__ inline void load_once(const float* p) {
+    a = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p));
+    b = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p + 4));
+  }
   __device__ inline void get(float (&v)[8]) const {
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
@@ -35,6 +39,7 @@ template <>
 struct Row8<__bf16> {
   bf16x8 a;
   __device__ inline void load(const __bf16* p) { a = *reinterpret_cast<const bf16x8*>(p); }
+  __device__ inline void load_once(const __bf16* p) { a = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(p)); }
   __device__ inline void get(float (&v)[8]) const {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = (float)a[i];
@@ -55,19 +60,12 @@ struct Batch {
 
 // Id of a slot, V where it does not count; error bits of what it met.
 __device__ inline uint32_t id_of(const Batch& b, uint32_t i, int& err) {
-  const uint32_t r = i / (uint32_t)b.T;
-  int n = b.T;
-  if (b.len) {
-    n = b.len[r];
-    if (n < 0 || n > b.T) err |= kErrLen;
-  }
-  if ((int)(i - r * (uint32_t)b.T) >= n) return b.V;
-  const int v = b.tok[i];
-  if (v < 0 || v >= b.V) {
-    err |= kErrTok;
-    return b.V;
-  }
-  return v;
+  // both loads leave before either result is looked at
+  const uint32_t r = i / (uint32_t)b.T, v = (uint32_t)b.tok[i];
+  const int n = b.len ? b.len[r] : b.T, t = (int)(i - r * (uint32_t)b.T);
+  const bool counts = t < n, known = v < (uint32_t)b.V;
+  err |= ((uint32_t)n > (uint32_t)b.T ? kErrLen : 0) | (counts && !known ? kErrTok : 0);
+  return counts && known ? v : (uint32_t)b.V;
 }
 
 __device__ inline int wave_or(int x) {
@@ -89,39 +87,48 @@ __device__ inline void report_all(const Batch& b, EmbedHeader* hdr) {
 
 __global__ void embed_clear_kernel(EmbedHeader* hdr) { hdr->err = 0; }
 
-// 2^lanes neighbouring lanes per row.  Of a batch of few slots the last workgroup reports for all (`reports`); otherwise the header
-// has been cleared, and whoever meets an error adds it.
-template <typename TW, typename TX>
+// Units of 256 threads and 16 bytes each of X, in the order of the addresses; a workgroup has kLookup of them in flight, so that
+// the wait for an id and then for its row is shared.  Long rows: `parts` units to a row, and the id is the same for all
+// threads; short ones: 2^lanes neighbouring threads to a row.
+// Of a batch of few slots the last workgroup reports for all (`reports`); otherwise the header has been cleared, and whoever meets
+// an error adds it.
+constexpr int kLookup = 4;
+template <typename TW, typename TX, bool kLong>
 __global__ __launch_bounds__(256) void embed_fwd_kernel(Batch b, const TW* __restrict__ W, int64_t ldW, int d, float scale,
-                                                        TX* __restrict__ X, int64_t ldX, EmbedHeader* hdr, int lanes, bool reports) {
-  constexpr int U = 4;
+                                                        TX* __restrict__ X, int64_t ldX, EmbedHeader* hdr, int lanes, uint32_t parts,
+                                                        bool reports) {
+  constexpr int E = 16 / (int)sizeof(TX), U = kLookup;
+  typedef __attribute__((ext_vector_type(E))) TW in_t;
+  typedef __attribute__((ext_vector_type(E))) TX out_t;
   if (reports && blockIdx.x == gridDim.x - 1) return report_all(b, hdr);
-  const uint32_t N = (uint32_t)b.R * (uint32_t)b.T, step = (gridDim.x - reports) * (256u >> lanes);
-  const int in_row = threadIdx.x & ((1 << lanes) - 1), width = 8 << lanes;
-  for (uint64_t i = blockIdx.x * (256u >> lanes) + (threadIdx.x >> lanes); i < N; i += step) {
-    int err = 0;
-    const uint32_t v = id_of(b, (uint32_t)i, err);
-    if (!reports && err && in_row == 0) atomicOr(&hdr->err, err);
-    const bool valid = v < (uint32_t)b.V;
-    const TW* w = W + (int64_t)(valid ? v : 0) * ldW;
-    TX* x = X + (int64_t)i * ldX;
-    for (int c0 = in_row * 8; c0 < d; c0 += width * U) {
-      Row8<TW> in[U];
+  const uint32_t N = (uint32_t)b.R * (uint32_t)b.T;
+  const uint64_t u0 = (uint64_t)blockIdx.x * U;
+  int64_t i[U];
+  int c[U];
+  uint32_t v[U];
+  int err = 0;
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (valid && c0 + u * width < d) in[u].load(w + c0 + u * width);
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (c0 + u * width < d) {
-          float y[8] = {};
-          if (valid) {
-            in[u].get(y);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) y[k] *= scale;
-          }
-          Row8<TX>::store(x + c0 + u * width, y);
-        }
+  for (int u = 0; u < U; ++u) {
+    if (kLong) {
+      i[u] = (int64_t)((u0 + u) / parts);
+      c[u] = ((int)((u0 + u) % parts) * 256 + (int)threadIdx.x) * E;
+    } else {
+      i[u] = (int64_t)(((u0 + u) << (8 - lanes)) + (threadIdx.x >> lanes));
+      c[u] = (int)(threadIdx.x & ((1u << lanes) - 1)) * E;
     }
+    v[u] = i[u] < N ? id_of(b, (uint32_t)i[u], err) : 0;
+  }
+  if (!reports && err) atomicOr(&hdr->err, err);
+  in_t x[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (i[u] < N && c[u] < d && v[u] < (uint32_t)b.V) x[u] = *reinterpret_cast<const in_t*>(W + (int64_t)v[u] * ldW + c[u]);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    out_t y;
+#pragma unroll
+    for (int k = 0; k < E; ++k) y[k] = v[u] < (uint32_t)b.V ? (TX)((float)x[u][k] * scale) : (TX)0.f;
+    if (i[u] < N && c[u] < d) __builtin_nontemporal_store(y, reinterpret_cast<out_t*>(X + i[u] * ldX + c[u]));
   }
 }
 
@@ -274,10 +281,10 @@ struct Fill {
   float* p;
   int64_t lo, hi;
 };
-constexpr int kFillEach = 16384;   // floats per workgroup
+constexpr int kFillEach = 1024;    // floats per workgroup
 __device__ inline void fill(const Fill& f, int64_t block) {
-  const int64_t lo = f.lo + block * kFillEach, hi = lo + kFillEach < f.hi ? lo + kFillEach : f.hi;
-  for (int64_t i = lo + threadIdx.x * 4; i < hi; i += 1024) *reinterpret_cast<f32x4*>(f.p + i) = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int64_t i = f.lo + block * kFillEach + threadIdx.x * 4;
+  if (i < f.hi) *reinterpret_cast<f32x4*>(f.p + i) = f32x4{0.f, 0.f, 0.f, 0.f};
 }
 
 struct SortArgs {
@@ -444,21 +451,30 @@ struct SumArgs {
   int C;                   // sorted slots of a chunk, at most 64
   int V;
   float* part;
-  int32_t* list;
+  int64_t ld_part;
+  int col_groups;          // workgroups that a chunk's columns are spread over
+  struct LongId* list;
   EmbedHeader* hdr;
 };
 
 __device__ inline uint32_t key_at(const SumArgs& a, int64_t p) { return p >= 0 && p < a.N ? a.key[p] : 0xffffffffu; }
 
+// What embed_join_kernel has to add up for an id: the partial sums of chunks first .. last.
+struct LongId {
+  uint32_t id;
+  int32_t first, last, pad;
+};
+static_assert(sizeof(LongId) == kLongIdBytes, "workspace");
+
 // A wavefront per chunk of sorted slots and 512 columns.  An id belongs to the chunk in which its first slot lies, which reads on
-// into the next chunk where the id ends there.  An id that ends later still is long: every chunk that it touches
-// leaves a partial sum, and embed_join_kernel adds them up.
+// into the next chunk where the id ends there.  An id that ends later still is long: every chunk that it touches leaves a partial
+// sum, and embed_join_kernel adds them up.
 template <typename T>
 __global__ __launch_bounds__(256) void embed_sum_kernel(SumArgs a) {
   constexpr int U = 8;
   const int lane = threadIdx.x & 63, C = a.C, d = a.r.d;
-  const int64_t chunk = blockIdx.x, p0 = chunk * C;
-  const int c = (blockIdx.y * (blockDim.x >> 6) + (threadIdx.x >> 6)) * 512 + lane * 8;
+  const int64_t chunk = blockIdx.x / a.col_groups, p0 = chunk * C;
+  const int c = ((int)(blockIdx.x % a.col_groups) * (blockDim.x >> 6) + (threadIdx.x >> 6)) * 512 + lane * 8;
   const bool in = c < d;
   const T* gX = static_cast<const T*>(a.r.g) + (in ? c : d - 8);     // lanes past the row read its end along
   const uint32_t V = (uint32_t)a.V;
@@ -472,7 +488,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(SumArgs a) {
       Row8<T> x[U];
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (i + u < to) x[u].load(gX + (int64_t)(uint32_t)__builtin_amdgcn_readlane(slots, i + u) * a.r.ld);
+        if (i + u < to) x[u].load_once(gX + (int64_t)(uint32_t)__builtin_amdgcn_readlane(slots, i + u) * a.r.ld);
 #pragma unroll
       for (int u = 0; u < U; ++u)
         if (i + u < to) {
@@ -487,7 +503,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(SumArgs a) {
     }
   };
   auto partial = [&](int which, const float (&s)[8]) {
-    if (in) Row8<float>::store(a.part + (chunk * 2 + which) * d + c, s);
+    if (in) Row8<float>::store(a.part + (chunk * 2 + which) * a.ld_part + c, s);
   };
   // an id that began in an earlier chunk
   const uint32_t before = key_at(a, p0 - 1);
@@ -499,6 +515,22 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(SumArgs a) {
       uint32_t cur = before;
       rows(s0, 0, lead, k0, cur, s, false);
       partial(0, s);
+      if (!on && c == lane * 8 && blockIdx.x % a.col_groups == 0) {
+        // it ends here: where it began, 64 probes at a time (chunks from hi on begin inside it, those below lo do not)
+        int64_t lo = 1, hi = chunk;
+        while (lo < hi) {
+          const int64_t step = (hi - lo + 63) / 64, q = hi - 1 - lane * step;
+          const int have = __popcll(__ballot(q >= lo && a.key[q * C] == before && a.key[q * C - 1] == before));
+          if (have == 0) {
+            lo = hi;
+            break;
+          }
+          const int64_t below = hi - 1 - have * step;      // the first probe that was not inside, if there was one
+          hi = hi - 1 - (have - 1) * step;
+          lo = below + 1 > lo ? below + 1 : lo;
+        }
+        if (lane == 0) a.list[atomicAdd(&a.hdr->nlong, 1)] = LongId{before, (int32_t)(hi - 1), (int32_t)chunk, 0};
+      }
     }
   }
   if (lead == n) return;
@@ -521,50 +553,42 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(SumArgs a) {
     clear(s);
     rows(s0, end, n, k0, cur, s, false);
     partial(1, s);
-    if (c == 0) a.list[atomicAdd(&a.hdr->nlong, 1)] = (int32_t)chunk;
   }
 }
 
-// The long ids: a workgroup per id and 512 columns.  Wavefront w takes the w-th sixteenth of the id's partial sums in order, and
-// the sixteen sums are added in order.
-__global__ __launch_bounds__(1024) void embed_join_kernel(SumArgs a) {
-  constexpr int U = 8;
-  __shared__ float sums[16][512];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, c = blockIdx.y * 512 + lane * 8, d = a.r.d;
+// The long ids: a workgroup per id and 256 columns, those of one id next to each other (a launch that went through all ids with the same
+// columns first met on few memory channels: 60 us for the 3600 partial rows of 4096 that 330000 slots leave, now 34).  Wavefront w takes
+// the w-th eighth of the id's partial sums in order, and the eight sums are added in order.
+constexpr int kJoinWaves = 8;
+__global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(SumArgs a) {
+    constexpr int U = 8, W = kJoinWaves;
+  __shared__ f32x4 sums[W][64];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), d = a.r.d;
+  const int cols = (d + 255) / 256, c = (int)(blockIdx.x % cols) * 256 + lane * 4;
   const bool in = c < d;
-  const float* part = a.part + (in ? c : d - 8);
+  const float* part = a.part + (in ? c : d - 4);
   const int nlong = a.hdr->nlong;
-  for (int i = blockIdx.x; i < nlong; i += gridDim.x) {
-    const int64_t first = a.list[i];
-    const uint32_t v = a.key[first * a.C + a.C - 1];
-    int64_t end = first + 3;         // one past its last chunk: it reaches the third
-    for (;;) {
-      const int64_t q = end + lane;
-      const uint64_t m = __ballot(q < a.chunks && a.key[q * a.C] == v);
-      end += __popcll(m);
-      if (m != ~0ull) break;
-    }
-    const int64_t n = end - first, lo = first + n * w / 16, hi = first + n * (w + 1) / 16;
-    float s[8] = {};
-    for (int64_t q = lo; q < hi; q += U) {
-      Row8<float> x[U];
+  for (int i = blockIdx.x / cols; i < nlong; i += gridDim.x / cols) {
+    const LongId l = a.list[i];
+    const int n = l.last + 1 - l.first, from = l.first + (int)((int64_t)n * w / W), to = l.first + (int)((int64_t)n * (w + 1) / W);
+    f32x4* p = reinterpret_cast<f32x4*>(a.r.dW + (int64_t)l.id * d + c);
+    f32x4 s = {0.f, 0.f, 0.f, 0.f}, old = s;
+    if (w == 0 && in && a.r.add) old = *p;
+    for (int q = from; q < to; q += U) {
+      f32x4 x[U];
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (q + u < hi) x[u].load(part + ((q + u) * 2 + (q + u == first)) * d);
+        if (q + u < to) x[u] = *reinterpret_cast<const f32x4*>(part + ((int64_t)(q + u) * 2 + (q + u == l.first)) * a.ld_part);
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (q + u < hi) add_to(s, x[u]);
+        if (q + u < to) s += x[u];
     }
-    Row8<float>::store(&sums[w][lane * 8], s);
+    sums[w][lane] = s;
     __syncthreads();
-    if (w == 0) {
-      clear(s);
-      for (int k = 0; k < 16; ++k) {
-        Row8<float> x;
-        x.load(&sums[k][lane * 8]);
-        add_to(s, x);
-      }
-      if (in) put_row(a.r, v, c, s);
+    if (w == 0 && in) {
+      for (int k = 1; k < W; ++k) s += sums[k][lane];
+      s *= a.r.scale;
+      *p = a.r.add ? old + s : s;
     }
     __syncthreads();
   }
@@ -573,14 +597,19 @@ __global__ __launch_bounds__(1024) void embed_join_kernel(SumArgs a) {
 template <typename TW, typename TX>
 void run_fwd(const lmhead_embed_desc& d, const Batch& b, const void* W, float scale, void* X, EmbedHeader* hdr, hipStream_t s) {
   const int64_t N = (int64_t)d.R * d.T;
+  constexpr int E = 16 / (int)sizeof(TX);
   int lanes = 0;
-  while (lanes < 6 && (8 << lanes) < d.d) ++lanes;
+  while (lanes < 8 && (E << lanes) < d.d) ++lanes;
+  const int64_t parts = (d.d + E * 256 - 1) / (E * 256);
   const bool reports = N <= kReportSlots;
-  int64_t wgs = (N + (256 >> lanes) - 1) / (256 >> lanes);
-  if (wgs > 65536) wgs = 65536;
+  const int64_t units = lanes == 8 ? N * parts : (N + (256 >> lanes) - 1) / (256 >> lanes), wgs = (units + kLookup - 1) / kLookup;
   if (!reports) hipLaunchKernelGGL(embed_clear_kernel, dim3(1), dim3(1), 0, s, hdr);
-  hipLaunchKernelGGL((embed_fwd_kernel<TW, TX>), dim3((unsigned)wgs + reports), dim3(256), 0, s, b, static_cast<const TW*>(W), d.ldW, d.d,
-                     scale, static_cast<TX*>(X), d.ldX, hdr, lanes, reports);
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(wgs + reports)), dim3(256), 0, s, b, static_cast<const TW*>(W), d.ldW, d.d, scale,
+                       static_cast<TX*>(X), d.ldX, hdr, lanes, (uint32_t)parts, reports);
+  };
+  if (lanes == 8) go(embed_fwd_kernel<TW, TX, true>);
+  else go(embed_fwd_kernel<TW, TX, false>);
 }
 
 }  // namespace
@@ -653,15 +682,17 @@ hipError_t launch_embed_bwd(const lmhead_embed_desc& d, const void* gX, const in
   a.chunks = L.chunks;
   a.V = d.V;
   a.part = reinterpret_cast<float*>(ws + L.part);
-  a.list = reinterpret_cast<int32_t*>(ws + L.list);
+  a.ld_part = L.ld_part;
+  a.list = reinterpret_cast<LongId*>(ws + L.list);
   a.hdr = hdr;
-  const unsigned cols = (unsigned)((d.d + 511) / 512), waves = cols < 4 ? cols : 4;
-  const dim3 grid((unsigned)L.chunks, (cols + waves - 1) / waves);
+  const int cols = (d.d + 511) / 512, waves = cols < 4 ? cols : 4;
+  a.col_groups = (cols + waves - 1) / waves;
+  const dim3 grid((unsigned)(L.chunks * a.col_groups));
   if (bf16) hipLaunchKernelGGL(embed_sum_kernel<__bf16>, grid, dim3(64 * waves), 0, s, a);
   else hipLaunchKernelGGL(embed_sum_kernel<float>, grid, dim3(64 * waves), 0, s, a);
   // an id is long from two chunks' slots on
   const int64_t most = L.N / (2 * L.C) + 1;
-  hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)(most < 64 ? most : 64), cols), dim3(1024), 0, s, a);
+  hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)(most < 512 ? most : 512) * ((d.d + 255) / 256)), dim3(64 * kJoinWaves), 0, s, a);
   return hipGetLastError();
 }
 

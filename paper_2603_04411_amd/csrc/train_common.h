@@ -37,6 +37,7 @@ hipError_t launch_preference(const lmhead_preference& q, const float* lp, const 
 constexpr int kSortTile = 1024;      // slots per workgroup of a sorting pass
 constexpr int kSortBits = 9;         // digits have at most so many bits
 constexpr int kScanTiles = 64;       // up to so many tiles each adds up the counts of all of them itself
+constexpr int kLongIdBytes = 16;
 constexpr int kFewSlots = 2048;      // up to so many slots the gradient is one launch without a sort
 constexpr int kReportSlots = 4096;   // up to so many slots one workgroup of the lookup reports the errors of all
 
@@ -53,6 +54,7 @@ struct EmbedLayout {
   int bits, passes, digit;   // bits of a key (ids and V, the key of a slot that does not count), sorting passes, bits of a pass
   int64_t tiles, chunks;
   int C;                     // sorted slots per chunk of the sums
+  int64_t ld_part;           // row pitch of the partial sums: a line more than d, or rows a power of two apart meet on one memory channel
   size_t hdr, key[2], slot[2], hist, list, part, total;
 };
 static inline EmbedLayout embed_layout(const lmhead_embed_desc* d) {
@@ -82,8 +84,9 @@ static inline EmbedLayout embed_layout(const lmhead_embed_desc* d) {
   for (int i = 0; i < 2; ++i) L.key[i] = take((size_t)L.N * 4);
   for (int i = 0; i < 2; ++i) L.slot[i] = take((size_t)L.N * 4);
   L.hist = take(((size_t)L.tiles << L.digit) * 4 + ((size_t)4 << L.digit));   // [digit][tile], then the totals
-  L.list = take((size_t)room * 4);
-  L.part = take((size_t)room * 2 * d->d * 4);              // [chunk]{of an id that began earlier, of one that goes on}[d]
+  L.list = take((size_t)room * kLongIdBytes);
+  L.ld_part = d->d + 32;
+  L.part = take((size_t)room * 2 * L.ld_part * 4);              // [chunk]{of an id that began earlier, of one that goes on}[d]
   L.total = off;
   return L;
 }

@@ -160,7 +160,7 @@ def test_sorted_ids_that_end_around_the_edges_of_the_pieces(d, N, piece):
     backward(1, N, d, int(tok.max()) + 2, "f32" if piece % 2 else "bf16", tok[perm].astype(np.int32), None, add=piece % 3 == 0)
 
 
-@pytest.mark.parametrize("piece", [1, 63, 64, 65, 127, 128, 129, 191, 192, 193, 70000])
+@pytest.mark.parametrize("piece", [1, 63, 64, 65, 127, 128, 129, 191, 192, 193, 511, 512, 513, 575, 576, 577, 640, 703, 1100, 4133, 70000, 600000])
 def test_pieces_of_64(piece):
     N = 530003
     tok = (np.random.default_rng(piece).permutation(N) // piece).astype(np.int32)
