@@ -341,7 +341,8 @@ LMHEAD_API int embed_bwd(const lmhead_embed_desc* desc, const void* gX, const in
  *        of an output with an input or an output is refused (LMHEAD_E_SHAPE).
  *   ws   grad_workspace_bytes() bytes, 256-byte aligned
  * The arrays are read during the call and not kept; the call may be captured into a graph, which then holds the pointers.
- * LMHEAD_E_SHAPE also for max_norm < 0 or NaN, for eps < 0 or not finite, for more than 2^37 elements in a tensor.
+ * LMHEAD_E_SHAPE also for max_norm < 0 or NaN, for eps < 0 or not finite, for more than 2^37 elements in a tensor
+ * or 2^41 in all.
  */
 typedef struct lmhead_tensor {
   void* data;         /* device memory                    */

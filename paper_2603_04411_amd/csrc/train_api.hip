@@ -41,13 +41,15 @@ int validate_preference(const lmhead_preference* q) {
 }
 
 int validate_tensors(const lmhead_tensor* t, int32_t count) {
+  int64_t chunks = 0;
   for (int i = 0; i < count; ++i) {
     if (t[i].n < 0 || t[i].n > kGradMost || t[i].reserved != 0) return LMHEAD_E_SHAPE;
     if (!known(t[i].dtype)) return LMHEAD_E_DTYPE;
     if (t[i].n > 0 && !t[i].data) return LMHEAD_E_NULL;
     if (!aligned(t[i].data, element_bytes(t[i].dtype))) return LMHEAD_E_ALIGN;
+    chunks += (t[i].n + kGradChunk - 1) / kGradChunk;
   }
-  return LMHEAD_OK;
+  return chunks <= kGradChunks ? LMHEAD_OK : LMHEAD_E_SHAPE;
 }
 
 struct Span {

@@ -97,12 +97,21 @@ hipError_t launch_embed_bwd(const lmhead_embed_desc& d, const void* gX, const in
 
 // ---- gradient norm and clipping (lmhead_grad.hip) -----------------------------------------
 
-constexpr int kGradParts = 2048;     // workgroups, each with a partial sum, that one call's norm is shared by (at least one a launch)
 constexpr int kGradTensors = 96;     // tensors whose table one launch carries in its arguments
 constexpr int kGradCount = 65536;    // tensors of one call
-constexpr int64_t kGradMost = 1ll << 37;   // elements of a tensor; kGradTensors times its chunks fit 31 bits
-constexpr int kGradLaunches = (kGradCount + kGradTensors - 1) / kGradTensors;
-static inline size_t grad_ws_bytes() { return (size_t)(kGradParts + kGradLaunches) * sizeof(double) + 256; }
+constexpr int kGradChunk = 8192;     // elements
+constexpr int kClipParts = 4;        // workgroups of the scaling pass per chunk
+constexpr int64_t kGradMost = 1ll << 37;   // elements of a tensor
+constexpr int64_t kGradChunks = 1ll << 28; // chunks of a call
+constexpr int kGradSpread = 2048;    // from twice so many chunks on a workgroup of the first pass takes several,
+constexpr int kGradEach = 16;        // up to so many,
+constexpr int kGradParts = 16384;    // and more where the partial sums would be more than these
+constexpr int kGradShared = 512;     // up to so many partial sums every workgroup of the second pass adds up itself
+constexpr int kFewChunk = 2048;      // elements of a chunk where the call is one workgroup:
+constexpr int kGradFew = 48;         // up to so many of those
+constexpr int kGradEntryBytes = 32;
+static inline size_t grad_table_bytes() { return round_up((size_t)kGradCount * kGradEntryBytes, 256); }
+static inline size_t grad_ws_bytes() { return grad_table_bytes() + (size_t)kGradParts * (sizeof(double) + sizeof(int32_t)); }
 hipError_t launch_grads(const lmhead_tensor* g, const lmhead_tensor* out, int count, bool clip, float max_norm, float eps, float* norm,
                         char* ws, hipStream_t s);
 

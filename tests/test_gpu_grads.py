@@ -78,7 +78,7 @@ def test_addresses_that_are_not_aligned(shift):
     check(ts, None, 1.0, in_place=True)
 
 
-@pytest.mark.parametrize("count", [95, 96, 97, 192, 193, 500])
+@pytest.mark.parametrize("count", [47, 48, 49, 95, 96, 97, 164, 165, 192, 193, 328, 329, 500])
 def test_more_tensors_than_one_launch_takes(count):
     r = np.random.default_rng(count)
     ts = [tensor(int(n), "bf16" if i % 3 else "f32", i) for i, n in enumerate(np.exp(r.uniform(0, 9, count)).astype(int))]
