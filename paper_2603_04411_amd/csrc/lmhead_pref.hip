@@ -1,4 +1,8 @@
-// Preference loss: one pass over the log-probabilities for the sums of the responses, one over the gradient.
+// Preference loss: one pass over the log-probabilities for the sums of the responses, one over the gradient, whose last workgroup adds up
+// loss and statistics; of few tokens both in one workgroup.  A token is 4 bytes in (8 with a reference) and 4 out, its arithmetic two
+// additions: up to a million tokens what it takes is launches and the latency of their first loads, so
+//  - a response's pairs are looked at by one wavefront, which counts by ballots and meets the others at one barrier;
+//  - loads leave before the length that they are masked by has arrived.
 #include "train_common.h"
 
 namespace lmhead {
@@ -16,16 +20,6 @@ __device__ inline int wave_sum(int x) {
   return x;
 }
 
-// Sum over a 256-thread block, valid in every thread; sh[4] is free again after the next barrier.
-template <typename T>
-__device__ inline T block_sum(T x, T* sh) {
-  x = wave_sum(x);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = x;
-  __syncthreads();
-  return (sh[0] + sh[1]) + (sh[2] + sh[3]);
-}
-
 struct PrefArgs {
   const float* lp;
   const float* lr;
@@ -33,160 +27,313 @@ struct PrefArgs {
   const int32_t* len;
   int P, G, T, nb;
   lmhead_preference q;
-  double* sums;
-  int32_t* rank;
-  double* part;
-  int32_t* done;
+  double2* sums;       // [response][block]{log-ratio, log-probability}
+  int2* rank;          // [response]{pairs in which it is preferred, best | worst << 1}
+  double* part;        // [response]{loss, u > 0, beta s_a, beta s_b} of those pairs
+  int32_t* done;       // responses that have left theirs
+  int32_t* pairs;      // pairs of all prompts, where pref_count_kernel has added them up
   float* loss;
   float* g;
   float* ratio;
   float* stats;
 };
 
-// Block (r, b): sums over its slots of response r; b = 0 also places r among its prompt's rewards.
-__global__ __launch_bounds__(256) void pref_sum_kernel(PrefArgs a) {
-  __shared__ double sh[4];
-  __shared__ int shi[4];
-  const int r = blockIdx.x / a.nb, b = blockIdx.x % a.nb;
-  if (blockIdx.x == 0 && threadIdx.x == 0) *a.done = 0;
-  const int n = min(max(a.len[r], 0), a.T);
-  double s = 0.0, l = 0.0;
-  const int t0 = b * kLossSlotsPerBlock;
-  for (int t = t0 + threadIdx.x; t < min(t0 + kLossSlotsPerBlock, n); t += 256) {
-    const int64_t i = (int64_t)r * a.T + t;
-    const double x = a.lp[i];
-    l += x;
-    s += a.lr ? x - (double)a.lr[i] : x;
+__device__ inline int length(const PrefArgs& a, int r) { return min(max(a.len[r], 0), a.T); }
+__device__ inline double per_token(const PrefArgs& a, int r) {
+  const int n = length(a, r);
+  return n > 0 ? 1.0 / n : 0.0;
+}
+
+// Sums of thread t's share (t, t + step, ..) of slots t0 .. t0 + U * step of response r.
+template <int U>
+__device__ inline double2 slot_sums(const PrefArgs& a, int r, int n, int t0, int t, int step) {
+  const float* lp = a.lp + (int64_t)r * a.T;
+  const float* lr = a.lr ? a.lr + (int64_t)r * a.T : nullptr;
+  float x[U], y[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int i = t0 + u * step + t;
+    x[u] = i < a.T ? lp[i] : 0.f;
+    y[u] = lr && i < a.T ? lr[i] : 0.f;
   }
-  s = block_sum(s, sh);
-  l = block_sum(l, sh);
-  if (threadIdx.x == 0) {
-    a.sums[((int64_t)r * a.nb + b) * 2] = s;
-    a.sums[((int64_t)r * a.nb + b) * 2 + 1] = l;
-  }
-  if (b != 0) return;
+  double2 s = {0.0, 0.0};
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (t0 + u * step + t < n) {
+      s.x += (double)x[u] - (double)y[u];
+      s.y += (double)x[u];
+    }
+  return s;
+}
+
+// Where r stands among its prompt's rewards; one wavefront.
+__device__ inline int2 rank_of(const PrefArgs& a, int r, int lane) {
   const int first = r / a.G * a.G;
   const float mine = a.reward[r];
   int less = 0, before = 0, after = 0;   // how many have less, come before r as the best, come before r as the worst
-  for (int c = first + threadIdx.x; c < first + a.G; c += 256) {
-    const float x = a.reward[c];
-    less += x < mine;
-    before += x > mine || (x == mine && c < r);
-    after += x < mine || (x == mine && c < r);
+  for (int c0 = 0; c0 < a.G; c0 += 64) {
+    const int c = first + c0 + lane;
+    const bool have = c0 + lane < a.G;
+    const float x = have ? a.reward[c] : 0.f;
+    less += __popcll(__ballot(have && x < mine));
+    before += __popcll(__ballot(have && (x > mine || (x == mine && c < r))));
+    after += __popcll(__ballot(have && (x < mine || (x == mine && c < r))));
   }
-  less = block_sum(less, shi);
-  before = block_sum(before, shi);
-  after = block_sum(after, shi);
-  if (threadIdx.x == 0) {
-    const bool number = mine == mine;
-    const int best = number && before == 0, worst = number && after == 0;
-    a.rank[2 * r] = a.q.pairs == LMHEAD_PAIRS_ALL ? less : (best && less > 0);
-    a.rank[2 * r + 1] = best | worst << 1;
-  }
+  const bool number = mine == mine;
+  const int best = number && before == 0, worst = number && after == 0;
+  return {a.q.pairs == LMHEAD_PAIRS_ALL ? less : best && less > 0, best | worst << 1};
 }
 
-// Block (r, b): dloss/dlogp on its slots of response r; b = 0 also what the pairs with r preferred add to loss and stats, and
-// the last block sums those.
-__global__ __launch_bounds__(256) void pref_grad_kernel(PrefArgs a) {
-  __shared__ double sh[4];
-  __shared__ long long shl[4];
-  __shared__ int last;
-  const lmhead_preference q = a.q;
-  const int r = blockIdx.x / a.nb, b = blockIdx.x % a.nb, R = a.P * a.G;
+// What the pairs with r come to: w times the slope of its log-ratio, and of those in which it is preferred the number, how often u > 0,
+// the loss and the sum of the others' log-ratios.  One wavefront; `total`: pairs of all prompts (weights = 1).
+struct Outcome {
+  double w, slope, loss, other;
+  int won, hit;
+};
+template <typename Ratio, typename Rank>
+__device__ inline Outcome outcome(const PrefArgs& a, int r, double sr, int lane, Ratio&& ratio, Rank&& rank, int64_t total) {
+  const lmhead_preference& q = a.q;
   const int first = r / a.G * a.G;
-  auto response = [&](int c, int which) {
-    double s = 0.0;
-    for (int k = 0; k < a.nb; ++k) s += a.sums[((int64_t)c * a.nb + k) * 2 + which];
-    return s;
-  };
-  auto per_token = [&](int c) {
-    const int n = min(max(a.len[c], 0), a.T);
-    return n > 0 ? 1.0 / n : 0.0;
-  };
-  // pairs: of the prompt, or of all prompts
-  double pairs = 0.0;
-  for (int c = (q.weights ? 0 : first) + (int)threadIdx.x; c < (q.weights ? R : first + a.G); c += 256) pairs += a.rank[2 * c];
-  pairs = block_sum(pairs, sh);
-  const double w = pairs > 0.0 ? 1.0 / (q.weights ? pairs : pairs * a.P) : 0.0;
-
-  const double sr = response(r, 0) * (q.mean ? per_token(r) : 1.0), like = response(r, 1) * per_token(r);
+  const bool all = q.pairs == LMHEAD_PAIRS_ALL;
   const double beta = q.beta, smooth = q.smoothing;
   const float mine = a.reward[r];
-  const int best_r = a.rank[2 * r + 1];
-  double du = 0.0, won = 0.0, l = 0.0, hit = 0.0, other = 0.0;
-  for (int c = first + threadIdx.x; c < first + a.G; c += 256) {
-    const float x = a.reward[c];
-    const int best_c = a.rank[2 * c + 1];
-    const bool up = mine > x && (q.pairs == LMHEAD_PAIRS_ALL || ((best_r & 1) && (best_c & 2)));
-    const bool down = x > mine && (q.pairs == LMHEAD_PAIRS_ALL || ((best_c & 1) && (best_r & 2)));
-    if (!up && !down) continue;
-    const double sc = response(c, 0) * (q.mean ? per_token(c) : 1.0);
-    const double u = up ? sr - sc : sc - sr;
-    double h = beta * u - q.margin;
-    if (q.margin_scale != 0.f) h -= (double)q.margin_scale * (up ? (double)mine - x : (double)x - mine);
-    double each, d;
-    if (q.loss == LMHEAD_PREF_LOGISTIC) {
-      // e^-|h| once: log(1 + e^-|h|) for both logarithms, and sigma(-h) from it without overflow
-      const double e = exp(-fabs(h)), soft = log1p(e), small = e / (1.0 + e);
-      each = (1.0 - smooth) * (fmax(-h, 0.0) + soft);
-      if (smooth != 0.0) each += smooth * (fmax(h, 0.0) + soft);
-      d = beta * (smooth - (h > 0.0 ? small : 1.0 - small));
-    } else if (q.loss == LMHEAD_PREF_HINGE) {
-      each = h >= 1.0 ? 0.0 : 1.0 - h;     // NaN stays
-      d = h >= 1.0 ? 0.0 : -beta;
-    } else {
-      const double e = h / beta - 0.5 / beta;
-      each = e * e;
-      d = 2.0 * e;
+  const int place = rank(r).y;
+  double du = 0.0, l = 0.0, other = 0.0;
+  int won = 0, hit = 0;
+  int pairs = 0;
+  for (int c0 = 0; c0 < a.G; c0 += 64) {
+    const int c = first + c0 + lane;
+    const bool have = c0 + lane < a.G;
+    const float x = have ? a.reward[c] : mine;
+    const int2 k = have ? rank(c) : int2{0, 0};
+    pairs += k.x;
+    const bool up = mine > x && (all || ((place & 1) && (k.y & 2))), down = x > mine && (all || ((k.y & 1) && (place & 2)));
+    const double sc = have ? ratio(c) : 0.0, u = up ? sr - sc : sc - sr;   // (asked for without waiting for the rewards)
+    if (up || down) {
+      double h = beta * u - q.margin;
+      if (q.margin_scale != 0.f) h -= (double)q.margin_scale * (up ? (double)mine - x : (double)x - mine);
+      double each, d;
+      if (q.loss == LMHEAD_PREF_LOGISTIC) {
+        // e^-|h| once: log(1 + e^-|h|) for both logarithms, and sigma(-h) from it without overflow
+        const double e = exp(-fabs(h)), soft = log1p(e), small = e / (1.0 + e);
+        each = (1.0 - smooth) * (fmax(-h, 0.0) + soft);
+        if (smooth != 0.0) each += smooth * (fmax(h, 0.0) + soft);
+        d = beta * (smooth - (h > 0.0 ? small : 1.0 - small));
+      } else if (q.loss == LMHEAD_PREF_HINGE) {
+        each = h >= 1.0 ? 0.0 : 1.0 - h;     // NaN stays
+        d = h >= 1.0 ? 0.0 : -beta;
+      } else {
+        const double e = h / beta - 0.5 / beta;
+        each = e * e;
+        d = 2.0 * e;
+      }
+      du += up ? d : -d;
+      if (up) {
+        l += each;
+        other += sc;
+      }
     }
-    du += up ? d : -d;
-    if (up) {
-      won += 1.0;
-      l += each;
-      hit += u > 0.0 ? 1.0 : 0.0;
-      other += sc;
-    }
+    won += __popcll(__ballot(up));
+    hit += __popcll(__ballot(up && u > 0.0));
   }
-  du = block_sum(du, sh);
-  won = block_sum(won, sh);
-  if (a.g) {
-    double g = w * du * (q.mean ? per_token(r) : 1.0);
-    if (q.nll_coef != 0.f) g -= w * won * q.nll_coef * per_token(r);
-    const float gf = (float)g;
-    const int n = min(max(a.len[r], 0), a.T), t0 = b * kLossSlotsPerBlock;
-    for (int t = t0 + threadIdx.x; t < min(t0 + kLossSlotsPerBlock, a.T); t += 256) a.g[(int64_t)r * a.T + t] = t < n ? gf : 0.f;
+  const int64_t m = q.weights ? total : (int64_t)wave_sum(pairs) * a.P;
+  const double w = m > 0 ? 1.0 / (double)m : 0.0;
+  return {w, w * wave_sum(du), wave_sum(l), wave_sum(other), won, hit};
+}
+
+// dloss/dlogp of every slot of r.
+__device__ inline float slot_gradient(const PrefArgs& a, int r, const Outcome& o) {
+  const double each = per_token(a, r);
+  double g = o.slope * (a.q.mean ? each : 1.0);
+  if (a.q.nll_coef != 0.f) g -= o.w * o.won * a.q.nll_coef * each;
+  return (float)g;
+}
+
+// What r adds to loss and stats.
+__device__ inline void contribution(const PrefArgs& a, int r, const Outcome& o, double ratio, double logp_sum, double (&p)[4]) {
+  double l = o.loss;
+  if (a.q.nll_coef != 0.f && o.won > 0) l -= o.won * a.q.nll_coef * (logp_sum * per_token(a, r));
+  p[0] = o.w * l;
+  p[1] = o.hit;
+  p[2] = o.won > 0 ? a.q.beta * ratio * o.won : 0.0;
+  p[3] = (double)a.q.beta * o.other;
+}
+
+__device__ inline void put_results(const PrefArgs& a, const double (&v)[4], double pairs) {
+  a.loss[0] = (float)v[0];
+  if (!a.stats) return;
+  const double inv = pairs > 0.0 ? 1.0 / pairs : 0.0;
+#pragma unroll
+  for (int k = 1; k < 4; ++k) a.stats[k - 1] = (float)(v[k] * inv);
+  a.stats[3] = (float)pairs;
+}
+
+// Block (r, b): sums over its slots of response r; b = 0 also places r among its prompt's rewards.
+__global__ __launch_bounds__(256) void pref_sum_kernel(PrefArgs a) {
+  __shared__ double2 sh[4];
+  const int r = blockIdx.x / a.nb, b = blockIdx.x % a.nb, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.done = 0;
+  double2 s = slot_sums<kLossSlotsPerBlock / 256>(a, r, length(a, r), b * kLossSlotsPerBlock, threadIdx.x, 256);
+  if (b == 0 && w == 3) {
+    const int2 k = rank_of(a, r, lane);
+    if (lane == 0) a.rank[r] = k;
   }
-  if (b != 0) return;
-  l = block_sum(l, sh);
-  hit = block_sum(hit, sh);
-  other = block_sum(other, sh);
+  s.x = wave_sum(s.x);
+  s.y = wave_sum(s.y);
+  if (lane == 0) sh[w] = s;
+  __syncthreads();
+  if (threadIdx.x == 0)
+    a.sums[(int64_t)r * a.nb + b] = {(sh[0].x + sh[1].x) + (sh[2].x + sh[3].x), (sh[0].y + sh[1].y) + (sh[2].y + sh[3].y)};
+}
+
+__global__ __launch_bounds__(1024) void pref_count_kernel(PrefArgs a) {
+  __shared__ int sh[16];
+  int m = 0;
+  for (int c = threadIdx.x; c < a.P * a.G; c += 1024) m += a.rank[c].x;
+  m = wave_sum(m);
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = m;
+  __syncthreads();
   if (threadIdx.x == 0) {
-    if (q.nll_coef != 0.f && won > 0.0) l -= won * q.nll_coef * like;
-    double* p = a.part + (int64_t)r * 4;
-    p[0] = w * l;
-    p[1] = hit;
-    p[2] = won > 0.0 ? beta * sr * won : 0.0;
-    p[3] = beta * other;
-    if (a.ratio) a.ratio[r] = (float)sr;
+    m = 0;
+    for (int k = 0; k < 16; ++k) m += sh[k];
+    *a.pairs = m;
   }
 }
 
-__global__ __launch_bounds__(256) void pref_final_kernel(PrefArgs a) {
-  __shared__ double sh[4];
-  const int R = a.P * a.G;
-  double v[4] = {}, m = 0.0;
-  for (int r = threadIdx.x; r < R; r += 256) {
-    for (int c = 0; c < 4; ++c) v[c] += a.part[(int64_t)r * 4 + c];
-    m += a.rank[2 * r];
+// Block (r, b): dloss/dlogp on its slots of response r; b = 0 also what r adds to loss and stats, and the last of those
+// blocks sums all.
+__global__ __launch_bounds__(256) void pref_grad_kernel(PrefArgs a, bool counted) {
+  __shared__ double sh[4][4];
+  __shared__ int shm[4];
+  __shared__ float gs;
+  __shared__ int last;
+  const int r = blockIdx.x / a.nb, b = blockIdx.x % a.nb, R = a.P * a.G, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int n = length(a, r);
+  auto sums = [&](int c) {
+    double2 s = {0.0, 0.0};
+    for (int k0 = 0; k0 < a.nb; k0 += 4) {
+      double2 x[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[k] = a.sums[(int64_t)c * a.nb + min(k0 + k, a.nb - 1)];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (k0 + k < a.nb) {
+          s.x += x[k].x;
+          s.y += x[k].y;
+        }
+    }
+    return s;
+  };
+  auto ratio = [&](int c) { return sums(c).x * (a.q.mean ? per_token(a, c) : 1.0); };
+  if (w == 0) {
+    const double2 mine = sums(r);
+    const double sr = mine.x * (a.q.mean ? per_token(a, r) : 1.0);
+    int64_t total = 0;
+    if (a.q.weights && counted) {
+      total = *a.pairs;
+    } else if (a.q.weights) {
+      int m = 0;
+      for (int c = lane; c < R; c += 64) m += a.rank[c].x;
+      total = wave_sum(m);
+    }
+    const Outcome o = outcome(a, r, sr, lane, ratio, [&](int c) { return a.rank[c]; }, total);
+    // What all have left is added up by the last one here.  Its parts go past the caches (a release fence would first write back
+    // all of g_logp that L2 holds: 20 us), and have arrived when the count goes up.
+    if (b == 0) {
+      double p[4];
+      contribution(a, r, o, sr, mine.y, p);
+      if (lane < 4)
+        __hip_atomic_store(a.part + (int64_t)r * 4 + lane, lane & 2 ? lane & 1 ? p[3] : p[2] : lane & 1 ? p[1] : p[0], __ATOMIC_RELAXED,
+                           __HIP_MEMORY_SCOPE_AGENT);
+    }
+    if (lane == 0) {
+      gs = slot_gradient(a, r, o);
+      if (b == 0 && a.ratio) a.ratio[r] = (float)sr;
+    }
   }
-  for (int c = 0; c < 4; ++c) v[c] = block_sum(v[c], sh);
-  m = block_sum(m, sh);
+  __syncthreads();
+  if (b == 0 && w == 0) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if (lane == 0) last = __hip_atomic_fetch_add(a.done, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == R - 1;
+  }
+  if (a.g) {
+    const float g = gs;
+    const int t0 = b * kLossSlotsPerBlock, t1 = min(t0 + kLossSlotsPerBlock, a.T);
+    for (int t = t0 + threadIdx.x; t < t1; t += 256) a.g[(int64_t)r * a.T + t] = t < n ? g : 0.f;
+  }
+  if (b != 0) return;
+  __syncthreads();
+  if (!last) return;
+  double v[4] = {};
+  int m = 0;
+  for (int c = threadIdx.x; c < R; c += 256) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] += __hip_atomic_load(a.part + (int64_t)c * 4 + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    m += a.rank[c].x;
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = wave_sum(v[k]);
+  m = wave_sum(m);
+  if (lane == 0) {
+    for (int k = 0; k < 4; ++k) sh[w][k] = v[k];
+    shm[w] = m;
+  }
+  __syncthreads();
   if (threadIdx.x != 0) return;
-  a.loss[0] = (float)v[0];
-  if (!a.stats) return;
-  const double inv = m > 0.0 ? 1.0 / m : 0.0;
-  for (int c = 1; c < 4; ++c) a.stats[c - 1] = (float)(v[c] * inv);
-  a.stats[3] = (float)m;
+  for (int k = 0; k < 4; ++k) v[k] = (sh[0][k] + sh[1][k]) + (sh[2][k] + sh[3][k]);
+  put_results(a, v, (double)(shm[0] + shm[1] + shm[2] + shm[3]));
+}
+
+// Few responses of few tokens: one workgroup, a wavefront per response.
+__global__ __launch_bounds__(1024) void pref_few_kernel(PrefArgs a) {
+  constexpr int U = 8;
+  __shared__ double2 sums[kPrefFewResponses];
+  __shared__ int2 rank[kPrefFewResponses];
+  __shared__ double part[kPrefFewResponses][4];
+  const int R = a.P * a.G, lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  for (int r = w; r < R; r += 16) {
+    const int n = length(a, r);
+    double2 s = {0.0, 0.0};
+    for (int t0 = 0; t0 < a.T; t0 += 64 * U) {
+      const double2 x = slot_sums<U>(a, r, n, t0, lane, 64);
+      s.x += x.x;
+      s.y += x.y;
+    }
+    s.x = wave_sum(s.x);
+    s.y = wave_sum(s.y);
+    const int2 k = rank_of(a, r, lane);
+    if (lane == 0) {
+      sums[r] = s;
+      rank[r] = k;
+    }
+  }
+  __syncthreads();
+  int m = 0;
+  for (int c = lane; c < R; c += 64) m += rank[c].x;
+  m = wave_sum(m);
+  auto ratio = [&](int c) { return sums[c].x * (a.q.mean ? per_token(a, c) : 1.0); };
+  for (int r = w; r < R; r += 16) {
+    const double sr = ratio(r);
+    const Outcome o = outcome(a, r, sr, lane, ratio, [&](int c) { return rank[c]; }, m);
+    const float g = slot_gradient(a, r, o);
+    const int n = length(a, r);
+    if (a.g)
+      for (int t = lane; t < a.T; t += 64) a.g[(int64_t)r * a.T + t] = t < n ? g : 0.f;
+    if (lane == 0) {
+      double p[4];
+      contribution(a, r, o, sr, sums[r].y, p);
+      for (int k = 0; k < 4; ++k) part[r][k] = p[k];
+      if (a.ratio) a.ratio[r] = (float)sr;
+    }
+  }
+  __syncthreads();
+  if (w != 0) return;
+  double v[4] = {};
+  for (int c = lane; c < R; c += 64)
+    for (int k = 0; k < 4; ++k) v[k] += part[c][k];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = wave_sum(v[k]);
+  if (lane == 0) put_results(a, v, (double)m);
 }
 
 }  // namespace
@@ -195,18 +342,25 @@ hipError_t launch_preference(const lmhead_preference& q, const float* lp, const 
                              int P, int G, int T, float* loss, float* g, float* ratio, float* stats, char* ws, hipStream_t s) {
   const PrefLayout L = pref_layout(P, G, T);
   PrefArgs a{lp, lr, reward, len, P, G, T, (int)L.nb, q};
-  a.sums = reinterpret_cast<double*>(ws + L.sums);
-  a.rank = reinterpret_cast<int32_t*>(ws + L.rank);
+  a.sums = reinterpret_cast<double2*>(ws + L.sums);
+  a.rank = reinterpret_cast<int2*>(ws + L.rank);
   a.part = reinterpret_cast<double*>(ws + L.part);
   a.done = reinterpret_cast<int32_t*>(ws + L.done);
+  a.pairs = a.done + 1;
   a.loss = loss;
   a.g = g;
   a.ratio = ratio;
   a.stats = stats;
+  if (L.R <= kPrefFewResponses && L.R * T <= kPrefFewSlots) {
+    hipLaunchKernelGGL(pref_few_kernel, dim3(1), dim3(1024), 0, s, a);
+    return hipGetLastError();
+  }
   const dim3 grid((unsigned)(L.R * L.nb));
   hipLaunchKernelGGL(pref_sum_kernel, grid, dim3(256), 0, s, a);
-  hipLaunchKernelGGL(pref_grad_kernel, grid, dim3(256), 0, s, a);
-  hipLaunchKernelGGL(pref_final_kernel, dim3(1), dim3(256), 0, s, a);
+  // every workgroup adds up the pairs of few prompts itself
+  const bool counted = q.weights && L.R > kPrefCounted;
+  if (counted) hipLaunchKernelGGL(pref_count_kernel, dim3(1), dim3(1024), 0, s, a);
+  hipLaunchKernelGGL(pref_grad_kernel, grid, dim3(256), 0, s, a, counted);
   return hipGetLastError();
 }
 

@@ -8,6 +8,10 @@ namespace lmhead {
 
 // ---- preference loss (lmhead_pref.hip) --------------------------------------------------
 
+constexpr int kPrefFewResponses = 64;   // up to so many responses
+constexpr int kPrefFewSlots = 8192;     // and slots the loss is one workgroup
+constexpr int kPrefCounted = 1024;      // up to so many responses each workgroup counts all pairs itself
+
 struct PrefLayout {
   int64_t R, nb;         // responses, blocks of kLossSlotsPerBlock slots in one
   size_t done, sums, rank, part, total;
@@ -23,9 +27,9 @@ static inline PrefLayout pref_layout(int64_t P, int64_t G, int64_t T) {
     return o;
   };
   L.done = take(256);
-  L.sums = take((size_t)(L.R * L.nb) * 2 * sizeof(double));   // [response][block]{log-ratio, log-prob}
-  L.rank = take((size_t)L.R * 2 * sizeof(int32_t));           // [response]{pairs in which it is preferred, best | worst << 1}
-  L.part = take((size_t)L.R * 4 * sizeof(double));            // [response]{loss, u > 0, beta s_a, beta s_b} of those pairs
+  L.sums = take((size_t)(L.R * L.nb) * 2 * sizeof(double));
+  L.rank = take((size_t)L.R * 2 * sizeof(int32_t));
+  L.part = take((size_t)L.R * 4 * sizeof(double));
   L.total = off;
   return L;
 }

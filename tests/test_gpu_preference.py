@@ -68,10 +68,12 @@ def test_every_form(loss, extremes, mean, per_pair):
 
 
 @pytest.mark.parametrize("P,G,T", [(1, 1, 1), (1, 2, 1), (2, 2, 2), (1, 2, 2047), (1, 2, 2048), (1, 2, 2049), (3, 3, 4097), (300, 2, 5),
+                                   (2, 4, 1024), (2, 4, 1025), (32, 2, 128), (33, 2, 124), (32, 2, 129), (512, 2, 3), (513, 2, 3),
                                    (1, 63, 3), (1, 64, 3), (1, 65, 3), (2, 255, 2), (1, 257, 2), (2, 300, 1), (1, 700, 2), (17, 16, 130)])
 def test_sizes(P, G, T):
     check(P, G, T, 11, mean=G > 2, per_pair=T % 2 == 0, nll_coef=0.1)
     check(P, G, T, 12, extremes=True, loss="squared", margin=0.1, use_ref=False)
+    check(P, G, T, 13, per_pair=T % 2 == 1, lens=[T] * (P * G))
 
 
 def test_lengths_of_none_one_and_out_of_range():
