@@ -281,9 +281,9 @@ struct Fill {
   float* p;
   int64_t lo, hi;
 };
-constexpr int kFillEach = 1024;    // floats per workgroup
+template <int kThreads = 256>
 __device__ inline void fill(const Fill& f, int64_t block) {
-  const int64_t i = f.lo + block * kFillEach + threadIdx.x * 4;
+  const int64_t i = f.lo + (block * kThreads + threadIdx.x) * 4;    // one store per thread: 6.9 TB/s, in a loop 5.5
   if (i < f.hi) *reinterpret_cast<f32x4*>(f.p + i) = f32x4{0.f, 0.f, 0.f, 0.f};
 }
 
@@ -439,6 +439,94 @@ __global__ __launch_bounds__(256) void sort_place_kernel(SortArgs a) {
     }
   }
   if (a.first && err) atomicOr(&a.hdr->err, err);
+}
+
+// ---- the sort of a few tiles ---------------------------------------------------------------
+
+// Up to kMergeTiles tiles take two launches instead of two per digit: each tile is sorted by itself, then each slot looks up how
+// many slots of every other tile come before it.  The gradient of 3000 / 8192 / 12000 / 16384 rows of 64, added to 152064 ids: 19 / 24 / 27 /
+// 31 us, by digits 26 / 29 / 32 / 32; of 32768 48 and 41.
+
+// A tile's values id << 10 | place in the tile, ascending; one value per thread.  Bitonic: exchanges over less than 64 places stay in a
+// wavefront.
+__global__ __launch_bounds__(kSortTile) void tile_sort_kernel(SortArgs a) {
+  __shared__ uint32_t sh[kSortTile];
+  __shared__ int bits[kSortTile / 64];
+  if ((int)blockIdx.x >= a.tiles) return fill<kSortTile>(a.f, blockIdx.x - a.tiles);
+  const uint32_t t = threadIdx.x, i = blockIdx.x * (uint32_t)kSortTile + t;
+  int err = 0;
+  uint32_t x = i < a.N ? id_of(a.b, i, err) << 10 | t : 0xffffffffu;
+  err = wave_or(err);
+  if ((t & 63) == 0) bits[t >> 6] = err;
+#pragma unroll
+  for (uint32_t size = 2; size <= kSortTile; size <<= 1) {
+#pragma unroll
+    for (uint32_t step = size >> 1; step > 0; step >>= 1) {
+      uint32_t y;
+      if (step >= 64) {
+        __syncthreads();
+        sh[t] = x;
+        __syncthreads();
+        y = sh[t ^ step];
+      } else {
+        y = __shfl_xor(x, step);
+      }
+      const bool low = ((t & step) == 0) == ((t & size) == 0);     // this place gets the smaller value
+      x = low ? (x < y ? x : y) : (x < y ? y : x);
+    }
+  }
+  if (i < a.N) a.key_out[i] = x;
+  __syncthreads();
+  if (t == 0) {
+    err = 0;
+    for (int k = 0; k < kSortTile / 64; ++k) err |= bits[k];
+    a.hist[blockIdx.x] = err;
+    if (blockIdx.x == 0) a.hdr->nlong = 0;
+  }
+}
+
+// Each workgroup holds all tiles in LDS (eleven dependent steps through each of them would each wait for L2: 26 us for 16 tiles) and places
+// 256 slots (a tile's 1024 are four times the reads of one compute unit's LDS: 19 us).
+__global__ __launch_bounds__(256) void tile_merge_kernel(SortArgs a) {
+  constexpr int U = 4;
+  extern __shared__ __align__(16) uint32_t all[];
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    uint32_t err = 0;
+    for (int q = 0; q < a.tiles; ++q) err |= a.hist[q];
+    a.hdr->err = (int)err;
+  }
+  for (uint32_t i = threadIdx.x * 4; i < (a.N & ~3u); i += 1024) *reinterpret_cast<uint4*>(all + i) = *reinterpret_cast<const uint4*>(a.key + i);
+  if (threadIdx.x < (a.N & 3u)) all[(a.N & ~3u) + threadIdx.x] = a.key[(a.N & ~3u) + threadIdx.x];
+  __syncthreads();
+  const int tile = (int)(blockIdx.x * 256 / kSortTile);
+  const uint32_t i = blockIdx.x * 256u + threadIdx.x;
+  if (i >= a.N) return;
+  const uint32_t x = all[i], id = x >> 10;
+  uint32_t p = i % kSortTile;
+  for (int q0 = 0; q0 < a.tiles; q0 += U) {
+    // slots of the same id come first where their tile does
+    uint32_t below[U], n[U], at[U], k[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int q = q0 + u;
+      k[u] = q < a.tiles ? (uint32_t)q * kSortTile : 0;
+      n[u] = q >= a.tiles || q == tile ? 0 : q + 1 < a.tiles ? kSortTile : a.N - k[u];
+      below[u] = (id + (q < tile)) << 10;
+      at[u] = 0;
+    }
+#pragma unroll
+    for (uint32_t step = kSortTile; step > 0; step >>= 1)
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        // read whether it counts or not: a branch would wait for one of the U reads at a time
+        const uint32_t to = at[u] + step, v = all[min(k[u] + to - 1, a.N - 1)];
+        at[u] = ((to <= n[u]) & (v < below[u])) ? to : at[u];
+      }
+#pragma unroll
+    for (int u = 0; u < U; ++u) p += at[u];
+  }
+  a.key_out[p] = id;
+  a.slot_out[p] = (uint32_t)tile * kSortTile + (x & 1023u);
 }
 
 // ---- the sums --------------------------------------------------------------------------
@@ -631,8 +719,9 @@ hipError_t launch_embed_bwd(const lmhead_embed_desc& d, const void* gX, const in
   const Batch b{tok, len, d.R, d.T, d.V};
   const bool add = (d.flags & LMHEAD_FLAG_ACCUM_DW) != 0, bf16 = d.rows == LMHEAD_BF16;
   const Rows r{gX, d.ldX, dW, d.d, scale, add};
-  if (L.N <= kFewSlots) {
-    const int cols = (d.d + 511) / 512, owners = (int)((L.N + 3) / 4) * cols;
+  const int cols = (d.d + 511) / 512;
+  if (L.N <= kFewSlots && L.N * L.N * cols <= kFewWork) {
+    const int owners = (int)((L.N + 3) / 4) * cols;
     int rows_each = 16384 / d.d;
     rows_each = rows_each < 1 ? 1 : rows_each > 64 ? 64 : rows_each;
     const int64_t fills = add ? 0 : ((int64_t)d.V + rows_each - 1) / rows_each;
@@ -653,21 +742,33 @@ hipError_t launch_embed_bwd(const lmhead_embed_desc& d, const void* gX, const in
   so.hist = u32(L.hist);
   so.totals = so.hist + ((int64_t)L.tiles << L.digit);
   so.hdr = hdr;
-  const int launches = L.passes * (so.scanned ? 3 : 2);
-  int launch = 0;
   const int64_t cells = add ? 0 : (int64_t)d.V * d.d;
+  // Where many zeros are written they hide all launches of the sort by digits, but not tile_merge_kernel, whose LDS would leave them few
+  // workgroups.  8192 rows of 1024: 64 MB of zeros 33 us, by digits 42; 125 MB 46 and 51; 594 MB 129 and 122.
+  const bool merged = L.tiles <= kMergeTiles && d.V < (1 << 22) - 1 && cells <= kMergeCells;
+  const int launches = merged ? 1 : L.passes * (so.scanned ? 3 : 2);
+  int launch = 0;
   // one launch of the sort, with its share of the zeros
-  auto go = [&](auto kernel, int64_t wgs) {
+  auto go = [&](auto kernel, int64_t wgs, int threads = 256) {
     so.f = Fill{dW, cells / 8 * launch / launches * 8, cells / 8 * (launch + 1) / launches * 8};
     ++launch;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(wgs + (so.f.hi - so.f.lo + kFillEach - 1) / kFillEach)), dim3(256), 0, s, so);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(wgs + (so.f.hi - so.f.lo + threads * 4 - 1) / (threads * 4))), dim3(threads), 0, s, so);
   };
-  for (int p = 0; p < L.passes; ++p) {
+  auto buffers = [&](int from) {
+    so.key = u32(L.key[from]);
+    so.slot = u32(L.slot[from]);
+    so.key_out = u32(L.key[from ^ 1]);
+    so.slot_out = u32(L.slot[from ^ 1]);
+  };
+  if (merged) {
+    buffers(1);
+    go(tile_sort_kernel, L.tiles, kSortTile);
+    buffers(0);
+    hipLaunchKernelGGL(tile_merge_kernel, dim3((unsigned)((L.N + 255) / 256)), dim3(256), (size_t)L.N * 4, s, so);
+  }
+  for (int p = 0; !merged && p < L.passes; ++p) {
     so.first = p == 0;
-    so.key = u32(L.key[(p + 1) & 1]);
-    so.slot = u32(L.slot[(p + 1) & 1]);
-    so.key_out = u32(L.key[p & 1]);
-    so.slot_out = u32(L.slot[p & 1]);
+    buffers((p & 1) ^ 1);
     so.shift = p * L.digit;
     go(sort_count_kernel, L.tiles);
     if (so.scanned) go(sort_scan_kernel, ((1 << L.digit) + 3) / 4);
@@ -685,7 +786,7 @@ hipError_t launch_embed_bwd(const lmhead_embed_desc& d, const void* gX, const in
   a.ld_part = L.ld_part;
   a.list = reinterpret_cast<LongId*>(ws + L.list);
   a.hdr = hdr;
-  const int cols = (d.d + 511) / 512, waves = cols < 4 ? cols : 4;
+  const int waves = cols < 4 ? cols : 4;
   a.col_groups = (cols + waves - 1) / waves;
   const dim3 grid((unsigned)(L.chunks * a.col_groups));
   if (bf16) hipLaunchKernelGGL(embed_sum_kernel<__bf16>, grid, dim3(64 * waves), 0, s, a);

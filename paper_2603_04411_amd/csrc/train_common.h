@@ -42,7 +42,12 @@ constexpr int kSortTile = 1024;      // slots per workgroup of a sorting pass
 constexpr int kSortBits = 9;         // digits have at most so many bits
 constexpr int kScanTiles = 64;       // up to so many tiles each adds up the counts of all of them itself
 constexpr int kLongIdBytes = 16;
-constexpr int kFewSlots = 2048;      // up to so many slots the gradient is one launch without a sort
+constexpr int kMergeTiles = 16;      // up to so many tiles are sorted by themselves and merged by ranks (64 KB of LDS)
+constexpr int64_t kMergeCells = 64 << 20;   // unless more elements than these are to be zeroed
+// Up to so many slots, and so many (slot, slot, 512 columns), the gradient is one launch without a sort.  Added to 152064 ids, one launch /
+// sorted, us: 1024 x 1024 11 / 23   1024 x 4096 17 / 27   2048 x 1024 20 / 24   2048 x 4096 43 / 28   3000 x 1024 40 / 22.
+constexpr int kFewSlots = 2048;
+constexpr int64_t kFewWork = 12 << 20;
 constexpr int kReportSlots = 4096;   // up to so many slots one workgroup of the lookup reports the errors of all
 
 struct EmbedHeader {
