@@ -160,6 +160,13 @@ def main() -> int:
     ap.add_argument("--fp8-logits", action="store_true",
                     help="variant: logits (forward and recompute) from e4m3 copies of H and W; NOT the headline "
                          "configuration (it changes the numerics), reported for comparison")
+    ap.add_argument("--preference", action="store_true",
+                    help="variant: preference_loss over all ordered pairs of each prompt's rewards in place of the workload's loss")
+    ap.add_argument("--tied", action="store_true",
+                    help="variant: W is the model's input embedding too; the step also looks up the rows of its tokens and adds the "
+                         "lookup's gradient (of dH, as if the model between were the identity) to dW")
+    ap.add_argument("--clip", type=float, default=0.0, metavar="NORM",
+                    help="variant: the step also clips dW, in place, to this norm")
     ap.add_argument("--no-ceiling", action="store_true",
                     help="skip the bare matrix-core loop that is reported next to the nominal peak")
     ap.add_argument("--calibrate-copy", action="store_true",
@@ -222,12 +229,26 @@ def main() -> int:
     dH = torch.empty(N, cfg.d, **f32)
     dW = torch.empty(cfg.V, cfg.d, **f32)
 
+    if args.preference:
+        pref = L.make_preference(beta=0.1)
+        pref_ws = torch.empty(L.preference_workspace_bytes(cfg.P, cfg.G, cfg.T), dtype=torch.uint8, device="cuda")
+    if args.tied:
+        embed = L.make_embed_desc(cfg.R, cfg.T, cfg.d, cfg.V, cfg.dtype)
+        embed_grad = L.make_embed_desc(cfg.R, cfg.T, cfg.d, cfg.V, cfg.dtype, rows="f32", flags=L.FLAG_ACCUM_DW)
+        embed_ws = torch.empty(max(L.embed_workspace_bytes(embed), L.embed_workspace_bytes(embed_grad)), dtype=torch.uint8, device="cuda")
+        X = torch.empty(cfg.N, cfg.d, dtype=W.dtype, device="cuda")
+    if args.clip > 0:
+        grads, norm = L.make_grad_list([dW]), torch.empty(2, **f32)
+        grad_ws = torch.empty(L.grad_workspace_bytes(), dtype=torch.uint8, device="cuda")
+
     def fwd_other():
         if W_old is not None:
             L.lmhead_logprob_fwd(desc, H, W_old, tok_d, lens_d, lp_old, scratch_lse, None, None, None, ws)
         L.lmhead_logprob_fwd(desc, H, W_ref, tok_d, lens_d, lp_ref, scratch_lse, None, None, None, ws)
 
     def step():
+        if args.tied:
+            L.embed_fwd(embed, W, tok_d, lens_d, 1.0, X, embed_ws)
         if cfg.recompute_old_ref and args.separate_forwards:
             L.lmhead_logprob_fwd(desc, H, W, tok_d, lens_d, logp, lse, ent, None, None, ws)
             fwd_other()
@@ -238,7 +259,9 @@ def main() -> int:
             L.lmhead_logprob_fwd_multi(desc, H, mats, tok_d, lens_d, outs, lse, ent, None, None, ws)
         else:
             L.lmhead_logprob_fwd(desc, H, W, tok_d, lens_d, logp, lse, ent, None, None, ws)
-        if cfg.loss == "grpo":
+        if args.preference:
+            L.preference_loss(pref, logp, lp_ref, rew_d, lens_d, cfg.P, cfg.G, cfg.T, loss, g_logp, None, stats, pref_ws)
+        elif cfg.loss == "grpo":
             L.group_advantage(rew_d, cfg.P, cfg.G, 1e-6, 0, adv)
             L.grpo_loss(logp, lp_old, lp_ref, adv, lens_d, cfg.P, cfg.G, cfg.T, cfg.clip_eps, cfg.clip_eps,
                         cfg.kl_coef, 0, loss, g_logp, stats, loss_ws)
@@ -246,6 +269,10 @@ def main() -> int:
             L.flowrl_tb_loss(logp, lp_ref, rew_d, logZ_d, lens_d, cfg.P, cfg.G, cfg.T, cfg.beta, loss, g_logp,
                              g_logZ, None, loss_ws)
         L.lmhead_logprob_bwd(desc, H, W, tok_d, lens_d, lse, g_logp, dH, dW, ws)
+        if args.tied:
+            L.embed_bwd(embed_grad, dH, tok_d, lens_d, 1.0, dW, embed_ws)
+        if args.clip > 0:
+            L.grad_clip(grads, None, args.clip, 1e-6, norm, grad_ws)
 
     if args.calibrate_copy:
         src = torch.zeros(1 << 28, dtype=torch.float32, device="cuda")     # 1 GiB
@@ -324,7 +351,8 @@ def main() -> int:
         "higher_is_better": True, "scaling": "weak", "vs_baseline": None,
         "dtype": cfg.dtype + ("+e4m3 logits" if args.fp8_logits else ""), "data": "synthetic",
         "config": {"workload": f"configs[{cfg.index}] {cfg.name}", "P": cfg.P, "G": cfg.G, "T": cfg.T,
-                   "d": cfg.d, "V": cfg.V, "token_slots": cfg.N, "valid_tokens": nv, "loss": cfg.loss,
+                   "d": cfg.d, "V": cfg.V, "token_slots": cfg.N, "valid_tokens": nv, "loss": "preference" if args.preference else cfg.loss,
+                   **({"tied": True} if args.tied else {}), **({"clip": args.clip, "grad_norm": float(norm[0])} if args.clip > 0 else {}),
                    "vocab_chunk": int(args.vocab_chunk) or "library default",
                    "tokens_counted": "valid (unpadded) tokens", "slots_per_s": cfg.N / (ms_per_step * 1e-3)},
         # executed = 2 N_v V d per matrix-core pass (logits, logits recompute, dH, dW: 8 N_v V d per step
