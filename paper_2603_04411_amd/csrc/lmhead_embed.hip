@@ -726,7 +726,8 @@ hipError_t launch_embed_bwd(const lmhead_embed_desc& d, const void* gX, const in
   const int cols = (d.d + 511) / 512;
   if (L.N <= kFewSlots && L.N * L.N * cols <= kFewWork) {
     const int owners = (int)((L.N + 3) / 4) * cols;
-    int rows_each = 16384 / d.d;
+    // 16 KB of zeros per workgroup, or 32 where it has many ids to look through (64 KB: 5.4 TB/s)
+    int rows_each = (L.N <= 256 ? 4096 : 8192) / d.d;
     rows_each = rows_each < 1 ? 1 : rows_each > 64 ? 64 : rows_each;
     const int64_t fills = add ? 0 : ((int64_t)d.V + rows_each - 1) / rows_each;
     auto go = [&](auto kernel) {

@@ -29,8 +29,8 @@ struct PrefArgs {
   lmhead_preference q;
   double2* sums;       // [response][block]{log-ratio, log-probability}
   int2* rank;          // [response]{pairs in which it is preferred, best | worst << 1}
-  double* part;        // [response]{loss, u > 0, beta s_a, beta s_b} of those pairs
-  int32_t* done;       // responses that have left theirs
+  double* part;        // [response, or four short ones]{loss, u > 0, beta s_a, beta s_b, pairs} where it is preferred
+  int32_t* done;       // workgroups that have left theirs
   int32_t* pairs;      // pairs of all prompts, where pref_count_kernel has added them up
   float* loss;
   float* g;
@@ -150,25 +150,27 @@ __device__ inline float slot_gradient(const PrefArgs& a, int r, const Outcome& o
 }
 
 // What r adds to loss and stats.
-__device__ inline void contribution(const PrefArgs& a, int r, const Outcome& o, double ratio, double logp_sum, double (&p)[4]) {
+constexpr int kParts = 5;
+__device__ inline void contribution(const PrefArgs& a, int r, const Outcome& o, double ratio, double logp_sum, double (&p)[kParts]) {
   double l = o.loss;
   if (a.q.nll_coef != 0.f && o.won > 0) l -= o.won * a.q.nll_coef * (logp_sum * per_token(a, r));
   p[0] = o.w * l;
   p[1] = o.hit;
   p[2] = o.won > 0 ? a.q.beta * ratio * o.won : 0.0;
   p[3] = (double)a.q.beta * o.other;
+  p[4] = o.won;
 }
 
-__device__ inline void put_results(const PrefArgs& a, const double (&v)[4], double pairs) {
+__device__ inline void put_results(const PrefArgs& a, const double (&v)[kParts]) {
   a.loss[0] = (float)v[0];
   if (!a.stats) return;
-  const double inv = pairs > 0.0 ? 1.0 / pairs : 0.0;
+  const double pairs = v[4], inv = pairs > 0.0 ? 1.0 / pairs : 0.0;
 #pragma unroll
   for (int k = 1; k < 4; ++k) a.stats[k - 1] = (float)(v[k] * inv);
   a.stats[3] = (float)pairs;
 }
 
-// Block (r, b): sums over its slots of response r; b = 0 also places r among its prompt's rewards.
+// Long responses: block (r, b) sums its slots of response r; b = 0 also places r among its prompt's rewards.
 __global__ __launch_bounds__(256) void pref_sum_kernel(PrefArgs a) {
   __shared__ double2 sh[4];
   const int r = blockIdx.x / a.nb, b = blockIdx.x % a.nb, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
@@ -186,6 +188,32 @@ __global__ __launch_bounds__(256) void pref_sum_kernel(PrefArgs a) {
     a.sums[(int64_t)r * a.nb + b] = {(sh[0].x + sh[1].x) + (sh[2].x + sh[3].x), (sh[0].y + sh[1].y) + (sh[2].y + sh[3].y)};
 }
 
+// Sums of all slots of response r; one wavefront.
+__device__ inline double2 response_sums(const PrefArgs& a, int r, int lane) {
+  constexpr int U = 8;
+  const int n = length(a, r);
+  double2 s = {0.0, 0.0};
+  for (int t0 = 0; t0 < a.T; t0 += 64 * U) {
+    const double2 x = slot_sums<U>(a, r, n, t0, lane, 64);
+    s.x += x.x;
+    s.y += x.y;
+  }
+  return {wave_sum(s.x), wave_sum(s.y)};
+}
+
+// Short ones: a wavefront per response.
+__global__ __launch_bounds__(256) void pref_sum_short_kernel(PrefArgs a) {
+  const int r = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.done = 0;
+  if (r >= a.P * a.G) return;
+  const double2 s = response_sums(a, r, lane);
+  const int2 k = rank_of(a, r, lane);
+  if (lane == 0) {
+    a.sums[r] = s;
+    a.rank[r] = k;
+  }
+}
+
 __global__ __launch_bounds__(1024) void pref_count_kernel(PrefArgs a) {
   __shared__ int sh[16];
   int m = 0;
@@ -200,15 +228,39 @@ __global__ __launch_bounds__(1024) void pref_count_kernel(PrefArgs a) {
   }
 }
 
-// Block (r, b): dloss/dlogp on its slots of response r; b = 0 also what r adds to loss and stats, and the last of those
-// blocks sums all.
-__global__ __launch_bounds__(256) void pref_grad_kernel(PrefArgs a, bool counted) {
-  __shared__ double sh[4][4];
-  __shared__ int shm[4];
+// Loss and statistics from the n parts that all have left; one workgroup of up to 16 wavefronts.
+__device__ inline void add_up(const PrefArgs& a, int n) {
+  __shared__ double sh[16][kParts];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  double v[kParts] = {};
+  for (int c = threadIdx.x; c < n; c += blockDim.x)
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) v[k] += __hip_atomic_load(a.part + (int64_t)c * kParts + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+  for (int k = 0; k < kParts; ++k) v[k] = wave_sum(v[k]);
+  if (lane == 0)
+    for (int k = 0; k < kParts; ++k) sh[w][k] = v[k];
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  for (int q = 1; q < (int)blockDim.x >> 6; ++q)
+    for (int k = 0; k < kParts; ++k) v[k] += sh[q][k];
+  put_results(a, v);
+}
+
+__global__ __launch_bounds__(1024) void pref_final_kernel(PrefArgs a, int n) { add_up(a, n); }
+
+// dloss/dlogp.  kLong: block (r, b) writes its slots of response r, one wavefront looks at r's pairs, and b = 0 leaves what they add to
+// loss and stats; otherwise a wavefront per response does all that, and the block leaves the sum of its four.  ticket: the last block to
+// leave something adds it all up.
+template <bool kLong>
+__global__ __launch_bounds__(256) void pref_grad_kernel(PrefArgs a, bool counted, bool ticket) {
   __shared__ float gs;
   __shared__ int last;
-  const int r = blockIdx.x / a.nb, b = blockIdx.x % a.nb, R = a.P * a.G, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int n = length(a, r);
+  __shared__ double four[4][kParts];
+  const int R = a.P * a.G, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int r = kLong ? blockIdx.x / a.nb : blockIdx.x * 4 + w, b = kLong ? blockIdx.x % a.nb : 0;
+  const bool have = r < R;
+  const int n = have ? length(a, r) : 0;
   auto sums = [&](int c) {
     double2 s = {0.0, 0.0};
     for (int k0 = 0; k0 < a.nb; k0 += 4) {
@@ -225,7 +277,8 @@ __global__ __launch_bounds__(256) void pref_grad_kernel(PrefArgs a, bool counted
     return s;
   };
   auto ratio = [&](int c) { return sums(c).x * (a.q.mean ? per_token(a, c) : 1.0); };
-  if (w == 0) {
+  float g = 0.f;
+  if (have && (!kLong || w == 0)) {
     const double2 mine = sums(r);
     const double sr = mine.x * (a.q.mean ? per_token(a, r) : 1.0);
     int64_t total = 0;
@@ -237,70 +290,49 @@ __global__ __launch_bounds__(256) void pref_grad_kernel(PrefArgs a, bool counted
       total = wave_sum(m);
     }
     const Outcome o = outcome(a, r, sr, lane, ratio, [&](int c) { return a.rank[c]; }, total);
-    // What all have left is added up by the last one here.  Its parts go past the caches (a release fence would first write back
-    // all of g_logp that L2 holds: 20 us), and have arrived when the count goes up.
     if (b == 0) {
-      double p[4];
+      double p[kParts];
       contribution(a, r, o, sr, mine.y, p);
-      if (lane < 4)
-        __hip_atomic_store(a.part + (int64_t)r * 4 + lane, lane & 2 ? lane & 1 ? p[3] : p[2] : lane & 1 ? p[1] : p[0], __ATOMIC_RELAXED,
-                           __HIP_MEMORY_SCOPE_AGENT);
+      if (lane == 0) {
+        for (int k = 0; k < kParts; ++k) four[w][k] = p[k];
+        if (a.ratio) a.ratio[r] = (float)sr;
+      }
     }
-    if (lane == 0) {
-      gs = slot_gradient(a, r, o);
-      if (b == 0 && a.ratio) a.ratio[r] = (float)sr;
-    }
+    g = slot_gradient(a, r, o);
+    if (kLong && lane == 0) gs = g;
   }
   __syncthreads();
+  // What all have left is added up by the last one here, or by a launch of its own.  It goes past the caches (a release fence would
+  // first write back all of g_logp that L2 holds: 20 us), and has arrived when the count goes up.
   if (b == 0 && w == 0) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    if (lane == 0) last = __hip_atomic_fetch_add(a.done, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == R - 1;
+    if (lane < kParts) {
+      double p = four[0][lane];
+      for (int q = 1; !kLong && q < 4 && (int)blockIdx.x * 4 + q < R; ++q) p += four[q][lane];
+      __hip_atomic_store(a.part + (int64_t)(kLong ? r : (int)blockIdx.x) * kParts + lane, p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    if (ticket) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      if (lane == 0) last = __hip_atomic_fetch_add(a.done, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (kLong ? R : (R + 3) / 4) - 1;
+    }
   }
-  if (a.g) {
-    const float g = gs;
-    const int t0 = b * kLossSlotsPerBlock, t1 = min(t0 + kLossSlotsPerBlock, a.T);
-    for (int t = t0 + threadIdx.x; t < t1; t += 256) a.g[(int64_t)r * a.T + t] = t < n ? g : 0.f;
+  if (a.g && have) {
+    if (kLong) g = gs;
+    const int t0 = b * kLossSlotsPerBlock, t1 = kLong ? min(t0 + kLossSlotsPerBlock, a.T) : a.T;
+    for (int t = t0 + (kLong ? (int)threadIdx.x : lane); t < t1; t += kLong ? 256 : 64) a.g[(int64_t)r * a.T + t] = t < n ? g : 0.f;
   }
-  if (b != 0) return;
+  if (!ticket || b != 0) return;
   __syncthreads();
-  if (!last) return;
-  double v[4] = {};
-  int m = 0;
-  for (int c = threadIdx.x; c < R; c += 256) {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] += __hip_atomic_load(a.part + (int64_t)c * 4 + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    m += a.rank[c].x;
-  }
-#pragma unroll
-  for (int k = 0; k < 4; ++k) v[k] = wave_sum(v[k]);
-  m = wave_sum(m);
-  if (lane == 0) {
-    for (int k = 0; k < 4; ++k) sh[w][k] = v[k];
-    shm[w] = m;
-  }
-  __syncthreads();
-  if (threadIdx.x != 0) return;
-  for (int k = 0; k < 4; ++k) v[k] = (sh[0][k] + sh[1][k]) + (sh[2][k] + sh[3][k]);
-  put_results(a, v, (double)(shm[0] + shm[1] + shm[2] + shm[3]));
+  if (last) add_up(a, kLong ? R : (R + 3) / 4);
 }
 
 // Few responses of few tokens: one workgroup, a wavefront per response.
 __global__ __launch_bounds__(1024) void pref_few_kernel(PrefArgs a) {
-  constexpr int U = 8;
   __shared__ double2 sums[kPrefFewResponses];
   __shared__ int2 rank[kPrefFewResponses];
-  __shared__ double part[kPrefFewResponses][4];
+  __shared__ double part[kPrefFewResponses][kParts];
   const int R = a.P * a.G, lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   for (int r = w; r < R; r += 16) {
-    const int n = length(a, r);
-    double2 s = {0.0, 0.0};
-    for (int t0 = 0; t0 < a.T; t0 += 64 * U) {
-      const double2 x = slot_sums<U>(a, r, n, t0, lane, 64);
-      s.x += x.x;
-      s.y += x.y;
-    }
-    s.x = wave_sum(s.x);
-    s.y = wave_sum(s.y);
+    const double2 s = response_sums(a, r, lane);
     const int2 k = rank_of(a, r, lane);
     if (lane == 0) {
       sums[r] = s;
@@ -320,20 +352,21 @@ __global__ __launch_bounds__(1024) void pref_few_kernel(PrefArgs a) {
     if (a.g)
       for (int t = lane; t < a.T; t += 64) a.g[(int64_t)r * a.T + t] = t < n ? g : 0.f;
     if (lane == 0) {
-      double p[4];
+      double p[kParts];
       contribution(a, r, o, sr, sums[r].y, p);
-      for (int k = 0; k < 4; ++k) part[r][k] = p[k];
+      for (int k = 0; k < kParts; ++k) part[r][k] = p[k];
       if (a.ratio) a.ratio[r] = (float)sr;
     }
   }
   __syncthreads();
   if (w != 0) return;
-  double v[4] = {};
+  double v[kParts] = {};
   for (int c = lane; c < R; c += 64)
     for (int k = 0; k < 4; ++k) v[k] += part[c][k];
 #pragma unroll
   for (int k = 0; k < 4; ++k) v[k] = wave_sum(v[k]);
-  if (lane == 0) put_results(a, v, (double)m);
+  v[4] = m;
+  if (lane == 0) put_results(a, v);
 }
 
 }  // namespace
@@ -355,12 +388,20 @@ hipError_t launch_preference(const lmhead_preference& q, const float* lp, const 
     hipLaunchKernelGGL(pref_few_kernel, dim3(1), dim3(1024), 0, s, a);
     return hipGetLastError();
   }
-  const dim3 grid((unsigned)(L.R * L.nb));
-  hipLaunchKernelGGL(pref_sum_kernel, grid, dim3(256), 0, s, a);
+  // few responses, or long ones, are spread over workgroups; many short ones are a wavefront each
+  const bool shorts = T <= kPrefShort && L.R > kPrefTickets;
+  const int parts = (int)(shorts ? (L.R + 3) / 4 : L.R);
+  const dim3 grid((unsigned)(shorts ? parts : L.R * L.nb));
+  if (shorts) hipLaunchKernelGGL(pref_sum_short_kernel, grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(pref_sum_kernel, grid, dim3(256), 0, s, a);
   // every workgroup adds up the pairs of few prompts itself
   const bool counted = q.weights && L.R > kPrefCounted;
   if (counted) hipLaunchKernelGGL(pref_count_kernel, dim3(1), dim3(1024), 0, s, a);
-  hipLaunchKernelGGL(pref_grad_kernel, grid, dim3(256), 0, s, a, counted);
+  // counts that meet on one word cost some 20 ns each: a launch is quicker than many
+  const bool ticket = parts <= kPrefTickets;
+  if (shorts) hipLaunchKernelGGL(pref_grad_kernel<false>, grid, dim3(256), 0, s, a, counted, ticket);
+  else hipLaunchKernelGGL(pref_grad_kernel<true>, grid, dim3(256), 0, s, a, counted, ticket);
+  if (!ticket) hipLaunchKernelGGL(pref_final_kernel, dim3(1), dim3(1024), 0, s, a, parts);
   return hipGetLastError();
 }
 

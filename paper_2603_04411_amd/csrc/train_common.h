@@ -8,8 +8,14 @@ namespace lmhead {
 
 // ---- preference loss (lmhead_pref.hip) --------------------------------------------------
 
-constexpr int kPrefFewResponses = 64;   // up to so many responses
-constexpr int kPrefFewSlots = 8192;     // and slots the loss is one workgroup
+// Up to so many responses and slots the loss is one workgroup: 8 x 32 8 us, 18 x 100 10 (in two launches 12), 32 x 64 14 (12).
+constexpr int kPrefFewResponses = 24;
+constexpr int kPrefFewSlots = 8192;
+// Of more responses than kPrefTickets those of up to kPrefShort slots are a wavefront each (512 x 256: 12 us, a workgroup each 16;
+// 8192 x 100: 26 and 124); up to kPrefTickets workgroups count themselves, and the last one adds up (a launch more costs what some 150
+// counts on one word do).
+constexpr int kPrefShort = 1024;
+constexpr int kPrefTickets = 160;
 constexpr int kPrefCounted = 1024;      // up to so many responses each workgroup counts all pairs itself
 
 struct PrefLayout {
@@ -29,7 +35,7 @@ static inline PrefLayout pref_layout(int64_t P, int64_t G, int64_t T) {
   L.done = take(256);
   L.sums = take((size_t)(L.R * L.nb) * 2 * sizeof(double));
   L.rank = take((size_t)L.R * 2 * sizeof(int32_t));
-  L.part = take((size_t)L.R * 4 * sizeof(double));
+  L.part = take((size_t)L.R * 5 * sizeof(double));
   L.total = off;
   return L;
 }

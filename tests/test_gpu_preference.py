@@ -68,7 +68,8 @@ def test_every_form(loss, extremes, mean, per_pair):
 
 
 @pytest.mark.parametrize("P,G,T", [(1, 1, 1), (1, 2, 1), (2, 2, 2), (1, 2, 2047), (1, 2, 2048), (1, 2, 2049), (3, 3, 4097), (300, 2, 5),
-                                   (2, 4, 1024), (2, 4, 1025), (32, 2, 128), (33, 2, 124), (32, 2, 129), (512, 2, 3), (513, 2, 3),
+                                   (2, 4, 1024), (2, 4, 1025), (32, 2, 128), (33, 2, 124), (32, 2, 129), (512, 2, 3), (513, 2, 3), (80, 2, 1025), (81, 2, 1030), (320, 2, 30),
+                                   (641, 1, 20), (160, 4, 1024), (3000, 2, 1), (9000, 3, 2), (2, 8, 512), (2, 8, 513), (1, 16, 40), (1, 17, 40), (4, 6, 341), (4, 6, 342), (5, 5, 20), (81, 2, 1024), (163, 1, 7),
                                    (1, 63, 3), (1, 64, 3), (1, 65, 3), (2, 255, 2), (1, 257, 2), (2, 300, 1), (1, 700, 2), (17, 16, 130)])
 def test_sizes(P, G, T):
     check(P, G, T, 11, mean=G > 2, per_pair=T % 2 == 0, nll_coef=0.1)
