@@ -313,8 +313,8 @@ LMHEAD_API int preference_loss(const lmhead_preference* params, const float* log
  * error word of ws (lmhead_check -> LMHEAD_E_RANGE; cleared when a call starts).
  */
 typedef struct lmhead_embed_desc {
-  int32_t R, T;       /* N = R*T <= 2^31 - 2^20 slots                                           */
-  int32_t d, V;       /* row length (a multiple of 8, at most 65536) and rows of the matrix       */
+  int32_t R, T;       /* N = R*T <= 2^31 - 2^20 slots, N*d <= 2^40                               */
+  int32_t d, V;       /* row length (a multiple of 8, at most 65536) and rows of the matrix, V <= 2^31 - 2^20, V*d <= 2^40 */
   int32_t dtype;      /* LMHEAD_F32 or LMHEAD_BF16: storage type of W                            */
   int32_t rows;       /* LMHEAD_F32 or LMHEAD_BF16: storage type of X, gX                        */
   uint32_t flags;     /* LMHEAD_FLAG_ACCUM_DW or 0 (embed_fwd ignores it)                        */
@@ -322,7 +322,9 @@ typedef struct lmhead_embed_desc {
   int64_t ldW, ldX;   /* row strides in elements (>= d, a multiple of 16 bytes)                  */
 } lmhead_embed_desc;
 LMHEAD_API int embed_validate_desc(const lmhead_embed_desc* desc);
-LMHEAD_API size_t embed_workspace_bytes(const lmhead_embed_desc* desc);   /* either call; 0 if the descriptor is invalid */
+/* Scratch bytes of embed_bwd for this descriptor; 0 if it is invalid.  embed_fwd needs 256 bytes, whatever the sizes, and
+ * leaves the others alone.  Host-only. */
+LMHEAD_API size_t embed_workspace_bytes(const lmhead_embed_desc* desc);
 LMHEAD_API int embed_fwd(const lmhead_embed_desc* desc, const void* W, const int32_t* tok, const int32_t* len, float scale,
                          void* X, void* ws, size_t ws_bytes, void* stream);
 LMHEAD_API int embed_bwd(const lmhead_embed_desc* desc, const void* gX, const int32_t* tok, const int32_t* len, float scale,

@@ -176,6 +176,39 @@ def test_backward_of_many_rows(R, T, V, hot):
     backward(R, T, 24, V, "f32", ids(V, R * T, 9, hot), None)
 
 
+# the most slots of each form and one more, the most ids whose tiles are sorted by themselves, zeros that ride along
+@pytest.mark.parametrize("n,d,V,add", [(2047, 520, 900, False), (2048, 520, 900, True), (2049, 520, 900, True), (1254, 4096, 300, True),
+                                       (1255, 4104, 300, False), (16384, 8, 3000, True), (16385, 8, 3000, True), (65536, 8, 700, False),
+                                       (65537, 8, 700, True), (5000, 8, (1 << 22) - 2, True), (5000, 8, (1 << 22) - 1, False),
+                                       (5000, 8, 1 << 22, True), (3000, 8, (8 << 20) + 1, False), (300, 8, (1 << 22) + 5, False)])
+def test_the_edges_between_the_forms(n, d, V, add):
+    import torch
+    import paper_2603_04411_amd as L
+    g = torch.randint(-8, 9, (n, d), generator=torch.Generator(device="cuda").manual_seed(n), device="cuda").to(torch.bfloat16)
+    tok = (torch.rand(n, generator=torch.Generator(device="cuda").manual_seed(V), device="cuda", dtype=torch.float64) ** 6 * V).to(torch.int32)
+    tok[0], tok[-1] = V - 1, 0
+    desc = L.make_embed_desc(1, n, d, V, "bf16", flags=L.FLAG_ACCUM_DW if add else 0)
+    dW = torch.full((V, d), 3.0, device="cuda")
+    ws = torch.full((L.embed_workspace_bytes(desc),), 0xFF, dtype=torch.uint8, device="cuda")
+    L.embed_bwd(desc, g, tok, None, 2.0, dW, ws)
+    assert L.lmhead_check(ws) == 0
+    # whole numbers below 2^24: exact in any order
+    want = torch.full((V, d), 3.0 if add else 0.0, device="cuda").index_add_(0, tok.long(), 2 * g.float())
+    assert torch.equal(dW, want)
+
+
+def test_forward_in_256_bytes():
+    import torch
+    import paper_2603_04411_amd as L
+    for n in (100, 5000):
+        desc = L.make_embed_desc(1, n, 64, 30, "bf16")
+        W, X = torch.randn(30, 64, device="cuda").bfloat16(), torch.empty(n, 64, dtype=torch.bfloat16, device="cuda")
+        tok = torch.arange(n, device="cuda", dtype=torch.int32) % 30
+        ws = torch.full((1024,), 0xFF, dtype=torch.uint8, device="cuda")
+        L.embed_fwd(desc, W, tok, None, 1.0, X, ws[:256])
+        assert L.lmhead_check(ws) == 0 and torch.equal(X, W[tok.long()]) and bool((ws[256:] == 0xFF).all())
+
+
 def test_backward_of_nothing():
     for add in (False, True):
         backward(3, 50, 64, 20, "bf16", ids(20, 150, 1), [0, 0, 0], add=add)
