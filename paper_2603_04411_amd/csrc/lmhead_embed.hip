@@ -444,8 +444,8 @@ __global__ __launch_bounds__(256) void sort_place_kernel(SortArgs a) {
 // ---- the sort of a few tiles ---------------------------------------------------------------
 
 // Up to kMergeTiles tiles take two launches instead of two per digit: each tile is sorted by itself, then each slot looks up how
-// many slots of every other tile come before it.  The gradient of 3000 / 8192 / 12000 / 16384 rows of 64, added to 152064 ids: 19 / 24 / 27 /
-// 31 us, by digits 26 / 29 / 32 / 32; of 32768 48 and 41.
+// many slots of every other tile come before it.  The gradient of 3000 / 8192 / 16384 rows of 64, added to 152064 ids: 18 / 22 / 27 us, by
+// digits 26 / 29 / 32; with twice the LDS 24000 rows take 39, by digits 36.
 
 // A tile's values id << 10 | place in the tile, ascending; one value per thread.  Bitonic: exchanges over less than 64 places stay in a
 // wavefront.
@@ -486,45 +486,47 @@ __global__ __launch_bounds__(kSortTile) void tile_sort_kernel(SortArgs a) {
 }
 
 // Each workgroup holds all tiles in LDS (eleven dependent steps through each of them would each wait for L2: 26 us for 16 tiles) and places
-// 256 slots (a tile's 1024 are four times the reads of one compute unit's LDS: 19 us).
+// 64 slots, each wavefront looking through a quarter of the tiles (256 slots, every wavefront through all: 11 us; 1024: 19).
 __global__ __launch_bounds__(256) void tile_merge_kernel(SortArgs a) {
-  constexpr int U = 4;
+  constexpr int U = kMergeTiles / 4;
   extern __shared__ __align__(16) uint32_t all[];
+  __shared__ uint32_t parts[4][64];
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     uint32_t err = 0;
     for (int q = 0; q < a.tiles; ++q) err |= a.hist[q];
     a.hdr->err = (int)err;
   }
-  for (uint32_t i = threadIdx.x * 4; i < (a.N & ~3u); i += 1024) *reinterpret_cast<uint4*>(all + i) = *reinterpret_cast<const uint4*>(a.key + i);
-  if (threadIdx.x < (a.N & 3u)) all[(a.N & ~3u) + threadIdx.x] = a.key[(a.N & ~3u) + threadIdx.x];
+  const uint32_t whole = a.N & ~3u;
+  for (uint32_t i = threadIdx.x * 4; i < whole; i += 1024) *reinterpret_cast<uint4*>(all + i) = *reinterpret_cast<const uint4*>(a.key + i);
+  if (threadIdx.x < (a.N & 3u)) all[whole + threadIdx.x] = a.key[whole + threadIdx.x];
   __syncthreads();
-  const int tile = (int)(blockIdx.x * 256 / kSortTile);
-  const uint32_t i = blockIdx.x * 256u + threadIdx.x;
-  if (i >= a.N) return;
-  const uint32_t x = all[i], id = x >> 10;
-  uint32_t p = i % kSortTile;
-  for (int q0 = 0; q0 < a.tiles; q0 += U) {
-    // slots of the same id come first where their tile does
-    uint32_t below[U], n[U], at[U], k[U];
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, tile = (int)(blockIdx.x * 64 / kSortTile);
+  const uint32_t i = blockIdx.x * 64u + lane, x = all[min(i, a.N - 1)], id = x >> 10;
+  // slots of the same id come first where their tile does
+  uint32_t below[U], n[U], at[U], k[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int q = u * 4 + w;
+    k[u] = q < a.tiles ? (uint32_t)q * kSortTile : 0;
+    n[u] = q >= a.tiles || q == tile ? 0 : q + 1 < a.tiles ? kSortTile : a.N - k[u];
+    below[u] = (id + (q < tile)) << 10;
+    at[u] = 0;
+  }
+#pragma unroll
+  for (uint32_t step = kSortTile; step > 0; step >>= 1)
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int q = q0 + u;
-      k[u] = q < a.tiles ? (uint32_t)q * kSortTile : 0;
-      n[u] = q >= a.tiles || q == tile ? 0 : q + 1 < a.tiles ? kSortTile : a.N - k[u];
-      below[u] = (id + (q < tile)) << 10;
-      at[u] = 0;
+      // read whether it counts or not: a branch would wait for one of the U reads at a time
+      const uint32_t to = at[u] + step, v = all[min(k[u] + to - 1, a.N - 1)];
+      at[u] = ((to <= n[u]) & (v < below[u])) ? to : at[u];
     }
+  uint32_t p = 0;
 #pragma unroll
-    for (uint32_t step = kSortTile; step > 0; step >>= 1)
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        // read whether it counts or not: a branch would wait for one of the U reads at a time
-        const uint32_t to = at[u] + step, v = all[min(k[u] + to - 1, a.N - 1)];
-        at[u] = ((to <= n[u]) & (v < below[u])) ? to : at[u];
-      }
-#pragma unroll
-    for (int u = 0; u < U; ++u) p += at[u];
-  }
+  for (int u = 0; u < U; ++u) p += at[u];
+  parts[w][lane] = p;
+  __syncthreads();
+  if (w != 0 || i >= a.N) return;
+  p = i % kSortTile + parts[0][lane] + parts[1][lane] + parts[2][lane] + parts[3][lane];
   a.key_out[p] = id;
   a.slot_out[p] = (uint32_t)tile * kSortTile + (x & 1023u);
 }
@@ -650,10 +652,9 @@ __global__ __launch_bounds__(64) void embed_sum_kernel(SumArgs a) {
 
 // The long ids: a workgroup per id and 256 columns, those of one id next to each other (a launch that went through all ids with the same
 // columns first met on few memory channels: 60 us for the 3600 partial rows of 4096 that 330000 slots leave, now 34).  Wavefront w takes
-// the w-th eighth of the id's partial sums in order, and the eight sums are added in order.
-constexpr int kJoinWaves = 8;
-__global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(SumArgs a) {
-    constexpr int U = 8, W = kJoinWaves;
+// the w-th part of the id's partial sums in order, U at a time, and the W sums are added in order.
+template <int W, int U>
+__global__ __launch_bounds__(64 * W) void embed_join_kernel(SumArgs a) {
   __shared__ f32x4 sums[W][64];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), d = a.r.d;
   const int cols = (d + 255) / 256, c = (int)(blockIdx.x % cols) * 256 + lane * 4;
@@ -749,7 +750,8 @@ hipError_t launch_embed_bwd(const lmhead_embed_desc& d, const void* gX, const in
   so.hdr = hdr;
   const int64_t cells = add ? 0 : (int64_t)d.V * d.d;
   // Where many zeros are written they hide all launches of the sort by digits, but not tile_merge_kernel, whose LDS would leave them few
-  // workgroups.  8192 rows of 1024: 64 MB of zeros 33 us, by digits 42; 125 MB 46 and 51; 594 MB 129 and 122.
+  // workgroups.  8192 rows of 1024: 64 MB of zeros 33 us, by digits 42; 125 MB 46 and 51; 594 MB 129
+  // and 122.
   const bool merged = L.tiles <= kMergeTiles && d.V < (1 << 22) - 1 && cells <= kMergeCells;
   const int launches = merged ? 1 : L.passes * (so.scanned ? 3 : 2);
   int launch = 0;
@@ -769,7 +771,7 @@ hipError_t launch_embed_bwd(const lmhead_embed_desc& d, const void* gX, const in
     buffers(1);
     go(tile_sort_kernel, L.tiles, kSortTile);
     buffers(0);
-    hipLaunchKernelGGL(tile_merge_kernel, dim3((unsigned)((L.N + 255) / 256)), dim3(256), (size_t)L.N * 4, s, so);
+    hipLaunchKernelGGL(tile_merge_kernel, dim3((unsigned)((L.N + 63) / 64)), dim3(256), (size_t)(L.N + 3) / 4 * 16, s, so);
   }
   for (int p = 0; !merged && p < L.passes; ++p) {
     so.first = p == 0;
@@ -797,7 +799,11 @@ hipError_t launch_embed_bwd(const lmhead_embed_desc& d, const void* gX, const in
   else hipLaunchKernelGGL(embed_sum_kernel<float>, grid, dim3(64), 0, s, a);
   // an id is long from two chunks' slots on
   const int64_t most = L.N / (2 * L.C) + 1;
-  hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)(most < 512 ? most : 512) * ((d.d + 255) / 256)), dim3(64 * kJoinWaves), 0, s, a);
+  const dim3 joins((unsigned)(most < 512 ? most : 512) * ((d.d + 255) / 256));
+  // Of many short rows the most frequent id decides: 65536 / 200000 x 64 54 / 76 us, with eight wavefronts 57 / 81; of 16384 27.4 and 26.8,
+  // of 65536 x 1024 as much either way.
+  if (d.d <= 512 && L.N > 32768) hipLaunchKernelGGL((embed_join_kernel<16, 16>), joins, dim3(1024), 0, s, a);
+  else hipLaunchKernelGGL((embed_join_kernel<8, 8>), joins, dim3(512), 0, s, a);
   return hipGetLastError();
 }
 
