@@ -90,6 +90,9 @@ __global__ void embed_clear_kernel(EmbedHeader* hdr) { hdr->err = 0; }
 // Units of 256 threads and 16 bytes each of X, in the order of the addresses; a workgroup has kLookup of them in flight, so that
 // the wait for an id and then for its row is shared.  Long rows: `parts` units to a row, and the id is the same for all
 // threads; short ones: 2^lanes neighbouring threads to a row.
+// Bound by memory: 524288 slots x 4096 bf16 write 4.3 GB and fetch 1.2 GB of W past L2 (41000 different rows are 0.34), in 805 us: 6.8 TB/s.
+// One unit 1290 us, two 1020, eight as four; X through the caches 923 (it pushes W out of them; what reads X next is not slower for it
+// from 8 MB to 540 MB of X).
 // Of a batch of few slots the last workgroup reports for all (`reports`); otherwise the header has been cleared, and whoever meets
 // an error adds it.
 constexpr int kLookup = 4;
@@ -287,6 +290,8 @@ __device__ inline void fill(const Fill& f, int64_t block) {
   if (i < f.hi) *reinterpret_cast<f32x4*>(f.p + i) = f32x4{0.f, 0.f, 0.f, 0.f};
 }
 
+// A radix sort, least digit first, in tiles of 1024 slots: counts, their sums, places.  Launches and latency: of 524288 slots 7.6, 6 and 10 us
+// a digit, of which 152064 ids have two.  (Tiles of 4096 slots: places alone 20, sixteen rounds of ballots one after the other.)
 struct SortArgs {
   Batch b;                 // first pass: keys come from here
   bool first;
@@ -750,8 +755,7 @@ hipError_t launch_embed_bwd(const lmhead_embed_desc& d, const void* gX, const in
   so.hdr = hdr;
   const int64_t cells = add ? 0 : (int64_t)d.V * d.d;
   // Where many zeros are written they hide all launches of the sort by digits, but not tile_merge_kernel, whose LDS would leave them few
-  // workgroups.  8192 rows of 1024: 64 MB of zeros 33 us, by digits 42; 125 MB 46 and 51; 594 MB 129
-  // and 122.
+  // workgroups.  8192 rows of 1024: 64 MB of zeros 33 us, by digits 42; 125 MB 46 and 51; 594 MB 129 and 122.
   const bool merged = L.tiles <= kMergeTiles && d.V < (1 << 22) - 1 && cells <= kMergeCells;
   const int launches = merged ? 1 : L.passes * (so.scanned ? 3 : 2);
   int launch = 0;

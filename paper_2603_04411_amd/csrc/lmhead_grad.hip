@@ -136,6 +136,7 @@ __device__ inline double squares_of(const GradEntry& e, int64_t at, int most, in
 }
 
 // Workgroup b takes chunks b * each .. and leaves the tensor in which they begin, where the second pass starts to look.
+// 3.0 GB (the head's dW beside a few layers) in 435 us: 6.9 TB/s, a bare loop of loads 7.0; through the caches 6.0.
 template <typename Table>
 __global__ __launch_bounds__(256) void grad_norm_kernel(Table t, uint32_t each, double* part, int32_t* begins) {
   double s = 0.0;
@@ -219,7 +220,10 @@ __device__ inline void scaled_of(const GradEntry& e, int64_t at, int most, float
   }
 }
 
-// A part of a chunk per workgroup.  shared: each workgroup derives the factor from the partial sums, and the first one writes
+// A part of a chunk per workgroup: two vectors a thread.  620 million elements in 1015 us, 6.1 TB/s, a bare copy of
+// one vector a thread 6.6; whole chunks 1090, halves 1065, eighths as quarters, but slower where tensors are many.  Looking the tensor up
+// from the first pass's place on instead of among all: 290 tensors 270 -> 209 us.
+// shared: each workgroup derives the factor from the partial sums, and the first one writes
 // the norm; otherwise grad_final_kernel has done both.
 template <typename Table>
 __global__ __launch_bounds__(256) void grad_clip_kernel(Table t, uint32_t each, const double* part, const int32_t* begins, int parts,

@@ -56,6 +56,8 @@ def test_forward(dtype, rows, R, T, d):
     tok, lens = ids(V, R * T, R + d), np.random.default_rng(d).integers(0, T + 1, R)
     forward(R, T, d, V, dtype, rows, tok, lens, 1.0)
     forward(R, T, d, V, dtype, rows, tok, None, 45.25, ldW=d + 8, ldX=d + 16)
+    # rows that begin 16 bytes apart from any larger power of two
+    forward(R, T, d, V, dtype, rows, tok, lens, 3.0, ldW=d + (4 if dtype == "f32" else 8), ldX=d + (4 if rows == "f32" else 8))
 
 
 def test_forward_of_many_rows():
