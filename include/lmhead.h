@@ -334,8 +334,8 @@ LMHEAD_API int embed_bwd(const lmhead_embed_desc* desc, const void* gX, const in
  * The norm over all gradients of a step, and their clipping.
  *     norm = sqrt(sum over all tensors and elements of g^2)       (squares and sums in fp64: no overflow, no lost small ones)
  *     c    = min(1, max_norm / (norm + eps)),    out = c g        (in fp32, rounded once to the type of out)
- * norm[0] = norm; grad_clip also writes norm[1] = c.  As the formulas say, a norm of +inf gives c = 0 and a norm of NaN gives NaN
- * everywhere: look at norm[0] before the optimiser takes such a step.
+ * norm[0] = norm; grad_clip also writes norm[1] = c.  As the formulas say, a norm of +inf gives c = 0 (NaN if max_norm is +inf too, and
+ * 0 / 0 is NaN) and a norm of NaN gives NaN everywhere: look at norm[0] before the optimiser takes such a step.
  *   g    host array of `count` tensors (1 .. 65536): device pointer, elements (0 allowed), LMHEAD_F32 or LMHEAD_BF16.  Pointers need
  *        only their type's alignment; tensors that are not 16-byte aligned are read and written more slowly.
  *   out  host array of `count` tensors with the same element counts, of either type, or NULL: g is scaled in place (and left

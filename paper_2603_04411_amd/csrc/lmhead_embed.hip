@@ -105,7 +105,7 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(Batch b, const TW* __res
   typedef __attribute__((ext_vector_type(E))) TX out_t;
   if (reports && blockIdx.x == gridDim.x - 1) return report_all(b, hdr);
   const uint32_t N = (uint32_t)b.R * (uint32_t)b.T;
-  const uint64_t u0 = (uint64_t)blockIdx.x * U;
+  const uint64_t u0 = (uint64_t)grid_wg() * U;
   int64_t i[U];
   int c[U];
   uint32_t v[U];
@@ -195,16 +195,17 @@ __global__ __launch_bounds__(256) void embed_few_kernel(Batch b, Rows a, EmbedHe
   const uint32_t V = (uint32_t)b.V;
   int err = 0;
   for (int i = threadIdx.x; i < N; i += 256) id[i] = id_of(b, i, err);
-  if (blockIdx.x == 0) {
+  if (grid_wg() == 0) {
     err = wave_or(err);
     if (lane == 0) bits[w] = err;
   }
-  if ((int)blockIdx.x >= owners) {
+  const uint32_t wg = grid_wg();
+  if (wg >= (uint32_t)owners) {
     // at most 64 ids: bit k of `present`, gathered by the four wavefronts
     __shared__ uint64_t present;
     if (threadIdx.x == 0) present = 0;
     __syncthreads();
-    const uint32_t v0 = (blockIdx.x - owners) * (uint32_t)rows_each;
+    const uint32_t v0 = (wg - owners) * (uint32_t)rows_each;
     for (int i = threadIdx.x; i < N; i += 256)
       if (id[i] - v0 < (uint32_t)rows_each) atomicOr(reinterpret_cast<unsigned long long*>(&present), 1ull << (id[i] - v0));
     __syncthreads();
@@ -217,8 +218,8 @@ __global__ __launch_bounds__(256) void embed_few_kernel(Batch b, Rows a, EmbedHe
     return;
   }
   __syncthreads();
-  if (blockIdx.x == 0 && threadIdx.x == 0) hdr->err = bits[0] | bits[1] | bits[2] | bits[3];
-  const int slot = (int)blockIdx.x / cols * 4 + w;
+  if (wg == 0 && threadIdx.x == 0) hdr->err = bits[0] | bits[1] | bits[2] | bits[3];
+  const int slot = (int)wg / cols * 4 + w;
   const uint32_t mine = slot < N ? id[slot] : V;
   int n = 0;
   if (mine < V) {
@@ -237,7 +238,7 @@ __global__ __launch_bounds__(256) void embed_few_kernel(Batch b, Rows a, EmbedHe
     count[w] = n;
     whose[w] = mine;
   }
-  const int c = (int)blockIdx.x % cols * 512 + lane * 8;
+  const int c = (int)wg % cols * 512 + lane * 8;
   const bool in = c < a.d;
   const T* g = static_cast<const T*>(a.g) + (in ? c : a.d - 8);
   auto sum = [&](const uint16_t* l, int from, int to, float (&s)[8]) {
@@ -314,7 +315,7 @@ __device__ inline uint32_t sort_key(const SortArgs& a, uint32_t i, int& err) {
 
 __global__ __launch_bounds__(256) void sort_count_kernel(SortArgs a) {
   __shared__ uint32_t h[1 << kSortBits];
-  if ((int)blockIdx.x >= a.tiles) return fill(a.f, blockIdx.x - a.tiles);
+  if (grid_wg() >= (uint32_t)a.tiles) return fill(a.f, grid_wg() - a.tiles);
   const int D = 1 << a.digit;
   for (int i = threadIdx.x; i < D; i += 256) h[i] = 0;
   if (a.first && blockIdx.x == 0 && threadIdx.x == 0) {
@@ -335,7 +336,7 @@ __global__ __launch_bounds__(256) void sort_count_kernel(SortArgs a) {
 // A wavefront per digit value: exclusive sums over the tiles, and the total.
 __global__ __launch_bounds__(256) void sort_scan_kernel(SortArgs a) {
   const int D = 1 << a.digit, groups = (D + 3) / 4;
-  if ((int)blockIdx.x >= groups) return fill(a.f, blockIdx.x - groups);
+  if (grid_wg() >= (uint32_t)groups) return fill(a.f, grid_wg() - groups);
   const int lane = threadIdx.x & 63, v = blockIdx.x * 4 + (threadIdx.x >> 6);
   if (v >= D) return;
   uint32_t* h = a.hist + (int64_t)v * a.tiles;
@@ -359,7 +360,7 @@ __global__ __launch_bounds__(256) void sort_place_kernel(SortArgs a) {
   constexpr int K = kSortTile / 256;
   __shared__ uint32_t at[4][1 << kSortBits];
   __shared__ uint32_t wsum[4];
-  if ((int)blockIdx.x >= a.tiles) return fill(a.f, blockIdx.x - a.tiles);
+  if (grid_wg() >= (uint32_t)a.tiles) return fill(a.f, grid_wg() - a.tiles);
   const int D = 1 << a.digit, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const uint32_t base = blockIdx.x * (uint32_t)kSortTile + w * (kSortTile / 4) + lane;
   for (int i = threadIdx.x; i < 4 * (1 << kSortBits); i += 256) (&at[0][0])[i] = 0;
@@ -457,7 +458,7 @@ __global__ __launch_bounds__(256) void sort_place_kernel(SortArgs a) {
 __global__ __launch_bounds__(kSortTile) void tile_sort_kernel(SortArgs a) {
   __shared__ uint32_t sh[kSortTile];
   __shared__ int bits[kSortTile / 64];
-  if ((int)blockIdx.x >= a.tiles) return fill<kSortTile>(a.f, blockIdx.x - a.tiles);
+  if (grid_wg() >= (uint32_t)a.tiles) return fill<kSortTile>(a.f, grid_wg() - a.tiles);
   const uint32_t t = threadIdx.x, i = blockIdx.x * (uint32_t)kSortTile + t;
   int err = 0;
   uint32_t x = i < a.N ? id_of(a.b, i, err) << 10 | t : 0xffffffffu;
@@ -703,7 +704,7 @@ void run_fwd(const lmhead_embed_desc& d, const Batch& b, const void* W, float sc
   const int64_t units = lanes == 8 ? N * parts : (N + (256 >> lanes) - 1) / (256 >> lanes), wgs = (units + kLookup - 1) / kLookup;
   if (!reports) hipLaunchKernelGGL(embed_clear_kernel, dim3(1), dim3(1), 0, s, hdr);
   auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(wgs + reports)), dim3(256), 0, s, b, static_cast<const TW*>(W), d.ldW, d.d, scale,
+    hipLaunchKernelGGL(kernel, grid_of(wgs + reports), dim3(256), 0, s, b, static_cast<const TW*>(W), d.ldW, d.d, scale,
                        static_cast<TX*>(X), d.ldX, hdr, lanes, (uint32_t)parts, reports);
   };
   if (lanes == 8) go(embed_fwd_kernel<TW, TX, true>);
@@ -737,7 +738,7 @@ hipError_t launch_embed_bwd(const lmhead_embed_desc& d, const void* gX, const in
     rows_each = rows_each < 1 ? 1 : rows_each > 64 ? 64 : rows_each;
     const int64_t fills = add ? 0 : ((int64_t)d.V + rows_each - 1) / rows_each;
     auto go = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, dim3((unsigned)(owners + fills)), dim3(256), 0, s, b, r, hdr, owners, cols, rows_each);
+      hipLaunchKernelGGL(kernel, grid_of(owners + fills), dim3(256), 0, s, b, r, hdr, owners, cols, rows_each);
     };
     if (bf16) go(embed_few_kernel<__bf16>);
     else go(embed_few_kernel<float>);
@@ -763,7 +764,7 @@ hipError_t launch_embed_bwd(const lmhead_embed_desc& d, const void* gX, const in
   auto go = [&](auto kernel, int64_t wgs, int threads = 256) {
     so.f = Fill{dW, cells / 8 * launch / launches * 8, cells / 8 * (launch + 1) / launches * 8};
     ++launch;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(wgs + (so.f.hi - so.f.lo + threads * 4 - 1) / (threads * 4))), dim3(threads), 0, s, so);
+    hipLaunchKernelGGL(kernel, grid_of(wgs + (so.f.hi - so.f.lo + threads * 4 - 1) / (threads * 4)), dim3(threads), 0, s, so);
   };
   auto buffers = [&](int from) {
     so.key = u32(L.key[from]);

@@ -228,20 +228,21 @@ __device__ inline void scaled_of(const GradEntry& e, int64_t at, int most, float
 template <typename Table>
 __global__ __launch_bounds__(256) void grad_clip_kernel(Table t, uint32_t each, const double* part, const int32_t* begins, int parts,
                                                         bool shared, Clip k) {
-  const uint32_t chunk = blockIdx.x / kClipParts, b = chunk / each;
+  const uint32_t wg = grid_wg(), chunk = wg / kClipParts, b = chunk / each;
+  if (chunk >= t.chunks) return;
   const GradEntry& e = t.at(tensor_of(t, chunk, begins[b], (b + 1 < (uint32_t)parts ? begins[b + 1] : t.count - 1) + 1));
   float c;
   if (shared) {
     const double n = norm_of(part, parts);
     c = factor(n, k);
-    if (blockIdx.x == 0 && threadIdx.x == 0) {
+    if (wg == 0 && threadIdx.x == 0) {
       k.norm[0] = (float)n;
       k.norm[1] = c;
     }
   } else {
     c = k.norm[1];
   }
-  scaled_of(e, (int64_t)(chunk - e.first) * kGradChunk + blockIdx.x % kClipParts * (kGradChunk / kClipParts), kGradChunk / kClipParts, c,
+  scaled_of(e, (int64_t)(chunk - e.first) * kGradChunk + wg % kClipParts * (kGradChunk / kClipParts), kGradChunk / kClipParts, c,
             threadIdx.x, 256);
 }
 
@@ -324,7 +325,7 @@ hipError_t launch_grads(const lmhead_tensor* g, const lmhead_tensor* out, int co
   const bool shared = clip && parts <= kGradShared;
   if (!shared) hipLaunchKernelGGL(grad_final_kernel, dim3(1), dim3(1024), 0, s, part, parts, k, clip);
   if (!clip) return hipGetLastError();
-  const dim3 grid(chunks * kClipParts);
+  const dim3 grid = grid_of((int64_t)chunks * kClipParts);
   if (args) hipLaunchKernelGGL(grad_clip_kernel<ArgTable>, grid, dim3(256), 0, s, t, each, part, begins, parts, shared, k);
   else hipLaunchKernelGGL(grad_clip_kernel<WsTable>, grid, dim3(256), 0, s, wt, each, part, begins, parts, shared, k);
   return hipGetLastError();

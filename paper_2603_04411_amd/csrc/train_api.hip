@@ -23,8 +23,7 @@ int validate_embed(const lmhead_embed_desc* d) {
   if (!known(d->dtype) || !known(d->rows) || (d->flags & ~(uint32_t)LMHEAD_FLAG_ACCUM_DW)) return LMHEAD_E_DTYPE;
   if (d->d % 8 != 0 || d->d > 65536 || d->ldW < d->d || d->ldX < d->d) return LMHEAD_E_SHAPE;
   if ((int64_t)d->R * d->T > (int64_t)INT32_MAX - (1 << 20) + 1 || d->V > INT32_MAX - (1 << 20)) return LMHEAD_E_SHAPE;
-  // byte offsets are 64-bit; sizes that no memory holds are a mistake, and would not fit a launch's grid
-  constexpr int64_t kMost = 1ll << 40;
+  constexpr int64_t kMost = 1ll << 40;   // sizes that no memory holds are a mistake
   if (d->ldW > kMost || d->ldX > kMost || (int64_t)d->R * d->T > kMost / d->d || d->V > kMost / d->d) return LMHEAD_E_SHAPE;
   if (d->ldW * element_bytes(d->dtype) % 16 != 0 || d->ldX * element_bytes(d->rows) % 16 != 0) return LMHEAD_E_ALIGN;
   return LMHEAD_OK;

@@ -6,6 +6,13 @@
 
 namespace lmhead {
 
+// A launch has fewer than 2^32 threads along x: workgroups in rows of kGridRow (the last row may be longer than what there is to do).
+constexpr uint32_t kGridRow = 1 << 21;
+static inline dim3 grid_of(int64_t wgs) {
+  return dim3((unsigned)(wgs < kGridRow ? wgs : kGridRow), (unsigned)((wgs + kGridRow - 1) / kGridRow));
+}
+__device__ inline uint32_t grid_wg() { return blockIdx.y * kGridRow + blockIdx.x; }
+
 // ---- preference loss (lmhead_pref.hip) --------------------------------------------------
 
 // Up to so many responses and slots the loss is one workgroup: 8 x 32 8 us, 18 x 100 10 (in two launches 12), 32 x 64 14 (12).

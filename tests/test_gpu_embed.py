@@ -272,3 +272,33 @@ def test_offsets_beyond_32_bits():
     L.embed_bwd(desc, X, tok, None, 1.0, W, ws)
     assert L.lmhead_check(ws) == 0
     assert torch.equal(W[-1], 2 * X[-1]) and bool((W[0] == 1).all()) and not bool(W[1:-1].any())
+
+
+def test_more_threads_than_one_row_of_workgroups():
+    import torch
+    import paper_2603_04411_amd as L
+    if torch.cuda.mem_get_info()[0] < 160 << 30:
+        pytest.skip("needs 160 GB")
+    # rows that are filled up to 2048 columns: 2^33 threads' worth of them
+    d, V, N = 1032, 50, (1 << 25) + 1000
+    W = torch.randn(V, d, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    tok = torch.randint(0, V, (N,), dtype=torch.int32, device="cuda", generator=torch.Generator(device="cuda").manual_seed(2))
+    X = torch.full((N, d), 5.0, device="cuda")
+    ws = torch.empty(256, dtype=torch.uint8, device="cuda")
+    L.embed_fwd(L.make_embed_desc(1, N, d, V, "f32"), W, tok, None, 1.0, X, ws)
+    assert L.lmhead_check(ws) == 0
+    for lo in range(0, N, 1 << 21):
+        assert torch.equal(X[lo:lo + (1 << 21)], W[tok[lo:lo + (1 << 21)].long()]), lo
+    del X
+    # few slots and 2^30 ids of eight columns
+    V, ids_ = (1 << 30) + 5, [0, (1 << 30) + 4, 1 << 29, 0]
+    g = torch.randn(4, 8, device="cuda", generator=torch.Generator(device="cuda").manual_seed(3))
+    dW = torch.full((V, 8), 7.0, device="cuda")
+    desc = L.make_embed_desc(1, 4, 8, V, "f32")
+    ws = torch.empty(L.embed_workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+    L.embed_bwd(desc, g, torch.tensor(ids_, dtype=torch.int32, device="cuda"), None, 1.0, dW, ws)
+    assert L.lmhead_check(ws) == 0
+    for v, row in ((0, g[0] + g[3]), ((1 << 30) + 4, g[1]), (1 << 29, g[2])):
+        assert torch.equal(dW[v], row)
+        dW[v] = 0.0
+    assert all(not bool(dW[lo:lo + (1 << 26)].any()) for lo in range(0, V, 1 << 26))
