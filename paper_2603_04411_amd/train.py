@@ -176,11 +176,12 @@ def embed_bwd(desc, gX, tok, lens, scale, dW, ws) -> None:
 
 
 class GradList:
-    """The tensors of a call to grad_norm or grad_clip, as the ABI takes them.  Holds on to the tensors; buffers that stay the same
-    from step to step need one list."""
+    """The tensors of a call to grad_norm or grad_clip, as the ABI takes them.  Buffers that stay the same from step to step need one
+    list.  It holds on to the memory that the tensors had when it was made: a tensor that is given other memory later (``set_``,
+    assigning ``data``) needs a new list."""
 
     def __init__(self, tensors):
-        self.tensors = list(tensors)
+        self.tensors = [t.detach() for t in tensors]
         self.array = (_Tensor * max(len(self.tensors), 1))()
         self.device = None
         for i, t in enumerate(self.tensors):

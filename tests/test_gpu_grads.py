@@ -141,6 +141,38 @@ def test_what_lies_around_the_tensors_is_left_alone():
             assert bool((out[:at] == 9).all()) and bool((out[at + n:] == 9).all()) and bool((buf == 9).all()) and bool((out[at:at + n] < 9).all())
 
 
+def test_more_elements_than_one_row_of_workgroups():
+    """2^35 elements and some: the scaling pass has more workgroups than a launch takes along one axis."""
+    import torch
+    import paper_2603_04411_amd as L
+    n = (1 << 35) + 3 * 8192 + 5
+    if torch.cuda.mem_get_info()[0] < 2 * n + (4 << 30):
+        pytest.skip("64 GiB of device memory are not free")
+    t = torch.empty(n, dtype=torch.bfloat16, device="cuda").zero_()
+    at = [0, 8191, 8192, (1 << 34) + 1, (1 << 35) - 1, 1 << 35, (1 << 35) + 8192, n - 2, n - 1]
+    for i in at:
+        t[i] = 2.0
+    norm = torch.empty(2, device="cuda")
+    L.grad_clip(L.make_grad_list([t]), None, 3.0, 0.0, norm, workspace())
+    assert norm.tolist() == [6.0, 0.5]
+    for i in at:
+        near = t[max(i - 2, 0):i + 3].tolist()
+        assert near[min(i, 2)] == 1.0 and all(v in (0.0, 1.0) for v in near), i
+    assert int(sum(int((t[lo:lo + (1 << 32)] != 0).sum()) for lo in range(0, n, 1 << 32))) == len(at)
+
+
+def test_a_list_keeps_the_memory_that_it_was_made_with():
+    import torch
+    import paper_2603_04411_amd as L
+    t = torch.full((1000,), 2.0, device="cuda")
+    grads, norm = L.make_grad_list([t]), torch.empty(2, device="cuda")
+    old = t.detach()
+    t.data = torch.full((1000,), 5.0, device="cuda")
+    assert grads.tensors[0].data_ptr() == old.data_ptr() and grads.array[0].data == old.data_ptr()
+    L.grad_clip(grads, None, 1.0, 0.0, norm, workspace())
+    assert bool((t == 5.0).all()) and bool((old < 2.0).all())
+
+
 def test_the_same_bits_each_time():
     import torch
     import paper_2603_04411_amd as L
