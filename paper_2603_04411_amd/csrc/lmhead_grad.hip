@@ -220,7 +220,7 @@ __device__ inline void scaled_of(const GradEntry& e, int64_t at, int most, float
   }
 }
 
-// A part of a chunk per workgroup: two vectors a thread.  620 million elements in 1015 us, 6.1 TB/s, a bare copy of
+// A part of a chunk per workgroup: two vectors a thread.  790 million elements in 1007 us, 6.1 TB/s, a bare copy of
 // one vector a thread 6.6; whole chunks 1090, halves 1065, eighths as quarters, but slower where tensors are many.  Looking the tensor up
 // from the first pass's place on instead of among all: 290 tensors 270 -> 209 us.
 // shared: each workgroup derives the factor from the partial sums, and the first one writes
