@@ -228,14 +228,19 @@ __global__ __launch_bounds__(1024) void pref_count_kernel(PrefArgs a) {
   }
 }
 
-// Loss and statistics from the n parts that all have left; one workgroup of up to 16 wavefronts.
+// Loss and statistics from the n parts that all have left, this launch's (kSame: past the caches) or another's; one workgroup of up
+// to 16 wavefronts.
+template <bool kSame>
 __device__ inline void add_up(const PrefArgs& a, int n) {
   __shared__ double sh[16][kParts];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   double v[kParts] = {};
   for (int c = threadIdx.x; c < n; c += blockDim.x)
 #pragma unroll
-    for (int k = 0; k < kParts; ++k) v[k] += __hip_atomic_load(a.part + (int64_t)c * kParts + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for (int k = 0; k < kParts; ++k) {
+      const double* p = a.part + (int64_t)c * kParts + k;
+      v[k] += kSame ? __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : *p;
+    }
 #pragma unroll
   for (int k = 0; k < kParts; ++k) v[k] = wave_sum(v[k]);
   if (lane == 0)
@@ -247,7 +252,7 @@ __device__ inline void add_up(const PrefArgs& a, int n) {
   put_results(a, v);
 }
 
-__global__ __launch_bounds__(1024) void pref_final_kernel(PrefArgs a, int n) { add_up(a, n); }
+__global__ __launch_bounds__(1024) void pref_final_kernel(PrefArgs a, int n) { add_up<false>(a, n); }
 
 // dloss/dlogp.  kLong: block (r, b) writes its slots of response r, one wavefront looks at r's pairs, and b = 0 leaves what they add to
 // loss and stats; otherwise a wavefront per response does all that, and the block leaves the sum of its four.  ticket: the last block to
@@ -322,7 +327,7 @@ __global__ __launch_bounds__(256) void pref_grad_kernel(PrefArgs a, bool counted
   }
   if (!ticket || b != 0) return;
   __syncthreads();
-  if (last) add_up(a, kLong ? R : (R + 3) / 4);
+  if (last) add_up<true>(a, kLong ? R : (R + 3) / 4);
 }
 
 // Few responses of few tokens: one workgroup, a wavefront per response.
