@@ -25,9 +25,10 @@ struct PrefArgs {
   const float* lr;
   const float* reward;
   const int32_t* len;
-  int P, G, T, nb;
+  int P, G, T, nb, ns;   // nb: blocks of slots in a response, ns: sums that the gradient's launch finds for one
   lmhead_preference q;
   double2* sums;       // [response][block]{log-ratio, log-probability}
+  double2* totals;     // [response], the same of all its blocks; with one sum to a response the same memory
   int2* rank;          // [response]{pairs in which it is preferred, best | worst << 1}
   double* part;        // [response, or four short ones]{loss, u > 0, beta s_a, beta s_b, pairs} where it is preferred
   int32_t* done;       // workgroups that have left theirs
@@ -188,6 +189,34 @@ __global__ __launch_bounds__(256) void pref_sum_kernel(PrefArgs a) {
     a.sums[(int64_t)r * a.nb + b] = {(sh[0].x + sh[1].x) + (sh[2].x + sh[3].x), (sh[0].y + sh[1].y) + (sh[2].y + sh[3].y)};
 }
 
+// Of very long responses a workgroup adds up the blocks of one, which in the gradient's launch each block would do again.
+__global__ __launch_bounds__(1024) void pref_join_kernel(PrefArgs a) {
+  constexpr int U = 4;
+  __shared__ double2 sh[16];
+  const double2* from = a.sums + (int64_t)blockIdx.x * a.nb;
+  double2 s = {0.0, 0.0};
+  for (int b0 = threadIdx.x; b0 < a.nb; b0 += 1024 * U) {
+    double2 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u] = b0 + u * 1024 < a.nb ? from[b0 + u * 1024] : double2{0.0, 0.0};
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      s.x += x[u].x;
+      s.y += x[u].y;
+    }
+  }
+  s.x = wave_sum(s.x);
+  s.y = wave_sum(s.y);
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  for (int k = 1; k < 16; ++k) {
+    s.x += sh[k].x;
+    s.y += sh[k].y;
+  }
+  a.totals[blockIdx.x] = s;
+}
+
 // Sums of all slots of response r; one wavefront.
 __device__ inline double2 response_sums(const PrefArgs& a, int r, int lane) {
   constexpr int U = 8;
@@ -268,13 +297,13 @@ __global__ __launch_bounds__(256) void pref_grad_kernel(PrefArgs a, bool counted
   const int n = have ? length(a, r) : 0;
   auto sums = [&](int c) {
     double2 s = {0.0, 0.0};
-    for (int k0 = 0; k0 < a.nb; k0 += 4) {
+    for (int k0 = 0; k0 < a.ns; k0 += 4) {
       double2 x[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) x[k] = a.sums[(int64_t)c * a.nb + min(k0 + k, a.nb - 1)];
+      for (int k = 0; k < 4; ++k) x[k] = a.totals[(int64_t)c * a.ns + min(k0 + k, a.ns - 1)];
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        if (k0 + k < a.nb) {
+        if (k0 + k < a.ns) {
           s.x += x[k].x;
           s.y += x[k].y;
         }
@@ -379,8 +408,8 @@ __global__ __launch_bounds__(1024) void pref_few_kernel(PrefArgs a) {
 hipError_t launch_preference(const lmhead_preference& q, const float* lp, const float* lr, const float* reward, const int32_t* len,
                              int P, int G, int T, float* loss, float* g, float* ratio, float* stats, char* ws, hipStream_t s) {
   const PrefLayout L = pref_layout(P, G, T);
-  PrefArgs a{lp, lr, reward, len, P, G, T, (int)L.nb, q};
-  a.sums = reinterpret_cast<double2*>(ws + L.sums);
+  PrefArgs a{lp, lr, reward, len, P, G, T, (int)L.nb, (int)L.nb, q};
+  a.sums = a.totals = reinterpret_cast<double2*>(ws + L.sums);
   a.rank = reinterpret_cast<int2*>(ws + L.rank);
   a.part = reinterpret_cast<double*>(ws + L.part);
   a.done = reinterpret_cast<int32_t*>(ws + L.done);
@@ -399,6 +428,11 @@ hipError_t launch_preference(const lmhead_preference& q, const float* lp, const 
   const dim3 grid((unsigned)(shorts ? parts : L.R * L.nb));
   if (shorts) hipLaunchKernelGGL(pref_sum_short_kernel, grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL(pref_sum_kernel, grid, dim3(256), 0, s, a);
+  if (L.nb > kPrefBlocks) {
+    a.totals = reinterpret_cast<double2*>(ws + L.totals);
+    a.ns = 1;
+    hipLaunchKernelGGL(pref_join_kernel, dim3((unsigned)L.R), dim3(1024), 0, s, a);
+  }
   // every workgroup adds up the pairs of few prompts itself
   const bool counted = q.weights && L.R > kPrefCounted;
   if (counted) hipLaunchKernelGGL(pref_count_kernel, dim3(1), dim3(1024), 0, s, a);

@@ -23,11 +23,14 @@ constexpr int kPrefFewSlots = 8192;
 // counts on one word do).
 constexpr int kPrefShort = 1024;
 constexpr int kPrefTickets = 160;
+// From more blocks of a response on they are added up once, by a launch of its own: 2 x 2 responses of 16 blocks 12.4 us, so 13.7;
+// of 32 14.0 and 13.7; 4 x 4 of 128 53 and 25.
+constexpr int kPrefBlocks = 16;
 constexpr int kPrefCounted = 1024;      // up to so many responses each workgroup counts all pairs itself
 
 struct PrefLayout {
   int64_t R, nb;         // responses, blocks of kLossSlotsPerBlock slots in one
-  size_t done, sums, rank, part, total;
+  size_t done, sums, totals, rank, part, total;
 };
 static inline PrefLayout pref_layout(int64_t P, int64_t G, int64_t T) {
   PrefLayout L{};
@@ -41,6 +44,7 @@ static inline PrefLayout pref_layout(int64_t P, int64_t G, int64_t T) {
   };
   L.done = take(256);
   L.sums = take((size_t)(L.R * L.nb) * 2 * sizeof(double));
+  L.totals = take((size_t)L.R * 2 * sizeof(double));
   L.rank = take((size_t)L.R * 2 * sizeof(int32_t));
   L.part = take((size_t)L.R * 5 * sizeof(double));
   L.total = off;

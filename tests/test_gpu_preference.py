@@ -77,6 +77,36 @@ def test_sizes(P, G, T):
     check(P, G, T, 13, per_pair=T % 2 == 1, lens=[T] * (P * G))
 
 
+@pytest.mark.parametrize("P,G,T", [(2, 2, 32768), (2, 2, 32769), (1, 3, 100000), (1, 2, 2048 * 1024 + 5)])
+def test_long_responses(P, G, T):
+    check(P, G, T, 21, mean=True, nll_coef=0.1)
+    check(P, G, T, 22, lens=[T, 0, 70, T - 1][:P * G], use_ref=False)
+
+
+def test_as_many_slots_as_a_call_takes():
+    """Two responses of 2^30 - 1 slots, of numbers whose sums are exact."""
+    import torch
+    import paper_2603_04411_amd as L
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB")
+    T, lens = (1 << 30) - 1, [(1 << 30) - 1, (1 << 29) + 3]
+    logp = torch.full((2 * T,), -0.5, device="cuda")
+    logp[T - 1], logp[T], logp[T + lens[1] - 1], logp[T + lens[1]] = -3.5, -1.5, -7.5, float("nan")
+    loss, g, ratio, stats = (torch.full((n,), 7.0, device="cuda") for n in (1, 2 * T, 2, 4))
+    ws = torch.empty(L.preference_workspace_bytes(1, 2, T), dtype=torch.uint8, device="cuda")
+    q = L.make_preference(mean=True, beta=1.0)
+    L.preference_loss(q, logp, None, torch.tensor([1.0, 0.0], device="cuda"), torch.tensor(lens, dtype=torch.int32, device="cuda"), 1, 2, T,
+                      loss, g, ratio, stats, ws)
+    s = [-0.5 - 3 / lens[0], -0.5 - 8 / lens[1]]
+    slope = -1 / (1 + np.exp(s[0] - s[1]))
+    assert abs(float(loss) - np.log1p(np.exp(s[1] - s[0]))) <= 1.01 * EPS and np.all(np.abs(np64(ratio) - s) <= 1.01 * EPS * 0.5 + 1e-15)
+    want = [slope / lens[0], -slope / lens[1]]
+    for r in range(2):
+        at = g[r * T:(r + 1) * T]
+        got = float(at[0])
+        assert abs(got - want[r]) <= 1.01 * EPS * abs(want[r]) and bool((at[:lens[r]] == got).all()) and not bool(at[lens[r]:].any())
+
+
 def test_lengths_of_none_one_and_out_of_range():
     check(2, 3, 9, 3, lens=[0, 0, 0, 0, 1, 9], nll_coef=0.5)
     check(2, 3, 9, 3, lens=[0, 0, 0, 0, 1, 9], mean=True)
