@@ -335,22 +335,28 @@ __global__ __launch_bounds__(256) void sort_count_kernel(SortArgs a) {
 
 // A wavefront per digit value: exclusive sums over the tiles, and the total.
 __global__ __launch_bounds__(256) void sort_scan_kernel(SortArgs a) {
+  constexpr int U = 8;
   const int D = 1 << a.digit, groups = (D + 3) / 4;
   if (grid_wg() >= (uint32_t)groups) return fill(a.f, grid_wg() - groups);
   const int lane = threadIdx.x & 63, v = blockIdx.x * 4 + (threadIdx.x >> 6);
   if (v >= D) return;
   uint32_t* h = a.hist + (int64_t)v * a.tiles;
   uint32_t sum = 0;
-  for (int t0 = 0; t0 < a.tiles; t0 += 64) {
-    const uint32_t x = t0 + lane < a.tiles ? h[t0 + lane] : 0;
-    uint32_t s = x;
+  for (int t0 = 0; t0 < a.tiles; t0 += 64 * U) {
+    uint32_t x[U];
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint32_t y = __shfl_up(s, o);
-      if (lane >= o) s += y;
+    for (int u = 0; u < U; ++u) x[u] = t0 + u * 64 + lane < a.tiles ? h[t0 + u * 64 + lane] : 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      uint32_t s = x[u];
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t y = __shfl_up(s, o);
+        if (lane >= o) s += y;
+      }
+      if (t0 + u * 64 + lane < a.tiles) h[t0 + u * 64 + lane] = sum + s - x[u];
+      sum += __shfl(s, 63);
     }
-    if (t0 + lane < a.tiles) h[t0 + lane] = sum + s - x;
-    sum += __shfl(s, 63);
   }
   if (lane == 0) a.totals[v] = sum;
 }
