@@ -291,7 +291,7 @@ __device__ inline void fill(const Fill& f, int64_t block) {
   if (i < f.hi) *reinterpret_cast<f32x4*>(f.p + i) = f32x4{0.f, 0.f, 0.f, 0.f};
 }
 
-// A radix sort, least digit first, in tiles of 1024 slots: counts, their sums, places.  Launches and latency: of 524288 slots 7.6, 6 and 10 us
+// A radix sort, least digit first, in tiles of 1024 slots: counts, their sums, places.  Launches and latency: of 524288 slots 7, 4.8 and 9 us
 // a digit, of which 152064 ids have two.  (Tiles of 4096 slots: places alone 20, sixteen rounds of ballots one after the other.)
 struct SortArgs {
   Batch b;                 // first pass: keys come from here
@@ -333,7 +333,8 @@ __global__ __launch_bounds__(256) void sort_count_kernel(SortArgs a) {
   for (int i = threadIdx.x; i < D; i += 256) a.hist[a.scanned ? (int64_t)i * a.tiles + blockIdx.x : (int64_t)blockIdx.x * D + i] = h[i];
 }
 
-// A wavefront per digit value: exclusive sums over the tiles, and the total.
+// A wavefront per digit value: exclusive sums over the tiles, and the total.  Eight segments of 64 tiles are asked for at once (16.7
+// million rows of 64 columns 1444 us, with one segment after the other 1546).
 __global__ __launch_bounds__(256) void sort_scan_kernel(SortArgs a) {
   constexpr int U = 8;
   const int D = 1 << a.digit, groups = (D + 3) / 4;
