@@ -86,6 +86,20 @@ def test_more_tensors_than_one_launch_takes(count):
     check(ts, None, 2.0, in_place=True)
 
 
+def test_as_many_tensors_as_a_call_takes():
+    import torch
+    import paper_2603_04411_amd as L
+    sizes = [i % 6 for i in range(65536)]
+    starts = np.concatenate([[0], np.cumsum(sizes)[:-1]]).tolist()
+    buf = tensor(sum(sizes), "f32", 3)
+    before = np64(buf)
+    grads, norm = L.make_grad_list([buf[b:b + n] for b, n in zip(starts, sizes)]), torch.empty(2, device="cuda")
+    L.grad_clip(grads, None, 1.0, 0.0, norm, workspace())
+    n, c, want = O.grad_clip([before], 1.0, 0.0)
+    assert abs(float(norm[0]) - n) <= 1.01 * EPS * n and abs(float(norm[1]) - c) <= 1.01 * EPS * c
+    assert np.all(np.abs(np64(buf) - want[0]) <= 1.01 * 2 * EPS * np.abs(want[0]) + 1e-40)
+
+
 def test_one_long_tensor_among_small_ones():
     check([tensor(5, "f32", 1), tensor((1 << 24) + 77, "f32", 2), tensor(0, "bf16", 3), tensor(3, "bf16", 4)], ["bf16"] * 4, 1.0)
     check([tensor((1 << 24) + 77, "bf16", 2), tensor(1, "f32", 1)], None, 1.0, in_place=True)

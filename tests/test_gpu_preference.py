@@ -107,6 +107,24 @@ def test_as_many_slots_as_a_call_takes():
         assert abs(got - want[r]) <= 1.01 * EPS * abs(want[r]) and bool((at[:lens[r]] == got).all()) and not bool(at[lens[r]:].any())
 
 
+@pytest.mark.parametrize("weights", ["prompt", "pair"])
+def test_one_prompt_of_as_many_responses_as_a_call_takes(weights):
+    """2^31 pairs, all of them level: every loss is log 2, and a response's slope counts those above it and those below."""
+    import torch
+    import paper_2603_04411_amd as L
+    R = 65535
+    order = torch.randperm(R, generator=torch.Generator(device="cuda").manual_seed(4), device="cuda")
+    logp, lens = torch.full((R,), -0.5, device="cuda"), torch.ones(R, dtype=torch.int32, device="cuda")
+    loss, g, ratio, stats = run(L.make_preference(weights=weights, beta=0.5), logp, None, order.float(), lens, 1, R, 1)
+    pairs = R * (R - 1) // 2
+    # one rounding to fp32; fp64 sums of equal numbers, a thousand in a row and those in pairs, are off by 1e-13
+    assert abs(float(loss) - np.log(2.0)) <= 1.01 * EPS * np.log(2.0)
+    assert bool((ratio == -0.5).all()) and stats.tolist() == [0.0, -0.25, -0.25, float(np.float32(pairs))]
+    below = np64(order)
+    want = (below - (R - 1 - below)) * -0.25 / pairs
+    assert np.all(np.abs(np64(g) - want) <= 1.01 * EPS * np.abs(want) + 1e-25)
+
+
 def test_lengths_of_none_one_and_out_of_range():
     check(2, 3, 9, 3, lens=[0, 0, 0, 0, 1, 9], nll_coef=0.5)
     check(2, 3, 9, 3, lens=[0, 0, 0, 0, 1, 9], mean=True)
