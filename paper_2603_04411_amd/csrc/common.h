@@ -300,8 +300,6 @@ hipError_t launch_flowrl(const float* lp, const float* lr, const float* reward, 
 // flop each; operands: 256 bytes per thread, sink: one float per thread.
 hipError_t launch_mfma_probe(const void* operands, float* sink, int workgroups, int iters, hipStream_t s);
 
-constexpr int kLossSlotsPerBlock = 2048;
-
 // grpo_loss_noalloc keeps its block partials (four floats per block of kLossSlotsPerBlock slots of one
 // response) in a device array of the library image: at most this many blocks, 1 MiB.
 constexpr int kStaticLossParts = 65536;

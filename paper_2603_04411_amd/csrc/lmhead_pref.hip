@@ -351,8 +351,9 @@ __global__ __launch_bounds__(256) void pref_grad_kernel(PrefArgs a, bool counted
   }
   if (a.g && have) {
     if (kLong) g = gs;
-    const int t0 = b * kLossSlotsPerBlock, t1 = kLong ? min(t0 + kLossSlotsPerBlock, a.T) : a.T;
-    for (int t = t0 + (kLong ? (int)threadIdx.x : lane); t < t1; t += kLong ? 256 : 64) a.g[(int64_t)r * a.T + t] = t < n ? g : 0.f;
+    const int t0 = b * kLossSlotsPerBlock, slots = kLong ? block_slots(t0, a.T) : a.T;
+    float* out = a.g + (int64_t)r * a.T + t0;
+    for (int k = kLong ? (int)threadIdx.x : lane; k < slots; k += kLong ? 256 : 64) out[k] = t0 + k < n ? g : 0.f;
   }
   if (!ticket || b != 0) return;
   __syncthreads();

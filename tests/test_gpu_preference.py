@@ -107,6 +107,23 @@ def test_as_many_slots_as_a_call_takes():
         assert abs(got - want[r]) <= 1.01 * EPS * abs(want[r]) and bool((at[:lens[r]] == got).all()) and not bool(at[lens[r]:].any())
 
 
+@pytest.mark.parametrize("T", [(1 << 31) - 2048, (1 << 31) - 2047, (1 << 31) - 1])
+def test_one_response_of_as_many_slots_as_a_call_takes(T):
+    """The last block of 2048 slots ends where an int does, or one slot of it lies before that."""
+    import torch
+    import paper_2603_04411_amd as L
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB")
+    logp, lens = torch.full((T,), -0.5, device="cuda"), torch.tensor([T], dtype=torch.int32, device="cuda")
+    logp[0], logp[T - 1] = -2.0, -4.0
+    loss, g, ratio, stats = (torch.full((n,), 7.0, device="cuda") for n in (1, T, 1, 4))
+    ws = torch.empty(L.preference_workspace_bytes(1, 1, T), dtype=torch.uint8, device="cuda")
+    L.preference_loss(L.make_preference(), logp, None, torch.zeros(1, device="cuda"), lens, 1, 1, T, loss, g, ratio, stats, ws)
+    # one response is in no pair: loss, statistics and the gradient of every slot are 0
+    assert float(loss) == 0.0 and not stats.any() and float(ratio) == float(np.float32(-0.5 * T - 5.0))
+    assert all(not bool(g[lo:lo + (1 << 28)].any()) for lo in range(0, T, 1 << 28))
+
+
 @pytest.mark.parametrize("weights", ["prompt", "pair"])
 def test_one_prompt_of_as_many_responses_as_a_call_takes(weights):
     """2^31 pairs, all of them level: every loss is log 2, and a response's slope counts those above it and those below."""
