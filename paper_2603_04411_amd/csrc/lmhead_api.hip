@@ -82,9 +82,9 @@ IndexArgs index_args(const lmhead_desc* d, const Ws& w, const void* H, const int
   return a;
 }
 
-size_t loss_ws_bytes(int64_t P, int64_t G, int64_t T) {
+size_t loss_ws_bytes(int64_t P, int64_t G, int32_t T) {
   const int64_t R = P * G;
-  const int64_t nb = (T + kLossSlotsPerBlock - 1) / kLossSlotsPerBlock;
+  const int64_t nb = loss_blocks(T);
   return (size_t)(R * nb * 4 + R) * sizeof(float) + 256;
 }
 
@@ -410,7 +410,7 @@ int grpo_loss_noalloc(const float* logp, const float* logp_old, const float* log
   if (rc != LMHEAD_OK) return rc;
   if (agg_mode != 0 && agg_mode != 1) return LMHEAD_E_SHAPE;
   if (!logp || !logp_old || !adv || !len || !loss) return LMHEAD_E_NULL;
-  const int64_t nb = ((int64_t)T + kLossSlotsPerBlock - 1) / kLossSlotsPerBlock;
+  const int64_t nb = loss_blocks(T);
   if ((int64_t)P * G * nb > kStaticLossParts) return LMHEAD_E_WORKSPACE;   // beyond the static scratch
   float* scratch_dev = nullptr;
   LM_TRY(static_scratch(&scratch_dev));

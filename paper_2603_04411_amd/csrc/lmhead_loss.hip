@@ -87,7 +87,8 @@ __global__ __launch_bounds__(256) void grpo_kernel(const float* __restrict__ lp,
   const float A = adv[r];
   float s_loss = 0.f, s_clip = 0.f, s_k3 = 0.f, s_rho = 0.f;
   const int t0 = b * kLossSlotsPerBlock;
-  for (int t = t0 + threadIdx.x; t < min(t0 + kLossSlotsPerBlock, T); t += 256) {
+  for (int k = threadIdx.x; k < block_slots(t0, T); k += 256) {
+    const int t = t0 + k;
     const size_t i = (size_t)r * T + t;
     float g = 0.f;
     if (t < n) {
@@ -172,7 +173,8 @@ __global__ __launch_bounds__(256) void ce_kernel(const float* __restrict__ lp, c
   const float gv = nv_s > 0 ? -1.f / (float)nv_s : 0.f;
   float a = 0.f;
   const int t0 = b * kLossSlotsPerBlock;
-  for (int t = t0 + threadIdx.x; t < min(t0 + kLossSlotsPerBlock, T); t += 256) {
+  for (int k = threadIdx.x; k < block_slots(t0, T); k += 256) {
+    const int t = t0 + k;
     const size_t i = (size_t)r * T + t;
     if (t < n) a += lp[i];
     if (g_out) g_out[i] = t < n ? gv : 0.f;
@@ -204,8 +206,8 @@ __global__ __launch_bounds__(256) void tb_sum_kernel(const float* __restrict__ l
   const int n = min(max(len[r], 0), T);
   float a = 0.f, c = 0.f;
   const int t0 = b * kLossSlotsPerBlock;
-  for (int t = t0 + threadIdx.x; t < min(t0 + kLossSlotsPerBlock, n); t += 256) {
-    const size_t i = (size_t)r * T + t;
+  for (int k = threadIdx.x; k < block_slots(t0, n); k += 256) {
+    const size_t i = (size_t)r * T + t0 + k;
     a += lp[i];
     c += lr[i];
   }
@@ -261,8 +263,8 @@ __global__ __launch_bounds__(256) void tb_grad_kernel(const float* __restrict__ 
   const int n = min(max(len[r], 0), T);
   const float gv = n > 0 ? 2.f * dl[r] / ((float)R * (float)n) : 0.f;
   const int t0 = blockIdx.x * kLossSlotsPerBlock;
-  for (int t = t0 + threadIdx.x; t < min(t0 + kLossSlotsPerBlock, T); t += 256)
-    g_out[(size_t)r * T + t] = t < n ? gv : 0.f;
+  for (int k = threadIdx.x; k < block_slots(t0, T); k += 256)
+    g_out[(size_t)r * T + t0 + k] = t0 + k < n ? gv : 0.f;
 }
 
 }  // namespace
@@ -277,7 +279,7 @@ hipError_t launch_grpo(const float* lp, const float* lo, const float* lr, const 
                        const int32_t* len, int P, int G, int T, float clip_lo, float clip_hi, float kl,
                        int agg, float* loss, float* g, float* stats, float* ws, hipStream_t s) {
   const int R = P * G;
-  const int nb = (T + kLossSlotsPerBlock - 1) / kLossSlotsPerBlock;
+  const int nb = loss_blocks(T);
   hipLaunchKernelGGL(grpo_kernel, dim3(nb, R), dim3(256), 0, s, lp, lo, lr, adv, len, R, T,
                      1.f - clip_lo, 1.f + clip_hi, kl, agg, g, ws);
   hipLaunchKernelGGL(grpo_final_kernel, dim3(1), dim3(256), 0, s, ws, R * nb, len, R, T, loss, stats);
@@ -308,7 +310,7 @@ hipError_t static_scratch(float** out) {
 
 hipError_t launch_ce(const float* lp, const int32_t* len, int R, int T, float* loss, float* g, float* ws,
                      hipStream_t s) {
-  const int nb = (T + kLossSlotsPerBlock - 1) / kLossSlotsPerBlock;
+  const int nb = loss_blocks(T);
   hipLaunchKernelGGL(ce_kernel, dim3(nb, R), dim3(256), 0, s, lp, len, R, T, g, ws);
   hipLaunchKernelGGL(ce_final_kernel, dim3(1), dim3(256), 0, s, ws, R * nb, len, R, T, loss);
   return hipGetLastError();
@@ -318,7 +320,7 @@ hipError_t launch_flowrl(const float* lp, const float* lr, const float* reward, 
                          const int32_t* len, int P, int G, int T, float beta, float* loss, float* g,
                          float* gz, float* resid, float* ws, hipStream_t s) {
   const int R = P * G;
-  const int nb = (T + kLossSlotsPerBlock - 1) / kLossSlotsPerBlock;
+  const int nb = loss_blocks(T);
   float* dl = ws + (size_t)R * nb * 2;
   hipLaunchKernelGGL(tb_sum_kernel, dim3(nb, R), dim3(256), 0, s, lp, lr, len, T, ws);
   hipLaunchKernelGGL(tb_resid_kernel, dim3(1), dim3(256), 0, s, ws, nb, reward, logZ, len, P, G, T, beta,

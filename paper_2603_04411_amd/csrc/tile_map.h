@@ -23,6 +23,7 @@ inline int64_t chunk_rows(int64_t V, int64_t c0, int64_t n_tiles) { return V - c
 // The losses cut a response into blocks of so many slots.  A response has up to 2^31 - 1 of them: the end of its last block need not be an
 // int, so a block is its first slot and a count.
 constexpr int kLossSlotsPerBlock = 2048;
+LMHEAD_HD inline int loss_blocks(int T) { return (T - 1) / kLossSlotsPerBlock + 1; }   // T > 0
 LMHEAD_HD inline int block_slots(int t0, int T) { return T - t0 < kLossSlotsPerBlock ? T - t0 : kLossSlotsPerBlock; }
 
 // Workgroup -> tile mapping that keeps L2 traffic local to an XCD.

@@ -32,10 +32,10 @@ struct PrefLayout {
   int64_t R, nb;         // responses, blocks of kLossSlotsPerBlock slots in one
   size_t done, sums, totals, rank, part, total;
 };
-static inline PrefLayout pref_layout(int64_t P, int64_t G, int64_t T) {
+static inline PrefLayout pref_layout(int64_t P, int64_t G, int32_t T) {
   PrefLayout L{};
   L.R = P * G;
-  L.nb = (T + kLossSlotsPerBlock - 1) / kLossSlotsPerBlock;
+  L.nb = loss_blocks(T);
   size_t off = 0;
   auto take = [&](size_t bytes) {
     const size_t o = off;

@@ -13,6 +13,7 @@ int main() {
   long bad = 0, cases = 0;
   for (int T : {1, 2, k - 1, k, k + 1, 3 * k + 5, 1 << 30, most - k, most - k + 1, most - k + 2, most - 1, most}) {
     const int64_t blocks = ((int64_t)T + k - 1) / k;
+    if (loss_blocks(T) != blocks) ++bad;
     const int64_t from = blocks > 4 ? blocks - 4 : 0;
     int64_t next = from * k;
     for (int64_t b = from; b < blocks; ++b) {
