@@ -275,6 +275,7 @@ LMHEAD_API int flowrl_tb_loss(const float* logp, const float* logp_ref, const fl
  *     loss = sum over pairs of w l,   w = 1 / (P M_p) (weights = 0: mean over prompts of the mean over the prompt's M_p pairs; a prompt
  *     without pairs contributes 0) or 1 / M (weights = 1: mean over all M pairs)
  *     g_logp[r,t] = dloss/dlogp[r,t], the sum over all pairs that r is in; 0 on padding.  The reference is a constant.
+ * A term whose factor (smoothing, 1 - smoothing, margin_scale, nll_coef) is 0 is left out, also where it is not finite.
  * Sums over a response, the pairs and their sums are evaluated in fp64: u is a small difference of long sums.
  *   logp, logp_ref float[N]; reward float[R]; len int32[R] (clamped into [0, T]);
  *   loss float[1] (out; 0 without pairs); g_logp float[N] or NULL (out); ratio float[R] or NULL: s_r (out);

@@ -58,7 +58,8 @@ def preference_loss(logp, logp_ref, reward, lens, P, G, T, loss="logistic", extr
         u = ratio[a] - ratio[b]
         h = beta * u - margin - (margin_scale * (rw[a] - rw[b]) if margin_scale else 0.0)
         if loss == "logistic":
-            each = (1 - smoothing) * np.logaddexp(0.0, -h) + smoothing * np.logaddexp(0.0, h)
+            # a term whose factor is 0 is left out, also where it is infinite
+            each = ((1 - smoothing) * np.logaddexp(0.0, -h) if smoothing != 1 else 0.0) + (smoothing * np.logaddexp(0.0, h) if smoothing else 0.0)
             slope = beta * (smoothing - 0.5 * (1.0 - math.tanh(0.5 * h)))
         elif loss == "hinge":
             each, slope = max(0.0, 1.0 - h), -beta if h < 1.0 else 0.0
@@ -67,7 +68,7 @@ def preference_loss(logp, logp_ref, reward, lens, P, G, T, loss="logistic", extr
             each, slope = e * e, 2.0 * e
         else:
             raise ValueError(loss)
-        total += w * (each - nll_coef * like[a])
+        total += w * (each - (nll_coef * like[a] if nll_coef else 0.0))
         c[a] += w * slope
         c[b] -= w * slope
         nll[a] += w * nll_coef

@@ -115,9 +115,10 @@ __device__ inline Outcome outcome(const PrefArgs& a, int r, double sr, int lane,
       if (q.margin_scale != 0.f) h -= (double)q.margin_scale * (up ? (double)mine - x : (double)x - mine);
       double each, d;
       if (q.loss == LMHEAD_PREF_LOGISTIC) {
-        // e^-|h| once: log(1 + e^-|h|) for both logarithms, and sigma(-h) from it without overflow
+        // e^-|h| once: log(1 + e^-|h|) for both logarithms, and sigma(-h) from it without overflow.  A term whose factor is 0 is left
+        // out: at h = -inf or +inf one of the logarithms is infinite.
         const double e = exp(-fabs(h)), soft = log1p(e), small = e / (1.0 + e);
-        each = (1.0 - smooth) * (fmax(-h, 0.0) + soft);
+        each = smooth != 1.0 ? (1.0 - smooth) * (fmax(-h, 0.0) + soft) : 0.0;
         if (smooth != 0.0) each += smooth * (fmax(h, 0.0) + soft);
         d = beta * (smooth - (h > 0.0 ? small : 1.0 - small));
       } else if (q.loss == LMHEAD_PREF_HINGE) {

@@ -218,3 +218,16 @@ def test_the_gradient_is_the_difference_quotient_of_the_loss():
         slope = (at[0][0] - at[1][0]) / (at[0][1] - at[1][1])
         # losses below 4 are known to 2^-23 and divided by 2^-4; the third derivative of the logistic loss is at most beta^3 / 8, times step^2 / 6
         assert abs(slope - g[i]) <= 2 * 2.0 ** -23 * 4 / (2 * step) + 0.5 ** 3 / 8 * step ** 2 / 6 + 1e-7
+
+
+@pytest.mark.parametrize("side", [0, 1])
+@pytest.mark.parametrize("smoothing", [0.0, 0.25, 1.0])
+def test_a_term_whose_factor_is_zero_is_left_out(smoothing, side):
+    """h is -inf or +inf: what is left of the loss is one logarithm, or none."""
+    import paper_2603_04411_amd as L
+    logp, lens, rw = np.array([-1, -1, -2, -3], dtype=np.float32), np.array([2, 2], dtype=np.int32), np.array([1, 0], dtype=np.float32)
+    logp[2 * side] = -np.inf
+    want = O.preference_loss(logp, None, rw, lens, 1, 2, 2, beta=0.5, smoothing=smoothing)
+    loss, g, _, _ = run(L.make_preference(beta=0.5, smoothing=smoothing), to_device(logp), None, to_device(rw), to_device(lens), 1, 2, 2)
+    assert want[0] == (np.inf if 0 < smoothing < 1 or side == smoothing else 0.0) and float(loss) == want[0]
+    assert np.array_equal(np64(g), want[1]) and want[1][0] == (0.5 * (smoothing - 1) if side == 0 else 0.5 * smoothing)

@@ -49,6 +49,18 @@ def test_preference_closed_forms():
     assert abs(g.reshape(3, 24).sum(1)).max() < 1e-15
 
 
+def test_preference_terms_without_a_factor_are_left_out():
+    for side, h in ((0, -math.inf), (1, math.inf)):
+        logp = [-1.0, -1.0]
+        logp[side] = -math.inf
+        for smoothing in (0.0, 0.25, 1.0):
+            l, g, _, _ = O.preference_loss(logp, None, [1.0, 0.0], [1, 1], 1, 2, 1, beta=0.5, smoothing=smoothing)
+            # -(1 - smoothing) log sigma(h) - smoothing log sigma(-h), and its slope beta (smoothing - sigma(-h))
+            left = (1 - smoothing if h < 0 else smoothing)
+            assert l == (math.inf if left else 0.0)
+            assert g.tolist() == [0.5 * (smoothing - (h < 0)), -0.5 * (smoothing - (h < 0))]
+
+
 def test_extreme_pairs_take_the_first_of_equals():
     assert O.prompt_pairs([0.5, 1.0, 0.0, 1.0, 0.0, 0.5], 1, 6, True) == [(1, 2, 1)]
     assert O.prompt_pairs([2.0, 1.0, 1.0, 2.0], 2, 2, True) == [(0, 1, 1), (3, 2, 1)]
