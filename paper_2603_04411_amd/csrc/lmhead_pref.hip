@@ -123,7 +123,7 @@ __device__ inline Outcome outcome(const PrefArgs& a, int r, double sr, int lane,
         d = beta * (smooth - (h > 0.0 ? small : 1.0 - small));
       } else if (q.loss == LMHEAD_PREF_HINGE) {
         each = h >= 1.0 ? 0.0 : 1.0 - h;     // NaN stays
-        d = h >= 1.0 ? 0.0 : -beta;
+        d = h < 1.0 ? -beta : 0.0;
       } else {
         const double e = h / beta - 0.5 / beta;
         each = e * e;

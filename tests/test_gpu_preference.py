@@ -231,3 +231,14 @@ def test_a_term_whose_factor_is_zero_is_left_out(smoothing, side):
     loss, g, _, _ = run(L.make_preference(beta=0.5, smoothing=smoothing), to_device(logp), None, to_device(rw), to_device(lens), 1, 2, 2)
     assert want[0] == (np.inf if 0 < smoothing < 1 or side == smoothing else 0.0) and float(loss) == want[0]
     assert np.array_equal(np64(g), want[1]) and want[1][0] == (0.5 * (smoothing - 1) if side == 0 else 0.5 * smoothing)
+
+
+def test_a_hinge_of_no_number_has_no_slope():
+    """[h < 1] of a NaN is 0; the pairs that are numbers keep their slopes."""
+    import paper_2603_04411_amd as L
+    logp, lens, rw = np.array([-1, np.nan, -2, -3], dtype=np.float32), np.ones(4, dtype=np.int32), np.array([2, 1, 0, 0], dtype=np.float32)
+    want = O.preference_loss(logp, None, rw, lens, 1, 4, 1, loss="hinge", beta=0.5)
+    loss, g, _, _ = run(L.make_preference("hinge", beta=0.5), to_device(logp), None, to_device(rw), to_device(lens), 1, 4, 1)
+    assert np.isnan(float(loss))
+    # of the five pairs three are NaN, one has h = 0.5 * (3 - 1), where the slope has ended, and one 0.5 * (2 - 1)
+    assert want[1].tolist() == [-0.1, 0.0, 0.1, 0.0] and np.all(np.abs(np64(g) - want[1]) <= 1.01 * EPS * np.abs(want[1]))
