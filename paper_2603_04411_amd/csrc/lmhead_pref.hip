@@ -155,7 +155,7 @@ __device__ inline float slot_gradient(const PrefArgs& a, int r, const Outcome& o
 constexpr int kParts = 5;
 __device__ inline void contribution(const PrefArgs& a, int r, const Outcome& o, double ratio, double logp_sum, double (&p)[kParts]) {
   double l = o.loss;
-  if (a.q.nll_coef != 0.f && o.won > 0) l -= o.won * a.q.nll_coef * (logp_sum * per_token(a, r));
+  if (a.q.nll_coef != 0.f && o.won > 0) l -= o.won * (double)a.q.nll_coef * (logp_sum * per_token(a, r));
   p[0] = o.w * l;
   p[1] = o.hit;
   p[2] = o.won > 0 ? a.q.beta * ratio * o.won : 0.0;

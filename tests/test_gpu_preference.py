@@ -242,3 +242,18 @@ def test_a_hinge_of_no_number_has_no_slope():
     assert np.isnan(float(loss))
     # of the five pairs three are NaN, one has h = 0.5 * (3 - 1), where the slope has ended, and one 0.5 * (2 - 1)
     assert want[1].tolist() == [-0.1, 0.0, 0.1, 0.0] and np.all(np.abs(np64(g) - want[1]) <= 1.01 * EPS * np.abs(want[1]))
+
+
+def test_the_likelihood_is_counted_in_64_bits():
+    """One response preferred to six at the same log-ratio: the factor 6 * 1.333483, rounded to fp32 on the way, is off by a whole half step,
+    and what the loss then rounds to by another."""
+    import paper_2603_04411_amd as L
+    x, nll = float(np.float32(-1537.689208984375)), float(np.float32(1.333483))
+    for T, G in ((1, 7), (1300, 7)):
+        logp, lens = np.full(G * T, x, dtype=np.float32), np.ones(G, dtype=np.int32)
+        rw = np.array([1] + [0] * (G - 1), dtype=np.float32)
+        for weights in ("prompt", "pair"):
+            loss, *_ = run(L.make_preference(nll_coef=nll, weights=weights), to_device(logp), None, to_device(rw), to_device(lens), 1, G, T)
+            want = np.log(2.0) - nll * x
+            # fp64 sums of a few terms are far below the one rounding to fp32
+            assert abs(float(loss) - want) <= 1.01 * EPS * want
