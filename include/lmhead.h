@@ -342,7 +342,8 @@ LMHEAD_API int embed_bwd(const lmhead_embed_desc* desc, const void* gX, const in
  *   out  host array of `count` tensors with the same element counts, of either type, or NULL: g is scaled in place (and left
  *        untouched in memory where c is 1).  An output may be its own input (same pointer, same type); any other overlap
  *        of an output with an input or an output is refused (LMHEAD_E_SHAPE).
- *   ws   grad_workspace_bytes() bytes, 256-byte aligned
+ *   norm float[1], of grad_clip float[2] (out);   ws   grad_workspace_bytes() bytes, 256-byte aligned.  Neither may overlap a tensor or the
+ *        other (LMHEAD_E_SHAPE).
  * The arrays are read during the call and not kept; the call may be captured into a graph, which then holds the pointers.
  * LMHEAD_E_SHAPE also for max_norm < 0 or NaN, for eps < 0 or not finite, for more than 2^37 elements in a tensor
  * or 2^41 in all.

@@ -57,6 +57,19 @@ struct Span {
   bool written;
 };
 
+// Whether `norm` (of `norms` elements) and the workspace share no memory with a tensor, nor with each other.
+bool scratch_apart(const lmhead_tensor* g, const lmhead_tensor* out, int32_t count, const float* norm, int norms, const void* ws) {
+  const uintptr_t n0 = reinterpret_cast<uintptr_t>(norm), n1 = n0 + norms * sizeof(float);
+  const uintptr_t w0 = reinterpret_cast<uintptr_t>(ws), w1 = w0 + grad_ws_bytes();
+  auto clear = [&](const lmhead_tensor& t) {
+    const uintptr_t lo = reinterpret_cast<uintptr_t>(t.data), hi = lo + (uintptr_t)t.n * element_bytes(t.dtype);
+    return t.n == 0 || ((hi <= n0 || n1 <= lo) && (hi <= w0 || w1 <= lo));
+  };
+  for (int i = 0; i < count; ++i)
+    if (!clear(g[i]) || (out && !clear(out[i]))) return false;
+  return n1 <= w0 || w1 <= n0;
+}
+
 // Whether some output shares memory with another output, or with an input that is not itself.
 int outputs_apart(const lmhead_tensor* g, const lmhead_tensor* out, int32_t count) {
   constexpr int kOnStack = 256;
@@ -149,6 +162,7 @@ int grad_norm(const lmhead_tensor* g, int32_t count, float* norm, void* ws, size
   if (rc != LMHEAD_OK) return rc;
   if (!aligned(ws, 256)) return LMHEAD_E_ALIGN;
   if (ws_bytes < grad_ws_bytes()) return LMHEAD_E_WORKSPACE;
+  if (!scratch_apart(g, nullptr, count, norm, 1, ws)) return LMHEAD_E_SHAPE;
   LM_TRY(launch_grads(g, nullptr, count, false, 0.f, 0.f, norm, static_cast<char*>(ws), static_cast<hipStream_t>(stream)));
   return LMHEAD_OK;
 }
@@ -165,6 +179,7 @@ int grad_clip(const lmhead_tensor* g, const lmhead_tensor* out, int32_t count, f
     if (out[i].n != g[i].n) return LMHEAD_E_SHAPE;
   if (!aligned(ws, 256)) return LMHEAD_E_ALIGN;
   if (ws_bytes < grad_ws_bytes()) return LMHEAD_E_WORKSPACE;
+  if (!scratch_apart(g, out, count, norm, 2, ws)) return LMHEAD_E_SHAPE;
   rc = outputs_apart(g, out, count);
   if (rc != LMHEAD_OK) return rc;
   LM_TRY(launch_grads(g, out, count, true, max_norm, eps, norm, static_cast<char*>(ws), static_cast<hipStream_t>(stream)));

@@ -136,6 +136,46 @@ def test_outputs_of_clipping_have_to_lie_apart(lib):
     assert code(inside, _tensors((1 << 26, 1000), (far + 2000, 4))) == -2                           # an output inside a long input
 
 
+def test_norm_and_workspace_have_to_lie_apart_from_the_gradients(lib):
+    need, at, norm, ws = L.grad_workspace_bytes(), 1 << 30, 1 << 24, 1 << 26
+    far = 1 << 32
+    g, out = _tensors((at, 100), (at + 4096, 7, 1), (far, 0)), _tensors((at + 8192, 100), (at + 16384, 7), (far, 0))
+
+    def clip(t, o, norm, ws):
+        return lib.grad_clip(t, o, 3, 1.0, 0.0, norm, ws, need, None)
+    # the first and the last element of an input in either type, and of an output; norm has two elements
+    for o in (None, out):
+        for p in (at, at + 396, at - 4, at + 4096, at + 4108):
+            assert clip(g, o, p, ws) == -2, p
+    for p in (at + 8192, at + 8192 + 396, at + 8188, at + 16384 + 24):
+        assert clip(g, out, p, ws) == -2
+    for p in (at, at + 256, at + 4096, at + 256 - (need + 255) // 256 * 256):
+        assert clip(g, None, norm, p) == -2 and lib.grad_norm(g, 3, norm, p, need, None) == -2
+    assert clip(g, out, norm, at + 16384) == -2
+    for p in (ws, ws + need - 4, ws - 4):
+        assert clip(g, None, p, ws) == -2, p
+    # the norm alone is one element
+    for p in (at, at + 396, at + 4096, at + 4108, ws, ws + need - 4):
+        assert lib.grad_norm(g, 3, p, ws, need, None) == -2, p
+
+
+def test_outputs_of_clipping_have_to_lie_apart_where_norm_and_workspace_do(lib):
+    need, far = L.grad_workspace_bytes(), 1 << 24
+
+    def code(g, out):
+        return lib.grad_clip(g, out, len(g), 1.0, 0.0, 1 << 40, 1 << 41, need, None)
+    g = _tensors((P_, 100), (P_ + 400, 100))
+    assert code(_tensors((P_, 100), (P_ + 396, 100)), None) == -2                                   # in place, twice the same element
+    assert code(_tensors((P_, 100), (P_, 100)), None) == -2
+    assert code(g, _tensors((far, 100), (far + 396, 100))) == -2                                    # output on output
+    assert code(g, _tensors((far, 100), (P_ + 396, 100))) == -2                                     # output on another's input
+    assert code(g, _tensors((P_ + 4, 100), (far, 100))) == -2                                       # its own input, shifted
+    assert code(g, _tensors((P_, 100, 1), (far, 100))) == -2                                        # its own input, another type
+    assert code(g, _tensors((P_ + 400, 100), (P_, 100))) == -2                                      # exchanged
+    assert code(_tensors(*[(far + 64 * i, 16) for i in range(1000)], (far + 64 * 500 + 60, 1)), None) == -2
+    assert code(_tensors((far, 1000), (P_, 4)), _tensors((1 << 26, 1000), (far + 2000, 4))) == -2   # an output inside a long input
+
+
 def test_binding_refuses_what_the_call_cannot_take():
     import torch
     cpu = torch.zeros(64)
