@@ -178,12 +178,14 @@ def embed_bwd(desc, gX, tok, lens, scale, dW, ws) -> None:
 class GradList:
     """The tensors of a call to grad_norm or grad_clip, as the ABI takes them.  Buffers that stay the same from step to step need one
     list.  It holds on to the memory that the tensors had when it was made: a tensor that is given other memory later (``set_``,
-    assigning ``data``) needs a new list."""
+    assigning ``data``) needs a new list.  Resizing a tensor or its storage frees that memory; a call with the list then raises
+    ``ValueError``."""
 
     def __init__(self, tensors):
         self.tensors = [t.detach() for t in tensors]
         self.array = (_Tensor * max(len(self.tensors), 1))()
         self.device = None
+        found = {}              # by the address that the list relies on: the storage, and the first tensor in it
         for i, t in enumerate(self.tensors):
             name = f"gradient {i}"
             if not t.is_cuda:
@@ -197,6 +199,10 @@ class GradList:
             elif t.get_device() != self.device:
                 _bad(name, f"on cuda:{t.get_device()}, others on cuda:{self.device}")
             self.array[i] = _Tensor(t.data_ptr() or None, t.numel(), _CODES[t.dtype], 0)
+            if t.numel():
+                storage = t.untyped_storage()
+                found.setdefault(storage.data_ptr(), (storage, i))
+        self.addresses, self.storages, self.first = list(found), [s for s, _ in found.values()], [i for _, i in found.values()]
 
     def __len__(self):
         return len(self.tensors)
@@ -211,6 +217,10 @@ def _list(g, device):
         return None
     if g.device is not None and g.device != device:
         _bad("gradients", f"on cuda:{g.device}, the current device is cuda:{device}")
+    now = list(map(torch.UntypedStorage.data_ptr, g.storages))      # 0.07 us each
+    if now != g.addresses:
+        i = next(i for i, a, b in zip(g.first, now, g.addresses) if a != b)
+        _bad(f"gradient {i}", "its storage was resized after the list was made")
     return g.array
 
 

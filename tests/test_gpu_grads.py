@@ -187,6 +187,24 @@ def test_a_list_keeps_the_memory_that_it_was_made_with():
     assert bool((t == 5.0).all()) and bool((old < 2.0).all())
 
 
+def test_a_list_refuses_memory_that_was_freed():
+    import torch
+    import paper_2603_04411_amd as L
+    norm, ws = torch.empty(2, device="cuda"), workspace()
+    for change in (lambda t: t.resize_(1 << 20), lambda t: t.untyped_storage().resize_(0)):
+        keep, moved = tensor(1000, "f32", 1), tensor(2000, "bf16", 2)
+        good, bad = L.make_grad_list([keep, keep.clone()]), L.make_grad_list([keep, moved])
+        L.grad_clip(bad, None, 1.0, 0.0, norm, ws)
+        change(moved)
+        before = keep.clone()
+        for call in (lambda: L.grad_norm(bad, norm, ws), lambda: L.grad_clip(bad, None, 0.5, 0.0, norm, ws),
+                     lambda: L.grad_clip(good, bad, 0.5, 0.0, norm, ws)):
+            with pytest.raises(ValueError, match="gradient 1"):
+                call()
+        assert torch.equal(keep, before)
+        L.grad_clip(good, None, 0.5, 0.0, norm, ws)
+
+
 def test_the_same_bits_each_time():
     import torch
     import paper_2603_04411_amd as L

@@ -223,3 +223,44 @@ def test_binding_refuses_what_the_call_cannot_take():
                              (Fake((4, 8), (16, 1)), 4, 8, 0), (Fake((4, 8), (8, 1)), 4, 16, 0), (Fake((4, 8), (16, 1)), 4, 16, 1)):
         with pytest.raises(ValueError):
             B._rows(t, "x", f32, rows, 8, ld, dev)
+
+
+class OnDevice:
+    """A host tensor that says it is on cuda:0; what it holds is never read."""
+
+    def __init__(self, t):
+        self.t = t
+    is_cuda = True
+
+    def get_device(self): return 0
+    def detach(self): return OnDevice(self.t.detach())
+    def __getattr__(self, name): return getattr(self.t, name)
+
+
+def test_a_list_refuses_tensors_whose_memory_has_been_freed():
+    """Resizing a storage frees what the list points to, whoever holds on to the tensor."""
+    import torch
+
+    def bigger(t): t.resize_(4096)
+    def gone(t): t.untyped_storage().resize_(0)
+    def other(t): t.untyped_storage().resize_(1 << 16)
+    for change in (bigger, gone, other):
+        ts = [torch.zeros(100), torch.zeros(200, dtype=torch.bfloat16)]
+        g = L.make_grad_list([OnDevice(t) for t in ts])
+        assert B._list(g, 0) is g.array
+        change(ts[1])
+        with pytest.raises(ValueError, match="gradient 1"):
+            B._list(g, 0)
+    # views of one buffer, and empty tensors, which may get memory later
+    buf, none = torch.zeros(1000), torch.zeros(0)
+    g = L.make_grad_list([OnDevice(none)] + [OnDevice(buf[i:i + 10]) for i in range(0, 1000, 10)])
+    none.resize_(100)
+    assert B._list(g, 0) is g.array and g.array[0].n == 0
+    buf.untyped_storage().resize_(1 << 16)
+    with pytest.raises(ValueError, match="gradient 1"):
+        B._list(g, 0)
+    # the list keeps what it was made with where the tensor moves on by itself
+    t = torch.zeros(100)
+    g, at = L.make_grad_list([OnDevice(t)]), t.data_ptr()
+    t.data = torch.zeros(300)
+    assert B._list(g, 0) is g.array and g.array[0].data == at == g.tensors[0].data_ptr()
