@@ -9,7 +9,7 @@ import ctypes as C
 
 import torch
 
-from .binding import FLAG_ACCUM_DW, LMHEAD_BF16, LMHEAD_F32, _check, load_library
+from .binding import FLAG_ACCUM_DW, LMHEAD_BF16, LMHEAD_F32, LmheadError, _check, load_library
 
 _DTYPES = {"bf16": LMHEAD_BF16, "f32": LMHEAD_F32}
 _TORCH = {LMHEAD_BF16: torch.bfloat16, LMHEAD_F32: torch.float32}
@@ -126,6 +126,8 @@ def preference_workspace_bytes(P: int, G: int, T: int) -> int:
 
 
 def preference_loss(params, logp, logp_ref, reward, lens, P, G, T, loss, g_logp, ratio, stats, ws) -> None:
+    if P < 0 or G < 0 or T < 0:      # as an int32 of the call it might not be
+        raise LmheadError(-2, "preference_loss")
     lib, dev, f32 = _lib(), _device(), torch.float32
     R, N = P * G, P * G * T
     rc = lib.preference_loss(

@@ -48,6 +48,16 @@ def test_preference_refusals(lib):
     assert call(q=q) == -2
 
 
+def test_preference_sizes_are_not_taken_modulo_2_to_the_32(lib):
+    """-(2^32) + 2 arrives as 2 where an int is 32 bits wide; the elements that tensors have to hold would be a negative number."""
+    import torch
+    t = torch.zeros(1)
+    for P, G, T in ((2 - (1 << 32), 2, 4), (2, 2 - (1 << 32), 4), (2, 2, 4 - (1 << 32)), (-1, 2, 4)):
+        with pytest.raises(L.LmheadError) as e:
+            L.preference_loss(L.make_preference(), t, None, t, t, P, G, T, t, None, None, None, t)
+        assert e.value.code == -2
+
+
 def test_embed_refusals(lib):
     kw0 = dict(R=3, T=7, d=64, V=100, dtype="bf16")
     ok = L.make_embed_desc(**kw0)
