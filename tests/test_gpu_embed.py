@@ -226,6 +226,65 @@ def test_backward_reports_what_is_out_of_range():
         backward(2, 4, 16, 5, "bf16", np.abs(tok) % 5, [5, -3], add=add, code=-6)
 
 
+BAD_IDS = [-1, 500, 501, (1 << 22) - 1, 1 << 22, (1 << 31) - 1, -(1 << 31)]       # of 500
+
+
+def batch_with_faults(R, T, fault):
+    """(ids, lengths, the code that the call leaves): faults at the first, the last and some other slot that counts, on padding alone, or in
+    a length."""
+    tok, lens, N = ids(500, R * T, R * T), np.full(R, T, dtype=np.int64), R * T
+    if fault == "ids":
+        tok[np.random.default_rng(N).permutation(N)[:len(BAD_IDS)]] = BAD_IDS
+        tok[0], tok[-1] = BAD_IDS[0], BAD_IDS[1]
+    elif fault == "first id":
+        tok[0] = -1
+    elif fault == "last id":
+        tok[-1] = 500
+    elif fault == "ids on padding":
+        lens[:] = T - len(BAD_IDS)
+        tok.reshape(R, T)[:, -len(BAD_IDS):] = BAD_IDS
+    elif fault == "negative length":
+        lens[-1] = -3
+    elif fault == "long length":
+        lens[0] = T + 1
+    return tok, lens, 0 if fault in ("none", "ids on padding") else -6
+
+
+FAULTS = ["ids", "first id", "last id", "ids on padding", "negative length", "long length"]
+
+
+# without a sort, tiles sorted by themselves, by digits, by digits with a scan
+@pytest.mark.parametrize("R,T", [(3, 300), (3, 1001), (3, 6700), (5, 14001)])
+@pytest.mark.parametrize("add", [False, True])
+def test_every_sort_reports_what_is_out_of_range(R, T, add):
+    import torch
+    import paper_2603_04411_amd as L
+    d, V = 16, 500
+    ws = torch.full((L.embed_workspace_bytes(L.make_embed_desc(R, T, d, V, "bf16")),), 0xFF, dtype=torch.uint8, device="cuda")
+    for fault in FAULTS + ["none"]:      # each call starts with what the one before has left
+        tok, lens, code = batch_with_faults(R, T, fault)
+        backward(R, T, d, V, "bf16", tok, lens, add=add, code=code, ws=ws)
+
+
+# the line where another workgroup reports what all have met
+@pytest.mark.parametrize("R,T", [(4, 1024), (17, 241), (3, 20000)])
+@pytest.mark.parametrize("d", [16, 2056])
+def test_every_lookup_reports_what_is_out_of_range(R, T, d):
+    import torch
+    import paper_2603_04411_amd as L
+    V = 500
+    W = torch.randn(V, d, generator=torch.Generator(device="cuda").manual_seed(d), device="cuda").to(torch.bfloat16)
+    desc, ws = L.make_embed_desc(R, T, d, V, "bf16"), torch.full((256,), 0xFF, dtype=torch.uint8, device="cuda")
+    for fault in FAULTS + ["none"]:
+        tok, lens, code = batch_with_faults(R, T, fault)
+        X = torch.full((R * T, d), 3.0, dtype=torch.bfloat16, device="cuda")
+        L.embed_fwd(desc, W, to_device(tok), to_device(lens.astype(np.int32)), 1.0, X, ws)
+        assert L.lmhead_check(ws) == code, fault
+        ok = torch.from_numpy(O.valid_slots(tok, lens, R, T, V)).cuda()
+        rows = W[torch.from_numpy(np.where(ok.cpu(), tok, 0).astype(np.int64)).cuda()]
+        assert torch.equal(X, torch.where(ok[:, None], rows, torch.zeros_like(rows))), fault
+
+
 def test_padded_gradients_do_not_matter():
     import torch
     R, T, d, V = 3, 40, 64, 9
