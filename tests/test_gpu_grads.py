@@ -105,6 +105,73 @@ def test_one_long_tensor_among_small_ones():
     check([tensor((1 << 24) + 77, "bf16", 2), tensor(1, "f32", 1)], None, 1.0, in_place=True)
 
 
+def ragged(total, count, unit, seed):
+    """`count` sizes that take `total` pieces of `unit` elements in all; some are empty, some end with a piece, some in it."""
+    r = np.random.default_rng(seed)
+    pieces = np.zeros(count, dtype=np.int64)
+    full = r.permutation(count)[:max(1, count - count // 8)]
+    cuts = np.sort(r.choice(np.arange(1, total), len(full) - 1, replace=False)) if len(full) > 1 else np.array([], dtype=np.int64)
+    pieces[full] = np.diff(np.concatenate([[0], cuts, [total]]))
+    assert pieces.sum() == total
+    return [0 if p == 0 else int(p) * unit - (0 if i % 3 == 0 else int(r.integers(0, unit))) for i, p in enumerate(pieces)]
+
+
+def check_on_the_card(sizes, kinds, max_norm=1.0):
+    """Norm and factor against fp64 sums, every element against the product in fp32 with the factor that was written."""
+    import torch
+    import paper_2603_04411_amd as L
+    types = [torch.bfloat16 if k == "bf16" else torch.float32 for k in kinds]
+    starts = np.concatenate([[0], np.cumsum([-(-n // 8) * 8 for n in sizes])]).tolist()
+    bufs = {t: torch.randn(starts[-1], generator=torch.Generator(device="cuda").manual_seed(len(sizes)), device="cuda").to(t) for t in set(types)}
+    ts = [bufs[t][b:b + n] for t, b, n in zip(types, starts, sizes)]
+    # tensors weigh differently: a piece that is left out, or counted with another tensor, shows
+    for i, t in enumerate(ts):
+        t.mul_(2.0 ** (i % 5))
+    n = float(torch.stack([t.double().square().sum() for t in ts]).sum().sqrt())
+    c = min(1.0, float(np.float32(max_norm)) / n)
+    norm = torch.full((2,), 7.0, device="cuda")
+    grads = L.make_grad_list(ts)
+    L.grad_norm(grads, norm, workspace())
+    assert abs(float(norm[0]) - n) <= 1.01 * EPS * n and float(norm[1]) == 7.0
+    outs = [torch.full_like(t, 9.0, dtype=torch.float32 if i % 2 else torch.bfloat16) for i, t in enumerate(ts)]
+    for out in (outs, None):
+        L.grad_clip(grads, None if out is None else L.make_grad_list(out), max_norm, 0.0, norm, workspace())
+        assert abs(float(norm[0]) - n) <= 1.01 * EPS * n and abs(float(norm[1]) - c) <= 1.01 * EPS * c
+        if out is not None:
+            f = norm[1].clone()
+            assert all(torch.equal(o, (t.float() * f).to(o.dtype)) for o, t in zip(out, ts))
+            want = [(t.float() * f).to(t.dtype) for t in ts]
+    assert all(torch.equal(t, w) for t, w in zip(ts, want))
+
+
+# where the second pass stops adding up the partial sums itself, where a workgroup takes two pieces and then three; the table in the
+# arguments and in the workspace
+@pytest.mark.parametrize("count", [1, 90, 96, 97, 300])
+@pytest.mark.parametrize("pieces", [511, 512, 513, 4095, 4096, 4097, 6145])
+def test_where_the_passes_change(count, pieces):
+    sizes = ragged(pieces, count, 8192, pieces + count)
+    assert sum(-(-n // 8192) for n in sizes) == pieces
+    check_on_the_card(sizes, ["bf16" if i % 3 else "f32" for i in range(count)])
+
+
+# one workgroup takes up to 48 pieces of 2048 elements
+@pytest.mark.parametrize("count", [1, 7, 48])
+@pytest.mark.parametrize("pieces", [48, 49])
+def test_where_one_workgroup_ends(count, pieces):
+    sizes = ragged(pieces, count, 2048, pieces + count)
+    assert sum(-(-n // 2048) for n in sizes) == pieces
+    check_on_the_card(sizes, ["f32" if i % 3 else "bf16" for i in range(count)])
+
+
+# sixteen pieces a workgroup, and more where the partial sums would be more than 16384
+@pytest.mark.parametrize("pieces", [(1 << 15) - 1, 1 << 15, 1 << 18, (1 << 18) + 1])
+def test_where_workgroups_take_sixteen_pieces_and_more(pieces):
+    import torch
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("needs 60 GB")
+    check_on_the_card(ragged(pieces, 60, 8192, pieces), ["bf16"] * 60)
+
+
 def test_empty_tensors():
     import torch
     import paper_2603_04411_amd as L
