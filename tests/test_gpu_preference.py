@@ -257,3 +257,54 @@ def test_the_likelihood_is_counted_in_64_bits():
             want = np.log(2.0) - nll * x
             # fp64 sums of a few terms are far below the one rounding to fp32
             assert abs(float(loss) - want) <= 1.01 * EPS * want
+
+
+def check_each(P, G, T, seed, lens=None, **kw):
+    """`check` of the logistic loss with a bound of its own for each output."""
+    import paper_2603_04411_amd as L
+    logp, ref, rw, lens = inputs(P, G, T, seed, lens)
+    beta, nll, mean, per_pair = float(np.float32(kw["beta"])), float(np.float32(kw.get("nll_coef", 0.0))), kw.get("mean", False), kw.get("per_pair", False)
+    q = L.make_preference(mean=mean, weights="pair" if per_pair else "prompt", beta=beta, nll_coef=nll)
+    got = [np64(t) for t in run(q, to_device(logp), to_device(ref), to_device(rw), to_device(lens), P, G, T)]
+    want = O.preference_loss(logp, ref, rw, lens, P, G, T, beta=beta, nll_coef=nll, mean=mean, per_pair=per_pair)
+    n = np.clip(lens, 0, T)
+    valid = np.arange(T)[None, :] < n[:, None]
+    sizes = np.where(valid, np.abs(np.where(valid, logp.reshape(P * G, T), 0.0)) + np.abs(np.where(valid, ref.reshape(P * G, T), 0.0)), 0.0)
+    per = np.where(n > 0, 1.0 / np.maximum(n, 1), 0.0)
+    # a sum over a response: at most 64 additions one after the other on the way of each slot, half a step of what has been added each
+    f64 = 2.0 ** -53
+    off = 64 * f64 * sizes.sum(1) * (per if mean else 1.0)
+    like = np.where(valid, np.abs(np.where(valid, logp.reshape(P * G, T), 0.0)), 0.0).sum(1) * per
+    pairs = O.prompt_pairs(rw, P, G)
+    weight = np.zeros(P * G)
+    for a, b, m in pairs:
+        w = 1.0 / len(pairs) if per_pair else 1.0 / (P * m)
+        weight[a] += w
+        weight[b] += w
+    # the loss of a pair moves by beta for its log-ratio, its slope by beta^2 / 4; what is added up over up to 256 pairs one after the other
+    # and with exp and log1p is off by as many half steps
+    many = 512 * f64
+    e_loss = 2 * beta * off.max() + many * (np.log(2.0) + beta * np.abs(want[2]).max() * 2 + nll * like.max())
+    e_g = weight * (beta ** 2 / 4 * 2 * off.max() + many * beta) * (per if mean else 1.0) + weight * nll * many * per
+    e_stats = np.array([0.0, beta * (off.max() + many * np.abs(want[2]).max()), beta * (off.max() + many * np.abs(want[2]).max()), 0.0])
+    bounds = (e_loss, np.repeat(e_g, T), off + 4 * f64 * np.abs(want[2]), e_stats)
+    for name, a, b, e in zip(("loss", "g_logp", "ratio", "stats"), got, want, bounds):
+        assert np.all(np.abs(a.reshape(-1) - b) <= 1.01 * EPS * np.abs(b) + e + 2.0 ** -149), name
+    # none of these bounds would let a wrong gradient through
+    assert not pairs or np.abs(want[1]).max() > 1e3 * (e_g.max() + 2.0 ** -149)
+    return len(pairs)
+
+
+@pytest.mark.parametrize("P,G,T", [(2, 2, 32769), (1, 3, 100000), (1, 2, 2048 * 1024 + 5), (1, 4, 700001)])
+@pytest.mark.parametrize("mean", [False, True])
+def test_long_responses_each_output_by_itself(P, G, T, mean):
+    for seed in (31, 32, 33):
+        check_each(P, G, T, seed, mean=mean, beta=0.5 if mean else 1e-3, nll_coef=0.0 if seed == 31 else 0.1, per_pair=seed == 33)
+
+
+# responses a wavefront each, the last workgroup not full, 161 and 162 workgroups; 160 and 161 responses a workgroup each
+@pytest.mark.parametrize("P,G,T", [(55, 3, 7), (107, 6, 20), (215, 3, 20), (40, 4, 1025), (23, 7, 1025)])
+def test_counts_and_launches_with_pairs_on_both_sides(P, G, T):
+    for per_pair in (False, True):
+        assert check_each(P, G, T, 41, beta=0.1, nll_coef=0.1, per_pair=per_pair) > P // 2
+        check_each(P, G, T, 42, beta=0.5, mean=True, per_pair=per_pair)
