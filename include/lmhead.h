@@ -301,7 +301,7 @@ LMHEAD_API int preference_loss(const lmhead_preference* params, const float* log
 /*
  * Rows of a weight matrix by token id, and the gradient of that matrix: the other end of a model whose head is the matrix W above
  * (tied weights), or an embedding of its own.  R responses of T slots, N = R*T; slot i = r*T + t is valid iff t < len[r].
- *   embed_fwd:  X[i,:] = scale W[tok[i],:], rounded once to the rows' type; 0 on padded slots
+ *   embed_fwd:  X[i,:] = scale W[tok[i],:], the product in fp32, rounded to the rows' type; 0 on padded slots
  *   embed_bwd:  dW[v,:] = scale sum_{valid i, tok[i] = v} gX[i,:]    (fp32; rows of ids that do not occur = 0)
  * With LMHEAD_FLAG_ACCUM_DW embed_bwd adds to the contents of dW instead, e.g. to what lmhead_logprob_bwd left there; rows of ids
  * that do not occur are then not touched.  The rows of one id are summed in the order of their slots, in pieces that are joined in a

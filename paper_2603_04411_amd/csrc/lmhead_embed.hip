@@ -572,8 +572,8 @@ static_assert(sizeof(LongId) == kLongIdBytes, "workspace");
 // A wavefront per chunk of sorted slots and 512 columns.  An id belongs to the chunk in which its first slot lies, which reads on
 // into the next chunk where the id ends there.  An id that ends later still is long: every chunk that it touches leaves a partial
 // sum, and embed_join_kernel adds them up.
-// Bound by memory: 524288 slots x 4096 bf16 (327000 of them valid, 41000 ids) added to a dW move 4.1 GB, measured and needed, in 790 us:
-// 5.2 TB/s, as much as this card gives a mix of reads and scattered read-modify-writes (reads alone, 200 ids: 5.8).  Rows in the order
+// Bound by memory: 524288 slots x 4096 bf16 (327000 of them valid, 41000 ids) added to a dW move 4.1 GB, measured and needed, in 726 to 805 us
+// by the card: 5.2 to 5.7 TB/s, as much as this card gives a mix of reads and scattered read-modify-writes (reads alone, 200 ids: 5.8).  Rows in the order
 // of memory, 4 or 16 rows in flight, dW past the caches and workgroups of 4 or 8 wavefronts are within 2 % of it.
 template <typename T>
 __global__ __launch_bounds__(64) void embed_sum_kernel(SumArgs a) {

@@ -2,7 +2,7 @@
 // loss and statistics; of few tokens both in one workgroup.  A token is 4 bytes in (8 with a reference) and 4 out, its arithmetic two
 // additions: up to a million tokens what it takes is launches and the latency of their first loads, so
 //  - a response's pairs are looked at by one wavefront, which counts by ballots and meets the others at one barrier;
-//  - loads leave before the length that they are masked by has arrived.
+//  - loads leave before the length that they are masked by has arrived, padding's too (4 x 4 x 262144 full 25.1 us, with 2000 tokens 23.9).
 #include "train_common.h"
 
 namespace lmhead {
