@@ -2,7 +2,8 @@
  * dynakv.h - C ABI of the token-adaptive KV-cache compression path for AMD MI355X (gfx950):
  * spectral projection, differentiable truncation gate, ragged store and low-rank
  * reconstruction (Sec. 3 "Dynamic Compressing" of the paper, Eqs. 1-8) and the retain-rate
- * regulariser of the training objective (Sec. 3.3, Eq. 9).
+ * regulariser of the training objective (Sec. 3.3, Eq. 9).  Further below, what reads a KV cache
+ * and makes it smaller: attention, eviction, a cache in 4 bits.
  *
  * Notation (the paper's): a token's pre-RoPE key or value state is the row vector x with
  * d = d_kv entries; U [d x d] is the spectral basis, W [d x d] and b [d] the gate layer,
@@ -168,6 +169,145 @@ LMHEAD_API int dynakv_gate_bwd(const dynakv_desc* desc, const void* x, const voi
  * `ws` met a device-side range fault (see dynakv_store / dynakv_reconstruct), else LMHEAD_OK
  * (every call clears the word when it starts). */
 LMHEAD_API int dynakv_check(void* ws, void* stream);
+
+/*
+ * ---- What reads a KV cache and makes it smaller: attention with a sliding window and a few first tokens that stay visible,
+ * and its backward; eviction of tokens by accumulated attention weight; a cache held in 4 bits and attention over it. ----
+ *
+ * Notation: B sequences; sequence b has lk = len_k[b] keys, in slots 0 .. lk-1 of Tk, and lq = len_q[b] queries, in slots
+ * 0 .. lq-1 of Tq, which are its last tokens: query i stands at key position p = lk - lq + i.  It sees key j if
+ *     0 <= j <= p   and   (window == 0  or  j > p - window  or  j < sinks).
+ * Query head h reads key head h / (Hq / Hkv).  With s = scale <q_i, k_j> over the keys that i sees,
+ *     lse_i = log sum_j exp(s_ij),   P_ij = exp(s_ij - lse_i),   out_i = sum_j P_ij v_j.
+ * A query that sees no key (p < 0, or a slot from lq on) gives out = 0 and lse = -inf, and so does one whose logits are all -inf.
+ *
+ *  - As above, the library allocates nothing and keeps no state between calls, argument errors are found before anything is
+ *    launched, and results are bit-reproducible (the grouping of sums depends on the sizes of the call).  Descriptors and plane
+ *    lists are host memory.  The workspace's error word is read by lmhead_check(): a length outside [0, T], taken as the nearest
+ *    one inside.  A workspace belongs to one call at a time.
+ *  - What lies in slots from a sequence's length on is never used, whatever its bits, nor are keys that no query of the call
+ *    sees.  An infinity or NaN in a key or value that some queries see and others do not reaches only those that do.
+ *  - Logits, softmax and all sums are fp32.  With bf16 storage P, and in the backward dS, are rounded to bf16 before they
+ *    enter a matrix product, as are the outputs.
+ */
+
+/* Where element (sequence b, slot t, head h, c) lies: b * seq + t * slot + h * head + c, in elements.  Each stride is a
+ * multiple of 16 bytes, not negative, and such that tensors which are written do not overlap themselves; slot strides are below 16 MiB. */
+typedef struct attn_layout {
+  int64_t seq, slot, head;
+} attn_layout;
+
+/* Problem descriptor (host memory). */
+typedef struct attn_desc {
+  int32_t B;        /* sequences, at most 65535                                               */
+  int32_t Tq, Tk;   /* slots for queries, and for keys, of one sequence                       */
+  int32_t Hq, Hkv;  /* heads; Hq is a multiple of Hkv, at most 1024                           */
+  int32_t D;        /* width of a head: a multiple of 8, at most 128 (4-bit cache: of 32)     */
+  int32_t window;   /* 0: all keys up to the query's own position                             */
+  int32_t sinks;    /* >= 0                                                                   */
+  int32_t dtype;    /* LMHEAD_F32 or LMHEAD_BF16: q, k, v, out and their gradients            */
+  float scale;      /* of the logits: finite, > 0                                             */
+  uint32_t flags;   /* must be 0                                                              */
+  int32_t reserved; /* must be 0                                                              */
+  attn_layout q, k, v, o;  /* o: out and its gradient; gradients of q, k, v lie as those do.  */
+                           /* Pointers are 16-byte aligned                                    */
+} attn_desc;
+
+/* LMHEAD_OK or the code that the calls below would return for this descriptor.  Host-only. */
+LMHEAD_API int attn_validate_desc(const attn_desc* desc);
+
+/* Scratch bytes of attn_fwd, kv4_store and kv4_attn; 0 if the descriptor is invalid.  Host-only. */
+LMHEAD_API size_t attn_workspace_bytes(const attn_desc* desc);
+
+/*
+ * Attention, and the weight that each key gets.
+ *   q, k, v         (in)
+ *   len_q, len_k    int32[B] or NULL: all slots  (in)
+ *   out             (out) 0 in the slots of queries that see no key
+ *   lse             float[B][Hq][Tq] or NULL     (out)
+ *   weight          float[B][Hkv][Tk] or NULL    (in/out) weight[b][h][j] = decay * weight[b][h][j] + sum of P_ij over the
+ *                   queries i and the heads that read h, for j < len_k[b]; the rest is left as it was.  With decay = 0 the old
+ *                   value is not read.
+ *   decay           finite, >= 0
+ * `out` and `weight` share no memory with an input or each other.
+ */
+LMHEAD_API int attn_fwd(const attn_desc* desc, const void* q, const void* k, const void* v, const int32_t* len_q,
+                        const int32_t* len_k, void* out, float* lse, float* weight, float decay, void* ws, size_t ws_bytes,
+                        void* stream);
+
+/*
+ * Backward, given g_out = dL/dout:
+ *     dP_ij = <g_i, v_j>,   delta_i = <g_i, out_i>,   dS_ij = P_ij (dP_ij - delta_i)
+ *     dq_i = scale sum_j dS_ij k_j,   dk_j = scale sum_i dS_ij q_i,   dv_j = sum_i P_ij g_i
+ * (dk, dv: over the queries of all heads that read the key's head).  P is recomputed from q, k and lse.
+ *   out, lse        as attn_fwd left them for the same q, k, v and lengths  (in)
+ *   dq, dk, dv      (out) every slot is written: 0 where nothing is seen, or seen by nobody.  A slot of the padding is 0 too.
+ *   ws              attn_bwd_workspace_bytes(desc) bytes
+ */
+LMHEAD_API size_t attn_bwd_workspace_bytes(const attn_desc* desc);
+LMHEAD_API int attn_bwd(const attn_desc* desc, const void* q, const void* k, const void* v, const int32_t* len_q,
+                        const int32_t* len_k, const void* out, const float* lse, const void* g_out, void* dq, void* dk,
+                        void* dv, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * A cache in 4 bits.  A row of D values of a token and head is cut into blocks of 32.  A block has the scale 2^e with
+ * the smallest e >= -126 for which max |x| <= 6 * 2^e, but at most 2^125, stored as the byte e + 127, and a code of four bits
+ * for each value: bit 3 the sign, bits 0-2 the index into { 0, 0.5, 1, 1.5, 2, 3, 4, 6 } of x / 2^e, rounded to nearest, of two
+ * as near ones to the even index (so the values are e2m1 numbers, and all are finite in bf16).  A block with an infinity or a NaN has the scale byte 255 and codes 0 and
+ * stands for 32 NaN.
+ *   k_codes, v_codes    uint8[B][Hkv][Tk][D / 2]: value 2c in the lower half of byte c, value 2c + 1 in the upper half
+ *   k_scales, v_scales  uint8[B][Hkv][Tk][D / 32]
+ * Both are dense; codes are 16-byte aligned, scales 4-byte aligned.  Tk and the descriptor's heads are the cache's.
+ *
+ * kv4_store puts the last len_q[b] tokens of each sequence into it: row i of k and v (Tq slots, layouts desc->k and desc->v)
+ * goes to slot len_k[b] - len_q[b] + i; rows of negative slots are left out.  Other slots are left as they are.
+ */
+LMHEAD_API int kv4_store(const attn_desc* desc, const void* k, const void* v, const int32_t* len_q, const int32_t* len_k,
+                         uint8_t* k_codes, uint8_t* k_scales, uint8_t* v_codes, uint8_t* v_scales, void* ws, size_t ws_bytes,
+                         void* stream);
+
+/* attn_fwd over such a cache (desc->k and desc->v are not used). */
+LMHEAD_API int kv4_attn(const attn_desc* desc, const void* q, const uint8_t* k_codes, const uint8_t* k_scales,
+                        const uint8_t* v_codes, const uint8_t* v_scales, const int32_t* len_q, const int32_t* len_k, void* out,
+                        float* lse, float* weight, float decay, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- eviction ---- */
+
+typedef struct evict_desc {
+  int32_t B, T, Hkv;  /* sequences (at most 65535), slots, key heads (at most 1024)            */
+  int32_t keep;       /* tokens that stay, 1 .. T                                              */
+  int32_t sinks;      /* the first ones, which stay whatever their weight                      */
+  int32_t recent;     /* the last ones, which stay too; sinks + recent <= keep                 */
+  int32_t flags, reserved; /* must be 0                                                        */
+} evict_desc;
+
+/* One tensor of the cache, of rows of `bytes` bytes: row (b, t, h) begins at data + b * seq + t * slot + h * head.  Everything
+ * here is in bytes and a multiple of 4 (of 16: rows are then moved 16 bytes at a time). */
+typedef struct cache_plane {
+  void* data;
+  int64_t seq, slot, head;
+  int64_t bytes;      /* 4 .. 4096 */
+} cache_plane;
+
+enum { EVICT_PLANES = 4 };
+
+LMHEAD_API int evict_validate_desc(const evict_desc* desc);
+LMHEAD_API size_t evict_workspace_bytes(const evict_desc* desc);
+
+/*
+ * Tokens leave the cache, per key head.  Of a sequence with n = len[b] > keep tokens each key head keeps the first `sinks`, the last
+ * `recent` and, of those between, the keep - sinks - recent with the largest weight; of equal weights the lowest slot stays.  A
+ * NaN counts as less than any number.  The kept rows close up to slots 0 .. keep-1 in their order, in all planes and in `weight`,
+ * whose slots keep .. n-1 become 0.  A sequence with n <= keep stays as it is.  Rows of slots from keep on are left as they were.
+ *   planes   1 .. EVICT_PLANES of them (host memory); they share no memory with each other  (in/out)
+ *   weight   float[B][Hkv][T]                                                    (in/out)
+ *   len      int32[B] or NULL: T each                                            (in)
+ *   len_out  int32[B]                                                            (out) min(n, keep); not `len` itself
+ *   kept     int32[B][Hkv][keep]: the old slot of each row, ascending; -1 from n on   (out)
+ *   ws       evict_workspace_bytes(desc) bytes
+ */
+LMHEAD_API int cache_evict(const evict_desc* desc, const cache_plane* planes, int32_t count, float* weight, const int32_t* len,
+                           int32_t* len_out, int32_t* kept, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,256 @@
+"""ctypes binding of the operators that read a KV cache and make it smaller (``include/dynakv.h``): attention over a window and its backward,
+the cache in 4 bits, eviction.  Same conventions as ``train.py``: torch CUDA (ROCm) tensors in, the current stream, ``LmheadError`` on a
+negative status; a tensor of the wrong type or shape, or on another device than the current one, raises ``ValueError`` before the call.
+Nothing is computed here.
+
+Queries, keys, values and outputs are 4-D tensors [sequence, slot, head, channel] with any strides that the descriptor names: a cache that
+keeps each head's tokens together is passed as its ``transpose(1, 2)``.
+"""
+from __future__ import annotations
+
+import ctypes as C
+
+import torch
+
+from .binding import LmheadError, _check, load_library
+from .train import _CODES, _DTYPES, _TORCH, _arg, _bad, _device, _refuse, _stream
+
+EVICT_PLANES = 4
+
+
+class AttnLayout(C.Structure):
+    _fields_ = [("seq", C.c_int64), ("slot", C.c_int64), ("head", C.c_int64)]
+
+
+class AttnDesc(C.Structure):
+    _fields_ = [
+        ("B", C.c_int32), ("Tq", C.c_int32), ("Tk", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32),
+        ("window", C.c_int32), ("sinks", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float), ("flags", C.c_uint32),
+        ("reserved", C.c_int32), ("q", AttnLayout), ("k", AttnLayout), ("v", AttnLayout), ("o", AttnLayout),
+    ]
+
+
+class EvictDesc(C.Structure):
+    _fields_ = [
+        ("B", C.c_int32), ("T", C.c_int32), ("Hkv", C.c_int32), ("keep", C.c_int32), ("sinks", C.c_int32), ("recent", C.c_int32),
+        ("flags", C.c_int32), ("reserved", C.c_int32),
+    ]
+
+
+class _Plane(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("seq", C.c_int64), ("slot", C.c_int64), ("head", C.c_int64), ("bytes", C.c_int64)]
+
+
+_ready = None
+
+
+def _lib():
+    global _ready
+    if _ready is None:
+        lib = load_library()
+        vp, i32, f32, sz = C.c_void_p, C.c_int32, C.c_float, C.c_size_t
+        ap, ep, pp = C.POINTER(AttnDesc), C.POINTER(EvictDesc), C.POINTER(_Plane)
+        lib.attn_validate_desc.restype = C.c_int
+        lib.attn_validate_desc.argtypes = [ap]
+        lib.attn_workspace_bytes.restype = sz
+        lib.attn_workspace_bytes.argtypes = [ap]
+        lib.attn_fwd.restype = C.c_int
+        lib.attn_fwd.argtypes = [ap, vp, vp, vp, vp, vp, vp, vp, vp, f32, vp, sz, vp]
+        lib.attn_bwd_workspace_bytes.restype = sz
+        lib.attn_bwd_workspace_bytes.argtypes = [ap]
+        lib.attn_bwd.restype = C.c_int
+        lib.attn_bwd.argtypes = [ap, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        lib.kv4_store.restype = C.c_int
+        lib.kv4_store.argtypes = [ap, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        lib.kv4_attn.restype = C.c_int
+        lib.kv4_attn.argtypes = [ap, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, f32, vp, sz, vp]
+        lib.evict_validate_desc.restype = C.c_int
+        lib.evict_validate_desc.argtypes = [ep]
+        lib.evict_workspace_bytes.restype = sz
+        lib.evict_workspace_bytes.argtypes = [ep]
+        lib.cache_evict.restype = C.c_int
+        lib.cache_evict.argtypes = [ep, pp, i32, vp, vp, vp, vp, vp, sz, vp]
+        _ready = lib
+    return _ready
+
+
+# ---- attention ------------------------------------------------------------------------------------------------------
+
+
+def attn_layout(t):
+    """Strides (sequence, slot, head) of a [B, T, H, D] tensor.  Those of dimensions with one element can be anything in torch: they are
+    taken as if the dimension had more, dense behind the others."""
+    if t.dim() != 4:
+        raise ValueError(f"[sequence, slot, head, channel] expected, got {tuple(t.shape)}")
+    s, n = list(t.stride()[:3]), t.shape
+    span = max([n[3]] + [abs(s[i]) * n[i] for i in range(3) if n[i] > 1])
+    return tuple(s[i] if n[i] > 1 else (n[3] if i == 1 else span) for i in range(3))
+
+
+def make_attn_desc(B, Tq, Tk, Hq, Hkv, D, dtype, window=0, sinks=0, scale=None, q=None, k=None, v=None, o=None) -> AttnDesc:
+    """Layouts are (sequence, slot, head) strides in elements; by default tensors are dense [B, T, H, D].  scale: default D ** -0.5."""
+    def layout(x, T, H):
+        return AttnLayout(*((T * H * D, H * D, D) if x is None else x))
+    return AttnDesc(B=B, Tq=Tq, Tk=Tk, Hq=Hq, Hkv=Hkv, D=D, window=window, sinks=sinks, dtype=_DTYPES.get(dtype, dtype),
+                    scale=(D ** -0.5 if D > 0 else 1.0) if scale is None else scale, flags=0, reserved=0,
+                    q=layout(q, Tq, Hq), k=layout(k, Tk, Hkv), v=layout(v, Tk, Hkv), o=layout(o, Tq, Hq))
+
+
+def attn_validate_desc(desc: AttnDesc) -> int:
+    return int(_lib().attn_validate_desc(C.byref(desc)))
+
+
+def attn_workspace_bytes(desc: AttnDesc) -> int:
+    return int(_lib().attn_workspace_bytes(C.byref(desc)))
+
+
+def attn_bwd_workspace_bytes(desc: AttnDesc) -> int:
+    return int(_lib().attn_bwd_workspace_bytes(C.byref(desc)))
+
+
+def _heads(t, name, desc, T, H, x, device):
+    """Device pointer of a [B, T, H, D] tensor that lies as layout `x` says."""
+    n, s = t.shape, t.stride()
+    if (t.dtype is _TORCH.get(desc.dtype) and t.get_device() == device and len(n) == 4 and n[0] >= desc.B and n[1] >= T and n[2] >= H
+            and n[3] >= desc.D and s[3] == 1 and (s[0] == x.seq or desc.B == 1) and (s[1] == x.slot or T == 1)
+            and (s[2] == x.head or H == 1)):
+        return t.data_ptr()
+    if t.is_cuda and t.dtype is _TORCH.get(desc.dtype) and t.get_device() == device:
+        _bad(name, f"[{desc.B}, {T}, {H}, {desc.D}] with strides ({x.seq}, {x.slot}, {x.head}, 1) expected, got {tuple(n)} with {tuple(s)}")
+    return _refuse(t, name, _TORCH.get(desc.dtype), device, "")
+
+
+def _out_args(desc, out, lse, weight, dev):
+    return (_heads(out, "out", desc, desc.Tq, desc.Hq, desc.o, dev), _arg(lse, "lse", torch.float32, desc.B * desc.Hq * desc.Tq, dev),
+            _arg(weight, "weight", torch.float32, desc.B * desc.Hkv * desc.Tk, dev))
+
+
+def _good(desc, where):
+    """The descriptor's own refusal comes first: the checks of tensors rely on its sizes."""
+    rc = _lib().attn_validate_desc(C.byref(desc))
+    if rc != 0:
+        raise LmheadError(rc, where)
+
+
+def attn_fwd(desc, q, k, v, len_q, len_k, out, lse, weight, decay, ws) -> None:
+    """len_q, len_k: int32[B], or None where every slot is valid; lse, weight: or None."""
+    _good(desc, "attn_fwd")
+    lib, dev, i32 = _lib(), _device(), torch.int32
+    rc = lib.attn_fwd(
+        C.byref(desc), _heads(q, "q", desc, desc.Tq, desc.Hq, desc.q, dev), _heads(k, "k", desc, desc.Tk, desc.Hkv, desc.k, dev),
+        _heads(v, "v", desc, desc.Tk, desc.Hkv, desc.v, dev), _arg(len_q, "len_q", i32, desc.B, dev), _arg(len_k, "len_k", i32, desc.B, dev),
+        *_out_args(desc, out, lse, weight, dev), decay, _arg(ws, "ws", torch.uint8, 0, dev), ws.numel(), _stream(dev))
+    _check(rc, "attn_fwd")
+
+
+def attn_bwd(desc, q, k, v, len_q, len_k, out, lse, g_out, dq, dk, dv, ws) -> None:
+    _good(desc, "attn_bwd")
+    lib, dev, i32 = _lib(), _device(), torch.int32
+    Tq, Tk, Hq, Hkv = desc.Tq, desc.Tk, desc.Hq, desc.Hkv
+    rc = lib.attn_bwd(
+        C.byref(desc), _heads(q, "q", desc, Tq, Hq, desc.q, dev), _heads(k, "k", desc, Tk, Hkv, desc.k, dev),
+        _heads(v, "v", desc, Tk, Hkv, desc.v, dev), _arg(len_q, "len_q", i32, desc.B, dev), _arg(len_k, "len_k", i32, desc.B, dev),
+        _heads(out, "out", desc, Tq, Hq, desc.o, dev), _arg(lse, "lse", torch.float32, desc.B * Hq * Tq, dev),
+        _heads(g_out, "g_out", desc, Tq, Hq, desc.o, dev), _heads(dq, "dq", desc, Tq, Hq, desc.q, dev),
+        _heads(dk, "dk", desc, Tk, Hkv, desc.k, dev), _heads(dv, "dv", desc, Tk, Hkv, desc.v, dev), _arg(ws, "ws", torch.uint8, 0, dev),
+        ws.numel(), _stream(dev))
+    _check(rc, "attn_bwd")
+
+
+# ---- the cache in 4 bits --------------------------------------------------------------------------------------------
+
+
+def _cache(desc, k_codes, k_scales, v_codes, v_scales, dev):
+    rows, u8 = desc.B * desc.Hkv * desc.Tk, torch.uint8
+    return (_arg(k_codes, "k_codes", u8, rows * (desc.D // 2), dev), _arg(k_scales, "k_scales", u8, rows * (desc.D // 32), dev),
+            _arg(v_codes, "v_codes", u8, rows * (desc.D // 2), dev), _arg(v_scales, "v_scales", u8, rows * (desc.D // 32), dev))
+
+
+def kv4_store(desc, k, v, len_q, len_k, k_codes, k_scales, v_codes, v_scales, ws) -> None:
+    """k, v: the new tokens' rows, [B, Tq, Hkv, D]."""
+    _good(desc, "kv4_store")
+    lib, dev, i32 = _lib(), _device(), torch.int32
+    rc = lib.kv4_store(
+        C.byref(desc), _heads(k, "k", desc, desc.Tq, desc.Hkv, desc.k, dev), _heads(v, "v", desc, desc.Tq, desc.Hkv, desc.v, dev),
+        _arg(len_q, "len_q", i32, desc.B, dev), _arg(len_k, "len_k", i32, desc.B, dev), *_cache(desc, k_codes, k_scales, v_codes, v_scales, dev),
+        _arg(ws, "ws", torch.uint8, 0, dev), ws.numel(), _stream(dev))
+    _check(rc, "kv4_store")
+
+
+def kv4_attn(desc, q, k_codes, k_scales, v_codes, v_scales, len_q, len_k, out, lse, weight, decay, ws) -> None:
+    _good(desc, "kv4_attn")
+    lib, dev, i32 = _lib(), _device(), torch.int32
+    rc = lib.kv4_attn(
+        C.byref(desc), _heads(q, "q", desc, desc.Tq, desc.Hq, desc.q, dev), *_cache(desc, k_codes, k_scales, v_codes, v_scales, dev),
+        _arg(len_q, "len_q", i32, desc.B, dev), _arg(len_k, "len_k", i32, desc.B, dev), *_out_args(desc, out, lse, weight, dev), decay,
+        _arg(ws, "ws", torch.uint8, 0, dev), ws.numel(), _stream(dev))
+    _check(rc, "kv4_attn")
+
+
+# ---- eviction -------------------------------------------------------------------------------------------------------
+
+
+def make_evict_desc(B, T, Hkv, keep, sinks=0, recent=0) -> EvictDesc:
+    return EvictDesc(B=B, T=T, Hkv=Hkv, keep=keep, sinks=sinks, recent=recent, flags=0, reserved=0)
+
+
+def evict_validate_desc(desc: EvictDesc) -> int:
+    return int(_lib().evict_validate_desc(C.byref(desc)))
+
+
+def evict_workspace_bytes(desc: EvictDesc) -> int:
+    return int(_lib().evict_workspace_bytes(C.byref(desc)))
+
+
+class CachePlanes:
+    """The tensors of a cache, [sequence, slot, head, channel] each with any strides, as cache_evict takes them.  It holds on to them."""
+
+    def __init__(self, tensors):
+        self.tensors = [t.detach() for t in tensors]
+        self.array = (_Plane * max(len(self.tensors), 1))()
+        self.device = None
+        spans = []
+        for i, t in enumerate(self.tensors):
+            name = f"plane {i}"
+            if not t.is_cuda:
+                _bad(name, "device tensor expected")
+            if t.dim() != 4 or t.stride(3) != 1 and t.shape[3] != 1:
+                _bad(name, "[sequence, slot, head, channel] with dense channels expected")
+            if self.device is None:
+                self.device = t.get_device()
+            elif t.get_device() != self.device:
+                _bad(name, f"on cuda:{t.get_device()}, others on cuda:{self.device}")
+            seq, slot, head = (x * t.element_size() for x in attn_layout(t))
+            self.array[i] = _Plane(t.data_ptr() or None, seq, slot, head, t.shape[3] * t.element_size())
+            if t.numel():
+                last = sum((n - 1) * s for n, s in zip(t.shape, t.stride())) + 1
+                spans.append((t.data_ptr(), t.data_ptr() + last * t.element_size(), i))
+        self.storages = [t.untyped_storage() for t in self.tensors]
+        self.addresses = [s.data_ptr() for s in self.storages]
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+def make_cache_planes(tensors) -> CachePlanes:
+    return CachePlanes(tensors)
+
+
+def cache_evict(desc, planes: CachePlanes, weight, lens, lens_out, kept, ws) -> None:
+    """lens: int32[B], or None where every slot is valid."""
+    rc = _lib().evict_validate_desc(C.byref(desc))
+    if rc != 0:
+        raise LmheadError(rc, "cache_evict")
+    lib, dev, i32 = _lib(), _device(), torch.int32
+    if planes.device is not None and planes.device != dev:
+        _bad("planes", f"on cuda:{planes.device}, the current device is cuda:{dev}")
+    for i, t in enumerate(planes.tensors):
+        if t.shape[0] < desc.B or t.shape[1] < desc.T or t.shape[2] < desc.Hkv:
+            _bad(f"plane {i}", f"[{desc.B}, {desc.T}, {desc.Hkv}, .] expected, got {tuple(t.shape)}")
+        if planes.storages[i].data_ptr() != planes.addresses[i]:
+            _bad(f"plane {i}", "its storage was resized after the list was made")
+    rc = lib.cache_evict(
+        C.byref(desc), planes.array, len(planes), _arg(weight, "weight", torch.float32, desc.B * desc.Hkv * desc.T, dev),
+        _arg(lens, "lens", i32, desc.B, dev), _arg(lens_out, "lens_out", i32, desc.B, dev),
+        _arg(kept, "kept", i32, desc.B * desc.Hkv * desc.keep, dev), _arg(ws, "ws", torch.uint8, 0, dev), ws.numel(), _stream(dev))
+    _check(rc, "cache_evict")

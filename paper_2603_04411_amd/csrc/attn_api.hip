@@ -1,0 +1,248 @@
+// extern "C" entry points of the attention operators.  As in lmhead_api.hip every argument error is returned before anything is
+// enqueued.
+#include <math.h>
+
+#include <algorithm>
+
+#include "attn_common.h"
+
+namespace lmhead {
+
+AttnPlan attn_plan(const attn_desc* d, bool cache4) {
+  AttnPlan p{};
+  p.DP = d->D <= 64 ? 64 : 128;
+  const int64_t G = d->Hq / d->Hkv, R = d->Tq * G;
+  p.rows = R <= 32 ? 32 : 128;
+  p.nblk = (int)((R + p.rows - 1) / p.rows);
+  const int64_t wgs = (int64_t)d->B * d->Hkv * p.nblk;
+  const int64_t most = p.rows == 32 ? 2048 : 512;     // workgroups that are worth having
+  const int64_t span = d->window ? std::min<int64_t>(d->Tk, (int64_t)d->window + d->sinks + p.rows / G + 1) : d->Tk;
+  const int64_t tiles = (span + 63) / 64;
+  p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>({most / wgs, tiles, (int64_t)256}));
+  (void)cache4;
+  p.part = 256;
+  p.total = p.part;
+  if (p.nsplit > 1) p.total += round_up((size_t)wgs * p.nsplit * p.rows * (p.DP + 2) * sizeof(float), 256);
+  return p;
+}
+
+}  // namespace lmhead
+
+using namespace lmhead;
+
+namespace {
+
+bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+constexpr int64_t kMostStride = 1ll << 40;
+
+// A layout that a tensor of n sequences, t slots and h heads can have; `apart`: no two of its elements at one place.
+int check_layout(const attn_layout& x, int64_t n, int64_t t, int64_t h, int64_t D, int esz, bool apart) {
+  for (int64_t v : {x.seq, x.slot, x.head})
+    if (v < 0 || v > kMostStride) return LMHEAD_E_SHAPE;
+  if (x.slot < D || x.slot * esz >= (1 << 24)) return LMHEAD_E_SHAPE;
+  for (int64_t v : {x.seq, x.slot, x.head})
+    if (v * esz % 16 != 0) return LMHEAD_E_ALIGN;
+  if (apart) {
+    struct Dim {
+      int64_t stride, size;
+    } d[3] = {{x.seq, n}, {x.slot, t}, {x.head, h}};
+    std::sort(d, d + 3, [](const Dim& a, const Dim& b) { return a.stride < b.stride; });
+    int64_t extent = D;      // of what the dimensions so far span
+    for (const Dim& k : d) {
+      if (k.size == 1) continue;
+      if (k.stride < extent) return LMHEAD_E_SHAPE;
+      extent += k.stride * (k.size - 1);
+    }
+  }
+  return LMHEAD_OK;
+}
+
+int validate(const attn_desc* d) {
+  if (!d) return LMHEAD_E_NULL;
+  if (d->B <= 0 || d->B > 65535 || d->Tq <= 0 || d->Tk <= 0 || d->Hq <= 0 || d->Hkv <= 0 || d->Hq > 1024) return LMHEAD_E_SHAPE;
+  if (d->Hq % d->Hkv != 0 || d->D <= 0 || d->D > 128 || d->D % 8 != 0) return LMHEAD_E_SHAPE;
+  if (d->Tq > kNoWindow / 1024 || d->Tk > kNoWindow - 4096) return LMHEAD_E_SHAPE;
+  if (d->window < 0 || d->sinks < 0 || !isfinite(d->scale) || d->scale <= 0.f) return LMHEAD_E_SHAPE;
+  if (d->dtype != LMHEAD_F32 && d->dtype != LMHEAD_BF16) return LMHEAD_E_DTYPE;
+  if (d->flags != 0) return LMHEAD_E_DTYPE;
+  if (d->reserved != 0) return LMHEAD_E_SHAPE;
+  const int esz = d->dtype == LMHEAD_BF16 ? 2 : 4;
+  // work items are counted in 32 bits
+  const int64_t rows = (int64_t)d->Tq * (d->Hq / d->Hkv), blocks = std::max((rows + 31) / 32, ((int64_t)d->Tk + 127) / 128);
+  if ((int64_t)d->B * d->Hkv > ((int64_t)INT32_MAX - 8) / blocks) return LMHEAD_E_SHAPE;
+  int rc = check_layout(d->q, d->B, d->Tq, d->Hq, d->D, esz, false);
+  if (rc == LMHEAD_OK) rc = check_layout(d->k, d->B, d->Tk, d->Hkv, d->D, esz, false);
+  if (rc == LMHEAD_OK) rc = check_layout(d->v, d->B, d->Tk, d->Hkv, d->D, esz, false);
+  if (rc == LMHEAD_OK) rc = check_layout(d->o, d->B, d->Tq, d->Hq, d->D, esz, true);
+  return rc;
+}
+
+AttnTensor tensor(const void* p, const attn_layout& x, int esz) {
+  return AttnTensor{static_cast<char*>(const_cast<void*>(p)), x.seq * esz, x.slot * esz, x.head * esz};
+}
+
+AttnArgs arguments(const attn_desc* d, const AttnPlan& p, const int32_t* len_q, const int32_t* len_k, void* ws) {
+  AttnArgs a{};
+  a.B = d->B, a.Tq = d->Tq, a.Tk = d->Tk, a.Hq = d->Hq, a.Hkv = d->Hkv, a.G = d->Hq / d->Hkv, a.D = d->D;
+  a.window = d->window && d->window < kNoWindow ? d->window : kNoWindow;
+  a.sinks = std::min(d->sinks, d->Tk);
+  a.scale = d->scale;
+  a.scale2 = d->scale * kLog2e;
+  a.len_q = len_q, a.len_k = len_k;
+  a.hdr = static_cast<AttnHeader*>(ws);
+  a.nblk = p.nblk, a.nsplit = p.nsplit;
+  a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + p.part);
+  return a;
+}
+
+size_t lse_bytes(const attn_desc* d) { return round_up((size_t)d->B * d->Hq * d->Tq * sizeof(float), 256); }
+
+int run_fwd(const attn_desc* d, const AttnPlan& p, AttnArgs& a, void* ws, float* lse, float* weight, float decay, hipStream_t s) {
+  // the weights need lse: where the caller does not want it, it stays in the workspace
+  a.lse = lse || !weight ? lse : reinterpret_cast<float*>(static_cast<char*>(ws) + p.total);
+  a.weight = weight;
+  a.decay = decay;
+  LM_TRY(launch_attn_fwd(d, p, a, s));
+  if (weight) LM_TRY(launch_attn_weight(d, p, a, s));
+  return LMHEAD_OK;
+}
+
+int check_weight(const float* weight, float decay) {
+  return weight && !(decay >= 0.f && isfinite(decay)) ? LMHEAD_E_SHAPE : LMHEAD_OK;
+}
+
+int validate_evict(const evict_desc* d) {
+  if (!d) return LMHEAD_E_NULL;
+  if (d->B <= 0 || d->B > 65535 || d->T <= 0 || d->T > kNoWindow - 4096 || d->Hkv <= 0 || d->Hkv > 1024) return LMHEAD_E_SHAPE;
+  if (d->keep <= 0 || d->keep > d->T || d->sinks < 0 || d->recent < 0 || d->sinks > d->keep || d->recent > d->keep - d->sinks) return LMHEAD_E_SHAPE;
+  if (d->flags != 0) return LMHEAD_E_DTYPE;
+  return d->reserved == 0 ? LMHEAD_OK : LMHEAD_E_SHAPE;
+}
+
+}  // namespace
+
+extern "C" {
+
+int attn_validate_desc(const attn_desc* desc) { return validate(desc); }
+
+size_t attn_workspace_bytes(const attn_desc* desc) {
+  if (validate(desc) != LMHEAD_OK) return 0;
+  return attn_plan(desc, false).total + lse_bytes(desc);
+}
+
+int attn_fwd(const attn_desc* desc, const void* q, const void* k, const void* v, const int32_t* len_q, const int32_t* len_k, void* out,
+             float* lse, float* weight, float decay, void* ws, size_t ws_bytes, void* stream) {
+  int rc = validate(desc);
+  if (rc != LMHEAD_OK) return rc;
+  if (!q || !k || !v || !out || !ws) return LMHEAD_E_NULL;
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16) || !aligned(ws, 256)) return LMHEAD_E_ALIGN;
+  rc = check_weight(weight, decay);
+  if (rc != LMHEAD_OK) return rc;
+  const AttnPlan p = attn_plan(desc, false);
+  if (ws_bytes < p.total + lse_bytes(desc)) return LMHEAD_E_WORKSPACE;
+  const int esz = desc->dtype == LMHEAD_BF16 ? 2 : 4;
+  AttnArgs a = arguments(desc, p, len_q, len_k, ws);
+  a.q = tensor(q, desc->q, esz), a.k = tensor(k, desc->k, esz), a.v = tensor(v, desc->v, esz), a.o = tensor(out, desc->o, esz);
+  return run_fwd(desc, p, a, ws, lse, weight, decay, static_cast<hipStream_t>(stream));
+}
+
+size_t attn_bwd_workspace_bytes(const attn_desc* desc) {
+  if (validate(desc) != LMHEAD_OK) return 0;
+  return sizeof(AttnHeader) + lse_bytes(desc);
+}
+
+int attn_bwd(const attn_desc* desc, const void* q, const void* k, const void* v, const int32_t* len_q, const int32_t* len_k,
+             const void* out, const float* lse, const void* g_out, void* dq, void* dk, void* dv, void* ws, size_t ws_bytes,
+             void* stream) {
+  int rc = validate(desc);
+  if (rc != LMHEAD_OK) return rc;
+  const int esz = desc->dtype == LMHEAD_BF16 ? 2 : 4;
+  // gradients are written: theirs must not lie upon each other
+  rc = check_layout(desc->q, desc->B, desc->Tq, desc->Hq, desc->D, esz, true);
+  if (rc == LMHEAD_OK) rc = check_layout(desc->k, desc->B, desc->Tk, desc->Hkv, desc->D, esz, true);
+  if (rc == LMHEAD_OK) rc = check_layout(desc->v, desc->B, desc->Tk, desc->Hkv, desc->D, esz, true);
+  if (rc != LMHEAD_OK) return rc;
+  if (!q || !k || !v || !out || !lse || !g_out || !dq || !dk || !dv || !ws) return LMHEAD_E_NULL;
+  for (const void* x : {q, k, v, out, g_out, static_cast<const void*>(dq), static_cast<const void*>(dk), static_cast<const void*>(dv)})
+    if (!aligned(x, 16)) return LMHEAD_E_ALIGN;
+  if (!aligned(ws, 256)) return LMHEAD_E_ALIGN;
+  if (ws_bytes < attn_bwd_workspace_bytes(desc)) return LMHEAD_E_WORKSPACE;
+  const AttnPlan p = attn_plan(desc, false);
+  AttnArgs a = arguments(desc, p, len_q, len_k, ws);
+  a.q = tensor(q, desc->q, esz), a.k = tensor(k, desc->k, esz), a.v = tensor(v, desc->v, esz), a.o = tensor(out, desc->o, esz);
+  a.g = tensor(g_out, desc->o, esz);
+  a.dq = tensor(dq, desc->q, esz), a.dk = tensor(dk, desc->k, esz), a.dv = tensor(dv, desc->v, esz);
+  a.lse = const_cast<float*>(lse);
+  a.delta = reinterpret_cast<float*>(static_cast<char*>(ws) + sizeof(AttnHeader));
+  LM_TRY(launch_attn_bwd(desc, p, a, static_cast<hipStream_t>(stream)));
+  return LMHEAD_OK;
+}
+
+int kv4_store(const attn_desc* desc, const void* k, const void* v, const int32_t* len_q, const int32_t* len_k, uint8_t* k_codes,
+              uint8_t* k_scales, uint8_t* v_codes, uint8_t* v_scales, void* ws, size_t ws_bytes, void* stream) {
+  const int rc = validate(desc);
+  if (rc != LMHEAD_OK) return rc;
+  if (desc->D % 32 != 0) return LMHEAD_E_SHAPE;
+  if (!k || !v || !k_codes || !k_scales || !v_codes || !v_scales || !ws) return LMHEAD_E_NULL;
+  if (!aligned(k, 16) || !aligned(v, 16) || !aligned(k_codes, 16) || !aligned(v_codes, 16) || !aligned(k_scales, 4) ||
+      !aligned(v_scales, 4) || !aligned(ws, 256))
+    return LMHEAD_E_ALIGN;
+  if (ws_bytes < sizeof(AttnHeader)) return LMHEAD_E_WORKSPACE;
+  const int esz = desc->dtype == LMHEAD_BF16 ? 2 : 4;
+  AttnArgs a = arguments(desc, attn_plan(desc, true), len_q, len_k, ws);
+  a.k = tensor(k, desc->k, esz), a.v = tensor(v, desc->v, esz);
+  uint8_t* const cache[4] = {k_codes, k_scales, v_codes, v_scales};
+  LM_TRY(launch_kv4_store(desc, a, cache, static_cast<hipStream_t>(stream)));
+  return LMHEAD_OK;
+}
+
+int kv4_attn(const attn_desc* desc, const void* q, const uint8_t* k_codes, const uint8_t* k_scales, const uint8_t* v_codes,
+             const uint8_t* v_scales, const int32_t* len_q, const int32_t* len_k, void* out, float* lse, float* weight, float decay,
+             void* ws, size_t ws_bytes, void* stream) {
+  int rc = validate(desc);
+  if (rc != LMHEAD_OK) return rc;
+  if (desc->D % 32 != 0) return LMHEAD_E_SHAPE;
+  if (!q || !k_codes || !k_scales || !v_codes || !v_scales || !out || !ws) return LMHEAD_E_NULL;
+  if (!aligned(q, 16) || !aligned(k_codes, 16) || !aligned(v_codes, 16) || !aligned(k_scales, 4) || !aligned(v_scales, 4) ||
+      !aligned(out, 16) || !aligned(ws, 256))
+    return LMHEAD_E_ALIGN;
+  rc = check_weight(weight, decay);
+  if (rc != LMHEAD_OK) return rc;
+  const AttnPlan p = attn_plan(desc, true);
+  if (ws_bytes < p.total + lse_bytes(desc)) return LMHEAD_E_WORKSPACE;
+  const int esz = desc->dtype == LMHEAD_BF16 ? 2 : 4;
+  AttnArgs a = arguments(desc, p, len_q, len_k, ws);
+  a.q = tensor(q, desc->q, esz), a.o = tensor(out, desc->o, esz);
+  a.k_codes = k_codes, a.k_scales = k_scales, a.v_codes = v_codes, a.v_scales = v_scales;
+  return run_fwd(desc, p, a, ws, lse, weight, decay, static_cast<hipStream_t>(stream));
+}
+
+int evict_validate_desc(const evict_desc* desc) { return validate_evict(desc); }
+
+size_t evict_workspace_bytes(const evict_desc* desc) { return validate_evict(desc) == LMHEAD_OK ? sizeof(AttnHeader) : 0; }
+
+int cache_evict(const evict_desc* desc, const cache_plane* planes, int32_t count, float* weight, const int32_t* len, int32_t* len_out,
+                int32_t* kept, void* ws, size_t ws_bytes, void* stream) {
+  const int rc = validate_evict(desc);
+  if (rc != LMHEAD_OK) return rc;
+  if (!planes || !weight || !len_out || !kept || !ws) return LMHEAD_E_NULL;
+  if (count < 1 || count > EVICT_PLANES || len == len_out) return LMHEAD_E_SHAPE;
+  for (int i = 0; i < count; ++i) {
+    const cache_plane& p = planes[i];
+    if (!p.data) return LMHEAD_E_NULL;
+    if (p.bytes < 4 || p.bytes > 4096) return LMHEAD_E_SHAPE;
+    for (int64_t v : {p.seq, p.slot, p.head, p.bytes})
+      if (v % 4 != 0) return LMHEAD_E_ALIGN;
+    if (!aligned(p.data, 4)) return LMHEAD_E_ALIGN;
+    const attn_layout x{p.seq, p.slot, p.head};
+    if (check_layout(attn_layout{x.seq * 4, x.slot * 4, x.head * 4}, desc->B, desc->T, desc->Hkv, p.bytes * 4, 1, true) == LMHEAD_E_SHAPE)
+      return LMHEAD_E_SHAPE;
+  }
+  if (!aligned(ws, 256)) return LMHEAD_E_ALIGN;
+  if (ws_bytes < sizeof(AttnHeader)) return LMHEAD_E_WORKSPACE;
+  LM_TRY(launch_evict(*desc, planes, count, weight, len, len_out, kept, static_cast<char*>(ws), static_cast<hipStream_t>(stream)));
+  return LMHEAD_OK;
+}
+
+}  // extern "C"

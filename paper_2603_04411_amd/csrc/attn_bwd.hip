@@ -1,0 +1,272 @@
+// Backward of attention over a window and a few first tokens: dq by blocks of queries, then dk and dv by blocks of keys, each recomputing
+// P from the logits and lse.  Seven products instead of the five that one pass over the pairs would take, and no atomics.
+#include "attn_common.h"
+
+namespace lmhead {
+
+namespace {
+
+// Rows as in the forward: a lane holds one query's column of S^T, dP^T and dQ^T, so lse and delta are one value each.
+template <typename E, int DP, int BK>
+__global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
+  using El = AttnElem<E>;
+  using Frag = typename El::Frag;
+  using Tile = AttnTile<E, DP, BK>;
+  constexpr int KS = Tile::KS, KB = BK / 32, DB = DP / 32, ROWS = 128;
+  extern __shared__ char lds[];
+  const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t works = (uint32_t)(a.B * a.Hkv) * (uint32_t)a.nblk, id = attn_work(works);
+  if (id == 0) report_lengths(a);
+  if (id >= works) return;
+  const int blk = uniform(a.nblk - 1 - id % a.nblk);
+  const uint32_t bh = uniform(id / a.nblk);
+  const int hk = uniform(bh % a.Hkv), b = uniform(bh / a.Hkv);
+  const int lq = clamp_len(a.len_q, b, a.Tq), lk = clamp_len(a.len_k, b, a.Tk);
+  const uint32_t r = blk * ROWS + w * 32 + (l & 31);
+  const int qi = r / (uint32_t)a.G, head = hk * a.G + r % (uint32_t)a.G;
+  const bool in = qi < a.Tq;
+  const int p = qi < lq ? lk - lq + qi : -1;
+  const float lse = p >= 0 ? a.lse[((int64_t)b * a.Hq + head) * a.Tq + qi] : -INFINITY;
+  const float end = lse == -INFINITY ? INFINITY : lse * kLog2e;
+  Frag q[KS], g[KS];
+  float delta = 0.f;
+  {
+    const char* qs = a.q.p + b * a.q.seq + (int64_t)qi * a.q.slot + head * a.q.head;
+    const int64_t at = b * a.o.seq + (int64_t)qi * a.o.slot + head * a.o.head;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const int d = 16 * ks + 8 * (l >> 5);
+      const bool has = p >= 0 && d < a.D;
+      q[ks] = has ? El::load(qs + d * El::size) : El::zero();
+      g[ks] = has ? El::load(a.g.p + at + d * El::size) : El::zero();
+      const Frag o = has ? El::load(a.o.p + at + d * El::size) : El::zero();
+#pragma unroll
+      for (int j = 0; j < 8; ++j) delta = fmaf(El::value(g[ks], j), El::value(o, j), delta);
+    }
+    delta += other_half(delta);
+    if (in && l < 32) a.delta[((int64_t)b * a.Hq + head) * a.Tq + qi] = delta;
+  }
+  const uint32_t r0 = blk * ROWS;
+  auto first = [&](uint32_t row) { const int i = uniform(row / (uint32_t)a.G); return i < lq ? max(0, lk - lq + i) : -1; };
+  auto last = [&](uint32_t row) { const int i = uniform(row / (uint32_t)a.G); return lk - lq + (i < lq ? i : lq - 1); };
+  const int bmin = first(r0), bmax = bmin < 0 ? -1 : last(r0 + ROWS - 1);
+  const int wmin = first(r0 + w * 32), wmax = wmin < 0 ? -1 : last(r0 + w * 32 + 31);
+  const int wlow = __any(p < 0) ? -1 : wmin;      // with a row that sees nothing no tile is seen whole
+  KeyTiles kt = key_tiles<BK>(bmin < 0 ? 0 : bmin, bmax, a.window, a.sinks);
+  if (bmax < 0) kt.n = 0;
+
+  const char* kbase = a.k.p + b * a.k.seq + hk * a.k.head;
+  const char* vbase = a.v.p + b * a.v.seq + hk * a.v.head;
+  auto load = [&](int t, char* to) {
+    const int s = tile_start<BK>(kt, t), n = tile_end(kt, t) - s;
+    Tile::template load<4>(to, kbase + s * a.k.slot, (uint32_t)a.k.slot, n, a.D * El::size, w, l);
+    Tile::template load<4>(to + Tile::BYTES, vbase + s * a.v.slot, (uint32_t)a.v.slot, n, a.D * El::size, w, l);
+  };
+  f32x16_t dq[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) dq[db][i] = 0.f;
+
+  if (kt.n) load(0, lds);
+  for (int t = 0; t < kt.n; ++t) {
+    char* const cur = lds + (t & 1) * 2 * Tile::BYTES;
+    __builtin_amdgcn_s_waitcnt(kWaitVm0);
+    __syncthreads();
+    if (t + 1 < kt.n) load(t + 1, lds + ((t + 1) & 1) * 2 * Tile::BYTES);
+    const int s0 = tile_start<BK>(kt, t), n = min(BK, tile_end(kt, t) - s0);
+    if (none_seen(s0, n, wmin, wmax, a.window, a.sinks)) continue;
+    const bool part = n < BK || !all_seen(s0, n, wlow, wmax, a.window, a.sinks);
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      f32x16_t s, dp;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        El::mma(s, Tile::row_frag(cur, kb, ks, l), q[ks]);
+        El::mma(dp, Tile::row_frag(cur + Tile::BYTES, kb, ks, l), g[ks]);
+      }
+      float ds[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) ds[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.scale2, -end)) * (dp[i] - delta);
+      if (part) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int j = kb * 32 + acc_row(i, l);
+          ds[i] = ((j < n) & seen(s0 + j, p, a.window, a.sinks)) ? ds[i] : 0.f;
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const Frag f = El::of(ds + 8 * h);
+#pragma unroll
+        for (int db = 0; db < DB; ++db) El::mma(dq[db], Tile::col_frag(cur, db, kb * 2 + h, l), f);
+      }
+    }
+  }
+  if (!in) return;
+  char* const out = a.dq.p + b * a.dq.seq + (int64_t)qi * a.dq.slot + head * a.dq.head;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const int d = db * 32 + acc_row(i, l);
+      if (d < a.D)
+        El::store4(out + d * El::size, dq[db][i] * a.scale, dq[db][i + 1] * a.scale, dq[db][i + 2] * a.scale, dq[db][i + 3] * a.scale);
+    }
+}
+
+// A wavefront holds 32 keys and their values; the workgroup's four walk the queries that see them, head by head, in tiles of BQ.  S and dP
+// have the queries along the accumulators' rows, so P and dS are operands of dV^T = g^T P and dK^T = Q^T dS as they lie.
+template <typename E, int DP, int BQ>
+__global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a, int nkey) {
+  using El = AttnElem<E>;
+  using Frag = typename El::Frag;
+  using Tile = AttnTile<E, DP, BQ>;
+  constexpr int KS = Tile::KS, QB = BQ / 32, DB = DP / 32, STAGE = 2 * Tile::BYTES + 2 * BQ * 4;
+  extern __shared__ char lds[];
+  const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t works = (uint32_t)(a.B * a.Hkv) * (uint32_t)nkey, id = attn_work(works);
+  if (id >= works) return;
+  const uint32_t bh = uniform(id / nkey);
+  const int blk = uniform(id % nkey), hk = uniform(bh % a.Hkv), b = uniform(bh / a.Hkv);
+  const int lq = clamp_len(a.len_q, b, a.Tq), lk = clamp_len(a.len_k, b, a.Tk);
+  const int s0 = blk * 128, key0 = s0 + w * 32, key = key0 + (l & 31);
+  Frag k[KS], v[KS];
+  {
+    const char* ks_ = a.k.p + b * a.k.seq + (int64_t)key * a.k.slot + hk * a.k.head;
+    const char* vs_ = a.v.p + b * a.v.seq + (int64_t)key * a.v.slot + hk * a.v.head;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const int d = 16 * ks + 8 * (l >> 5);
+      k[ks] = key < lk && d < a.D ? El::load(ks_ + d * El::size) : El::zero();
+      v[ks] = key < lk && d < a.D ? El::load(vs_ + d * El::size) : El::zero();
+    }
+  }
+  const int off = lk - lq, end_key = min(lk, s0 + 128) - 1;
+  const int i0 = max(0, s0 - off);
+  const int i1 = s0 < a.sinks ? lq : (int)min((int64_t)lq, (int64_t)end_key + a.window - off);
+  const int tiles = s0 < lk && i1 > i0 ? (i1 - i0 + BQ - 1) / BQ : 0, n = tiles * a.G;
+
+  float end_next = 0.f, delta_next = 0.f;      // of the tile that is loaded next: one query a thread
+  auto load = [&](int t, char* to) {
+    const int g = uniform((uint32_t)t / (uint32_t)tiles), i = i0 + uniform((uint32_t)t % (uint32_t)tiles) * BQ, head = hk * a.G + g;
+    Tile::template load<4>(to, a.q.p + b * a.q.seq + head * a.q.head + i * a.q.slot, (uint32_t)a.q.slot, i1 - i, a.D * El::size, w, l);
+    Tile::template load<4>(to + Tile::BYTES, a.g.p + b * a.g.seq + head * a.g.head + i * a.g.slot, (uint32_t)a.g.slot, i1 - i,
+                           a.D * El::size, w, l);
+    if (threadIdx.x < BQ) {
+      const int qi = i + threadIdx.x;
+      const int64_t at = ((int64_t)b * a.Hq + head) * a.Tq + qi;
+      const float lse = qi < i1 ? a.lse[at] : -INFINITY;
+      end_next = lse == -INFINITY ? INFINITY : lse * kLog2e;
+      delta_next = qi < i1 ? a.delta[at] : 0.f;
+    }
+  };
+  auto put = [&](char* to) {
+    if (threadIdx.x < BQ) {
+      float* const f = reinterpret_cast<float*>(to + 2 * Tile::BYTES);
+      f[threadIdx.x] = end_next;
+      f[BQ + threadIdx.x] = delta_next;
+    }
+  };
+  f32x16_t dk[DB], dv[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) dk[db][i] = dv[db][i] = 0.f;
+
+  if (n) {
+    load(0, lds);
+    put(lds);
+  }
+  for (int t = 0; t < n; ++t) {
+    char* const cur = lds + (t & 1) * STAGE;
+    char* const next = lds + ((t + 1) & 1) * STAGE;
+    __builtin_amdgcn_s_waitcnt(kWaitVm0);
+    __syncthreads();
+    if (t + 1 < n) load(t + 1, next);
+    const int i = i0 + uniform((uint32_t)t % (uint32_t)tiles) * BQ, rows = min(BQ, i1 - i);
+    const float* const end = reinterpret_cast<const float*>(cur + 2 * Tile::BYTES);
+    const float* const delta = end + BQ;
+    const int pmin = off + i, pmax = off + i + rows - 1;
+    if (!none_seen(key0, 32, pmin, pmax, a.window, a.sinks)) {
+      const bool part = rows < BQ || !all_seen(key0, 32, pmin, pmax, a.window, a.sinks);
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) {
+        f32x16_t s, dp;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) s[x] = dp[x] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          El::mma(s, Tile::row_frag(cur, qb, ks, l), k[ks]);
+          El::mma(dp, Tile::row_frag(cur + Tile::BYTES, qb, ks, l), v[ks]);
+        }
+        float pr[16], ds[16];
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+          const int row = qb * 32 + acc_row(x, l);
+          pr[x] = __builtin_amdgcn_exp2f(fmaf(s[x], a.scale2, -end[row]));
+          ds[x] = pr[x] * (dp[x] - delta[row]);
+        }
+        if (part) {
+#pragma unroll
+          for (int x = 0; x < 16; ++x) {
+            const int row = qb * 32 + acc_row(x, l);
+            const bool sees = (row < rows) & seen(key, pmin + row, a.window, a.sinks);
+            pr[x] = sees ? pr[x] : 0.f;
+            ds[x] = sees ? ds[x] : 0.f;
+          }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const Frag pf = El::of(pr + 8 * h), sf = El::of(ds + 8 * h);
+#pragma unroll
+          for (int db = 0; db < DB; ++db) {
+            El::mma(dv[db], Tile::col_frag(cur + Tile::BYTES, db, qb * 2 + h, l), pf);
+            El::mma(dk[db], Tile::col_frag(cur, db, qb * 2 + h, l), sf);
+          }
+        }
+      }
+    }
+    if (t + 1 < n) put(next);
+  }
+  if (key >= a.Tk) return;
+  char* const ok = a.dk.p + b * a.dk.seq + (int64_t)key * a.dk.slot + hk * a.dk.head;
+  char* const ov = a.dv.p + b * a.dv.seq + (int64_t)key * a.dv.slot + hk * a.dv.head;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const int d = db * 32 + acc_row(i, l);
+      if (d >= a.D) continue;
+      El::store4(ok + d * El::size, dk[db][i] * a.scale, dk[db][i + 1] * a.scale, dk[db][i + 2] * a.scale, dk[db][i + 3] * a.scale);
+      El::store4(ov + d * El::size, dv[db][i], dv[db][i + 1], dv[db][i + 2], dv[db][i + 3]);
+    }
+}
+
+template <typename E, int DP>
+hipError_t bwd(AttnArgs a, hipStream_t s) {
+  constexpr int BK = AttnElem<E>::size == 2 ? 64 : 32;
+  constexpr auto dq = attn_dq_kernel<E, DP, BK>;
+  constexpr auto dkv = attn_dkv_kernel<E, DP, BK>;
+  const int bytes = 4 * AttnTile<E, DP, BK>::BYTES, more = bytes + 4 * BK * 4, nkey = (a.Tk + 127) / 128;
+  hipError_t e = allow_lds<dq>(bytes);
+  if (e == hipSuccess) e = allow_lds<dkv>(more);
+  if (e != hipSuccess) return e;
+  a.nblk = (int)(((int64_t)a.Tq * a.G + 127) / 128);
+  dq<<<attn_grid(attn_wgs((int64_t)a.B * a.Hkv * a.nblk)), 256, bytes, s>>>(a);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  dkv<<<attn_grid(attn_wgs((int64_t)a.B * a.Hkv * nkey)), 256, more, s>>>(a, nkey);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attn_bwd(const attn_desc* d, const AttnPlan& p, AttnArgs& a, hipStream_t s) {
+  if (d->dtype == LMHEAD_BF16) return p.DP == 64 ? bwd<bf16_tag, 64>(a, s) : bwd<bf16_tag, 128>(a, s);
+  return p.DP == 64 ? bwd<f32_tag, 64>(a, s) : bwd<f32_tag, 128>(a, s);
+}
+
+}  // namespace lmhead

@@ -1,0 +1,267 @@
+// Internal declarations of the attention operators: launchers, workspace layout, and the tiles and fragments that their kernels share.
+#pragma once
+
+#include "../../include/dynakv.h"
+#include "common.h"
+#include "gemm_core.h"
+
+namespace lmhead {
+
+struct AttnHeader {
+  int32_t err;      // sticky error bits, where lmhead_check reads them
+  int32_t nv;       // unused; lmhead_check copies it along
+  int32_t pad[62];
+};
+static_assert(sizeof(AttnHeader) == 256, "header is one 256-byte line");
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// One tensor as a kernel sees it: strides in bytes.
+struct AttnTensor {
+  char* p;
+  int64_t seq, slot, head;
+};
+
+struct AttnArgs {
+  int B, Tq, Tk, Hq, Hkv, G, D;
+  int window, sinks;        // window: kNoWindow for none
+  float scale, scale2;      // scale2 = scale * log2(e)
+  AttnTensor q, k, v, o;
+  const uint8_t *k_codes, *k_scales, *v_codes, *v_scales;   // the cache in 4 bits (k and v are not set then)
+  const int32_t *len_q, *len_k;
+  float* lse;
+  float* weight;
+  float decay;
+  AttnHeader* hdr;
+  int nblk, nsplit;         // blocks of rows, and parts of a block's keys
+  float* part;              // [b][key head][split][row of the block-padded rows]{DP sums, maximum, sum}
+  // backward
+  AttnTensor g, dq, dk, dv;
+  float* delta;             // [b][head][query]
+};
+
+// What a call needs in its workspace, and how its work is cut: the same for every call with this descriptor.
+struct AttnPlan {
+  int DP;            // width of a head in the kernels: 64 or 128
+  int rows;          // rows (query, head of the key head) of a workgroup
+  int nblk, nsplit;
+  size_t part, total;
+};
+AttnPlan attn_plan(const attn_desc* d, bool cache4);
+
+hipError_t launch_attn_fwd(const attn_desc* d, const AttnPlan& p, AttnArgs& a, hipStream_t s);
+hipError_t launch_attn_weight(const attn_desc* d, const AttnPlan& p, AttnArgs& a, hipStream_t s);
+hipError_t launch_attn_bwd(const attn_desc* d, const AttnPlan& p, AttnArgs& a, hipStream_t s);
+hipError_t launch_kv4_store(const attn_desc* d, const AttnArgs& a, uint8_t* const* cache, hipStream_t s);
+hipError_t launch_evict(const evict_desc& d, const cache_plane* planes, int count, float* weight, const int32_t* len, int32_t* len_out,
+                        int32_t* kept, char* ws, hipStream_t s);
+
+// A launch has fewer than 2^32 threads along x: workgroups in rows of kAttnRow.
+constexpr uint32_t kAttnRow = 1 << 21;
+static inline dim3 attn_grid(int64_t wgs) {
+  return dim3((unsigned)(wgs < kAttnRow ? wgs : kAttnRow), (unsigned)((wgs + kAttnRow - 1) / kAttnRow));
+}
+
+// ---- device side --------------------------------------------------------------------------
+
+// Workgroups go to the eight XCDs in turn; each XCD takes a range of consecutive work, so that the blocks of one key head meet in its L2.
+__device__ inline uint32_t attn_work(uint32_t n) {
+  const uint32_t w = blockIdx.y * kAttnRow + blockIdx.x, per = (n + 7) / 8;
+  return w / 8 < per ? (w % 8) * per + w / 8 : n;      // n or more: nothing to do
+}
+__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+static inline int64_t attn_wgs(int64_t n) { return (n + 7) / 8 * 8; }
+
+__device__ inline int clamp_len(const int32_t* len, int b, int T) {
+  if (!len) return T;
+  const int n = uniform(len[b]);
+  return n < 0 ? 0 : n > T ? T : n;
+}
+
+// The workgroup of the first work item reports the lengths that are out of range.
+__device__ inline void report_lengths(const AttnArgs& a) {
+  int bad = 0;
+  for (int b = threadIdx.x; b < a.B; b += blockDim.x) {
+    if (a.len_q) bad |= (uint32_t)a.len_q[b] > (uint32_t)a.Tq;
+    if (a.len_k) bad |= (uint32_t)a.len_k[b] > (uint32_t)a.Tk;
+  }
+  bad = __syncthreads_or(bad);
+  if (threadIdx.x == 0) a.hdr->err = bad ? kErrLen : 0;
+}
+
+__device__ inline uint32_t pack_bf16(float lo, float hi) {
+  typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+  const bf16x2_t r = {(__bf16)lo, (__bf16)hi};
+  return __builtin_bit_cast(uint32_t, r);
+}
+
+// Fragments of the 32x32 MFMA blocks.  Sixteen values of K make a step: lane l holds row (or column) l % 32 and, with h = l / 32,
+// eight of them.  In which order the sixteen are dealt out is immaterial as long as both operands agree:
+//  - contiguous K (a tile's rows, or registers filled from memory): 8 h .. 8 h + 7;
+//  - K along the rows of a tile, and accumulators that become an operand: 4 h .. 4 h + 3, then 8 + 4 h .. 8 + 4 h + 3, which is
+//    where an accumulator block has its rows, so that the exponentials never leave their lane.
+template <typename E>
+struct AttnElem;
+template <>
+struct AttnElem<bf16_tag> {
+  static constexpr int size = 2;
+  using Frag = u32x4_t;
+  __device__ static inline Frag zero() { return u32x4_t{0, 0, 0, 0}; }
+  __device__ static inline void mma(f32x16_t& c, const Frag& a, const Frag& b) {
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+  }
+  __device__ static inline Frag of(const float* x) {
+    return u32x4_t{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
+  }
+  __device__ static inline Frag load(const char* p) { return *reinterpret_cast<const u32x4_t*>(p); }
+  __device__ static inline float value(const Frag& f, int j) {
+    const uint32_t w = f[j >> 1];
+    return __builtin_bit_cast(float, j & 1 ? w & 0xffff0000u : w << 16);
+  }
+  __device__ static inline void store4(char* p, float a, float b, float c, float d) {
+    *reinterpret_cast<u32x2_t*>(p) = u32x2_t{pack_bf16(a, b), pack_bf16(c, d)};
+  }
+};
+template <>
+struct AttnElem<f32_tag> {
+  static constexpr int size = 4;
+  struct Frag {
+    f32x4_t x[2];
+  };
+  __device__ static inline Frag zero() { return Frag{{f32x4_t{0, 0, 0, 0}, f32x4_t{0, 0, 0, 0}}}; }
+  __device__ static inline void mma(f32x16_t& c, const Frag& a, const Frag& b) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x[i].x, b.x[i].x, c, 0, 0, 0);
+      c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x[i].y, b.x[i].y, c, 0, 0, 0);
+      c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x[i].z, b.x[i].z, c, 0, 0, 0);
+      c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x[i].w, b.x[i].w, c, 0, 0, 0);
+    }
+  }
+  __device__ static inline Frag of(const float* x) { return Frag{{f32x4_t{x[0], x[1], x[2], x[3]}, f32x4_t{x[4], x[5], x[6], x[7]}}}; }
+  __device__ static inline Frag load(const char* p) {
+    return Frag{{reinterpret_cast<const f32x4_t*>(p)[0], reinterpret_cast<const f32x4_t*>(p)[1]}};
+  }
+  __device__ static inline float value(const Frag& f, int j) { return f.x[j >> 2][j & 3]; }
+  __device__ static inline void store4(char* p, float a, float b, float c, float d) {
+    *reinterpret_cast<f32x4_t*>(p) = f32x4_t{a, b, c, d};
+  }
+};
+
+typedef __attribute__((address_space(3))) char lds_char;
+
+// ROWS rows of DP values in LDS.  A row is CH chunks of 16 bytes; chunk c of row r sits at position c ^ swz(r) of its row, so that both the
+// reads along rows (eight consecutive rows, one chunk) and those across them (four or eight rows, 32 or 64 bytes) spread over the banks.
+template <typename E, int DP, int ROWS>
+struct AttnTile {
+  using El = AttnElem<E>;
+  using Frag = typename El::Frag;
+  static constexpr int CH = DP * El::size / 16;
+  static constexpr int ROW = CH * 16;
+  static constexpr int BYTES = ROWS * ROW;
+  static constexpr int KS = DP / 16;      // steps along a row
+  static_assert(64 % CH == 0 && BYTES % 1024 == 0, "a load instruction fills whole rows");
+
+  __device__ static inline int swz(int r) { return r & 7; }
+  __device__ static inline int at(int r, int c) { return r * ROW + ((c ^ swz(r)) << 4); }
+
+  // Rows straight from memory by NW wavefronts (wavefront w, lane l): `p` is row 0, `valid` rows exist; the others, and columns from
+  // `width` bytes on, become zeros: the offsets of theirs lie outside the buffer, and such a load touches no memory.
+  template <int NW>
+  __device__ static inline void load(char* lds, const char* p, uint32_t stride, int valid, int width, int w, int l) {
+    constexpr int PER = BYTES / 1024 / NW;
+    static_assert(PER * 1024 * NW == BYTES, "loads divide evenly");
+    const int rows = valid < 0 ? 0 : valid < ROWS ? valid : ROWS;
+    const uint64_t base = reinterpret_cast<uint64_t>(p);
+    const uint64_t first = (uint64_t)(uint32_t)uniform((int)(base >> 32)) << 32 | (uint32_t)uniform((int)base);
+    const __amdgpu_buffer_rsrc_t rsrc =
+        __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<char*>(first), 0, uniform((int)(rows * stride)), 0x00020000);
+    typedef __attribute__((address_space(3))) void* lptr_t;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int r = (w * PER + i) * (64 / CH) + l / CH, c = (l % CH) ^ swz(r);
+      const uint32_t off = c * 16 < width ? (uint32_t)r * stride + c * 16 : 0x80000000u;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lptr_t)(lds + (w * PER + i) * 1024), 16, off, 0, 0, 0);
+    }
+  }
+  // Step `ks` of rows 32 rb + l % 32.
+  __device__ static inline Frag row_frag(const char* lds, int rb, int ks, int l) {
+    const int r = rb * 32 + (l & 31);
+    if constexpr (El::size == 2) {
+      return *reinterpret_cast<const u32x4_t*>(lds + at(r, 2 * ks + (l >> 5)));
+    } else {
+      const int c = 4 * ks + 2 * (l >> 5);
+      return Frag{{*reinterpret_cast<const f32x4_t*>(lds + at(r, c)), *reinterpret_cast<const f32x4_t*>(lds + at(r, c + 1))}};
+    }
+  }
+  // Columns 32 db + l % 32 of rows 16 s .. 16 s + 15 (dealt out as accumulators are).
+  __device__ static inline Frag col_frag(const char* lds, int db, int s, int l) {
+    if constexpr (El::size == 2) {
+      typedef __attribute__((address_space(3))) i16x4_t* tptr_t;
+      u32x4_t f;
+      const int t = l & 15, c = db * 4 + ((l >> 4) & 1) * 2 + ((t & 3) >> 1);
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        const int r = 16 * s + 8 * p + 4 * (l >> 5) + (t >> 2);
+        const u32x2_t v = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tptr_t)(lds + at(r, c) + 8 * (t & 1))));
+        f[2 * p] = v.x;
+        f[2 * p + 1] = v.y;
+      }
+      return f;
+    } else {
+      Frag f;
+      const int d = db * 32 + (l & 31);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int r = 16 * s + 8 * (j >> 2) + 4 * (l >> 5) + (j & 3);
+        f.x[j >> 2][j & 3] = *reinterpret_cast<const float*>(lds + at(r, d >> 2) + 4 * (d & 3));
+      }
+      return f;
+    }
+  }
+};
+
+// Row of accumulator element i of a 32x32 block.
+__device__ inline int acc_row(int i, int l) { return 8 * (i >> 2) + 4 * (l >> 5) + (i & 3); }
+
+// The other half's value of a lane of the same column.
+__device__ inline float other_half(float x) {
+  typedef __attribute__((ext_vector_type(2))) unsigned u2;
+  const u2 r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+  return __builtin_bit_cast(float, (threadIdx.x & 32) ? r[0] : r[1]);
+}
+
+// The keys that a block of queries at positions [pmin, pmax] sees: [0, e0) and [lo, e1), in tiles of BK.
+struct KeyTiles {
+  int e0, lo, e1, n0, n;
+};
+template <int BK>
+__device__ inline KeyTiles key_tiles(int pmin, int pmax, int window, int sinks) {
+  KeyTiles t;
+  t.lo = pmin - window + 1 > 0 ? pmin - window + 1 : 0;
+  t.e0 = sinks < t.lo ? sinks : 0;
+  if (sinks >= t.lo) t.lo = 0;
+  t.e1 = pmax + 1;
+  t.n0 = (t.e0 + BK - 1) / BK;
+  t.n = t.n0 + (t.e1 > t.lo ? (int)(((int64_t)t.e1 - t.lo + BK - 1) / BK) : 0);
+  return t;
+}
+template <int BK>
+__device__ inline int tile_start(const KeyTiles& t, int i) { return i < t.n0 ? i * BK : t.lo + (i - t.n0) * BK; }
+__device__ inline int tile_end(const KeyTiles& t, int i) { return i < t.n0 ? t.e0 : t.e1; }
+
+// (query, key) pairs: whether all, or none, of keys [s, s + n) are seen from positions [pmin, pmax].
+__device__ inline bool all_seen(int s, int n, int pmin, int pmax, int window, int sinks) {
+  return (s + n - 1 <= pmin) & ((s > pmax - window) | (s + n <= sinks));
+}
+__device__ inline bool none_seen(int s, int n, int pmin, int pmax, int window, int sinks) {
+  return (s > pmax) | ((s + n - 1 <= pmin - window) & (s >= sinks));
+}
+// `span` is the window, or more than any position where there is none.
+__device__ inline bool seen(int key, int p, int span, int sinks) {
+  return (key <= p) & ((key > p - span) | (key < sinks));
+}
+constexpr int kNoWindow = 1 << 30;    // Tk is at most this
+
+}  // namespace lmhead

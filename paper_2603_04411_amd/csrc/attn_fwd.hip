@@ -1,0 +1,352 @@
+// Attention over a window and a few first tokens, and the join of its parts.
+#include "attn_common.h"
+
+namespace lmhead {
+
+namespace {
+
+// 32 values of a row from their codes, as four chunks (fp32: eight) of a tile's row.
+template <typename Tile>
+__device__ inline void put_block(char* lds, int r, int block, const u32x4_t& codes, uint32_t scale) {
+  const float size = __builtin_bit_cast(float, scale << 23);
+  const bool bad = scale == 255;
+  typedef __attribute__((ext_vector_type(2))) float f32x2_t;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {        // eight values: a word of codes
+    const f32x2_t x0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[i], size, 0), x1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[i], size, 1);
+    const f32x2_t x2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[i], size, 2), x3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[i], size, 3);
+    float x[8] = {x0[0], x0[1], x1[0], x1[1], x2[0], x2[1], x3[0], x3[1]};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = bad ? NAN : x[j];
+    if constexpr (Tile::El::size == 2) {
+      *reinterpret_cast<u32x4_t*>(lds + Tile::at(r, block * 4 + i)) = Tile::El::of(x);
+    } else {
+      const auto f = Tile::El::of(x);
+      *reinterpret_cast<f32x4_t*>(lds + Tile::at(r, block * 8 + 2 * i)) = f.x[0];
+      *reinterpret_cast<f32x4_t*>(lds + Tile::at(r, block * 8 + 2 * i + 1)) = f.x[1];
+    }
+  }
+}
+
+// BK rows of the cache in 4 bits, the ones from `valid` on and the columns from D on as zeros.
+template <typename Tile, int NW, int BK>
+__device__ inline void load_cache(char* lds, const uint8_t* codes, const uint8_t* scales, int valid, int D, int w, int l) {
+  constexpr int BLOCKS = Tile::KS / 2;      // blocks of 32 in a row
+  for (int i = w * 64 + l; i < BK * BLOCKS; i += NW * 64) {
+    const int r = i / BLOCKS, block = i % BLOCKS;
+    const bool in = r < valid && block * 32 < D;
+    const u32x4_t c = in ? *reinterpret_cast<const u32x4_t*>(codes + (int64_t)r * (D / 2) + block * 16) : u32x4_t{0, 0, 0, 0};
+    put_block<Tile>(lds, r, block, c, in ? scales[(int64_t)r * (D / 32) + block] : 127u);
+  }
+}
+
+// One workgroup takes NW * 32 rows (query i, head g of the key head: row r = i G + g) of one key head and walks the keys that
+// they see in tiles of BK: S^T = K Q^T with the keys along the accumulators' rows, so that a lane holds one query's logits and the
+// softmax needs one exchange between lane halves; the exponentials are the second operand of O^T = V^T P^T as they lie.
+template <typename E, int DP, int NW, int BK, bool kCache>
+__global__ __launch_bounds__(NW * 64, 2) void attn_fwd_kernel(AttnArgs a) {
+  using El = AttnElem<E>;
+  using Frag = typename El::Frag;
+  using Tile = AttnTile<E, DP, BK>;
+  constexpr int KS = Tile::KS, KB = BK / 32, DB = DP / 32, ROWS = NW * 32;
+  extern __shared__ char lds[];
+  const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t works = (uint32_t)(a.B * a.Hkv) * (uint32_t)(a.nblk * a.nsplit), id = attn_work(works);
+  if (id == 0) report_lengths(a);
+  if (id >= works) return;
+  const int split = uniform(id % a.nsplit), blk = uniform(a.nblk - 1 - id / a.nsplit % a.nblk);
+  const uint32_t bh = uniform(id / a.nsplit / a.nblk);
+  const int hk = uniform(bh % a.Hkv), b = uniform(bh / a.Hkv);
+  const int lq = clamp_len(a.len_q, b, a.Tq), lk = clamp_len(a.len_k, b, a.Tk);
+
+  // this lane's row
+  const uint32_t r = blk * ROWS + w * 32 + (l & 31);
+  const int qi = r / (uint32_t)a.G, head = hk * a.G + r % (uint32_t)a.G;
+  const bool in = qi < a.Tq;
+  const int p = qi < lq ? lk - lq + qi : -1;     // below 0: sees nothing
+  Frag q[KS];
+  {
+    const char* src = a.q.p + b * a.q.seq + (int64_t)qi * a.q.slot + head * a.q.head;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const int d = 16 * ks + 8 * (l >> 5);
+      q[ks] = p >= 0 && d < a.D ? El::load(src + d * El::size) : El::zero();
+    }
+  }
+  // positions of the block's rows, and of this wavefront's
+  const uint32_t r0 = blk * ROWS;
+  auto first = [&](uint32_t row) { const int i = uniform(row / (uint32_t)a.G); return i < lq ? max(0, lk - lq + i) : -1; };
+  auto last = [&](uint32_t row) { const int i = uniform(row / (uint32_t)a.G); return lk - lq + (i < lq ? i : lq - 1); };
+  const int bmin = first(r0), bmax = bmin < 0 ? -1 : last(r0 + ROWS - 1);
+  const int wmin = first(r0 + w * 32), wmax = wmin < 0 ? -1 : last(r0 + w * 32 + 31);
+  const int wlow = __any(p < 0) ? -1 : wmin;      // with a row that sees nothing no tile is seen whole
+  KeyTiles kt = key_tiles<BK>(bmin < 0 ? 0 : bmin, bmax, a.window, a.sinks);
+  if (bmax < 0) kt.n = 0;
+  const int per = uniform((kt.n + a.nsplit - 1) / (uint32_t)a.nsplit), t0 = split * per, t1 = min(kt.n, t0 + per);
+
+  const char* kbase = a.k.p + b * a.k.seq + hk * a.k.head;
+  const char* vbase = a.v.p + b * a.v.seq + hk * a.v.head;
+  auto load = [&](int t, char* to) {
+    const int s = tile_start<BK>(kt, t), n = tile_end(kt, t) - s;
+    if constexpr (kCache) {
+      const int64_t row = (int64_t)bh * a.Tk + s;
+      load_cache<Tile, NW, BK>(to, a.k_codes + row * (a.D / 2), a.k_scales + row * (a.D / 32), n, a.D, w, l);
+      load_cache<Tile, NW, BK>(to + Tile::BYTES, a.v_codes + row * (a.D / 2), a.v_scales + row * (a.D / 32), n, a.D, w, l);
+    } else {
+      Tile::template load<NW>(to, kbase + s * a.k.slot, (uint32_t)a.k.slot, n, a.D * El::size, w, l);
+      Tile::template load<NW>(to + Tile::BYTES, vbase + s * a.v.slot, (uint32_t)a.v.slot, n, a.D * El::size, w, l);
+    }
+  };
+
+  f32x16_t o[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
+  float m = -INFINITY, sum = 0.f;
+
+  if (t0 < t1) load(t0, lds);
+  for (int t = t0; t < t1; ++t) {
+    char* const cur = lds + ((t - t0) & 1) * 2 * Tile::BYTES;
+    __builtin_amdgcn_s_waitcnt(kWaitVm0);
+    __syncthreads();
+    if (t + 1 < t1) load(t + 1, lds + ((t + 1 - t0) & 1) * 2 * Tile::BYTES);
+    const int s0 = tile_start<BK>(kt, t), n = min(BK, tile_end(kt, t) - s0);
+    if (none_seen(s0, n, wmin, wmax, a.window, a.sinks)) continue;
+    f32x16_t s[KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) El::mma(s[kb], Tile::row_frag(cur, kb, ks, l), q[ks]);
+    }
+    if (n < BK || !all_seen(s0, n, wlow, wmax, a.window, a.sinks)) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int j = kb * 32 + acc_row(i, l);
+          s[kb][i] = ((j < n) & seen(s0 + j, p, a.window, a.sinks)) ? s[kb][i] : -INFINITY;
+        }
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
+    top = fmaxf(top, other_half(top));
+    const float now = fmaxf(m, top * a.scale2), base = now == -INFINITY ? 0.f : now;
+    const float keep = __builtin_amdgcn_exp2f(m - base);
+    m = now;
+    sum *= keep;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[db][i] *= keep;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      float e[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        e[i] = __builtin_amdgcn_exp2f(fmaf(s[kb][i], a.scale2, -base));
+        sum += e[i];
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const Frag pf = El::of(e + 8 * h);
+#pragma unroll
+        for (int db = 0; db < DB; ++db) El::mma(o[db], Tile::col_frag(cur + Tile::BYTES, db, kb * 2 + h, l), pf);
+      }
+    }
+  }
+  sum += other_half(sum);
+
+  if (a.nsplit > 1) {
+    float* const part = a.part + ((int64_t)(bh * a.nsplit + split) * (a.nblk * ROWS) + r) * (DP + 2);
+    if (!in) return;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) part[db * 32 + acc_row(i, l)] = o[db][i];
+    if (l < 32) {
+      part[DP] = m;
+      part[DP + 1] = sum;
+    }
+    return;
+  }
+  if (!in) return;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  char* const out = a.o.p + b * a.o.seq + (int64_t)qi * a.o.slot + head * a.o.head;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const int d = db * 32 + acc_row(i, l);
+      if (d < a.D) El::store4(out + d * El::size, o[db][i] * inv, o[db][i + 1] * inv, o[db][i + 2] * inv, o[db][i + 3] * inv);
+    }
+  if (a.lse && l < 32) a.lse[((int64_t)b * a.Hq + head) * a.Tq + qi] = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2;
+}
+
+// Joins the parts of a row: a wavefront each.
+template <typename E, int DP>
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int rows) {
+  const int l = threadIdx.x & 63;
+  const int64_t R = (int64_t)a.Tq * a.G, id = ((int64_t)blockIdx.y * kAttnRow + blockIdx.x) * 4 + (threadIdx.x >> 6);
+  if (id >= R * a.B * a.Hkv) return;
+  const int64_t bh = id / R, r = id % R;
+  const float* const part = a.part + (bh * a.nsplit * a.nblk * rows + r) * (DP + 2);
+  const int64_t step = (int64_t)a.nblk * rows * (DP + 2);
+  float m = -INFINITY;
+  for (int s = l; s < a.nsplit; s += 64) m = fmaxf(m, part[s * step + DP]);
+#pragma unroll
+  for (int x = 32; x; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
+  const float base = m == -INFINITY ? 0.f : m;
+  float sum = 0.f, o[DP / 64] = {};
+  for (int s = 0; s < a.nsplit; ++s) {
+    const float f = __builtin_amdgcn_exp2f(part[s * step + DP] - base);
+    sum += f * part[s * step + DP + 1];
+#pragma unroll
+    for (int i = 0; i < DP / 64; ++i) o[i] += f * part[s * step + i * 64 + l];
+  }
+  const int b = (int)(bh / a.Hkv), head = (int)(bh % a.Hkv) * a.G + (int)(r % a.G), qi = (int)(r / a.G);
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  char* const out = a.o.p + b * a.o.seq + (int64_t)qi * a.o.slot + head * a.o.head;
+#pragma unroll
+  for (int i = 0; i < DP / 64; ++i) {
+    const int d = i * 64 + l;
+    if (d >= a.D) continue;
+    if constexpr (AttnElem<E>::size == 2) reinterpret_cast<uint16_t*>(out)[d] = (uint16_t)pack_bf16(o[i] * inv, 0.f);
+    else reinterpret_cast<float*>(out)[d] = o[i] * inv;
+  }
+  if (a.lse && l == 0) a.lse[((int64_t)b * a.Hq + head) * a.Tq + qi] = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2;
+}
+
+// Weight that the keys got: S = Q K^T with the queries along the accumulators' rows, so that a lane adds up one key's column.  A workgroup
+// takes four times 32 keys of a key head and goes through the queries that see them, head by head, in tiles of 32.
+template <typename E, int DP, bool kCache>
+__global__ __launch_bounds__(256) void attn_weight_kernel(AttnArgs a, int nkey) {
+  using El = AttnElem<E>;
+  using Frag = typename El::Frag;
+  using Tile = AttnTile<E, DP, 32>;
+  constexpr int KS = Tile::KS;
+  extern __shared__ char lds[];
+  __shared__ float ends[32];
+  const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t works = (uint32_t)(a.B * a.Hkv) * (uint32_t)nkey, id = attn_work(works);
+  if (id >= works) return;
+  const uint32_t bh = uniform(id / nkey);
+  const int blk = uniform(id % nkey), hk = uniform(bh % a.Hkv), b = uniform(bh / a.Hkv);
+  const int lq = clamp_len(a.len_q, b, a.Tq), lk = clamp_len(a.len_k, b, a.Tk);
+  const int s0 = blk * 128, key = s0 + w * 32 + (l & 31);
+  if (s0 >= lk) return;
+  Frag k[KS];
+  if constexpr (kCache) {
+    // through LDS, a wavefront's rows at a time
+    for (int x = 0; x < 4; ++x) {
+      const int64_t row = (int64_t)bh * a.Tk + s0 + x * 32;
+      __syncthreads();
+      load_cache<Tile, 4, 32>(lds, a.k_codes + row * (a.D / 2), a.k_scales + row * (a.D / 32), lk - s0 - x * 32, a.D, w, l);
+      __syncthreads();
+      if (w == x) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) k[ks] = Tile::row_frag(lds, 0, ks, l);
+      }
+    }
+    __syncthreads();
+  } else {
+    const char* src = a.k.p + b * a.k.seq + (int64_t)key * a.k.slot + hk * a.k.head;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const int d = 16 * ks + 8 * (l >> 5);
+      k[ks] = key < lk && d < a.D ? El::load(src + d * El::size) : El::zero();
+    }
+  }
+  float sum = 0.f;
+  // queries from the first at or behind the first key to the last whose window reaches the last one, or to the end
+  const int off = lk - lq, end_key = min(lk, s0 + 128) - 1;
+  const int i0 = max(0, s0 - off);
+  const int i1 = s0 < a.sinks ? lq : (int)min((int64_t)lq, (int64_t)end_key + a.window - off);
+  for (int g = 0; g < a.G; ++g) {
+    const int head = hk * a.G + g;
+    const char* qbase = a.q.p + b * a.q.seq + head * a.q.head;
+    for (int i = i0; i < i1; i += 32) {
+      __syncthreads();
+      Tile::template load<4>(lds, qbase + i * a.q.slot, (uint32_t)a.q.slot, lq - i, a.D * El::size, w, l);
+      if (threadIdx.x < 32) {
+        const int qi = i + threadIdx.x;
+        const float lse = qi < lq ? a.lse[((int64_t)b * a.Hq + head) * a.Tq + qi] : -INFINITY;
+        ends[threadIdx.x] = lse == -INFINITY ? INFINITY : lse * kLog2e;
+      }
+      __builtin_amdgcn_s_waitcnt(kWaitVm0);
+      __syncthreads();
+      f32x16_t s;
+#pragma unroll
+      for (int x = 0; x < 16; ++x) s[x] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) El::mma(s, Tile::row_frag(lds, 0, ks, l), k[ks]);
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        const int row = acc_row(x, l);
+        const float e = __builtin_amdgcn_exp2f(fmaf(s[x], a.scale2, -ends[row]));
+        sum += ((i + row < lq) & seen(key, off + i + row, a.window, a.sinks)) ? e : 0.f;
+      }
+    }
+  }
+  sum += other_half(sum);
+  if (l < 32 && key < lk) {
+    float* const to = a.weight + (int64_t)bh * a.Tk + key;
+    *to = a.decay == 0.f ? sum : fmaf(a.decay, *to, sum);
+  }
+}
+
+template <typename E, int DP, int NW, int BK, bool kCache>
+hipError_t fwd(const AttnArgs& a, hipStream_t s) {
+  constexpr auto kernel = attn_fwd_kernel<E, DP, NW, BK, kCache>;
+  const int bytes = 4 * AttnTile<E, DP, BK>::BYTES;
+  hipError_t e = allow_lds<kernel>(bytes);
+  if (e != hipSuccess) return e;
+  kernel<<<attn_grid(attn_wgs((int64_t)a.B * a.Hkv * a.nblk * a.nsplit)), NW * 64, bytes, s>>>(a);
+  e = hipGetLastError();
+  if (e != hipSuccess || a.nsplit == 1) return e;
+  attn_join_kernel<E, DP><<<attn_grid(((int64_t)a.B * a.Hkv * a.Tq * a.G + 3) / 4), 256, 0, s>>>(a, NW * 32);
+  return hipGetLastError();
+}
+
+template <typename E, int DP, bool kCache>
+hipError_t fwd_rows(const AttnPlan& p, const AttnArgs& a, hipStream_t s) {
+  constexpr int BK = AttnElem<E>::size == 2 ? 64 : 32;
+  return p.rows == 32 ? fwd<E, DP, 1, 32, kCache>(a, s) : fwd<E, DP, 4, BK, kCache>(a, s);
+}
+
+template <typename E, int DP, bool kCache>
+hipError_t weight(const AttnArgs& a, hipStream_t s) {
+  constexpr auto kernel = attn_weight_kernel<E, DP, kCache>;
+  const int bytes = AttnTile<E, DP, 32>::BYTES, nkey = (a.Tk + 127) / 128;
+  kernel<<<attn_grid(attn_wgs((int64_t)a.B * a.Hkv * nkey)), 256, bytes, s>>>(a, nkey);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attn_fwd(const attn_desc* d, const AttnPlan& p, AttnArgs& a, hipStream_t s) {
+  const bool c = a.k_codes != nullptr;
+  if (d->dtype == LMHEAD_BF16) {
+    if (p.DP == 64) return c ? fwd_rows<bf16_tag, 64, true>(p, a, s) : fwd_rows<bf16_tag, 64, false>(p, a, s);
+    return c ? fwd_rows<bf16_tag, 128, true>(p, a, s) : fwd_rows<bf16_tag, 128, false>(p, a, s);
+  }
+  if (p.DP == 64) return c ? fwd_rows<f32_tag, 64, true>(p, a, s) : fwd_rows<f32_tag, 64, false>(p, a, s);
+  return c ? fwd_rows<f32_tag, 128, true>(p, a, s) : fwd_rows<f32_tag, 128, false>(p, a, s);
+}
+
+hipError_t launch_attn_weight(const attn_desc* d, const AttnPlan& p, AttnArgs& a, hipStream_t s) {
+  const bool c = a.k_codes != nullptr;
+  if (d->dtype == LMHEAD_BF16) {
+    if (p.DP == 64) return c ? weight<bf16_tag, 64, true>(a, s) : weight<bf16_tag, 64, false>(a, s);
+    return c ? weight<bf16_tag, 128, true>(a, s) : weight<bf16_tag, 128, false>(a, s);
+  }
+  if (p.DP == 64) return c ? weight<f32_tag, 64, true>(a, s) : weight<f32_tag, 64, false>(a, s);
+  return c ? weight<f32_tag, 128, true>(a, s) : weight<f32_tag, 128, false>(a, s);
+}
+
+}  // namespace lmhead

@@ -11,6 +11,9 @@ from .binding import LMHEAD_BF16, LMHEAD_F32, _check, _ptr, _stream, load_librar
 DYNAKV_SYMBOLS = [
     "dynakv_workspace_bytes", "dynakv_validate_desc", "dynakv_gate", "dynakv_store",
     "dynakv_reconstruct", "dynakv_retain", "dynakv_check", "dynakv_bwd_workspace_bytes", "dynakv_gate_bwd",
+    # bound in attention.py
+    "attn_validate_desc", "attn_workspace_bytes", "attn_fwd", "attn_bwd_workspace_bytes", "attn_bwd", "kv4_store", "kv4_attn",
+    "evict_validate_desc", "evict_workspace_bytes", "cache_evict",
 ]
 
 FLAG_LITERAL_FLIP = 1 << 0

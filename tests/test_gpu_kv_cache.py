@@ -1,0 +1,243 @@
+"""The cache in 4 bits (kv4_store, kv4_attn) and eviction (cache_evict) against the fp64 oracle: codes, scales and kept slots are equal, attention
+keeps the bounds of ``tests/attention_cases.py``."""
+import numpy as np
+import pytest
+
+from oracle import attention_oracle as A
+from tests.attention_cases import bounds, holds
+
+pytestmark = pytest.mark.gpu
+
+
+def np64(t):
+    return t.double().cpu().numpy()
+
+
+class Cache4:
+    """A cache of Tk slots filled with codes and scales of all kinds, and garbage behind each sequence's end."""
+
+    def __init__(self, B, Tq, Tk, Hq, Hkv, D, dtype="bf16", window=0, sinks=0, len_q=None, len_k=None, seed=0):
+        import torch
+        import paper_2603_04411_amd as L
+        self.L, self.dtype, self.window, self.sinks = L, dtype, window, sinks
+        self.tdt = torch.bfloat16 if dtype == "bf16" else torch.float32
+        rng = np.random.default_rng(seed + 100 * Tk + Tq)
+        self.lq, self.lk = np.array([Tq] * B if len_q is None else len_q), np.array([Tk] * B if len_k is None else len_k)
+        self.host = []
+        for _ in range(2):
+            codes = rng.integers(0, 256, (B, Hkv, Tk, D // 2), dtype=np.uint8)
+            scales = rng.integers(122, 129, (B, Hkv, Tk, D // 32), dtype=np.uint8)
+            for b, n in enumerate(self.lk):
+                scales[b, :, max(n, 0):] = 255
+            self.host += [codes, scales]
+        self.cache = [torch.from_numpy(x.copy()).cuda() for x in self.host]
+        self.rows = [torch.from_numpy(rng.standard_normal((B, Tq, H, D))).to(self.tdt) for H in (Hq, Hkv, Hkv)]
+        self.q, self.k, self.v = (x.cuda() for x in self.rows)
+        for b, n in enumerate(self.lq):
+            for x in (self.q, self.k, self.v):
+                x[b, max(n, 0):] = float("nan")
+        self.desc = L.make_attn_desc(B, Tq, Tk, Hq, Hkv, D, dtype, window=window, sinks=sinks, k=(Tq * Hkv * D, Hkv * D, D), v=(Tq * Hkv * D, Hkv * D, D))
+        assert L.attn_validate_desc(self.desc) == 0
+        self.len_q, self.len_k = (torch.from_numpy(x.astype(np.int32)).cuda() for x in (self.lq, self.lk))
+        self.out, self.lse = torch.full_like(self.q, 7.0), torch.full((B, Hq, Tq), 7.0, device="cuda")
+        self.weight = torch.rand(B, Hkv, Tk, device="cuda", generator=torch.Generator(device="cuda").manual_seed(seed))
+        self.ws = torch.full((L.attn_workspace_bytes(self.desc),), 255, dtype=torch.uint8, device="cuda")
+
+    def store(self):
+        self.L.kv4_store(self.desc, self.k, self.v, self.len_q, self.len_k, *self.cache, self.ws)
+
+    def attend(self, decay=0.5):
+        self.L.kv4_attn(self.desc, self.q, *self.cache, self.len_q, self.len_k, self.out, self.lse, self.weight, decay, self.ws)
+
+
+CACHES = [
+    dict(B=1, Tq=1, Tk=1, Hq=1, Hkv=1, D=32),
+    dict(B=2, Tq=1, Tk=40, Hq=4, Hkv=2, D=64, len_k=[40, 33]),
+    dict(B=2, Tq=1, Tk=40, Hq=4, Hkv=2, D=64, len_k=[40, 33], dtype="f32"),
+    dict(B=3, Tq=4, Tk=100, Hq=8, Hkv=1, D=96, len_q=[4, 0, 2], len_k=[99, 50, 1]),
+    dict(B=1, Tq=8, Tk=3001, Hq=32, Hkv=8, D=128),
+    dict(B=1, Tq=8, Tk=3001, Hq=32, Hkv=8, D=128, dtype="f32"),
+    dict(B=2, Tq=1, Tk=2500, Hq=28, Hkv=4, D=128, window=1000, sinks=4, len_k=[2500, 1003]),
+    dict(B=2, Tq=70, Tk=300, Hq=6, Hkv=3, D=32, window=100, sinks=65, len_q=[70, 30], len_k=[300, 20]),
+    dict(B=1, Tq=200, Tk=200, Hq=2, Hkv=2, D=128),
+    dict(B=1, Tq=130, Tk=260, Hq=2, Hkv=1, D=96, dtype="f32"),
+    dict(B=2, Tq=40, Tk=30, Hq=2, Hkv=2, D=64, len_q=[40, 5], len_k=[30, 30]),
+]
+
+
+def _name(c):
+    return "-".join(f"{k}{v}" for k, v in c.items()).replace(" ", "")
+
+
+@pytest.mark.parametrize("case", CACHES, ids=_name)
+def test_store_and_attention(case):
+    c = Cache4(**case)
+    c.store()
+    assert c.L.lmhead_check(c.ws) == 0
+    host = [x.copy() for x in c.host]
+    for x, at in ((c.rows[1], 0), (c.rows[2], 2)):
+        codes, scales = A.quantise4(x.double().numpy())
+        for b, (lq, lk) in enumerate(zip(c.lq, c.lk)):
+            for i in range(lq):
+                if lk - lq + i >= 0:
+                    host[at][b, :, lk - lq + i], host[at + 1][b, :, lk - lq + i] = codes[b, i], scales[b, i]
+    for got, want in zip(c.cache, host):
+        assert np.array_equal(got.cpu().numpy(), want)
+    before = np64(c.weight)
+    c.attend()
+    assert c.L.lmhead_check(c.ws) == 0
+    k, v = (np.nan_to_num(A.values4(host[i], host[i + 1])).transpose(0, 2, 1, 3) for i in (0, 2))
+    want, bound = bounds(c.rows[0].double().numpy(), k, v, c.lq, c.lk, float(np.float32(case["D"] ** -0.5)), c.window, c.sinks, c.dtype)
+    holds(np64(c.out), want["out"], bound["out"], "out")
+    holds(np64(c.lse), want["lse"], bound["lse"], "lse")
+    for b, n in enumerate(c.lk):
+        total = 0.5 * before[b, :, :n] + want["weight"][b, :, :n]
+        holds(np64(c.weight)[b, :, :n], total, bound["weight"][b, :, :n] + 2.0 ** -22 * total, "weight")
+        assert np.array_equal(np64(c.weight)[b, :, n:], before[b, :, n:])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_every_scale_and_rounding(dtype):
+    """Blocks of all magnitudes, values on and beside the half steps, zeros of both signs, subnormals, infinities and NaN."""
+    import torch
+    c = Cache4(1, 64, 64, 1, 1, 128, dtype)
+    rng = np.random.default_rng(5)
+    x = rng.standard_normal((64, 4, 32)) * 2.0 ** rng.integers(-149, 126, (64, 4, 1))
+    half = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0])
+    beside = np.concatenate([half, half * (1 + 2.0 ** -7), half * (1 - 2.0 ** -7), -half])
+    for r in range(20):
+        x[r, 0] = beside * 2.0 ** (12 * r - 130)      # the block's largest value, 6, sets its scale
+    x[20, 1], x[21, 1], x[22, 1] = 0.0, -0.0, 2.0 ** -149
+    x[23, 1, 5], x[24, 1, 6], x[25, 1, 7] = np.inf, -np.inf, np.nan
+    x[26, 1] = 3.3e38
+    x[27, 1] = 6.0 * 2.0 ** -126
+    x[28, 1] = 7.0 * 2.0 ** -126
+    t = torch.from_numpy(x.reshape(1, 64, 1, 128)).to(c.tdt)
+    c.k, c.v = t.cuda(), t.flip(-1).contiguous().cuda()
+    c.store()
+    for got, y in ((c.cache[:2], t), (c.cache[2:], t.flip(-1))):
+        codes, scales = A.quantise4(y.double().numpy())
+        assert np.array_equal(got[1].cpu().numpy()[0, 0], scales[0, :, 0])
+        assert np.array_equal(got[0].cpu().numpy()[0, 0], codes[0, :, 0])
+    # what a value stands for: one query, one key after the other
+    back = []
+    c.q.zero_()
+    for i in range(64):
+        d = c.L.make_attn_desc(1, 1, 64, 1, 1, 128, dtype, window=1)
+        c.L.kv4_attn(d, c.q, *c.cache, None, torch.tensor([i + 1], dtype=torch.int32, device="cuda"), c.out, None, None, 1.0, c.ws)
+        back.append(np64(c.out)[0, 0, 0])
+    codes, scales = A.quantise4(t.flip(-1).double().numpy())
+    want = A.values4(codes, scales)[0, :, 0]
+    keys = A.values4(*A.quantise4(t.double().numpy()))[0, :, 0]
+    for i in range(64):
+        if np.isnan(keys[i]).any():
+            assert np.isnan(back[i]).all()            # a logit of NaN
+        else:
+            assert np.array_equal(np.isnan(back[i]), np.isnan(want[i]))
+            fine = ~np.isnan(want[i]) & ((np.abs(want[i]) >= 2.0 ** -126) | (want[i] == 0))
+            assert np.array_equal(back[i][fine], want[i][fine]), i
+            assert (np.abs(back[i][~fine & ~np.isnan(want[i])]) < 2.0 ** -125).all()      # subnormals may be flushed
+
+
+# ---- eviction -------------------------------------------------------------------------------------------------------
+
+
+EVICTIONS = [
+    # B, T, Hkv, keep, sinks, recent, lens
+    (1, 1, 1, 1, 0, 0, None),
+    (1, 2, 1, 1, 0, 0, None),
+    (2, 50, 3, 49, 0, 0, [50, 49]),
+    (3, 300, 2, 100, 4, 30, [300, 100, 101]),
+    (4, 300, 2, 100, 4, 96, [300, 0, 1, 250]),
+    (2, 1024, 2, 512, 0, 0, [1024, 777]),
+    (2, 1025, 2, 512, 1, 511, [1025, 777]),
+    (1, 5000, 2, 4999, 4, 512, None),
+    (2, 5000, 2, 300, 0, 100, [5000, 4097]),
+    (1, 40000, 1, 20000, 64, 1000, None),
+    (70, 64, 5, 32, 2, 2, list(range(1, 65)) + [64] * 6),
+]
+
+
+def weights(kind, shape, rng):
+    w = rng.random(shape).astype(np.float32) ** 8 * 30
+    if kind == "ties":
+        w = np.round(w * 4).astype(np.float32) / 4
+    elif kind == "equal":
+        w[...] = 0.5
+    elif kind == "odd":
+        w = rng.standard_normal(shape).astype(np.float32)
+        w[rng.random(shape) < 0.1] = np.nan
+        w[rng.random(shape) < 0.1] = np.inf
+        w[rng.random(shape) < 0.1] = -np.inf
+        w[rng.random(shape) < 0.1] = -0.0
+        w[rng.random(shape) < 0.1] = 0.0
+        w[rng.random(shape) < 0.1] = 1e-42
+    return w
+
+
+def plane(rng, B, T, H, width, dtype, layout):
+    import torch
+    x = torch.from_numpy(rng.integers(-100, 100, (B, T, H, width))).to(dtype).cuda()
+    if layout == "head":
+        return x.transpose(1, 2).contiguous().transpose(1, 2)
+    if layout == "wide":
+        pad = 16 // x.element_size()
+        big = torch.zeros(T, B, H + 1, width + pad, dtype=dtype, device="cuda")
+        view = big[:, :, :H, :width].permute(1, 0, 2, 3)
+        view.copy_(x)
+        return view
+    return x
+
+
+@pytest.mark.parametrize("kind", ["random", "ties", "equal", "odd"])
+@pytest.mark.parametrize("size", EVICTIONS, ids=lambda s: "-".join(str(x) for x in s[:6]))
+def test_eviction(size, kind):
+    import torch
+    import paper_2603_04411_amd as L
+    B, T, H, keep, sinks, recent, lens = size
+    rng = np.random.default_rng(T + keep)
+    w = weights(kind, (B, H, T), rng)
+    sets = {"random": [(128, torch.bfloat16, "dense"), (128, torch.bfloat16, "head")],
+            "ties": [(40, torch.float32, "wide"), (8, torch.bfloat16, "dense"), (4, torch.int8, "head"), (20, torch.uint8, "dense")],
+            "equal": [(1024, torch.float32, "dense")], "odd": [(64, torch.uint8, "head"), (4, torch.uint8, "head")]}[kind]
+    planes = [plane(rng, B, T, H, *s) for s in sets]
+    before = [p.clone() for p in planes]
+    desc = L.make_evict_desc(B, T, H, keep, sinks=sinks, recent=recent)
+    assert L.evict_validate_desc(desc) == 0
+    i32 = dict(dtype=torch.int32, device="cuda")
+    n = [T] * B if lens is None else lens
+    weight = torch.from_numpy(w.copy()).cuda()
+    lens_out, kept = torch.full((B,), -9, **i32), torch.full((B, H, keep), -9, **i32)
+    ws = torch.empty(L.evict_workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+    L.cache_evict(desc, L.make_cache_planes(planes), weight, None if lens is None else torch.tensor(lens, **i32), lens_out, kept, ws)
+    assert L.lmhead_check(ws) == 0
+    assert lens_out.tolist() == [min(x, keep) for x in n]
+    kept, weight = kept.cpu().numpy(), weight.cpu().numpy()
+    for b in range(B):
+        for h in range(H):
+            at = A.evict(w[b, h], n[b], keep, sinks, recent)
+            assert kept[b, h].tolist() == at + [-1] * (keep - len(at))
+            want = w[b, h].copy()
+            if n[b] > keep:
+                want[keep:n[b]] = 0.0
+                want[:keep] = w[b, h, at]
+            assert np.array_equal(weight[b, h].view(np.uint32), want.view(np.uint32))
+            if n[b] > keep:
+                index = torch.tensor(at, device="cuda")
+                for x in before:
+                    x[b, :keep, h] = x[b, index, h].clone()
+    for got, want in zip(planes, before):
+        assert torch.equal(got, want)
+
+
+def test_eviction_takes_lengths_out_of_range_as_the_nearest():
+    import torch
+    import paper_2603_04411_amd as L
+    i32 = dict(dtype=torch.int32, device="cuda")
+    desc = L.make_evict_desc(3, 40, 1, 10)
+    x = torch.arange(3 * 40 * 8, dtype=torch.float32, device="cuda").view(3, 40, 1, 8)
+    weight = torch.rand(3, 1, 40, device="cuda")
+    lens_out, kept, ws = torch.empty(3, **i32), torch.empty(3, 1, 10, **i32), torch.empty(256, dtype=torch.uint8, device="cuda")
+    L.cache_evict(desc, L.make_cache_planes([x]), weight, torch.tensor([41, -1, 5], **i32), lens_out, kept, ws)
+    assert L.lmhead_check(ws) == -6 and lens_out.tolist() == [10, 0, 5]
+    assert (kept[1] == -1).all() and kept[2, 0].tolist() == [0, 1, 2, 3, 4] + [-1] * 5
