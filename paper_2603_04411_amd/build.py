@@ -21,7 +21,7 @@ TRACE_LIB = os.path.join(HERE, "liblmhead_trace.so")
 SOURCES = ["lmhead_api.hip", "lmhead_aux.hip", "lmhead_loss.hip", "lmhead_gemm.hip", "lmhead_stream.hip", "lmhead_probe.hip",
            "lmhead_pref.hip", "lmhead_embed.hip", "lmhead_grad.hip", "train_api.hip",
            "dynakv_api.hip", "dynakv_aux.hip", "dynakv_gemm.hip", "dynakv_gate.hip",
-           "attn_api.hip", "attn_fwd.hip", "attn_bwd.hip", "attn_cache.hip"]
+           "attn_api.hip", "attn_fwd.hip", "attn_few.hip", "attn_bwd.hip", "attn_cache.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",
     # packed fp32 VALU forms are kept off for every device translation unit

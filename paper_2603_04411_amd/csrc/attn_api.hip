@@ -11,18 +11,25 @@ namespace lmhead {
 AttnPlan attn_plan(const attn_desc* d, bool cache4) {
   AttnPlan p{};
   p.DP = d->D <= 64 ? 64 : 128;
-  const int64_t G = d->Hq / d->Hkv, R = d->Tq * G;
-  p.rows = R <= 32 ? 32 : 128;
+  const int64_t G = d->Hq / d->Hkv, R = d->Tq * G, heads = (int64_t)d->B * d->Hkv;
+  const bool few = R <= kFewRows;
+  p.rows = few ? (int)R : 128;
   p.nblk = (int)((R + p.rows - 1) / p.rows);
-  const int64_t wgs = (int64_t)d->B * d->Hkv * p.nblk;
-  const int64_t most = p.rows == 32 ? 2048 : 512;     // workgroups that are worth having
+  const int64_t wgs = heads * p.nblk;
   const int64_t span = d->window ? std::min<int64_t>(d->Tk, (int64_t)d->window + d->sinks + p.rows / G + 1) : d->Tk;
   const int64_t tiles = (span + 63) / 64;
-  p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>({most / wgs, tiles, (int64_t)256}));
+  p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>({(few ? 1024 : 512) / wgs, tiles / (few ? 4 : 1), (int64_t)256}));
+  size_t off = sizeof(AttnHeader);
+  auto take = [&](size_t bytes) {
+    const size_t o = off;
+    off += round_up(bytes, 256);
+    return o;
+  };
+  p.part = take(few || p.nsplit > 1 ? (size_t)wgs * p.nsplit * p.rows * (p.DP + 2) * sizeof(float) : 0);
+  p.logits = take(R <= kLogitRows ? (size_t)heads * d->Tk * R * sizeof(float) : 0);
+  p.lse = take((size_t)d->B * d->Hq * d->Tq * sizeof(float));
+  p.total = off;
   (void)cache4;
-  p.part = 256;
-  p.total = p.part;
-  if (p.nsplit > 1) p.total += round_up((size_t)wgs * p.nsplit * p.rows * (p.DP + 2) * sizeof(float), 256);
   return p;
 }
 
@@ -99,11 +106,19 @@ AttnArgs arguments(const attn_desc* d, const AttnPlan& p, const int32_t* len_q, 
 size_t lse_bytes(const attn_desc* d) { return round_up((size_t)d->B * d->Hq * d->Tq * sizeof(float), 256); }
 
 int run_fwd(const attn_desc* d, const AttnPlan& p, AttnArgs& a, void* ws, float* lse, float* weight, float decay, hipStream_t s) {
-  // the weights need lse: where the caller does not want it, it stays in the workspace
-  a.lse = lse || !weight ? lse : reinterpret_cast<float*>(static_cast<char*>(ws) + p.total);
+  char* const base = static_cast<char*>(ws);
   a.weight = weight;
   a.decay = decay;
-  LM_TRY(launch_attn_fwd(d, p, a, s));
+  const int64_t rows = (int64_t)d->Tq * a.G;
+  if (weight && rows <= kLogitRows) {
+    a.lse = lse;
+    a.logits = reinterpret_cast<float*>(base + p.logits);
+    LM_TRY(launch_attn_few(d, p, a, s));
+    return LMHEAD_OK;
+  }
+  // the weights need lse: where the caller does not want it, it stays in the workspace
+  a.lse = lse || !weight ? lse : reinterpret_cast<float*>(base + p.lse);
+  LM_TRY(rows <= kFewRows ? launch_attn_few(d, p, a, s) : launch_attn_fwd(d, p, a, s));
   if (weight) LM_TRY(launch_attn_weight(d, p, a, s));
   return LMHEAD_OK;
 }
@@ -128,7 +143,7 @@ int attn_validate_desc(const attn_desc* desc) { return validate(desc); }
 
 size_t attn_workspace_bytes(const attn_desc* desc) {
   if (validate(desc) != LMHEAD_OK) return 0;
-  return attn_plan(desc, false).total + lse_bytes(desc);
+  return std::max(attn_plan(desc, false).total, attn_plan(desc, true).total);
 }
 
 int attn_fwd(const attn_desc* desc, const void* q, const void* k, const void* v, const int32_t* len_q, const int32_t* len_k, void* out,
@@ -140,7 +155,7 @@ int attn_fwd(const attn_desc* desc, const void* q, const void* k, const void* v,
   rc = check_weight(weight, decay);
   if (rc != LMHEAD_OK) return rc;
   const AttnPlan p = attn_plan(desc, false);
-  if (ws_bytes < p.total + lse_bytes(desc)) return LMHEAD_E_WORKSPACE;
+  if (ws_bytes < p.total) return LMHEAD_E_WORKSPACE;
   const int esz = desc->dtype == LMHEAD_BF16 ? 2 : 4;
   AttnArgs a = arguments(desc, p, len_q, len_k, ws);
   a.q = tensor(q, desc->q, esz), a.k = tensor(k, desc->k, esz), a.v = tensor(v, desc->v, esz), a.o = tensor(out, desc->o, esz);
@@ -210,7 +225,7 @@ int kv4_attn(const attn_desc* desc, const void* q, const uint8_t* k_codes, const
   rc = check_weight(weight, decay);
   if (rc != LMHEAD_OK) return rc;
   const AttnPlan p = attn_plan(desc, true);
-  if (ws_bytes < p.total + lse_bytes(desc)) return LMHEAD_E_WORKSPACE;
+  if (ws_bytes < p.total) return LMHEAD_E_WORKSPACE;
   const int esz = desc->dtype == LMHEAD_BF16 ? 2 : 4;
   AttnArgs a = arguments(desc, p, len_q, len_k, ws);
   a.q = tensor(q, desc->q, esz), a.o = tensor(out, desc->o, esz);

@@ -43,7 +43,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) delta = fmaf(El::value(g[ks], j), El::value(o, j), delta);
     }
-    delta += other_half(delta);
+    delta = add_halves(delta);
     if (in && l < 32) a.delta[((int64_t)b * a.Hq + head) * a.Tq + qi] = delta;
   }
   const uint32_t r0 = blk * ROWS;

@@ -35,21 +35,26 @@ struct AttnArgs {
   float decay;
   AttnHeader* hdr;
   int nblk, nsplit;         // blocks of rows, and parts of a block's keys
+  float* logits;            // of a few rows: [b][key head][key][row], for the weights
   float* part;              // [b][key head][split][row of the block-padded rows]{DP sums, maximum, sum}
   // backward
   AttnTensor g, dq, dk, dv;
   float* delta;             // [b][head][query]
 };
 
+constexpr int kFewRows = 32;
+constexpr int kLogitRows = 8;      // up to so many rows their logits are kept for the weights; of more K is read again
+
 // What a call needs in its workspace, and how its work is cut: the same for every call with this descriptor.
 struct AttnPlan {
   int DP;            // width of a head in the kernels: 64 or 128
   int rows;          // rows (query, head of the key head) of a workgroup
   int nblk, nsplit;
-  size_t part, total;
+  size_t part, logits, lse, total;     // offsets of the parts' sums, of the logits of a few rows, of lse where the caller has no use for it
 };
 AttnPlan attn_plan(const attn_desc* d, bool cache4);
 
+hipError_t launch_attn_few(const attn_desc* d, const AttnPlan& p, const AttnArgs& a, hipStream_t s);   // at most kFewRows rows
 hipError_t launch_attn_fwd(const attn_desc* d, const AttnPlan& p, AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_weight(const attn_desc* d, const AttnPlan& p, AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_bwd(const attn_desc* d, const AttnPlan& p, AttnArgs& a, hipStream_t s);
@@ -111,6 +116,9 @@ struct AttnElem<bf16_tag> {
   __device__ static inline void mma(f32x16_t& c, const Frag& a, const Frag& b) {
     c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
   }
+  __device__ static inline void mma(f32x4_t& c, const Frag& a, const Frag& b) {
+    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+  }
   __device__ static inline Frag of(const float* x) {
     return u32x4_t{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
   }
@@ -139,6 +147,15 @@ struct AttnElem<f32_tag> {
       c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x[i].w, b.x[i].w, c, 0, 0, 0);
     }
   }
+  __device__ static inline void mma(f32x4_t& c, const Frag& a, const Frag& b) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.x[i].x, b.x[i].x, c, 0, 0, 0);
+      c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.x[i].y, b.x[i].y, c, 0, 0, 0);
+      c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.x[i].z, b.x[i].z, c, 0, 0, 0);
+      c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.x[i].w, b.x[i].w, c, 0, 0, 0);
+    }
+  }
   __device__ static inline Frag of(const float* x) { return Frag{{f32x4_t{x[0], x[1], x[2], x[3]}, f32x4_t{x[4], x[5], x[6], x[7]}}}; }
   __device__ static inline Frag load(const char* p) {
     return Frag{{reinterpret_cast<const f32x4_t*>(p)[0], reinterpret_cast<const f32x4_t*>(p)[1]}};
@@ -151,8 +168,9 @@ struct AttnElem<f32_tag> {
 
 typedef __attribute__((address_space(3))) char lds_char;
 
-// ROWS rows of DP values in LDS.  A row is CH chunks of 16 bytes; chunk c of row r sits at position c ^ swz(r) of its row, so that both the
-// reads along rows (eight consecutive rows, one chunk) and those across them (four or eight rows, 32 or 64 bytes) spread over the banks.
+// ROWS rows of DP values in LDS.  A row is CH chunks of 16 bytes; chunk c of row r sits at position c ^ swz(r) of its row.  The banks are 256
+// bytes wide: the swizzle spreads a chunk of sixteen consecutive rows (reads along rows) and a pair of chunks of eight rows (transposing
+// reads across them) over all of them.
 template <typename E, int DP, int ROWS>
 struct AttnTile {
   using El = AttnElem<E>;
@@ -163,7 +181,9 @@ struct AttnTile {
   static constexpr int KS = DP / 16;      // steps along a row
   static_assert(64 % CH == 0 && BYTES % 1024 == 0, "a load instruction fills whole rows");
 
-  __device__ static inline int swz(int r) { return r & 7; }
+  __device__ static inline int swz(int r) {
+    return CH == 8 ? (((r >> 1) & 3) << 1) | ((r >> 3) & 1) : ((r & 7) << 1) | ((r >> 3) & 1);
+  }
   __device__ static inline int at(int r, int c) { return r * ROW + ((c ^ swz(r)) << 4); }
 
   // Rows straight from memory by NW wavefronts (wavefront w, lane l): `p` is row 0, `valid` rows exist; the others, and columns from
@@ -220,17 +240,55 @@ struct AttnTile {
       return f;
     }
   }
+  // The same for 16x16 blocks (steps of 32): columns 16 db + l % 16 of rows 32 s .. 32 s + 31, of which lane group g = l / 16 holds
+  // 4 g .. 4 g + 3 and 16 + 4 g .. 16 + 4 g + 3, as two accumulator blocks do.
+  __device__ static inline Frag col_frag16(const char* lds, int db, int s, int l) {
+    if constexpr (El::size == 2) {
+      typedef __attribute__((address_space(3))) i16x4_t* tptr_t;
+      u32x4_t f;
+      const int t = l & 15, c = db * 2 + ((t & 3) >> 1);
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        const int r = 32 * s + 16 * p + 4 * (l >> 4) + (t >> 2);
+        const u32x2_t v = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tptr_t)(lds + at(r, c) + 8 * (t & 1))));
+        f[2 * p] = v.x;
+        f[2 * p + 1] = v.y;
+      }
+      return f;
+    } else {
+      Frag f;
+      const int d = db * 16 + (l & 15);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int r = 32 * s + 16 * (j >> 2) + 4 * (l >> 4) + (j & 3);
+        f.x[j >> 2][j & 3] = *reinterpret_cast<const float*>(lds + at(r, d >> 2) + 4 * (d & 3));
+      }
+      return f;
+    }
+  }
 };
 
 // Row of accumulator element i of a 32x32 block.
 __device__ inline int acc_row(int i, int l) { return 8 * (i >> 2) + 4 * (l >> 5) + (i & 3); }
 
-// The other half's value of a lane of the same column.
-__device__ inline float other_half(float x) {
-  typedef __attribute__((ext_vector_type(2))) unsigned u2;
-  const u2 r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
-  return __builtin_bit_cast(float, (threadIdx.x & 32) ? r[0] : r[1]);
+// A value and that of the lane 32 (16) further, each in both of them: what is symmetric in the two needs no more.
+struct Pair {
+  float a, b;
+};
+__device__ inline Pair halves(float x) {
+  const u32x2_t r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+  const uint32_t a = r.x, b = r.y;      // (bit casts of a vector's elements are avoided)
+  return Pair{__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)};
 }
+__device__ inline Pair quarters(float x) {
+  const u32x2_t r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+  const uint32_t a = r.x, b = r.y;      // (bit casts of a vector's elements are avoided)
+  return Pair{__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)};
+}
+__device__ inline float max_halves(float x) { const Pair p = halves(x); return fmaxf(p.a, p.b); }
+__device__ inline float add_halves(float x) { const Pair p = halves(x); return p.a + p.b; }
+__device__ inline float max_quarters(float x) { const Pair p = quarters(x); return max_halves(fmaxf(p.a, p.b)); }
+__device__ inline float add_quarters(float x) { const Pair p = quarters(x); return add_halves(p.a + p.b); }
 
 // The keys that a block of queries at positions [pmin, pmax] sees: [0, e0) and [lo, e1), in tiles of BK.
 struct KeyTiles {

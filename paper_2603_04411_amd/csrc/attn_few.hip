@@ -1,0 +1,426 @@
+// Attention of a few rows (the queries of a step, times the heads of a key head: at most 32) over a long cache, in bf16, fp32 or 4 bits.
+#include "attn_common.h"
+
+namespace lmhead {
+
+namespace {
+
+constexpr int kFewWaves = 4;
+
+// A tile of TK keys of one key head in registers, on its way: K as fragments (lane l holds keys 16 kb + l % 16), V as it lies in memory.
+template <typename E, int DP, int TK>
+struct Plain {
+  using El = AttnElem<E>;
+  using Frag = typename El::Frag;
+  using Tile = AttnTile<E, DP, TK>;
+  static constexpr int KS = DP / 32, KB = TK / 16, VL = Tile::BYTES / 1024;
+  u32x4_t k[KB][KS][El::size / 2], v[VL];
+
+  // First channel of this lane's eight of step ks.
+  __device__ static inline int channel(int ks, int l) { return 32 * ks + 8 * (l >> 4); }
+
+  __device__ inline void load(const AttnArgs& a, uint32_t, int b, int hk, int s, int n, int l) {
+    const int rows = n < TK ? n : TK, width = a.D * El::size;
+    const __amdgpu_buffer_rsrc_t kr = rsrc(a.k.p + b * a.k.seq + hk * a.k.head + s * a.k.slot, rows * (int)a.k.slot);
+    const __amdgpu_buffer_rsrc_t vr = rsrc(a.v.p + b * a.v.seq + hk * a.v.head + s * a.v.slot, rows * (int)a.v.slot);
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int c = 0; c < El::size / 2; ++c) {
+          const int at = channel(ks, l) * El::size + 16 * c;
+          k[kb][ks][c] = fetch(kr, at < width ? (uint32_t)(16 * kb + (l & 15)) * (uint32_t)a.k.slot + at : 0x80000000u);
+        }
+#pragma unroll
+    for (int i = 0; i < VL; ++i) {
+      const int r = (i * 64 + l) / Tile::CH, at = (l % Tile::CH) * 16;
+      v[i] = fetch(vr, at < width ? (uint32_t)r * (uint32_t)a.v.slot + at : 0x80000000u);
+    }
+  }
+  __device__ inline Frag key(int kb, int ks) const {
+    if constexpr (El::size == 2) return k[kb][ks][0];
+    else return Frag{{__builtin_bit_cast(f32x4_t, k[kb][ks][0]), __builtin_bit_cast(f32x4_t, k[kb][ks][1])}};
+  }
+  __device__ inline void put_values(char* lds, int l) const {
+#pragma unroll
+    for (int i = 0; i < VL; ++i) *reinterpret_cast<u32x4_t*>(lds + Tile::at((i * 64 + l) / Tile::CH, l % Tile::CH)) = v[i];
+  }
+  __device__ static inline __amdgpu_buffer_rsrc_t rsrc(const char* p, int bytes) {
+    const uint64_t x = reinterpret_cast<uint64_t>(p);
+    const uint64_t first = (uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x);
+    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<char*>(first), 0, uniform(bytes), 0x00020000);
+  }
+  __device__ static inline u32x4_t fetch(__amdgpu_buffer_rsrc_t r, uint32_t off) { return __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0); }
+};
+
+// Eight values from a word of codes.
+template <typename E>
+__device__ inline typename AttnElem<E>::Frag decode8(uint32_t codes, float size) {
+  if constexpr (AttnElem<E>::size == 2) {
+    return u32x4_t{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, size, 0)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, size, 1)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, size, 2)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, size, 3))};
+  } else {
+    const auto x0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, size, 0), x1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, size, 1);
+    const auto x2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, size, 2), x3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, size, 3);
+    return typename AttnElem<E>::Frag{{f32x4_t{x0[0], x0[1], x1[0], x1[1]}, f32x4_t{x2[0], x2[1], x3[0], x3[1]}}};
+  }
+}
+
+// The same in 4 bits.  A lane's channels of a key are DP / 4 consecutive ones (q is dealt out alike), so that its codes are one load and it
+// needs no exchange; V is written to LDS in the storage type, which holds its values exactly.
+template <typename E, int DP, int TK>
+struct Coded {
+  using El = AttnElem<E>;
+  using Frag = typename El::Frag;
+  using Tile = AttnTile<E, DP, TK>;
+  static constexpr int KS = DP / 32, KB = TK / 16, VL = TK * DP / 2 / 1024;   // (of 16 bytes = a block)
+  typedef __attribute__((ext_vector_type(KS))) uint32_t Codes;
+  Codes k[KB];
+  u32x4_t v[VL];
+  uint32_t ks_[KB], vs[VL];
+
+  __device__ static inline int channel(int ks, int l) { return (DP / 4) * (l >> 4) + 8 * ks; }
+
+  __device__ inline void load(const AttnArgs& a, uint32_t bh, int, int, int s, int n, int l) {
+    const int64_t row = (int64_t)bh * a.Tk + s;
+    const int rows = n < TK ? n : TK, cb = a.D / 2, sb = a.D / 32;
+    const __amdgpu_buffer_rsrc_t kr = P::rsrc((const char*)a.k_codes + row * cb, rows * cb), kq = P::rsrc((const char*)a.k_scales + row * sb, rows * sb);
+    const __amdgpu_buffer_rsrc_t vr = P::rsrc((const char*)a.v_codes + row * cb, rows * cb), vq = P::rsrc((const char*)a.v_scales + row * sb, rows * sb);
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      const int r = 16 * kb + (l & 15), at = channel(0, l) / 2;
+      const uint32_t off = at < cb ? r * cb + at : 0x80000000u, sc = at < cb ? r * sb + at / 16 : 0x80000000u;
+      if constexpr (KS == 4) k[kb] = P::fetch(kr, off);
+      else k[kb] = __builtin_amdgcn_raw_buffer_load_b64(kr, off, 0, 0);
+      ks_[kb] = __builtin_amdgcn_raw_buffer_load_b8(kq, sc, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < VL; ++i) {
+      const int r = (i * 64 + l) / (DP / 32), block = l % (DP / 32);
+      v[i] = P::fetch(vr, block < sb ? r * cb + block * 16 : 0x80000000u);
+      vs[i] = __builtin_amdgcn_raw_buffer_load_b8(vq, block < sb ? r * sb + block : 0x80000000u, 0, 0);
+    }
+  }
+  __device__ inline Frag key(int kb, int ks) const { return decode8<E>(k[kb][ks], __builtin_bit_cast(float, ks_[kb] << 23)); }
+  __device__ inline void put_values(char* lds, int l) const {
+#pragma unroll
+    for (int i = 0; i < VL; ++i) {
+      const int r = (i * 64 + l) / (DP / 32), block = l % (DP / 32);
+      const float size = __builtin_bit_cast(float, vs[i] << 23);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const Frag f = decode8<E>(v[i][c], size);
+        if constexpr (El::size == 2) {
+          *reinterpret_cast<u32x4_t*>(lds + Tile::at(r, block * 4 + c)) = f;
+        } else {
+          *reinterpret_cast<f32x4_t*>(lds + Tile::at(r, block * 8 + 2 * c)) = f.x[0];
+          *reinterpret_cast<f32x4_t*>(lds + Tile::at(r, block * 8 + 2 * c + 1)) = f.x[1];
+        }
+      }
+    }
+  }
+  using P = Plain<E, DP, TK>;
+};
+
+template <typename E, int DP, int NN, int TK>
+constexpr int few_lds() {      // of a wavefront: a tile of values, then its sums with their maxima and totals
+  constexpr int tile = AttnTile<E, DP, TK>::BYTES, sums = NN * 16 * (DP + 4) * 4;
+  return tile > sums ? tile : sums;
+}
+
+// A workgroup takes the rows of one key head and a part of the keys they see; its wavefronts take tiles in turn, each with sums of its own,
+// and join them through LDS.  Nothing is shared in the loop, so there is no barrier in it: a wavefront asks for its next tile in registers
+// before the softmax of this one.
+template <typename E, int DP, int NN, int TK, bool kCache>
+__global__ __launch_bounds__(kFewWaves * 64, AttnElem<E>::size == 2 ? 2 : 1) void attn_few_kernel(AttnArgs a) {
+  using El = AttnElem<E>;
+  using Frag = typename El::Frag;
+  using Load = typename std::conditional<kCache, Coded<E, DP, TK>, Plain<E, DP, TK>>::type;
+  using Tile = AttnTile<E, DP, TK>;
+  constexpr int KS = DP / 32, KB = TK / 16, DB = DP / 16, WLDS = few_lds<E, DP, NN, TK>();
+  extern __shared__ char lds_all[];
+  const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = l >> 4;
+  char* const lds = lds_all + w * WLDS;
+  const uint32_t works = (uint32_t)(a.B * a.Hkv) * (uint32_t)a.nsplit, id = attn_work(works);
+  if (id == 0) report_lengths(a);
+  if (id >= works) return;
+  const int split = uniform(id % a.nsplit);
+  const uint32_t bh = uniform(id / a.nsplit);
+  const int hk = uniform(bh % a.Hkv), b = uniform(bh / a.Hkv);
+  const int lq = clamp_len(a.len_q, b, a.Tq), lk = clamp_len(a.len_k, b, a.Tk);
+  const int R = a.Tq * a.G;
+
+  Frag q[NN][KS];
+  int p[NN];
+#pragma unroll
+  for (int nn = 0; nn < NN; ++nn) {
+    const int r = nn * 16 + (l & 15), qi = r / (uint32_t)a.G, head = hk * a.G + r % (uint32_t)a.G;
+    p[nn] = qi < lq ? lk - lq + qi : -1;
+    const char* const src = a.q.p + b * a.q.seq + (int64_t)qi * a.q.slot + head * a.q.head;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const int d = Load::channel(ks, l);
+      q[nn][ks] = p[nn] >= 0 && d < a.D ? El::load(src + d * El::size) : El::zero();
+    }
+  }
+  const int pmin = lq ? max(0, lk - lq) : -1, pmax = lq ? lk - 1 : -1;
+  KeyTiles kt = key_tiles<TK>(max(pmin, 0), pmax, a.window, a.sinks);
+  if (pmax < 0) kt.n = 0;
+  const int per = uniform((kt.n + a.nsplit - 1) / (uint32_t)a.nsplit), t1 = min(kt.n, (split + 1) * per);
+  // with rows beside the last, or before position 0, no tile is seen whole; those rows are not looked at at the end
+  const bool few_rows = lk < lq;
+
+  f32x4_t o[NN][DB];
+  float m[NN], sum[NN];
+#pragma unroll
+  for (int nn = 0; nn < NN; ++nn) {
+    m[nn] = -INFINITY, sum[nn] = 0.f;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) o[nn][db] = f32x4_t{0, 0, 0, 0};
+  }
+  Load next;
+  int t = split * per + w;
+  auto fetch = [&](int i) {
+    const int s = tile_start<TK>(kt, i);
+    next.load(a, bh, b, hk, s, tile_end(kt, i) - s, l);
+  };
+  if (t < t1) fetch(t);
+  for (; t < t1; t += kFewWaves) {
+    const int s0 = tile_start<TK>(kt, t), n = min(TK, tile_end(kt, t) - s0);
+    next.put_values(lds, l);
+    f32x4_t s[NN][KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int nn = 0; nn < NN; ++nn) s[nn][kb] = f32x4_t{0, 0, 0, 0};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        const Frag kf = next.key(kb, ks);
+#pragma unroll
+        for (int nn = 0; nn < NN; ++nn) El::mma(s[nn][kb], kf, q[nn][ks]);
+      }
+    if (t + kFewWaves < t1) fetch(t + kFewWaves);
+    const bool part = few_rows || n < TK || !all_seen(s0, n, pmin, pmax, a.window, a.sinks);
+#pragma unroll
+    for (int nn = 0; nn < NN; ++nn) {
+      if (part) {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int j = 16 * kb + 4 * g + i;
+            s[nn][kb][i] = ((j < n) & seen(s0 + j, p[nn], a.window, a.sinks)) ? s[nn][kb][i] : -INFINITY;
+          }
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s[nn][kb][i] *= a.scale2;
+          top = fmaxf(top, s[nn][kb][i]);
+        }
+      if (a.logits) {
+        const int r = nn * 16 + (l & 15);
+        if (r < R) {
+          float* const to = a.logits + ((int64_t)bh * a.Tk + s0) * R + r;
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int j = 16 * kb + 4 * g + i;
+              if (j < n) to[(int64_t)j * R] = s[nn][kb][i];
+            }
+        }
+      }
+      top = max_quarters(top);
+      if (__any(top > m[nn])) {
+        const float now = fmaxf(m[nn], top), keep = __builtin_amdgcn_exp2f(m[nn] - (now == -INFINITY ? 0.f : now));
+        m[nn] = now;
+        sum[nn] *= keep;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[nn][db] *= keep;
+      }
+      const float base = m[nn] == -INFINITY ? 0.f : m[nn];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s[nn][kb][i] = __builtin_amdgcn_exp2f(s[nn][kb][i] - base);
+          sum[nn] += s[nn][kb][i];
+        }
+    }
+#pragma unroll
+    for (int kg = 0; kg < KB / 2; ++kg) {
+      Frag pf[NN];
+#pragma unroll
+      for (int nn = 0; nn < NN; ++nn) {
+        const float x[8] = {s[nn][2 * kg][0], s[nn][2 * kg][1], s[nn][2 * kg][2], s[nn][2 * kg][3],
+                            s[nn][2 * kg + 1][0], s[nn][2 * kg + 1][1], s[nn][2 * kg + 1][2], s[nn][2 * kg + 1][3]};
+        pf[nn] = El::of(x);
+      }
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const Frag vf = Tile::col_frag16(lds, db, kg, l);
+#pragma unroll
+        for (int nn = 0; nn < NN; ++nn) El::mma(o[nn][db], vf, pf[nn]);
+      }
+    }
+  }
+
+  // join: sums of a wavefront are rows of DP + 4 floats (a row further apart by four banks)
+  __syncthreads();
+  float* const mine = reinterpret_cast<float*>(lds);
+#pragma unroll
+  for (int nn = 0; nn < NN; ++nn) {
+    const float total = add_quarters(sum[nn]);
+    float* const row = mine + (nn * 16 + (l & 15)) * (DP + 4);
+#pragma unroll
+    for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4_t*>(row + db * 16 + 4 * g) = o[nn][db];
+    if (g == 0) {
+      row[DP] = m[nn];
+      row[DP + 1] = total;
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < R * DP; i += kFewWaves * 64) {
+    const int r = i / DP, d = i % DP;
+    const float* const row = reinterpret_cast<const float*>(lds_all) + r * (DP + 4);
+    constexpr int step = WLDS / 4;
+    float top = -INFINITY;
+#pragma unroll
+    for (int x = 0; x < kFewWaves; ++x) top = fmaxf(top, row[x * step + DP]);
+    const float base = top == -INFINITY ? 0.f : top;
+    float total = 0.f, acc = 0.f;
+#pragma unroll
+    for (int x = 0; x < kFewWaves; ++x) {
+      const float f = __builtin_amdgcn_exp2f(row[x * step + DP] - base);
+      total += f * row[x * step + DP + 1];
+      acc += f * row[x * step + d];
+    }
+    const int qi = r / (uint32_t)a.G, head = hk * a.G + r % (uint32_t)a.G;
+    if (a.nsplit > 1 || a.logits) {
+      float* const part = a.part + ((int64_t)(bh * a.nsplit + split) * R + r) * (DP + 2);
+      part[d] = acc;
+      if (d == 0) {
+        part[DP] = top;
+        part[DP + 1] = total;
+      }
+    }
+    if (a.nsplit > 1) continue;
+    if (d < a.D) {
+      char* const out = a.o.p + b * a.o.seq + (int64_t)qi * a.o.slot + head * a.o.head;
+      const float y = total == 0.f ? 0.f : acc / total;
+      if constexpr (El::size == 2) reinterpret_cast<uint16_t*>(out)[d] = (uint16_t)pack_bf16(y, 0.f);
+      else reinterpret_cast<float*>(out)[d] = y;
+    }
+    if (d == 0 && a.lse)
+      a.lse[((int64_t)b * a.Hq + head) * a.Tq + qi] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * kLn2;
+  }
+}
+
+// What follows the parts: rows are joined (workgroups 0 .. njoin - 1 of a key head), and the weight of the keys is added up from the logits
+// that the parts left (the others, of kWeightKeys keys each).
+constexpr int kWeightKeys = 2048;
+template <typename E, int DP>
+__global__ __launch_bounds__(256) void attn_finish_kernel(AttnArgs a, int njoin, int nkey) {
+  __shared__ float s_top[32], s_total[32];
+  const uint32_t per = njoin + nkey, id = attn_work((uint32_t)(a.B * a.Hkv) * per);
+  if (id >= (uint32_t)(a.B * a.Hkv) * per) return;
+  const uint32_t bh = uniform(id / per);
+  const int part_of = uniform(id % per), hk = uniform(bh % a.Hkv), b = uniform(bh / a.Hkv), R = a.Tq * a.G, ns = a.nsplit;
+  const int lq = clamp_len(a.len_q, b, a.Tq), lk = clamp_len(a.len_k, b, a.Tk);
+  const float* const part = a.part + (int64_t)bh * ns * R * (DP + 2);
+  const int64_t step = (int64_t)R * (DP + 2);
+  // maximum and total of each row: eight threads a row
+  {
+    const int r = threadIdx.x >> 3, c = threadIdx.x & 7;
+    float top = -INFINITY, total = 0.f;
+    if (r < R)
+      for (int s = c; s < ns; s += 8) top = fmaxf(top, part[s * step + (int64_t)r * (DP + 2) + DP]);
+#pragma unroll
+    for (int x = 4; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+    const float base = top == -INFINITY ? 0.f : top;
+    if (r < R)
+      for (int s = c; s < ns; s += 8) {
+        const float* const at = part + s * step + (int64_t)r * (DP + 2) + DP;
+        total += __builtin_amdgcn_exp2f(at[0] - base) * at[1];
+      }
+#pragma unroll
+    for (int x = 4; x; x >>= 1) total += __shfl_xor(total, x);
+    if (c == 0 && r < R) s_top[r] = base, s_total[r] = total;
+  }
+  __syncthreads();
+  if (part_of < njoin) {
+    const int i = part_of * 256 + threadIdx.x, r = i / DP, d = i % DP;
+    if (r >= R) return;
+    const float base = s_top[r], total = s_total[r];
+    float acc = 0.f;
+    for (int s = 0; s < ns; ++s) {
+      const float* const at = part + s * step + (int64_t)r * (DP + 2);
+      acc += __builtin_amdgcn_exp2f(at[DP] - base) * at[d];
+    }
+    const int qi = r / (uint32_t)a.G, head = hk * a.G + r % (uint32_t)a.G;
+    if (d < a.D) {
+      char* const out = a.o.p + b * a.o.seq + (int64_t)qi * a.o.slot + head * a.o.head;
+      const float y = total == 0.f ? 0.f : acc / total;
+      if constexpr (AttnElem<E>::size == 2) reinterpret_cast<uint16_t*>(out)[d] = (uint16_t)pack_bf16(y, 0.f);
+      else reinterpret_cast<float*>(out)[d] = y;
+    }
+    if (d == 0 && a.lse)
+      a.lse[((int64_t)b * a.Hq + head) * a.Tq + qi] = total == 0.f ? -INFINITY : (base + __builtin_amdgcn_logf(total)) * kLn2;
+    return;
+  }
+  // keys outside [0, e0) and [lo, e1) are seen by no row and have no logits
+  const int pmin = lq ? max(0, lk - lq) : 0, pmax = lq ? lk - 1 : -1;
+  const KeyTiles kt = key_tiles<32>(pmin, pmax, a.window, a.sinks);
+  for (int x = 0; x < kWeightKeys / 256; ++x) {
+    const int key = (part_of - njoin) * kWeightKeys + x * 256 + threadIdx.x;
+    if (key >= lk) return;
+    float sum = 0.f;
+    if (pmax >= 0 && (key < kt.e0 || key >= kt.lo)) {
+      const float* const at = a.logits + ((int64_t)bh * a.Tk + key) * R;
+      for (int r = 0; r < R; ++r) {
+        const float e = __builtin_amdgcn_exp2f(at[r] - s_top[r]) / s_total[r];
+        sum += s_total[r] == 0.f ? 0.f : e;
+      }
+    }
+    float* const to = a.weight + (int64_t)bh * a.Tk + key;
+    *to = a.decay == 0.f ? sum : fmaf(a.decay, *to, sum);
+  }
+}
+
+template <typename E, int DP, int NN, int TK, bool kCache>
+hipError_t few(const AttnArgs& a, hipStream_t s) {
+  constexpr auto kernel = attn_few_kernel<E, DP, NN, TK, kCache>;
+  constexpr int bytes = kFewWaves * few_lds<E, DP, NN, TK>();
+  hipError_t e = allow_lds<kernel>(bytes);
+  if (e != hipSuccess) return e;
+  kernel<<<attn_grid(attn_wgs((int64_t)a.B * a.Hkv * a.nsplit)), kFewWaves * 64, bytes, s>>>(a);
+  e = hipGetLastError();
+  if (e != hipSuccess || (a.nsplit == 1 && !a.logits)) return e;
+  const int njoin = a.nsplit > 1 ? (a.Tq * a.G * DP + 255) / 256 : 0, nkey = a.logits ? (a.Tk + kWeightKeys - 1) / kWeightKeys : 0;
+  attn_finish_kernel<E, DP><<<attn_grid(attn_wgs((int64_t)a.B * a.Hkv * (njoin + nkey))), 256, 0, s>>>(a, njoin, nkey);
+  return hipGetLastError();
+}
+
+template <typename E, int DP>
+hipError_t few_rows(const AttnArgs& a, hipStream_t s) {
+  const bool one = a.Tq * a.G <= 16;
+  if (a.k_codes) return one ? few<E, DP, 1, 64, true>(a, s) : few<E, DP, 2, 32, true>(a, s);
+  return one ? few<E, DP, 1, 32, false>(a, s) : few<E, DP, 2, 32, false>(a, s);
+}
+
+}  // namespace
+
+hipError_t launch_attn_few(const attn_desc* d, const AttnPlan& p, const AttnArgs& a, hipStream_t s) {
+  if (d->dtype == LMHEAD_BF16) return p.DP == 64 ? few_rows<bf16_tag, 64>(a, s) : few_rows<bf16_tag, 128>(a, s);
+  return p.DP == 64 ? few_rows<f32_tag, 64>(a, s) : few_rows<f32_tag, 128>(a, s);
+}
+
+}  // namespace lmhead

@@ -135,7 +135,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_fwd_kernel(AttnArgs a) {
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
-    top = fmaxf(top, other_half(top));
+    top = max_halves(top);
     const float now = fmaxf(m, top * a.scale2), base = now == -INFINITY ? 0.f : now;
     const float keep = __builtin_amdgcn_exp2f(m - base);
     m = now;
@@ -160,7 +160,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_fwd_kernel(AttnArgs a) {
       }
     }
   }
-  sum += other_half(sum);
+  sum = add_halves(sum);
 
   if (a.nsplit > 1) {
     float* const part = a.part + ((int64_t)(bh * a.nsplit + split) * (a.nblk * ROWS) + r) * (DP + 2);
@@ -293,7 +293,7 @@ __global__ __launch_bounds__(256) void attn_weight_kernel(AttnArgs a, int nkey) 
       }
     }
   }
-  sum += other_half(sum);
+  sum = add_halves(sum);
   if (l < 32 && key < lk) {
     float* const to = a.weight + (int64_t)bh * a.Tk + key;
     *to = a.decay == 0.f ? sum : fmaf(a.decay, *to, sum);
@@ -316,7 +316,7 @@ hipError_t fwd(const AttnArgs& a, hipStream_t s) {
 template <typename E, int DP, bool kCache>
 hipError_t fwd_rows(const AttnPlan& p, const AttnArgs& a, hipStream_t s) {
   constexpr int BK = AttnElem<E>::size == 2 ? 64 : 32;
-  return p.rows == 32 ? fwd<E, DP, 1, 32, kCache>(a, s) : fwd<E, DP, 4, BK, kCache>(a, s);
+  return fwd<E, DP, 4, BK, kCache>(a, s);
 }
 
 template <typename E, int DP, bool kCache>

@@ -122,9 +122,10 @@ def test_every_scale_and_rounding(dtype):
     # what a value stands for: one query, one key after the other
     back = []
     c.q.zero_()
+    d = c.L.make_attn_desc(1, 1, 64, 1, 1, 128, dtype, window=1)
+    ws = torch.empty(c.L.attn_workspace_bytes(d), dtype=torch.uint8, device="cuda")
     for i in range(64):
-        d = c.L.make_attn_desc(1, 1, 64, 1, 1, 128, dtype, window=1)
-        c.L.kv4_attn(d, c.q, *c.cache, None, torch.tensor([i + 1], dtype=torch.int32, device="cuda"), c.out, None, None, 1.0, c.ws)
+        c.L.kv4_attn(d, c.q, *c.cache, None, torch.tensor([i + 1], dtype=torch.int32, device="cuda"), c.out, None, None, 1.0, ws)
         back.append(np64(c.out)[0, 0, 0])
     codes, scales = A.quantise4(t.flip(-1).double().numpy())
     want = A.values4(codes, scales)[0, :, 0]
