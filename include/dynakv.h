@@ -239,7 +239,8 @@ LMHEAD_API int attn_fwd(const attn_desc* desc, const void* q, const void* k, con
  * Backward, given g_out = dL/dout:
  *     dP_ij = <g_i, v_j>,   delta_i = <g_i, out_i>,   dS_ij = P_ij (dP_ij - delta_i)
  *     dq_i = scale sum_j dS_ij k_j,   dk_j = scale sum_i dS_ij q_i,   dv_j = sum_i P_ij g_i
- * (dk, dv: over the queries of all heads that read the key's head).  P is recomputed from q, k and lse.
+ * (dk, dv: over the queries of all heads that read the key's head).  P is recomputed from q, k and lse.  With bf16 storage
+ * <g_i, out_i> is corrected for the rounding of out, so that sum_j dS_ij = 0 as it is for the exact output.
  *   out, lse        as attn_fwd left them for the same q, k, v and lengths  (in)
  *   dq, dk, dv      (out) every slot is written: 0 where nothing is seen, or seen by nobody.  A slot of the padding is 0 too.
  *   ws              attn_bwd_workspace_bytes(desc) bytes

@@ -57,6 +57,7 @@ AttnPlan attn_plan(const attn_desc* d, bool cache4);
 hipError_t launch_attn_few(const attn_desc* d, const AttnPlan& p, const AttnArgs& a, hipStream_t s);   // at most kFewRows rows
 hipError_t launch_attn_fwd(const attn_desc* d, const AttnPlan& p, AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_weight(const attn_desc* d, const AttnPlan& p, AttnArgs& a, hipStream_t s);
+size_t attn_first_bytes(const attn_desc* d);      // of the parts of dk and dv of the first tokens
 hipError_t launch_attn_bwd(const attn_desc* d, const AttnPlan& p, AttnArgs& a, hipStream_t s);
 hipError_t launch_kv4_store(const attn_desc* d, const AttnArgs& a, uint8_t* const* cache, hipStream_t s);
 hipError_t launch_evict(const evict_desc& d, const cache_plane* planes, int count, float* weight, const int32_t* len, int32_t* len_out,
@@ -182,7 +183,7 @@ struct AttnTile {
   static_assert(64 % CH == 0 && BYTES % 1024 == 0, "a load instruction fills whole rows");
 
   __device__ static inline int swz(int r) {
-    return CH == 8 ? (((r >> 1) & 3) << 1) | ((r >> 3) & 1) : ((r & 7) << 1) | ((r >> 3) & 1);
+    return ((r & 3) << 1) | ((r >> 2) & 1) | (CH == 8 ? 0 : r & 8);
   }
   __device__ static inline int at(int r, int c) { return r * ROW + ((c ^ swz(r)) << 4); }
 
@@ -203,6 +204,17 @@ struct AttnTile {
       const int r = (w * PER + i) * (64 / CH) + l / CH, c = (l % CH) ^ swz(r);
       const uint32_t off = c * 16 < width ? (uint32_t)r * stride + c * 16 : 0x80000000u;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lptr_t)(lds + (w * PER + i) * 1024), 16, off, 0, 0, 0);
+    }
+  }
+  // Step `ks` of row l % 32, as row_frag reads it.
+  __device__ static inline void put_row(char* lds, int ks, int l, const Frag& f) {
+    const int r = l & 31;
+    if constexpr (El::size == 2) {
+      *reinterpret_cast<u32x4_t*>(lds + at(r, 2 * ks + (l >> 5))) = f;
+    } else {
+      const int c = 4 * ks + 2 * (l >> 5);
+      *reinterpret_cast<f32x4_t*>(lds + at(r, c)) = f.x[0];
+      *reinterpret_cast<f32x4_t*>(lds + at(r, c + 1)) = f.x[1];
     }
   }
   // Step `ks` of rows 32 rb + l % 32.

@@ -8,7 +8,10 @@ With u the half step of the storage type (bf16 2^-8, fp32 2^-24) and w = 2^-24:
  lse       Z + (lk + A + 16) w + 4 w |lse|
  weight    (r + (rows + 4) w) weight + 4 w |result|
  backward  P from the given lse: r' = r + error of lse (the bound above);  dP and delta: e = (D + 4) w (sum |g||v| and sum |g||out|);
-           dS: (u + r') |dS| + P e;  dq: scale (sum err(dS) |k| + (lk + 4) w sum |dS||k|) + u |dq|;  dk, dv alike over rows
+           dS: (u + r') |dS| + P e;  dq: scale (sum err(dS) |k| + (lk + 4) w sum |dS||k|) + u |dq|;  dk, dv alike over rows.
+           bf16: delta is <g, out> less F = sum dS, which takes the rounding of out away but leaves what F is off by,
+           f = sum (r' |dS| + P e) + (lk + 4) w sum |dS|, and u |F| <= u^2 sum |g||out| where F meets rounded P: both times sum P|k| in dq;
+           f alone, times P |q|, in dk.  fp32: the rounding of out, w sum |g||out|, is within e
 Second orders: every bound times 1.1, and 2^-126 times what a product's second factor can be for subnormal P (they may be flushed).
 """
 from __future__ import annotations
@@ -23,7 +26,7 @@ U = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
 
 
 def bounds(q, k, v, len_q, len_k, scale, window, sinks, dtype, out=None, g=None):
-    """Exact results and their bounds; with g the gradients' too (out: the output that the backward was handed)."""
+    """Exact results and their bounds; with g the gradients' too (out: the rounded output that the backward was handed)."""
     B, Tq, Hq, D = q.shape
     Tk, Hkv = k.shape[1:3]
     G, u = Hq // Hkv, U[dtype]
@@ -55,13 +58,20 @@ def bounds(q, k, v, len_q, len_k, scale, window, sinks, dtype, out=None, g=None)
                 continue
             go = g[b, :lq, h]
             oo = out[b, :lq, h]
-            dP, delta = go @ V.T, (go * oo).sum(1)
+            dP, delta = go @ V.T, (go * o).sum(1)
             dS = P * (dP - delta[:, None])
             rel2 = (rel + e_lse)[:, None]
             err = (D + 4) * W * (np.abs(go) @ np.abs(V).T + (np.abs(go) * np.abs(oo)).sum(1)[:, None])
+            go_oo = (np.abs(go) * np.abs(oo)).sum(1)
             e_S = (u + rel2) * np.abs(dS) + (1 + rel2) * P * err
+            f = np.zeros(lq)
+            if dtype == "bf16":
+                f = (rel2 * np.abs(dS) + (1 + rel2) * P * err).sum(1) + (lk + 4) * W * (np.abs(dS) + P * u * go_oo[:, None]).sum(1)
+                e_S = e_S + P * f[:, None]
             r["dq"][b, :lq, h] = scale * dS @ K
-            e["dq"][b, :lq, h] = scale * (e_S + (lk + 4) * W * np.abs(dS)) @ np.abs(K) + u * np.abs(r["dq"][b, :lq, h])
+            if dtype == "bf16":
+                e["dq"][b, :lq, h] += scale * (u * u * go_oo)[:, None] * (P @ np.abs(K))
+            e["dq"][b, :lq, h] += scale * (e_S + (lk + 4) * W * np.abs(dS)) @ np.abs(K) + u * np.abs(r["dq"][b, :lq, h])
             r["dk"][b, :lk, hk] += scale * dS.T @ Q
             e["dk"][b, :lk, hk] += scale * (e_S + (lq * G + 4) * W * np.abs(dS)).T @ np.abs(Q)
             r["dv"][b, :lk, hk] += P.T @ go
