@@ -27,6 +27,7 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dq_kernel(Att
   constexpr int KS = Tile::KS, KB = BK / 32, DB = DP / 32, ROWS = 128, STAGE = 2 * Tile::BYTES;
   extern __shared__ char lds[];
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t rbase = Tile::row_base(l), cbase = Tile::col_base(l);      // (of Rows too)
   char* const grows = lds + 2 * STAGE + w * Rows::BYTES;
   const uint32_t works = (uint32_t)(a.B * a.Hkv) * (uint32_t)a.nblk, id = attn_work(works);
   if (id == 0) report_lengths(a);
@@ -55,7 +56,7 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dq_kernel(Att
       const Frag o = has ? El::load(a.o.p + at + d * El::size) : El::zero();
 #pragma unroll
       for (int j = 0; j < 8; ++j) delta = fmaf(El::value(f, j), El::value(o, j), delta);
-      if constexpr (kRowsInLds<E>) Rows::put_row(grows, ks, l, f);
+      if constexpr (kRowsInLds<E>) Rows::put_row(grows, rbase, ks, f);
       else g[ks] = f;
     }
     delta = add_halves(delta);
@@ -102,9 +103,9 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dq_kernel(Att
       for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0.f;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        El::mma(s, Tile::row_frag(cur, kb, ks, l), q[ks]);
-        if constexpr (kRowsInLds<E>) El::mma(dp, Tile::row_frag(cur + Tile::BYTES, kb, ks, l), Rows::row_frag(grows, 0, ks, l));
-        else El::mma(dp, Tile::row_frag(cur + Tile::BYTES, kb, ks, l), g[ks]);
+        El::mma(s, Tile::row_frag(cur, rbase, kb, ks), q[ks]);
+        if constexpr (kRowsInLds<E>) El::mma(dp, Tile::row_frag(cur + Tile::BYTES, rbase, kb, ks), Rows::row_frag(grows, rbase, 0, ks));
+        else El::mma(dp, Tile::row_frag(cur + Tile::BYTES, rbase, kb, ks), g[ks]);
       }
       float e[16], ds[16];
 #pragma unroll
@@ -113,12 +114,12 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dq_kernel(Att
         ds[i] = e[i] * (dp[i] - delta);
       }
       if (part) {
+        const Seen sees(s0, n, p, a.window, a.sinks, 4 * (l >> 5));
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const int j = kb * 32 + acc_row(i, l);
-          const bool sees = (j < n) & seen(s0 + j, p, a.window, a.sinks);
-          e[i] = sees ? e[i] : 0.f;
-          ds[i] = sees ? ds[i] : 0.f;
+          const bool yes = sees(kb * 32 + acc_row(i, 0));
+          e[i] = yes ? e[i] : 0.f;
+          ds[i] = yes ? ds[i] : 0.f;
         }
       }
       if constexpr (kFix) {
@@ -132,7 +133,7 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dq_kernel(Att
         if constexpr (kFix) pf = El::of(e + 8 * h);
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
-          const Frag kf = Tile::col_frag(cur, db, kb * 2 + h, l);
+          const Frag kf = Tile::col_frag(cur, cbase, db, kb * 2 + h);
           El::mma(dq[db], kf, f);
           if constexpr (kFix) El::mma(mean[db], kf, pf);
         }
@@ -177,6 +178,7 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dkv_kernel(At
   constexpr int KS = Tile::KS, QB = BQ / 32, DB = DP / 32, STAGE = 2 * Tile::BYTES + 2 * BQ * 4;
   extern __shared__ char lds[];
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t rbase = Tile::row_base(l), cbase = Tile::col_base(l);      // (of Rows too)
   char* const vrows = lds + 2 * STAGE + w * Rows::BYTES;
   const uint32_t per = kw.items(), works = (uint32_t)(a.B * a.Hkv) * per, id = attn_work(works);
   if (id >= works) return;
@@ -195,7 +197,7 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dkv_kernel(At
       const int d = 16 * ks + 8 * (l >> 5);
       k[ks] = key < lk && d < a.D ? El::load(ks_ + d * El::size) : El::zero();
       const Frag f = key < lk && d < a.D ? El::load(vs_ + d * El::size) : El::zero();
-      if constexpr (kRowsInLds<E>) Rows::put_row(vrows, ks, l, f);
+      if constexpr (kRowsInLds<E>) Rows::put_row(vrows, rbase, ks, f);
       else v[ks] = f;
     }
   }
@@ -258,9 +260,9 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dkv_kernel(At
         for (int x = 0; x < 16; ++x) s[x] = dp[x] = 0.f;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-          El::mma(s, Tile::row_frag(cur, qb, ks, l), k[ks]);
-          if constexpr (kRowsInLds<E>) El::mma(dp, Tile::row_frag(cur + Tile::BYTES, qb, ks, l), Rows::row_frag(vrows, 0, ks, l));
-          else El::mma(dp, Tile::row_frag(cur + Tile::BYTES, qb, ks, l), v[ks]);
+          El::mma(s, Tile::row_frag(cur, rbase, qb, ks), k[ks]);
+          if constexpr (kRowsInLds<E>) El::mma(dp, Tile::row_frag(cur + Tile::BYTES, rbase, qb, ks), Rows::row_frag(vrows, rbase, 0, ks));
+          else El::mma(dp, Tile::row_frag(cur + Tile::BYTES, rbase, qb, ks), v[ks]);
         }
         float pr[16], ds[16];
 #pragma unroll
@@ -270,12 +272,15 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dkv_kernel(At
           ds[x] = pr[x] * (dp[x] - delta[row]);
         }
         if (part) {
+          // row c sees the key from position pmin + c on, to the end or to the last one whose window reaches it
+          const int lane = 4 * (l >> 5), from = key - pmin - lane;
+          const int to = (key < a.sinks ? rows - 1 : min(rows - 1, key + a.window - 1 - pmin)) - lane;
 #pragma unroll
           for (int x = 0; x < 16; ++x) {
-            const int row = qb * 32 + acc_row(x, l);
-            const bool sees = (row < rows) & seen(key, pmin + row, a.window, a.sinks);
-            pr[x] = sees ? pr[x] : 0.f;
-            ds[x] = sees ? ds[x] : 0.f;
+            const int c = qb * 32 + acc_row(x, 0);
+            const bool yes = (c >= from) & (c <= to);
+            pr[x] = yes ? pr[x] : 0.f;
+            ds[x] = yes ? ds[x] : 0.f;
           }
         }
 #pragma unroll
@@ -283,8 +288,8 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dkv_kernel(At
           const Frag pf = El::of(pr + 8 * h), sf = El::of(ds + 8 * h);
 #pragma unroll
           for (int db = 0; db < DB; ++db) {
-            El::mma(dv[db], Tile::col_frag(cur + Tile::BYTES, db, qb * 2 + h, l), pf);
-            El::mma(dk[db], Tile::col_frag(cur, db, qb * 2 + h, l), sf);
+            El::mma(dv[db], Tile::col_frag(cur + Tile::BYTES, cbase, db, qb * 2 + h), pf);
+            El::mma(dk[db], Tile::col_frag(cur, cbase, db, qb * 2 + h), sf);
           }
         }
       }

@@ -69,6 +69,9 @@ static inline dim3 attn_grid(int64_t wgs) {
   return dim3((unsigned)(wgs < kAttnRow ? wgs : kAttnRow), (unsigned)((wgs + kAttnRow - 1) / kAttnRow));
 }
 
+// Instruction kinds of __builtin_amdgcn_sched_group_barrier.
+constexpr int kMfma = 0x008, kDsRead = 0x100, kValu = 0x002, kTrans = 0x400;
+
 // ---- device side --------------------------------------------------------------------------
 
 // Workgroups go to the eight XCDs in turn; each XCD takes a range of consecutive work, so that the blocks of one key head meet in its L2.
@@ -206,74 +209,83 @@ struct AttnTile {
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lptr_t)(lds + (w * PER + i) * 1024), 16, off, 0, 0, 0);
     }
   }
-  // Step `ks` of row l % 32, as row_frag reads it.
-  __device__ static inline void put_row(char* lds, int ks, int l, const Frag& f) {
-    const int r = l & 31;
+  // A lane's reads are a base of its own, with the step or the column block put in by xor or as a constant: chunk numbers and swizzles
+  // meet bit by bit, and a row begins at a multiple of its length.
+  //
+  // Step `ks` of rows 32 rb + l % 32.
+  __device__ static inline uint32_t row_base(int l) {
+    const int r = l & 31, h = l >> 5;
+    return r * ROW + (((El::size == 2 ? h : 2 * h) ^ swz(r)) << 4);
+  }
+  __device__ static inline Frag row_frag(const char* lds, uint32_t base, int rb, int ks) {
     if constexpr (El::size == 2) {
-      *reinterpret_cast<u32x4_t*>(lds + at(r, 2 * ks + (l >> 5))) = f;
+      return *reinterpret_cast<const u32x4_t*>(lds + (base ^ (ks << 5)) + rb * 32 * ROW);
     } else {
-      const int c = 4 * ks + 2 * (l >> 5);
-      *reinterpret_cast<f32x4_t*>(lds + at(r, c)) = f.x[0];
-      *reinterpret_cast<f32x4_t*>(lds + at(r, c + 1)) = f.x[1];
+      return Frag{{*reinterpret_cast<const f32x4_t*>(lds + (base ^ (ks << 6)) + rb * 32 * ROW),
+                   *reinterpret_cast<const f32x4_t*>(lds + (base ^ (ks << 6) ^ 16) + rb * 32 * ROW)}};
     }
   }
-  // Step `ks` of rows 32 rb + l % 32.
-  __device__ static inline Frag row_frag(const char* lds, int rb, int ks, int l) {
-    const int r = rb * 32 + (l & 31);
+  __device__ static inline void put_row(char* lds, uint32_t base, int ks, const Frag& f) {
     if constexpr (El::size == 2) {
-      return *reinterpret_cast<const u32x4_t*>(lds + at(r, 2 * ks + (l >> 5)));
+      *reinterpret_cast<u32x4_t*>(lds + (base ^ (ks << 5))) = f;
     } else {
-      const int c = 4 * ks + 2 * (l >> 5);
-      return Frag{{*reinterpret_cast<const f32x4_t*>(lds + at(r, c)), *reinterpret_cast<const f32x4_t*>(lds + at(r, c + 1))}};
+      *reinterpret_cast<f32x4_t*>(lds + (base ^ (ks << 6))) = f.x[0];
+      *reinterpret_cast<f32x4_t*>(lds + (base ^ (ks << 6) ^ 16)) = f.x[1];
     }
   }
   // Columns 32 db + l % 32 of rows 16 s .. 16 s + 15 (dealt out as accumulators are).
-  __device__ static inline Frag col_frag(const char* lds, int db, int s, int l) {
+  __device__ static inline uint32_t col_base(int l) {
+    const int h = l >> 5, t = l & 15;
+    if constexpr (El::size == 2) return (4 * h + (t >> 2)) * ROW + (((((l >> 4) & 1) * 2 + ((t & 3) >> 1)) ^ swz(4 * h + (t >> 2))) << 4) + 8 * (t & 1);
+    else return 4 * h * ROW + ((((l & 31) >> 2) ^ h) << 4) + 4 * (l & 3);
+  }
+  __device__ static inline Frag col_frag(const char* lds, uint32_t base, int db, int s) {
     if constexpr (El::size == 2) {
       typedef __attribute__((address_space(3))) i16x4_t* tptr_t;
       u32x4_t f;
-      const int t = l & 15, c = db * 4 + ((l >> 4) & 1) * 2 + ((t & 3) >> 1);
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
-        const int r = 16 * s + 8 * p + 4 * (l >> 5) + (t >> 2);
-        const u32x2_t v = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tptr_t)(lds + at(r, c) + 8 * (t & 1))));
+        const uint32_t at = (base ^ ((db & 1) << 6)) + (CH == 8 ? 0 : ((db >> 1) ^ p) << 7) + (16 * s + 8 * p) * ROW;
+        const u32x2_t v = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tptr_t)(lds + at)));
         f[2 * p] = v.x;
         f[2 * p + 1] = v.y;
       }
       return f;
     } else {
       Frag f;
-      const int d = db * 32 + (l & 31);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const int r = 16 * s + 8 * (j >> 2) + 4 * (l >> 5) + (j & 3);
-        f.x[j >> 2][j & 3] = *reinterpret_cast<const float*>(lds + at(r, d >> 2) + 4 * (d & 3));
+        const uint32_t at = (base ^ ((j & 3) << 5)) + ((db ^ (j >> 2)) << 7) + (16 * s + 8 * (j >> 2) + (j & 3)) * ROW;
+        f.x[j >> 2][j & 3] = *reinterpret_cast<const float*>(lds + at);
       }
       return f;
     }
   }
   // The same for 16x16 blocks (steps of 32): columns 16 db + l % 16 of rows 32 s .. 32 s + 31, of which lane group g = l / 16 holds
   // 4 g .. 4 g + 3 and 16 + 4 g .. 16 + 4 g + 3, as two accumulator blocks do.
-  __device__ static inline Frag col_frag16(const char* lds, int db, int s, int l) {
+  __device__ static inline uint32_t col_base16(int l) {
+    const int g = l >> 4, t = l & 15;
+    if constexpr (El::size == 2) return (4 * g + (t >> 2)) * ROW + ((((t & 3) >> 1) ^ swz(4 * g + (t >> 2))) << 4) + 8 * (t & 1);
+    else return 4 * g * ROW + (((t >> 2) ^ swz(4 * g)) << 4) + 4 * (t & 3);
+  }
+  __device__ static inline Frag col_frag16(const char* lds, uint32_t base, int db, int s) {
     if constexpr (El::size == 2) {
       typedef __attribute__((address_space(3))) i16x4_t* tptr_t;
       u32x4_t f;
-      const int t = l & 15, c = db * 2 + ((t & 3) >> 1);
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
-        const int r = 32 * s + 16 * p + 4 * (l >> 4) + (t >> 2);
-        const u32x2_t v = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tptr_t)(lds + at(r, c) + 8 * (t & 1))));
+        const uint32_t at = (base ^ (db << 5)) + (32 * s + 16 * p) * ROW;
+        const u32x2_t v = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tptr_t)(lds + at)));
         f[2 * p] = v.x;
         f[2 * p + 1] = v.y;
       }
       return f;
     } else {
       Frag f;
-      const int d = db * 16 + (l & 15);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const int r = 32 * s + 16 * (j >> 2) + 4 * (l >> 4) + (j & 3);
-        f.x[j >> 2][j & 3] = *reinterpret_cast<const float*>(lds + at(r, d >> 2) + 4 * (d & 3));
+        const uint32_t at = (base ^ ((j & 3) << 5) ^ (db << 6)) + (32 * s + 16 * (j >> 2) + (j & 3)) * ROW;
+        f.x[j >> 2][j & 3] = *reinterpret_cast<const float*>(lds + at);
       }
       return f;
     }
@@ -332,6 +344,13 @@ __device__ inline bool none_seen(int s, int n, int pmin, int pmax, int window, i
 __device__ inline bool seen(int key, int p, int span, int sinks) {
   return (key <= p) & ((key > p - span) | (key < sinks));
 }
+// The same for the keys s + c, c < n, of a tile from position p, less `lane` (what of c depends on the lane): comparisons with constants.
+struct Seen {
+  int last, before, first;
+  __device__ inline Seen(int s, int n, int p, int span, int sinks, int lane)
+      : last(min(n - 1, p - s) - lane), before(p - span - s - lane), first(sinks - s - lane) {}
+  __device__ inline bool operator()(int c) const { return (c <= last) & ((c > before) | (c < first)); }
+};
 constexpr int kNoWindow = 1 << 30;    // Tk is at most this
 
 }  // namespace lmhead

@@ -182,6 +182,7 @@ __global__ __launch_bounds__(kFewWaves * 64, AttnElem<E>::size == 2 ? 2 : 1) voi
     for (int db = 0; db < DB; ++db) o[nn][db] = f32x4_t{0, 0, 0, 0};
   }
   Load next;
+  const uint32_t cbase = Tile::col_base16(l);
   int t = split * per + w;
   auto fetch = [&](int i) {
     const int s = tile_start<TK>(kt, i);
@@ -209,13 +210,11 @@ __global__ __launch_bounds__(kFewWaves * 64, AttnElem<E>::size == 2 ? 2 : 1) voi
 #pragma unroll
     for (int nn = 0; nn < NN; ++nn) {
       if (part) {
+        const Seen sees(s0, n, p[nn], a.window, a.sinks, 4 * g);
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int j = 16 * kb + 4 * g + i;
-            s[nn][kb][i] = ((j < n) & seen(s0 + j, p[nn], a.window, a.sinks)) ? s[nn][kb][i] : -INFINITY;
-          }
+          for (int i = 0; i < 4; ++i) s[nn][kb][i] = sees(16 * kb + i) ? s[nn][kb][i] : -INFINITY;
       }
       float top = -INFINITY;
 #pragma unroll
@@ -266,7 +265,7 @@ __global__ __launch_bounds__(kFewWaves * 64, AttnElem<E>::size == 2 ? 2 : 1) voi
       }
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
-        const Frag vf = Tile::col_frag16(lds, db, kg, l);
+        const Frag vf = Tile::col_frag16(lds, cbase, db, kg);
 #pragma unroll
         for (int nn = 0; nn < NN; ++nn) El::mma(o[nn][db], vf, pf[nn]);
       }

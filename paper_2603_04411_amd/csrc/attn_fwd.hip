@@ -40,6 +40,8 @@ __device__ inline void load_cache(char* lds, const uint8_t* codes, const uint8_t
   }
 }
 
+constexpr float kSlack = 8.f;
+
 // One workgroup takes NW * 32 rows (query i, head g of the key head: row r = i G + g) of one key head and walks the keys that
 // they see in tiles of BK: S^T = K Q^T with the keys along the accumulators' rows, so that a lane holds one query's logits and the
 // softmax needs one exchange between lane halves; the exponentials are the second operand of O^T = V^T P^T as they lie.
@@ -86,15 +88,25 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_fwd_kernel(AttnArgs a) {
 
   const char* kbase = a.k.p + b * a.k.seq + hk * a.k.head;
   const char* vbase = a.v.p + b * a.v.seq + hk * a.v.head;
-  auto load = [&](int t, char* to) {
+  // K and V have two tiles each in LDS: K runs one tile ahead
+  auto load_k = [&](int t, int at) {
+    char* const to = lds + at * Tile::BYTES;
     const int s = tile_start<BK>(kt, t), n = tile_end(kt, t) - s;
     if constexpr (kCache) {
       const int64_t row = (int64_t)bh * a.Tk + s;
       load_cache<Tile, NW, BK>(to, a.k_codes + row * (a.D / 2), a.k_scales + row * (a.D / 32), n, a.D, w, l);
-      load_cache<Tile, NW, BK>(to + Tile::BYTES, a.v_codes + row * (a.D / 2), a.v_scales + row * (a.D / 32), n, a.D, w, l);
     } else {
       Tile::template load<NW>(to, kbase + s * a.k.slot, (uint32_t)a.k.slot, n, a.D * El::size, w, l);
-      Tile::template load<NW>(to + Tile::BYTES, vbase + s * a.v.slot, (uint32_t)a.v.slot, n, a.D * El::size, w, l);
+    }
+  };
+  auto load_v = [&](int t, int at) {
+    char* const to = lds + (2 + at) * Tile::BYTES;
+    const int s = tile_start<BK>(kt, t), n = tile_end(kt, t) - s;
+    if constexpr (kCache) {
+      const int64_t row = (int64_t)bh * a.Tk + s;
+      load_cache<Tile, NW, BK>(to, a.v_codes + row * (a.D / 2), a.v_scales + row * (a.D / 32), n, a.D, w, l);
+    } else {
+      Tile::template load<NW>(to, vbase + s * a.v.slot, (uint32_t)a.v.slot, n, a.D * El::size, w, l);
     }
   };
 
@@ -103,61 +115,102 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_fwd_kernel(AttnArgs a) {
   for (int db = 0; db < DB; ++db)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
-  float m = -INFINITY, sum = 0.f;
+  float m = -INFINITY, sum = 0.f;      // the maximum that the exponentials are taken against, see below
+  using Logits = f32x16_t[KB];
+  const uint32_t rbase = Tile::row_base(l), cbase = Tile::col_base(l);
 
-  if (t0 < t1) load(t0, lds);
-  for (int t = t0; t < t1; ++t) {
-    char* const cur = lds + ((t - t0) & 1) * 2 * Tile::BYTES;
-    __builtin_amdgcn_s_waitcnt(kWaitVm0);
-    __syncthreads();
-    if (t + 1 < t1) load(t + 1, lds + ((t + 1 - t0) & 1) * 2 * Tile::BYTES);
-    const int s0 = tile_start<BK>(kt, t), n = min(BK, tile_end(kt, t) - s0);
-    if (none_seen(s0, n, wmin, wmax, a.window, a.sinks)) continue;
-    f32x16_t s[KB];
+  auto logits = [&](Logits& s, const char* k) {
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
+    for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) El::mma(s[kb], Tile::row_frag(cur, kb, ks, l), q[ks]);
-    }
+    for (int x = 0; x < KS * KB; ++x) El::mma(s[x % KB], Tile::row_frag(k, rbase, x % KB, x / KB), q[x / KB]);
+  };
+
+  // One tile: the softmax of `s`, beside which the matrix cores form the next tile's logits, and the product with V.
+  auto step = [&](int t, auto which, Logits& s, Logits& next) {
+    constexpr int P = decltype(which)::value;      // where its K and V lie
+    __builtin_amdgcn_s_waitcnt(kWaitVm0);
+    __syncthreads();
+    if (t + 2 < t1) load_k(t + 2, P);
+    if (t + 1 < t1) load_v(t + 1, 1 - P);
+    const int s0 = tile_start<BK>(kt, t), n = min(BK, tile_end(kt, t) - s0);
     if (n < BK || !all_seen(s0, n, wlow, wmax, a.window, a.sinks)) {
+      const Seen sees(s0, n, p, a.window, a.sinks, 4 * (l >> 5));
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int j = kb * 32 + acc_row(i, l);
-          s[kb][i] = ((j < n) & seen(s0 + j, p, a.window, a.sinks)) ? s[kb][i] : -INFINITY;
-        }
+        for (int i = 0; i < 16; ++i) s[kb][i] = sees(kb * 32 + acc_row(i, 0)) ? s[kb][i] : -INFINITY;
     }
     float top = s[0][0];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
-    top = max_halves(top);
-    const float now = fmaxf(m, top * a.scale2), base = now == -INFINITY ? 0.f : now;
-    const float keep = __builtin_amdgcn_exp2f(m - base);
-    m = now;
-    sum *= keep;
+    top = max_halves(top) * a.scale2;
+    // The exponentials are taken against a maximum that is only moved once a logit passes it by kSlack (powers of two): the sums
+    // then need no scaling in most tiles, and nothing comes near fp32's range.
+    if (__any(top > m + kSlack)) {
+      const float now = fmaxf(m, top), keep = __builtin_amdgcn_exp2f(m - (now == -INFINITY ? 0.f : now));
+      m = now;
+      sum *= keep;
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
+      for (int db = 0; db < DB; ++db)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) o[db][i] *= keep;
+        for (int i = 0; i < 16; ++i) o[db][i] *= keep;
+    }
+    const float base = m == -INFINITY ? 0.f : m;
+    const char* const k = lds + (1 - P) * Tile::BYTES;
+    const char* const v = lds + (2 + P) * Tile::BYTES;
+    Frag pf[2 * KB];
+    auto weights = [&]() {
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-      float e[16];
+      for (int kb = 0; kb < KB; ++kb) {
+        float e[16];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        e[i] = __builtin_amdgcn_exp2f(fmaf(s[kb][i], a.scale2, -base));
-        sum += e[i];
+        for (int i = 0; i < 16; ++i) {
+          e[i] = __builtin_amdgcn_exp2f(fmaf(s[kb][i], a.scale2, -base));
+          sum += e[i];
+        }
+        pf[2 * kb] = El::of(e);
+        pf[2 * kb + 1] = El::of(e + 8);
       }
+    };
+    if (t + 1 < t1) {
+      logits(next, k);
+      weights();
+      if constexpr (El::size == 2) {
+        constexpr int M = KS * KB;
+        __builtin_amdgcn_sched_group_barrier(kDsRead, 3, 0);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const Frag pf = El::of(e + 8 * h);
-#pragma unroll
-        for (int db = 0; db < DB; ++db) El::mma(o[db], Tile::col_frag(cur + Tile::BYTES, db, kb * 2 + h, l), pf);
+        for (int x = 0; x < M; ++x) {
+          __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(kTrans, 32 / M * KB / 2, 0);
+          __builtin_amdgcn_sched_group_barrier(kValu, 8, 0);
+        }
       }
+    } else {
+      weights();
+    }
+#pragma unroll
+    for (int x = 0; x < 2 * KB; ++x)
+#pragma unroll
+      for (int db = 0; db < DB; ++db) El::mma(o[db], Tile::col_frag(v, cbase, db, x), pf[x]);
+  };
+
+  if (t0 < t1) {
+    Logits s[2];
+    load_k(t0, 0);
+    load_v(t0, 0);
+    __builtin_amdgcn_s_waitcnt(kWaitVm0);
+    __syncthreads();
+    if (t0 + 1 < t1) load_k(t0 + 1, 1);
+    logits(s[0], lds);
+    for (int t = t0; t < t1; t += 2) {
+      step(t, std::integral_constant<int, 0>{}, s[0], s[1]);
+      if (t + 1 < t1) step(t + 1, std::integral_constant<int, 1>{}, s[1], s[0]);
     }
   }
   sum = add_halves(sum);
@@ -239,6 +292,7 @@ __global__ __launch_bounds__(256) void attn_weight_kernel(AttnArgs a, int nkey) 
   const int blk = uniform(id % nkey), hk = uniform(bh % a.Hkv), b = uniform(bh / a.Hkv);
   const int lq = clamp_len(a.len_q, b, a.Tq), lk = clamp_len(a.len_k, b, a.Tk);
   const int s0 = blk * 128, key = s0 + w * 32 + (l & 31);
+  const uint32_t rbase = Tile::row_base(l);
   if (s0 >= lk) return;
   Frag k[KS];
   if constexpr (kCache) {
@@ -250,7 +304,7 @@ __global__ __launch_bounds__(256) void attn_weight_kernel(AttnArgs a, int nkey) 
       __syncthreads();
       if (w == x) {
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) k[ks] = Tile::row_frag(lds, 0, ks, l);
+        for (int ks = 0; ks < KS; ++ks) k[ks] = Tile::row_frag(lds, rbase, 0, ks);
       }
     }
     __syncthreads();
@@ -284,7 +338,7 @@ __global__ __launch_bounds__(256) void attn_weight_kernel(AttnArgs a, int nkey) 
 #pragma unroll
       for (int x = 0; x < 16; ++x) s[x] = 0.f;
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) El::mma(s, Tile::row_frag(lds, 0, ks, l), k[ks]);
+      for (int ks = 0; ks < KS; ++ks) El::mma(s, Tile::row_frag(lds, rbase, 0, ks), k[ks]);
 #pragma unroll
       for (int x = 0; x < 16; ++x) {
         const int row = acc_row(x, l);
