@@ -29,11 +29,11 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dq_kernel(Att
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t rbase = Tile::row_base(l), cbase = Tile::col_base(l);      // (of Rows too)
   char* const grows = lds + 2 * STAGE + w * Rows::BYTES;
-  const uint32_t works = (uint32_t)(a.B * a.Hkv) * (uint32_t)a.nblk, id = attn_work(works);
-  if (id == 0) report_lengths(a);
-  if (id >= works) return;
-  const int blk = uniform(a.nblk - 1 - id % a.nblk);
-  const uint32_t bh = uniform(id / a.nblk);
+  report_lengths(a);
+  Work work;
+  if (!attn_work(a.B * a.Hkv, a.nblk, work)) return;
+  const int blk = a.nblk - 1 - work.in;
+  const uint32_t bh = work.bh;
   const int hk = uniform(bh % a.Hkv), b = uniform(bh / a.Hkv);
   const int lq = clamp_len(a.len_q, b, a.Tq), lk = clamp_len(a.len_k, b, a.Tk);
   const uint32_t r = blk * ROWS + w * 32 + (l & 31);
@@ -180,10 +180,10 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dkv_kernel(At
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t rbase = Tile::row_base(l), cbase = Tile::col_base(l);      // (of Rows too)
   char* const vrows = lds + 2 * STAGE + w * Rows::BYTES;
-  const uint32_t per = kw.items(), works = (uint32_t)(a.B * a.Hkv) * per, id = attn_work(works);
-  if (id >= works) return;
-  const uint32_t bh = uniform(id / per);
-  const int item = uniform(id % per), hk = uniform(bh % a.Hkv), b = uniform(bh / a.Hkv);
+  Work work;
+  if (!attn_work(a.B * a.Hkv, kw.items(), work)) return;
+  const uint32_t bh = work.bh;
+  const int item = work.in, hk = uniform(bh % a.Hkv), b = uniform(bh / a.Hkv);
   const bool far = item >= kw.nkey;
   const int blk = far ? uniform((item - kw.nkey) / (uint32_t)kw.nchunk) : item, chunk = far ? uniform((item - kw.nkey) % (uint32_t)kw.nchunk) : 0;
   const int lq = clamp_len(a.len_q, b, a.Tq), lk = clamp_len(a.len_k, b, a.Tk);
@@ -367,10 +367,10 @@ hipError_t bwd(const KeyWork& kw, AttnArgs a, hipStream_t s) {
   if (e == hipSuccess) e = allow_lds<dkv>(more);
   if (e != hipSuccess) return e;
   a.nblk = (int)(((int64_t)a.Tq * a.G + 127) / 128);
-  dq<<<attn_grid(attn_wgs((int64_t)a.B * a.Hkv * a.nblk)), 256, bytes, s>>>(a);
+  dq<<<attn_grid(attn_wgs((int64_t)a.B * a.Hkv, a.nblk)), 256, bytes, s>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  dkv<<<attn_grid(attn_wgs((int64_t)a.B * a.Hkv * kw.items())), 256, more, s>>>(a, kw);
+  dkv<<<attn_grid(attn_wgs((int64_t)a.B * a.Hkv, kw.items())), 256, more, s>>>(a, kw);
   e = hipGetLastError();
   if (e != hipSuccess || !kw.nfirst) return e;
   const int64_t threads = (int64_t)a.B * a.Hkv * kw.nfirst * kw.rows * (2 * DP / 4);

@@ -74,13 +74,27 @@ constexpr int kMfma = 0x008, kDsRead = 0x100, kValu = 0x002, kTrans = 0x400;
 
 // ---- device side --------------------------------------------------------------------------
 
-// Workgroups go to the eight XCDs in turn; each XCD takes a range of consecutive work, so that the blocks of one key head meet in its L2.
-__device__ inline uint32_t attn_work(uint32_t n) {
-  const uint32_t w = blockIdx.y * kAttnRow + blockIdx.x, per = (n + 7) / 8;
-  return w / 8 < per ? (w % 8) * per + w / 8 : n;      // n or more: nothing to do
-}
 __device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-static inline int64_t attn_wgs(int64_t n) { return (n + 7) / 8 * 8; }
+// A workgroup's place: which (sequence, key head), and which of the `inner` works on it.
+struct Work {
+  uint32_t bh, in;
+};
+// Workgroups go to the eight XCDs in turn.  The works of a key head read the same keys, so they go to one XCD's L2, and key heads go to
+// the XCDs in turn, so that sequences of unequal lengths do not leave some XCDs idle (8 x 2048, lengths from 512: a range of consecutive
+// work for each XCD 263 us).  Where their number is no multiple of eight each is dealt out to 2, 4 or 8 XCDs, its works in turn.
+__host__ __device__ inline uint32_t attn_parts(uint32_t heads) { return heads % 8 == 0 ? 1 : heads % 4 == 0 ? 2 : heads % 2 == 0 ? 4 : 8; }
+static inline int64_t attn_wgs(int64_t heads, int64_t inner) {
+  const int64_t s = attn_parts((uint32_t)heads);
+  return heads * s * ((inner + s - 1) / s);
+}
+// false: a workgroup without work.
+__device__ inline bool attn_work(uint32_t heads, uint32_t inner, Work& x) {
+  const uint32_t w = blockIdx.y * kAttnRow + blockIdx.x, s = attn_parts(heads), per = (inner + s - 1) / s;
+  const uint32_t k = w / 8, unit = (uint32_t)uniform(k / per) * 8 + w % 8, bh = unit / s;
+  x.bh = bh;
+  x.in = (uint32_t)uniform(k % per) * s + unit % s;
+  return bh < heads && x.in < inner;
+}
 
 __device__ inline int clamp_len(const int32_t* len, int b, int T) {
   if (!len) return T;
@@ -88,8 +102,9 @@ __device__ inline int clamp_len(const int32_t* len, int b, int T) {
   return n < 0 ? 0 : n > T ? T : n;
 }
 
-// The workgroup of the first work item reports the lengths that are out of range.
+// The first workgroup reports the lengths that are out of range.
 __device__ inline void report_lengths(const AttnArgs& a) {
+  if (blockIdx.x | blockIdx.y) return;
   int bad = 0;
   for (int b = threadIdx.x; b < a.B; b += blockDim.x) {
     if (a.len_q) bad |= (uint32_t)a.len_q[b] > (uint32_t)a.Tq;

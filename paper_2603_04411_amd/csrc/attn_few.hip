@@ -144,11 +144,11 @@ __global__ __launch_bounds__(kFewWaves * 64, AttnElem<E>::size == 2 ? 2 : 1) voi
   extern __shared__ char lds_all[];
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = l >> 4;
   char* const lds = lds_all + w * WLDS;
-  const uint32_t works = (uint32_t)(a.B * a.Hkv) * (uint32_t)a.nsplit, id = attn_work(works);
-  if (id == 0) report_lengths(a);
-  if (id >= works) return;
-  const int split = uniform(id % a.nsplit);
-  const uint32_t bh = uniform(id / a.nsplit);
+  report_lengths(a);
+  Work work;
+  if (!attn_work(a.B * a.Hkv, a.nsplit, work)) return;
+  const int split = work.in;
+  const uint32_t bh = work.bh;
   const int hk = uniform(bh % a.Hkv), b = uniform(bh / a.Hkv);
   const int lq = clamp_len(a.len_q, b, a.Tq), lk = clamp_len(a.len_k, b, a.Tk);
   const int R = a.Tq * a.G;
@@ -329,10 +329,10 @@ constexpr int kWeightKeys = 2048;
 template <typename E, int DP>
 __global__ __launch_bounds__(256) void attn_finish_kernel(AttnArgs a, int njoin, int nkey) {
   __shared__ float s_top[32], s_total[32];
-  const uint32_t per = njoin + nkey, id = attn_work((uint32_t)(a.B * a.Hkv) * per);
-  if (id >= (uint32_t)(a.B * a.Hkv) * per) return;
-  const uint32_t bh = uniform(id / per);
-  const int part_of = uniform(id % per), hk = uniform(bh % a.Hkv), b = uniform(bh / a.Hkv), R = a.Tq * a.G, ns = a.nsplit;
+  Work work;
+  if (!attn_work(a.B * a.Hkv, njoin + nkey, work)) return;
+  const uint32_t bh = work.bh;
+  const int part_of = work.in, hk = uniform(bh % a.Hkv), b = uniform(bh / a.Hkv), R = a.Tq * a.G, ns = a.nsplit;
   const int lq = clamp_len(a.len_q, b, a.Tq), lk = clamp_len(a.len_k, b, a.Tk);
   const float* const part = a.part + (int64_t)bh * ns * R * (DP + 2);
   const int64_t step = (int64_t)R * (DP + 2);
@@ -400,11 +400,11 @@ hipError_t few(const AttnArgs& a, hipStream_t s) {
   constexpr int bytes = kFewWaves * few_lds<E, DP, NN, TK>();
   hipError_t e = allow_lds<kernel>(bytes);
   if (e != hipSuccess) return e;
-  kernel<<<attn_grid(attn_wgs((int64_t)a.B * a.Hkv * a.nsplit)), kFewWaves * 64, bytes, s>>>(a);
+  kernel<<<attn_grid(attn_wgs((int64_t)a.B * a.Hkv, a.nsplit)), kFewWaves * 64, bytes, s>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess || (a.nsplit == 1 && !a.logits)) return e;
   const int njoin = a.nsplit > 1 ? (a.Tq * a.G * DP + 255) / 256 : 0, nkey = a.logits ? (a.Tk + kWeightKeys - 1) / kWeightKeys : 0;
-  attn_finish_kernel<E, DP><<<attn_grid(attn_wgs((int64_t)a.B * a.Hkv * (njoin + nkey))), 256, 0, s>>>(a, njoin, nkey);
+  attn_finish_kernel<E, DP><<<attn_grid(attn_wgs((int64_t)a.B * a.Hkv, njoin + nkey)), 256, 0, s>>>(a, njoin, nkey);
   return hipGetLastError();
 }
 

@@ -53,11 +53,11 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_fwd_kernel(AttnArgs a) {
   constexpr int KS = Tile::KS, KB = BK / 32, DB = DP / 32, ROWS = NW * 32;
   extern __shared__ char lds[];
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t works = (uint32_t)(a.B * a.Hkv) * (uint32_t)(a.nblk * a.nsplit), id = attn_work(works);
-  if (id == 0) report_lengths(a);
-  if (id >= works) return;
-  const int split = uniform(id % a.nsplit), blk = uniform(a.nblk - 1 - id / a.nsplit % a.nblk);
-  const uint32_t bh = uniform(id / a.nsplit / a.nblk);
+  report_lengths(a);
+  Work work;
+  if (!attn_work(a.B * a.Hkv, a.nblk * a.nsplit, work)) return;
+  const int split = uniform(work.in % a.nsplit), blk = uniform(a.nblk - 1 - work.in / a.nsplit);
+  const uint32_t bh = work.bh;
   const int hk = uniform(bh % a.Hkv), b = uniform(bh / a.Hkv);
   const int lq = clamp_len(a.len_q, b, a.Tq), lk = clamp_len(a.len_k, b, a.Tk);
 
@@ -286,10 +286,10 @@ __global__ __launch_bounds__(256) void attn_weight_kernel(AttnArgs a, int nkey) 
   extern __shared__ char lds[];
   __shared__ float ends[32];
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t works = (uint32_t)(a.B * a.Hkv) * (uint32_t)nkey, id = attn_work(works);
-  if (id >= works) return;
-  const uint32_t bh = uniform(id / nkey);
-  const int blk = uniform(id % nkey), hk = uniform(bh % a.Hkv), b = uniform(bh / a.Hkv);
+  Work work;
+  if (!attn_work(a.B * a.Hkv, nkey, work)) return;
+  const uint32_t bh = work.bh;
+  const int blk = work.in, hk = uniform(bh % a.Hkv), b = uniform(bh / a.Hkv);
   const int lq = clamp_len(a.len_q, b, a.Tq), lk = clamp_len(a.len_k, b, a.Tk);
   const int s0 = blk * 128, key = s0 + w * 32 + (l & 31);
   const uint32_t rbase = Tile::row_base(l);
@@ -360,7 +360,7 @@ hipError_t fwd(const AttnArgs& a, hipStream_t s) {
   const int bytes = 4 * AttnTile<E, DP, BK>::BYTES;
   hipError_t e = allow_lds<kernel>(bytes);
   if (e != hipSuccess) return e;
-  kernel<<<attn_grid(attn_wgs((int64_t)a.B * a.Hkv * a.nblk * a.nsplit)), NW * 64, bytes, s>>>(a);
+  kernel<<<attn_grid(attn_wgs((int64_t)a.B * a.Hkv, (int64_t)a.nblk * a.nsplit)), NW * 64, bytes, s>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess || a.nsplit == 1) return e;
   attn_join_kernel<E, DP><<<attn_grid(((int64_t)a.B * a.Hkv * a.Tq * a.G + 3) / 4), 256, 0, s>>>(a, NW * 32);
@@ -377,7 +377,7 @@ template <typename E, int DP, bool kCache>
 hipError_t weight(const AttnArgs& a, hipStream_t s) {
   constexpr auto kernel = attn_weight_kernel<E, DP, kCache>;
   const int bytes = AttnTile<E, DP, 32>::BYTES, nkey = (a.Tk + 127) / 128;
-  kernel<<<attn_grid(attn_wgs((int64_t)a.B * a.Hkv * nkey)), 256, bytes, s>>>(a, nkey);
+  kernel<<<attn_grid(attn_wgs((int64_t)a.B * a.Hkv, nkey)), 256, bytes, s>>>(a, nkey);
   return hipGetLastError();
 }
 
