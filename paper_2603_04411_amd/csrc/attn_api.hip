@@ -25,8 +25,8 @@ AttnPlan attn_plan(const attn_desc* d, bool cache4) {
     off += round_up(bytes, 256);
     return o;
   };
-  p.part = take(few || p.nsplit > 1 ? (size_t)wgs * p.nsplit * p.rows * (p.DP + 2) * sizeof(float) : 0);
-  p.logits = take(R <= kLogitRows ? (size_t)heads * d->Tk * R * sizeof(float) : 0);
+  p.part = take(few || p.nsplit > 1 ? (size_t)wgs * p.nsplit * p.rows * (p.DP + 4) * sizeof(float) : 0);
+  p.logits = take(R <= kLogitRows ? (size_t)heads * logit_groups(d->Tk) * R * 4 * sizeof(float) : 0);
   p.lse = take((size_t)d->B * d->Hq * d->Tq * sizeof(float));
   p.total = off;
   (void)cache4;

@@ -43,6 +43,8 @@ struct AttnArgs {
 };
 
 constexpr int kFewRows = 32;
+// Groups of four keys whose logits a key head has room for: tiles of first tokens and of the window, rounded up.
+__host__ __device__ inline int64_t logit_groups(int Tk) { return ((int64_t)Tk + 3) / 4 + 32; }
 constexpr int kLogitRows = 8;      // up to so many rows their logits are kept for the weights; of more K is read again
 
 // What a call needs in its workspace, and how its work is cut: the same for every call with this descriptor.

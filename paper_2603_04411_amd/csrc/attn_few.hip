@@ -183,11 +183,11 @@ __global__ __launch_bounds__(kFewWaves * 64, AttnElem<E>::size == 2 ? 2 : 1) voi
   }
   Load next;
   const uint32_t cbase = Tile::col_base16(l);
-  int t = split * per + w;
   auto fetch = [&](int i) {
     const int s = tile_start<TK>(kt, i);
     next.load(a, bh, b, hk, s, tile_end(kt, i) - s, l);
   };
+  int t = split * per + w;
   if (t < t1) fetch(t);
   for (; t < t1; t += kFewWaves) {
     const int s0 = tile_start<TK>(kt, t), n = min(TK, tile_end(kt, t) - s0);
@@ -224,17 +224,12 @@ __global__ __launch_bounds__(kFewWaves * 64, AttnElem<E>::size == 2 ? 2 : 1) voi
           s[nn][kb][i] *= a.scale2;
           top = fmaxf(top, s[nn][kb][i]);
         }
-      if (a.logits) {
+      if (a.logits) {      // [four keys][row][key]: sixteen bytes a lane, and what a tile leaves is one piece
         const int r = nn * 16 + (l & 15);
         if (r < R) {
-          float* const to = a.logits + ((int64_t)bh * a.Tk + s0) * R + r;
+          f32x4_t* const to = reinterpret_cast<f32x4_t*>(a.logits) + (((int64_t)bh * logit_groups(a.Tk) + (int64_t)t * (TK / 4) + g) * R + r);
 #pragma unroll
-          for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int j = 16 * kb + 4 * g + i;
-              if (j < n) to[(int64_t)j * R] = s[nn][kb][i];
-            }
+          for (int kb = 0; kb < KB; ++kb) to[kb * 4 * R] = s[nn][kb];
         }
       }
       top = max_quarters(top);
@@ -304,7 +299,7 @@ __global__ __launch_bounds__(kFewWaves * 64, AttnElem<E>::size == 2 ? 2 : 1) voi
     }
     const int qi = r / (uint32_t)a.G, head = hk * a.G + r % (uint32_t)a.G;
     if (a.nsplit > 1 || a.logits) {
-      float* const part = a.part + ((int64_t)(bh * a.nsplit + split) * R + r) * (DP + 2);
+      float* const part = a.part + ((int64_t)(bh * a.nsplit + split) * R + r) * (DP + 4);
       part[d] = acc;
       if (d == 0) {
         part[DP] = top;
@@ -323,75 +318,100 @@ __global__ __launch_bounds__(kFewWaves * 64, AttnElem<E>::size == 2 ? 2 : 1) voi
   }
 }
 
-// What follows the parts: rows are joined (workgroups 0 .. njoin - 1 of a key head), and the weight of the keys is added up from the logits
-// that the parts left (the others, of kWeightKeys keys each).
-constexpr int kWeightKeys = 2048;
-template <typename E, int DP>
+// What follows the parts.  Rows are joined by a workgroup each: 32 threads take a row's channels, four each (half of them where there are 64),
+// and eight groups of them every eighth part.  The weight of the keys is added up from the logits that the parts left, by workgroups of
+// kWeightKeys keys.
+constexpr int kWeightKeys = 1024;
+template <typename E, int DP, int TK>
 __global__ __launch_bounds__(256) void attn_finish_kernel(AttnArgs a, int njoin, int nkey) {
   __shared__ float s_top[32], s_total[32];
+  __shared__ f32x4_t s_sum[8][DP / 4];
   Work work;
   if (!attn_work(a.B * a.Hkv, njoin + nkey, work)) return;
   const uint32_t bh = work.bh;
   const int part_of = work.in, hk = uniform(bh % a.Hkv), b = uniform(bh / a.Hkv), R = a.Tq * a.G, ns = a.nsplit;
   const int lq = clamp_len(a.len_q, b, a.Tq), lk = clamp_len(a.len_k, b, a.Tk);
-  const float* const part = a.part + (int64_t)bh * ns * R * (DP + 2);
-  const int64_t step = (int64_t)R * (DP + 2);
-  // maximum and total of each row: eight threads a row
+  const float* const part = a.part + (int64_t)bh * ns * R * (DP + 4);
+  const int step = R * (DP + 4);
+  const bool joins = part_of < njoin;
+  // maximum and total of the rows that are wanted: a wavefront takes every fourth row, its lanes the parts
   {
-    const int r = threadIdx.x >> 3, c = threadIdx.x & 7;
-    float top = -INFINITY, total = 0.f;
-    if (r < R)
-      for (int s = c; s < ns; s += 8) top = fmaxf(top, part[s * step + (int64_t)r * (DP + 2) + DP]);
+    const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
+    for (int r = joins ? part_of : w; r < (joins ? part_of + 1 : R); r += 4) {
+      const float* const at = part + (int64_t)r * (DP + 4) + DP;
+      float top = -INFINITY, total = 0.f;
+      for (int s = l; s < ns; s += 64) top = fmaxf(top, at[(int64_t)s * step]);
 #pragma unroll
-    for (int x = 4; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
-    const float base = top == -INFINITY ? 0.f : top;
-    if (r < R)
-      for (int s = c; s < ns; s += 8) {
-        const float* const at = part + s * step + (int64_t)r * (DP + 2) + DP;
-        total += __builtin_amdgcn_exp2f(at[0] - base) * at[1];
-      }
+      for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+      const float base = top == -INFINITY ? 0.f : top;
+      for (int s = l; s < ns; s += 64) total += __builtin_amdgcn_exp2f(at[(int64_t)s * step] - base) * at[(int64_t)s * step + 1];
 #pragma unroll
-    for (int x = 4; x; x >>= 1) total += __shfl_xor(total, x);
-    if (c == 0 && r < R) s_top[r] = base, s_total[r] = total;
+      for (int x = 32; x; x >>= 1) total += __shfl_xor(total, x);
+      if (l == 0) s_top[r] = base, s_total[r] = total;      // (of a joined row all wavefronts write the same)
+    }
   }
   __syncthreads();
-  if (part_of < njoin) {
-    const int i = part_of * 256 + threadIdx.x, r = i / DP, d = i % DP;
-    if (r >= R) return;
+  if (joins) {
+    const int r = part_of, c = threadIdx.x & 31, of = threadIdx.x >> 5;
     const float base = s_top[r], total = s_total[r];
-    float acc = 0.f;
-    for (int s = 0; s < ns; ++s) {
-      const float* const at = part + s * step + (int64_t)r * (DP + 2);
-      acc += __builtin_amdgcn_exp2f(at[DP] - base) * at[d];
+    if (c < DP / 4) {
+      f32x4_t acc = f32x4_t{0, 0, 0, 0};
+#pragma unroll 4
+      for (int s = of; s < ns; s += 8) {
+        const float* const at = part + (int64_t)s * step + (int64_t)r * (DP + 4);
+        const float f = __builtin_amdgcn_exp2f(at[DP] - base);
+        const f32x4_t x = *reinterpret_cast<const f32x4_t*>(at + 4 * c);
+        acc.x = fmaf(f, x.x, acc.x), acc.y = fmaf(f, x.y, acc.y), acc.z = fmaf(f, x.z, acc.z), acc.w = fmaf(f, x.w, acc.w);
+      }
+      s_sum[of][c] = acc;
     }
+    __syncthreads();
     const int qi = r / (uint32_t)a.G, head = hk * a.G + r % (uint32_t)a.G;
-    if (d < a.D) {
+    if (threadIdx.x < DP / 4 && 4 * (int)threadIdx.x < a.D) {
+      f32x4_t y = s_sum[0][threadIdx.x];
+#pragma unroll
+      for (int x = 1; x < 8; ++x) y += s_sum[x][threadIdx.x];
+      const float inv = total == 0.f ? 0.f : 1.f / total;
+      if (total == 0.f) y = f32x4_t{0, 0, 0, 0};
       char* const out = a.o.p + b * a.o.seq + (int64_t)qi * a.o.slot + head * a.o.head;
-      const float y = total == 0.f ? 0.f : acc / total;
-      if constexpr (AttnElem<E>::size == 2) reinterpret_cast<uint16_t*>(out)[d] = (uint16_t)pack_bf16(y, 0.f);
-      else reinterpret_cast<float*>(out)[d] = y;
+      AttnElem<E>::store4(out + 4 * threadIdx.x * AttnElem<E>::size, y.x * inv, y.y * inv, y.z * inv, y.w * inv);
     }
-    if (d == 0 && a.lse)
+    if (threadIdx.x == 0 && a.lse)
       a.lse[((int64_t)b * a.Hq + head) * a.Tq + qi] = total == 0.f ? -INFINITY : (base + __builtin_amdgcn_logf(total)) * kLn2;
     return;
   }
   // keys outside [0, e0) and [lo, e1) are seen by no row and have no logits
   const int pmin = lq ? max(0, lk - lq) : 0, pmax = lq ? lk - 1 : -1;
-  const KeyTiles kt = key_tiles<32>(pmin, pmax, a.window, a.sinks);
-  for (int x = 0; x < kWeightKeys / 256; ++x) {
-    const int key = (part_of - njoin) * kWeightKeys + x * 256 + threadIdx.x;
-    if (key >= lk) return;
-    float sum = 0.f;
-    if (pmax >= 0 && (key < kt.e0 || key >= kt.lo)) {
-      const float* const at = a.logits + ((int64_t)bh * a.Tk + key) * R;
-      for (int r = 0; r < R; ++r) {
-        const float e = __builtin_amdgcn_exp2f(at[r] - s_top[r]) / s_total[r];
-        sum += s_total[r] == 0.f ? 0.f : e;
-      }
+  const KeyTiles kt = key_tiles<TK>(pmin, pmax, a.window, a.sinks);
+  if (threadIdx.x < R) s_total[threadIdx.x] = s_total[threadIdx.x] == 0.f ? 0.f : 1.f / s_total[threadIdx.x];
+  __syncthreads();
+  // four keys a thread: their logits are one load a row unless a range begins or ends among them, or keys and groups of logits are out of step
+  const int key0 = (part_of - njoin) * kWeightKeys + 4 * threadIdx.x;
+  if (key0 >= lk) return;
+  f32x4_t sum = f32x4_t{0, 0, 0, 0};
+  const f32x4_t* const logits = reinterpret_cast<const f32x4_t*>(a.logits) + (int64_t)bh * logit_groups(a.Tk) * R;
+  auto place = [&](int key) { return key < kt.e0 ? key : kt.n0 * TK + key - kt.lo; };
+  if (pmax >= 0 && (key0 + 3 < kt.e0 || key0 >= kt.lo) && (place(key0) & 3) == 0) {
+    const f32x4_t* const z = logits + (int64_t)(place(key0) >> 2) * R;
+    for (int r = 0; r < R; ++r) {
+      const f32x4_t x = z[r];
+      const float top = s_top[r], inv = s_total[r];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum[i] = fmaf(inv == 0.f ? 0.f : __builtin_amdgcn_exp2f(x[i] - top), inv, sum[i]);
     }
-    float* const to = a.weight + (int64_t)bh * a.Tk + key;
-    *to = a.decay == 0.f ? sum : fmaf(a.decay, *to, sum);
+  } else if (pmax >= 0) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int key = key0 + i;
+      if (key >= kt.e0 && key < kt.lo) continue;
+      const float* const z = reinterpret_cast<const float*>(logits + (int64_t)(place(key) >> 2) * R) + (place(key) & 3);
+      for (int r = 0; r < R; ++r) sum[i] = fmaf(s_total[r] == 0.f ? 0.f : __builtin_amdgcn_exp2f(z[r * 4] - s_top[r]), s_total[r], sum[i]);
+    }
   }
+  float* const to = a.weight + (int64_t)bh * a.Tk + key0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (key0 + i < lk) to[i] = a.decay == 0.f ? sum[i] : fmaf(a.decay, to[i], sum[i]);
 }
 
 template <typename E, int DP, int NN, int TK, bool kCache>
@@ -403,8 +423,8 @@ hipError_t few(const AttnArgs& a, hipStream_t s) {
   kernel<<<attn_grid(attn_wgs((int64_t)a.B * a.Hkv, a.nsplit)), kFewWaves * 64, bytes, s>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess || (a.nsplit == 1 && !a.logits)) return e;
-  const int njoin = a.nsplit > 1 ? (a.Tq * a.G * DP + 255) / 256 : 0, nkey = a.logits ? (a.Tk + kWeightKeys - 1) / kWeightKeys : 0;
-  attn_finish_kernel<E, DP><<<attn_grid(attn_wgs((int64_t)a.B * a.Hkv, njoin + nkey)), 256, 0, s>>>(a, njoin, nkey);
+  const int njoin = a.nsplit > 1 ? a.Tq * a.G : 0, nkey = a.logits ? (a.Tk + kWeightKeys - 1) / kWeightKeys : 0;
+  attn_finish_kernel<E, DP, TK><<<attn_grid(attn_wgs((int64_t)a.B * a.Hkv, njoin + nkey)), 256, 0, s>>>(a, njoin, nkey);
   return hipGetLastError();
 }
 
