@@ -108,82 +108,92 @@ def attn_bwd_workspace_bytes(desc: AttnDesc) -> int:
     return int(_lib().attn_bwd_workspace_bytes(C.byref(desc)))
 
 
-def _heads(t, name, desc, T, H, x, device):
-    """Device pointer of a [B, T, H, D] tensor that lies as layout `x` says."""
-    n, s = t.shape, t.stride()
-    if (t.dtype is _TORCH.get(desc.dtype) and t.get_device() == device and len(n) == 4 and n[0] >= desc.B and n[1] >= T and n[2] >= H
-            and n[3] >= desc.D and s[3] == 1 and (s[0] == x.seq or desc.B == 1) and (s[1] == x.slot or T == 1)
-            and (s[2] == x.head or H == 1)):
-        return t.data_ptr()
-    if t.is_cuda and t.dtype is _TORCH.get(desc.dtype) and t.get_device() == device:
-        _bad(name, f"[{desc.B}, {T}, {H}, {desc.D}] with strides ({x.seq}, {x.slot}, {x.head}, 1) expected, got {tuple(n)} with {tuple(s)}")
-    return _refuse(t, name, _TORCH.get(desc.dtype), device, "")
+class _Sizes:
+    """What the checks of a descriptor's tensors compare with, made once for its contents."""
+
+    def __init__(self, desc, raw):
+        self.raw, d = raw, desc
+        self.status = int(_lib().attn_validate_desc(C.byref(desc)))
+        if self.status:
+            return
+        self.dtype, self.ref, self.B = _TORCH[d.dtype], C.byref(desc), d.B
+        B, Tq, Tk, Hq, Hkv, D = d.B, d.Tq, d.Tk, d.Hq, d.Hkv, d.D
+        # shape and strides of each tensor; those of the new rows of a cache in 4 bits
+        self.q, self.k, self.v, self.o = ((torch.Size((B, T, H, D)), (x.seq, x.slot, x.head, 1)) for T, H, x in
+                                          ((Tq, Hq, d.q), (Tk, Hkv, d.k), (Tk, Hkv, d.v), (Tq, Hq, d.o)))
+        self.k_new, self.v_new = ((torch.Size((B, Tq, Hkv, D)), (x.seq, x.slot, x.head, 1)) for x in (d.k, d.v))
+        self.lse, self.weight, rows = B * Hq * Tq, B * Hkv * Tk, B * Hkv * Tk
+        self.codes, self.scales = rows * (D // 2), rows * (D // 32)
 
 
-def _out_args(desc, out, lse, weight, dev):
-    return (_heads(out, "out", desc, desc.Tq, desc.Hq, desc.o, dev), _arg(lse, "lse", torch.float32, desc.B * desc.Hq * desc.Tq, dev),
-            _arg(weight, "weight", torch.float32, desc.B * desc.Hkv * desc.Tk, dev))
-
-
-def _good(desc, where):
+def _sizes(desc, where):
     """The descriptor's own refusal comes first: the checks of tensors rely on its sizes."""
-    rc = _lib().attn_validate_desc(C.byref(desc))
-    if rc != 0:
-        raise LmheadError(rc, where)
+    raw = bytes(desc)
+    sizes = desc.__dict__.get("_sizes")
+    if sizes is None or sizes.raw != raw:
+        sizes = desc._sizes = _Sizes(desc, raw)
+    if sizes.status:
+        raise LmheadError(sizes.status, where)
+    return sizes
+
+
+def _heads(t, name, s, want, device):
+    """Device pointer of a [B, T, H, D] tensor with the shape and strides that are wanted; it may have more of each."""
+    if t.dtype is s.dtype and t.get_device() == device:
+        n, st = t.shape, t.stride()
+        if n == want[0] and st == want[1]:
+            return t.data_ptr()
+        if len(n) == 4 and all(a >= b for a, b in zip(n, want[0])) and all(a == b or c == 1 for a, b, c in zip(st, want[1], want[0])):
+            return t.data_ptr()
+        _bad(name, f"{tuple(want[0])} with strides {want[1]} expected, got {tuple(n)} with {tuple(st)}")
+    return _refuse(t, name, s.dtype, device, "")
 
 
 def attn_fwd(desc, q, k, v, len_q, len_k, out, lse, weight, decay, ws) -> None:
     """len_q, len_k: int32[B], or None where every slot is valid; lse, weight: or None."""
-    _good(desc, "attn_fwd")
-    lib, dev, i32 = _lib(), _device(), torch.int32
-    rc = lib.attn_fwd(
-        C.byref(desc), _heads(q, "q", desc, desc.Tq, desc.Hq, desc.q, dev), _heads(k, "k", desc, desc.Tk, desc.Hkv, desc.k, dev),
-        _heads(v, "v", desc, desc.Tk, desc.Hkv, desc.v, dev), _arg(len_q, "len_q", i32, desc.B, dev), _arg(len_k, "len_k", i32, desc.B, dev),
-        *_out_args(desc, out, lse, weight, dev), decay, _arg(ws, "ws", torch.uint8, 0, dev), ws.numel(), _stream(dev))
+    s, dev, i32, f32 = _sizes(desc, "attn_fwd"), _device(), torch.int32, torch.float32
+    rc = _lib().attn_fwd(
+        s.ref, _heads(q, "q", s, s.q, dev), _heads(k, "k", s, s.k, dev), _heads(v, "v", s, s.v, dev), _arg(len_q, "len_q", i32, s.B, dev),
+        _arg(len_k, "len_k", i32, s.B, dev), _heads(out, "out", s, s.o, dev), _arg(lse, "lse", f32, s.lse, dev),
+        _arg(weight, "weight", f32, s.weight, dev), decay, _arg(ws, "ws", torch.uint8, 0, dev), ws.numel(), _stream(dev))
     _check(rc, "attn_fwd")
 
 
 def attn_bwd(desc, q, k, v, len_q, len_k, out, lse, g_out, dq, dk, dv, ws) -> None:
-    _good(desc, "attn_bwd")
-    lib, dev, i32 = _lib(), _device(), torch.int32
-    Tq, Tk, Hq, Hkv = desc.Tq, desc.Tk, desc.Hq, desc.Hkv
-    rc = lib.attn_bwd(
-        C.byref(desc), _heads(q, "q", desc, Tq, Hq, desc.q, dev), _heads(k, "k", desc, Tk, Hkv, desc.k, dev),
-        _heads(v, "v", desc, Tk, Hkv, desc.v, dev), _arg(len_q, "len_q", i32, desc.B, dev), _arg(len_k, "len_k", i32, desc.B, dev),
-        _heads(out, "out", desc, Tq, Hq, desc.o, dev), _arg(lse, "lse", torch.float32, desc.B * Hq * Tq, dev),
-        _heads(g_out, "g_out", desc, Tq, Hq, desc.o, dev), _heads(dq, "dq", desc, Tq, Hq, desc.q, dev),
-        _heads(dk, "dk", desc, Tk, Hkv, desc.k, dev), _heads(dv, "dv", desc, Tk, Hkv, desc.v, dev), _arg(ws, "ws", torch.uint8, 0, dev),
-        ws.numel(), _stream(dev))
+    s, dev, i32 = _sizes(desc, "attn_bwd"), _device(), torch.int32
+    rc = _lib().attn_bwd(
+        s.ref, _heads(q, "q", s, s.q, dev), _heads(k, "k", s, s.k, dev), _heads(v, "v", s, s.v, dev), _arg(len_q, "len_q", i32, s.B, dev),
+        _arg(len_k, "len_k", i32, s.B, dev), _heads(out, "out", s, s.o, dev), _arg(lse, "lse", torch.float32, s.lse, dev),
+        _heads(g_out, "g_out", s, s.o, dev), _heads(dq, "dq", s, s.q, dev), _heads(dk, "dk", s, s.k, dev), _heads(dv, "dv", s, s.v, dev),
+        _arg(ws, "ws", torch.uint8, 0, dev), ws.numel(), _stream(dev))
     _check(rc, "attn_bwd")
 
 
 # ---- the cache in 4 bits --------------------------------------------------------------------------------------------
 
 
-def _cache(desc, k_codes, k_scales, v_codes, v_scales, dev):
-    rows, u8 = desc.B * desc.Hkv * desc.Tk, torch.uint8
-    return (_arg(k_codes, "k_codes", u8, rows * (desc.D // 2), dev), _arg(k_scales, "k_scales", u8, rows * (desc.D // 32), dev),
-            _arg(v_codes, "v_codes", u8, rows * (desc.D // 2), dev), _arg(v_scales, "v_scales", u8, rows * (desc.D // 32), dev))
+def _cache(s, k_codes, k_scales, v_codes, v_scales, dev):
+    u8 = torch.uint8
+    return (_arg(k_codes, "k_codes", u8, s.codes, dev), _arg(k_scales, "k_scales", u8, s.scales, dev),
+            _arg(v_codes, "v_codes", u8, s.codes, dev), _arg(v_scales, "v_scales", u8, s.scales, dev))
 
 
 def kv4_store(desc, k, v, len_q, len_k, k_codes, k_scales, v_codes, v_scales, ws) -> None:
     """k, v: the new tokens' rows, [B, Tq, Hkv, D]."""
-    _good(desc, "kv4_store")
-    lib, dev, i32 = _lib(), _device(), torch.int32
-    rc = lib.kv4_store(
-        C.byref(desc), _heads(k, "k", desc, desc.Tq, desc.Hkv, desc.k, dev), _heads(v, "v", desc, desc.Tq, desc.Hkv, desc.v, dev),
-        _arg(len_q, "len_q", i32, desc.B, dev), _arg(len_k, "len_k", i32, desc.B, dev), *_cache(desc, k_codes, k_scales, v_codes, v_scales, dev),
-        _arg(ws, "ws", torch.uint8, 0, dev), ws.numel(), _stream(dev))
+    s, dev, i32 = _sizes(desc, "kv4_store"), _device(), torch.int32
+    rc = _lib().kv4_store(
+        s.ref, _heads(k, "k", s, s.k_new, dev), _heads(v, "v", s, s.v_new, dev), _arg(len_q, "len_q", i32, s.B, dev),
+        _arg(len_k, "len_k", i32, s.B, dev), *_cache(s, k_codes, k_scales, v_codes, v_scales, dev), _arg(ws, "ws", torch.uint8, 0, dev),
+        ws.numel(), _stream(dev))
     _check(rc, "kv4_store")
 
 
 def kv4_attn(desc, q, k_codes, k_scales, v_codes, v_scales, len_q, len_k, out, lse, weight, decay, ws) -> None:
-    _good(desc, "kv4_attn")
-    lib, dev, i32 = _lib(), _device(), torch.int32
-    rc = lib.kv4_attn(
-        C.byref(desc), _heads(q, "q", desc, desc.Tq, desc.Hq, desc.q, dev), *_cache(desc, k_codes, k_scales, v_codes, v_scales, dev),
-        _arg(len_q, "len_q", i32, desc.B, dev), _arg(len_k, "len_k", i32, desc.B, dev), *_out_args(desc, out, lse, weight, dev), decay,
-        _arg(ws, "ws", torch.uint8, 0, dev), ws.numel(), _stream(dev))
+    s, dev, i32, f32 = _sizes(desc, "kv4_attn"), _device(), torch.int32, torch.float32
+    rc = _lib().kv4_attn(
+        s.ref, _heads(q, "q", s, s.q, dev), *_cache(s, k_codes, k_scales, v_codes, v_scales, dev), _arg(len_q, "len_q", i32, s.B, dev),
+        _arg(len_k, "len_k", i32, s.B, dev), _heads(out, "out", s, s.o, dev), _arg(lse, "lse", f32, s.lse, dev),
+        _arg(weight, "weight", f32, s.weight, dev), decay, _arg(ws, "ws", torch.uint8, 0, dev), ws.numel(), _stream(dev))
     _check(rc, "kv4_attn")
 
 

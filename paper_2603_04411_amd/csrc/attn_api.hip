@@ -17,8 +17,15 @@ AttnPlan attn_plan(const attn_desc* d, bool cache4) {
   p.nblk = (int)((R + p.rows - 1) / p.rows);
   const int64_t wgs = heads * p.nblk;
   const int64_t span = d->window ? std::min<int64_t>(d->Tk, (int64_t)d->window + d->sinks + p.rows / G + 1) : d->Tk;
-  const int64_t tiles = (span + 63) / 64;
-  p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>({(few ? 1024 : 512) / wgs, tiles / (few ? 4 : 1), (int64_t)256}));
+  if (few) {
+    // A workgroup's part: 1024 keys (its wavefronts' eight tiles each hide the start), less where that leaves compute units idle, down to
+    // two tiles a wavefront; not more parts than the joining workgroups want to add up.
+    const int64_t tiles = (span + 31) / 32;
+    const int64_t want = std::max(tiles / 32, std::min(tiles / 8, 512 / heads));
+    p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>({want, 4096 / heads, 256}));
+  } else {
+    p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>({512 / wgs, (span + 63) / 64, 256}));
+  }
   size_t off = sizeof(AttnHeader);
   auto take = [&](size_t bytes) {
     const size_t o = off;
@@ -110,6 +117,10 @@ int run_fwd(const attn_desc* d, const AttnPlan& p, AttnArgs& a, void* ws, float*
   a.weight = weight;
   a.decay = decay;
   const int64_t rows = (int64_t)d->Tq * a.G;
+  // what the call reads of the cache, against what the last-level cache holds
+  const int64_t span = d->window ? std::min<int64_t>(d->Tk, (int64_t)d->window + d->sinks + d->Tq) : d->Tk;
+  const int64_t row = a.k_codes ? d->D / 2 + d->D / 32 : (int64_t)d->D * (d->dtype == LMHEAD_BF16 ? 2 : 4);
+  a.past = 2 * (int64_t)d->B * d->Hkv * span * row > (256ll << 20);
   if (weight && rows <= kLogitRows) {
     a.lse = lse;
     a.logits = reinterpret_cast<float*>(base + p.logits);

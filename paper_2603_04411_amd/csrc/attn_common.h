@@ -35,6 +35,7 @@ struct AttnArgs {
   float decay;
   AttnHeader* hdr;
   int nblk, nsplit;         // blocks of rows, and parts of a block's keys
+  bool past;                // few rows: read K and V past the caches
   float* logits;            // of a few rows: [b][key head][key][row], for the weights
   float* part;              // [b][key head][split][row of the block-padded rows]{DP sums, maximum, sum}
   // backward

@@ -8,7 +8,10 @@ namespace {
 constexpr int kFewWaves = 4;
 
 // A tile of TK keys of one key head in registers, on its way: K as fragments (lane l holds keys 16 kb + l % 16), V as it lies in memory.
-template <typename E, int DP, int TK>
+//
+// kPast: keys and values that no cache will hold are asked for past them (decoding 64 x 8192, 1.3 GB: 252 us, so 225; 16 x 2048, 134 MB,
+// called again and again: 29 us, so 33).
+template <typename E, int DP, int TK, bool kPast>
 struct Plain {
   using El = AttnElem<E>;
   using Frag = typename El::Frag;
@@ -24,19 +27,18 @@ struct Plain {
     const __amdgpu_buffer_rsrc_t kr = rsrc(a.k.p + b * a.k.seq + hk * a.k.head + s * a.k.slot, rows * (int)a.k.slot);
     const __amdgpu_buffer_rsrc_t vr = rsrc(a.v.p + b * a.v.seq + hk * a.v.head + s * a.v.slot, rows * (int)a.v.slot);
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
+    for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
+      for (int c = 0; c < El::size / 2; ++c) {
+        const int at = channel(ks, l) * El::size + 16 * c;
+        const uint32_t off = at < width ? (uint32_t)(l & 15) * (uint32_t)a.k.slot + at : 0x80000000u;
 #pragma unroll
-        for (int c = 0; c < El::size / 2; ++c) {
-          const int at = channel(ks, l) * El::size + 16 * c;
-          k[kb][ks][c] = fetch(kr, at < width ? (uint32_t)(16 * kb + (l & 15)) * (uint32_t)a.k.slot + at : 0x80000000u);
-        }
+        for (int kb = 0; kb < KB; ++kb) k[kb][ks][c] = fetch(kr, off, 16 * kb * (int)a.k.slot);
+      }
+    const int at = (l % Tile::CH) * 16;
+    const uint32_t off = at < width ? (uint32_t)(l / Tile::CH) * (uint32_t)a.v.slot + at : 0x80000000u;
 #pragma unroll
-    for (int i = 0; i < VL; ++i) {
-      const int r = (i * 64 + l) / Tile::CH, at = (l % Tile::CH) * 16;
-      v[i] = fetch(vr, at < width ? (uint32_t)r * (uint32_t)a.v.slot + at : 0x80000000u);
-    }
+    for (int i = 0; i < VL; ++i) v[i] = fetch(vr, off, i * (64 / Tile::CH) * (int)a.v.slot);
   }
   __device__ inline Frag key(int kb, int ks) const {
     if constexpr (El::size == 2) return k[kb][ks][0];
@@ -51,7 +53,10 @@ struct Plain {
     const uint64_t first = (uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x);
     return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<char*>(first), 0, uniform(bytes), 0x00020000);
   }
-  __device__ static inline u32x4_t fetch(__amdgpu_buffer_rsrc_t r, uint32_t off) { return __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0); }
+  // `off` of the lane and `more` of the wavefront together are held against the buffer's length
+  __device__ static inline u32x4_t fetch(__amdgpu_buffer_rsrc_t r, uint32_t off, int more) {
+    return __builtin_amdgcn_raw_buffer_load_b128(r, off, more, kPast ? 2 : 0);
+  }
 };
 
 // Eight values from a word of codes.
@@ -71,7 +76,7 @@ __device__ inline typename AttnElem<E>::Frag decode8(uint32_t codes, float size)
 
 // The same in 4 bits.  A lane's channels of a key are DP / 4 consecutive ones (q is dealt out alike), so that its codes are one load and it
 // needs no exchange; V is written to LDS in the storage type, which holds its values exactly.
-template <typename E, int DP, int TK>
+template <typename E, int DP, int TK, bool kPast>
 struct Coded {
   using El = AttnElem<E>;
   using Frag = typename El::Frag;
@@ -89,19 +94,22 @@ struct Coded {
     const int rows = n < TK ? n : TK, cb = a.D / 2, sb = a.D / 32;
     const __amdgpu_buffer_rsrc_t kr = P::rsrc((const char*)a.k_codes + row * cb, rows * cb), kq = P::rsrc((const char*)a.k_scales + row * sb, rows * sb);
     const __amdgpu_buffer_rsrc_t vr = P::rsrc((const char*)a.v_codes + row * cb, rows * cb), vq = P::rsrc((const char*)a.v_scales + row * sb, rows * sb);
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-      const int r = 16 * kb + (l & 15), at = channel(0, l) / 2;
+    {
+      const int r = l & 15, at = channel(0, l) / 2;
       const uint32_t off = at < cb ? r * cb + at : 0x80000000u, sc = at < cb ? r * sb + at / 16 : 0x80000000u;
-      if constexpr (KS == 4) k[kb] = P::fetch(kr, off);
-      else k[kb] = __builtin_amdgcn_raw_buffer_load_b64(kr, off, 0, 0);
-      ks_[kb] = __builtin_amdgcn_raw_buffer_load_b8(kq, sc, 0, 0);
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        if constexpr (KS == 4) k[kb] = P::fetch(kr, off, 16 * kb * cb);
+        else k[kb] = __builtin_amdgcn_raw_buffer_load_b64(kr, off, 16 * kb * cb, 0);
+        ks_[kb] = __builtin_amdgcn_raw_buffer_load_b8(kq, sc, 16 * kb * sb, 0);
+      }
     }
+    const int r = l / (DP / 32), block = l % (DP / 32);
+    const uint32_t off = block < sb ? r * cb + block * 16 : 0x80000000u, sc = block < sb ? r * sb + block : 0x80000000u;
 #pragma unroll
     for (int i = 0; i < VL; ++i) {
-      const int r = (i * 64 + l) / (DP / 32), block = l % (DP / 32);
-      v[i] = P::fetch(vr, block < sb ? r * cb + block * 16 : 0x80000000u);
-      vs[i] = __builtin_amdgcn_raw_buffer_load_b8(vq, block < sb ? r * sb + block : 0x80000000u, 0, 0);
+      v[i] = P::fetch(vr, off, i * (2048 / DP) * cb);
+      vs[i] = __builtin_amdgcn_raw_buffer_load_b8(vq, sc, i * (2048 / DP) * sb, 0);
     }
   }
   __device__ inline Frag key(int kb, int ks) const { return decode8<E>(k[kb][ks], __builtin_bit_cast(float, ks_[kb] << 23)); }
@@ -122,7 +130,7 @@ struct Coded {
       }
     }
   }
-  using P = Plain<E, DP, TK>;
+  using P = Plain<E, DP, TK, kPast>;
 };
 
 template <typename E, int DP, int NN, int TK>
@@ -134,11 +142,11 @@ constexpr int few_lds() {      // of a wavefront: a tile of values, then its sum
 // A workgroup takes the rows of one key head and a part of the keys they see; its wavefronts take tiles in turn, each with sums of its own,
 // and join them through LDS.  Nothing is shared in the loop, so there is no barrier in it: a wavefront asks for its next tile in registers
 // before the softmax of this one.
-template <typename E, int DP, int NN, int TK, bool kCache>
+template <typename E, int DP, int NN, int TK, bool kCache, bool kPast>
 __global__ __launch_bounds__(kFewWaves * 64, AttnElem<E>::size == 2 ? 2 : 1) void attn_few_kernel(AttnArgs a) {
   using El = AttnElem<E>;
   using Frag = typename El::Frag;
-  using Load = typename std::conditional<kCache, Coded<E, DP, TK>, Plain<E, DP, TK>>::type;
+  using Load = typename std::conditional<kCache, Coded<E, DP, TK, kPast>, Plain<E, DP, TK, kPast>>::type;
   using Tile = AttnTile<E, DP, TK>;
   constexpr int KS = DP / 32, KB = TK / 16, DB = DP / 16, WLDS = few_lds<E, DP, NN, TK>();
   extern __shared__ char lds_all[];
@@ -205,7 +213,8 @@ __global__ __launch_bounds__(kFewWaves * 64, AttnElem<E>::size == 2 ? 2 : 1) voi
 #pragma unroll
         for (int nn = 0; nn < NN; ++nn) El::mma(s[nn][kb], kf, q[nn][ks]);
       }
-    if (t + kFewWaves < t1) fetch(t + kFewWaves);
+    // (where logits are stored, behind their stores: a wait for loads then finds older stores only, not ones that were issued since)
+    if (!a.logits && t + kFewWaves < t1) fetch(t + kFewWaves);
     const bool part = few_rows || n < TK || !all_seen(s0, n, pmin, pmax, a.window, a.sinks);
 #pragma unroll
     for (int nn = 0; nn < NN; ++nn) {
@@ -231,6 +240,7 @@ __global__ __launch_bounds__(kFewWaves * 64, AttnElem<E>::size == 2 ? 2 : 1) voi
 #pragma unroll
           for (int kb = 0; kb < KB; ++kb) to[kb * 4 * R] = s[nn][kb];
         }
+        if (nn == NN - 1 && t + kFewWaves < t1) fetch(t + kFewWaves);
       }
       top = max_quarters(top);
       if (__any(top > m[nn])) {
@@ -324,7 +334,7 @@ __global__ __launch_bounds__(kFewWaves * 64, AttnElem<E>::size == 2 ? 2 : 1) voi
 constexpr int kWeightKeys = 1024;
 template <typename E, int DP, int TK>
 __global__ __launch_bounds__(256) void attn_finish_kernel(AttnArgs a, int njoin, int nkey) {
-  __shared__ float s_top[32], s_total[32];
+  __shared__ float s_top[8], s_total[8];      // of a row that is joined: of its eight groups of parts; else: of the rows
   __shared__ f32x4_t s_sum[8][DP / 4];
   Work work;
   if (!attn_work(a.B * a.Hkv, njoin + nkey, work)) return;
@@ -334,43 +344,66 @@ __global__ __launch_bounds__(256) void attn_finish_kernel(AttnArgs a, int njoin,
   const float* const part = a.part + (int64_t)bh * ns * R * (DP + 4);
   const int step = R * (DP + 4);
   const bool joins = part_of < njoin;
-  // maximum and total of the rows that are wanted: a wavefront takes every fourth row, its lanes the parts
-  {
-    const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
-    for (int r = joins ? part_of : w; r < (joins ? part_of + 1 : R); r += 4) {
-      const float* const at = part + (int64_t)r * (DP + 4) + DP;
-      float top = -INFINITY, total = 0.f;
-      for (int s = l; s < ns; s += 64) top = fmaxf(top, at[(int64_t)s * step]);
+  // Four keys a thread: their logits are one load a row unless a range begins or ends among them, or keys and groups of logits are out of
+  // step.  They are asked for before the parts are looked at.  Keys outside [0, e0) and [lo, e1) are seen by no row and have no logits.
+  const int pmin = lq ? max(0, lk - lq) : 0, pmax = lq ? lk - 1 : -1, key0 = (part_of - njoin) * kWeightKeys + 4 * threadIdx.x;
+  const KeyTiles kt = key_tiles<TK>(pmin, pmax, a.window, a.sinks);
+  const f32x4_t* const logits = reinterpret_cast<const f32x4_t*>(a.logits) + (int64_t)bh * logit_groups(a.Tk) * R;
+  auto place = [&](int key) { return key < kt.e0 ? key : kt.n0 * TK + key - kt.lo; };
+  const bool all = !joins && key0 < lk && pmax >= 0 && (key0 + 3 < kt.e0 || key0 >= kt.lo) && (place(key0) & 3) == 0;
+  f32x4_t z[kLogitRows];
 #pragma unroll
-      for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
-      const float base = top == -INFINITY ? 0.f : top;
-      for (int s = l; s < ns; s += 64) total += __builtin_amdgcn_exp2f(at[(int64_t)s * step] - base) * at[(int64_t)s * step + 1];
-#pragma unroll
-      for (int x = 32; x; x >>= 1) total += __shfl_xor(total, x);
-      if (l == 0) s_top[r] = base, s_total[r] = total;      // (of a joined row all wavefronts write the same)
-    }
-  }
-  __syncthreads();
+  for (int r = 0; r < kLogitRows; ++r) z[r] = all && r < R ? logits[(int64_t)(place(key0) >> 2) * R + r] : f32x4_t{0, 0, 0, 0};
   if (joins) {
     const int r = part_of, c = threadIdx.x & 31, of = threadIdx.x >> 5;
-    const float base = s_top[r], total = s_total[r];
-    if (c < DP / 4) {
-      f32x4_t acc = f32x4_t{0, 0, 0, 0};
-#pragma unroll 4
-      for (int s = of; s < ns; s += 8) {
-        const float* const at = part + (int64_t)s * step + (int64_t)r * (DP + 4);
-        const float f = __builtin_amdgcn_exp2f(at[DP] - base);
-        const f32x4_t x = *reinterpret_cast<const f32x4_t*>(at + 4 * c);
-        acc.x = fmaf(f, x.x, acc.x), acc.y = fmaf(f, x.y, acc.y), acc.z = fmaf(f, x.z, acc.z), acc.w = fmaf(f, x.w, acc.w);
+    float top = -INFINITY, total = 0.f;
+    f32x4_t acc = f32x4_t{0, 0, 0, 0};
+    constexpr int U = 4;      // parts asked for at once
+    for (int s0 = of; s0 < ns; s0 += 8 * U) {
+      float m[U], l[U];
+      f32x4_t x[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int s = s0 + 8 * u;
+        const float* const at = part + (int64_t)(s < ns ? s : s0) * step + (int64_t)r * (DP + 4);
+        m[u] = s < ns ? at[DP] : -INFINITY;
+        l[u] = at[DP + 1];
+        x[u] = c < DP / 4 ? *reinterpret_cast<const f32x4_t*>(at + 4 * c) : f32x4_t{0, 0, 0, 0};
       }
-      s_sum[of][c] = acc;
+      float now = top;
+#pragma unroll
+      for (int u = 0; u < U; ++u) now = fmaxf(now, m[u]);
+      const float base = now == -INFINITY ? 0.f : now, keep = __builtin_amdgcn_exp2f(top - base);
+      total *= keep;
+      acc *= keep;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float f = __builtin_amdgcn_exp2f(m[u] - base);
+        total = fmaf(f, l[u], total);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] = fmaf(f, x[u][i], acc[i]);
+      }
+      top = now;
     }
+    if (c < DP / 4) s_sum[of][c] = acc;
+    if (c == 0) s_top[of] = top, s_total[of] = total;
     __syncthreads();
+    float base = s_top[0];
+#pragma unroll
+    for (int x = 1; x < 8; ++x) base = fmaxf(base, s_top[x]);
+    if (base == -INFINITY) base = 0.f;
+    total = 0.f;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) total = fmaf(__builtin_amdgcn_exp2f(s_top[x] - base), s_total[x], total);
     const int qi = r / (uint32_t)a.G, head = hk * a.G + r % (uint32_t)a.G;
     if (threadIdx.x < DP / 4 && 4 * (int)threadIdx.x < a.D) {
-      f32x4_t y = s_sum[0][threadIdx.x];
+      f32x4_t y = f32x4_t{0, 0, 0, 0};
 #pragma unroll
-      for (int x = 1; x < 8; ++x) y += s_sum[x][threadIdx.x];
+      for (int x = 0; x < 8; ++x) {
+        const float f = __builtin_amdgcn_exp2f(s_top[x] - base);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = fmaf(f, s_sum[x][threadIdx.x][i], y[i]);
+      }
       const float inv = total == 0.f ? 0.f : 1.f / total;
       if (total == 0.f) y = f32x4_t{0, 0, 0, 0};
       char* const out = a.o.p + b * a.o.seq + (int64_t)qi * a.o.slot + head * a.o.head;
@@ -380,32 +413,42 @@ __global__ __launch_bounds__(256) void attn_finish_kernel(AttnArgs a, int njoin,
       a.lse[((int64_t)b * a.Hq + head) * a.Tq + qi] = total == 0.f ? -INFINITY : (base + __builtin_amdgcn_logf(total)) * kLn2;
     return;
   }
-  // keys outside [0, e0) and [lo, e1) are seen by no row and have no logits
-  const int pmin = lq ? max(0, lk - lq) : 0, pmax = lq ? lk - 1 : -1;
-  const KeyTiles kt = key_tiles<TK>(pmin, pmax, a.window, a.sinks);
+  // maximum and total of each row: a wavefront takes every fourth row, its lanes the parts
+  {
+    const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
+    for (int r = w; r < R; r += 4) {
+      const float* const at = part + (int64_t)r * (DP + 4) + DP;
+      float top = -INFINITY, total = 0.f;
+      for (int s = l; s < ns; s += 64) top = fmaxf(top, at[(int64_t)s * step]);
+#pragma unroll
+      for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+      const float base = top == -INFINITY ? 0.f : top;
+      for (int s = l; s < ns; s += 64) total = fmaf(__builtin_amdgcn_exp2f(at[(int64_t)s * step] - base), at[(int64_t)s * step + 1], total);
+#pragma unroll
+      for (int x = 32; x; x >>= 1) total += __shfl_xor(total, x);
+      if (l == 0) s_top[r] = base, s_total[r] = total;
+    }
+  }
+  __syncthreads();
   if (threadIdx.x < R) s_total[threadIdx.x] = s_total[threadIdx.x] == 0.f ? 0.f : 1.f / s_total[threadIdx.x];
   __syncthreads();
-  // four keys a thread: their logits are one load a row unless a range begins or ends among them, or keys and groups of logits are out of step
-  const int key0 = (part_of - njoin) * kWeightKeys + 4 * threadIdx.x;
   if (key0 >= lk) return;
   f32x4_t sum = f32x4_t{0, 0, 0, 0};
-  const f32x4_t* const logits = reinterpret_cast<const f32x4_t*>(a.logits) + (int64_t)bh * logit_groups(a.Tk) * R;
-  auto place = [&](int key) { return key < kt.e0 ? key : kt.n0 * TK + key - kt.lo; };
-  if (pmax >= 0 && (key0 + 3 < kt.e0 || key0 >= kt.lo) && (place(key0) & 3) == 0) {
-    const f32x4_t* const z = logits + (int64_t)(place(key0) >> 2) * R;
-    for (int r = 0; r < R; ++r) {
-      const f32x4_t x = z[r];
+  if (all) {
+#pragma unroll
+    for (int r = 0; r < kLogitRows; ++r) {
+      if (r >= R) break;
       const float top = s_top[r], inv = s_total[r];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sum[i] = fmaf(inv == 0.f ? 0.f : __builtin_amdgcn_exp2f(x[i] - top), inv, sum[i]);
+      for (int i = 0; i < 4; ++i) sum[i] = fmaf(inv == 0.f ? 0.f : __builtin_amdgcn_exp2f(z[r][i] - top), inv, sum[i]);
     }
   } else if (pmax >= 0) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int key = key0 + i;
       if (key >= kt.e0 && key < kt.lo) continue;
-      const float* const z = reinterpret_cast<const float*>(logits + (int64_t)(place(key) >> 2) * R) + (place(key) & 3);
-      for (int r = 0; r < R; ++r) sum[i] = fmaf(s_total[r] == 0.f ? 0.f : __builtin_amdgcn_exp2f(z[r * 4] - s_top[r]), s_total[r], sum[i]);
+      const float* const x = reinterpret_cast<const float*>(logits + (int64_t)(place(key) >> 2) * R) + (place(key) & 3);
+      for (int r = 0; r < R; ++r) sum[i] = fmaf(s_total[r] == 0.f ? 0.f : __builtin_amdgcn_exp2f(x[r * 4] - s_top[r]), s_total[r], sum[i]);
     }
   }
   float* const to = a.weight + (int64_t)bh * a.Tk + key0;
@@ -414,9 +457,9 @@ __global__ __launch_bounds__(256) void attn_finish_kernel(AttnArgs a, int njoin,
     if (key0 + i < lk) to[i] = a.decay == 0.f ? sum[i] : fmaf(a.decay, to[i], sum[i]);
 }
 
-template <typename E, int DP, int NN, int TK, bool kCache>
-hipError_t few(const AttnArgs& a, hipStream_t s) {
-  constexpr auto kernel = attn_few_kernel<E, DP, NN, TK, kCache>;
+template <typename E, int DP, int NN, int TK, bool kCache, bool kPast>
+hipError_t few_with(const AttnArgs& a, hipStream_t s) {
+  constexpr auto kernel = attn_few_kernel<E, DP, NN, TK, kCache, kPast>;
   constexpr int bytes = kFewWaves * few_lds<E, DP, NN, TK>();
   hipError_t e = allow_lds<kernel>(bytes);
   if (e != hipSuccess) return e;
@@ -428,10 +471,15 @@ hipError_t few(const AttnArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <typename E, int DP, int NN, int TK, bool kCache>
+hipError_t few(const AttnArgs& a, hipStream_t s) {
+  return a.past ? few_with<E, DP, NN, TK, kCache, true>(a, s) : few_with<E, DP, NN, TK, kCache, false>(a, s);
+}
+
 template <typename E, int DP>
 hipError_t few_rows(const AttnArgs& a, hipStream_t s) {
   const bool one = a.Tq * a.G <= 16;
-  if (a.k_codes) return one ? few<E, DP, 1, 64, true>(a, s) : few<E, DP, 2, 32, true>(a, s);
+  if (a.k_codes) return one ? few<E, DP, 1, 32, true>(a, s) : few<E, DP, 2, 32, true>(a, s);
   return one ? few<E, DP, 1, 32, false>(a, s) : few<E, DP, 2, 32, false>(a, s);
 }
 
