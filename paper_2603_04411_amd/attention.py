@@ -108,6 +108,15 @@ def attn_bwd_workspace_bytes(desc: AttnDesc) -> int:
     return int(_lib().attn_bwd_workspace_bytes(C.byref(desc)))
 
 
+class _Heads:
+    """What a [B, T, H, D] tensor of a call has to be."""
+
+    def __init__(self, B, T, H, D, x):
+        self.shape, self.strides, self.n = torch.Size((B, T, H, D)), (x.seq, x.slot, x.head, 1), B * T * H * D
+        dense = (T * H * D, H * D, D)
+        self.dense = all(a == b or n == 1 for a, b, n in zip(self.strides, dense, self.shape))
+
+
 class _Sizes:
     """What the checks of a descriptor's tensors compare with, made once for its contents."""
 
@@ -118,12 +127,11 @@ class _Sizes:
             return
         self.dtype, self.ref, self.B = _TORCH[d.dtype], C.byref(desc), d.B
         B, Tq, Tk, Hq, Hkv, D = d.B, d.Tq, d.Tk, d.Hq, d.Hkv, d.D
-        # shape and strides of each tensor; those of the new rows of a cache in 4 bits
-        self.q, self.k, self.v, self.o = ((torch.Size((B, T, H, D)), (x.seq, x.slot, x.head, 1)) for T, H, x in
-                                          ((Tq, Hq, d.q), (Tk, Hkv, d.k), (Tk, Hkv, d.v), (Tq, Hq, d.o)))
-        self.k_new, self.v_new = ((torch.Size((B, Tq, Hkv, D)), (x.seq, x.slot, x.head, 1)) for x in (d.k, d.v))
-        self.lse, self.weight, rows = B * Hq * Tq, B * Hkv * Tk, B * Hkv * Tk
-        self.codes, self.scales = rows * (D // 2), rows * (D // 32)
+        self.q, self.o = _Heads(B, Tq, Hq, D, d.q), _Heads(B, Tq, Hq, D, d.o)
+        self.k, self.v = _Heads(B, Tk, Hkv, D, d.k), _Heads(B, Tk, Hkv, D, d.v)
+        self.k_new, self.v_new = _Heads(B, Tq, Hkv, D, d.k), _Heads(B, Tq, Hkv, D, d.v)      # rows for a cache in 4 bits
+        rows = B * Hkv * Tk
+        self.lse, self.weight, self.codes, self.scales = B * Hq * Tq, rows, rows * (D // 2), rows * (D // 32)
 
 
 def _sizes(desc, where):
@@ -138,14 +146,17 @@ def _sizes(desc, where):
 
 
 def _heads(t, name, s, want, device):
-    """Device pointer of a [B, T, H, D] tensor with the shape and strides that are wanted; it may have more of each."""
+    """Device pointer of a [B, T, H, D] tensor with the shape and strides that are wanted (it may have more of each), or of a dense buffer where
+    they are dense."""
     if t.dtype is s.dtype and t.get_device() == device:
+        if want.dense and t.is_contiguous() and t.numel() == want.n:
+            return t.data_ptr()
         n, st = t.shape, t.stride()
-        if n == want[0] and st == want[1]:
+        if n == want.shape and st == want.strides:
             return t.data_ptr()
-        if len(n) == 4 and all(a >= b for a, b in zip(n, want[0])) and all(a == b or c == 1 for a, b, c in zip(st, want[1], want[0])):
+        if len(n) == 4 and all(a >= b for a, b in zip(n, want.shape)) and all(a == b or c == 1 for a, b, c in zip(st, want.strides, want.shape)):
             return t.data_ptr()
-        _bad(name, f"{tuple(want[0])} with strides {want[1]} expected, got {tuple(n)} with {tuple(st)}")
+        _bad(name, f"{tuple(want.shape)} with strides {want.strides} expected, got {tuple(n)} with {tuple(st)}")
     return _refuse(t, name, s.dtype, device, "")
 
 
