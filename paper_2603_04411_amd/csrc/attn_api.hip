@@ -175,7 +175,7 @@ int attn_fwd(const attn_desc* desc, const void* q, const void* k, const void* v,
 
 size_t attn_bwd_workspace_bytes(const attn_desc* desc) {
   if (validate(desc) != LMHEAD_OK) return 0;
-  return sizeof(AttnHeader) + lse_bytes(desc) + attn_first_bytes(desc);
+  return sizeof(AttnHeader) + lse_bytes(desc) + attn_before_bytes(desc) + attn_parts_bytes(desc);
 }
 
 int attn_bwd(const attn_desc* desc, const void* q, const void* k, const void* v, const int32_t* len_q, const int32_t* len_k,
@@ -201,7 +201,8 @@ int attn_bwd(const attn_desc* desc, const void* q, const void* k, const void* v,
   a.dq = tensor(dq, desc->q, esz), a.dk = tensor(dk, desc->k, esz), a.dv = tensor(dv, desc->v, esz);
   a.lse = const_cast<float*>(lse);
   a.delta = reinterpret_cast<float*>(static_cast<char*>(ws) + sizeof(AttnHeader));
-  a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + sizeof(AttnHeader) + lse_bytes(desc));
+  a.before = reinterpret_cast<int64_t*>(static_cast<char*>(ws) + sizeof(AttnHeader) + lse_bytes(desc));
+  a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + sizeof(AttnHeader) + lse_bytes(desc) + attn_before_bytes(desc));
   LM_TRY(launch_attn_bwd(desc, p, a, static_cast<hipStream_t>(stream)));
   return LMHEAD_OK;
 }

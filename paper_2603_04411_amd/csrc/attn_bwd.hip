@@ -6,6 +6,114 @@ namespace lmhead {
 
 namespace {
 
+// How dk and dv are cut.  An item is a block of 128 keys of a key head; its tiles are the queries that see some of them, 32 of one head each: those
+// that the block reaches through its window and, for a block with first tokens, the ones behind.  Items differ in length, with the
+// window, the sequences' lengths and the first tokens, so the workgroups (as many as are resident) take equal shares of the row of all tiles.  A
+// share may begin and end inside an item: what it has of that item it leaves as fp32 sums, which attn_parts_kernel adds up in order.
+// (Eight sequences of 1024 to 4096 under a window of 1024, 28 and 4 heads: a workgroup an item, with the queries behind in items of their own, 920 us.)
+struct KeyItem {
+  int i0, main, far0, far;      // first query and tiles of a head through the window, and behind
+  __host__ __device__ int tiles() const { return main + far; }
+};
+constexpr int kKeyBlock = 128, kQueryTile = 32;
+constexpr int kLeastShare = 8;      // tiles
+
+__host__ __device__ inline KeyItem key_item(int s0, int lq, int lk, int window, int sinks) {
+  KeyItem x{0, 0, 0, 0};
+  if (s0 >= lk) return x;
+  const int offset = lk - lq, last = (lk < s0 + kKeyBlock ? lk : s0 + kKeyBlock) - 1;
+  x.i0 = s0 > offset ? s0 - offset : 0;
+  const int64_t end = (int64_t)last + window - offset;
+  const int i1 = end < lq ? (int)end : lq;
+  if (i1 > x.i0) x.main = (i1 - x.i0 + kQueryTile - 1) / kQueryTile;
+  x.far0 = i1 > x.i0 ? i1 : x.i0;
+  if (s0 < sinks && lq > x.far0) x.far = (lq - x.far0 + kQueryTile - 1) / kQueryTile;
+  return x;
+}
+
+// How many workgroups there are, and whether each has one item (short ones are not cut).
+struct KeyShares {
+  int nkey, wgs;
+  bool whole;
+};
+KeyShares key_shares(const attn_desc* d, int resident) {
+  KeyShares k{};
+  k.nkey = (d->Tk + kKeyBlock - 1) / kKeyBlock;
+  const int64_t G = d->Hq / d->Hkv, each = ((int64_t)d->Tq + kQueryTile - 1) / kQueryTile + 1, items = (int64_t)d->B * d->Hkv * k.nkey;
+  k.whole = each * G <= kLeastShare;
+  k.wgs = (int)(k.whole ? items : items >= resident ? resident : (items * each * G + kLeastShare - 1) / kLeastShare);
+  if (!k.whole && k.wgs > resident) k.wgs = resident;
+  k.wgs = (k.wgs + 7) / 8 * 8;
+  return k;
+}
+
+// before[b * nkey + blk]: tiles of one head's items before this one, over sequences and blocks; the last entry: all.  By one workgroup.
+__device__ inline void count_tiles(const AttnArgs& a, int nkey) {
+  __shared__ int64_t s_wave[4];
+  const int n = a.B * nkey, l = threadIdx.x & 63, w = threadIdx.x >> 6;
+  int64_t sum = 0;
+  for (int x = 0; x < n; x += 256) {
+    const int at = x + threadIdx.x;
+    int64_t mine = 0;
+    if (at < n) {
+      const int b = at / nkey;
+      const int lq = a.len_q ? min(max(a.len_q[b], 0), a.Tq) : a.Tq, lk = a.len_k ? min(max(a.len_k[b], 0), a.Tk) : a.Tk;
+      mine = key_item(at % nkey * kKeyBlock, lq, lk, a.window, a.sinks).tiles();
+    }
+    int64_t upto = mine;
+#pragma unroll
+    for (int y = 1; y < 64; y <<= 1) {
+      const int64_t v = __shfl_up(upto, y);
+      upto += l >= y ? v : 0;
+    }
+    if (l == 63) s_wave[w] = upto;
+    __syncthreads();
+    int64_t prior = sum;
+    for (int y = 0; y < 4; ++y) {
+      if (y < w) prior += s_wave[y];
+      sum += s_wave[y];
+    }
+    if (at < n) a.before[at] = prior + upto - mine;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) a.before[n] = sum;
+}
+
+// Part of an item that a workgroup does: tiles [from, to) of the item's `tiles` (all heads).
+struct Share {
+  int64_t at, end;       // of this workgroup, in the row of all tiles
+  int hk, item, from, to, tiles;
+};
+// The share's piece that begins at x.at; false: none is left.
+__device__ inline bool next_piece(const AttnArgs& a, int nkey, Share& x) {
+  if (x.at >= x.end) return false;
+  const int n = a.B * nkey;
+  const int64_t all = a.before[n] * a.G;      // of a key head
+  x.hk = uniform((int)(x.at / all));
+  const int64_t in = x.at - x.hk * all;
+  int lo = 0, hi = n - 1;      // the last item that begins at or before `in` and is not empty: the last one of equal beginnings
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (a.before[mid] * a.G <= in) lo = mid;
+    else hi = mid - 1;
+  }
+  x.item = uniform(lo);
+  const int64_t begin = a.before[x.item] * a.G, stop = a.before[x.item + 1] * a.G;
+  x.tiles = uniform((int)(stop - begin));
+  x.from = uniform((int)(in - begin));
+  const int64_t left = x.end - x.at;
+  x.to = uniform((int)min((int64_t)x.tiles, x.from + left));
+  x.at += x.to - x.from;
+  return true;
+}
+__device__ inline void share_of(const AttnArgs& a, int nkey, int wg, int wgs, Share& x) {
+  const int64_t all = a.before[a.B * nkey] * a.G * a.Hkv;
+  int64_t each = (all + wgs - 1) / wgs;
+  if (each < kLeastShare) each = kLeastShare;
+  x.at = min(all, each * wg);
+  x.end = min(all, x.at + each);
+}
+
 // bf16: the fourth operand of the pairs' products (g beside q, v beside k) stays in LDS, a wavefront's rows read by itself, since registers hold
 // the sums; fp32: 512 registers a lane hold it.
 template <typename E>
@@ -18,7 +126,7 @@ constexpr bool kRowsInLds = AttnElem<E>::size == 2;
 // sum_j P_j k_j is added up beside dq (the same fragments of K) and taken out at the end, and dk gets the better delta: dq of eight sequences
 // of 4096 was 2.7e-3 off without it, of which the rounding of dq itself is 1.7e-3.
 template <typename E, int DP, int BK>
-__global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dq_kernel(AttnArgs a) {
+__global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dq_kernel(AttnArgs a, int nkey) {
   using El = AttnElem<E>;
   using Frag = typename El::Frag;
   using Tile = AttnTile<E, DP, BK>;
@@ -30,6 +138,7 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dq_kernel(Att
   const uint32_t rbase = Tile::row_base(l), cbase = Tile::col_base(l);      // (of Rows too)
   char* const grows = lds + 2 * STAGE + w * Rows::BYTES;
   report_lengths(a);
+  if (nkey && !(blockIdx.x | blockIdx.y)) count_tiles(a, nkey);      // for the kernel that follows
   Work work;
   if (!attn_work(a.B * a.Hkv, a.nblk, work)) return;
   const int blk = a.nblk - 1 - work.in;
@@ -159,128 +268,133 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dq_kernel(Att
     }
 }
 
-// How dk and dv are cut: per key head the blocks of 128 keys, each with the queries that it reaches through its window, and for
-// the first tokens, which all later queries see, chunks of the queries behind those.  The rows of the first tokens are then sums of parts.
-struct KeyWork {
-  int nkey, nfirst, nchunk, rows;      // blocks; those with first tokens; chunks of queries; first tokens of a block that have parts
-  __host__ __device__ int items() const { return nkey + nfirst * nchunk; }
-};
-constexpr int kFarQueries = 512;
-
-// A wavefront holds 32 keys and their values; the workgroup's four walk the queries that see them, head by head, in tiles of BQ.  S and dP
+// A wavefront holds 32 keys and their values; the workgroup's four walk the queries that see them, head by head, in tiles of 32.  S and dP
 // have the queries along the accumulators' rows, so P and dS are operands of dV^T = g^T P and dK^T = Q^T dS as they lie.
-template <typename E, int DP, int BQ>
-__global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dkv_kernel(AttnArgs a, KeyWork kw) {
+template <typename E, int DP>
+__global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dkv_kernel(AttnArgs a, KeyShares sh) {
   using El = AttnElem<E>;
   using Frag = typename El::Frag;
+  constexpr int BQ = kQueryTile;
   using Tile = AttnTile<E, DP, BQ>;
-  using Rows = AttnTile<E, DP, 32>;
-  constexpr int KS = Tile::KS, QB = BQ / 32, DB = DP / 32, STAGE = 2 * Tile::BYTES + 2 * BQ * 4;
+  constexpr int KS = Tile::KS, DB = DP / 32, STAGE = 2 * Tile::BYTES + 2 * BQ * 4;
   extern __shared__ char lds[];
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t rbase = Tile::row_base(l), cbase = Tile::col_base(l);      // (of Rows too)
-  char* const vrows = lds + 2 * STAGE + w * Rows::BYTES;
-  Work work;
-  if (!attn_work(a.B * a.Hkv, kw.items(), work)) return;
-  const uint32_t bh = work.bh;
-  const int item = work.in, hk = uniform(bh % a.Hkv), b = uniform(bh / a.Hkv);
-  const bool far = item >= kw.nkey;
-  const int blk = far ? uniform((item - kw.nkey) / (uint32_t)kw.nchunk) : item, chunk = far ? uniform((item - kw.nkey) % (uint32_t)kw.nchunk) : 0;
-  const int lq = clamp_len(a.len_q, b, a.Tq), lk = clamp_len(a.len_k, b, a.Tk);
-  const int s0 = blk * 128, key0 = s0 + w * 32, key = key0 + (l & 31);
-  Frag k[KS], v[kRowsInLds<E> ? 1 : KS];
-  {
-    const char* ks_ = a.k.p + b * a.k.seq + (int64_t)key * a.k.slot + hk * a.k.head;
-    const char* vs_ = a.v.p + b * a.v.seq + (int64_t)key * a.v.slot + hk * a.v.head;
+  const uint32_t rbase = Tile::row_base(l), cbase = Tile::col_base(l);
+  char* const vrows = lds + 2 * STAGE + w * Tile::BYTES;
+  // consecutive shares go to one XCD
+  const int id = blockIdx.y * kAttnRow + blockIdx.x, wg = (id % 8) * (sh.wgs / 8) + id / 8;
+  if (id >= sh.wgs) return;
+  Share x;
+  if (sh.whole) {
+    if (wg >= a.B * a.Hkv * sh.nkey) return;
+    x.hk = wg % a.Hkv, x.item = wg / a.Hkv, x.from = 0, x.to = x.tiles = -1, x.at = x.end = 0;
+  } else {
+    share_of(a, sh.nkey, wg, sh.wgs, x);
+  }
+  for (bool first = true;; first = false) {
+    if (sh.whole ? !first : !next_piece(a, sh.nkey, x)) return;
+    const int b = uniform(x.item / (uint32_t)sh.nkey), s0 = uniform(x.item % (uint32_t)sh.nkey) * kKeyBlock, hk = x.hk;
+    const int lq = clamp_len(a.len_q, b, a.Tq), lk = clamp_len(a.len_k, b, a.Tk);
+    const KeyItem item = key_item(s0, lq, lk, a.window, a.sinks);
+    const int each = item.tiles(), from = x.from, n = sh.whole ? each * a.G : x.to - x.from;
+    const int key0 = s0 + w * 32, key = key0 + (l & 31), offset = lk - lq;
+    __syncthreads();      // the piece before is done with LDS
+    Frag k[KS], v[kRowsInLds<E> ? 1 : KS];
+    {
+      const char* ks_ = a.k.p + b * a.k.seq + (int64_t)key * a.k.slot + hk * a.k.head;
+      const char* vs_ = a.v.p + b * a.v.seq + (int64_t)key * a.v.slot + hk * a.v.head;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      const int d = 16 * ks + 8 * (l >> 5);
-      k[ks] = key < lk && d < a.D ? El::load(ks_ + d * El::size) : El::zero();
-      const Frag f = key < lk && d < a.D ? El::load(vs_ + d * El::size) : El::zero();
-      if constexpr (kRowsInLds<E>) Rows::put_row(vrows, rbase, ks, f);
-      else v[ks] = f;
+      for (int ks = 0; ks < KS; ++ks) {
+        const int d = 16 * ks + 8 * (l >> 5);
+        k[ks] = key < lk && d < a.D ? El::load(ks_ + d * El::size) : El::zero();
+        const Frag f = key < lk && d < a.D ? El::load(vs_ + d * El::size) : El::zero();
+        if constexpr (kRowsInLds<E>) Tile::put_row(vrows, rbase, ks, f);
+        else v[ks] = f;
+      }
     }
-  }
-  // queries from the first at the block's first key to the last whose window reaches its last one
-  const int offset = lk - lq, end_key = min(lk, s0 + 128) - 1;
-  int i0 = max(0, s0 - offset), i1 = (int)min((int64_t)lq, (int64_t)end_key + a.window - offset);
-  if (far) {
-    i0 = max(max(i0, i1), chunk * kFarQueries);
-    i1 = min(lq, (chunk + 1) * kFarQueries);
-  }
-  const int tiles = s0 < lk && i1 > i0 ? (i1 - i0 + BQ - 1) / BQ : 0, n = tiles * a.G;
+    // The tile that is loaded next: its head, its first query and the end of its run of queries.
+    int g = each ? uniform((uint32_t)from / (uint32_t)each) : 0, c = each ? uniform((uint32_t)from % (uint32_t)each) : 0, ni = 0, nend = 0;
+    auto place = [&]() {
+      const bool main = c < item.main;
+      ni = main ? item.i0 + c * BQ : item.far0 + (c - item.main) * BQ;
+      nend = main ? item.far0 : lq;
+    };
+    float end_next = 0.f, delta_next = 0.f;      // of the tile that is loaded next: one query a thread
+    auto load = [&](char* to) {
+      const int head = hk * a.G + g;
+      Tile::template load<4>(to, a.q.p + b * a.q.seq + head * a.q.head + ni * a.q.slot, (uint32_t)a.q.slot, nend - ni, a.D * El::size, w, l);
+      Tile::template load<4>(to + Tile::BYTES, a.g.p + b * a.g.seq + head * a.g.head + ni * a.g.slot, (uint32_t)a.g.slot, nend - ni,
+                             a.D * El::size, w, l);
+      if (threadIdx.x < BQ) {
+        const int qi = ni + threadIdx.x;
+        const int64_t at = ((int64_t)b * a.Hq + head) * a.Tq + qi;
+        const float lse = qi < nend ? a.lse[at] : -INFINITY;
+        end_next = lse == -INFINITY ? INFINITY : lse * kLog2e;
+        delta_next = qi < nend ? a.delta[at] : 0.f;
+      }
+    };
+    auto put = [&](char* to) {
+      if (threadIdx.x < BQ) {
+        float* const f = reinterpret_cast<float*>(to + 2 * Tile::BYTES);
+        f[threadIdx.x] = end_next;
+        f[BQ + threadIdx.x] = delta_next;
+      }
+    };
+    f32x16_t dk[DB], dv[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) dk[db][i] = dv[db][i] = 0.f;
 
-  float end_next = 0.f, delta_next = 0.f;      // of the tile that is loaded next: one query a thread
-  auto load = [&](int t, char* to) {
-    const int g = uniform((uint32_t)t / (uint32_t)tiles), i = i0 + uniform((uint32_t)t % (uint32_t)tiles) * BQ, head = hk * a.G + g;
-    Tile::template load<4>(to, a.q.p + b * a.q.seq + head * a.q.head + i * a.q.slot, (uint32_t)a.q.slot, i1 - i, a.D * El::size, w, l);
-    Tile::template load<4>(to + Tile::BYTES, a.g.p + b * a.g.seq + head * a.g.head + i * a.g.slot, (uint32_t)a.g.slot, i1 - i,
-                           a.D * El::size, w, l);
-    if (threadIdx.x < BQ) {
-      const int qi = i + threadIdx.x;
-      const int64_t at = ((int64_t)b * a.Hq + head) * a.Tq + qi;
-      const float lse = qi < i1 ? a.lse[at] : -INFINITY;
-      end_next = lse == -INFINITY ? INFINITY : lse * kLog2e;
-      delta_next = qi < i1 ? a.delta[at] : 0.f;
+    if (n) {
+      place();
+      load(lds);
+      put(lds);
     }
-  };
-  auto put = [&](char* to) {
-    if (threadIdx.x < BQ) {
-      float* const f = reinterpret_cast<float*>(to + 2 * Tile::BYTES);
-      f[threadIdx.x] = end_next;
-      f[BQ + threadIdx.x] = delta_next;
-    }
-  };
-  f32x16_t dk[DB], dv[DB];
-#pragma unroll
-  for (int db = 0; db < DB; ++db)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) dk[db][i] = dv[db][i] = 0.f;
-
-  if (n) {
-    load(0, lds);
-    put(lds);
-  }
-  for (int t = 0; t < n; ++t) {
-    char* const cur = lds + (t & 1) * STAGE;
-    char* const next = lds + ((t + 1) & 1) * STAGE;
-    __builtin_amdgcn_s_waitcnt(kWaitVm0);
-    __syncthreads();
-    if (t + 1 < n) load(t + 1, next);
-    const int i = i0 + uniform((uint32_t)t % (uint32_t)tiles) * BQ, rows = min(BQ, i1 - i);
-    const float* const end = reinterpret_cast<const float*>(cur + 2 * Tile::BYTES);
-    const float* const delta = end + BQ;
-    const int pmin = offset + i, pmax = offset + i + rows - 1;
-    if (!none_seen(key0, 32, pmin, pmax, a.window, a.sinks)) {
-      const bool part = rows < BQ || !all_seen(key0, 32, pmin, pmax, a.window, a.sinks);
-#pragma unroll
-      for (int qb = 0; qb < QB; ++qb) {
+    for (int t = 0; t < n; ++t) {
+      char* const cur = lds + (t & 1) * STAGE;
+      char* const next = lds + ((t + 1) & 1) * STAGE;
+      __builtin_amdgcn_s_waitcnt(kWaitVm0);
+      __syncthreads();
+      // (hidden from the compiler, which would keep every address of the loop in a register of its own)
+      uint32_t rb = rbase, cb = cbase;
+      asm volatile("" : "+v"(rb), "+v"(cb));
+      const int rows = min(BQ, nend - ni), pmin = offset + ni, pmax = pmin + rows - 1;
+      if (t + 1 < n) {
+        if (++c == each) c = 0, ++g;
+        place();
+        load(next);
+      }
+      const float* const end = reinterpret_cast<const float*>(cur + 2 * Tile::BYTES);
+      const float* const delta = end + BQ;
+      if (!none_seen(key0, 32, pmin, pmax, a.window, a.sinks)) {
+        const bool part = rows < BQ || !all_seen(key0, 32, pmin, pmax, a.window, a.sinks);
         f32x16_t s, dp;
 #pragma unroll
-        for (int x = 0; x < 16; ++x) s[x] = dp[x] = 0.f;
+        for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0.f;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-          El::mma(s, Tile::row_frag(cur, rbase, qb, ks), k[ks]);
-          if constexpr (kRowsInLds<E>) El::mma(dp, Tile::row_frag(cur + Tile::BYTES, rbase, qb, ks), Rows::row_frag(vrows, rbase, 0, ks));
-          else El::mma(dp, Tile::row_frag(cur + Tile::BYTES, rbase, qb, ks), v[ks]);
+          El::mma(s, Tile::row_frag(cur, rb, 0, ks), k[ks]);
+          if constexpr (kRowsInLds<E>) El::mma(dp, Tile::row_frag(cur + Tile::BYTES, rb, 0, ks), Tile::row_frag(vrows, rb, 0, ks));
+          else El::mma(dp, Tile::row_frag(cur + Tile::BYTES, rb, 0, ks), v[ks]);
         }
         float pr[16], ds[16];
 #pragma unroll
-        for (int x = 0; x < 16; ++x) {
-          const int row = qb * 32 + acc_row(x, l);
-          pr[x] = __builtin_amdgcn_exp2f(fmaf(s[x], a.scale2, -end[row]));
-          ds[x] = pr[x] * (dp[x] - delta[row]);
+        for (int i = 0; i < 16; ++i) {
+          const int row = acc_row(i, l);
+          pr[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.scale2, -end[row]));
+          ds[i] = pr[i] * (dp[i] - delta[row]);
         }
         if (part) {
           // row c sees the key from position pmin + c on, to the end or to the last one whose window reaches it
-          const int lane = 4 * (l >> 5), from = key - pmin - lane;
-          const int to = (key < a.sinks ? rows - 1 : min(rows - 1, key + a.window - 1 - pmin)) - lane;
+          const int lane = 4 * (l >> 5), low = key - pmin - lane;
+          const int high = (key < a.sinks ? rows - 1 : min(rows - 1, key + a.window - 1 - pmin)) - lane;
 #pragma unroll
-          for (int x = 0; x < 16; ++x) {
-            const int c = qb * 32 + acc_row(x, 0);
-            const bool yes = (c >= from) & (c <= to);
-            pr[x] = yes ? pr[x] : 0.f;
-            ds[x] = yes ? ds[x] : 0.f;
+          for (int i = 0; i < 16; ++i) {
+            const int c = acc_row(i, 0);
+            const bool yes = (c >= low) & (c <= high);
+            pr[i] = yes ? pr[i] : 0.f;
+            ds[i] = yes ? ds[i] : 0.f;
           }
         }
 #pragma unroll
@@ -288,107 +402,121 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dkv_kernel(At
           const Frag pf = El::of(pr + 8 * h), sf = El::of(ds + 8 * h);
 #pragma unroll
           for (int db = 0; db < DB; ++db) {
-            El::mma(dv[db], Tile::col_frag(cur + Tile::BYTES, cbase, db, qb * 2 + h), pf);
-            El::mma(dk[db], Tile::col_frag(cur, cbase, db, qb * 2 + h), sf);
+            El::mma(dv[db], Tile::col_frag(cur + Tile::BYTES, cb, db, h), pf);
+            El::mma(dk[db], Tile::col_frag(cur, cb, db, h), sf);
           }
         }
       }
+      if (t + 1 < n) put(next);
     }
-    if (t + 1 < n) put(next);
-  }
-  if (key >= a.Tk) return;
-  const bool parts = blk < kw.nfirst && key - s0 < kw.rows && key < a.sinks;
-  if (far && !parts) return;
-  if (parts) {
-    float* const to = a.part + (((int64_t)(bh * kw.nfirst + blk) * (kw.nchunk + 1) + (far ? chunk + 1 : 0)) * kw.rows + (key - s0)) * (2 * DP);
+    if (!sh.whole && (x.from > 0 || x.to < x.tiles)) {
+      // slot 0: the end of an item, or its middle; slot 1: the beginning of one
+      float* const to = a.part + ((int64_t)(2 * wg + (x.from > 0 ? 0 : 1)) * kKeyBlock + w * 32 + (l & 31)) * (2 * DP);
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          const int d = db * 32 + acc_row(i, l);
+          *reinterpret_cast<f32x4_t*>(to + d) = f32x4_t{dk[db][i], dk[db][i + 1], dk[db][i + 2], dk[db][i + 3]};
+          *reinterpret_cast<f32x4_t*>(to + DP + d) = f32x4_t{dv[db][i], dv[db][i + 1], dv[db][i + 2], dv[db][i + 3]};
+        }
+      continue;
+    }
+    if (key >= a.Tk) continue;
+    char* const ok = a.dk.p + b * a.dk.seq + (int64_t)key * a.dk.slot + hk * a.dk.head;
+    char* const ov = a.dv.p + b * a.dv.seq + (int64_t)key * a.dv.slot + hk * a.dv.head;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
       for (int i = 0; i < 16; i += 4) {
         const int d = db * 32 + acc_row(i, l);
-        *reinterpret_cast<f32x4_t*>(to + d) = f32x4_t{dk[db][i], dk[db][i + 1], dk[db][i + 2], dk[db][i + 3]};
-        *reinterpret_cast<f32x4_t*>(to + DP + d) = f32x4_t{dv[db][i], dv[db][i + 1], dv[db][i + 2], dv[db][i + 3]};
+        if (d >= a.D) continue;
+        El::store4(ok + d * El::size, dk[db][i] * a.scale, dk[db][i + 1] * a.scale, dk[db][i + 2] * a.scale, dk[db][i + 3] * a.scale);
+        El::store4(ov + d * El::size, dv[db][i], dv[db][i + 1], dv[db][i + 2], dv[db][i + 3]);
       }
-    return;
   }
-  char* const ok = a.dk.p + b * a.dk.seq + (int64_t)key * a.dk.slot + hk * a.dk.head;
-  char* const ov = a.dv.p + b * a.dv.seq + (int64_t)key * a.dv.slot + hk * a.dv.head;
-#pragma unroll
-  for (int db = 0; db < DB; ++db)
-#pragma unroll
-    for (int i = 0; i < 16; i += 4) {
-      const int d = db * 32 + acc_row(i, l);
-      if (d >= a.D) continue;
-      El::store4(ok + d * El::size, dk[db][i] * a.scale, dk[db][i + 1] * a.scale, dk[db][i + 2] * a.scale, dk[db][i + 3] * a.scale);
-      El::store4(ov + d * El::size, dv[db][i], dv[db][i + 1], dv[db][i + 2], dv[db][i + 3]);
-    }
 }
 
-// Rows of the first tokens: a thread adds up four channels of one row's parts, in order.
+// Items that were cut: the workgroup whose share has the beginning adds up the parts, which lie with the shares that follow.  And blocks of
+// keys without any tile, which no share has, become zeros (workgroups from sh.wgs on, one for each block of a key head).
 template <typename E, int DP>
-__global__ __launch_bounds__(256) void attn_first_kernel(AttnArgs a, KeyWork kw) {
+__global__ __launch_bounds__(256) void attn_parts_kernel(AttnArgs a, KeyShares sh) {
   using El = AttnElem<E>;
   constexpr int UNITS = 2 * DP / 4;
-  const int64_t id = ((int64_t)blockIdx.y * kAttnRow + blockIdx.x) * 256 + threadIdx.x, row = id / UNITS;
-  const int c = (int)(id % UNITS) * 4, keys = kw.nfirst * kw.rows;
-  const int64_t bh = row / keys;
-  if (bh >= (int64_t)a.B * a.Hkv) return;
-  const int blk = (int)(row % keys) / kw.rows, in = (int)(row % keys) % kw.rows, key = blk * 128 + in;
-  if (key >= a.sinks || key >= a.Tk) return;
-  const float* at = a.part + ((bh * kw.nfirst + blk) * (kw.nchunk + 1) * kw.rows + in) * (2 * DP) + c;
-  f32x4_t sum = f32x4_t{0, 0, 0, 0};
-  for (int i = 0; i <= kw.nchunk; ++i, at += (int64_t)kw.rows * 2 * DP) sum += *reinterpret_cast<const f32x4_t*>(at);
-  const bool value = c >= DP;
-  const int d = value ? c - DP : c, b = (int)(bh / a.Hkv), hk = (int)(bh % a.Hkv);
-  if (d >= a.D) return;
-  if (!value) sum *= a.scale;
-  const AttnTensor& t = value ? a.dv : a.dk;
-  El::store4(t.p + b * t.seq + (int64_t)key * t.slot + hk * t.head + d * El::size, sum.x, sum.y, sum.z, sum.w);
+  const int id = blockIdx.y * kAttnRow + blockIdx.x;
+  if (id >= sh.wgs) {
+    const int x = id - sh.wgs, item = x / a.Hkv, hk = x % a.Hkv, b = item / sh.nkey, s0 = item % sh.nkey * kKeyBlock;
+    if (item >= a.B * sh.nkey || a.before[item + 1] != a.before[item]) return;
+    for (int y = threadIdx.x; y < kKeyBlock * UNITS; y += 256) {
+      const int key = s0 + y / UNITS, c = y % UNITS * 4, d = c >= DP ? c - DP : c;
+      if (key >= a.Tk || d >= a.D) continue;
+      const AttnTensor& t = c >= DP ? a.dv : a.dk;
+      El::store4(t.p + b * t.seq + (int64_t)key * t.slot + hk * t.head + d * El::size, 0.f, 0.f, 0.f, 0.f);
+    }
+    return;
+  }
+  // the last piece of this share
+  Share x, y;
+  share_of(a, sh.nkey, id, sh.wgs, x);
+  if (x.at >= x.end) return;
+  y = x;
+  y.at = x.end - 1;
+  next_piece(a, sh.nkey, y);
+  // the item's first tile is in this share, its last one is not
+  const int64_t begin = x.end - 1 - y.from;
+  if (begin < x.at || begin + y.tiles <= x.end) return;
+  const int64_t each = x.end - x.at;      // of the shares that follow too, less the last one
+  const int parts = (int)((begin + y.tiles - x.end + each - 1) / each);
+  const int b = y.item / sh.nkey, s0 = y.item % sh.nkey * kKeyBlock;
+  for (int u = threadIdx.x; u < kKeyBlock * UNITS; u += 256) {
+    const int key = s0 + u / UNITS, c = u % UNITS * 4, d = c >= DP ? c - DP : c;
+    if (key >= a.Tk || d >= a.D) continue;
+    const int64_t in = (int64_t)(u / UNITS) * (2 * DP) + c, slot = (int64_t)kKeyBlock * 2 * DP;
+    f32x4_t sum = *reinterpret_cast<const f32x4_t*>(a.part + (2 * (int64_t)id + 1) * slot + in);
+    for (int z = 1; z <= parts; ++z) sum += *reinterpret_cast<const f32x4_t*>(a.part + 2 * (int64_t)(id + z) * slot + in);
+    if (c < DP) sum *= a.scale;
+    const AttnTensor& t = c >= DP ? a.dv : a.dk;
+    El::store4(t.p + b * t.seq + (int64_t)key * t.slot + y.hk * t.head + d * El::size, sum.x, sum.y, sum.z, sum.w);
+  }
 }
 
-KeyWork key_work(int Tq, int Tk, int window, int sinks) {
-  KeyWork w{};
-  w.nkey = (Tk + 127) / 128;
-  if (window == 0 || window >= Tk || sinks == 0) return w;
-  sinks = sinks < Tk ? sinks : Tk;
-  w.nfirst = (sinks + 127) / 128;
-  w.nchunk = (Tq + kFarQueries - 1) / kFarQueries;
-  w.rows = sinks < 128 ? sinks : 128;
-  return w;
-}
+int resident(const attn_desc* d) { return device_compute_units() * (d->dtype == LMHEAD_BF16 ? 2 : 1); }
 
 template <typename E, int DP>
-hipError_t bwd(const KeyWork& kw, AttnArgs a, hipStream_t s) {
+hipError_t bwd(const KeyShares& sh, AttnArgs a, hipStream_t s) {
   constexpr int BK = 32, fixed = kRowsInLds<E> ? 4 * AttnTile<E, DP, 32>::BYTES : 0;
   constexpr auto dq = attn_dq_kernel<E, DP, BK>;
-  constexpr auto dkv = attn_dkv_kernel<E, DP, BK>;
+  constexpr auto dkv = attn_dkv_kernel<E, DP>;
   const int bytes = 4 * AttnTile<E, DP, BK>::BYTES + fixed, more = bytes + 4 * BK * 4;
   hipError_t e = allow_lds<dq>(bytes);
   if (e == hipSuccess) e = allow_lds<dkv>(more);
   if (e != hipSuccess) return e;
   a.nblk = (int)(((int64_t)a.Tq * a.G + 127) / 128);
-  dq<<<attn_grid(attn_wgs((int64_t)a.B * a.Hkv, a.nblk)), 256, bytes, s>>>(a);
+  dq<<<attn_grid(attn_wgs((int64_t)a.B * a.Hkv, a.nblk)), 256, bytes, s>>>(a, sh.whole ? 0 : sh.nkey);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  dkv<<<attn_grid(attn_wgs((int64_t)a.B * a.Hkv, kw.items())), 256, more, s>>>(a, kw);
+  dkv<<<attn_grid(sh.wgs), 256, more, s>>>(a, sh);
   e = hipGetLastError();
-  if (e != hipSuccess || !kw.nfirst) return e;
-  const int64_t threads = (int64_t)a.B * a.Hkv * kw.nfirst * kw.rows * (2 * DP / 4);
-  attn_first_kernel<E, DP><<<attn_grid((threads + 255) / 256), 256, 0, s>>>(a, kw);
+  if (e != hipSuccess || sh.whole) return e;
+  attn_parts_kernel<E, DP><<<attn_grid((int64_t)sh.wgs + (int64_t)a.B * a.Hkv * sh.nkey), 256, 0, s>>>(a, sh);
   return hipGetLastError();
 }
 
 }  // namespace
 
-size_t attn_first_bytes(const attn_desc* d) {
-  const KeyWork w = key_work(d->Tq, d->Tk, d->window, d->sinks);
-  return (size_t)d->B * d->Hkv * w.nfirst * (w.nchunk + 1) * w.rows * 2 * (d->D <= 64 ? 64 : 128) * sizeof(float);
+size_t attn_before_bytes(const attn_desc* d) {
+  const KeyShares k = key_shares(d, resident(d));
+  return k.whole ? 0 : round_up(((size_t)d->B * k.nkey + 1) * sizeof(int64_t), 256);
+}
+size_t attn_parts_bytes(const attn_desc* d) {
+  const KeyShares k = key_shares(d, resident(d));
+  return k.whole ? 0 : (size_t)k.wgs * 2 * kKeyBlock * 2 * (d->D <= 64 ? 64 : 128) * sizeof(float);
 }
 
 hipError_t launch_attn_bwd(const attn_desc* d, const AttnPlan& p, AttnArgs& a, hipStream_t s) {
-  const KeyWork w = key_work(d->Tq, d->Tk, d->window, d->sinks);
-  if (d->dtype == LMHEAD_BF16) return p.DP == 64 ? bwd<bf16_tag, 64>(w, a, s) : bwd<bf16_tag, 128>(w, a, s);
-  return p.DP == 64 ? bwd<f32_tag, 64>(w, a, s) : bwd<f32_tag, 128>(w, a, s);
+  const KeyShares k = key_shares(d, resident(d));
+  if (d->dtype == LMHEAD_BF16) return p.DP == 64 ? bwd<bf16_tag, 64>(k, a, s) : bwd<bf16_tag, 128>(k, a, s);
+  return p.DP == 64 ? bwd<f32_tag, 64>(k, a, s) : bwd<f32_tag, 128>(k, a, s);
 }
 
 }  // namespace lmhead

@@ -41,6 +41,7 @@ struct AttnArgs {
   // backward
   AttnTensor g, dq, dk, dv;
   float* delta;             // [b][head][query]
+  int64_t* before;          // [b][block of keys]: tiles of the items before
 };
 
 constexpr int kFewRows = 32;
@@ -60,7 +61,8 @@ AttnPlan attn_plan(const attn_desc* d, bool cache4);
 hipError_t launch_attn_few(const attn_desc* d, const AttnPlan& p, const AttnArgs& a, hipStream_t s);   // at most kFewRows rows
 hipError_t launch_attn_fwd(const attn_desc* d, const AttnPlan& p, AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_weight(const attn_desc* d, const AttnPlan& p, AttnArgs& a, hipStream_t s);
-size_t attn_first_bytes(const attn_desc* d);      // of the parts of dk and dv of the first tokens
+size_t attn_before_bytes(const attn_desc* d);     // how dk and dv are cut: counts of tiles
+size_t attn_parts_bytes(const attn_desc* d);      // and the sums of items that were cut
 hipError_t launch_attn_bwd(const attn_desc* d, const AttnPlan& p, AttnArgs& a, hipStream_t s);
 hipError_t launch_kv4_store(const attn_desc* d, const AttnArgs& a, uint8_t* const* cache, hipStream_t s);
 hipError_t launch_evict(const evict_desc& d, const cache_plane* planes, int count, float* weight, const int32_t* len, int32_t* len_out,
@@ -190,9 +192,10 @@ struct AttnElem<f32_tag> {
 
 typedef __attribute__((address_space(3))) char lds_char;
 
-// ROWS rows of DP values in LDS.  A row is CH chunks of 16 bytes; chunk c of row r sits at position c ^ swz(r) of its row.  The banks are 256
-// bytes wide: the swizzle spreads a chunk of sixteen consecutive rows (reads along rows) and a pair of chunks of eight rows (transposing
-// reads across them) over all of them.
+// ROWS rows of DP values in LDS.  A row is CH chunks of 16 bytes; chunk c of row r sits at position c ^ swz(r) of its row.  A read along rows
+// takes a chunk of eight consecutive rows at a time, which then lie in different 16-byte banks (of 128 bytes, and sixteen rows in those of 256);
+// a transposing read takes 64 bytes of four rows (32 of eight where blocks are sixteen wide), which cover 256 bytes.  (With pairs of chunks
+// spread instead, the transposing reads met twice on every bank: a third of the forward's LDS cycles.)
 template <typename E, int DP, int ROWS>
 struct AttnTile {
   using El = AttnElem<E>;
@@ -204,7 +207,8 @@ struct AttnTile {
   static_assert(64 % CH == 0 && BYTES % 1024 == 0, "a load instruction fills whole rows");
 
   __device__ static inline int swz(int r) {
-    return ((r & 3) << 1) | ((r >> 2) & 1) | (CH == 8 ? 0 : r & 8);
+    const int r0 = r & 1, r1 = (r >> 1) & 1, r2 = (r >> 2) & 1, r3 = (r >> 3) & 1;
+    return CH == 8 ? r1 << 2 | r2 << 1 | (r0 ^ r3) : (r1 ^ r3) << 3 | r0 << 2 | r2 << 1 | r1;
   }
   __device__ static inline int at(int r, int c) { return r * ROW + ((c ^ swz(r)) << 4); }
 
@@ -255,7 +259,7 @@ struct AttnTile {
   __device__ static inline uint32_t col_base(int l) {
     const int h = l >> 5, t = l & 15;
     if constexpr (El::size == 2) return (4 * h + (t >> 2)) * ROW + (((((l >> 4) & 1) * 2 + ((t & 3) >> 1)) ^ swz(4 * h + (t >> 2))) << 4) + 8 * (t & 1);
-    else return 4 * h * ROW + ((((l & 31) >> 2) ^ h) << 4) + 4 * (l & 3);
+    else return 4 * h * ROW + ((((l & 31) >> 2) ^ swz(4 * h)) << 4) + 4 * (l & 3);
   }
   __device__ static inline Frag col_frag(const char* lds, uint32_t base, int db, int s) {
     if constexpr (El::size == 2) {
@@ -263,7 +267,7 @@ struct AttnTile {
       u32x4_t f;
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
-        const uint32_t at = (base ^ ((db & 1) << 6)) + (CH == 8 ? 0 : ((db >> 1) ^ p) << 7) + (16 * s + 8 * p) * ROW;
+        const uint32_t at = (base ^ (CH == 8 ? db << 6 | p << 4 : (db ^ p << 1) << 6)) + (16 * s + 8 * p) * ROW;
         const u32x2_t v = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tptr_t)(lds + at)));
         f[2 * p] = v.x;
         f[2 * p + 1] = v.y;
@@ -273,7 +277,8 @@ struct AttnTile {
       Frag f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const uint32_t at = (base ^ ((j & 3) << 5)) + ((db ^ (j >> 2)) << 7) + (16 * s + 8 * (j >> 2) + (j & 3)) * ROW;
+        const int row = 8 * (j >> 2) + (j & 3);
+        const uint32_t at = (base ^ (swz(row) & 7) << 4) + ((db ^ swz(row) >> 3) << 7) + (16 * s + row) * ROW;
         f.x[j >> 2][j & 3] = *reinterpret_cast<const float*>(lds + at);
       }
       return f;
@@ -302,7 +307,7 @@ struct AttnTile {
       Frag f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const uint32_t at = (base ^ ((j & 3) << 5) ^ (db << 6)) + (32 * s + 16 * (j >> 2) + (j & 3)) * ROW;
+        const uint32_t at = (base ^ (swz(j & 3) ^ db << 2) << 4) + (32 * s + 16 * (j >> 2) + (j & 3)) * ROW;
         f.x[j >> 2][j & 3] = *reinterpret_cast<const float*>(lds + at);
       }
       return f;
