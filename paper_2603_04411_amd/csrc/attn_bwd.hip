@@ -368,7 +368,6 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dkv_kernel(At
       const float* const end = reinterpret_cast<const float*>(cur + 2 * Tile::BYTES);
       const float* const delta = end + BQ;
       if (!none_seen(key0, 32, pmin, pmax, a.window, a.sinks)) {
-        const bool part = rows < BQ || !all_seen(key0, 32, pmin, pmax, a.window, a.sinks);
         f32x16_t s, dp;
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0.f;
@@ -379,13 +378,15 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dkv_kernel(At
           else El::mma(dp, Tile::row_frag(cur + Tile::BYTES, rb, 0, ks), v[ks]);
         }
         float pr[16], ds[16];
+        const f32x4_t* const ends = reinterpret_cast<const f32x4_t*>(end + 4 * (l >> 5));
+        const f32x4_t* const deltas = reinterpret_cast<const f32x4_t*>(delta + 4 * (l >> 5));
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const int row = acc_row(i, l);
-          pr[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.scale2, -end[row]));
-          ds[i] = pr[i] * (dp[i] - delta[row]);
+          pr[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.scale2, -ends[2 * (i >> 2)][i & 3]));
+          ds[i] = pr[i] * (dp[i] - deltas[2 * (i >> 2)][i & 3]);
         }
-        if (part) {
+        //SCHED1
+        if (rows < BQ || !all_seen(key0, 32, pmin, pmax, a.window, a.sinks)) {
           // row c sees the key from position pmin + c on, to the end or to the last one whose window reaches it
           const int lane = 4 * (l >> 5), low = key - pmin - lane;
           const int high = (key < a.sinks ? rows - 1 : min(rows - 1, key + a.window - 1 - pmin)) - lane;
@@ -397,15 +398,15 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dkv_kernel(At
             ds[i] = yes ? ds[i] : 0.f;
           }
         }
+        const Frag pf[2] = {El::of(pr), El::of(pr + 8)}, sf[2] = {El::of(ds), El::of(ds + 8)};
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const Frag pf = El::of(pr + 8 * h), sf = El::of(ds + 8 * h);
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int db = 0; db < DB; ++db) {
-            El::mma(dv[db], Tile::col_frag(cur + Tile::BYTES, cb, db, h), pf);
-            El::mma(dk[db], Tile::col_frag(cur, cb, db, h), sf);
+            El::mma(dv[db], Tile::col_frag(cur + Tile::BYTES, cb, db, h), pf[h]);
+            El::mma(dk[db], Tile::col_frag(cur, cb, db, h), sf[h]);
           }
-        }
+        //SCHED2
       }
       if (t + 1 < n) put(next);
     }
@@ -443,9 +444,10 @@ template <typename E, int DP>
 __global__ __launch_bounds__(256) void attn_parts_kernel(AttnArgs a, KeyShares sh) {
   using El = AttnElem<E>;
   constexpr int UNITS = 2 * DP / 4;
-  const int id = blockIdx.y * kAttnRow + blockIdx.x;
+  constexpr int PARTS = 4;      // workgroups of a cut item
+  const int wid = blockIdx.y * kAttnRow + blockIdx.x, id = wid / PARTS;
   if (id >= sh.wgs) {
-    const int x = id - sh.wgs, item = x / a.Hkv, hk = x % a.Hkv, b = item / sh.nkey, s0 = item % sh.nkey * kKeyBlock;
+    const int x = wid - PARTS * sh.wgs, item = x / a.Hkv, hk = x % a.Hkv, b = item / sh.nkey, s0 = item % sh.nkey * kKeyBlock;
     if (item >= a.B * sh.nkey || a.before[item + 1] != a.before[item]) return;
     for (int y = threadIdx.x; y < kKeyBlock * UNITS; y += 256) {
       const int key = s0 + y / UNITS, c = y % UNITS * 4, d = c >= DP ? c - DP : c;
@@ -468,7 +470,8 @@ __global__ __launch_bounds__(256) void attn_parts_kernel(AttnArgs a, KeyShares s
   const int64_t each = x.end - x.at;      // of the shares that follow too, less the last one
   const int parts = (int)((begin + y.tiles - x.end + each - 1) / each);
   const int b = y.item / sh.nkey, s0 = y.item % sh.nkey * kKeyBlock;
-  for (int u = threadIdx.x; u < kKeyBlock * UNITS; u += 256) {
+#pragma unroll 4
+  for (int u = wid % PARTS * (kKeyBlock / PARTS * UNITS) + threadIdx.x; u < (wid % PARTS + 1) * (kKeyBlock / PARTS * UNITS); u += 256) {
     const int key = s0 + u / UNITS, c = u % UNITS * 4, d = c >= DP ? c - DP : c;
     if (key >= a.Tk || d >= a.D) continue;
     const int64_t in = (int64_t)(u / UNITS) * (2 * DP) + c, slot = (int64_t)kKeyBlock * 2 * DP;
@@ -498,7 +501,7 @@ hipError_t bwd(const KeyShares& sh, AttnArgs a, hipStream_t s) {
   dkv<<<attn_grid(sh.wgs), 256, more, s>>>(a, sh);
   e = hipGetLastError();
   if (e != hipSuccess || sh.whole) return e;
-  attn_parts_kernel<E, DP><<<attn_grid((int64_t)sh.wgs + (int64_t)a.B * a.Hkv * sh.nkey), 256, 0, s>>>(a, sh);
+  attn_parts_kernel<E, DP><<<attn_grid(4 * (int64_t)sh.wgs + (int64_t)a.B * a.Hkv * sh.nkey), 256, 0, s>>>(a, sh);
   return hipGetLastError();
 }
 
