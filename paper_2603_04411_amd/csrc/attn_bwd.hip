@@ -1,5 +1,6 @@
 // Backward of attention over a window and a few first tokens: dq by blocks of queries, then dk and dv by blocks of keys, each recomputing
-// P from the logits and lse.  Seven products (bf16: eight) instead of the five that one pass over the pairs would take, and no atomics.
+// P from the logits and lse.  Seven products instead of the five that one pass over the pairs would take, and no atomics; with bf16 storage two
+// more in dq (and one in dk of few queries), for what rounding dS and out would cost.
 #include "attn_common.h"
 
 namespace lmhead {
@@ -30,6 +31,10 @@ __host__ __device__ inline KeyItem key_item(int s0, int lq, int lk, int window, 
   if (s0 < sinks && lq > x.far0) x.far = (lq - x.far0 + kQueryTile - 1) / kQueryTile;
   return x;
 }
+
+// Up to so many queries dS goes into dk with sixteen bits instead of eight: over many queries its rounding leaves dk 1.41 times as far off as
+// the rounding of dk alone, whatever the input; over few it depends on the few that carry weight (1.7 seen).
+constexpr int kFineQueries = 512;
 
 // How many workgroups there are, and whether each has one item (short ones are not cut).
 struct KeyShares {
@@ -123,8 +128,9 @@ constexpr bool kRowsInLds = AttnElem<E>::size == 2;
 //
 // delta = <g, out> carries the rounding of out.  Where few keys hold the weight that error is not small beside dP - delta, and its part of dq,
 // the error times sum_j P_j k_j, does not average out.  But sum_j dS_j = sum_j P_j dP_j - delta is exactly that error, so with bf16 storage
-// sum_j P_j k_j is added up beside dq (the same fragments of K) and taken out at the end, and dk gets the better delta: dq of eight sequences
-// of 4096 was 2.7e-3 off without it, of which the rounding of dq itself is 1.7e-3.
+// sum_j P_j k_j is added up beside dq (the same fragments of K) and taken out at the end, and dk gets the better delta.  And dS, whose few
+// large values carry dq, goes into it as a sum of two bf16 numbers.  dq of eight sequences of 4096, relative to 64 bits: 2.7e-3 off without
+// either, 2.4e-3 with the first, XXX with both; the rounding of dq itself is 1.7e-3.
 template <typename E, int DP, int BK>
 __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dq_kernel(AttnArgs a, int nkey) {
   using El = AttnElem<E>;
@@ -150,7 +156,7 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dq_kernel(Att
   const bool in = qi < a.Tq;
   const int p = qi < lq ? lk - lq + qi : -1;
   const float lse = p >= 0 ? a.lse[((int64_t)b * a.Hq + head) * a.Tq + qi] : -INFINITY;
-  const float end = lse == -INFINITY ? INFINITY : lse * kLog2e;
+  const Ends end(lse);
   Frag q[KS], g[kRowsInLds<E> ? 1 : KS];
   float delta = 0.f;
   {
@@ -219,7 +225,9 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dq_kernel(Att
       float e[16], ds[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        e[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.scale2, -end));
+        float x = fmaf(s[i], a.scale2, -end.a);
+        if constexpr (El::size == 4) x -= end.b;
+        e[i] = __builtin_amdgcn_exp2f(x);
         ds[i] = e[i] * (dp[i] - delta);
       }
       if (part) {
@@ -237,14 +245,14 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dq_kernel(Att
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const Frag f = El::of(ds + 8 * h);
-        Frag pf;
-        if constexpr (kFix) pf = El::of(e + 8 * h);
+        Frag f, low, pf;
+        if constexpr (kFix) El::split(ds + 8 * h, f, low), pf = El::of(e + 8 * h);
+        else f = El::of(ds + 8 * h);
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
           const Frag kf = Tile::col_frag(cur, cbase, db, kb * 2 + h);
           El::mma(dq[db], kf, f);
-          if constexpr (kFix) El::mma(mean[db], kf, pf);
+          if constexpr (kFix) El::mma(dq[db], kf, low), El::mma(mean[db], kf, pf);
         }
       }
     }
@@ -270,13 +278,13 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dq_kernel(Att
 
 // A wavefront holds 32 keys and their values; the workgroup's four walk the queries that see them, head by head, in tiles of 32.  S and dP
 // have the queries along the accumulators' rows, so P and dS are operands of dV^T = g^T P and dK^T = Q^T dS as they lie.
-template <typename E, int DP>
+template <typename E, int DP, bool kFine>
 __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dkv_kernel(AttnArgs a, KeyShares sh) {
   using El = AttnElem<E>;
   using Frag = typename El::Frag;
   constexpr int BQ = kQueryTile;
   using Tile = AttnTile<E, DP, BQ>;
-  constexpr int KS = Tile::KS, DB = DP / 32, STAGE = 2 * Tile::BYTES + 2 * BQ * 4;
+  constexpr int KS = Tile::KS, DB = DP / 32, STAGE = 2 * Tile::BYTES + 3 * BQ * 4;
   extern __shared__ char lds[];
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t rbase = Tile::row_base(l), cbase = Tile::col_base(l);
@@ -319,7 +327,7 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dkv_kernel(At
       ni = main ? item.i0 + c * BQ : item.far0 + (c - item.main) * BQ;
       nend = main ? item.far0 : lq;
     };
-    float end_next = 0.f, delta_next = 0.f;      // of the tile that is loaded next: one query a thread
+    float end_next = 0.f, low_next = 0.f, delta_next = 0.f;      // of the tile that is loaded next: one query a thread
     auto load = [&](char* to) {
       const int head = hk * a.G + g;
       Tile::template load<4>(to, a.q.p + b * a.q.seq + head * a.q.head + ni * a.q.slot, (uint32_t)a.q.slot, nend - ni, a.D * El::size, w, l);
@@ -329,7 +337,8 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dkv_kernel(At
         const int qi = ni + threadIdx.x;
         const int64_t at = ((int64_t)b * a.Hq + head) * a.Tq + qi;
         const float lse = qi < nend ? a.lse[at] : -INFINITY;
-        end_next = lse == -INFINITY ? INFINITY : lse * kLog2e;
+        const Ends e(lse);
+        end_next = e.a, low_next = e.b;
         delta_next = qi < nend ? a.delta[at] : 0.f;
       }
     };
@@ -338,6 +347,7 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dkv_kernel(At
         float* const f = reinterpret_cast<float*>(to + 2 * Tile::BYTES);
         f[threadIdx.x] = end_next;
         f[BQ + threadIdx.x] = delta_next;
+        if constexpr (El::size == 4) f[2 * BQ + threadIdx.x] = low_next;
       }
     };
     f32x16_t dk[DB], dv[DB];
@@ -382,10 +392,11 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dkv_kernel(At
         const f32x4_t* const deltas = reinterpret_cast<const f32x4_t*>(delta + 4 * (l >> 5));
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          pr[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.scale2, -ends[2 * (i >> 2)][i & 3]));
+          float x = fmaf(s[i], a.scale2, -ends[2 * (i >> 2)][i & 3]);
+          if constexpr (El::size == 4) x -= end[2 * BQ + acc_row(i, l)];
+          pr[i] = __builtin_amdgcn_exp2f(x);
           ds[i] = pr[i] * (dp[i] - deltas[2 * (i >> 2)][i & 3]);
         }
-        //SCHED1
         if (rows < BQ || !all_seen(key0, 32, pmin, pmax, a.window, a.sinks)) {
           // row c sees the key from position pmin + c on, to the end or to the last one whose window reaches it
           const int lane = 4 * (l >> 5), low = key - pmin - lane;
@@ -398,15 +409,22 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dkv_kernel(At
             ds[i] = yes ? ds[i] : 0.f;
           }
         }
-        const Frag pf[2] = {El::of(pr), El::of(pr + 8)}, sf[2] = {El::of(ds), El::of(ds + 8)};
+        const Frag pf[2] = {El::of(pr), El::of(pr + 8)};
+        Frag sf[2], low[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if constexpr (kFine) El::split(ds + 8 * h, sf[h], low[h]);
+          else sf[h] = El::of(ds + 8 * h);
+        }
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int db = 0; db < DB; ++db) {
             El::mma(dv[db], Tile::col_frag(cur + Tile::BYTES, cb, db, h), pf[h]);
-            El::mma(dk[db], Tile::col_frag(cur, cb, db, h), sf[h]);
+            const Frag qf = Tile::col_frag(cur, cb, db, h);
+            El::mma(dk[db], qf, sf[h]);
+            if constexpr (kFine) El::mma(dk[db], qf, low[h]);
           }
-        //SCHED2
       }
       if (t + 1 < n) put(next);
     }
@@ -489,16 +507,20 @@ template <typename E, int DP>
 hipError_t bwd(const KeyShares& sh, AttnArgs a, hipStream_t s) {
   constexpr int BK = 32, fixed = kRowsInLds<E> ? 4 * AttnTile<E, DP, 32>::BYTES : 0;
   constexpr auto dq = attn_dq_kernel<E, DP, BK>;
-  constexpr auto dkv = attn_dkv_kernel<E, DP>;
-  const int bytes = 4 * AttnTile<E, DP, BK>::BYTES + fixed, more = bytes + 4 * BK * 4;
+  constexpr bool kSplit = kRowsInLds<E>;
+  constexpr auto coarse = attn_dkv_kernel<E, DP, false>;
+  constexpr auto fine = attn_dkv_kernel<E, DP, kSplit>;
+  const int bytes = 4 * AttnTile<E, DP, BK>::BYTES + fixed, more = bytes + 6 * BK * 4;
   hipError_t e = allow_lds<dq>(bytes);
-  if (e == hipSuccess) e = allow_lds<dkv>(more);
+  if (e == hipSuccess) e = allow_lds<coarse>(more);
+  if (e == hipSuccess) e = allow_lds<fine>(more);
   if (e != hipSuccess) return e;
   a.nblk = (int)(((int64_t)a.Tq * a.G + 127) / 128);
   dq<<<attn_grid(attn_wgs((int64_t)a.B * a.Hkv, a.nblk)), 256, bytes, s>>>(a, sh.whole ? 0 : sh.nkey);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  dkv<<<attn_grid(sh.wgs), 256, more, s>>>(a, sh);
+  if (a.Tq <= kFineQueries) fine<<<attn_grid(sh.wgs), 256, more, s>>>(a, sh);
+  else coarse<<<attn_grid(sh.wgs), 256, more, s>>>(a, sh);
   e = hipGetLastError();
   if (e != hipSuccess || sh.whole) return e;
   attn_parts_kernel<E, DP><<<attn_grid(4 * (int64_t)sh.wgs + (int64_t)a.B * a.Hkv * sh.nkey), 256, 0, s>>>(a, sh);

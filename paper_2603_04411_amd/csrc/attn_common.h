@@ -15,7 +15,8 @@ struct AttnHeader {
 static_assert(sizeof(AttnHeader) == 256, "header is one 256-byte line");
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kLn2 = 0.6931471805599453f, kLn2Low = 0.6931471805599453 - (double)kLn2;
+constexpr float kLog2eLow = 1.4426950408889634 - (double)kLog2e;
 
 // One tensor as a kernel sees it: strides in bytes.
 struct AttnTensor {
@@ -145,6 +146,14 @@ struct AttnElem<bf16_tag> {
   }
   __device__ static inline Frag of(const float* x) {
     return u32x4_t{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
+  }
+  // x = high + low to sixteen bits
+  __device__ static inline void split(const float* x, Frag& high, Frag& low) {
+    high = of(x);
+    float r[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r[j] = x[j] - value(high, j);
+    low = of(r);
   }
   __device__ static inline Frag load(const char* p) { return *reinterpret_cast<const u32x4_t*>(p); }
   __device__ static inline float value(const Frag& f, int j) {
@@ -312,6 +321,19 @@ struct AttnTile {
       }
       return f;
     }
+  }
+};
+
+// log sum exp from a maximum in powers of two and the sum of 2^(logit - maximum): rounded once, but for the sum's logarithm.
+__device__ inline float lse_of(float m, float sum) {
+  return sum == 0.f ? -INFINITY : fmaf(m, kLn2, fmaf(m, kLn2Low, logf(sum)));
+}
+// lse in powers of two, which fp32 holds to half a unit only: P is 2^(logit - a - b).  (b only matters where P is not rounded to bf16.)
+struct Ends {
+  float a, b;
+  __device__ inline explicit Ends(float lse) {
+    a = lse == -INFINITY ? INFINITY : lse * kLog2e;
+    b = lse == -INFINITY || lse == INFINITY ? 0.f : fmaf(lse, kLog2e, -a) + lse * kLog2eLow;
   }
 };
 

@@ -324,7 +324,7 @@ __global__ __launch_bounds__(kFewWaves * 64, AttnElem<E>::size == 2 ? 2 : 1) voi
       else reinterpret_cast<float*>(out)[d] = y;
     }
     if (d == 0 && a.lse)
-      a.lse[((int64_t)b * a.Hq + head) * a.Tq + qi] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * kLn2;
+      a.lse[((int64_t)b * a.Hq + head) * a.Tq + qi] = lse_of(top, total);
   }
 }
 
@@ -410,7 +410,7 @@ __global__ __launch_bounds__(256) void attn_finish_kernel(AttnArgs a, int njoin,
       AttnElem<E>::store4(out + 4 * threadIdx.x * AttnElem<E>::size, y.x * inv, y.y * inv, y.z * inv, y.w * inv);
     }
     if (threadIdx.x == 0 && a.lse)
-      a.lse[((int64_t)b * a.Hq + head) * a.Tq + qi] = total == 0.f ? -INFINITY : (base + __builtin_amdgcn_logf(total)) * kLn2;
+      a.lse[((int64_t)b * a.Hq + head) * a.Tq + qi] = lse_of(base, total);
     return;
   }
   // maximum and total of each row: a wavefront takes every fourth row, its lanes the parts

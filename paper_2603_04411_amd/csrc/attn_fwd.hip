@@ -238,7 +238,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_fwd_kernel(AttnArgs a) {
       const int d = db * 32 + acc_row(i, l);
       if (d < a.D) El::store4(out + d * El::size, o[db][i] * inv, o[db][i + 1] * inv, o[db][i + 2] * inv, o[db][i + 3] * inv);
     }
-  if (a.lse && l < 32) a.lse[((int64_t)b * a.Hq + head) * a.Tq + qi] = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2;
+  if (a.lse && l < 32) a.lse[((int64_t)b * a.Hq + head) * a.Tq + qi] = lse_of(m, sum);
 }
 
 // Joins the parts of a row: a wavefront each.
@@ -272,7 +272,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int rows) {
     if constexpr (AttnElem<E>::size == 2) reinterpret_cast<uint16_t*>(out)[d] = (uint16_t)pack_bf16(o[i] * inv, 0.f);
     else reinterpret_cast<float*>(out)[d] = o[i] * inv;
   }
-  if (a.lse && l == 0) a.lse[((int64_t)b * a.Hq + head) * a.Tq + qi] = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2;
+  if (a.lse && l == 0) a.lse[((int64_t)b * a.Hq + head) * a.Tq + qi] = lse_of(m, sum);
 }
 
 // Weight that the keys got: S = Q K^T with the queries along the accumulators' rows, so that a lane adds up one key's column.  A workgroup
@@ -284,7 +284,7 @@ __global__ __launch_bounds__(256) void attn_weight_kernel(AttnArgs a, int nkey) 
   using Tile = AttnTile<E, DP, 32>;
   constexpr int KS = Tile::KS;
   extern __shared__ char lds[];
-  __shared__ float ends[32];
+  __shared__ float ends[32], lows[32];
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Work work;
   if (!attn_work(a.B * a.Hkv, nkey, work)) return;
@@ -330,7 +330,8 @@ __global__ __launch_bounds__(256) void attn_weight_kernel(AttnArgs a, int nkey) 
       if (threadIdx.x < 32) {
         const int qi = i + threadIdx.x;
         const float lse = qi < lq ? a.lse[((int64_t)b * a.Hq + head) * a.Tq + qi] : -INFINITY;
-        ends[threadIdx.x] = lse == -INFINITY ? INFINITY : lse * kLog2e;
+        const Ends e(lse);
+        ends[threadIdx.x] = e.a, lows[threadIdx.x] = e.b;
       }
       __builtin_amdgcn_s_waitcnt(kWaitVm0);
       __syncthreads();
@@ -342,7 +343,7 @@ __global__ __launch_bounds__(256) void attn_weight_kernel(AttnArgs a, int nkey) 
 #pragma unroll
       for (int x = 0; x < 16; ++x) {
         const int row = acc_row(x, l);
-        const float e = __builtin_amdgcn_exp2f(fmaf(s[x], a.scale2, -ends[row]));
+        const float e = __builtin_amdgcn_exp2f(fmaf(s[x], a.scale2, -ends[row]) - lows[row]);
         sum += ((i + row < lq) & seen(key, off + i + row, a.window, a.sinks)) ? e : 0.f;
       }
     }
