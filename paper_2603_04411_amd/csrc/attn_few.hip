@@ -178,8 +178,7 @@ __global__ __launch_bounds__(kFewWaves * 64, AttnElem<E>::size == 2 ? 2 : 1) voi
   KeyTiles kt = key_tiles<TK>(max(pmin, 0), pmax, a.window, a.sinks);
   if (pmax < 0) kt.n = 0;
   const int per = uniform((kt.n + a.nsplit - 1) / (uint32_t)a.nsplit), t1 = min(kt.n, (split + 1) * per);
-  // with rows beside the last, or before position 0, no tile is seen whole; those rows are not looked at at the end
-  const bool few_rows = lk < lq;
+  const bool blind = lk < lq || lq < a.Tq;      // some row sees nothing: no tile is seen whole
 
   f32x4_t o[NN][DB];
   float m[NN], sum[NN];
@@ -215,7 +214,7 @@ __global__ __launch_bounds__(kFewWaves * 64, AttnElem<E>::size == 2 ? 2 : 1) voi
       }
     // (where logits are stored, behind their stores: a wait for loads then finds older stores only, not ones that were issued since)
     if (!a.logits && t + kFewWaves < t1) fetch(t + kFewWaves);
-    const bool part = few_rows || n < TK || !all_seen(s0, n, pmin, pmax, a.window, a.sinks);
+    const bool part = blind || n < TK || !all_seen(s0, n, pmin, pmax, a.window, a.sinks);
 #pragma unroll
     for (int nn = 0; nn < NN; ++nn) {
       if (part) {

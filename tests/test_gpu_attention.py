@@ -151,6 +151,9 @@ CASES = [
     dict(B=1, Tq=4, Tk=3001, Hq=16, Hkv=2, D=128),
     dict(B=1, Tq=5, Tk=3001, Hq=14, Hkv=2, D=128, window=2000, sinks=1),
     dict(B=2, Tq=16, Tk=2000, Hq=16, Hkv=4, D=96, len_q=[16, 9], len_k=[1999, 64]),
+    dict(B=4, Tq=4, Tk=900, Hq=8, Hkv=2, D=128, len_q=[4, 1, 0, 3], len_k=[900, 800, 700, 2]),
+    dict(B=3, Tq=8, Tk=1200, Hq=4, Hkv=4, D=64, len_q=[8, 5, 1], len_k=[1200, 1100, 400], window=130, sinks=3),
+    dict(B=3, Tq=8, Tk=1200, Hq=8, Hkv=2, D=64, len_q=[8, 5, 1], len_k=[1200, 1100, 400], window=130, sinks=70, dtype="f32"),
     # layouts
     dict(B=2, Tq=90, Tk=130, Hq=4, Hkv=2, D=64, first="head", len_q=[90, 31], len_k=[130, 99]),
     dict(B=2, Tq=90, Tk=130, Hq=4, Hkv=2, D=56, first="wide", len_q=[90, 31], len_k=[130, 99]),
@@ -213,7 +216,7 @@ def test_lengths_out_of_range_are_reported_and_taken_as_the_nearest():
 
 def test_bits_are_the_same_from_run_to_run():
     import torch
-    for c in (CASES[12], CASES[20], CASES[27], CASES[29]):
+    for c in (CASES[12], CASES[20], CASES[27], CASES[29], CASES[33]):
         p = Problem(**c)
         p.fwd(decay=0.0)
         first = [p.out.clone(), p.lse.clone(), p.weight.clone()]

@@ -58,6 +58,8 @@ CACHES = [
     dict(B=1, Tq=8, Tk=3001, Hq=32, Hkv=8, D=128),
     dict(B=1, Tq=8, Tk=3001, Hq=32, Hkv=8, D=128, dtype="f32"),
     dict(B=2, Tq=1, Tk=2500, Hq=28, Hkv=4, D=128, window=1000, sinks=4, len_k=[2500, 1003]),
+    dict(B=3, Tq=4, Tk=900, Hq=8, Hkv=2, D=128, len_q=[4, 1, 3], len_k=[900, 800, 700], window=300, sinks=1),
+    dict(B=3, Tq=4, Tk=900, Hq=4, Hkv=2, D=64, len_q=[4, 1, 0], len_k=[900, 800, 700], dtype="f32"),
     dict(B=2, Tq=70, Tk=300, Hq=6, Hkv=3, D=32, window=100, sinks=65, len_q=[70, 30], len_k=[300, 20]),
     dict(B=1, Tq=200, Tk=200, Hq=2, Hkv=2, D=128),
     dict(B=1, Tq=130, Tk=260, Hq=2, Hkv=1, D=96, dtype="f32"),
