@@ -1,4 +1,6 @@
 // The cache itself: rows quantised to 4 bits, and tokens that leave it.
+#include <algorithm>
+
 #include "attn_common.h"
 
 namespace lmhead {
@@ -87,10 +89,12 @@ __device__ inline uint32_t order_of(float x) {
 }
 
 // One workgroup finds what a key head keeps: the threshold by four passes over eight bits each, then the tokens above it and the first of
-// those at it, in order.
+// those at it, in order.  kHold: values that a thread holds on to over the passes, so that the weights are read once (of more than
+// 1024 * kHold tokens they are read again for each pass).
+template <int kHold>
 __global__ __launch_bounds__(1024) void evict_choose_kernel(EvictArgs a) {
-  __shared__ uint32_t hist[256];
-  __shared__ uint32_t wave_sum[16][2];
+  __shared__ uint32_t hist[4][256];      // of four wavefronts each: the frequent digits are few
+  __shared__ uint32_t wave_sum[2][16];
   __shared__ uint32_t s_digit, s_need;
   const int tid = threadIdx.x, l = tid & 63, w = tid >> 6;
   const uint32_t row = blockIdx.y * kAttnRow + blockIdx.x;
@@ -112,20 +116,45 @@ __global__ __launch_bounds__(1024) void evict_choose_kernel(EvictArgs a) {
     return;
   }
   const int lo = a.sinks, hi = n - a.recent;
+  constexpr int HOLD = kHold ? kHold : 1;
+  float held[HOLD];
+  if constexpr (kHold > 0) {
+#pragma unroll
+    for (int u = 0; u < HOLD; ++u) held[u] = u * 1024 + tid < n ? weight[u * 1024 + tid] : 0.f;
+  }
+  const int rounds = (n + 1023) / 1024;
+  auto value = [&](int u, int i) -> float {
+    if constexpr (kHold > 0) return held[u];
+    else return i < n ? weight[i] : 0.f;
+  };
   uint32_t need = a.keep - a.sinks - a.recent, prefix = 0;     // of [lo, hi): more than `need` of them
   if (need) {
+#pragma unroll 1
     for (int shift = 24; shift >= 0; shift -= 8) {
-      if (tid < 256) hist[tid] = 0;
+      hist[tid >> 8][tid & 255] = 0;
       __syncthreads();
-      for (int i = lo + tid; i < hi; i += 1024) {
-        const uint32_t o = order_of(weight[i]);
-        if (shift == 24 || (o >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[o >> shift & 255], 1u);
+      auto count = [&](int u) {
+        const int i = u * 1024 + tid;
+        const uint32_t o = order_of(value(u, i));
+        if (i >= lo && i < hi && (shift == 24 || (o >> (shift + 8)) == (prefix >> (shift + 8)))) atomicAdd(&hist[w & 3][o >> shift & 255], 1u);
+      };
+      if constexpr (kHold > 0) {
+#pragma unroll
+        for (int u = 0; u < HOLD; ++u)
+          if (u < rounds) count(u);
+      } else {
+        for (int u = 0; u < rounds; ++u) count(u);
       }
       __syncthreads();
       if (w == 0) {      // the highest digits first: lane l has digits 255 - 4 l .. 252 - 4 l
         uint32_t c[4], sum = 0;
-        for (int j = 0; j < 4; ++j) sum += c[j] = hist[255 - 4 * l - j];
+        for (int j = 0; j < 4; ++j) {
+          const int d = 255 - 4 * l - j;
+          c[j] = hist[0][d] + hist[1][d] + hist[2][d] + hist[3][d];
+          sum += c[j];
+        }
         uint32_t before = sum;
+#pragma unroll
         for (int x = 1; x < 64; x <<= 1) {
           const uint32_t y = __shfl_up(before, x);
           before += l >= x ? y : 0;
@@ -142,44 +171,50 @@ __global__ __launch_bounds__(1024) void evict_choose_kernel(EvictArgs a) {
       __syncthreads();
       prefix |= s_digit << shift;
       need = s_need;
-      __syncthreads();
     }
   }
   // `need` of those equal to `prefix` stay, the first ones.  (With need = 0 from the start: none of [lo, hi).)
   const bool any = a.keep > a.sinks + a.recent;
   uint32_t equal = 0, out = 0;      // so far
-  for (int base = 0; base < n; base += 1024) {
-    const int i = base + tid;
-    const float x = i < n ? weight[i] : 0.f;
+  auto place = [&](int u) {
+    const int i = u * 1024 + tid;
+    const float x = value(u, i);
     const uint32_t o = order_of(x);
     const bool fixed = i < n && (i < lo || i >= hi), open = i >= lo && i < hi && any;
     const bool above = open && o > prefix, same = open && o == prefix;
-    const uint64_t below = (1ull << l) - 1;
-    const uint64_t eq = __ballot(same);
-    if (l == 0) wave_sum[w][0] = __popcll(eq);
+    const uint64_t below = (1ull << l) - 1, eq = __ballot(same);
+    if (l == 0) wave_sum[0][w] = __popcll(eq);
     __syncthreads();
-    uint32_t at = equal + __popcll(eq & below), all = equal;
-    for (int x2 = 0; x2 < 16; ++x2) {
-      if (x2 < w) at += wave_sum[x2][0];
-      all += wave_sum[x2][0];
-    }
-    equal = all;
+    uint32_t at = equal + __popcll(eq & below);
+    // (a sum over sixteen wavefronts: every lane has one of them)
+    const uint32_t e = wave_sum[0][l & 15];
+    uint32_t prior = (l & 15) < w ? e : 0, all = e;
+#pragma unroll
+    for (int x2 = 1; x2 < 16; x2 <<= 1) prior += __shfl_xor(prior, x2), all += __shfl_xor(all, x2);
+    at += prior;
+    equal += all;
     const bool stays = fixed || above || (same && at < need);
     const uint64_t st = __ballot(stays);
-    if (l == 0) wave_sum[w][1] = __popcll(st);
+    if (l == 0) wave_sum[1][w] = __popcll(st);
     __syncthreads();
-    uint32_t pos = out + __popcll(st & below), more = out;
-    for (int x2 = 0; x2 < 16; ++x2) {
-      if (x2 < w) pos += wave_sum[x2][1];
-      more += wave_sum[x2][1];
-    }
-    out = more;
-    // slots written here were read by this pass or an earlier one
+    const uint32_t m = wave_sum[1][l & 15];
+    prior = (l & 15) < w ? m : 0, all = m;
+#pragma unroll
+    for (int x2 = 1; x2 < 16; x2 <<= 1) prior += __shfl_xor(prior, x2), all += __shfl_xor(all, x2);
+    // slots written here were read by this round or an earlier one (by all threads: a barrier lies between)
     if (stays) {
+      const uint32_t pos = out + prior + __popcll(st & below);
       kept[pos] = i;
       weight[pos] = x;
     }
-    __syncthreads();
+    out += all;
+  };
+  if constexpr (kHold > 0) {
+#pragma unroll
+    for (int u = 0; u < HOLD; ++u)
+      if (u < rounds) place(u);
+  } else {
+    for (int u = 0; u < rounds; ++u) place(u);
   }
   for (int i = a.keep + tid; i < n; i += 1024) weight[i] = 0.f;
 }
@@ -188,43 +223,53 @@ struct MoveArgs {
   int B, T, Hkv, keep;
   const int32_t *len, *kept;
   cache_plane plane[EVICT_PLANES];
-  int count, slices;        // column slices of a row, each moved by a workgroup of its own
-  int words[EVICT_PLANES];  // units of a row
+  int slices, parts[EVICT_PLANES];      // column slices of a row in all planes, and in each
 };
 
 // Rows close up in place.  A workgroup takes rows in ascending order, and a row only moves towards the front: what a step reads lies at or
-// behind everything that it and the steps before it write, so a step reads all of its rows, waits, and writes them.
+// behind everything that it and the steps before it write, so a step reads all of its rows, waits, and writes them.  Slices of the
+// rows' columns are independent of each other and go to workgroups of their own.
 template <typename W>
 __global__ __launch_bounds__(256) void evict_move_kernel(MoveArgs a) {
   constexpr int U = 8;      // units a thread and step
-  const uint32_t id = blockIdx.y * kAttnRow + blockIdx.x, works = (uint32_t)a.B * a.Hkv * a.count;
+  const uint32_t id = blockIdx.y * kAttnRow + blockIdx.x, works = (uint32_t)a.B * a.Hkv * a.slices;
   if (id >= works) return;
-  const int which = id % a.count;
-  const uint32_t row = id / a.count;
+  int slice = id % a.slices, which = 0;
+  while (slice >= a.parts[which]) slice -= a.parts[which++];
+  const uint32_t row = id / a.slices;
   const int b = row / a.Hkv, h = row % a.Hkv;
   const int n = clamp_len(a.len, b, a.T);
   if (n <= a.keep) return;
   const cache_plane& p = a.plane[which];
-  const int words = a.words[which];
-  char* const base = static_cast<char*>(p.data) + b * p.seq + h * p.head;
+  const int all_words = (int)(p.bytes / (int)sizeof(W)), each = (all_words + a.parts[which] - 1) / a.parts[which];
+  const int w0 = slice * each, words = min(each, all_words - w0);
+  char* const base = static_cast<char*>(p.data) + b * p.seq + h * p.head + (int64_t)w0 * sizeof(W);
   const int32_t* const kept = a.kept + (int64_t)row * a.keep;
   const int64_t all = (int64_t)a.keep * words;
+  // (a row's first unit and its place in the row, carried along: no division in the loop)
+  int r[U], c[U];
+  const int dr = 256 * U / words, dc = 256 * U % words;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int i = u * 256 + threadIdx.x;
+    r[u] = i / words, c[u] = i % words;
+  }
   for (int64_t s = 0; s < all; s += 256 * U) {
     W x[U];
-    int64_t to[U];
+    int from[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t i = s + u * 256 + threadIdx.x;
-      const int r = (int)(i / words), c = (int)(i % words);
-      const int from = i < all ? kept[r] : r;
-      to[u] = from != r ? r * p.slot + c * (int64_t)sizeof(W) : -1;
-      if (to[u] >= 0) x[u] = *reinterpret_cast<const W*>(base + from * p.slot + c * (int64_t)sizeof(W));
-    }
+    for (int u = 0; u < U; ++u) from[u] = r[u] < a.keep ? kept[r[u]] : r[u];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (from[u] != r[u]) x[u] = *reinterpret_cast<const W*>(base + from[u] * p.slot + c[u] * (int64_t)sizeof(W));
     __builtin_amdgcn_s_waitcnt(kWaitVm0);
     __syncthreads();
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (to[u] >= 0) *reinterpret_cast<W*>(base + to[u]) = x[u];
+    for (int u = 0; u < U; ++u) {
+      if (from[u] != r[u]) *reinterpret_cast<W*>(base + r[u] * p.slot + c[u] * (int64_t)sizeof(W)) = x[u];
+      r[u] += dr, c[u] += dc;
+      if (c[u] >= words) c[u] -= words, ++r[u];
+    }
   }
 }
 
@@ -246,19 +291,29 @@ hipError_t launch_kv4_store(const attn_desc* d, const AttnArgs& a, uint8_t* cons
 hipError_t launch_evict(const evict_desc& d, const cache_plane* planes, int count, float* weight, const int32_t* len, int32_t* len_out,
                         int32_t* kept, char* ws, hipStream_t s) {
   EvictArgs a{d.B, d.T, d.Hkv, d.keep, d.sinks, d.recent, weight, len, len_out, kept, reinterpret_cast<AttnHeader*>(ws)};
-  evict_choose_kernel<<<attn_grid((int64_t)d.B * d.Hkv), 1024, 0, s>>>(a);
+  const dim3 rows = attn_grid((int64_t)d.B * d.Hkv);
+  if (d.T <= 1024) evict_choose_kernel<1><<<rows, 1024, 0, s>>>(a);
+  else if (d.T <= 4096) evict_choose_kernel<4><<<rows, 1024, 0, s>>>(a);
+  else if (d.T <= 16384) evict_choose_kernel<16><<<rows, 1024, 0, s>>>(a);
+  else evict_choose_kernel<0><<<rows, 1024, 0, s>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   MoveArgs m{};
-  m.B = d.B, m.T = d.T, m.Hkv = d.Hkv, m.keep = d.keep, m.len = len, m.kept = kept, m.count = count;
+  m.B = d.B, m.T = d.T, m.Hkv = d.Hkv, m.keep = d.keep, m.len = len, m.kept = kept;
   bool wide = true;
   for (int i = 0; i < count; ++i) {
     const cache_plane& p = planes[i];
     m.plane[i] = p;
     wide = wide && (reinterpret_cast<uintptr_t>(p.data) | p.seq | p.slot | p.head | p.bytes) % 16 == 0;
   }
-  for (int i = 0; i < count; ++i) m.words[i] = (int)(planes[i].bytes / (wide ? 16 : 4));
-  const dim3 grid = attn_grid((int64_t)d.B * d.Hkv * count);
+  // Slices of at least 64 bytes, as many as keep 1024 workgroups busy (2 sequences of 1024 tokens, 8 heads of 256 bytes in two planes: 20 us
+  // in one slice).
+  const int64_t most = (1024 + (int64_t)d.B * d.Hkv * count - 1) / ((int64_t)d.B * d.Hkv * count);
+  for (int i = 0; i < count; ++i) {
+    m.parts[i] = (int)std::max<int64_t>(1, std::min<int64_t>(most, planes[i].bytes / 64));
+    m.slices += m.parts[i];
+  }
+  const dim3 grid = attn_grid((int64_t)d.B * d.Hkv * m.slices);
   if (wide) evict_move_kernel<u32x4_t><<<grid, 256, 0, s>>>(m);
   else evict_move_kernel<uint32_t><<<grid, 256, 0, s>>>(m);
   return hipGetLastError();
