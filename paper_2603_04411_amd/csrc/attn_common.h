@@ -201,6 +201,13 @@ struct AttnElem<f32_tag> {
 
 typedef __attribute__((address_space(3))) char lds_char;
 
+// A transposing read.  With nothing known of its memory the compiler has it wait for all loads into LDS on their way, the next tile's too;
+// `restrict` is what it needs to know (kernels wait for a tile themselves).
+__device__ __attribute__((always_inline)) inline u32x2_t read_across(const char* __restrict p) {
+  typedef __attribute__((address_space(3))) i16x4_t* tptr_t;
+  return __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tptr_t)p));
+}
+
 // ROWS rows of DP values in LDS.  A row is CH chunks of 16 bytes; chunk c of row r sits at position c ^ swz(r) of its row.  A read along rows
 // takes a chunk of eight consecutive rows at a time, which then lie in different 16-byte banks (of 128 bytes, and sixteen rows in those of 256);
 // a transposing read takes 64 bytes of four rows (32 of eight where blocks are sixteen wide), which cover 256 bytes.  (With pairs of chunks
@@ -272,12 +279,11 @@ struct AttnTile {
   }
   __device__ static inline Frag col_frag(const char* lds, uint32_t base, int db, int s) {
     if constexpr (El::size == 2) {
-      typedef __attribute__((address_space(3))) i16x4_t* tptr_t;
       u32x4_t f;
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
         const uint32_t at = (base ^ (CH == 8 ? db << 6 | p << 4 : (db ^ p << 1) << 6)) + (16 * s + 8 * p) * ROW;
-        const u32x2_t v = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tptr_t)(lds + at)));
+        const u32x2_t v = read_across(lds + at);
         f[2 * p] = v.x;
         f[2 * p + 1] = v.y;
       }
@@ -302,12 +308,11 @@ struct AttnTile {
   }
   __device__ static inline Frag col_frag16(const char* lds, uint32_t base, int db, int s) {
     if constexpr (El::size == 2) {
-      typedef __attribute__((address_space(3))) i16x4_t* tptr_t;
       u32x4_t f;
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
         const uint32_t at = (base ^ (db << 5)) + (32 * s + 16 * p) * ROW;
-        const u32x2_t v = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tptr_t)(lds + at)));
+        const u32x2_t v = read_across(lds + at);
         f[2 * p] = v.x;
         f[2 * p + 1] = v.y;
       }

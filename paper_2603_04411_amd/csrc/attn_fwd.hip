@@ -46,7 +46,7 @@ constexpr float kSlack = 8.f;
 // they see in tiles of BK: S^T = K Q^T with the keys along the accumulators' rows, so that a lane holds one query's logits and the
 // softmax needs one exchange between lane halves; the exponentials are the second operand of O^T = V^T P^T as they lie.
 template <typename E, int DP, int NW, int BK, bool kCache>
-__global__ __launch_bounds__(NW * 64, 2) void attn_fwd_kernel(AttnArgs a) {
+__global__ __launch_bounds__(NW * 64, AttnElem<E>::size == 2 || DP == 64 ? 2 : 1) void attn_fwd_kernel(AttnArgs a) {
   using El = AttnElem<E>;
   using Frag = typename El::Frag;
   using Tile = AttnTile<E, DP, BK>;
@@ -129,12 +129,13 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_fwd_kernel(AttnArgs a) {
   };
 
   // One tile: the softmax of `s`, beside which the matrix cores form the next tile's logits, and the product with V.
-  auto step = [&](int t, auto which, Logits& s, Logits& next) {
+  auto step = [&](int t, auto which, auto last, Logits& s, Logits& next) {
     constexpr int P = decltype(which)::value;      // where its K and V lie
     __builtin_amdgcn_s_waitcnt(kWaitVm0);
     __syncthreads();
-    if (t + 2 < t1) load_k(t + 2, P);
-    if (t + 1 < t1) load_v(t + 1, 1 - P);
+    if constexpr (!decltype(last)::value)
+      if (t + 2 < t1) load_k(t + 2, P);
+    if constexpr (!decltype(last)::value) load_v(t + 1, 1 - P);
     const int s0 = tile_start<BK>(kt, t), n = min(BK, tile_end(kt, t) - s0);
     if (n < BK || !all_seen(s0, n, wlow, wmax, a.window, a.sinks)) {
       const Seen sees(s0, n, p, a.window, a.sinks, 4 * (l >> 5));
@@ -163,41 +164,60 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_fwd_kernel(AttnArgs a) {
     const float base = m == -INFINITY ? 0.f : m;
     const char* const k = lds + (1 - P) * Tile::BYTES;
     const char* const v = lds + (2 + P) * Tile::BYTES;
-    Frag pf[2 * KB];
-    auto weights = [&]() {
+    // In this order, which the compiler keeps between the steps: a product of the next tile's logits, two exponentials of this one's, the
+    // reads of LDS three products ahead.  (Left to itself it puts the exponentials before the products and each read before its product.)
+    constexpr int M = KS * KB, N = 2 * KB * DB, A = 3, EACH = 16 * KB / M;      // products, reads ahead, exponentials a product
+    constexpr bool kMore = !decltype(last)::value;
+    Frag pf[2 * KB], kf[A + 1], vf[A + 1];
+    float e[16 * KB], part[2] = {0.f, 0.f};
+    // fma, exponential and sum of a logit are a step apart each, so that none waits for the one before
+    auto weigh = [&](int x) {
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
-        float e[16];
+      for (int y = x * EACH; y < (x + 1) * EACH; ++y)
+        if (y < 16 * KB) e[y] = fmaf(s[y / 16][y % 16], a.scale2, -base);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          e[i] = __builtin_amdgcn_exp2f(fmaf(s[kb][i], a.scale2, -base));
-          sum += e[i];
+      for (int y = (x - 1) * EACH; y < x * EACH; ++y)
+        if (y >= 0 && y < 16 * KB) e[y] = __builtin_amdgcn_exp2f(e[y]);
+#pragma unroll
+      for (int y = (x - 2) * EACH; y < (x - 1) * EACH; ++y)
+        if (y >= 0) {
+          part[y & 1] += e[y];
+          if (y % 8 == 7) pf[y / 8] = El::of(e + y - 7);
         }
-        pf[2 * kb] = El::of(e);
-        pf[2 * kb + 1] = El::of(e + 8);
-      }
     };
-    if (t + 1 < t1) {
-      logits(next, k);
-      weights();
-      if constexpr (El::size == 2) {
-        constexpr int M = KS * KB;
-        __builtin_amdgcn_sched_group_barrier(kDsRead, 3, 0);
+    auto row = [&](int x) {
+      if (x < M) kf[x % (A + 1)] = Tile::row_frag(k, rbase, x % KB, x / KB);
+    };
+    auto col = [&](int x) {
+      if (x < N) vf[x % (A + 1)] = Tile::col_frag(v, cbase, x % DB, x / DB);
+    };
+    if constexpr (kMore) {
 #pragma unroll
-        for (int x = 0; x < M; ++x) {
-          __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(kTrans, 32 / M * KB / 2, 0);
-          __builtin_amdgcn_sched_group_barrier(kValu, 8, 0);
-        }
-      }
-    } else {
-      weights();
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) next[kb][i] = 0.f;
+#pragma unroll
+      for (int x = 0; x < A; ++x) row(x);
     }
 #pragma unroll
-    for (int x = 0; x < 2 * KB; ++x)
+    for (int x = 0; x < M; ++x) {
+      if constexpr (kMore) {
+        El::mma(next[x % KB], kf[x % (A + 1)], q[x / KB]);
+        row(x + A);
+      }
+      if (x >= M - A) col(x - (M - A));
+      weigh(x);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    weigh(M);
+    weigh(M + 1);
+    sum += part[0] + part[1];
 #pragma unroll
-      for (int db = 0; db < DB; ++db) El::mma(o[db], Tile::col_frag(v, cbase, db, x), pf[x]);
+    for (int x = 0; x < N; ++x) {
+      El::mma(o[x % DB], vf[x % (A + 1)], pf[x / DB]);
+      col(x + A);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   };
 
   if (t0 < t1) {
@@ -208,9 +228,18 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_fwd_kernel(AttnArgs a) {
     __syncthreads();
     if (t0 + 1 < t1) load_k(t0 + 1, 1);
     logits(s[0], lds);
-    for (int t = t0; t < t1; t += 2) {
-      step(t, std::integral_constant<int, 0>{}, s[0], s[1]);
-      if (t + 1 < t1) step(t + 1, std::integral_constant<int, 1>{}, s[1], s[0]);
+    const std::integral_constant<int, 0> even;
+    const std::integral_constant<int, 1> odd;
+    int t = t0;
+    for (; t + 2 < t1; t += 2) {
+      step(t, even, std::false_type{}, s[0], s[1]);
+      step(t + 1, odd, std::false_type{}, s[1], s[0]);
+    }
+    if (t + 1 < t1) {
+      step(t, even, std::false_type{}, s[0], s[1]);
+      step(t + 1, odd, std::true_type{}, s[1], s[0]);
+    } else {
+      step(t, even, std::true_type{}, s[0], s[1]);
     }
   }
   sum = add_halves(sum);
