@@ -185,8 +185,9 @@ LMHEAD_API int dynakv_check(void* ws, void* stream);
  *    launched, and results are bit-reproducible (the grouping of sums depends on the sizes of the call).  Descriptors and plane
  *    lists are host memory.  The workspace's error word is read by lmhead_check(): a length outside [0, T], taken as the nearest
  *    one inside.  A workspace belongs to one call at a time.
- *  - What lies in slots from a sequence's length on is never used, whatever its bits, nor are keys that no query of the call
- *    sees.  An infinity or NaN in a key or value that some queries see and others do not reaches only those that do.
+ *  - What lies in slots from a sequence's length on is never used, whatever its bits, nor is a key that no query of the call
+ *    sees.  An infinity or NaN in a key or value that some queries see can reach others that do not, whose rows share a tile of a
+ *    matrix product with it (0 times an infinity is NaN): those up to 127 positions away.
  *  - Logits, softmax and all sums are fp32.  With bf16 storage P, and in the backward dS, are rounded to bf16 before they
  *    enter a matrix product, as are the outputs.
  */
@@ -229,7 +230,7 @@ LMHEAD_API size_t attn_workspace_bytes(const attn_desc* desc);
  *                   queries i and the heads that read h, for j < len_k[b]; the rest is left as it was.  With decay = 0 the old
  *                   value is not read.
  *   decay           finite, >= 0
- * `out` and `weight` share no memory with an input or each other.
+ * Outputs share no memory with an input or each other; equal addresses are refused (LMHEAD_E_SHAPE), here and below.
  */
 LMHEAD_API int attn_fwd(const attn_desc* desc, const void* q, const void* k, const void* v, const int32_t* len_q,
                         const int32_t* len_k, void* out, float* lse, float* weight, float decay, void* ws, size_t ws_bytes,

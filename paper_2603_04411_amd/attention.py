@@ -230,7 +230,6 @@ class CachePlanes:
         self.tensors = [t.detach() for t in tensors]
         self.array = (_Plane * max(len(self.tensors), 1))()
         self.device = None
-        spans = []
         for i, t in enumerate(self.tensors):
             name = f"plane {i}"
             if not t.is_cuda:
@@ -243,9 +242,6 @@ class CachePlanes:
                 _bad(name, f"on cuda:{t.get_device()}, others on cuda:{self.device}")
             seq, slot, head = (x * t.element_size() for x in attn_layout(t))
             self.array[i] = _Plane(t.data_ptr() or None, seq, slot, head, t.shape[3] * t.element_size())
-            if t.numel():
-                last = sum((n - 1) * s for n, s in zip(t.shape, t.stride())) + 1
-                spans.append((t.data_ptr(), t.data_ptr() + last * t.element_size(), i))
         self.storages = [t.untyped_storage() for t in self.tensors]
         self.addresses = [s.data_ptr() for s in self.storages]
 

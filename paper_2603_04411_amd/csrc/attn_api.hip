@@ -3,12 +3,13 @@
 #include <math.h>
 
 #include <algorithm>
+#include <initializer_list>
 
 #include "attn_common.h"
 
 namespace lmhead {
 
-AttnPlan attn_plan(const attn_desc* d, bool cache4) {
+AttnPlan attn_plan(const attn_desc* d) {
   AttnPlan p{};
   p.DP = d->D <= 64 ? 64 : 128;
   const int64_t G = d->Hq / d->Hkv, R = d->Tq * G, heads = (int64_t)d->B * d->Hkv;
@@ -36,7 +37,6 @@ AttnPlan attn_plan(const attn_desc* d, bool cache4) {
   p.logits = take(R <= kLogitRows ? (size_t)heads * logit_groups(d->Tk) * R * 4 * sizeof(float) : 0);
   p.lse = take((size_t)d->B * d->Hq * d->Tq * sizeof(float));
   p.total = off;
-  (void)cache4;
   return p;
 }
 
@@ -50,25 +50,32 @@ bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(
 
 constexpr int64_t kMostStride = 1ll << 40;
 
-// A layout that a tensor of n sequences, t slots and h heads can have; `apart`: no two of its elements at one place.
-int check_layout(const attn_layout& x, int64_t n, int64_t t, int64_t h, int64_t D, int esz, bool apart) {
+bool strides(const attn_layout& x) {
   for (int64_t v : {x.seq, x.slot, x.head})
-    if (v < 0 || v > kMostStride) return LMHEAD_E_SHAPE;
-  if (x.slot < D || x.slot * esz >= (1 << 24)) return LMHEAD_E_SHAPE;
+    if (v < 0 || v > kMostStride) return false;
+  return true;
+}
+
+// Whether no two rows of `width` elements (n sequences, t slots, h heads) lie upon each other.
+bool apart(const attn_layout& x, int64_t n, int64_t t, int64_t h, int64_t width) {
+  struct Dim {
+    int64_t stride, size;
+  } d[3] = {{x.seq, n}, {x.slot, t}, {x.head, h}};
+  std::sort(d, d + 3, [](const Dim& a, const Dim& b) { return a.stride < b.stride; });
+  int64_t extent = width;      // of what the dimensions so far span
+  for (const Dim& k : d) {
+    if (k.size == 1) continue;
+    if (k.stride < extent) return false;
+    extent += k.stride * (k.size - 1);
+  }
+  return true;
+}
+
+// A layout that a tensor which is read can have: its slots lie apart, at most what a tile's 32-bit offsets reach.
+int check_layout(const attn_layout& x, int64_t D, int esz) {
+  if (!strides(x) || x.slot < D || x.slot * esz >= (1 << 24)) return LMHEAD_E_SHAPE;
   for (int64_t v : {x.seq, x.slot, x.head})
     if (v * esz % 16 != 0) return LMHEAD_E_ALIGN;
-  if (apart) {
-    struct Dim {
-      int64_t stride, size;
-    } d[3] = {{x.seq, n}, {x.slot, t}, {x.head, h}};
-    std::sort(d, d + 3, [](const Dim& a, const Dim& b) { return a.stride < b.stride; });
-    int64_t extent = D;      // of what the dimensions so far span
-    for (const Dim& k : d) {
-      if (k.size == 1) continue;
-      if (k.stride < extent) return LMHEAD_E_SHAPE;
-      extent += k.stride * (k.size - 1);
-    }
-  }
   return LMHEAD_OK;
 }
 
@@ -77,7 +84,7 @@ int validate(const attn_desc* d) {
   if (d->B <= 0 || d->B > 65535 || d->Tq <= 0 || d->Tk <= 0 || d->Hq <= 0 || d->Hkv <= 0 || d->Hq > 1024) return LMHEAD_E_SHAPE;
   if (d->Hq % d->Hkv != 0 || d->D <= 0 || d->D > 128 || d->D % 8 != 0) return LMHEAD_E_SHAPE;
   if (d->Tq > kNoWindow / 1024 || d->Tk > kNoWindow - 4096) return LMHEAD_E_SHAPE;
-  if (d->window < 0 || d->sinks < 0 || !isfinite(d->scale) || d->scale <= 0.f) return LMHEAD_E_SHAPE;
+  if (d->window < 0 || d->sinks < 0 || !isfinite(d->scale * kLog2e) || d->scale <= 0.f) return LMHEAD_E_SHAPE;
   if (d->dtype != LMHEAD_F32 && d->dtype != LMHEAD_BF16) return LMHEAD_E_DTYPE;
   if (d->flags != 0) return LMHEAD_E_DTYPE;
   if (d->reserved != 0) return LMHEAD_E_SHAPE;
@@ -85,11 +92,11 @@ int validate(const attn_desc* d) {
   // work items are counted in 32 bits
   const int64_t rows = (int64_t)d->Tq * (d->Hq / d->Hkv), blocks = std::max((rows + 31) / 32, ((int64_t)d->Tk + 127) / 128);
   if ((int64_t)d->B * d->Hkv > ((int64_t)INT32_MAX - 8) / blocks) return LMHEAD_E_SHAPE;
-  int rc = check_layout(d->q, d->B, d->Tq, d->Hq, d->D, esz, false);
-  if (rc == LMHEAD_OK) rc = check_layout(d->k, d->B, d->Tk, d->Hkv, d->D, esz, false);
-  if (rc == LMHEAD_OK) rc = check_layout(d->v, d->B, d->Tk, d->Hkv, d->D, esz, false);
-  if (rc == LMHEAD_OK) rc = check_layout(d->o, d->B, d->Tq, d->Hq, d->D, esz, true);
-  return rc;
+  for (const attn_layout* x : {&d->q, &d->k, &d->v, &d->o}) {
+    const int rc = check_layout(*x, d->D, esz);
+    if (rc != LMHEAD_OK) return rc;
+  }
+  return apart(d->o, d->B, d->Tq, d->Hq, d->D) ? LMHEAD_OK : LMHEAD_E_SHAPE;
 }
 
 AttnTensor tensor(const void* p, const attn_layout& x, int esz) {
@@ -134,6 +141,18 @@ int run_fwd(const attn_desc* d, const AttnPlan& p, AttnArgs& a, void* ws, float*
   return LMHEAD_OK;
 }
 
+// Whether no output is another output or an input.  (Views of one buffer begin at different places; that they lie apart is the caller's.)
+bool different(std::initializer_list<const void*> outputs, std::initializer_list<const void*> inputs) {
+  for (auto o = outputs.begin(); o != outputs.end(); ++o) {
+    if (!*o) continue;
+    for (auto x = outputs.begin(); x != o; ++x)
+      if (*x == *o) return false;
+    for (const void* x : inputs)
+      if (x == *o) return false;
+  }
+  return true;
+}
+
 int check_weight(const float* weight, float decay) {
   return weight && !(decay >= 0.f && isfinite(decay)) ? LMHEAD_E_SHAPE : LMHEAD_OK;
 }
@@ -154,7 +173,7 @@ int attn_validate_desc(const attn_desc* desc) { return validate(desc); }
 
 size_t attn_workspace_bytes(const attn_desc* desc) {
   if (validate(desc) != LMHEAD_OK) return 0;
-  return std::max(attn_plan(desc, false).total, attn_plan(desc, true).total);
+  return attn_plan(desc).total;
 }
 
 int attn_fwd(const attn_desc* desc, const void* q, const void* k, const void* v, const int32_t* len_q, const int32_t* len_k, void* out,
@@ -165,7 +184,8 @@ int attn_fwd(const attn_desc* desc, const void* q, const void* k, const void* v,
   if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16) || !aligned(ws, 256)) return LMHEAD_E_ALIGN;
   rc = check_weight(weight, decay);
   if (rc != LMHEAD_OK) return rc;
-  const AttnPlan p = attn_plan(desc, false);
+  if (!different({out, lse, weight, ws}, {q, k, v, len_q, len_k})) return LMHEAD_E_SHAPE;
+  const AttnPlan p = attn_plan(desc);
   if (ws_bytes < p.total) return LMHEAD_E_WORKSPACE;
   const int esz = desc->dtype == LMHEAD_BF16 ? 2 : 4;
   AttnArgs a = arguments(desc, p, len_q, len_k, ws);
@@ -181,20 +201,20 @@ size_t attn_bwd_workspace_bytes(const attn_desc* desc) {
 int attn_bwd(const attn_desc* desc, const void* q, const void* k, const void* v, const int32_t* len_q, const int32_t* len_k,
              const void* out, const float* lse, const void* g_out, void* dq, void* dk, void* dv, void* ws, size_t ws_bytes,
              void* stream) {
-  int rc = validate(desc);
+  const int rc = validate(desc);
   if (rc != LMHEAD_OK) return rc;
   const int esz = desc->dtype == LMHEAD_BF16 ? 2 : 4;
   // gradients are written: theirs must not lie upon each other
-  rc = check_layout(desc->q, desc->B, desc->Tq, desc->Hq, desc->D, esz, true);
-  if (rc == LMHEAD_OK) rc = check_layout(desc->k, desc->B, desc->Tk, desc->Hkv, desc->D, esz, true);
-  if (rc == LMHEAD_OK) rc = check_layout(desc->v, desc->B, desc->Tk, desc->Hkv, desc->D, esz, true);
-  if (rc != LMHEAD_OK) return rc;
+  if (!apart(desc->q, desc->B, desc->Tq, desc->Hq, desc->D) || !apart(desc->k, desc->B, desc->Tk, desc->Hkv, desc->D) ||
+      !apart(desc->v, desc->B, desc->Tk, desc->Hkv, desc->D))
+    return LMHEAD_E_SHAPE;
   if (!q || !k || !v || !out || !lse || !g_out || !dq || !dk || !dv || !ws) return LMHEAD_E_NULL;
   for (const void* x : {q, k, v, out, g_out, static_cast<const void*>(dq), static_cast<const void*>(dk), static_cast<const void*>(dv)})
     if (!aligned(x, 16)) return LMHEAD_E_ALIGN;
   if (!aligned(ws, 256)) return LMHEAD_E_ALIGN;
+  if (!different({dq, dk, dv, ws}, {q, k, v, out, lse, g_out, len_q, len_k})) return LMHEAD_E_SHAPE;
   if (ws_bytes < attn_bwd_workspace_bytes(desc)) return LMHEAD_E_WORKSPACE;
-  const AttnPlan p = attn_plan(desc, false);
+  const AttnPlan p = attn_plan(desc);
   AttnArgs a = arguments(desc, p, len_q, len_k, ws);
   a.q = tensor(q, desc->q, esz), a.k = tensor(k, desc->k, esz), a.v = tensor(v, desc->v, esz), a.o = tensor(out, desc->o, esz);
   a.g = tensor(g_out, desc->o, esz);
@@ -216,9 +236,10 @@ int kv4_store(const attn_desc* desc, const void* k, const void* v, const int32_t
   if (!aligned(k, 16) || !aligned(v, 16) || !aligned(k_codes, 16) || !aligned(v_codes, 16) || !aligned(k_scales, 4) ||
       !aligned(v_scales, 4) || !aligned(ws, 256))
     return LMHEAD_E_ALIGN;
+  if (!different({k_codes, k_scales, v_codes, v_scales, ws}, {k, v, len_q, len_k})) return LMHEAD_E_SHAPE;
   if (ws_bytes < sizeof(AttnHeader)) return LMHEAD_E_WORKSPACE;
   const int esz = desc->dtype == LMHEAD_BF16 ? 2 : 4;
-  AttnArgs a = arguments(desc, attn_plan(desc, true), len_q, len_k, ws);
+  AttnArgs a = arguments(desc, attn_plan(desc), len_q, len_k, ws);
   a.k = tensor(k, desc->k, esz), a.v = tensor(v, desc->v, esz);
   uint8_t* const cache[4] = {k_codes, k_scales, v_codes, v_scales};
   LM_TRY(launch_kv4_store(desc, a, cache, static_cast<hipStream_t>(stream)));
@@ -237,7 +258,8 @@ int kv4_attn(const attn_desc* desc, const void* q, const uint8_t* k_codes, const
     return LMHEAD_E_ALIGN;
   rc = check_weight(weight, decay);
   if (rc != LMHEAD_OK) return rc;
-  const AttnPlan p = attn_plan(desc, true);
+  if (!different({out, lse, weight, ws}, {q, k_codes, k_scales, v_codes, v_scales, len_q, len_k})) return LMHEAD_E_SHAPE;
+  const AttnPlan p = attn_plan(desc);
   if (ws_bytes < p.total) return LMHEAD_E_WORKSPACE;
   const int esz = desc->dtype == LMHEAD_BF16 ? 2 : 4;
   AttnArgs a = arguments(desc, p, len_q, len_k, ws);
@@ -255,7 +277,7 @@ int cache_evict(const evict_desc* desc, const cache_plane* planes, int32_t count
   const int rc = validate_evict(desc);
   if (rc != LMHEAD_OK) return rc;
   if (!planes || !weight || !len_out || !kept || !ws) return LMHEAD_E_NULL;
-  if (count < 1 || count > EVICT_PLANES || len == len_out) return LMHEAD_E_SHAPE;
+  if (count < 1 || count > EVICT_PLANES || !different({weight, len_out, kept, ws}, {len})) return LMHEAD_E_SHAPE;
   for (int i = 0; i < count; ++i) {
     const cache_plane& p = planes[i];
     if (!p.data) return LMHEAD_E_NULL;
@@ -263,9 +285,11 @@ int cache_evict(const evict_desc* desc, const cache_plane* planes, int32_t count
     for (int64_t v : {p.seq, p.slot, p.head, p.bytes})
       if (v % 4 != 0) return LMHEAD_E_ALIGN;
     if (!aligned(p.data, 4)) return LMHEAD_E_ALIGN;
+    for (int j = 0; j < i; ++j)
+      if (planes[j].data == p.data) return LMHEAD_E_SHAPE;
+    if (!different({p.data}, {weight, len, len_out, kept, ws})) return LMHEAD_E_SHAPE;
     const attn_layout x{p.seq, p.slot, p.head};
-    if (check_layout(attn_layout{x.seq * 4, x.slot * 4, x.head * 4}, desc->B, desc->T, desc->Hkv, p.bytes * 4, 1, true) == LMHEAD_E_SHAPE)
-      return LMHEAD_E_SHAPE;
+    if (!strides(x) || !apart(x, desc->B, desc->T, desc->Hkv, p.bytes)) return LMHEAD_E_SHAPE;
   }
   if (!aligned(ws, 256)) return LMHEAD_E_ALIGN;
   if (ws_bytes < sizeof(AttnHeader)) return LMHEAD_E_WORKSPACE;

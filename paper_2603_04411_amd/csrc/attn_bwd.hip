@@ -463,9 +463,11 @@ __global__ __launch_bounds__(256) void attn_parts_kernel(AttnArgs a, KeyShares s
   using El = AttnElem<E>;
   constexpr int UNITS = 2 * DP / 4;
   constexpr int PARTS = 4;      // workgroups of a cut item
-  const int wid = blockIdx.y * kAttnRow + blockIdx.x, id = wid / PARTS;
+  const uint32_t wid = blockIdx.y * kAttnRow + blockIdx.x;
+  const int id = wid / PARTS;
   if (id >= sh.wgs) {
-    const int x = wid - PARTS * sh.wgs, item = x / a.Hkv, hk = x % a.Hkv, b = item / sh.nkey, s0 = item % sh.nkey * kKeyBlock;
+    const uint32_t x = wid - PARTS * sh.wgs;
+    const int item = x / a.Hkv, hk = x % a.Hkv, b = item / sh.nkey, s0 = item % sh.nkey * kKeyBlock;
     if (item >= a.B * sh.nkey || a.before[item + 1] != a.before[item]) return;
     for (int y = threadIdx.x; y < kKeyBlock * UNITS; y += 256) {
       const int key = s0 + y / UNITS, c = y % UNITS * 4, d = c >= DP ? c - DP : c;

@@ -57,7 +57,7 @@ struct AttnPlan {
   int nblk, nsplit;
   size_t part, logits, lse, total;     // offsets of the parts' sums, of the logits of a few rows, of lse where the caller has no use for it
 };
-AttnPlan attn_plan(const attn_desc* d, bool cache4);
+AttnPlan attn_plan(const attn_desc* d);
 
 hipError_t launch_attn_few(const attn_desc* d, const AttnPlan& p, const AttnArgs& a, hipStream_t s);   // at most kFewRows rows
 hipError_t launch_attn_fwd(const attn_desc* d, const AttnPlan& p, AttnArgs& a, hipStream_t s);
@@ -328,6 +328,10 @@ struct AttnTile {
     }
   }
 };
+
+// The exponentials are taken against a maximum that is only moved once a logit passes it by so many powers of two: the sums then
+// need no scaling in most tiles, and nothing comes near fp32's range.
+constexpr float kSlack = 8.f;
 
 // log sum exp from a maximum in powers of two and the sum of 2^(logit - maximum): rounded once, but for the sum's logarithm.
 __device__ inline float lse_of(float m, float sum) {

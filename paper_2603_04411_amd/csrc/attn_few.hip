@@ -224,25 +224,22 @@ __global__ __launch_bounds__(kFewWaves * 64, AttnElem<E>::size == 2 ? 2 : 1) voi
 #pragma unroll
           for (int i = 0; i < 4; ++i) s[nn][kb][i] = sees(16 * kb + i) ? s[nn][kb][i] : -INFINITY;
       }
-      float top = -INFINITY;
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          s[nn][kb][i] *= a.scale2;
-          top = fmaxf(top, s[nn][kb][i]);
-        }
       if (a.logits) {      // [four keys][row][key]: sixteen bytes a lane, and what a tile leaves is one piece
         const int r = nn * 16 + (l & 15);
         if (r < R) {
           f32x4_t* const to = reinterpret_cast<f32x4_t*>(a.logits) + (((int64_t)bh * logit_groups(a.Tk) + (int64_t)t * (TK / 4) + g) * R + r);
 #pragma unroll
-          for (int kb = 0; kb < KB; ++kb) to[kb * 4 * R] = s[nn][kb];
+          for (int kb = 0; kb < KB; ++kb) to[kb * 4 * R] = s[nn][kb] * a.scale2;
         }
         if (nn == NN - 1 && t + kFewWaves < t1) fetch(t + kFewWaves);
       }
-      top = max_quarters(top);
-      if (__any(top > m[nn])) {
+      float top = s[nn][0][0];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, s[nn][kb][i]);
+      top = max_quarters(top) * a.scale2;
+      if (__any(top > m[nn] + kSlack)) {
         const float now = fmaxf(m[nn], top), keep = __builtin_amdgcn_exp2f(m[nn] - (now == -INFINITY ? 0.f : now));
         m[nn] = now;
         sum[nn] *= keep;
@@ -253,10 +250,11 @@ __global__ __launch_bounds__(kFewWaves * 64, AttnElem<E>::size == 2 ? 2 : 1) voi
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          s[nn][kb][i] = __builtin_amdgcn_exp2f(s[nn][kb][i] - base);
-          sum[nn] += s[nn][kb][i];
-        }
+        for (int i = 0; i < 4; ++i) s[nn][kb][i] = __builtin_amdgcn_exp2f(fmaf(s[nn][kb][i], a.scale2, -base));
+      f32x4_t part = s[nn][0];
+#pragma unroll
+      for (int kb = 1; kb < KB; ++kb) part += s[nn][kb];
+      sum[nn] += (part.x + part.y) + (part.z + part.w);
     }
 #pragma unroll
     for (int kg = 0; kg < KB / 2; ++kg) {

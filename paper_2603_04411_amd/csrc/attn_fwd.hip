@@ -40,8 +40,6 @@ __device__ inline void load_cache(char* lds, const uint8_t* codes, const uint8_t
   }
 }
 
-constexpr float kSlack = 8.f;
-
 // One workgroup takes NW * 32 rows (query i, head g of the key head: row r = i G + g) of one key head and walks the keys that
 // they see in tiles of BK: S^T = K Q^T with the keys along the accumulators' rows, so that a lane holds one query's logits and the
 // softmax needs one exchange between lane halves; the exponentials are the second operand of O^T = V^T P^T as they lie.
@@ -150,8 +148,6 @@ __global__ __launch_bounds__(NW * 64, AttnElem<E>::size == 2 || DP == 64 ? 2 : 1
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
     top = max_halves(top) * a.scale2;
-    // The exponentials are taken against a maximum that is only moved once a logit passes it by kSlack (powers of two): the sums
-    // then need no scaling in most tiles, and nothing comes near fp32's range.
     if (__any(top > m + kSlack)) {
       const float now = fmaxf(m, top), keep = __builtin_amdgcn_exp2f(m - (now == -INFINITY ? 0.f : now));
       m = now;
