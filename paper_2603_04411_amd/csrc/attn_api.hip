@@ -9,6 +9,27 @@
 
 namespace lmhead {
 
+namespace {
+
+// The queries of a block of keys are cut for about 4096 workgroups in all, into parts of eight tiles at least; those behind the window of a
+// block with first tokens into parts of about the same length.
+void weight_parts(const attn_desc* d, AttnPlan& p) {
+  const int64_t G = d->Hq / d->Hkv, heads = (int64_t)d->B * d->Hkv, nkey = (d->Tk + kKeyBlock - 1) / kKeyBlock;
+  const int64_t all = ((int64_t)d->Tq + kQueryTile - 1) / kQueryTile * G;
+  const int64_t most = d->window ? std::min(all, (((int64_t)d->window + kKeyBlock - 1) / kQueryTile + 2) * G) : all;
+  p.main = (int)std::max<int64_t>(1, std::min(4096 / (heads * nkey), most / 8));
+  p.nsink = d->window && d->window < d->Tk ? (std::min(d->sinks, d->Tk) + kKeyBlock - 1) / kKeyBlock : 0;
+  if (p.nsink == 0) return;
+  const int64_t each = (most + p.main - 1) / p.main;
+  p.far = (int)std::max<int64_t>(1, std::min((all + each - 1) / each, 16384 / (heads * p.nsink)));
+}
+
+}  // namespace
+
+int64_t attn_weight_parts(const attn_desc* d, const AttnPlan& p) {
+  return (int64_t)p.nsink * p.far + (int64_t)(d->Tk + kKeyBlock - 1) / kKeyBlock * p.main;
+}
+
 AttnPlan attn_plan(const attn_desc* d) {
   AttnPlan p{};
   p.DP = d->D <= 64 ? 64 : 128;
@@ -35,6 +56,8 @@ AttnPlan attn_plan(const attn_desc* d) {
   };
   p.part = take(few || p.nsplit > 1 ? (size_t)wgs * p.nsplit * p.rows * (p.DP + 4) * sizeof(float) : 0);
   p.logits = take(R <= kLogitRows ? (size_t)heads * logit_groups(d->Tk) * R * 4 * sizeof(float) : 0);
+  if (R > kLogitRows) weight_parts(d, p);
+  p.sums = take(R > kLogitRows && p.main + p.nsink > 1 ? (size_t)heads * attn_weight_parts(d, p) * kKeyBlock * sizeof(float) : 0);
   p.lse = take((size_t)d->B * d->Hq * d->Tq * sizeof(float));
   p.total = off;
   return p;
@@ -135,6 +158,8 @@ int run_fwd(const attn_desc* d, const AttnPlan& p, AttnArgs& a, void* ws, float*
     return LMHEAD_OK;
   }
   // the weights need lse: where the caller does not want it, it stays in the workspace
+  a.nsink = p.nsink, a.far = p.far, a.main = p.main;
+  a.sums = p.main + p.nsink > 1 ? reinterpret_cast<float*>(base + p.sums) : nullptr;
   a.lse = lse || !weight ? lse : reinterpret_cast<float*>(base + p.lse);
   LM_TRY(rows <= kFewRows ? launch_attn_few(d, p, a, s) : launch_attn_fwd(d, p, a, s));
   if (weight) LM_TRY(launch_attn_weight(d, p, a, s));

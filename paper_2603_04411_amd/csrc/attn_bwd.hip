@@ -7,30 +7,11 @@ namespace lmhead {
 
 namespace {
 
-// How dk and dv are cut.  An item is a block of 128 keys of a key head; its tiles are the queries that see some of them, 32 of one head each: those
-// that the block reaches through its window and, for a block with first tokens, the ones behind.  Items differ in length, with the
+// How dk and dv are cut.  Items (KeyItem: a block of keys of a key head, and the queries that see it) differ in length, with the
 // window, the sequences' lengths and the first tokens, so the workgroups (as many as are resident) take equal shares of the row of all tiles.  A
 // share may begin and end inside an item: what it has of that item it leaves as fp32 sums, which attn_parts_kernel adds up in order.
 // (Eight sequences of 1024 to 4096 under a window of 1024, 28 and 4 heads: a workgroup an item, with the queries behind in items of their own, 920 us.)
-struct KeyItem {
-  int i0, main, far0, far;      // first query and tiles of a head through the window, and behind
-  __host__ __device__ int tiles() const { return main + far; }
-};
-constexpr int kKeyBlock = 128, kQueryTile = 32;
 constexpr int kLeastShare = 8;      // tiles
-
-__host__ __device__ inline KeyItem key_item(int s0, int lq, int lk, int window, int sinks) {
-  KeyItem x{0, 0, 0, 0};
-  if (s0 >= lk) return x;
-  const int offset = lk - lq, last = (lk < s0 + kKeyBlock ? lk : s0 + kKeyBlock) - 1;
-  x.i0 = s0 > offset ? s0 - offset : 0;
-  const int64_t end = (int64_t)last + window - offset;
-  const int i1 = end < lq ? (int)end : lq;
-  if (i1 > x.i0) x.main = (i1 - x.i0 + kQueryTile - 1) / kQueryTile;
-  x.far0 = i1 > x.i0 ? i1 : x.i0;
-  if (s0 < sinks && lq > x.far0) x.far = (lq - x.far0 + kQueryTile - 1) / kQueryTile;
-  return x;
-}
 
 // Up to so many queries dS goes into dk with sixteen bits instead of eight: over many queries its rounding leaves dk 1.41 times as far off as
 // the rounding of dk alone, whatever the input; over few it depends on the few that carry weight (1.7 seen).
@@ -131,6 +112,9 @@ constexpr bool kRowsInLds = AttnElem<E>::size == 2;
 // sum_j P_j k_j is added up beside dq (the same fragments of K) and taken out at the end, and dk gets the better delta.  And dS, whose few
 // large values carry dq, goes into it as a sum of two bf16 numbers.  dq of eight sequences of 4096, relative to 64 bits: 2.7e-3 off without
 // either, 2.4e-3 with the first, 1.7e-3 with both; the rounding of dq itself is 1.7e-3.
+//
+// Five products of a pair, bound by them and the exponentials.  Eight sequences of 1024 to 4096 under a window of 1024, 28 and 4 heads of 128:
+// 620 to 710 us.
 template <typename E, int DP, int BK>
 __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dq_kernel(AttnArgs a, int nkey) {
   using El = AttnElem<E>;
@@ -278,6 +262,9 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dq_kernel(Att
 
 // A wavefront holds 32 keys and their values; the workgroup's four walk the queries that see them, head by head, in tiles of 32.  S and dP
 // have the queries along the accumulators' rows, so P and dS are operands of dV^T = g^T P and dK^T = Q^T dS as they lie.
+//
+// Four products of a pair, bound by reads of LDS beside them (q and g are read along rows and across).  The sequences above: 670 to 740 us.
+// (64 keys a wavefront, which halves those reads, takes 512 registers and one wavefront a unit, and was slower by a tenth.)
 template <typename E, int DP, bool kFine>
 __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dkv_kernel(AttnArgs a, KeyShares sh) {
   using El = AttnElem<E>;
@@ -457,7 +444,8 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dkv_kernel(At
 }
 
 // Items that were cut: the workgroup whose share has the beginning adds up the parts, which lie with the shares that follow.  And blocks of
-// keys without any tile, which no share has, become zeros (workgroups from sh.wgs on, one for each block of a key head).
+// keys without any tile, which no share has, become zeros (workgroups from sh.wgs on, one for each block of a key head).  Bound by reading
+// the parts, 128 KB each and at most two for each of 512 workgroups: 37 us (a workgroup an item: 110).
 template <typename E, int DP>
 __global__ __launch_bounds__(256) void attn_parts_kernel(AttnArgs a, KeyShares sh) {
   using El = AttnElem<E>;

@@ -20,7 +20,8 @@ __device__ inline uint32_t e2m1(float y) {     // y = |x| / 2^e <= 6: between tw
   return (y > 0.25f) + (y >= 0.75f) + (y > 1.25f) + (y >= 1.75f) + (y > 2.5f) + (y >= 3.5f) + (y > 5.f);
 }
 
-// Four lanes make a block of 32, eight values each.
+// Four lanes make a block of 32, eight values each: its maximum takes two exchanges, its codes are a word a lane.  A step's rows are few: it is
+// the launch (4 us).  A prompt's are bound by their reading.
 template <typename E>
 __global__ __launch_bounds__(256) void kv4_store_kernel(StoreArgs a) {
   using El = AttnElem<E>;
@@ -91,6 +92,9 @@ __device__ inline uint32_t order_of(float x) {
 // One workgroup finds what a key head keeps: the threshold by four passes over eight bits each, then the tokens above it and the first of
 // those at it, in order.  kHold: values that a thread holds on to over the passes, so that the weights are read once (of more than
 // 1024 * kHold tokens they are read again for each pass).
+//
+// A key head is one workgroup's, since a pass has to know the one before: bound by the chain of passes (a count of 256 bins each, their sum, the
+// ranks), 7 us of 1024 tokens, 23 of 8192.
 template <int kHold>
 __global__ __launch_bounds__(1024) void evict_choose_kernel(EvictArgs a) {
   __shared__ uint32_t hist[4][256];      // of four wavefronts each: the frequent digits are few
@@ -229,6 +233,9 @@ struct MoveArgs {
 // Rows close up in place.  A workgroup takes rows in ascending order, and a row only moves towards the front: what a step reads lies at or
 // behind everything that it and the steps before it write, so a step reads all of its rows, waits, and writes them.  Slices of the
 // rows' columns are independent of each other and go to workgroups of their own.
+//
+// Bound by the rows that move, read and written once, and by the steps' waits where few workgroups have long columns.  32 sequences of 4096 to
+// 8192 tokens, 8 heads, half of them kept: 40 to 50 us where the kept rows lie in front already, 140 where they have to close up.
 template <typename W>
 __global__ __launch_bounds__(256) void evict_move_kernel(MoveArgs a) {
   constexpr int U = 8;      // units a thread and step
@@ -306,8 +313,8 @@ hipError_t launch_evict(const evict_desc& d, const cache_plane* planes, int coun
     m.plane[i] = p;
     wide = wide && (reinterpret_cast<uintptr_t>(p.data) | p.seq | p.slot | p.head | p.bytes) % 16 == 0;
   }
-  // Slices of at least 64 bytes, as many as keep 1024 workgroups busy (2 sequences of 1024 tokens, 8 heads of 256 bytes in two planes: 20 us
-  // in one slice).
+  // Slices of at least 64 bytes, as many as keep 1024 workgroups busy (2 sequences of 1024 tokens, 8 heads of 256 bytes in two planes: 5 us, in
+  // one slice 20).
   const int64_t most = (1024 + (int64_t)d.B * d.Hkv * count - 1) / ((int64_t)d.B * d.Hkv * count);
   for (int i = 0; i < count; ++i) {
     m.parts[i] = (int)std::max<int64_t>(1, std::min<int64_t>(most, planes[i].bytes / 64));

@@ -39,6 +39,9 @@ struct AttnArgs {
   bool past;                // few rows: read K and V past the caches
   float* logits;            // of a few rows: [b][key head][key][row], for the weights
   float* part;              // [b][key head][split][row of the block-padded rows]{DP sums, maximum, sum}
+  // weights of more rows than a few: see attn_weight_kernel
+  int nsink, far, main;     // blocks with first tokens, parts of their queries behind the window, parts of a block's others
+  float* sums;              // [b][key head][part][128], or null: one part, and the weights are written at once
   // backward
   AttnTensor g, dq, dk, dv;
   float* delta;             // [b][head][query]
@@ -55,9 +58,12 @@ struct AttnPlan {
   int DP;            // width of a head in the kernels: 64 or 128
   int rows;          // rows (query, head of the key head) of a workgroup
   int nblk, nsplit;
-  size_t part, logits, lse, total;     // offsets of the parts' sums, of the logits of a few rows, of lse where the caller has no use for it
+  int nsink, far, main;                // how the weights of more rows are cut
+  // offsets of the parts' sums, of the logits of a few rows, of the weights' sums, of lse where the caller has no use for it
+  size_t part, logits, sums, lse, total;
 };
 AttnPlan attn_plan(const attn_desc* d);
+int64_t attn_weight_parts(const attn_desc* d, const AttnPlan& p);      // of a key head, over all blocks
 
 hipError_t launch_attn_few(const attn_desc* d, const AttnPlan& p, const AttnArgs& a, hipStream_t s);   // at most kFewRows rows
 hipError_t launch_attn_fwd(const attn_desc* d, const AttnPlan& p, AttnArgs& a, hipStream_t s);
@@ -75,8 +81,26 @@ static inline dim3 attn_grid(int64_t wgs) {
   return dim3((unsigned)(wgs < kAttnRow ? wgs : kAttnRow), (unsigned)((wgs + kAttnRow - 1) / kAttnRow));
 }
 
-// Instruction kinds of __builtin_amdgcn_sched_group_barrier.
-constexpr int kMfma = 0x008, kDsRead = 0x100, kValu = 0x002, kTrans = 0x400;
+// A block of 128 keys of a key head, and the queries that see some of them in tiles of 32 of one head: those that the block reaches through its
+// window and, for a block with first tokens, the ones behind.
+struct KeyItem {
+  int i0, main, far0, far;      // first query and tiles of a head through the window, and behind
+  __host__ __device__ int tiles() const { return main + far; }
+};
+constexpr int kKeyBlock = 128, kQueryTile = 32;
+
+__host__ __device__ inline KeyItem key_item(int s0, int lq, int lk, int window, int sinks) {
+  KeyItem x{0, 0, 0, 0};
+  if (s0 >= lk) return x;
+  const int offset = lk - lq, last = (lk < s0 + kKeyBlock ? lk : s0 + kKeyBlock) - 1;
+  x.i0 = s0 > offset ? s0 - offset : 0;
+  const int64_t end = (int64_t)last + window - offset;
+  const int i1 = end < lq ? (int)end : lq;
+  if (i1 > x.i0) x.main = (i1 - x.i0 + kQueryTile - 1) / kQueryTile;
+  x.far0 = i1 > x.i0 ? i1 : x.i0;
+  if (s0 < sinks && lq > x.far0) x.far = (lq - x.far0 + kQueryTile - 1) / kQueryTile;
+  return x;
+}
 
 // ---- device side --------------------------------------------------------------------------
 
@@ -198,8 +222,6 @@ struct AttnElem<f32_tag> {
     *reinterpret_cast<f32x4_t*>(p) = f32x4_t{a, b, c, d};
   }
 };
-
-typedef __attribute__((address_space(3))) char lds_char;
 
 // A transposing read.  With nothing known of its memory the compiler has it wait for all loads into LDS on their way, the next tile's too;
 // `restrict` is what it needs to know (kernels wait for a tile themselves).

@@ -40,9 +40,17 @@ __device__ inline void load_cache(char* lds, const uint8_t* codes, const uint8_t
   }
 }
 
+// O = softmax(scale Q K^T) V in one pass over the keys, with the running maximum and sum of each row.
+//
 // One workgroup takes NW * 32 rows (query i, head g of the key head: row r = i G + g) of one key head and walks the keys that
 // they see in tiles of BK: S^T = K Q^T with the keys along the accumulators' rows, so that a lane holds one query's logits and the
 // softmax needs one exchange between lane halves; the exponentials are the second operand of O^T = V^T P^T as they lie.
+//
+// Bound by the matrix cores and the exponentials, whose instructions overlap only so far (matrix cores busy 55 % of the time, the other units
+// 52 %, both at once 20 %).  32 and 8 heads of 128, 4 sequences of 4096: 535 us, 1.0 PFLOP/s over the pairs that are seen; 8 of
+// 512 to 2048: 157 us (263 with a key head's workgroups on all XCDs, 160 with the compiler's order of a tile's steps); 40 and 8 heads, 4 of
+// 1024 to 8192 under a window of 1024: 440 to 570 us, as the clocks allow.
+// The grid is a workgroup for 128 rows, the last ones (which see most) first; where that leaves compute units idle the keys are cut.
 template <typename E, int DP, int NW, int BK, bool kCache>
 __global__ __launch_bounds__(NW * 64, AttnElem<E>::size == 2 || DP == 64 ? 2 : 1) void attn_fwd_kernel(AttnArgs a) {
   using El = AttnElem<E>;
@@ -266,7 +274,7 @@ __global__ __launch_bounds__(NW * 64, AttnElem<E>::size == 2 || DP == 64 ? 2 : 1
   if (a.lse && l < 32) a.lse[((int64_t)b * a.Hq + head) * a.Tq + qi] = lse_of(m, sum);
 }
 
-// Joins the parts of a row: a wavefront each.
+// Joins the parts of a row, sums and maxima of which it reads once: a wavefront each.  (Of a launch that did not fill the card, so short.)
 template <typename E, int DP>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int rows) {
   const int l = threadIdx.x & 63;
@@ -301,83 +309,136 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int rows) {
 }
 
 // Weight that the keys got: S = Q K^T with the queries along the accumulators' rows, so that a lane adds up one key's column.  A workgroup
-// takes four times 32 keys of a key head and goes through the queries that see them, head by head, in tiles of 32.
+// takes a block of 128 keys of a key head (a wavefront 32 of them, in registers) and a part of the queries that see it, head by head in tiles
+// of 32, one tile ahead in LDS.  The queries behind the window that see a block's first tokens are parts of their own.
+//
+// Bound by the exponentials and the masks beside one product.  4 sequences of 8192 under a window of 1024 with 28 and 4 heads of 128: 340 us (a
+// workgroup a block of keys, one tile at a time: 2440, as long as the block of the first tokens takes); 8 of 2048 without: 180 (546).
 template <typename E, int DP, bool kCache>
-__global__ __launch_bounds__(256) void attn_weight_kernel(AttnArgs a, int nkey) {
+__global__ __launch_bounds__(256) void attn_weight_kernel(AttnArgs a, int parts) {
   using El = AttnElem<E>;
   using Frag = typename El::Frag;
-  using Tile = AttnTile<E, DP, 32>;
+  using Tile = AttnTile<E, DP, kQueryTile>;
   constexpr int KS = Tile::KS;
   extern __shared__ char lds[];
-  __shared__ float ends[32], lows[32];
+  __shared__ __attribute__((aligned(16))) float ends[2][kQueryTile], lows[2][kQueryTile];
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Work work;
-  if (!attn_work(a.B * a.Hkv, nkey, work)) return;
+  if (!attn_work(a.B * a.Hkv, parts, work)) return;
   const uint32_t bh = work.bh;
-  const int blk = work.in, hk = uniform(bh % a.Hkv), b = uniform(bh / a.Hkv);
+  const int hk = uniform(bh % a.Hkv), b = uniform(bh / a.Hkv);
   const int lq = clamp_len(a.len_q, b, a.Tq), lk = clamp_len(a.len_k, b, a.Tk);
-  const int s0 = blk * 128, key = s0 + w * 32 + (l & 31);
+  const int behind = a.nsink * a.far;
+  const bool far = (int)work.in < behind;
+  const uint32_t x = far ? work.in : work.in - behind, cut = far ? a.far : a.main;
+  const int blk = uniform(x / cut), part = uniform(x % cut);
+  const int s0 = blk * kKeyBlock, k0 = s0 + w * 32, key = k0 + (l & 31);
   const uint32_t rbase = Tile::row_base(l);
   if (s0 >= lk) return;
-  Frag k[KS];
-  if constexpr (kCache) {
-    // through LDS, a wavefront's rows at a time
-    for (int x = 0; x < 4; ++x) {
-      const int64_t row = (int64_t)bh * a.Tk + s0 + x * 32;
-      __syncthreads();
-      load_cache<Tile, 4, 32>(lds, a.k_codes + row * (a.D / 2), a.k_scales + row * (a.D / 32), lk - s0 - x * 32, a.D, w, l);
-      __syncthreads();
-      if (w == x) {
+  const KeyItem item = key_item(s0, lq, lk, a.window, a.sinks);
+  // the part's tiles, of all heads
+  const int run = far ? item.far : item.main, begin = far ? item.far0 : item.i0, end = far ? lq : item.far0;
+  const int64_t all = (int64_t)run * a.G;
+  const int t0 = uniform((int)(all * part / cut)), t1 = uniform((int)(all * (part + 1) / cut));
+  float sum[2] = {0.f, 0.f};
+  if (t0 < t1) {
+    Frag k[KS];
+    if constexpr (kCache) {
+      // through LDS, a wavefront's rows at a time
+      for (int y = 0; y < 4; ++y) {
+        const int64_t row = (int64_t)bh * a.Tk + s0 + y * 32;
+        __syncthreads();
+        load_cache<Tile, 4, 32>(lds, a.k_codes + row * (a.D / 2), a.k_scales + row * (a.D / 32), lk - s0 - y * 32, a.D, w, l);
+        __syncthreads();
+        if (w == y) {
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) k[ks] = Tile::row_frag(lds, rbase, 0, ks);
+          for (int ks = 0; ks < KS; ++ks) k[ks] = Tile::row_frag(lds, rbase, 0, ks);
+        }
+      }
+      __syncthreads();
+    } else {
+      const char* src = a.k.p + b * a.k.seq + (int64_t)key * a.k.slot + hk * a.k.head;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const int d = 16 * ks + 8 * (l >> 5);
+        k[ks] = key < lk && d < a.D ? El::load(src + d * El::size) : El::zero();
       }
     }
-    __syncthreads();
-  } else {
-    const char* src = a.k.p + b * a.k.seq + (int64_t)key * a.k.slot + hk * a.k.head;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      const int d = 16 * ks + 8 * (l >> 5);
-      k[ks] = key < lk && d < a.D ? El::load(src + d * El::size) : El::zero();
-    }
-  }
-  float sum = 0.f;
-  // queries from the first at or behind the first key to the last whose window reaches the last one, or to the end
-  const int off = lk - lq, end_key = min(lk, s0 + 128) - 1;
-  const int i0 = max(0, s0 - off);
-  const int i1 = s0 < a.sinks ? lq : (int)min((int64_t)lq, (int64_t)end_key + a.window - off);
-  for (int g = 0; g < a.G; ++g) {
-    const int head = hk * a.G + g;
-    const char* qbase = a.q.p + b * a.q.seq + head * a.q.head;
-    for (int i = i0; i < i1; i += 32) {
-      __syncthreads();
-      Tile::template load<4>(lds, qbase + i * a.q.slot, (uint32_t)a.q.slot, lq - i, a.D * El::size, w, l);
-      if (threadIdx.x < 32) {
-        const int qi = i + threadIdx.x;
-        const float lse = qi < lq ? a.lse[((int64_t)b * a.Hq + head) * a.Tq + qi] : -INFINITY;
+    const int offset = lk - lq;
+    int head = hk * a.G + t0 / run, i = begin + t0 % run * kQueryTile;      // of the tile that is loaded next
+    float lse = 0.f;
+    auto load = [&](int at) {
+      Tile::template load<4>(lds + at * Tile::BYTES, a.q.p + b * a.q.seq + head * a.q.head + i * a.q.slot, (uint32_t)a.q.slot, end - i,
+                             a.D * El::size, w, l);
+      if (threadIdx.x < kQueryTile) lse = i + (int)threadIdx.x < end ? a.lse[((int64_t)b * a.Hq + head) * a.Tq + i + threadIdx.x] : -INFINITY;
+    };
+    load(0);
+    for (int t = t0; t < t1; ++t) {
+      const int at = (t - t0) & 1, i0 = i;
+      if (threadIdx.x < kQueryTile) {
         const Ends e(lse);
-        ends[threadIdx.x] = e.a, lows[threadIdx.x] = e.b;
+        ends[at][threadIdx.x] = e.a, lows[at][threadIdx.x] = e.b;
       }
       __builtin_amdgcn_s_waitcnt(kWaitVm0);
       __syncthreads();
+      i += kQueryTile;
+      if (i >= end) i = begin, ++head;
+      if (t + 1 < t1) load(1 - at);
+      const char* const q = lds + at * Tile::BYTES;
       f32x16_t s;
 #pragma unroll
-      for (int x = 0; x < 16; ++x) s[x] = 0.f;
+      for (int y = 0; y < 16; ++y) s[y] = 0.f;
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) El::mma(s, Tile::row_frag(lds, rbase, 0, ks), k[ks]);
+      for (int ks = 0; ks < KS; ++ks) El::mma(s, Tile::row_frag(q, rbase, 0, ks), k[ks]);
+      float e[16];
 #pragma unroll
-      for (int x = 0; x < 16; ++x) {
-        const int row = acc_row(x, l);
-        const float e = __builtin_amdgcn_exp2f(fmaf(s[x], a.scale2, -ends[row]) - lows[row]);
-        sum += ((i + row < lq) & seen(key, off + i + row, a.window, a.sinks)) ? e : 0.f;
+      for (int y = 0; y < 16; y += 4) {
+        const f32x4_t hi = *reinterpret_cast<const f32x4_t*>(&ends[at][acc_row(y, l)]);
+#pragma unroll
+        for (int z = 0; z < 4; ++z) e[y + z] = fmaf(s[y + z], a.scale2, -hi[z]);
+        if constexpr (El::size == 4) {
+          const f32x4_t lo = *reinterpret_cast<const f32x4_t*>(&lows[at][acc_row(y, l)]);
+#pragma unroll
+          for (int z = 0; z < 4; ++z) e[y + z] -= lo[z];
+        }
+      }
+      const int p0 = offset + i0;
+      if (i0 + kQueryTile <= end && all_seen(k0, 32, p0, p0 + kQueryTile - 1, a.window, a.sinks)) {
+#pragma unroll
+        for (int y = 0; y < 16; ++y) sum[y & 1] += __builtin_amdgcn_exp2f(e[y]);
+      } else {
+#pragma unroll
+        for (int y = 0; y < 16; ++y) {
+          const int row = acc_row(y, l);
+          const float v = __builtin_amdgcn_exp2f(e[y]);
+          sum[y & 1] += ((i0 + row < end) & seen(key, p0 + row, a.window, a.sinks)) ? v : 0.f;
+        }
       }
     }
   }
-  sum = add_halves(sum);
-  if (l < 32 && key < lk) {
+  const float mine = add_halves(sum[0] + sum[1]);
+  if (l >= 32) return;
+  if (a.sums) {
+    a.sums[((int64_t)bh * parts + work.in) * kKeyBlock + w * 32 + l] = mine;
+  } else if (key < lk) {
     float* const to = a.weight + (int64_t)bh * a.Tk + key;
-    *to = a.decay == 0.f ? sum : fmaf(a.decay, *to, sum);
+    *to = a.decay == 0.f ? mine : fmaf(a.decay, *to, mine);
   }
+}
+
+// Adds up the parts of a block of keys, in order.
+__global__ __launch_bounds__(kKeyBlock) void attn_weight_sum_kernel(AttnArgs a, int parts, int nkey) {
+  const int64_t x = (int64_t)blockIdx.y * kAttnRow + blockIdx.x, bh = x / nkey;
+  if (bh >= (int64_t)a.B * a.Hkv) return;
+  const int blk = (int)(x % nkey), key = blk * kKeyBlock + threadIdx.x;
+  if (key >= clamp_len(a.len_k, (int)(bh / a.Hkv), a.Tk)) return;
+  const float* const from = a.sums + bh * parts * kKeyBlock + threadIdx.x;
+  float sum = 0.f;
+  if (blk < a.nsink)
+    for (int y = 0; y < a.far; ++y) sum += from[((int64_t)blk * a.far + y) * kKeyBlock];
+  for (int y = 0; y < a.main; ++y) sum += from[((int64_t)a.nsink * a.far + (int64_t)blk * a.main + y) * kKeyBlock];
+  float* const to = a.weight + bh * a.Tk + key;
+  *to = a.decay == 0.f ? sum : fmaf(a.decay, *to, sum);
 }
 
 template <typename E, int DP, int NW, int BK, bool kCache>
@@ -400,10 +461,14 @@ hipError_t fwd_rows(const AttnPlan& p, const AttnArgs& a, hipStream_t s) {
 }
 
 template <typename E, int DP, bool kCache>
-hipError_t weight(const AttnArgs& a, hipStream_t s) {
+hipError_t weight(const attn_desc* d, const AttnPlan& p, const AttnArgs& a, hipStream_t s) {
   constexpr auto kernel = attn_weight_kernel<E, DP, kCache>;
-  const int bytes = AttnTile<E, DP, 32>::BYTES, nkey = (a.Tk + 127) / 128;
-  kernel<<<attn_grid(attn_wgs((int64_t)a.B * a.Hkv, nkey)), 256, bytes, s>>>(a, nkey);
+  const int bytes = 2 * AttnTile<E, DP, kQueryTile>::BYTES, nkey = (a.Tk + kKeyBlock - 1) / kKeyBlock;
+  const int64_t heads = (int64_t)a.B * a.Hkv, parts = attn_weight_parts(d, p);
+  kernel<<<attn_grid(attn_wgs(heads, parts)), 256, bytes, s>>>(a, (int)parts);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !a.sums) return e;
+  attn_weight_sum_kernel<<<attn_grid(heads * nkey), kKeyBlock, 0, s>>>(a, (int)parts, nkey);
   return hipGetLastError();
 }
 
@@ -422,11 +487,11 @@ hipError_t launch_attn_fwd(const attn_desc* d, const AttnPlan& p, AttnArgs& a, h
 hipError_t launch_attn_weight(const attn_desc* d, const AttnPlan& p, AttnArgs& a, hipStream_t s) {
   const bool c = a.k_codes != nullptr;
   if (d->dtype == LMHEAD_BF16) {
-    if (p.DP == 64) return c ? weight<bf16_tag, 64, true>(a, s) : weight<bf16_tag, 64, false>(a, s);
-    return c ? weight<bf16_tag, 128, true>(a, s) : weight<bf16_tag, 128, false>(a, s);
+    if (p.DP == 64) return c ? weight<bf16_tag, 64, true>(d, p, a, s) : weight<bf16_tag, 64, false>(d, p, a, s);
+    return c ? weight<bf16_tag, 128, true>(d, p, a, s) : weight<bf16_tag, 128, false>(d, p, a, s);
   }
-  if (p.DP == 64) return c ? weight<f32_tag, 64, true>(a, s) : weight<f32_tag, 64, false>(a, s);
-  return c ? weight<f32_tag, 128, true>(a, s) : weight<f32_tag, 128, false>(a, s);
+  if (p.DP == 64) return c ? weight<f32_tag, 64, true>(d, p, a, s) : weight<f32_tag, 64, false>(d, p, a, s);
+  return c ? weight<f32_tag, 128, true>(d, p, a, s) : weight<f32_tag, 128, false>(d, p, a, s);
 }
 
 }  // namespace lmhead

@@ -225,3 +225,17 @@ def test_bits_are_the_same_from_run_to_run():
         p.fwd(decay=0.0)
         p.bwd(p.out)
         assert all(torch.equal(a, b) for a, b in zip(first, [p.out, p.lse, p.weight, p.dq, p.dk, p.dv]))
+
+
+LONG = [      # queries that the weights' pass cuts: with a window and blocks of first tokens, without, in fp32, padded
+    dict(B=1, Tq=900, Tk=1300, Hq=4, Hkv=2, D=128, window=100, sinks=140),
+    dict(B=2, Tq=700, Tk=700, Hq=7, Hkv=1, D=64, len_q=[700, 333], len_k=[700, 333]),
+    dict(B=2, Tq=600, Tk=1000, Hq=2, Hkv=2, D=72, window=64, sinks=3, len_q=[600, 1], len_k=[1000, 900]),
+    dict(B=1, Tq=500, Tk=900, Hq=2, Hkv=1, D=128, dtype="f32", window=300, sinks=1),
+    dict(B=3, Tq=400, Tk=500, Hq=2, Hkv=1, D=40, window=1, sinks=129, len_q=[400, 0, 7], len_k=[300, 500, 0]),
+]
+
+
+@pytest.mark.parametrize("case", LONG, ids=_name)
+def test_weights_of_long_prompts(case):
+    check_fwd(Problem(seed=21, **case), decay=0.75)

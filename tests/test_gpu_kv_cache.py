@@ -244,3 +244,9 @@ def test_eviction_takes_lengths_out_of_range_as_the_nearest():
     L.cache_evict(desc, L.make_cache_planes([x]), weight, torch.tensor([41, -1, 5], **i32), lens_out, kept, ws)
     assert L.lmhead_check(ws) == -6 and lens_out.tolist() == [10, 0, 5]
     assert (kept[1] == -1).all() and kept[2, 0].tolist() == [0, 1, 2, 3, 4] + [-1] * 5
+
+
+@pytest.mark.parametrize("case", [dict(B=1, Tq=300, Tk=800, Hq=4, Hkv=2, D=96, window=200, sinks=130), dict(B=2, Tq=500, Tk=500, Hq=2, Hkv=1, D=32, dtype="f32")],
+                         ids=_name)
+def test_weights_of_long_prompts_over_codes(case):
+    test_store_and_attention(case)
