@@ -7,7 +7,8 @@ One step = one pass over one layer's key (or value) stream of n tokens, all tens
     segments) -> dynakv_reconstruct (x_bar = x^[0:k] U^-1[0:k, :] for every token).
 Prints ONE JSON line: tokens/s of the step, a `roofline` object for the kernel that takes the most
 time (timed with HIP events inside the library, on the launch stream) and a `cpu_baseline` object
-(the fp64 oracle on a bounded token sample).
+(the fp64 oracle on a bounded token sample).  --backward times the training pair; --decode what comes after:
+one step of decoding over the reconstructed keys and values, in their type, in 4 bits and after eviction.
 """
 from __future__ import annotations
 
@@ -208,6 +209,60 @@ def backward_main(args, cfg, inp, L, desc, params, ws, xt, k) -> int:
     return 0
 
 
+def decode_main(args, cfg, L, xbar, ws) -> int:
+    """One layer's share of a decoding step for each sequence: attention of one token (four query heads a key head) with the keys' weights, the same over
+    the cache in 4 bits, the same after eviction of half the tokens; and the eviction itself, with nothing left to move after the first time."""
+    import torch
+    B, heads, D = args.decode, cfg.d // 128, 128
+    T = cfg.n // B
+    if cfg.d % D or T < 2:
+        print("bench_dynakv.py: --decode takes heads of 128 and at least two tokens a sequence", file=sys.stderr)
+        return 2
+    k = xbar[:B * T].view(B, T, heads, D)
+    v = k.flip(1).contiguous()
+    q = torch.randn(B, 1, 4 * heads, D, device="cuda", generator=torch.Generator(device="cuda").manual_seed(0)).to(k.dtype)
+    out, weight = torch.empty_like(q), torch.zeros(B, heads, T, device="cuda")
+    desc = L.make_attn_desc(B, 1, T, 4 * heads, heads, D, cfg.dtype)
+    fill = L.make_attn_desc(B, T, T, 4 * heads, heads, D, cfg.dtype)
+    ws_a = torch.empty(max(L.attn_workspace_bytes(desc), L.attn_workspace_bytes(fill)), dtype=torch.uint8, device="cuda")
+    cache = [torch.empty(B, heads, T, w, dtype=torch.uint8, device="cuda") for w in (D // 2, D // 32) * 2]
+    ev = L.make_evict_desc(B, T, heads, T // 2, sinks=min(4, T // 4), recent=T // 8)
+    left, kept = (torch.empty(s, dtype=torch.int32, device="cuda") for s in ((B,), (B, heads, T // 2)))
+    full = torch.full((B,), T, dtype=torch.int32, device="cuda")
+    planes = L.make_cache_planes([k, v])
+
+    def timed(f):
+        for _ in range(args.warmup):
+            f()
+        torch.cuda.synchronize()
+        t0 = time.perf_counter()
+        for _ in range(args.steps):
+            f()
+        torch.cuda.synchronize()
+        return (time.perf_counter() - t0) * 1e3 / args.steps
+
+    def attend(n):
+        return timed(lambda: L.attn_fwd(desc, q, k, v, None, n, out, None, weight, 0.5, ws_a))
+    ms = {"attn_fwd with weights": attend(full)}
+    L.kv4_store(fill, k, v, None, full, *cache, ws_a)
+    ms["kv4_attn with weights"] = timed(lambda: L.kv4_attn(desc, q, *cache, None, full, out, None, weight, 0.5, ws_a))
+    ms["cache_evict"] = timed(lambda: L.cache_evict(ev, planes, weight, full, left, kept, ws_a))
+    ms["attn_fwd with weights, half the tokens"] = attend(left)
+    if L.dynakv_check(ws) != 0 or L.lmhead_check(ws_a) != 0:
+        print("bench_dynakv.py: device-side range error", file=sys.stderr)
+        return 4
+    first = ms["attn_fwd with weights"]
+    read = 2 * B * T * heads * D * k.element_size() / (first * 1e-3) / 1e9
+    print(json.dumps({
+        "metric": "sequences/s, one layer's attention of one token over its cache with the keys' weights (1 GPU)",
+        "value": B / (first * 1e-3), "unit": "sequences/s", "n_gpus": 1, "steps": args.steps, "warmup": args.warmup, "ms_per_step": first,
+        "higher_is_better": True, "scaling": "weak", "vs_baseline": None, "dtype": cfg.dtype, "data": "synthetic",
+        "config": {"workload": f"kv_configs[{args.config}] {cfg.name}", "sequences": B, "tokens": T, "key_heads": heads, "query_heads": 4 * heads, "head": D},
+        "cache_gbs": read, "ms": ms,
+    }), flush=True)
+    return 0
+
+
 def main(argv=None) -> int:
     ap = argparse.ArgumentParser()
     ap.add_argument("--gpus", type=int, default=1)
@@ -218,6 +273,9 @@ def main(argv=None) -> int:
     ap.add_argument("--calibrate-copy", action="store_true")
     ap.add_argument("--backward", action="store_true",
                     help="time the training pair dynakv_gate + dynakv_gate_bwd instead of gate + store + reconstruction")
+    ap.add_argument("--decode", type=int, default=0, metavar="SEQUENCES",
+                    help="time one token's attention over the reconstructed stream, taken as the keys (and, in another order, the values) of so "
+                         "many sequences with heads of 128")
     args = ap.parse_args(argv)
     if args.gpus != 1:
         print("bench_dynakv.py: this build runs on ONE GPU only; use --gpus 1", file=sys.stderr)
@@ -257,6 +315,12 @@ def main(argv=None) -> int:
         del src, dst
     if args.backward:
         return backward_main(args, cfg, inp, L, desc, (x, U, W, b), ws, xt, k)
+
+    if args.decode:
+        L.dynakv_gate(desc, x, U, W, b, cfg.tau, xt, k, None, None, ws)
+        L.dynakv_store(desc, xt, k, 0, off, packed, n * d, ws)
+        L.dynakv_reconstruct(desc, packed, n * d, off, k, Ui, xbar, ws)
+        return decode_main(args, cfg, L, xbar, ws)
 
     def step():
         L.dynakv_gate(desc, x, U, W, b, cfg.tau, xt, k, None, None, ws)
