@@ -56,8 +56,8 @@ AttnPlan attn_plan(const attn_desc* d) {
   };
   p.part = take(few || p.nsplit > 1 ? (size_t)wgs * p.nsplit * p.rows * (p.DP + 4) * sizeof(float) : 0);
   p.logits = take(R <= kLogitRows ? (size_t)heads * logit_groups(d->Tk) * R * 4 * sizeof(float) : 0);
-  if (R > kLogitRows) weight_parts(d, p);
-  p.sums = take(R > kLogitRows && p.main + p.nsink > 1 ? (size_t)heads * attn_weight_parts(d, p) * kKeyBlock * sizeof(float) : 0);
+  if (d->Tq >= kQueryTile) weight_parts(d, p);
+  p.sums = take(d->Tq >= kQueryTile && R > kLogitRows && p.main + p.nsink > 1 ? (size_t)heads * attn_weight_parts(d, p) * kKeyBlock * sizeof(float) : 0);
   p.lse = take((size_t)d->B * d->Hq * d->Tq * sizeof(float));
   p.total = off;
   return p;

@@ -11,23 +11,29 @@ namespace {
 // window, the sequences' lengths and the first tokens, so the workgroups (as many as are resident) take equal shares of the row of all tiles.  A
 // share may begin and end inside an item: what it has of that item it leaves as fp32 sums, which attn_parts_kernel adds up in order.
 // (Eight sequences of 1024 to 4096 under a window of 1024, 28 and 4 heads: a workgroup an item, with the queries behind in items of their own, 920 us.)
-constexpr int kLeastShare = 8;      // tiles
 
 // Up to so many queries dS goes into dk with sixteen bits instead of eight: over many queries its rounding leaves dk 1.41 times as far off as
 // the rounding of dk alone, whatever the input; over few it depends on the few that carry weight (1.7 seen).
 constexpr int kFineQueries = 512;
 
+// Least tiles of a share, where there are fewer than the card takes: a tile is 2 us in bf16 and 7 in fp32, and a part that is cut off is 128 KB
+// to write and to read again.  (2 sequences of 33, 8 heads of one key head of 96 in fp32: 70 us the whole step, with 8 tiles 120; 8 of 128, bf16
+// heads of 128: 65 and 71; 8 of 512: 134, but 137 in shares of 4 or 5.  So shares of up to twice that are made fewer, down to kFirstShares.)
+constexpr int kLeastShare = 4, kLeastShareF32 = 2, kFirstShares = 256;
+constexpr int kSumGroups = 8;       // workgroups that add up a cut item: with 4 they take twice as long for short sequences
+
 // How many workgroups there are, and whether each has one item (short ones are not cut).
 struct KeyShares {
-  int nkey, wgs;
+  int nkey, wgs, least;     // least: tiles of a share
   bool whole;
 };
 KeyShares key_shares(const attn_desc* d, int resident) {
   KeyShares k{};
   k.nkey = (d->Tk + kKeyBlock - 1) / kKeyBlock;
   const int64_t G = d->Hq / d->Hkv, each = ((int64_t)d->Tq + kQueryTile - 1) / kQueryTile + 1, items = (int64_t)d->B * d->Hkv * k.nkey;
-  k.whole = each * G <= kLeastShare;
-  k.wgs = (int)(k.whole ? items : items >= resident ? resident : (items * each * G + kLeastShare - 1) / kLeastShare);
+  k.least = d->dtype == LMHEAD_BF16 ? kLeastShare : kLeastShareF32;
+  k.whole = each * G <= k.least;
+  k.wgs = (int)(k.whole ? items : items >= resident ? resident : (items * each * G + k.least - 1) / k.least);
   if (!k.whole && k.wgs > resident) k.wgs = resident;
   k.wgs = (k.wgs + 7) / 8 * 8;
   return k;
@@ -92,10 +98,12 @@ __device__ inline bool next_piece(const AttnArgs& a, int nkey, Share& x) {
   x.at += x.to - x.from;
   return true;
 }
-__device__ inline void share_of(const AttnArgs& a, int nkey, int wg, int wgs, Share& x) {
-  const int64_t all = a.before[a.B * nkey] * a.G * a.Hkv;
-  int64_t each = (all + wgs - 1) / wgs;
-  if (each < kLeastShare) each = kLeastShare;
+__device__ inline void share_of(const AttnArgs& a, const KeyShares& sh, int wg, Share& x) {
+  const int64_t all = a.before[a.B * sh.nkey] * a.G * a.Hkv;
+  int64_t each = (all + sh.wgs - 1) / sh.wgs;
+  // a compute unit each first: longer shares leave fewer parts to add up
+  each = max(each, min((int64_t)2 * sh.least, (all + kFirstShares - 1) / kFirstShares));
+  if (each < sh.least) each = sh.least;
   x.at = min(all, each * wg);
   x.end = min(all, x.at + each);
 }
@@ -284,7 +292,7 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dkv_kernel(At
     if (wg >= a.B * a.Hkv * sh.nkey) return;
     x.hk = wg % a.Hkv, x.item = wg / a.Hkv, x.from = 0, x.to = x.tiles = -1, x.at = x.end = 0;
   } else {
-    share_of(a, sh.nkey, wg, sh.wgs, x);
+    share_of(a, sh, wg, x);
   }
   for (bool first = true;; first = false) {
     if (sh.whole ? !first : !next_piece(a, sh.nkey, x)) return;
@@ -450,11 +458,10 @@ template <typename E, int DP>
 __global__ __launch_bounds__(256) void attn_parts_kernel(AttnArgs a, KeyShares sh) {
   using El = AttnElem<E>;
   constexpr int UNITS = 2 * DP / 4;
-  constexpr int PARTS = 4;      // workgroups of a cut item
   const uint32_t wid = blockIdx.y * kAttnRow + blockIdx.x;
-  const int id = wid / PARTS;
+  const int id = wid / kSumGroups;
   if (id >= sh.wgs) {
-    const uint32_t x = wid - PARTS * sh.wgs;
+    const uint32_t x = wid - kSumGroups * sh.wgs;
     const int item = x / a.Hkv, hk = x % a.Hkv, b = item / sh.nkey, s0 = item % sh.nkey * kKeyBlock;
     if (item >= a.B * sh.nkey || a.before[item + 1] != a.before[item]) return;
     for (int y = threadIdx.x; y < kKeyBlock * UNITS; y += 256) {
@@ -467,7 +474,7 @@ __global__ __launch_bounds__(256) void attn_parts_kernel(AttnArgs a, KeyShares s
   }
   // the last piece of this share
   Share x, y;
-  share_of(a, sh.nkey, id, sh.wgs, x);
+  share_of(a, sh, id, x);
   if (x.at >= x.end) return;
   y = x;
   y.at = x.end - 1;
@@ -478,12 +485,12 @@ __global__ __launch_bounds__(256) void attn_parts_kernel(AttnArgs a, KeyShares s
   const int64_t each = x.end - x.at;      // of the shares that follow too, less the last one
   const int parts = (int)((begin + y.tiles - x.end + each - 1) / each);
   const int b = y.item / sh.nkey, s0 = y.item % sh.nkey * kKeyBlock;
-#pragma unroll 4
-  for (int u = wid % PARTS * (kKeyBlock / PARTS * UNITS) + threadIdx.x; u < (wid % PARTS + 1) * (kKeyBlock / PARTS * UNITS); u += 256) {
+  for (int u = wid % kSumGroups * (kKeyBlock / kSumGroups * UNITS) + threadIdx.x; u < (wid % kSumGroups + 1) * (kKeyBlock / kSumGroups * UNITS); u += 256) {
     const int key = s0 + u / UNITS, c = u % UNITS * 4, d = c >= DP ? c - DP : c;
     if (key >= a.Tk || d >= a.D) continue;
     const int64_t in = (int64_t)(u / UNITS) * (2 * DP) + c, slot = (int64_t)kKeyBlock * 2 * DP;
     f32x4_t sum = *reinterpret_cast<const f32x4_t*>(a.part + (2 * (int64_t)id + 1) * slot + in);
+#pragma unroll 8
     for (int z = 1; z <= parts; ++z) sum += *reinterpret_cast<const f32x4_t*>(a.part + 2 * (int64_t)(id + z) * slot + in);
     if (c < DP) sum *= a.scale;
     const AttnTensor& t = c >= DP ? a.dv : a.dk;
@@ -513,7 +520,7 @@ hipError_t bwd(const KeyShares& sh, AttnArgs a, hipStream_t s) {
   else coarse<<<attn_grid(sh.wgs), 256, more, s>>>(a, sh);
   e = hipGetLastError();
   if (e != hipSuccess || sh.whole) return e;
-  attn_parts_kernel<E, DP><<<attn_grid(4 * (int64_t)sh.wgs + (int64_t)a.B * a.Hkv * sh.nkey), 256, 0, s>>>(a, sh);
+  attn_parts_kernel<E, DP><<<attn_grid((int64_t)kSumGroups * sh.wgs + (int64_t)a.B * a.Hkv * sh.nkey), 256, 0, s>>>(a, sh);
   return hipGetLastError();
 }
 

@@ -289,6 +289,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int rows) {
   for (int x = 32; x; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
   const float base = m == -INFINITY ? 0.f : m;
   float sum = 0.f, o[DP / 64] = {};
+#pragma unroll 8
   for (int s = 0; s < a.nsplit; ++s) {
     const float f = __builtin_amdgcn_exp2f(part[s * step + DP] - base);
     sum += f * part[s * step + DP + 1];
@@ -306,6 +307,39 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int rows) {
     else reinterpret_cast<float*>(out)[d] = o[i] * inv;
   }
   if (a.lse && l == 0) a.lse[((int64_t)b * a.Hq + head) * a.Tq + qi] = lse_of(m, sum);
+}
+
+// 128 keys from s0 on, a wavefront 32 of them: lane l holds key 32 w + l % 32.  Codes come through `lds`, which is free again afterwards.
+template <typename Tile, bool kCache>
+__device__ inline void load_keys(const AttnArgs& a, typename Tile::Frag (&k)[Tile::KS], char* lds, uint32_t bh, int b, int hk, int s0, int lk, int w, int l) {
+  using El = typename Tile::El;
+  if constexpr (kCache) {
+    const uint32_t rbase = Tile::row_base(l);
+    for (int y = 0; y < 4; ++y) {
+      const int64_t row = (int64_t)bh * a.Tk + s0 + y * 32;
+      __syncthreads();
+      load_cache<Tile, 4, 32>(lds, a.k_codes + row * (a.D / 2), a.k_scales + row * (a.D / 32), lk - s0 - y * 32, a.D, w, l);
+      __syncthreads();
+      if (w == y) {
+#pragma unroll
+        for (int ks = 0; ks < Tile::KS; ++ks) k[ks] = Tile::row_frag(lds, rbase, 0, ks);
+      }
+    }
+    __syncthreads();
+  } else {
+    const int key = s0 + w * 32 + (l & 31);
+    const char* src = a.k.p + b * a.k.seq + (int64_t)key * a.k.slot + hk * a.k.head;
+#pragma unroll
+    for (int ks = 0; ks < Tile::KS; ++ks) {
+      const int d = 16 * ks + 8 * (l >> 5);
+      k[ks] = key < lk && d < a.D ? El::load(src + d * El::size) : El::zero();
+    }
+  }
+}
+
+__device__ inline void put_weight(const AttnArgs& a, uint32_t bh, int key, float sum) {
+  float* const to = a.weight + (int64_t)bh * a.Tk + key;
+  *to = a.decay == 0.f ? sum : fmaf(a.decay, *to, sum);
 }
 
 // Weight that the keys got: S = Q K^T with the queries along the accumulators' rows, so that a lane adds up one key's column.  A workgroup
@@ -343,27 +377,7 @@ __global__ __launch_bounds__(256) void attn_weight_kernel(AttnArgs a, int parts)
   float sum[2] = {0.f, 0.f};
   if (t0 < t1) {
     Frag k[KS];
-    if constexpr (kCache) {
-      // through LDS, a wavefront's rows at a time
-      for (int y = 0; y < 4; ++y) {
-        const int64_t row = (int64_t)bh * a.Tk + s0 + y * 32;
-        __syncthreads();
-        load_cache<Tile, 4, 32>(lds, a.k_codes + row * (a.D / 2), a.k_scales + row * (a.D / 32), lk - s0 - y * 32, a.D, w, l);
-        __syncthreads();
-        if (w == y) {
-#pragma unroll
-          for (int ks = 0; ks < KS; ++ks) k[ks] = Tile::row_frag(lds, rbase, 0, ks);
-        }
-      }
-      __syncthreads();
-    } else {
-      const char* src = a.k.p + b * a.k.seq + (int64_t)key * a.k.slot + hk * a.k.head;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const int d = 16 * ks + 8 * (l >> 5);
-        k[ks] = key < lk && d < a.D ? El::load(src + d * El::size) : El::zero();
-      }
-    }
+    load_keys<Tile, kCache>(a, k, lds, bh, b, hk, s0, lk, w, l);
     const int offset = lk - lq;
     int head = hk * a.G + t0 / run, i = begin + t0 % run * kQueryTile;      // of the tile that is loaded next
     float lse = 0.f;
@@ -421,9 +435,65 @@ __global__ __launch_bounds__(256) void attn_weight_kernel(AttnArgs a, int parts)
   if (a.sums) {
     a.sums[((int64_t)bh * parts + work.in) * kKeyBlock + w * 32 + l] = mine;
   } else if (key < lk) {
-    float* const to = a.weight + (int64_t)bh * a.Tk + key;
-    *to = a.decay == 0.f ? mine : fmaf(a.decay, *to, mine);
+    put_weight(a, bh, key, mine);
   }
+}
+
+// The same of fewer queries than a tile has rows: the rows (query, head) of a key head are packed as in the forward, and a workgroup goes
+// through all of them.  (9 x 7069 keys in 4 bits, two queries of five heads: 51 us with a tile for each head.)
+template <typename E, int DP, bool kCache>
+__global__ __launch_bounds__(256) void attn_weight_few_kernel(AttnArgs a, int nkey) {
+  using El = AttnElem<E>;
+  using Tile = AttnTile<E, DP, kQueryTile>;
+  constexpr int KS = Tile::KS;
+  extern __shared__ char lds[];
+  __shared__ float ends[kQueryTile], lows[kQueryTile];
+  __shared__ int positions[kQueryTile];
+  const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Work work;
+  if (!attn_work(a.B * a.Hkv, nkey, work)) return;
+  const uint32_t bh = work.bh;
+  const int hk = uniform(bh % a.Hkv), b = uniform(bh / a.Hkv);
+  const int lq = clamp_len(a.len_q, b, a.Tq), lk = clamp_len(a.len_k, b, a.Tk);
+  const int s0 = work.in * kKeyBlock, key = s0 + w * 32 + (l & 31), offset = lk - lq, rows = lq * a.G;
+  if (s0 >= lk) return;
+  float sum = 0.f;
+  if (!none_seen(s0, kKeyBlock, offset, lk - 1, a.window, a.sinks)) {
+    typename El::Frag k[KS];
+    load_keys<Tile, kCache>(a, k, lds, bh, b, hk, s0, lk, w, l);
+    const uint32_t rbase = Tile::row_base(l);
+    for (int r0 = 0; r0 < rows; r0 += kQueryTile) {
+      __syncthreads();
+      for (int x = threadIdx.x; x < kQueryTile * Tile::CH; x += 256) {
+        const uint32_t row = x / Tile::CH, r = r0 + row, c = x % Tile::CH, qi = r / (uint32_t)a.G;
+        u32x4_t v = {0, 0, 0, 0};
+        if ((int)r < rows && (int)c * 16 < a.D * El::size)
+          v = *reinterpret_cast<const u32x4_t*>(a.q.p + b * a.q.seq + (int64_t)qi * a.q.slot + (hk * a.G + r % (uint32_t)a.G) * a.q.head + c * 16);
+        *reinterpret_cast<u32x4_t*>(lds + Tile::at(row, c)) = v;
+      }
+      if (threadIdx.x < kQueryTile) {
+        const uint32_t r = r0 + threadIdx.x, qi = r / (uint32_t)a.G;
+        const bool in = (int)r < rows;
+        const Ends e(in ? a.lse[((int64_t)b * a.Hq + hk * a.G + r % (uint32_t)a.G) * a.Tq + qi] : -INFINITY);
+        ends[threadIdx.x] = e.a, lows[threadIdx.x] = e.b;
+        positions[threadIdx.x] = in ? offset + (int)qi : -1;
+      }
+      __syncthreads();
+      f32x16_t s;
+#pragma unroll
+      for (int x = 0; x < 16; ++x) s[x] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) El::mma(s, Tile::row_frag(lds, rbase, 0, ks), k[ks]);
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        const int row = acc_row(x, l);
+        const float e = __builtin_amdgcn_exp2f(fmaf(s[x], a.scale2, -ends[row]) - lows[row]);
+        sum += seen(key, positions[row], a.window, a.sinks) ? e : 0.f;
+      }
+    }
+    sum = add_halves(sum);
+  }
+  if (l < 32 && key < lk) put_weight(a, bh, key, sum);
 }
 
 // Adds up the parts of a block of keys, in order.
@@ -437,8 +507,7 @@ __global__ __launch_bounds__(kKeyBlock) void attn_weight_sum_kernel(AttnArgs a, 
   if (blk < a.nsink)
     for (int y = 0; y < a.far; ++y) sum += from[((int64_t)blk * a.far + y) * kKeyBlock];
   for (int y = 0; y < a.main; ++y) sum += from[((int64_t)a.nsink * a.far + (int64_t)blk * a.main + y) * kKeyBlock];
-  float* const to = a.weight + bh * a.Tk + key;
-  *to = a.decay == 0.f ? sum : fmaf(a.decay, *to, sum);
+  put_weight(a, (uint32_t)bh, key, sum);
 }
 
 template <typename E, int DP, int NW, int BK, bool kCache>
@@ -465,6 +534,10 @@ hipError_t weight(const attn_desc* d, const AttnPlan& p, const AttnArgs& a, hipS
   constexpr auto kernel = attn_weight_kernel<E, DP, kCache>;
   const int bytes = 2 * AttnTile<E, DP, kQueryTile>::BYTES, nkey = (a.Tk + kKeyBlock - 1) / kKeyBlock;
   const int64_t heads = (int64_t)a.B * a.Hkv, parts = attn_weight_parts(d, p);
+  if (d->Tq < kQueryTile) {
+    attn_weight_few_kernel<E, DP, kCache><<<attn_grid(attn_wgs(heads, nkey)), 256, bytes / 2, s>>>(a, nkey);
+    return hipGetLastError();
+  }
   kernel<<<attn_grid(attn_wgs(heads, parts)), 256, bytes, s>>>(a, (int)parts);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.sums) return e;

@@ -239,3 +239,16 @@ LONG = [      # queries that the weights' pass cuts: with a window and blocks of
 @pytest.mark.parametrize("case", LONG, ids=_name)
 def test_weights_of_long_prompts(case):
     check_fwd(Problem(seed=21, **case), decay=0.75)
+
+
+PACKED = [      # fewer queries than a tile of the weights' pass, whose rows are packed
+    dict(B=2, Tq=31, Tk=300, Hq=8, Hkv=2, D=128, window=70, sinks=130, len_q=[31, 5], len_k=[300, 2]),
+    dict(B=3, Tq=3, Tk=260, Hq=27, Hkv=3, D=64, len_q=[3, 0, 1], len_k=[260, 129, 128]),
+    dict(B=1, Tq=1, Tk=1000, Hq=40, Hkv=1, D=128, window=64, sinks=1, dtype="f32"),
+    dict(B=2, Tq=9, Tk=5, Hq=4, Hkv=1, D=96, len_q=[9, 9], len_k=[5, 0], first="wide"),
+]
+
+
+@pytest.mark.parametrize("case", PACKED, ids=_name)
+def test_weights_of_packed_rows(case):
+    check_fwd(Problem(seed=22, **case), decay=0.5)
