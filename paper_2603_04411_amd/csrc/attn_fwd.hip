@@ -47,9 +47,9 @@ __device__ inline void load_cache(char* lds, const uint8_t* codes, const uint8_t
 // softmax needs one exchange between lane halves; the exponentials are the second operand of O^T = V^T P^T as they lie.
 //
 // Bound by the matrix cores and the exponentials, whose instructions overlap only so far (matrix cores busy 55 % of the time, the other units
-// 52 %, both at once 20 %).  32 and 8 heads of 128, 4 sequences of 4096: 535 us, 1.0 PFLOP/s over the pairs that are seen; 8 of
+// 52 %, both at once 20 %).  32 and 8 heads of 128, 4 sequences of 4096: 525 to 555 us as the clocks allow, 1.0 PFLOP/s over the pairs that are seen; 8 of
 // 512 to 2048: 157 us (263 with a key head's workgroups on all XCDs, 160 with the compiler's order of a tile's steps); 40 and 8 heads, 4 of
-// 1024 to 8192 under a window of 1024: 440 to 570 us, as the clocks allow.
+// 1024 to 8192 under a window of 1024: 420 to 535 us.
 // The grid is a workgroup for 128 rows, the last ones (which see most) first; where that leaves compute units idle the keys are cut.
 template <typename E, int DP, int NW, int BK, bool kCache>
 __global__ __launch_bounds__(NW * 64, AttnElem<E>::size == 2 || DP == 64 ? 2 : 1) void attn_fwd_kernel(AttnArgs a) {
@@ -203,6 +203,8 @@ __global__ __launch_bounds__(NW * 64, AttnElem<E>::size == 2 || DP == 64 ? 2 : 1
 #pragma unroll
       for (int x = 0; x < A; ++x) row(x);
     }
+    // (of a unit's two wavefronts the one in these products goes first, so that they fall out of step: 566 -> 553 us of the full 4 x 4096)
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int x = 0; x < M; ++x) {
       if constexpr (kMore) {
@@ -213,6 +215,7 @@ __global__ __launch_bounds__(NW * 64, AttnElem<E>::size == 2 || DP == 64 ? 2 : 1
       weigh(x);
       __builtin_amdgcn_sched_barrier(0);
     }
+    __builtin_amdgcn_s_setprio(0);
     weigh(M);
     weigh(M + 1);
     sum += part[0] + part[1];
