@@ -255,8 +255,8 @@ LMHEAD_API int attn_bwd(const attn_desc* desc, const void* q, const void* k, con
  * A cache in 4 bits.  A row of D values of a token and head is cut into blocks of 32.  A block has the scale 2^e with
  * the smallest e >= -126 for which max |x| <= 6 * 2^e, but at most 2^125, stored as the byte e + 127, and a code of four bits
  * for each value: bit 3 the sign, bits 0-2 the index into { 0, 0.5, 1, 1.5, 2, 3, 4, 6 } of x / 2^e, rounded to nearest, of two
- * as near ones to the even index (so the values are e2m1 numbers, and all are finite in bf16).  A block with an infinity or a NaN has the scale byte 255 and codes 0 and
- * stands for 32 NaN.
+ * as near ones to the even index (so the values are e2m1 numbers, and all are finite in bf16).
+ * A block with an infinity or a NaN has the scale byte 255 and codes 0 and stands for 32 NaN.
  *   k_codes, v_codes    uint8[B][Hkv][Tk][D / 2]: value 2c in the lower half of byte c, value 2c + 1 in the upper half
  *   k_scales, v_scales  uint8[B][Hkv][Tk][D / 32]
  * Both are dense; codes are 16-byte aligned, scales 4-byte aligned.  Tk and the descriptor's heads are the cache's.
@@ -268,7 +268,8 @@ LMHEAD_API int kv4_store(const attn_desc* desc, const void* k, const void* v, co
                          uint8_t* k_codes, uint8_t* k_scales, uint8_t* v_codes, uint8_t* v_scales, void* ws, size_t ws_bytes,
                          void* stream);
 
-/* attn_fwd over such a cache (desc->k and desc->v are not used). */
+/* attn_fwd over such a cache (desc->k and desc->v are not used, but have to be valid).  Scale bytes that
+ * kv4_store does not write (0, 253, 254) are no error and stand for no particular value. */
 LMHEAD_API int kv4_attn(const attn_desc* desc, const void* q, const uint8_t* k_codes, const uint8_t* k_scales,
                         const uint8_t* v_codes, const uint8_t* v_scales, const int32_t* len_q, const int32_t* len_k, void* out,
                         float* lse, float* weight, float decay, void* ws, size_t ws_bytes, void* stream);
