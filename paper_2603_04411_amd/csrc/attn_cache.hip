@@ -250,6 +250,7 @@ __global__ __launch_bounds__(256) void evict_move_kernel(MoveArgs a) {
   const cache_plane& p = a.plane[which];
   const int all_words = (int)(p.bytes / (int)sizeof(W)), each = (all_words + a.parts[which] - 1) / a.parts[which];
   const int w0 = slice * each, words = min(each, all_words - w0);
+  if (words <= 0) return;      // (41 units in ten slices of five)
   char* const base = static_cast<char*>(p.data) + b * p.seq + h * p.head + (int64_t)w0 * sizeof(W);
   const int32_t* const kept = a.kept + (int64_t)row * a.keep;
   const int64_t all = (int64_t)a.keep * words;

@@ -250,3 +250,20 @@ def test_eviction_takes_lengths_out_of_range_as_the_nearest():
                          ids=_name)
 def test_weights_of_long_prompts_over_codes(case):
     test_store_and_attention(case)
+
+
+@pytest.mark.parametrize("width", [1, 3, 41, 164, 165, 1023, 1024])
+def test_eviction_of_rows_that_slices_do_not_divide(width):
+    """One key head, so that a row's columns are cut as often as they can be."""
+    import torch
+    import paper_2603_04411_amd as L
+    T, keep = 70, 33
+    w = torch.rand(1, 1, T, device="cuda", generator=torch.Generator(device="cuda").manual_seed(width))
+    x = torch.arange(T * width, device="cuda", dtype=torch.float32).view(1, T, 1, width)
+    old, at = x.clone(), A.evict(w[0, 0].cpu().numpy(), T, keep, 1, 2)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    desc, n, kept = L.make_evict_desc(1, T, 1, keep, 1, 2), torch.empty(1, **i32), torch.empty(1, 1, keep, **i32)
+    ws = torch.empty(L.evict_workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+    L.cache_evict(desc, L.make_cache_planes([x]), w, None, n, kept, ws)
+    assert kept[0, 0].tolist() == at and n.tolist() == [keep]
+    assert torch.equal(x[0, :keep], old[0, at]) and torch.equal(x[0, keep:], old[0, keep:])
