@@ -349,8 +349,8 @@ __device__ inline void put_weight(const AttnArgs& a, uint32_t bh, int key, float
 // takes a block of 128 keys of a key head (a wavefront 32 of them, in registers) and a part of the queries that see it, head by head in tiles
 // of 32, one tile ahead in LDS.  The queries behind the window that see a block's first tokens are parts of their own.
 //
-// Bound by the exponentials and the masks beside one product.  4 sequences of 8192 under a window of 1024 with 28 and 4 heads of 128: 340 us (a
-// workgroup a block of keys, one tile at a time: 2440, as long as the block of the first tokens takes); 8 of 2048 without: 180 (546).
+// Bound by the exponentials and the masks beside one product.  4 sequences of 8192 under a window of 1024 with 28 and 4 heads of 128: 410 us (a
+// workgroup a block of keys, one tile at a time: 2440, as long as the block of the first tokens takes); 8 of 2048 without: 205 (546).
 template <typename E, int DP, bool kCache>
 __global__ __launch_bounds__(256) void attn_weight_kernel(AttnArgs a, int parts) {
   using El = AttnElem<E>;
@@ -377,13 +377,13 @@ __global__ __launch_bounds__(256) void attn_weight_kernel(AttnArgs a, int parts)
   const int run = far ? item.far : item.main, begin = far ? item.far0 : item.i0, end = far ? lq : item.far0;
   const int64_t all = (int64_t)run * a.G;
   const int t0 = uniform((int)(all * part / cut)), t1 = uniform((int)(all * (part + 1) / cut));
-  float sum[2] = {0.f, 0.f};
+  float sum = 0.f;
   if (t0 < t1) {
     Frag k[KS];
     load_keys<Tile, kCache>(a, k, lds, bh, b, hk, s0, lk, w, l);
     const int offset = lk - lq;
     int head = hk * a.G + t0 / run, i = begin + t0 % run * kQueryTile;      // of the tile that is loaded next
-    float lse = 0.f;
+    float lse = 0.f, run_sum = 0.f;
     auto load = [&](int at) {
       Tile::template load<4>(lds + at * Tile::BYTES, a.q.p + b * a.q.seq + head * a.q.head + i * a.q.slot, (uint32_t)a.q.slot, end - i,
                              a.D * El::size, w, l);
@@ -407,33 +407,32 @@ __global__ __launch_bounds__(256) void attn_weight_kernel(AttnArgs a, int parts)
       for (int y = 0; y < 16; ++y) s[y] = 0.f;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) El::mma(s, Tile::row_frag(q, rbase, 0, ks), k[ks]);
-      float e[16];
+      float e[16], some[2] = {0.f, 0.f};
 #pragma unroll
       for (int y = 0; y < 16; y += 4) {
-        const f32x4_t hi = *reinterpret_cast<const f32x4_t*>(&ends[at][acc_row(y, l)]);
+        const f32x4_t hi = *reinterpret_cast<const f32x4_t*>(&ends[at][acc_row(y, l)]), lo = *reinterpret_cast<const f32x4_t*>(&lows[at][acc_row(y, l)]);
 #pragma unroll
-        for (int z = 0; z < 4; ++z) e[y + z] = fmaf(s[y + z], a.scale2, -hi[z]);
-        if constexpr (El::size == 4) {
-          const f32x4_t lo = *reinterpret_cast<const f32x4_t*>(&lows[at][acc_row(y, l)]);
-#pragma unroll
-          for (int z = 0; z < 4; ++z) e[y + z] -= lo[z];
-        }
+        for (int z = 0; z < 4; ++z) e[y + z] = fmaf(s[y + z], a.scale2, -hi[z]) - lo[z];
       }
+      // (sums of a tile, then of sixteen: over thousands of queries a third of the error of one running sum)
       const int p0 = offset + i0;
       if (i0 + kQueryTile <= end && all_seen(k0, 32, p0, p0 + kQueryTile - 1, a.window, a.sinks)) {
 #pragma unroll
-        for (int y = 0; y < 16; ++y) sum[y & 1] += __builtin_amdgcn_exp2f(e[y]);
+        for (int y = 0; y < 16; ++y) some[y & 1] += __builtin_amdgcn_exp2f(e[y]);
       } else {
 #pragma unroll
         for (int y = 0; y < 16; ++y) {
           const int row = acc_row(y, l);
           const float v = __builtin_amdgcn_exp2f(e[y]);
-          sum[y & 1] += ((i0 + row < end) & seen(key, p0 + row, a.window, a.sinks)) ? v : 0.f;
+          some[y & 1] += ((i0 + row < end) & seen(key, p0 + row, a.window, a.sinks)) ? v : 0.f;
         }
       }
+      run_sum += some[0] + some[1];
+      if ((t & 15) == 15) sum += run_sum, run_sum = 0.f;
     }
+    sum += run_sum;
   }
-  const float mine = add_halves(sum[0] + sum[1]);
+  const float mine = add_halves(sum);
   if (l >= 32) return;
   if (a.sums) {
     a.sums[((int64_t)bh * parts + work.in) * kKeyBlock + w * 32 + l] = mine;
