@@ -136,6 +136,8 @@ AttnArgs arguments(const attn_desc* d, const AttnPlan& p, const int32_t* len_q, 
   a.len_q = len_q, a.len_k = len_k;
   a.hdr = static_cast<AttnHeader*>(ws);
   a.nblk = p.nblk, a.nsplit = p.nsplit;
+  // against what the eight L2s hold
+  a.past_out = (int64_t)d->B * d->Tq * d->Hq * d->D * (d->dtype == LMHEAD_BF16 ? 2 : 4) > (32ll << 20);
   a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + p.part);
   return a;
 }

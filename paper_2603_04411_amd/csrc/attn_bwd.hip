@@ -250,22 +250,19 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dq_kernel(Att
     }
   }
   off = add_halves(off);
-  if (!in) return;
-  if (l < 32) a.delta[((int64_t)b * a.Hq + head) * a.Tq + qi] = delta + off;
-  char* const out = a.dq.p + b * a.dq.seq + (int64_t)qi * a.dq.slot + head * a.dq.head;
+  if (in && l < 32) a.delta[((int64_t)b * a.Hq + head) * a.Tq + qi] = delta + off;
+  if constexpr (kFix) {
 #pragma unroll
-  for (int db = 0; db < DB; ++db)
+    for (int db = 0; db < DB; ++db)
 #pragma unroll
-    for (int i = 0; i < 16; i += 4) {
-      const int d = db * 32 + acc_row(i, l);
-      float x[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        x[j] = dq[db][i + j];
-        if constexpr (kFix) x[j] = fmaf(-off, mean[db][i + j], x[j]);
-      }
-      if (d < a.D) El::store4(out + d * El::size, x[0] * a.scale, x[1] * a.scale, x[2] * a.scale, x[3] * a.scale);
-    }
+      for (int i = 0; i < 16; ++i) dq[db][i] = fmaf(-off, mean[db][i], dq[db][i]);
+  }
+  __syncthreads();      // the tiles are done with
+  const uint32_t row0 = r0 + w * 32;
+  store_rows<E, DP>(lds + w * AttnTile<E, DP, 32>::BYTES, dq, a.scale, a.D, a.past_out, l, [&](int row) -> char* {
+    const uint32_t i = (row0 + row) / (uint32_t)a.G, g = (row0 + row) % (uint32_t)a.G;
+    return (int)i < a.Tq ? a.dq.p + b * a.dq.seq + (int64_t)i * a.dq.slot + (hk * a.G + g) * a.dq.head : nullptr;
+  });
 }
 
 // A wavefront holds 32 keys and their values; the workgroup's four walk the queries that see them, head by head, in tiles of 32.  S and dP

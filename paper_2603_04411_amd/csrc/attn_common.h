@@ -37,6 +37,7 @@ struct AttnArgs {
   AttnHeader* hdr;
   int nblk, nsplit;         // blocks of rows, and parts of a block's keys
   bool past;                // few rows: read K and V past the caches
+  bool past_out;            // more: write the output (the backward: dq) past them
   float* logits;            // of a few rows: [b][key head][key][row], for the weights
   float* part;              // [b][key head][split][row of the block-padded rows]{DP sums, maximum, sum}
   // weights of more rows than a few: see attn_weight_kernel
@@ -370,6 +371,36 @@ struct Ends {
 
 // Row of accumulator element i of a 32x32 block.
 __device__ inline int acc_row(int i, int l) { return 8 * (i >> 2) + 4 * (l >> 5) + (i & 3); }
+
+// Rows that lie in accumulators across (lane l has columns 32 db + acc_row(i, l) of row l % 32) go to memory by way of 32 rows of LDS that are
+// this wavefront's: as they lie a store would write sixteen bytes here and there.  `to(row)`: where a row goes, or null.  `past`: past the caches,
+// where they would not hold the result (the forward of 8 x 2048, 134 MB: 158 us as they lie, 153 by rows, 151 past the caches).
+template <typename E, int DP, typename To>
+__device__ inline void store_rows(char* lds, const f32x16_t (&x)[DP / 32], float factor, int D, bool past, int l, const To& to) {
+  using El = AttnElem<E>;
+  using Tile = AttnTile<E, DP, 32>;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const int at = (db * 32 + acc_row(i, l)) * El::size;
+      El::store4(lds + Tile::at(l & 31, at / 16) + at % 16, x[db][i] * factor, x[db][i + 1] * factor, x[db][i + 2] * factor, x[db][i + 3] * factor);
+    }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  const int c = l % Tile::CH;
+#pragma unroll
+  for (int it = 0; it < 32 * Tile::CH / 64; ++it) {
+    const int row = it * (64 / Tile::CH) + l / Tile::CH;
+    const u32x4_t v = *reinterpret_cast<const u32x4_t*>(lds + Tile::at(row, c));
+    char* const p = to(row);
+    if (!p || c * 16 >= D * El::size) continue;
+    if (past) __builtin_nontemporal_store(v, reinterpret_cast<u32x4_t*>(p + c * 16));
+    else *reinterpret_cast<u32x4_t*>(p + c * 16) = v;
+  }
+}
 
 // A value and that of the lane 32 (16) further, each in both of them: what is symmetric in the two needs no more.
 struct Pair {

@@ -48,8 +48,8 @@ __device__ inline void load_cache(char* lds, const uint8_t* codes, const uint8_t
 //
 // Bound by the matrix cores and the exponentials, whose instructions overlap only so far (matrix cores busy 55 % of the time, the other units
 // 52 %, both at once 20 %).  32 and 8 heads of 128, 4 sequences of 4096: 525 to 555 us as the clocks allow, 1.0 PFLOP/s over the pairs that are seen; 8 of
-// 512 to 2048: 157 us (263 with a key head's workgroups on all XCDs, 160 with the compiler's order of a tile's steps); 40 and 8 heads, 4 of
-// 1024 to 8192 under a window of 1024: 420 to 535 us.
+// 512 to 2048: 151 us (263 with a key head's workgroups on all XCDs, 160 with the order of steps that the compiler chose, 158 with rows stored as they lie); 40 and 8 heads, 4 of
+// 1024 to 8192 under a window of 1024: 400 to 520 us, by the lengths.
 // The grid is a workgroup for 128 rows, the last ones (which see most) first; where that leaves compute units idle the keys are cut.
 template <typename E, int DP, int NW, int BK, bool kCache>
 __global__ __launch_bounds__(NW * 64, AttnElem<E>::size == 2 || DP == 64 ? 2 : 1) void attn_fwd_kernel(AttnArgs a) {
@@ -264,17 +264,13 @@ __global__ __launch_bounds__(NW * 64, AttnElem<E>::size == 2 || DP == 64 ? 2 : 1
     }
     return;
   }
-  if (!in) return;
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  char* const out = a.o.p + b * a.o.seq + (int64_t)qi * a.o.slot + head * a.o.head;
-#pragma unroll
-  for (int db = 0; db < DB; ++db)
-#pragma unroll
-    for (int i = 0; i < 16; i += 4) {
-      const int d = db * 32 + acc_row(i, l);
-      if (d < a.D) El::store4(out + d * El::size, o[db][i] * inv, o[db][i + 1] * inv, o[db][i + 2] * inv, o[db][i + 3] * inv);
-    }
-  if (a.lse && l < 32) a.lse[((int64_t)b * a.Hq + head) * a.Tq + qi] = lse_of(m, sum);
+  __syncthreads();      // the tiles are done with
+  const uint32_t row0 = r0 + w * 32;
+  store_rows<E, DP>(lds + w * AttnTile<E, DP, 32>::BYTES, o, sum == 0.f ? 0.f : 1.f / sum, a.D, a.past_out, l, [&](int row) -> char* {
+    const uint32_t i = (row0 + row) / (uint32_t)a.G, g = (row0 + row) % (uint32_t)a.G;
+    return (int)i < a.Tq ? a.o.p + b * a.o.seq + (int64_t)i * a.o.slot + (hk * a.G + g) * a.o.head : nullptr;
+  });
+  if (in && a.lse && l < 32) a.lse[((int64_t)b * a.Hq + head) * a.Tq + qi] = lse_of(m, sum);
 }
 
 // Joins the parts of a row, sums and maxima of which it reads once: a wavefront each.  (Of a launch that did not fill the card, so short.)
