@@ -47,9 +47,9 @@ __device__ inline void load_cache(char* lds, const uint8_t* codes, const uint8_t
 // softmax needs one exchange between lane halves; the exponentials are the second operand of O^T = V^T P^T as they lie.
 //
 // Bound by the matrix cores and the exponentials, whose instructions overlap only so far (matrix cores busy 55 % of the time, the other units
-// 52 %, both at once 20 %).  32 and 8 heads of 128, 4 sequences of 4096: 525 to 555 us as the clocks allow, 1.0 PFLOP/s over the pairs that are seen; 8 of
-// 512 to 2048: 151 us (263 with a key head's workgroups on all XCDs, 160 with the order of steps that the compiler chose, 158 with rows stored as they lie); 40 and 8 heads, 4 of
-// 1024 to 8192 under a window of 1024: 400 to 520 us, by the lengths.
+// 52 %, both at once 20 %).  32 and 8 heads of 128, 4 sequences of 4096: 525 to 555 us as the clocks allow, 1.0 PFLOP/s over the pairs that are
+// seen; 8 of 512 to 2048: 151 us (263 with a key head's workgroups on all XCDs, 160 with the order of steps that the compiler chose, 158 with
+// rows stored as they lie); 40 and 8 heads, 4 of 1024 to 8192 under a window of 1024: 400 to 520 us, by the lengths.
 // The grid is a workgroup for 128 rows, the last ones (which see most) first; where that leaves compute units idle the keys are cut.
 template <typename E, int DP, int NW, int BK, bool kCache>
 __global__ __launch_bounds__(NW * 64, AttnElem<E>::size == 2 || DP == 64 ? 2 : 1) void attn_fwd_kernel(AttnArgs a) {
