@@ -45,12 +45,13 @@ TRAFFIC_KEYS = ["fwd_kernel", "dz_kernel", "gemm_t_kernel<dH>", "gemm_t_kernel<d
 
 
 def kernel_sources_sha() -> str:
-    """Digest of the HIP sources the library is built from (identifies the kernels a profile was taken on)."""
+    """Digest of the HIP sources that the profiled kernels are built from (identifies the kernels a profile was taken on): the library's, but for
+    those of attention, which no profiled step launches and no other source includes."""
     import hashlib
     h = hashlib.sha256()
     d = os.path.join(ROOT, "paper_2603_04411_amd", "csrc")
     for name in sorted(os.listdir(d)):
-        if name.endswith((".hip", ".h")):
+        if name.endswith((".hip", ".h")) and not name.startswith("attn_"):
             h.update(name.encode())
             h.update(open(os.path.join(d, name), "rb").read())
     return h.hexdigest()[:16]
