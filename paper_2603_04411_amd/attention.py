@@ -118,14 +118,15 @@ class _Heads:
 
 
 class _Sizes:
-    """What the checks of a descriptor's tensors compare with, made once for its contents."""
+    """What the checks of a descriptor's tensors compare with, made once for its contents.  Nothing here refers to the descriptor: a copy of it
+    has these too."""
 
     def __init__(self, desc, raw):
         self.raw, d = raw, desc
         self.status = int(_lib().attn_validate_desc(C.byref(desc)))
         if self.status:
             return
-        self.dtype, self.ref, self.B = _TORCH[d.dtype], C.byref(desc), d.B
+        self.dtype, self.B = _TORCH[d.dtype], d.B
         B, Tq, Tk, Hq, Hkv, D = d.B, d.Tq, d.Tk, d.Hq, d.Hkv, d.D
         self.q, self.o = _Heads(B, Tq, Hq, D, d.q), _Heads(B, Tq, Hq, D, d.o)
         self.k, self.v = _Heads(B, Tk, Hkv, D, d.k), _Heads(B, Tk, Hkv, D, d.v)
@@ -164,7 +165,7 @@ def attn_fwd(desc, q, k, v, len_q, len_k, out, lse, weight, decay, ws) -> None:
     """len_q, len_k: int32[B], or None where every slot is valid; lse, weight: or None."""
     s, dev, i32, f32 = _sizes(desc, "attn_fwd"), _device(), torch.int32, torch.float32
     rc = _lib().attn_fwd(
-        s.ref, _heads(q, "q", s, s.q, dev), _heads(k, "k", s, s.k, dev), _heads(v, "v", s, s.v, dev), _arg(len_q, "len_q", i32, s.B, dev),
+        C.byref(desc), _heads(q, "q", s, s.q, dev), _heads(k, "k", s, s.k, dev), _heads(v, "v", s, s.v, dev), _arg(len_q, "len_q", i32, s.B, dev),
         _arg(len_k, "len_k", i32, s.B, dev), _heads(out, "out", s, s.o, dev), _arg(lse, "lse", f32, s.lse, dev),
         _arg(weight, "weight", f32, s.weight, dev), decay, _arg(ws, "ws", torch.uint8, 0, dev), ws.numel(), _stream(dev))
     _check(rc, "attn_fwd")
@@ -173,7 +174,7 @@ def attn_fwd(desc, q, k, v, len_q, len_k, out, lse, weight, decay, ws) -> None:
 def attn_bwd(desc, q, k, v, len_q, len_k, out, lse, g_out, dq, dk, dv, ws) -> None:
     s, dev, i32 = _sizes(desc, "attn_bwd"), _device(), torch.int32
     rc = _lib().attn_bwd(
-        s.ref, _heads(q, "q", s, s.q, dev), _heads(k, "k", s, s.k, dev), _heads(v, "v", s, s.v, dev), _arg(len_q, "len_q", i32, s.B, dev),
+        C.byref(desc), _heads(q, "q", s, s.q, dev), _heads(k, "k", s, s.k, dev), _heads(v, "v", s, s.v, dev), _arg(len_q, "len_q", i32, s.B, dev),
         _arg(len_k, "len_k", i32, s.B, dev), _heads(out, "out", s, s.o, dev), _arg(lse, "lse", torch.float32, s.lse, dev),
         _heads(g_out, "g_out", s, s.o, dev), _heads(dq, "dq", s, s.q, dev), _heads(dk, "dk", s, s.k, dev), _heads(dv, "dv", s, s.v, dev),
         _arg(ws, "ws", torch.uint8, 0, dev), ws.numel(), _stream(dev))
@@ -193,7 +194,7 @@ def kv4_store(desc, k, v, len_q, len_k, k_codes, k_scales, v_codes, v_scales, ws
     """k, v: the new tokens' rows, [B, Tq, Hkv, D]."""
     s, dev, i32 = _sizes(desc, "kv4_store"), _device(), torch.int32
     rc = _lib().kv4_store(
-        s.ref, _heads(k, "k", s, s.k_new, dev), _heads(v, "v", s, s.v_new, dev), _arg(len_q, "len_q", i32, s.B, dev),
+        C.byref(desc), _heads(k, "k", s, s.k_new, dev), _heads(v, "v", s, s.v_new, dev), _arg(len_q, "len_q", i32, s.B, dev),
         _arg(len_k, "len_k", i32, s.B, dev), *_cache(s, k_codes, k_scales, v_codes, v_scales, dev), _arg(ws, "ws", torch.uint8, 0, dev),
         ws.numel(), _stream(dev))
     _check(rc, "kv4_store")
@@ -202,7 +203,7 @@ def kv4_store(desc, k, v, len_q, len_k, k_codes, k_scales, v_codes, v_scales, ws
 def kv4_attn(desc, q, k_codes, k_scales, v_codes, v_scales, len_q, len_k, out, lse, weight, decay, ws) -> None:
     s, dev, i32, f32 = _sizes(desc, "kv4_attn"), _device(), torch.int32, torch.float32
     rc = _lib().kv4_attn(
-        s.ref, _heads(q, "q", s, s.q, dev), *_cache(s, k_codes, k_scales, v_codes, v_scales, dev), _arg(len_q, "len_q", i32, s.B, dev),
+        C.byref(desc), _heads(q, "q", s, s.q, dev), *_cache(s, k_codes, k_scales, v_codes, v_scales, dev), _arg(len_q, "len_q", i32, s.B, dev),
         _arg(len_k, "len_k", i32, s.B, dev), _heads(out, "out", s, s.o, dev), _arg(lse, "lse", f32, s.lse, dev),
         _arg(weight, "weight", f32, s.weight, dev), decay, _arg(ws, "ws", torch.uint8, 0, dev), ws.numel(), _stream(dev))
     _check(rc, "kv4_attn")
