@@ -1,6 +1,8 @@
 // Backward of attention over a window and a few first tokens: dq by blocks of queries, then dk and dv by blocks of keys, each recomputing
 // P from the logits and lse.  Seven products instead of the five that one pass over the pairs would take, and no atomics; with bf16 storage two
 // more in dq (and one in dk of few queries), for what rounding dS and out would cost.
+#include <algorithm>
+
 #include "attn_common.h"
 
 namespace lmhead {
@@ -33,9 +35,9 @@ KeyShares key_shares(const attn_desc* d, int resident) {
   const int64_t G = d->Hq / d->Hkv, each = ((int64_t)d->Tq + kQueryTile - 1) / kQueryTile + 1, items = (int64_t)d->B * d->Hkv * k.nkey;
   k.least = d->dtype == LMHEAD_BF16 ? kLeastShare : kLeastShareF32;
   k.whole = each * G <= k.least;
-  k.wgs = (int)(k.whole ? items : items >= resident ? resident : (items * each * G + k.least - 1) / k.least);
-  if (!k.whole && k.wgs > resident) k.wgs = resident;
-  k.wgs = (k.wgs + 7) / 8 * 8;
+  // (tiles of fewer items than are resident: up to 2^34)
+  const int64_t wgs = k.whole ? items : items >= resident ? resident : std::min<int64_t>(resident, (items * each * G + k.least - 1) / k.least);
+  k.wgs = (int)((wgs + 7) / 8 * 8);
   return k;
 }
 

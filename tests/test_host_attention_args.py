@@ -65,3 +65,15 @@ def test_a_copied_descriptor_is_the_one_that_is_passed(calls, copied):
         assert B.AttnDesc.from_buffer_copy(raw).Tk == Tk and raw == bytes(second), name
     with pytest.raises(ValueError):      # the first one is held against its new contents
         L.attn_fwd(first, *(getattr(tensors(), x) for x in ("q", "k", "k")), None, None, tensors().q, None, None, 1.0, tensors().ws)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,Tq,Tk,Hq,Hkv", [(1, 1 << 20, 33280, 1024, 1), (1, 1 << 20, 65000, 1024, 1), (1, 1 << 20, 16384, 1024, 1), (2, 1 << 20, 12800, 1024, 2),
+                                            (1, 1 << 20, 25600, 1024, 1), (3, 4096, 4096, 28, 4), (1, 1, 1, 1, 1), (1, 1 << 20, 1 << 25, 1, 1)])
+def test_backward_workspaces_of_the_largest_calls(B, Tq, Tk, Hq, Hkv, dtype):
+    """What is cut of dk and dv is counted in 64 bits: a call with many tiles and few blocks of keys has as many workgroups as are resident."""
+    d = L.make_attn_desc(B, Tq, Tk, Hq, Hkv, 8, dtype)
+    assert L.attn_validate_desc(d) == 0
+    lse, before, parts = 4 * B * Hq * Tq, 8 * (B * ((Tk + 127) // 128) + 1), 2 * 512 * 128 * 2 * 64 * 4     # at most 512 workgroups, two parts each
+    assert 256 + lse <= L.attn_bwd_workspace_bytes(d) <= 256 + lse + before + parts + 3 * 256
+    assert L.attn_workspace_bytes(d) >= 256 + lse
