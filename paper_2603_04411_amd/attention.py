@@ -9,6 +9,7 @@ keeps each head's tokens together is passed as its ``transpose(1, 2)``.
 from __future__ import annotations
 
 import ctypes as C
+import math
 
 import torch
 
@@ -108,6 +109,34 @@ def attn_bwd_workspace_bytes(desc: AttnDesc) -> int:
     return int(_lib().attn_bwd_workspace_bytes(C.byref(desc)))
 
 
+def _merges(n, want):
+    """Whether dimensions `n` are those of `want`, some of them neighbours taken together: dense tensors of either are the same memory."""
+    at = 0
+    for size in n:
+        have = 1
+        while have < size and at < len(want):
+            have *= want[at]
+            at += 1
+        if have != size:
+            return False
+    return all(x == 1 for x in want[at:])
+
+
+def _block(t, name, dtype, n, want, device):
+    """Device pointer of a dense tensor of the sizes `want`, `n` elements, of one that has more where that moves nothing of what is used (more sequences do not,
+    more slots would move every head but the first), or of a flat buffer with room for them; None for None."""
+    if t is None:
+        return None
+    if t.dtype is dtype and t.get_device() == device and t.is_contiguous():
+        sizes = t.shape
+        if sizes == want or len(sizes) == 1 and sizes[0] >= n or t.numel() == n and _merges(sizes, want):
+            return t.data_ptr()
+        if (len(sizes) == len(want) and all(a >= b for a, b in zip(sizes, want))
+                and all(a == math.prod(want[i + 1:]) or want[i] == 1 for i, a in enumerate(t.stride()))):
+            return t.data_ptr()
+    return _refuse(t, name, dtype, device, f"{tuple(want)} contiguous expected, got {tuple(t.shape)}")
+
+
 class _Heads:
     """What a [B, T, H, D] tensor of a call has to be."""
 
@@ -133,6 +162,8 @@ class _Sizes:
         self.k_new, self.v_new = _Heads(B, Tq, Hkv, D, d.k), _Heads(B, Tq, Hkv, D, d.v)      # rows for a cache in 4 bits
         rows = B * Hkv * Tk
         self.lse, self.weight, self.codes, self.scales = B * Hq * Tq, rows, rows * (D // 2), rows * (D // 32)
+        self.lse_shape, self.weight_shape = torch.Size((B, Hq, Tq)), torch.Size((B, Hkv, Tk))
+        self.codes_shape, self.scales_shape = torch.Size((B, Hkv, Tk, D // 2)), torch.Size((B, Hkv, Tk, D // 32))
 
 
 def _sizes(desc, where):
@@ -150,9 +181,9 @@ def _heads(t, name, s, want, device):
     """Device pointer of a [B, T, H, D] tensor with the shape and strides that are wanted (it may have more of each), or of a dense buffer where
     they are dense."""
     if t.dtype is s.dtype and t.get_device() == device:
-        if want.dense and t.is_contiguous() and t.numel() == want.n:
-            return t.data_ptr()
         n, st = t.shape, t.stride()
+        if want.dense and t.is_contiguous() and (n == want.shape or t.numel() == want.n and _merges(n, want.shape)):
+            return t.data_ptr()
         if n == want.shape and st == want.strides:
             return t.data_ptr()
         if len(n) == 4 and all(a >= b for a, b in zip(n, want.shape)) and all(a == b or c == 1 for a, b, c in zip(st, want.strides, want.shape)):
@@ -166,8 +197,8 @@ def attn_fwd(desc, q, k, v, len_q, len_k, out, lse, weight, decay, ws) -> None:
     s, dev, i32, f32 = _sizes(desc, "attn_fwd"), _device(), torch.int32, torch.float32
     rc = _lib().attn_fwd(
         C.byref(desc), _heads(q, "q", s, s.q, dev), _heads(k, "k", s, s.k, dev), _heads(v, "v", s, s.v, dev), _arg(len_q, "len_q", i32, s.B, dev),
-        _arg(len_k, "len_k", i32, s.B, dev), _heads(out, "out", s, s.o, dev), _arg(lse, "lse", f32, s.lse, dev),
-        _arg(weight, "weight", f32, s.weight, dev), decay, _arg(ws, "ws", torch.uint8, 0, dev), ws.numel(), _stream(dev))
+        _arg(len_k, "len_k", i32, s.B, dev), _heads(out, "out", s, s.o, dev), _block(lse, "lse", f32, s.lse, s.lse_shape, dev),
+        _block(weight, "weight", f32, s.weight, s.weight_shape, dev), decay, _arg(ws, "ws", torch.uint8, 0, dev), ws.numel(), _stream(dev))
     _check(rc, "attn_fwd")
 
 
@@ -175,7 +206,7 @@ def attn_bwd(desc, q, k, v, len_q, len_k, out, lse, g_out, dq, dk, dv, ws) -> No
     s, dev, i32 = _sizes(desc, "attn_bwd"), _device(), torch.int32
     rc = _lib().attn_bwd(
         C.byref(desc), _heads(q, "q", s, s.q, dev), _heads(k, "k", s, s.k, dev), _heads(v, "v", s, s.v, dev), _arg(len_q, "len_q", i32, s.B, dev),
-        _arg(len_k, "len_k", i32, s.B, dev), _heads(out, "out", s, s.o, dev), _arg(lse, "lse", torch.float32, s.lse, dev),
+        _arg(len_k, "len_k", i32, s.B, dev), _heads(out, "out", s, s.o, dev), _block(lse, "lse", torch.float32, s.lse, s.lse_shape, dev),
         _heads(g_out, "g_out", s, s.o, dev), _heads(dq, "dq", s, s.q, dev), _heads(dk, "dk", s, s.k, dev), _heads(dv, "dv", s, s.v, dev),
         _arg(ws, "ws", torch.uint8, 0, dev), ws.numel(), _stream(dev))
     _check(rc, "attn_bwd")
@@ -184,15 +215,22 @@ def attn_bwd(desc, q, k, v, len_q, len_k, out, lse, g_out, dq, dk, dv, ws) -> No
 # ---- the cache in 4 bits --------------------------------------------------------------------------------------------
 
 
+def _sizes4(desc, where):
+    s = _sizes(desc, where)
+    if desc.D % 32:      # what the library says of such a descriptor; there are no sizes to check tensors against
+        raise LmheadError(-2, where)
+    return s
+
+
 def _cache(s, k_codes, k_scales, v_codes, v_scales, dev):
     u8 = torch.uint8
-    return (_arg(k_codes, "k_codes", u8, s.codes, dev), _arg(k_scales, "k_scales", u8, s.scales, dev),
-            _arg(v_codes, "v_codes", u8, s.codes, dev), _arg(v_scales, "v_scales", u8, s.scales, dev))
+    return (_block(k_codes, "k_codes", u8, s.codes, s.codes_shape, dev), _block(k_scales, "k_scales", u8, s.scales, s.scales_shape, dev),
+            _block(v_codes, "v_codes", u8, s.codes, s.codes_shape, dev), _block(v_scales, "v_scales", u8, s.scales, s.scales_shape, dev))
 
 
 def kv4_store(desc, k, v, len_q, len_k, k_codes, k_scales, v_codes, v_scales, ws) -> None:
     """k, v: the new tokens' rows, [B, Tq, Hkv, D]."""
-    s, dev, i32 = _sizes(desc, "kv4_store"), _device(), torch.int32
+    s, dev, i32 = _sizes4(desc, "kv4_store"), _device(), torch.int32
     rc = _lib().kv4_store(
         C.byref(desc), _heads(k, "k", s, s.k_new, dev), _heads(v, "v", s, s.v_new, dev), _arg(len_q, "len_q", i32, s.B, dev),
         _arg(len_k, "len_k", i32, s.B, dev), *_cache(s, k_codes, k_scales, v_codes, v_scales, dev), _arg(ws, "ws", torch.uint8, 0, dev),
@@ -201,11 +239,11 @@ def kv4_store(desc, k, v, len_q, len_k, k_codes, k_scales, v_codes, v_scales, ws
 
 
 def kv4_attn(desc, q, k_codes, k_scales, v_codes, v_scales, len_q, len_k, out, lse, weight, decay, ws) -> None:
-    s, dev, i32, f32 = _sizes(desc, "kv4_attn"), _device(), torch.int32, torch.float32
+    s, dev, i32, f32 = _sizes4(desc, "kv4_attn"), _device(), torch.int32, torch.float32
     rc = _lib().kv4_attn(
         C.byref(desc), _heads(q, "q", s, s.q, dev), *_cache(s, k_codes, k_scales, v_codes, v_scales, dev), _arg(len_q, "len_q", i32, s.B, dev),
-        _arg(len_k, "len_k", i32, s.B, dev), _heads(out, "out", s, s.o, dev), _arg(lse, "lse", f32, s.lse, dev),
-        _arg(weight, "weight", f32, s.weight, dev), decay, _arg(ws, "ws", torch.uint8, 0, dev), ws.numel(), _stream(dev))
+        _arg(len_k, "len_k", i32, s.B, dev), _heads(out, "out", s, s.o, dev), _block(lse, "lse", f32, s.lse, s.lse_shape, dev),
+        _block(weight, "weight", f32, s.weight, s.weight_shape, dev), decay, _arg(ws, "ws", torch.uint8, 0, dev), ws.numel(), _stream(dev))
     _check(rc, "kv4_attn")
 
 
@@ -267,8 +305,11 @@ def cache_evict(desc, planes: CachePlanes, weight, lens, lens_out, kept, ws) -> 
             _bad(f"plane {i}", f"[{desc.B}, {desc.T}, {desc.Hkv}, .] expected, got {tuple(t.shape)}")
         if planes.storages[i].data_ptr() != planes.addresses[i]:
             _bad(f"plane {i}", "its storage was resized after the list was made")
+    rows = desc.B * desc.Hkv
     rc = lib.cache_evict(
-        C.byref(desc), planes.array, len(planes), _arg(weight, "weight", torch.float32, desc.B * desc.Hkv * desc.T, dev),
+        C.byref(desc), planes.array, len(planes),
+        _block(weight, "weight", torch.float32, rows * desc.T, torch.Size((desc.B, desc.Hkv, desc.T)), dev),
         _arg(lens, "lens", i32, desc.B, dev), _arg(lens_out, "lens_out", i32, desc.B, dev),
-        _arg(kept, "kept", i32, desc.B * desc.Hkv * desc.keep, dev), _arg(ws, "ws", torch.uint8, 0, dev), ws.numel(), _stream(dev))
+        _block(kept, "kept", i32, rows * desc.keep, torch.Size((desc.B, desc.Hkv, desc.keep)), dev), _arg(ws, "ws", torch.uint8, 0, dev),
+        ws.numel(), _stream(dev))
     _check(rc, "cache_evict")

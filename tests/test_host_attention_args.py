@@ -77,3 +77,76 @@ def test_backward_workspaces_of_the_largest_calls(B, Tq, Tk, Hq, Hkv, dtype):
     lse, before, parts = 4 * B * Hq * Tq, 8 * (B * ((Tk + 127) // 128) + 1), 2 * 512 * 128 * 2 * 64 * 4     # at most 512 workgroups, two parts each
     assert 256 + lse <= L.attn_bwd_workspace_bytes(d) <= 256 + lse + before + parts + 3 * 256
     assert L.attn_workspace_bytes(d) >= 256 + lse
+
+
+def test_tensors_with_more_slots_than_the_descriptor_are_refused(calls):
+    """A head's rows begin at a multiple of the descriptor's slots: in a tensor with more of them every head but the first would be read and written
+    at another head's place.  (The tensors hold more than the call needs, so no access would leave them.)"""
+    import torch
+    d, t, wide = L.make_attn_desc(Bn, Tq, Tk, Hq, Hkv, D, "bf16"), tensors(), tensors(2 * Tk)
+    more_lse = torch.zeros(Bn, Hq, 2 * Tq)
+
+    def fwd(lse=t.lse, weight=t.weight, q=t.q, k=t.k):
+        L.attn_fwd(d, q, k, t.k, None, None, t.q, lse, weight, 1.0, t.ws)
+
+    def store(codes=t.codes, scales=t.scales):
+        L.kv4_store(d, t.k[:, :Tq], t.k[:, :Tq], None, None, codes, scales, t.codes, t.scales, t.ws)
+
+    def attend(codes=t.codes, scales=t.scales, weight=t.weight):
+        L.kv4_attn(d, t.q, t.codes, t.scales, codes, scales, None, None, t.q, t.lse, weight, 1.0, t.ws)
+    fwd(), store(), attend()
+    assert len(calls) == 3
+    calls.clear()
+    for refused in (lambda: fwd(lse=more_lse), lambda: fwd(weight=wide.weight), lambda: store(codes=wide.codes), lambda: store(scales=wide.scales),
+                    lambda: attend(codes=wide.codes), lambda: attend(scales=wide.scales), lambda: attend(weight=wide.weight),
+                    lambda: fwd(weight=wide.weight[:, :, :Tk]), lambda: fwd(weight=wide.weight.view(Bn * Hkv, 2 * Tk)),
+                    lambda: L.attn_bwd(d, t.q, t.k, t.k, None, None, t.q, more_lse, t.q, t.q, t.k, t.k, t.ws),
+                    # as many elements, in another order
+                    lambda: fwd(weight=torch.zeros(Bn, Tk, Hkv)), lambda: fwd(q=torch.zeros(Bn, Hq, Tq, D, dtype=torch.bfloat16)),
+                    lambda: fwd(k=torch.zeros(Bn * Hkv, Tk, D, dtype=torch.bfloat16)), lambda: store(codes=torch.zeros(Bn, Tk, Hkv, D // 2, dtype=torch.uint8)),
+                    # too few
+                    lambda: fwd(weight=t.weight[:1]), lambda: fwd(lse=t.lse[:, :4].contiguous()), lambda: fwd(weight=t.weight.flatten()[1:])):
+        with pytest.raises(ValueError):
+            refused()
+    odd = L.make_attn_desc(Bn, Tq, Tk, Hq, Hkv, 40, "bf16")      # no cache has such rows
+    for call in (lambda: L.kv4_store(odd, t.k, t.k, None, None, t.codes, t.scales, t.codes, t.scales, t.ws),
+                 lambda: L.kv4_attn(odd, t.q, t.codes, t.scales, t.codes, t.scales, None, None, t.q, None, None, 1.0, t.ws)):
+        with pytest.raises(L.LmheadError) as e:
+            call()
+        assert e.value.code == -2
+    # more sequences, flat buffers and merged dimensions mean the same memory
+    for weight in (torch.zeros(Bn + 1, Hkv, Tk), torch.zeros(Bn * Hkv * Tk + 5), t.weight.view(Bn * Hkv, Tk), t.weight.view(Bn, Hkv * Tk), t.weight[None],
+                   t.weight.flatten()):
+        fwd(weight=weight)
+        assert calls[-1][2][7] == weight.data_ptr()
+    for q in (t.q.view(Bn, Tq, Hq * D), t.q.view(Bn * Tq, Hq, D), t.q.flatten(), t.q.view(1, Bn * Tq, Hq, D), torch.zeros(Bn + 1, Tq, Hq, D, dtype=torch.bfloat16)):
+        fwd(q=q)
+        assert calls[-1][2][0] == q.data_ptr()
+    # of one head of one sequence all slots that are used come first
+    one = L.make_attn_desc(1, 1, Tk, 1, 1, D, "bf16")
+    q, k, weight, ws = t.q[:1, :1, :1], t.k[:1, :, :1].contiguous(), torch.zeros(1, 1, 3 * Tk), t.ws
+    L.attn_fwd(one, q, k, k, None, None, q, None, weight, 1.0, ws)
+    assert calls[-1][2][7] == weight.data_ptr()
+
+
+def test_eviction_refuses_weights_and_slots_of_other_shapes(calls):
+    import torch
+    keep = 10
+    d, i32 = L.make_evict_desc(Bn, Tk, Hkv, keep), dict(dtype=torch.int32)
+    t, wide = tensors(), tensors(2 * Tk)
+    planes = SimpleNamespace(tensors=[], storages=[], addresses=[], device=None, array=None)
+    planes = type("Planes", (), dict(vars(planes), __len__=lambda self: 1))()
+    lens, kept = torch.zeros(Bn, **i32), torch.zeros(Bn, Hkv, keep, **i32)
+
+    def evict(weight=t.weight, kept=kept):
+        L.cache_evict(d, planes, weight, None, lens, kept, t.ws)
+    evict()
+    for weight in (torch.zeros(Bn + 1, Hkv, Tk), t.weight.flatten(), t.weight.view(Bn * Hkv, Tk)):
+        evict(weight)
+    evict(kept=kept.flatten())
+    n = len(calls)
+    for change in (dict(weight=wide.weight), dict(weight=torch.zeros(Bn, Tk, Hkv)), dict(kept=torch.zeros(Bn, Hkv, keep + 1, **i32)),
+                   dict(kept=torch.zeros(Bn, keep, Hkv, **i32)), dict(kept=kept[:1])):
+        with pytest.raises(ValueError):
+            evict(**change)
+    assert len(calls) == n
