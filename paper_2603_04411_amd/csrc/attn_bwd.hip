@@ -14,8 +14,9 @@ namespace {
 // share may begin and end inside an item: what it has of that item it leaves as fp32 sums, which attn_parts_kernel adds up in order.
 // (Eight sequences of 1024 to 4096 under a window of 1024, 28 and 4 heads: a workgroup an item, with the queries behind in items of their own, 920 us.)
 
-// Up to so many queries dS goes into dk with sixteen bits instead of eight: over many queries its rounding leaves dk 1.41 times as far off as
-// the rounding of dk alone, whatever the input; over few it depends on the few that carry weight (1.7 seen).
+// Where up to so many queries of a head see a block of keys, dS goes into its dk with sixteen bits instead of eight: over many queries its rounding
+// leaves dk 1.41 times as far off as the rounding of dk alone, whatever the input; over few it depends on the few that carry weight (1.7 seen).
+// That is decided for each block, so that neither a batch's padding nor what lies outside the window changes what a key gets.
 constexpr int kFineQueries = 512;
 
 // Least tiles of a share, where there are fewer than the card takes: a tile is 2 us in bf16 and 7 in fp32, and a part that is cut off is 128 KB
@@ -272,13 +273,14 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dq_kernel(Att
 //
 // Four products of a pair, bound by reads of LDS beside them (q and g are read along rows and across).  The sequences above: 670 to 740 us.
 // (64 keys a wavefront, which halves those reads, takes 512 registers and one wavefront a unit, and was slower by a tenth.)
-template <typename E, int DP, bool kFine>
+template <typename E, int DP>
 __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dkv_kernel(AttnArgs a, KeyShares sh) {
   using El = AttnElem<E>;
   using Frag = typename El::Frag;
   constexpr int BQ = kQueryTile;
   using Tile = AttnTile<E, DP, BQ>;
   constexpr int KS = Tile::KS, DB = DP / 32, STAGE = 2 * Tile::BYTES + 3 * BQ * 4;
+  constexpr bool kSplit = El::size == 2;
   extern __shared__ char lds[];
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t rbase = Tile::row_base(l), cbase = Tile::col_base(l);
@@ -355,73 +357,82 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dkv_kernel(At
       load(lds);
       put(lds);
     }
-    for (int t = 0; t < n; ++t) {
-      char* const cur = lds + (t & 1) * STAGE;
-      char* const next = lds + ((t + 1) & 1) * STAGE;
-      __builtin_amdgcn_s_waitcnt(kWaitVm0);
-      __syncthreads();
-      // (hidden from the compiler, which would keep every address of the loop in a register of its own)
-      uint32_t rb = rbase, cb = cbase;
-      asm volatile("" : "+v"(rb), "+v"(cb));
-      const int rows = min(BQ, nend - ni), pmin = offset + ni, pmax = pmin + rows - 1;
-      if (t + 1 < n) {
-        if (++c == each) c = 0, ++g;
-        place();
-        load(next);
-      }
-      const float* const end = reinterpret_cast<const float*>(cur + 2 * Tile::BYTES);
-      const float* const delta = end + BQ;
-      if (!none_seen(key0, 32, pmin, pmax, a.window, a.sinks)) {
-        f32x16_t s, dp;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0.f;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          El::mma(s, Tile::row_frag(cur, rb, 0, ks), k[ks]);
-          if constexpr (kRowsInLds<E>) El::mma(dp, Tile::row_frag(cur + Tile::BYTES, rb, 0, ks), Tile::row_frag(vrows, rb, 0, ks));
-          else El::mma(dp, Tile::row_frag(cur + Tile::BYTES, rb, 0, ks), v[ks]);
+    auto walk = [&](auto fine) {
+      for (int t = 0; t < n; ++t) {
+        char* const cur = lds + (t & 1) * STAGE;
+        char* const next = lds + ((t + 1) & 1) * STAGE;
+        __builtin_amdgcn_s_waitcnt(kWaitVm0);
+        __syncthreads();
+        // (hidden from the compiler, which would keep every address of the loop in a register of its own)
+        uint32_t rb = rbase, cb = cbase;
+        asm volatile("" : "+v"(rb), "+v"(cb));
+        const int rows = min(BQ, nend - ni), pmin = offset + ni, pmax = pmin + rows - 1;
+        if (t + 1 < n) {
+          if (++c == each) c = 0, ++g;
+          place();
+          load(next);
         }
-        float pr[16], ds[16];
-        const f32x4_t* const ends = reinterpret_cast<const f32x4_t*>(end + 4 * (l >> 5));
-        const f32x4_t* const deltas = reinterpret_cast<const f32x4_t*>(delta + 4 * (l >> 5));
+        const float* const end = reinterpret_cast<const float*>(cur + 2 * Tile::BYTES);
+        const float* const delta = end + BQ;
+        if (!none_seen(key0, 32, pmin, pmax, a.window, a.sinks)) {
+          f32x16_t s, dp;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          float x = fmaf(s[i], a.scale2, -ends[2 * (i >> 2)][i & 3]);
-          if constexpr (El::size == 4) x -= end[2 * BQ + acc_row(i, l)];
-          pr[i] = __builtin_amdgcn_exp2f(x);
-          ds[i] = pr[i] * (dp[i] - deltas[2 * (i >> 2)][i & 3]);
-        }
-        if (rows < BQ || !all_seen(key0, 32, pmin, pmax, a.window, a.sinks)) {
-          // row c sees the key from position pmin + c on, to the end or to the last one whose window reaches it
-          const int lane = 4 * (l >> 5), low = key - pmin - lane;
-          const int high = (key < a.sinks ? rows - 1 : min(rows - 1, key + a.window - 1 - pmin)) - lane;
+          for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0.f;
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) {
+            El::mma(s, Tile::row_frag(cur, rb, 0, ks), k[ks]);
+            if constexpr (kRowsInLds<E>) El::mma(dp, Tile::row_frag(cur + Tile::BYTES, rb, 0, ks), Tile::row_frag(vrows, rb, 0, ks));
+            else El::mma(dp, Tile::row_frag(cur + Tile::BYTES, rb, 0, ks), v[ks]);
+          }
+          float pr[16], ds[16];
+          const f32x4_t* const ends = reinterpret_cast<const f32x4_t*>(end + 4 * (l >> 5));
+          const f32x4_t* const deltas = reinterpret_cast<const f32x4_t*>(delta + 4 * (l >> 5));
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            const int c = acc_row(i, 0);
-            const bool yes = (c >= low) & (c <= high);
-            pr[i] = yes ? pr[i] : 0.f;
-            ds[i] = yes ? ds[i] : 0.f;
+            float x = fmaf(s[i], a.scale2, -ends[2 * (i >> 2)][i & 3]);
+            if constexpr (El::size == 4) x -= end[2 * BQ + acc_row(i, l)];
+            pr[i] = __builtin_amdgcn_exp2f(x);
+            ds[i] = pr[i] * (dp[i] - deltas[2 * (i >> 2)][i & 3]);
           }
-        }
-        const Frag pf[2] = {El::of(pr), El::of(pr + 8)};
-        Frag sf[2], low[2];
+          if (rows < BQ || !all_seen(key0, 32, pmin, pmax, a.window, a.sinks)) {
+            // row c sees the key from position pmin + c on, to the end or to the last one whose window reaches it
+            const int lane = 4 * (l >> 5), low = key - pmin - lane;
+            const int high = (key < a.sinks ? rows - 1 : min(rows - 1, key + a.window - 1 - pmin)) - lane;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if constexpr (kFine) El::split(ds + 8 * h, sf[h], low[h]);
-          else sf[h] = El::of(ds + 8 * h);
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int db = 0; db < DB; ++db) {
-            El::mma(dv[db], Tile::col_frag(cur + Tile::BYTES, cb, db, h), pf[h]);
-            const Frag qf = Tile::col_frag(cur, cb, db, h);
-            El::mma(dk[db], qf, sf[h]);
-            if constexpr (kFine) El::mma(dk[db], qf, low[h]);
+            for (int i = 0; i < 16; ++i) {
+              const int c = acc_row(i, 0);
+              const bool yes = (c >= low) & (c <= high);
+              pr[i] = yes ? pr[i] : 0.f;
+              ds[i] = yes ? ds[i] : 0.f;
+            }
           }
+          const Frag pf[2] = {El::of(pr), El::of(pr + 8)};
+          Frag sf[2], low[2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if constexpr (kSplit) {
+              if constexpr (decltype(fine)::value) El::split(ds + 8 * h, sf[h], low[h]);
+              else sf[h] = El::of(ds + 8 * h);
+            } else {
+              sf[h] = El::of(ds + 8 * h);
+            }
+          }
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int db = 0; db < DB; ++db) {
+              El::mma(dv[db], Tile::col_frag(cur + Tile::BYTES, cb, db, h), pf[h]);
+              const Frag qf = Tile::col_frag(cur, cb, db, h);
+              El::mma(dk[db], qf, sf[h]);
+              if constexpr (decltype(fine)::value) El::mma(dk[db], qf, low[h]);
+            }
+        }
+        if (t + 1 < n) put(next);
       }
-      if (t + 1 < n) put(next);
-    }
+    };
+    const int seers = item.far0 - item.i0 + (item.far ? lq - item.far0 : 0);      // queries of a head that see the block
+    if (kSplit && seers <= kFineQueries) walk(std::integral_constant<bool, kSplit>{});
+    else walk(std::false_type{});
     if (!sh.whole && (x.from > 0 || x.to < x.tiles)) {
       // slot 0: the end of an item, or its middle; slot 1: the beginning of one
       float* const to = a.part + ((int64_t)(2 * wg + (x.from > 0 ? 0 : 1)) * kKeyBlock + w * 32 + (l & 31)) * (2 * DP);
@@ -503,20 +514,16 @@ template <typename E, int DP>
 hipError_t bwd(const KeyShares& sh, AttnArgs a, hipStream_t s) {
   constexpr int BK = 32, fixed = kRowsInLds<E> ? 4 * AttnTile<E, DP, 32>::BYTES : 0;
   constexpr auto dq = attn_dq_kernel<E, DP, BK>;
-  constexpr bool kSplit = kRowsInLds<E>;
-  constexpr auto coarse = attn_dkv_kernel<E, DP, false>;
-  constexpr auto fine = attn_dkv_kernel<E, DP, kSplit>;
+  constexpr auto dkv = attn_dkv_kernel<E, DP>;
   const int bytes = 4 * AttnTile<E, DP, BK>::BYTES + fixed, more = bytes + 6 * BK * 4;
   hipError_t e = allow_lds<dq>(bytes);
-  if (e == hipSuccess) e = allow_lds<coarse>(more);
-  if (e == hipSuccess) e = allow_lds<fine>(more);
+  if (e == hipSuccess) e = allow_lds<dkv>(more);
   if (e != hipSuccess) return e;
   a.nblk = (int)(((int64_t)a.Tq * a.G + 127) / 128);
   dq<<<attn_grid(attn_wgs((int64_t)a.B * a.Hkv, a.nblk)), 256, bytes, s>>>(a, sh.whole ? 0 : sh.nkey);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (a.Tq <= kFineQueries) fine<<<attn_grid(sh.wgs), 256, more, s>>>(a, sh);
-  else coarse<<<attn_grid(sh.wgs), 256, more, s>>>(a, sh);
+  dkv<<<attn_grid(sh.wgs), 256, more, s>>>(a, sh);
   e = hipGetLastError();
   if (e != hipSuccess || sh.whole) return e;
   attn_parts_kernel<E, DP><<<attn_grid((int64_t)kSumGroups * sh.wgs + (int64_t)a.B * a.Hkv * sh.nkey), 256, 0, s>>>(a, sh);
