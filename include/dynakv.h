@@ -230,7 +230,9 @@ LMHEAD_API size_t attn_workspace_bytes(const attn_desc* desc);
  *                   queries i and the heads that read h, for j < len_k[b]; the rest is left as it was.  With decay = 0 the old
  *                   value is not read.
  *   decay           finite, >= 0
- * Outputs share no memory with an input or each other; equal addresses are refused (LMHEAD_E_SHAPE), here and below.
+ * Outputs, and the part of the workspace that is used, share no memory with an input or each other.  Here and below a call is refused
+ * (LMHEAD_E_SHAPE) where two of them begin at the same place, or where one without gaps shares memory with another; of two tensors
+ * with gaps, such as heads of one buffer side by side, that is the caller's to see to.
  */
 LMHEAD_API int attn_fwd(const attn_desc* desc, const void* q, const void* k, const void* v, const int32_t* len_q,
                         const int32_t* len_k, void* out, float* lse, float* weight, float decay, void* ws, size_t ws_bytes,

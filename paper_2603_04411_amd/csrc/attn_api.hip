@@ -6,6 +6,7 @@
 #include <initializer_list>
 
 #include "attn_common.h"
+#include "attn_regions.h"
 
 namespace lmhead {
 
@@ -89,7 +90,7 @@ bool apart(const attn_layout& x, int64_t n, int64_t t, int64_t h, int64_t width)
   for (const Dim& k : d) {
     if (k.size == 1) continue;
     if (k.stride < extent) return false;
-    extent += k.stride * (k.size - 1);
+    extent += spanned(k.stride, k.size);
   }
   return true;
 }
@@ -168,17 +169,32 @@ int run_fwd(const attn_desc* d, const AttnPlan& p, AttnArgs& a, void* ws, float*
   return LMHEAD_OK;
 }
 
-// Whether no output is another output or an input.  (Views of one buffer begin at different places; that they lie apart is the caller's.)
-bool different(std::initializer_list<const void*> outputs, std::initializer_list<const void*> inputs) {
+// Whether no output shares memory with another output or an input.
+bool different(std::initializer_list<Region> outputs, std::initializer_list<Region> inputs) {
   for (auto o = outputs.begin(); o != outputs.end(); ++o) {
-    if (!*o) continue;
     for (auto x = outputs.begin(); x != o; ++x)
-      if (*x == *o) return false;
-    for (const void* x : inputs)
-      if (x == *o) return false;
+      if (share(*x, *o)) return false;
+    for (const Region& x : inputs)
+      if (share(x, *o)) return false;
   }
   return true;
 }
+
+// The tensors of a descriptor.
+struct Regions {
+  const attn_desc* d;
+  int esz;
+  explicit Regions(const attn_desc* desc) : d(desc), esz(desc->dtype == LMHEAD_BF16 ? 2 : 4) {}
+  Region q(const void* p, const attn_layout& x) const { return Region(p, x, d->B, d->Tq, d->Hq, (int64_t)d->D * esz, esz); }
+  Region k(const void* p, const attn_layout& x) const { return Region(p, x, d->B, d->Tk, d->Hkv, (int64_t)d->D * esz, esz); }
+  Region added(const void* p, const attn_layout& x) const { return Region(p, x, d->B, d->Tq, d->Hkv, (int64_t)d->D * esz, esz); }
+  Region len(const int32_t* p) const { return Region(p, (int64_t)d->B * 4); }
+  Region lse(const float* p) const { return Region(p, (int64_t)d->B * d->Hq * d->Tq * 4); }
+  Region weight(const float* p) const { return Region(p, rows() * 4); }
+  Region codes(const uint8_t* p) const { return Region(p, rows() * (d->D / 2)); }
+  Region scales(const uint8_t* p) const { return Region(p, rows() * (d->D / 32)); }
+  int64_t rows() const { return (int64_t)d->B * d->Hkv * d->Tk; }
+};
 
 int check_weight(const float* weight, float decay) {
   return weight && !(decay >= 0.f && isfinite(decay)) ? LMHEAD_E_SHAPE : LMHEAD_OK;
@@ -211,9 +227,12 @@ int attn_fwd(const attn_desc* desc, const void* q, const void* k, const void* v,
   if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16) || !aligned(ws, 256)) return LMHEAD_E_ALIGN;
   rc = check_weight(weight, decay);
   if (rc != LMHEAD_OK) return rc;
-  if (!different({out, lse, weight, ws}, {q, k, v, len_q, len_k})) return LMHEAD_E_SHAPE;
   const AttnPlan p = attn_plan(desc);
   if (ws_bytes < p.total) return LMHEAD_E_WORKSPACE;
+  const Regions x(desc);
+  if (!different({x.q(out, desc->o), x.lse(lse), x.weight(weight), Region(ws, p.total)},
+                 {x.q(q, desc->q), x.k(k, desc->k), x.k(v, desc->v), x.len(len_q), x.len(len_k)}))
+    return LMHEAD_E_SHAPE;
   const int esz = desc->dtype == LMHEAD_BF16 ? 2 : 4;
   AttnArgs a = arguments(desc, p, len_q, len_k, ws);
   a.q = tensor(q, desc->q, esz), a.k = tensor(k, desc->k, esz), a.v = tensor(v, desc->v, esz), a.o = tensor(out, desc->o, esz);
@@ -239,8 +258,12 @@ int attn_bwd(const attn_desc* desc, const void* q, const void* k, const void* v,
   for (const void* x : {q, k, v, out, g_out, static_cast<const void*>(dq), static_cast<const void*>(dk), static_cast<const void*>(dv)})
     if (!aligned(x, 16)) return LMHEAD_E_ALIGN;
   if (!aligned(ws, 256)) return LMHEAD_E_ALIGN;
-  if (!different({dq, dk, dv, ws}, {q, k, v, out, lse, g_out, len_q, len_k})) return LMHEAD_E_SHAPE;
-  if (ws_bytes < attn_bwd_workspace_bytes(desc)) return LMHEAD_E_WORKSPACE;
+  const size_t need = attn_bwd_workspace_bytes(desc);
+  if (ws_bytes < need) return LMHEAD_E_WORKSPACE;
+  const Regions x(desc);
+  if (!different({x.q(dq, desc->q), x.k(dk, desc->k), x.k(dv, desc->v), Region(ws, need)},
+                 {x.q(q, desc->q), x.k(k, desc->k), x.k(v, desc->v), x.q(out, desc->o), x.lse(lse), x.q(g_out, desc->o), x.len(len_q), x.len(len_k)}))
+    return LMHEAD_E_SHAPE;
   const AttnPlan p = attn_plan(desc);
   AttnArgs a = arguments(desc, p, len_q, len_k, ws);
   a.q = tensor(q, desc->q, esz), a.k = tensor(k, desc->k, esz), a.v = tensor(v, desc->v, esz), a.o = tensor(out, desc->o, esz);
@@ -263,8 +286,11 @@ int kv4_store(const attn_desc* desc, const void* k, const void* v, const int32_t
   if (!aligned(k, 16) || !aligned(v, 16) || !aligned(k_codes, 16) || !aligned(v_codes, 16) || !aligned(k_scales, 4) ||
       !aligned(v_scales, 4) || !aligned(ws, 256))
     return LMHEAD_E_ALIGN;
-  if (!different({k_codes, k_scales, v_codes, v_scales, ws}, {k, v, len_q, len_k})) return LMHEAD_E_SHAPE;
   if (ws_bytes < sizeof(AttnHeader)) return LMHEAD_E_WORKSPACE;
+  const Regions x(desc);
+  if (!different({x.codes(k_codes), x.scales(k_scales), x.codes(v_codes), x.scales(v_scales), Region(ws, sizeof(AttnHeader))},
+                 {x.added(k, desc->k), x.added(v, desc->v), x.len(len_q), x.len(len_k)}))
+    return LMHEAD_E_SHAPE;
   const int esz = desc->dtype == LMHEAD_BF16 ? 2 : 4;
   AttnArgs a = arguments(desc, attn_plan(desc), len_q, len_k, ws);
   a.k = tensor(k, desc->k, esz), a.v = tensor(v, desc->v, esz);
@@ -285,9 +311,12 @@ int kv4_attn(const attn_desc* desc, const void* q, const uint8_t* k_codes, const
     return LMHEAD_E_ALIGN;
   rc = check_weight(weight, decay);
   if (rc != LMHEAD_OK) return rc;
-  if (!different({out, lse, weight, ws}, {q, k_codes, k_scales, v_codes, v_scales, len_q, len_k})) return LMHEAD_E_SHAPE;
   const AttnPlan p = attn_plan(desc);
   if (ws_bytes < p.total) return LMHEAD_E_WORKSPACE;
+  const Regions x(desc);
+  if (!different({x.q(out, desc->o), x.lse(lse), x.weight(weight), Region(ws, p.total)},
+                 {x.q(q, desc->q), x.codes(k_codes), x.scales(k_scales), x.codes(v_codes), x.scales(v_scales), x.len(len_q), x.len(len_k)}))
+    return LMHEAD_E_SHAPE;
   const int esz = desc->dtype == LMHEAD_BF16 ? 2 : 4;
   AttnArgs a = arguments(desc, p, len_q, len_k, ws);
   a.q = tensor(q, desc->q, esz), a.o = tensor(out, desc->o, esz);
@@ -304,7 +333,12 @@ int cache_evict(const evict_desc* desc, const cache_plane* planes, int32_t count
   const int rc = validate_evict(desc);
   if (rc != LMHEAD_OK) return rc;
   if (!planes || !weight || !len_out || !kept || !ws) return LMHEAD_E_NULL;
-  if (count < 1 || count > EVICT_PLANES || !different({weight, len_out, kept, ws}, {len})) return LMHEAD_E_SHAPE;
+  if (count < 1 || count > EVICT_PLANES) return LMHEAD_E_SHAPE;
+  const int64_t heads = (int64_t)desc->B * desc->Hkv;
+  const Region w(weight, heads * desc->T * 4), in(len, (int64_t)desc->B * 4), out(len_out, (int64_t)desc->B * 4), slots(kept, heads * desc->keep * 4);
+  const Region scratch(ws, sizeof(AttnHeader));
+  if (!different({w, out, slots, scratch}, {in})) return LMHEAD_E_SHAPE;
+  Region moved[EVICT_PLANES];
   for (int i = 0; i < count; ++i) {
     const cache_plane& p = planes[i];
     if (!p.data) return LMHEAD_E_NULL;
@@ -312,11 +346,12 @@ int cache_evict(const evict_desc* desc, const cache_plane* planes, int32_t count
     for (int64_t v : {p.seq, p.slot, p.head, p.bytes})
       if (v % 4 != 0) return LMHEAD_E_ALIGN;
     if (!aligned(p.data, 4)) return LMHEAD_E_ALIGN;
-    for (int j = 0; j < i; ++j)
-      if (planes[j].data == p.data) return LMHEAD_E_SHAPE;
-    if (!different({p.data}, {weight, len, len_out, kept, ws})) return LMHEAD_E_SHAPE;
     const attn_layout x{p.seq, p.slot, p.head};
     if (!strides(x) || !apart(x, desc->B, desc->T, desc->Hkv, p.bytes)) return LMHEAD_E_SHAPE;
+    moved[i] = Region(p.data, x, desc->B, desc->T, desc->Hkv, p.bytes, 1);
+    for (int j = 0; j < i; ++j)
+      if (share(moved[j], moved[i])) return LMHEAD_E_SHAPE;
+    if (!different({moved[i]}, {w, in, out, slots, scratch})) return LMHEAD_E_SHAPE;
   }
   if (!aligned(ws, 256)) return LMHEAD_E_ALIGN;
   if (ws_bytes < sizeof(AttnHeader)) return LMHEAD_E_WORKSPACE;

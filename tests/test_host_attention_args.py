@@ -2,6 +2,7 @@
 import copy
 import ctypes as C
 import os
+import subprocess
 from types import SimpleNamespace
 
 import pytest
@@ -150,3 +151,79 @@ def test_eviction_refuses_weights_and_slots_of_other_shapes(calls):
         with pytest.raises(ValueError):
             evict(**change)
     assert len(calls) == n
+
+
+# ---- tensors that share memory (pointers are never dereferenced: every call here is refused) ----
+
+FAR = 1 << 24
+
+
+def _raw(name, d, shift):
+    """The call with its pointers FAR apart but for argument `at`, which begins `by` bytes from argument `to`."""
+    at, to, by = shift
+    n = {"attn_fwd": 9, "attn_bwd": 12, "kv4_store": 9, "kv4_attn": 11}[name]
+    p = [FAR * (i + 1) for i in range(n)]
+    p[at] = p[to] + by
+    rest = (C.c_size_t(1 << 30), None)
+    if name in ("attn_fwd", "kv4_attn"):
+        return getattr(B._lib(), name)(C.byref(d), *p[:-1], 1.0, p[-1], *rest)
+    return getattr(B._lib(), name)(C.byref(d), *p, *rest)
+
+
+ARGS = {
+    "attn_fwd": ("q k v len_q len_k out lse weight ws", "out lse weight ws"), "attn_bwd": ("q k v len_q len_k out lse g dq dk dv ws", "dq dk dv ws"),
+    "kv4_store": ("k v len_q len_k k_codes k_scales v_codes v_scales ws", "k_codes k_scales v_codes v_scales ws"),
+    "kv4_attn": ("q k_codes k_scales v_codes v_scales len_q len_k out lse weight ws", "out lse weight ws"),
+}
+
+
+@pytest.mark.parametrize("name", ARGS)
+def test_outputs_that_share_memory_are_refused(name):
+    """Every output against every other tensor of the call: at the same place, 256 bytes behind its beginning, and the other way round."""
+    names, outputs = (x.split() for x in ARGS[name])
+    d = L.make_attn_desc(128, 40, 40, Hq, Hkv, 64, "bf16")      # every tensor takes 512 bytes at least
+    for o in outputs:
+        for i, x in enumerate(names):
+            if x == o:
+                continue
+            assert _raw(name, d, (names.index(o), i, 0)) == -2, (o, x)
+            for first, second in ((o, x), (x, o)):
+                if (name, second) != ("kv4_store", "ws"):      # its header is all that is used
+                    assert _raw(name, d, (names.index(first), names.index(second), 256)) == -2, (first, second)
+
+
+def test_a_dense_output_among_the_rows_of_a_tensor_with_gaps():
+    """lse (2560 bytes) in the gap of 3 KB behind each slot of q is the caller's; where it reaches into a row the call is refused."""
+    d = L.make_attn_desc(Bn, 40, 40, Hq, Hkv, 64, "bf16", q=(40 * 2048, 2048, 64))      # a slot's 1 KB, then nothing for 3 KB
+    row, slot = Hq * 64 * 2, 4096
+    names = ARGS["attn_fwd"][0].split()
+    assert 4 * Bn * Hq * 40 == 2560
+    for by in (row - 16, slot - 2560 + 16, 7 * slot - 1024, 79 * slot, 79 * slot + row - 16):
+        assert _raw("attn_fwd", d, (names.index("lse"), names.index("q"), by)) == -2, by
+
+
+def test_eviction_refuses_planes_that_share_memory():
+    d = L.make_evict_desc(2, 40, 3, 10)
+    row, lib = (40 * 3 * 64, 3 * 64, 64, 64), B._lib()
+
+    def evict(shift, plane=(FAR * 8, FAR * 9)):
+        p = [FAR * (i + 1) for i in range(5)]      # weight len len_out kept ws
+        for at, x in shift.items():
+            p[at] = x
+        a = (B._Plane * 2)()
+        for i, x in enumerate(plane):
+            a[i] = B._Plane(x, *row)
+        return lib.cache_evict(C.byref(d), a, 2, *p, 256, None)
+    size = 2 * 40 * 3 * 64
+    assert evict({}, (FAR * 8, FAR * 8 + size - 4)) == -2 and evict({}, (FAR * 8 + 64, FAR * 8)) == -2
+    for at, n in ((0, 2 * 3 * 40 * 4), (2, 8), (3, 2 * 3 * 10 * 4), (4, 256)):
+        assert evict({at: FAR * 8 + size - 256}) == -2 and evict({at: FAR * 9}) == -2, at
+    assert evict({3: FAR + 2 * 3 * 40 * 4 - 4}) == -2 and evict({2: FAR * 4 + 4}) == -2 and evict({2: FAR * 2 + 4}) == -2 and evict({0: FAR * 5 - 4}) == -2
+
+
+def test_overlaps_byte_by_byte(tmp_path):
+    exe = tmp_path / "regions_check"
+    source = os.path.join(os.path.dirname(os.path.abspath(__file__)), "host", "regions_check.cpp")
+    subprocess.run(["g++", "-O2", "-std=c++17", "-o", str(exe), source], check=True)
+    r = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert r.returncode == 0 and "bad=0" in r.stdout, r.stdout + r.stderr
