@@ -436,13 +436,17 @@ __global__ __launch_bounds__(256) void attn_finish_kernel(AttnArgs a, int njoin,
   __syncthreads();
   if (key0 >= lk) return;
   f32x4_t sum = f32x4_t{0, 0, 0, 0};
+  // (a key that a row does not see has the logit -inf: it adds nothing, also where the row's sum is NaN, or 0 because it sees no key)
   if (all) {
 #pragma unroll
     for (int r = 0; r < kLogitRows; ++r) {
       if (r >= R) break;
       const float top = s_top[r], inv = s_total[r];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sum[i] = fmaf(inv == 0.f ? 0.f : __builtin_amdgcn_exp2f(z[r][i] - top), inv, sum[i]);
+      for (int i = 0; i < 4; ++i) {
+        const float e = __builtin_amdgcn_exp2f(z[r][i] - top);
+        sum[i] = e == 0.f ? sum[i] : fmaf(e, inv, sum[i]);
+      }
     }
   } else if (pmax >= 0) {
 #pragma unroll
@@ -450,7 +454,10 @@ __global__ __launch_bounds__(256) void attn_finish_kernel(AttnArgs a, int njoin,
       const int key = key0 + i;
       if (key >= kt.e0 && key < kt.lo) continue;
       const float* const x = reinterpret_cast<const float*>(logits + (int64_t)(place(key) >> 2) * R) + (place(key) & 3);
-      for (int r = 0; r < R; ++r) sum[i] = fmaf(s_total[r] == 0.f ? 0.f : __builtin_amdgcn_exp2f(x[r * 4] - s_top[r]), s_total[r], sum[i]);
+      for (int r = 0; r < R; ++r) {
+        const float e = __builtin_amdgcn_exp2f(x[r * 4] - s_top[r]);
+        sum[i] = e == 0.f ? sum[i] : fmaf(e, s_total[r], sum[i]);
+      }
     }
   }
   float* const to = a.weight + (int64_t)bh * a.Tk + key0;
