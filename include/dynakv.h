@@ -186,8 +186,9 @@ LMHEAD_API int dynakv_check(void* ws, void* stream);
  *    lists are host memory.  The workspace's error word is read by lmhead_check(): a length outside [0, T], taken as the nearest
  *    one inside.  A workspace belongs to one call at a time.
  *  - What lies in slots from a sequence's length on is never used, whatever its bits, nor is a key that no query of the call
- *    sees.  An infinity or NaN in a key or value that some queries see can reach others that do not, whose rows share a tile of a
- *    matrix product with it (0 times an infinity is NaN): those up to 127 positions away.
+ *    sees.  An infinity or NaN in a key or value that some queries see can reach out and dq of others that do not, whose rows share a
+ *    tile of a matrix product with it (0 times an infinity is NaN): those up to 127 positions from one that sees it.  One in a query
+ *    or in its g_out can likewise reach dk and dv of keys that the query does not see: those up to 62 positions from one that it sees.
  *  - Logits, softmax and all sums are fp32.  With bf16 storage P, and in the backward dS, are rounded to bf16 before they
  *    enter a matrix product, as are the outputs.
  */

@@ -3,7 +3,8 @@ import numpy as np
 import pytest
 
 from oracle import attention_oracle as A
-from tests.test_gpu_attention import Problem
+from tests.attention_cases import holds
+from tests.test_gpu_attention import Problem, np64
 from tests.test_gpu_kv_cache import Cache4
 
 pytestmark = pytest.mark.gpu
@@ -47,3 +48,76 @@ def test_a_query_over_four_bits_gives_weight_only_to_keys_it_sees(bad):
     p = Cache4(2, 4, 900, 4, 2, 64, window=50, sinks=3, seed=52)
     seen = A.visible(4, 900, 50, 3)[1]
     _weights(p, lambda: p.attend(0.5), seen, 1, (1, 1, 2, bad))
+
+
+def _copy(ts):
+    return [t.clone() for t in ts]
+
+
+def _seen(p, b, i):
+    return A.visible(p.lq[b], p.lk[b], p.window, p.sinks)[i]
+
+
+CASES = [dict(B=2, Tq=500, Tk=600, Hq=4, Hkv=2, D=64, window=100, sinks=3), dict(B=2, Tq=500, Tk=600, Hq=4, Hkv=2, D=128, window=100, sinks=3, dtype="f32"),
+         dict(B=1, Tq=300, Tk=300, Hq=2, Hkv=2, D=64), dict(B=1, Tq=40, Tk=300, Hq=2, Hkv=2, D=64, window=33, sinks=40)]
+
+
+@BAD
+@pytest.mark.parametrize("where", ["q", "g"])
+@pytest.mark.parametrize("case", CASES, ids=range(len(CASES)))
+def test_a_query_or_its_gradient_reaches_keys_62_positions_from_those_it_sees(case, where, bad):
+    """dk and dv of keys further away, of other key heads and of other sequences stay, and dq of other queries."""
+    import torch
+    p = Problem(seed=53, **case)
+    p.fwd(weight=False)
+    p.bwd(p.out)
+    clean = _copy((p.dq, p.dk, p.dv))
+    i, h = 2 * p.lq[0] // 3, 1
+    (p.q if where == "q" else p.g)[0, i, h, 5] = bad
+    p.fwd(weight=False)
+    p.bwd(p.out)
+    near = np.zeros(p.lk[0], dtype=bool)
+    for j in np.flatnonzero(_seen(p, 0, i)):
+        near[max(0, j - 62):j + 63] = True
+    assert near.any()
+    dq, dk, dv = (x.clone() for x in (p.dq, p.dk, p.dv))
+    hk, rows = h // (case["Hq"] // case["Hkv"]), torch.from_numpy(np.flatnonzero(near)).cuda()
+    for got, want in ((dk, clean[1]), (dv, clean[2])):
+        got[0, rows, hk] = want[0, rows, hk]
+        assert torch.equal(got, want)
+    dq[0, i, h] = clean[0][0, i, h]
+    assert torch.equal(dq, clean[0])
+
+
+@BAD
+@pytest.mark.parametrize("where", ["k", "v"])
+@pytest.mark.parametrize("case", CASES, ids=range(len(CASES)))
+def test_a_key_or_value_reaches_queries_127_positions_from_those_that_see_it(case, where, bad):
+    """out, lse and dq of queries further away, of heads that read another key head and of other sequences stay.  lse of nearer ones that do not see it
+    keeps its derived bound: the maximum that a wavefront's exponentials are taken against moves for all of its rows when it moves for one."""
+    import torch
+    p = Problem(seed=54, **case)
+    p.fwd(weight=False)
+    p.bwd(p.out)
+    clean = _copy((p.out, p.dq, p.lse))
+    j = p.lk[0] - p.lq[0] + p.lq[0] // 4
+    (p.k if where == "k" else p.v)[0, j, 1, 5] = bad
+    p.fwd(weight=False)
+    p.bwd(p.out)
+    sees = A.visible(p.lq[0], p.lk[0], p.window, p.sinks)[:, j]
+    near = np.zeros(p.lq[0], dtype=bool)
+    for i in np.flatnonzero(sees):
+        near[max(0, i - 127):i + 128] = True
+    heads = slice(case["Hq"] // case["Hkv"], 2 * case["Hq"] // case["Hkv"])
+    out, dq, lse = _copy((p.out, p.dq, p.lse))
+    rows = torch.from_numpy(np.flatnonzero(near)).cuda()
+    for got, want in ((out, clean[0]), (dq, clean[1])):
+        got[0, rows, heads] = want[0, rows, heads]
+        assert torch.equal(got, want)
+    far = np.ones(clean[2].shape, dtype=bool)
+    far[0, heads] = ~near
+    far = torch.from_numpy(far).cuda()
+    assert torch.equal(lse[far], clean[2][far])
+    want, bound = p.exact()      # of the inputs without the bad one
+    for x in (lse, clean[2]):
+        holds(np64(x)[0, heads][:, ~sees], want["lse"][0, heads][:, ~sees], bound["lse"][0, heads][:, ~sees], "lse")
