@@ -190,7 +190,8 @@ LMHEAD_API int dynakv_check(void* ws, void* stream);
  *    tile of a matrix product with it (0 times an infinity is NaN): those up to 127 positions from one that sees it.  One in a query
  *    or in its g_out can likewise reach dk and dv of keys that the query does not see: those up to 62 positions from one that it sees.
  *  - Logits, softmax and all sums are fp32.  With bf16 storage P, and in the backward dS, are rounded to bf16 before they
- *    enter a matrix product, as are the outputs.
+ *    enter a matrix product, as are the outputs.  Sixteen bits of P enter out where a key head has up to 32 rows (queries times
+ *    heads) over keys in bf16, and sixteen of dS enter dq, and dk of keys that few queries see.
  */
 
 /* Where element (sequence b, slot t, head h, c) lies: b * seq + t * slot + h * head + c, in elements.  Each stride is a

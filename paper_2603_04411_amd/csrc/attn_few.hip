@@ -143,6 +143,10 @@ constexpr int few_lds() {      // of a wavefront: a tile of values, then its sum
 // and join them through LDS.  Nothing is shared in the loop, so there is no barrier in it: a wavefront asks for its next tile in registers
 // before the softmax of this one.
 //
+// P goes into its product as two bf16 numbers (kFineP): one leaves out 1.3 times as far off as its own rounding does (2.2e-3 against 1.66e-3, relative
+// to 64 bits), and beside the reading the second one's product costs nothing (64 x 8192: 229 us with and without).  Over 4 bits, where conversions count
+// and the cache itself is off by far more, it is one: 1.96e-3, and 143 us instead of 147 of 64 sequences up to 16001.
+//
 // Bound by the reading of the cache.  Rows and keys are on 16x16 blocks: a group of four rows fills a quarter of one, which is cheaper than
 // a product in vector instructions.  64 sequences of 2048 to 8192, 32 and 8 heads of 128: 225 us, 6.0 TB/s; in 4 bits, up to 16001: 129 us, and
 // 32 rows over 131072 keys 45 us, where the exponentials and the conversion to bf16 weigh more than the 143 MB.
@@ -153,6 +157,7 @@ __global__ __launch_bounds__(kFewWaves * 64, AttnElem<E>::size == 2 ? 2 : 1) voi
   using Load = typename std::conditional<kCache, Coded<E, DP, TK, kPast>, Plain<E, DP, TK, kPast>>::type;
   using Tile = AttnTile<E, DP, TK>;
   constexpr int KS = DP / 32, KB = TK / 16, DB = DP / 16, WLDS = few_lds<E, DP, NN, TK>();
+  constexpr bool kFineP = El::size == 2 && !kCache;
   extern __shared__ char lds_all[];
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = l >> 4;
   char* const lds = lds_all + w * WLDS;
@@ -262,18 +267,22 @@ __global__ __launch_bounds__(kFewWaves * 64, AttnElem<E>::size == 2 ? 2 : 1) voi
     }
 #pragma unroll
     for (int kg = 0; kg < KB / 2; ++kg) {
-      Frag pf[NN];
+      Frag pf[NN], low[NN];
 #pragma unroll
       for (int nn = 0; nn < NN; ++nn) {
         const float x[8] = {s[nn][2 * kg][0], s[nn][2 * kg][1], s[nn][2 * kg][2], s[nn][2 * kg][3],
                             s[nn][2 * kg + 1][0], s[nn][2 * kg + 1][1], s[nn][2 * kg + 1][2], s[nn][2 * kg + 1][3]};
-        pf[nn] = El::of(x);
+        if constexpr (kFineP) El::split(x, pf[nn], low[nn]);
+        else pf[nn] = El::of(x);
       }
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
         const Frag vf = Tile::col_frag16(lds, cbase, db, kg);
 #pragma unroll
-        for (int nn = 0; nn < NN; ++nn) El::mma(o[nn][db], vf, pf[nn]);
+        for (int nn = 0; nn < NN; ++nn) {
+          El::mma(o[nn][db], vf, pf[nn]);
+          if constexpr (kFineP) El::mma(o[nn][db], vf, low[nn]);
+        }
       }
     }
   }

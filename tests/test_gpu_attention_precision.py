@@ -1,7 +1,8 @@
-"""How dS enters dk with bf16 storage: where at most 512 queries of a head see a block of 128 keys, as two bf16 numbers, whatever the slots for queries.
+"""Where bf16 storage does not mean that a factor is rounded to bf16: dS in dk, where at most 512 queries of a head see a block of 128 keys (whatever the
+slots for queries), and P in out, of up to 32 rows over a plain cache, are two bf16 numbers.
 
-With two numbers what rounding leaves of dS is u^2 |dS| (the high part is off by u |dS| at most, the difference from it is exact in fp32, and the low
-part is off by u of that), where ``attention_cases.bounds`` has u |dS|: the bounds here are those less what the coarser rounding was allowed."""
+With two numbers what rounding leaves of x is u^2 |x| (the high part is off by u |x| at most, the difference from it is exact in fp32, and the low part
+is off by u of that), where ``attention_cases.bounds`` has u |x|: the bounds here are those less what the coarser rounding was allowed."""
 import numpy as np
 import pytest
 
@@ -59,3 +60,26 @@ def test_few_queries_keep_sixteen_bits_of_ds(case, share):
     holds(got, want["dk"], bound["dk"], "dk")
     fine = fine_bound(p, bound["dk"], out)
     holds(np.where(few[:, :, None, None], got, 0), np.where(few[:, :, None, None], want["dk"], 0), fine, "dk of few queries")
+
+
+@pytest.mark.parametrize("case", [
+    dict(B=2, Tq=1, Tk=1500, Hq=8, Hkv=2, D=128, len_k=[1500, 777]),
+    dict(B=1, Tq=1, Tk=700, Hq=8, Hkv=2, D=64, window=129, sinks=3),
+    dict(B=1, Tq=4, Tk=3001, Hq=16, Hkv=2, D=96),
+    dict(B=2, Tq=32, Tk=500, Hq=2, Hkv=2, D=128, len_q=[32, 9], len_k=[499, 64]),
+], ids=["decode", "window", "draft", "rows"])
+def test_few_rows_keep_sixteen_bits_of_p(case):
+    p = Problem(seed=32, **case)
+    u, (q, k, v, _) = U["bf16"], p.x
+    less = np.zeros(q.shape)
+    for b, (lq, lk) in enumerate(zip(p.lq, p.lk)):
+        see = A.visible(lq, lk, p.window, p.sinks)
+        for h, hk in A.heads(q.shape[2], k.shape[2]):
+            P, _, _ = A.probabilities(q[b, :lq, h], k[b, :lk, hk], p.scale, see)
+            less[b, :lq, h] = (u - u * u) * (P @ np.abs(v[b, :lk, hk]))
+    want, bound = p.exact()
+    p.fwd(weight=False)
+    plain = np64(p.out).copy()
+    p.fwd()
+    for got in (plain, np64(p.out)):
+        holds(got, want["out"], bound["out"] - 1.1 * less, "out")
