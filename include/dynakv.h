@@ -192,6 +192,8 @@ LMHEAD_API int dynakv_check(void* ws, void* stream);
  *  - Logits, softmax and all sums are fp32.  With bf16 storage P, and in the backward dS, are rounded to bf16 before they
  *    enter a matrix product, as are the outputs.  Sixteen bits of P enter out where a key head has up to 32 rows (queries times
  *    heads) over keys in bf16, and sixteen of dS enter dq, and dk of keys that few queries see.
+ *  - Logits of up to 2^30 either way are told apart as fp32 tells them.  lse is fp32 too: P that is recomputed from it (the backward, and
+ *    weights of more than 8 rows of a key head) is off by |lse| 2^-24 besides, relative to itself.
  */
 
 /* Where element (sequence b, slot t, head h, c) lies: b * seq + t * slot + h * head + c, in elements.  Each stride is a
@@ -219,7 +221,8 @@ typedef struct attn_desc {
 /* LMHEAD_OK or the code that the calls below would return for this descriptor.  Host-only. */
 LMHEAD_API int attn_validate_desc(const attn_desc* desc);
 
-/* Scratch bytes of attn_fwd, kv4_store and kv4_attn; 0 if the descriptor is invalid.  Host-only. */
+/* Scratch bytes of attn_fwd, kv4_store and kv4_attn; 0 if the descriptor is invalid.  Up to 8 rows of a key head (queries times the heads that read it)
+ * have four bytes for each row and key among them, for the logits that `weight` is added up from, whether a call asks for it or not.  Host-only. */
 LMHEAD_API size_t attn_workspace_bytes(const attn_desc* desc);
 
 /*

@@ -14,7 +14,7 @@ import math
 import torch
 
 from .binding import LmheadError, _check, load_library
-from .train import _CODES, _DTYPES, _TORCH, _arg, _bad, _device, _refuse, _stream
+from .train import _DTYPES, _TORCH, _arg, _bad, _device, _refuse, _stream
 
 EVICT_PLANES = 4
 

@@ -125,7 +125,7 @@ constexpr bool kRowsInLds = AttnElem<E>::size == 2;
 // either, 2.4e-3 with the first, 1.7e-3 with both; the rounding of dq itself is 1.7e-3.
 //
 // Five products of a pair, bound by them and the exponentials.  Eight sequences of 1024 to 4096 under a window of 1024, 28 and 4 heads of 128:
-// 620 to 710 us.
+// 680 to 780 us, matrix cores busy 49 % of the time.
 template <typename E, int DP, int BK>
 __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dq_kernel(AttnArgs a, int nkey) {
   using El = AttnElem<E>;
@@ -271,7 +271,11 @@ __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dq_kernel(Att
 // A wavefront holds 32 keys and their values; the workgroup's four walk the queries that see them, head by head, in tiles of 32.  S and dP
 // have the queries along the accumulators' rows, so P and dS are operands of dV^T = g^T P and dK^T = Q^T dS as they lie.
 //
-// Four products of a pair, bound by reads of LDS beside them (q and g are read along rows and across).  The sequences above: 670 to 740 us.
+// P in dv, and dS in dk of many queries, are single bf16 numbers: a second part of each would be two products more beside the four, and the outputs of
+// the step below are 2.3e-3 off together, where their own roundings leave 1.7e-3.
+//
+// Four products of a pair (five where few queries see the keys, see kFineQueries), bound by reads of LDS beside them (q and g are read along rows and
+// across).  The sequences above: 720 to 940 us (2 to 4 % of the backward less with four throughout).
 // (64 keys a wavefront, which halves those reads, takes 512 registers and one wavefront a unit, and was slower by a tenth.)
 template <typename E, int DP>
 __global__ __launch_bounds__(256, kRowsInLds<E> ? 2 : 1) void attn_dkv_kernel(AttnArgs a, KeyShares sh) {

@@ -46,10 +46,13 @@ __device__ inline void load_cache(char* lds, const uint8_t* codes, const uint8_t
 // they see in tiles of BK: S^T = K Q^T with the keys along the accumulators' rows, so that a lane holds one query's logits and the
 // softmax needs one exchange between lane halves; the exponentials are the second operand of O^T = V^T P^T as they lie.
 //
-// Bound by the matrix cores and the exponentials, whose instructions overlap only so far (matrix cores busy 55 % of the time, the other units
-// 52 %, both at once 20 %).  32 and 8 heads of 128, 4 sequences of 4096: 525 to 555 us as the clocks allow, 1.0 PFLOP/s over the pairs that are
-// seen; 8 of 512 to 2048: 151 us (263 with a key head's workgroups on all XCDs, 160 with the order of steps that the compiler chose, 158 with
-// rows stored as they lie); 40 and 8 heads, 4 of 1024 to 8192 under a window of 1024: 400 to 520 us, by the lengths.
+// P is rounded to bf16 for its product, which leaves out of 8 x 2048 2.1e-3 off (relative to 64 bits; its own rounding alone 1.6e-3): a second
+// part would be a product more beside the two.
+//
+// Bound by the matrix cores and the exponentials, whose instructions overlap only so far.  32 and 8 heads of 128, 4 sequences of 4096: 525 to 580 us
+// as the clocks allow, 0.95 to 1.05 PFLOP/s over the pairs that are seen, matrix cores busy 60 % of the time and vector units 58 %; 8 of 512 to
+// 2048: 145 to 195 us, by the lengths, 36 % and 50 % (of one draw 151, 263 with a key head's workgroups on all XCDs, 160 with the order of steps
+// that the compiler chose, 158 with rows stored as they lie); 40 and 8 heads, 4 of 1024 to 8192 under a window of 1024: 400 to 720 us, by the lengths.
 // The grid is a workgroup for 128 rows, the last ones (which see most) first; where that leaves compute units idle the keys are cut.
 template <typename E, int DP, int NW, int BK, bool kCache>
 __global__ __launch_bounds__(NW * 64, AttnElem<E>::size == 2 || DP == 64 ? 2 : 1) void attn_fwd_kernel(AttnArgs a) {
@@ -522,7 +525,7 @@ hipError_t fwd(const AttnArgs& a, hipStream_t s) {
 }
 
 template <typename E, int DP, bool kCache>
-hipError_t fwd_rows(const AttnPlan& p, const AttnArgs& a, hipStream_t s) {
+hipError_t fwd_rows(const AttnArgs& a, hipStream_t s) {
   constexpr int BK = AttnElem<E>::size == 2 ? 64 : 32;
   return fwd<E, DP, 4, BK, kCache>(a, s);
 }
@@ -548,11 +551,11 @@ hipError_t weight(const attn_desc* d, const AttnPlan& p, const AttnArgs& a, hipS
 hipError_t launch_attn_fwd(const attn_desc* d, const AttnPlan& p, AttnArgs& a, hipStream_t s) {
   const bool c = a.k_codes != nullptr;
   if (d->dtype == LMHEAD_BF16) {
-    if (p.DP == 64) return c ? fwd_rows<bf16_tag, 64, true>(p, a, s) : fwd_rows<bf16_tag, 64, false>(p, a, s);
-    return c ? fwd_rows<bf16_tag, 128, true>(p, a, s) : fwd_rows<bf16_tag, 128, false>(p, a, s);
+    if (p.DP == 64) return c ? fwd_rows<bf16_tag, 64, true>(a, s) : fwd_rows<bf16_tag, 64, false>(a, s);
+    return c ? fwd_rows<bf16_tag, 128, true>(a, s) : fwd_rows<bf16_tag, 128, false>(a, s);
   }
-  if (p.DP == 64) return c ? fwd_rows<f32_tag, 64, true>(p, a, s) : fwd_rows<f32_tag, 64, false>(p, a, s);
-  return c ? fwd_rows<f32_tag, 128, true>(p, a, s) : fwd_rows<f32_tag, 128, false>(p, a, s);
+  if (p.DP == 64) return c ? fwd_rows<f32_tag, 64, true>(a, s) : fwd_rows<f32_tag, 64, false>(a, s);
+  return c ? fwd_rows<f32_tag, 128, true>(a, s) : fwd_rows<f32_tag, 128, false>(a, s);
 }
 
 hipError_t launch_attn_weight(const attn_desc* d, const AttnPlan& p, AttnArgs& a, hipStream_t s) {
