@@ -121,3 +121,39 @@ def test_a_key_or_value_reaches_queries_127_positions_from_those_that_see_it(cas
     want, bound = p.exact()      # of the inputs without the bad one
     for x in (lse, clean[2]):
         holds(np64(x)[0, heads][:, ~sees], want["lse"][0, heads][:, ~sees], bound["lse"][0, heads][:, ~sees], "lse")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Tq,Hq", [(1, 2), (12, 2), (200, 2)], ids=["few", "rows", "prompt"])
+def test_logits_of_two_to_the_30(dtype, Tq, Hq):
+    """Logits of -2^30 to 2^30 in steps of 2^29: the keys with a query's largest one share its weight equally, whatever the fused product leaves of
+    numbers of that size (they leave the same of equal logits).  Values are whole numbers: their mean over up to Tk keys is off by its roundings."""
+    import torch
+    import paper_2603_04411_amd as L
+    Tk, D, tdt = 300, 64, torch.bfloat16 if dtype == "bf16" else torch.float32
+    rng = np.random.default_rng(55)
+    c = rng.integers(-2, 3, Tk).astype(np.float64)
+    c[0] = -2.0      # the first queries see no large one
+    sign = rng.choice([-1.0, 1.0], (1, Tq, Hq))
+    q, k = np.zeros((1, Tq, Hq, D)), np.zeros((1, Tk, 1, D))
+    q[..., 3], k[0, :, 0, 3] = sign * 2.0 ** 15, c * 2.0 ** 14
+    v = rng.integers(-8, 9, (1, Tk, 1, D)).astype(np.float64)
+    dq, dk, dv = (torch.from_numpy(x).to(tdt).cuda() for x in (q, k, v))
+    d = L.make_attn_desc(1, Tq, Tk, Hq, 1, D, dtype, scale=1.0)
+    out, lse = torch.empty_like(dq), torch.empty(1, Hq, Tq, device="cuda")
+    weight = torch.zeros(1, 1, Tk, device="cuda") if Tq * Hq <= 8 else None      # of more rows P comes from lse, which has steps of 64 here
+    ws = torch.empty(L.attn_workspace_bytes(d), dtype=torch.uint8, device="cuda")
+    L.attn_fwd(d, dq, dk, dv, None, None, out, lse, weight, 0.0, ws)
+    u, total = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}[dtype], np.zeros(Tk)
+    for i in range(Tq):
+        for h in range(Hq):
+            seen = Tk - Tq + i + 1
+            z = sign[0, i, h] * c[:seen]
+            top = np.flatnonzero(z == z.max())
+            total[top] += 1.0 / len(top)
+            want = v[0, top, 0].mean(0)
+            bound = 1.1 * (u * (np.abs(v[0, top, 0]).mean(0) + np.abs(want)) + 2 * (seen + 8) * 2.0 ** -24 * 8)
+            holds(np64(out)[0, i, h], want, bound + 1e-30, "out")
+            holds(np64(lse)[0, h, i:i + 1], np.array([z.max() * 2.0 ** 29]), np.array([2.0 ** 6 + 8.0]), "lse")
+    if weight is not None:
+        holds(np64(weight)[0, 0], total, 1.1 * (Tk + 16) * 2.0 ** -24 * total + 1e-30, "weight")

@@ -45,6 +45,15 @@ def test_more_blocks_of_keys_than_workgroups(case):
     check_bwd(Problem(seed=42, **case))
 
 
+@pytest.mark.parametrize("case", [dict(B=2, Tq=50, Tk=80, Hq=4, Hkv=2, D=64, len_q=[0, 0], len_k=[0, 0]),
+                                  dict(B=2, Tq=200, Tk=300, Hq=4, Hkv=2, D=128, len_q=[0, 200], len_k=[0, 0], window=3, sinks=2),
+                                  dict(B=1, Tq=700, Tk=700, Hq=2, Hkv=1, D=64, len_q=[0], len_k=[700], dtype="f32")], ids=range(3))
+def test_batches_without_a_single_pair(case):
+    p = Problem(seed=45, **case)
+    check_fwd(p)
+    check_bwd(p)
+
+
 LARGE = [
     dict(B=8, Tq=260, Tk=260, Hq=64, Hkv=8, D=128, window=200, sinks=3, len_q=_lengths(8, 260, 4), len_k=_lengths(8, 260, 4)),
     dict(B=9, Tq=260, Tk=300, Hq=64, Hkv=8, D=120, first="wide"),
