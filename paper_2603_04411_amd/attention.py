@@ -24,6 +24,7 @@ class AttnLayout(C.Structure):
 
 
 class AttnDesc(C.Structure):
+    _sizes = None
     _fields_ = [
         ("B", C.c_int32), ("Tq", C.c_int32), ("Tk", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32),
         ("window", C.c_int32), ("sinks", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float), ("flags", C.c_uint32),
@@ -164,12 +165,13 @@ class _Sizes:
         self.lse, self.weight, self.codes, self.scales = B * Hq * Tq, rows, rows * (D // 2), rows * (D // 32)
         self.lse_shape, self.weight_shape = torch.Size((B, Hq, Tq)), torch.Size((B, Hkv, Tk))
         self.codes_shape, self.scales_shape = torch.Size((B, Hkv, Tk, D // 2)), torch.Size((B, Hkv, Tk, D // 32))
+        self.odd = D % 32 != 0      # no cache in 4 bits has such rows, and the library refuses them
 
 
 def _sizes(desc, where):
     """The descriptor's own refusal comes first: the checks of tensors rely on its sizes."""
     raw = bytes(desc)
-    sizes = desc.__dict__.get("_sizes")
+    sizes = desc._sizes
     if sizes is None or sizes.raw != raw:
         sizes = desc._sizes = _Sizes(desc, raw)
     if sizes.status:
@@ -181,9 +183,10 @@ def _heads(t, name, s, want, device):
     """Device pointer of a [B, T, H, D] tensor with the shape and strides that are wanted (it may have more of each), or of a dense buffer where
     they are dense."""
     if t.dtype is s.dtype and t.get_device() == device:
-        n, st = t.shape, t.stride()
+        n = t.shape
         if want.dense and t.is_contiguous() and (n == want.shape or t.numel() == want.n and _merges(n, want.shape)):
             return t.data_ptr()
+        st = t.stride()
         if n == want.shape and st == want.strides:
             return t.data_ptr()
         if len(n) == 4 and all(a >= b for a, b in zip(n, want.shape)) and all(a == b or c == 1 for a, b, c in zip(st, want.strides, want.shape)):
@@ -215,13 +218,6 @@ def attn_bwd(desc, q, k, v, len_q, len_k, out, lse, g_out, dq, dk, dv, ws) -> No
 # ---- the cache in 4 bits --------------------------------------------------------------------------------------------
 
 
-def _sizes4(desc, where):
-    s = _sizes(desc, where)
-    if desc.D % 32:      # what the library says of such a descriptor; there are no sizes to check tensors against
-        raise LmheadError(-2, where)
-    return s
-
-
 def _cache(s, k_codes, k_scales, v_codes, v_scales, dev):
     u8 = torch.uint8
     return (_block(k_codes, "k_codes", u8, s.codes, s.codes_shape, dev), _block(k_scales, "k_scales", u8, s.scales, s.scales_shape, dev),
@@ -230,7 +226,9 @@ def _cache(s, k_codes, k_scales, v_codes, v_scales, dev):
 
 def kv4_store(desc, k, v, len_q, len_k, k_codes, k_scales, v_codes, v_scales, ws) -> None:
     """k, v: the new tokens' rows, [B, Tq, Hkv, D]."""
-    s, dev, i32 = _sizes4(desc, "kv4_store"), _device(), torch.int32
+    s, dev, i32 = _sizes(desc, "kv4_store"), _device(), torch.int32
+    if s.odd:
+        raise LmheadError(-2, "kv4_store")
     rc = _lib().kv4_store(
         C.byref(desc), _heads(k, "k", s, s.k_new, dev), _heads(v, "v", s, s.v_new, dev), _arg(len_q, "len_q", i32, s.B, dev),
         _arg(len_k, "len_k", i32, s.B, dev), *_cache(s, k_codes, k_scales, v_codes, v_scales, dev), _arg(ws, "ws", torch.uint8, 0, dev),
@@ -239,7 +237,9 @@ def kv4_store(desc, k, v, len_q, len_k, k_codes, k_scales, v_codes, v_scales, ws
 
 
 def kv4_attn(desc, q, k_codes, k_scales, v_codes, v_scales, len_q, len_k, out, lse, weight, decay, ws) -> None:
-    s, dev, i32, f32 = _sizes4(desc, "kv4_attn"), _device(), torch.int32, torch.float32
+    s, dev, i32, f32 = _sizes(desc, "kv4_attn"), _device(), torch.int32, torch.float32
+    if s.odd:
+        raise LmheadError(-2, "kv4_attn")
     rc = _lib().kv4_attn(
         C.byref(desc), _heads(q, "q", s, s.q, dev), *_cache(s, k_codes, k_scales, v_codes, v_scales, dev), _arg(len_q, "len_q", i32, s.B, dev),
         _arg(len_k, "len_k", i32, s.B, dev), _heads(out, "out", s, s.o, dev), _block(lse, "lse", f32, s.lse, s.lse_shape, dev),
