@@ -124,13 +124,16 @@ def _merges(n, want):
 
 
 def _block(t, name, dtype, n, want, device):
-    """Device pointer of a dense tensor of the sizes `want`, `n` elements, of one that has more where that moves nothing of what is used (more sequences do not,
-    more slots would move every head but the first), or of a flat buffer with room for them; None for None."""
+    """Device pointer of a dense tensor of the sizes `want` (`n` elements), of one that has more where that moves nothing of what is used (more sequences
+    do not, more slots would move every head but the first), or of a flat buffer with room for them; None for None."""
     if t is None:
         return None
     if t.dtype is dtype and t.get_device() == device and t.is_contiguous():
         sizes = t.shape
-        if sizes == want or len(sizes) == 1 and sizes[0] >= n or t.numel() == n and _merges(sizes, want):
+        if sizes == want:
+            return t.data_ptr()
+        inner = min(len(sizes), len(want)) - 1      # dimensions behind the first one, which may be larger
+        if t.numel() >= n and inner >= 0 and sizes[len(sizes) - inner:] == want[len(want) - inner:] or t.numel() == n and _merges(sizes, want):
             return t.data_ptr()
         if (len(sizes) == len(want) and all(a >= b for a, b in zip(sizes, want))
                 and all(a == math.prod(want[i + 1:]) or want[i] == 1 for i, a in enumerate(t.stride()))):

@@ -69,8 +69,8 @@ def test_a_copied_descriptor_is_the_one_that_is_passed(calls, copied):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("B,Tq,Tk,Hq,Hkv", [(1, 1 << 20, 33280, 1024, 1), (1, 1 << 20, 65000, 1024, 1), (1, 1 << 20, 16384, 1024, 1), (2, 1 << 20, 12800, 1024, 2),
-                                            (1, 1 << 20, 25600, 1024, 1), (3, 4096, 4096, 28, 4), (1, 1, 1, 1, 1), (1, 1 << 20, 1 << 25, 1, 1)])
+@pytest.mark.parametrize("B,Tq,Tk,Hq,Hkv", [(1, 1 << 20, 33280, 1024, 1), (1, 1 << 20, 65000, 1024, 1), (1, 1 << 20, 16384, 1024, 1),
+                                            (2, 1 << 20, 12800, 1024, 2), (1, 1 << 20, 25600, 1024, 1), (3, 4096, 4096, 28, 4), (1, 1, 1, 1, 1), (1, 1 << 20, 1 << 25, 1, 1)])
 def test_backward_workspaces_of_the_largest_calls(B, Tq, Tk, Hq, Hkv, dtype):
     """What is cut of dk and dv is counted in 64 bits: a call with many tiles and few blocks of keys has as many workgroups as are resident."""
     d = L.make_attn_desc(B, Tq, Tk, Hq, Hkv, 8, dtype)
@@ -117,7 +117,7 @@ def test_tensors_with_more_slots_than_the_descriptor_are_refused(calls):
         assert e.value.code == -2
     # more sequences, flat buffers and merged dimensions mean the same memory
     for weight in (torch.zeros(Bn + 1, Hkv, Tk), torch.zeros(Bn * Hkv * Tk + 5), t.weight.view(Bn * Hkv, Tk), t.weight.view(Bn, Hkv * Tk), t.weight[None],
-                   t.weight.flatten()):
+                   t.weight.flatten(), torch.zeros(Bn * Hkv + 1, Tk), torch.zeros(2, Bn, Hkv, Tk), torch.zeros(3, 1, Bn * Hkv, Tk)[:1]):
         fwd(weight=weight)
         assert calls[-1][2][7] == weight.data_ptr()
     for q in (t.q.view(Bn, Tq, Hq * D), t.q.view(Bn * Tq, Hq, D), t.q.flatten(), t.q.view(1, Bn * Tq, Hq, D), torch.zeros(Bn + 1, Tq, Hq, D, dtype=torch.bfloat16)):
